@@ -358,6 +358,132 @@ const char *psops_last_error(const psops_ctx *ctx);
 /* Waits for the stream, then frees the context (not the caller's buffers). */
 int psops_destroy(psops_ctx *ctx);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Operators of the training steps between two synchronisations
+ *
+ * A worker's local step needs the loss of its model (which at a sync point is
+ * also the particle's fitness), the gradients, and an optimiser step.  The
+ * operators below keep the conventions above: error codes, no device memory of
+ * their own, a caller-owned 256-byte aligned workspace, work enqueued on the
+ * stream given at creation, a context bound to the GPU current at creation and
+ * used by one host thread at a time.  All of them are deterministic: the same
+ * inputs give the same bits.
+ * ---------------------------------------------------------------------------
+ */
+
+/* element types */
+#define PSOPS_NONE       0
+#define PSOPS_F32        1
+#define PSOPS_F16        2
+#define PSOPS_BF16       3
+
+/*
+ * AdamW over many tensors in one launch.  Per element, with t the number of
+ * the step (the first one after steps_done earlier steps is steps_done + 1):
+ *   g  = grad * scale
+ *   m' = m * beta1 + g * (1 - beta1)
+ *   v' = v * beta2 + (g * g) * (1 - beta2)
+ *   p' = p * (1 - lr * weight_decay)
+ *        - (m' * (lr / (1 - beta1^t))) / (sqrt(v') * (1 / sqrt(1 - beta2^t)) + eps)
+ * The factors in brackets are formed in double and rounded to fp32 once; every
+ * operation on an element is fp32 round-to-nearest in the order written, each
+ * product and sum rounded by itself (no fused multiply-add, correctly rounded
+ * division and square root).
+ *
+ * state_bits 32: m and v are fp32.
+ * state_bits 8: what is kept is m and the root r = sqrt(v) as 8-bit e4m3
+ * numbers (no infinities, largest 448), with one fp32 scale for every 256
+ * consecutive elements of a tensor (the last block of a tensor may be short):
+ * value = number * scale, v = r * r.  The step itself uses the unrounded m'
+ * and v'; then, per block with top = the largest magnitude,
+ *   scale = top / 448,  number = round_to_nearest_even(value * (448 / top)),
+ * a block with top < 2^-100 is kept as zeros with scale 0, and a root that is
+ * not zero is never kept as zero (it becomes the smallest number), so that a
+ * nonzero m never meets a vanished r.  Keeping the root halves the range that
+ * 8 bits have to span.  A NaN or infinity in a gradient spoils its block.
+ */
+typedef struct {
+    double   beta1, beta2;   /* in [0, 1)                                              */
+    double   eps;            /* >= 0                                                   */
+    int64_t  steps_done;     /* steps already taken (0 for a new run, t at resume)     */
+    int32_t  state_bits;     /* 32 or 8                                                */
+    int32_t  grad_type;      /* PSOPS_F32, PSOPS_F16, PSOPS_BF16                       */
+    int32_t  copy_type;      /* PSOPS_NONE, PSOPS_F16, PSOPS_BF16: type of the copies  */
+    int32_t  n_tensors;      /* >= 1                                                   */
+} psops_adamw_config;
+
+/* One parameter tensor: contiguous device arrays of n elements each. */
+typedef struct {
+    float   *p;              /* fp32 weights, e.g. a piece of a swarm's row            */
+    const void *g;           /* gradient, grad_type                                    */
+    void    *copy;           /* NULL, or n elements of copy_type that receive p'
+                                (round to nearest): the weights a 16-bit model reads   */
+    void    *m, *v;          /* fp32 m and v; or 8-bit m and r                         */
+    float   *m_scale, *v_scale; /* 8 bits only: ceil(n / 256) fp32 scales each         */
+    int64_t  n;              /* >= 0                                                   */
+    double   weight_decay;
+} psops_adamw_tensor;
+
+typedef struct psops_adamw psops_adamw;  /* opaque */
+
+/* Workspace for these tensors (only n is looked at); 0 if an argument is invalid. */
+size_t psops_adamw_workspace_bytes(const psops_adamw_config *cfg, const psops_adamw_tensor *tensors);
+
+/*
+ * Adopts the caller's arrays (borrowed until psops_adamw_destroy; the list
+ * itself is copied).  Tensors must not overlap.  Where all arrays of a tensor
+ * lie alike within 8 elements (any view into flat buffers that are laid out the
+ * same), whole groups of 8 elements move in one access; otherwise single
+ * elements do, with the same results.
+ * Errors: EINVAL, EALIGN (an array not aligned to its element), EWORKSPACE,
+ * ENOMEM, ECUDA.  On error *out is NULL.
+ */
+int psops_adamw_create(psops_adamw **out, const psops_adamw_config *cfg, const psops_adamw_tensor *tensors,
+                       void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* New gradient addresses, one per tensor (a framework that allocates gradients
+ * anew for each step).  Enqueued on the stream: steps already enqueued keep the
+ * old ones.  Not inside a stream capture.  EINVAL, EALIGN, ECUDA. */
+int psops_adamw_set_grads(psops_adamw *opt, const void *const *grads);
+
+/*
+ * One step.  d_scale: NULL (scale 1) or a device float that every gradient is
+ * multiplied by (1 / loss scale, the clipping factor of psops_gradnorm, or
+ * their product).  If *d_scale is not finite the step leaves everything as it
+ * is and t does not advance.  t and the powers of beta live in device memory
+ * and are advanced by the step itself, so a captured step can be replayed from
+ * a CUDA graph (with the lr of the capture).
+ * Errors: EINVAL (lr not finite), EALIGN, ECUDA.
+ */
+int psops_adamw_step(psops_adamw *opt, double lr, const float *d_scale);
+
+/* t, read from the device (waits for the stream). */
+int psops_adamw_steps(psops_adamw *opt, int64_t *steps);
+
+int64_t psops_adamw_launch_count(const psops_adamw *opt);
+const char *psops_adamw_last_error(const psops_adamw *opt);
+int psops_adamw_destroy(psops_adamw *opt);   /* waits for the stream; frees nothing of the caller's */
+
+/*
+ * The 2-norm of many gradient tensors together and the factor that clips it:
+ *   d_out[0] = norm = sqrt(sum of all squares)
+ *   d_out[1] = min(1, max_norm / (norm + 1e-6)), or NaN if the norm is not
+ *              finite (psops_adamw_step then skips the step)
+ * Squares are fp32, eight of them (sixteen for 16-bit types) are added in fp32,
+ * everything beyond in double, in a fixed order.  max_norm may be +inf (factor 1).
+ * n[i] >= 0 elements at grads[i], contiguous.
+ */
+typedef struct psops_gradnorm psops_gradnorm;  /* opaque */
+size_t psops_gradnorm_workspace_bytes(int32_t n_tensors, const int64_t *n);
+int psops_gradnorm_create(psops_gradnorm **out, int32_t n_tensors, const void *const *grads, const int64_t *n,
+                          int32_t grad_type, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
+int psops_gradnorm_set_grads(psops_gradnorm *gn, const void *const *grads);
+int psops_gradnorm_run(psops_gradnorm *gn, float max_norm, float *d_out);
+int64_t psops_gradnorm_launch_count(const psops_gradnorm *gn);
+const char *psops_gradnorm_last_error(const psops_gradnorm *gn);
+int psops_gradnorm_destroy(psops_gradnorm *gn);
+
 #ifdef __cplusplus
 }
 #endif

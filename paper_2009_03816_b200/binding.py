@@ -23,6 +23,7 @@ PSOPS_STATIC_SCRATCH_DOUBLES = 1 << 20
 PSOPS_MAX_K = 1024
 PSOPS_KEEP_GBEST, PSOPS_QUADRATIC, PSOPS_GBEST_HISTORY, PSOPS_SEPARATE_SELECT = 1, 2, 4, 8
 PSOPS_X, PSOPS_V, PSOPS_PBEST, PSOPS_GBEST = 0, 1, 2, 3
+PSOPS_NONE, PSOPS_F32, PSOPS_F16, PSOPS_BF16 = 0, 1, 2, 3
 
 EXPORTS = [
     "psops_workspace_bytes", "psops_create", "psops_set_losses", "psops_sync",
@@ -33,6 +34,10 @@ EXPORTS = [
     "psops_quadratic_fitness_static", "psops_shard_select", "psops_shard_update",
     "psops_shard_update_range", "psops_get_history", "psops_set_history", "psops_ssgd",
     "psops_host_register", "psops_host_unregister",
+    "psops_adamw_workspace_bytes", "psops_adamw_create", "psops_adamw_set_grads", "psops_adamw_step",
+    "psops_adamw_steps", "psops_adamw_launch_count", "psops_adamw_last_error", "psops_adamw_destroy",
+    "psops_gradnorm_workspace_bytes", "psops_gradnorm_create", "psops_gradnorm_set_grads", "psops_gradnorm_run",
+    "psops_gradnorm_launch_count", "psops_gradnorm_last_error", "psops_gradnorm_destroy",
 ]
 
 
@@ -41,6 +46,18 @@ class psops_config(ctypes.Structure):
                 ("ld", ctypes.c_int64), ("m_max", ctypes.c_float), ("m_min", ctypes.c_float),
                 ("t_max", ctypes.c_int64), ("c1", ctypes.c_float), ("c2", ctypes.c_float),
                 ("seed", ctypes.c_uint64), ("flags", ctypes.c_uint32), ("K_total", ctypes.c_int32)]
+
+
+class psops_adamw_config(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("steps_done", ctypes.c_int64), ("state_bits", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+                ("copy_type", ctypes.c_int32), ("n_tensors", ctypes.c_int32)]
+
+
+class psops_adamw_tensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("weight_decay", ctypes.c_double)]
 
 
 class PsopsError(RuntimeError):
@@ -68,6 +85,7 @@ def load() -> ctypes.CDLL:
             "There is no CPU fallback.")
     lib = ctypes.CDLL(LIBRARY)
     cfgp = ctypes.POINTER(psops_config)
+    acfgp, atensp = ctypes.POINTER(psops_adamw_config), ctypes.POINTER(psops_adamw_tensor)
     sig = {
         "psops_workspace_bytes": (ctypes.c_size_t, [cfgp]),
         "psops_create": (ctypes.c_int, [ctypes.POINTER(_vp), cfgp, _f32p, _f32p, _f32p, _vp,
@@ -101,6 +119,23 @@ def load() -> ctypes.CDLL:
         "psops_host_unregister": (ctypes.c_int, [_vp]),
         "psops_quadratic_fitness_static": (ctypes.c_int, [_f32p, ctypes.c_int64, ctypes.c_int32,
                                                           ctypes.c_int64, _f32p, _f32p, _f32p, _vp]),
+        "psops_adamw_workspace_bytes": (ctypes.c_size_t, [acfgp, atensp]),
+        "psops_adamw_create": (ctypes.c_int, [ctypes.POINTER(_vp), acfgp, atensp, _vp, ctypes.c_size_t, _vp]),
+        "psops_adamw_set_grads": (ctypes.c_int, [_vp, ctypes.POINTER(_vp)]),
+        "psops_adamw_step": (ctypes.c_int, [_vp, ctypes.c_double, _f32p]),
+        "psops_adamw_steps": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_int64)]),
+        "psops_adamw_launch_count": (ctypes.c_int64, [_vp]),
+        "psops_adamw_last_error": (ctypes.c_char_p, [_vp]),
+        "psops_adamw_destroy": (ctypes.c_int, [_vp]),
+        "psops_gradnorm_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32, ctypes.POINTER(ctypes.c_int64)]),
+        "psops_gradnorm_create": (ctypes.c_int, [ctypes.POINTER(_vp), ctypes.c_int32, ctypes.POINTER(_vp),
+                                                 ctypes.POINTER(ctypes.c_int64), ctypes.c_int32, _vp,
+                                                 ctypes.c_size_t, _vp]),
+        "psops_gradnorm_set_grads": (ctypes.c_int, [_vp, ctypes.POINTER(_vp)]),
+        "psops_gradnorm_run": (ctypes.c_int, [_vp, ctypes.c_float, _f32p]),
+        "psops_gradnorm_launch_count": (ctypes.c_int64, [_vp]),
+        "psops_gradnorm_last_error": (ctypes.c_char_p, [_vp]),
+        "psops_gradnorm_destroy": (ctypes.c_int, [_vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)            # AttributeError if a symbol is missing
@@ -116,11 +151,11 @@ def _strerror(code: int) -> str:
         return "error"
 
 
-def _check(rc: int, where: str, ctx=None) -> None:
+def _check(rc: int, where: str, ctx=None, last_error="psops_last_error") -> None:
     if rc != PSOPS_OK:
         detail = ""
         if ctx is not None and rc == PSOPS_ECUDA:
-            detail = load().psops_last_error(ctx).decode()
+            detail = getattr(load(), last_error)(ctx).decode()
         raise PsopsError(rc, where, detail)
 
 
@@ -287,6 +322,83 @@ def psops_quadratic_fitness_static(d_x, ld, K, N, d_dvec, d_tvec, d_loss, stream
                                                  _ptr(d_tvec), _ptr(d_loss),
                                                  int(stream) if stream else None),
            "psops_quadratic_fitness_static")
+
+
+# ---- operators of the training steps ---------------------------------------
+
+def _addresses(buffers):
+    return (_vp * len(buffers))(*[_ptr(b) or None for b in buffers])
+
+
+def psops_adamw_workspace_bytes(cfg: psops_adamw_config, tensors) -> int:
+    return int(load().psops_adamw_workspace_bytes(ctypes.byref(cfg), tensors))
+
+
+def psops_adamw_create(cfg, tensors, d_workspace, workspace_bytes=None, stream=None):
+    """`tensors`: a ctypes array of psops_adamw_tensor, cfg.n_tensors of them."""
+    handle = _vp()
+    if workspace_bytes is None:
+        workspace_bytes = d_workspace.numel() * d_workspace.element_size() if d_workspace is not None else 0
+    rc = load().psops_adamw_create(ctypes.byref(handle), ctypes.byref(cfg), tensors, _ptr(d_workspace),
+                                   int(workspace_bytes), int(stream) if stream else None)
+    _check(rc, "psops_adamw_create")
+    return handle
+
+
+def psops_adamw_set_grads(opt, grads) -> None:
+    _check(load().psops_adamw_set_grads(opt, _addresses(grads)), "psops_adamw_set_grads", opt,
+           "psops_adamw_last_error")
+
+
+def psops_adamw_step(opt, lr: float, d_scale=None) -> None:
+    _check(load().psops_adamw_step(opt, float(lr), _ptr(d_scale)), "psops_adamw_step", opt, "psops_adamw_last_error")
+
+
+def psops_adamw_steps(opt) -> int:
+    steps = ctypes.c_int64(0)
+    _check(load().psops_adamw_steps(opt, ctypes.byref(steps)), "psops_adamw_steps", opt, "psops_adamw_last_error")
+    return int(steps.value)
+
+
+def psops_adamw_launch_count(opt) -> int:
+    return int(load().psops_adamw_launch_count(opt))
+
+
+def psops_adamw_destroy(opt) -> None:
+    _check(load().psops_adamw_destroy(opt), "psops_adamw_destroy")
+
+
+def psops_gradnorm_workspace_bytes(sizes) -> int:
+    return int(load().psops_gradnorm_workspace_bytes(len(sizes), (ctypes.c_int64 * len(sizes))(*sizes)))
+
+
+def psops_gradnorm_create(grads, sizes, grad_type, d_workspace, workspace_bytes=None, stream=None):
+    handle = _vp()
+    if workspace_bytes is None:
+        workspace_bytes = d_workspace.numel() * d_workspace.element_size() if d_workspace is not None else 0
+    rc = load().psops_gradnorm_create(ctypes.byref(handle), len(sizes), _addresses(grads),
+                                      (ctypes.c_int64 * len(sizes))(*sizes), int(grad_type), _ptr(d_workspace),
+                                      int(workspace_bytes), int(stream) if stream else None)
+    _check(rc, "psops_gradnorm_create")
+    return handle
+
+
+def psops_gradnorm_set_grads(gn, grads) -> None:
+    _check(load().psops_gradnorm_set_grads(gn, _addresses(grads)), "psops_gradnorm_set_grads", gn,
+           "psops_gradnorm_last_error")
+
+
+def psops_gradnorm_run(gn, max_norm: float, d_out) -> None:
+    _check(load().psops_gradnorm_run(gn, float(max_norm), _ptr(d_out)), "psops_gradnorm_run", gn,
+           "psops_gradnorm_last_error")
+
+
+def psops_gradnorm_launch_count(gn) -> int:
+    return int(load().psops_gradnorm_launch_count(gn))
+
+
+def psops_gradnorm_destroy(gn) -> None:
+    _check(load().psops_gradnorm_destroy(gn), "psops_gradnorm_destroy")
 
 
 # ---- convenience holder of the tensors a context borrows ------------------

@@ -1,0 +1,98 @@
+// psops_host.cuh -- host-side helpers shared by the training operators' C entries.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+#include <cstdio>
+
+namespace psops_host {
+
+inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// What every training-operator context has: its GPU, its stream, its launch
+// count and the text of the last CUDA error.
+struct Base {
+    cudaStream_t stream = nullptr;
+    int device = 0;
+    int sms = 0;
+    int64_t launches = 0;
+    char err[256] = {0};
+
+    int fail(cudaError_t e, const char *what)
+    {
+        std::snprintf(err, sizeof(err), "%s: %s", what, cudaGetErrorString(e));
+        return PSOPS_ECUDA;
+    }
+    int launched(const char *what)
+    {
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return fail(e, what);
+        launches += 1;
+        return PSOPS_OK;
+    }
+};
+
+// Work of a context belongs to the GPU that was current at its creation; the
+// entry points switch to it for their duration if another one is current.
+class OnDevice {
+public:
+    explicit OnDevice(const Base *b) : previous_(-1)
+    {
+        int now = -1;
+        if (b != nullptr && cudaGetDevice(&now) == cudaSuccess && now != b->device &&
+            cudaSetDevice(b->device) == cudaSuccess)
+            previous_ = now;
+    }
+    ~OnDevice()
+    {
+        if (previous_ >= 0) cudaSetDevice(previous_);
+    }
+    OnDevice(const OnDevice &) = delete;
+    OnDevice &operator=(const OnDevice &) = delete;
+
+private:
+    int previous_;
+};
+
+// Page-locked staging of a small table that is sent to the device again and
+// again: the copy is asynchronous, and the staging is not overwritten before
+// the copy that read it has run.
+class Staging {
+public:
+    ~Staging()
+    {
+        if (event_) cudaEventDestroy(event_);
+        if (host_) cudaFreeHost(host_);
+    }
+    cudaError_t reserve(size_t bytes)
+    {
+        cudaError_t e = cudaHostAlloc(&host_, bytes ? bytes : 1, cudaHostAllocDefault);
+        if (e == cudaSuccess) e = cudaEventCreateWithFlags(&event_, cudaEventDisableTiming);
+        return e;
+    }
+    cudaError_t wait() { return sent_ ? cudaEventSynchronize(event_) : cudaSuccess; }
+    void *host() { return host_; }
+    cudaError_t send(void *dst, size_t bytes, cudaStream_t stream)
+    {
+        cudaError_t e = cudaMemcpyAsync(dst, host_, bytes, cudaMemcpyHostToDevice, stream);
+        if (e == cudaSuccess) e = cudaEventRecord(event_, stream);
+        sent_ = sent_ || e == cudaSuccess;
+        return e;
+    }
+
+private:
+    void *host_ = nullptr;
+    cudaEvent_t event_ = nullptr;
+    bool sent_ = false;
+};
+
+} // namespace psops_host
+
+#define PSOPS_TRY(base, call)                                             \
+    do {                                                                  \
+        const cudaError_t e_ = (call);                                    \
+        if (e_ != cudaSuccess) return (base)->fail(e_, #call);            \
+    } while (0)

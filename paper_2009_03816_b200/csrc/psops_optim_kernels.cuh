@@ -1,0 +1,461 @@
+// psops_optim_kernels.cuh -- AdamW over many tensors and the 2-norm of many
+// gradients (C entries: psops_optim.cu).
+//
+// Both are streaming passes over a list of tensors.  The list lies in device
+// memory as one entry per tensor, and beside it a list of chunks (tensor, index
+// of the chunk within it), so that one launch covers tensors of any size: a
+// block takes chunks c, c + gridDim.x, ...
+//
+// Within a tensor a warp works on 256 consecutive elements at a time, eight per
+// lane.  Where all arrays of a tensor are misaligned alike -- by the same
+// number `lo` < 8 of elements against a group of eight -- their pointers are
+// moved back by lo and the elements are numbered lo .. hi - 1; a group of eight
+// that lies within [lo, hi) then moves in one access of 16 or 32 bytes, and
+// only a tensor's first and last group go element by element.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace {
+
+constexpr int kOptThreads = 256;
+constexpr int kOptWarps = kOptThreads / 32;
+constexpr int kGroup = 256;                     // elements of a warp's step, and of an 8-bit moment's scale
+
+struct AdamwEntry {
+    float *p;
+    const void *g;
+    void *copy, *m, *v;
+    float *m_scale, *v_scale;
+    long long lo, hi;
+    double weight_decay;
+    int vec;                                    // groups of eight are aligned in every array
+    int pad_;
+};
+
+struct AdamwState {
+    double pow1, pow2;                          // beta^t of the steps taken
+    double inv_bias1;                           // 1 / (1 - beta1^(t+1)): the next step's
+    float spread;                               // 1 / sqrt(1 - beta2^(t+1)), rounded
+    unsigned tickets;
+    long long steps;
+};
+
+struct AdamwParams {
+    const AdamwEntry *entries;
+    const uint2 *chunks;                        // {tensor, chunk within it}
+    AdamwState *state;
+    const float *scale;
+    double lr, beta1, beta2;
+    float b1, b1c, b2, b2c, eps;                // beta, 1 - beta
+    unsigned n_chunks;
+};
+
+struct alignas(32) Eight { float x[8]; };
+
+__device__ __forceinline__ void load_eight(const float *p, float (&x)[8])
+{
+    asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+                 : "l"(p));
+}
+__device__ __forceinline__ void store_eight(float *p, const float (&x)[8])
+{
+    asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]),
+                 "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+                 : "memory");
+}
+__device__ __forceinline__ float2 widen(const __half2 h) { return __half22float2(h); }
+__device__ __forceinline__ float2 widen(const __nv_bfloat162 h) { return __bfloat1622float2(h); }
+template <class T2, class T>
+__device__ __forceinline__ void load_eight_16(const T *p, float (&x)[8])
+{
+    const uint4 u = *reinterpret_cast<const uint4 *>(p);
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        T2 h;
+        memcpy(&h, &w[i], 4);
+        const float2 f = widen(h);
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ void load_eight(const __half *p, float (&x)[8]) { load_eight_16<__half2>(p, x); }
+__device__ __forceinline__ void load_eight(const __nv_bfloat16 *p, float (&x)[8]) { load_eight_16<__nv_bfloat162>(p, x); }
+
+__device__ __forceinline__ __half2 narrow2(const __half *, float a, float b) { return __floats2half2_rn(a, b); }
+__device__ __forceinline__ __nv_bfloat162 narrow2(const __nv_bfloat16 *, float a, float b) { return __floats2bfloat162_rn(a, b); }
+template <class T>
+__device__ __forceinline__ void store_eight(T *p, const float (&x)[8])
+{
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const auto h = narrow2((const T *)nullptr, x[2 * i], x[2 * i + 1]);
+        memcpy(&w[i], &h, 4);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ float one_in(const float *p) { return *p; }
+__device__ __forceinline__ float one_in(const __half *p) { return __half2float(*p); }
+__device__ __forceinline__ float one_in(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void one_out(float *p, float x) { *p = x; }
+__device__ __forceinline__ void one_out(__half *p, float x) { *p = __float2half_rn(x); }
+__device__ __forceinline__ void one_out(__nv_bfloat16 *p, float x) { *p = __float2bfloat16_rn(x); }
+
+// 8-bit e4m3 numbers
+struct Q8 { uint8_t b; };
+__device__ __forceinline__ float2 q8_decode2(unsigned short two)
+{
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
+    return __half22float2(__half2(h));
+}
+__device__ __forceinline__ unsigned short q8_encode2(float a, float b)
+{
+    return (unsigned short)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ void load_eight(const Q8 *p, float (&x)[8])
+{
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    const unsigned w[2] = {u.x, u.y};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = q8_decode2((unsigned short)(w[i >> 1] >> (16 * (i & 1))));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ void store_eight(Q8 *p, const float (&x)[8])
+{
+    unsigned w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = (unsigned)q8_encode2(x[4 * i], x[4 * i + 1]) | ((unsigned)q8_encode2(x[4 * i + 2], x[4 * i + 3]) << 16);
+    *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ float one_in(const Q8 *p) { return q8_decode2(p->b).x; }
+__device__ __forceinline__ void one_out(Q8 *p, float x) { p->b = (uint8_t)q8_encode2(x, 0.0f); }
+
+// The eight elements of one lane: consecutive ones from `first` (stride 1), or
+// every 32nd where the arrays of the tensor are not aligned alike.
+struct Lane {
+    long long first;
+    int stride;
+    bool whole;                                 // a full, aligned group of eight
+    unsigned mask;                              // bit j: element first + j * stride exists
+};
+
+__device__ __forceinline__ Lane lane_of(long long group, int lane, bool vec, long long lo, long long hi)
+{
+    Lane L;
+    L.first = vec ? group + lane * 8 : group + lane;
+    L.stride = vec ? 1 : 32;
+    L.mask = 0;
+    if (L.first >= lo && L.first + 7 * L.stride < hi) {
+        L.mask = 0xffu;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const long long i = L.first + j * L.stride;
+            L.mask |= (i >= lo && i < hi) ? 1u << j : 0u;
+        }
+    }
+    L.whole = vec && L.mask == 0xffu;
+    return L;
+}
+
+template <class T>
+__device__ __forceinline__ void load_lane(const T *base, const Lane &L, float (&x)[8])
+{
+    const T *at = base + L.first;
+    if (L.whole) {
+        load_eight(at, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = (L.mask >> j & 1u) ? one_in(at + j * L.stride) : 0.0f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_lane(T *base, const Lane &L, const float (&x)[8])
+{
+    T *at = base + L.first;
+    if (L.whole) {
+        store_eight(at, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (L.mask >> j & 1u) one_out(at + j * L.stride, x[j]);
+    }
+}
+
+// Largest magnitude of a warp's 256 values.  Magnitudes order like their bit
+// patterns, with NaN above everything, so this is an integer maximum.
+__device__ __forceinline__ float top_of(const float (&x)[8])
+{
+    unsigned t = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t = max(t, __float_as_uint(x[j]) & 0x7fffffffu);
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, t));
+}
+
+template <int BITS> struct MomentOf;
+template <> struct MomentOf<32> { using T = float; };
+template <> struct MomentOf<8> { using T = Q8; };
+
+template <int BITS>
+struct AdamwGroup {
+    Lane L;
+    float p[8], g[8], m[8], v[8];
+    float m_scale, v_scale;
+};
+
+template <int BITS, class G>
+__device__ __forceinline__ void adamw_load(const AdamwEntry &E, long long group, int lane, AdamwGroup<BITS> &X)
+{
+    using M = typename MomentOf<BITS>::T;
+    X.L = lane_of(group, lane, E.vec != 0, E.lo, E.hi);
+    load_lane(E.p, X.L, X.p);
+    load_lane((const G *)E.g, X.L, X.g);
+    load_lane((const M *)E.m, X.L, X.m);
+    load_lane((const M *)E.v, X.L, X.v);
+    if (BITS == 8 && group < E.hi) {
+        X.m_scale = E.m_scale[group / kGroup];
+        X.v_scale = E.v_scale[group / kGroup];
+    }
+}
+
+template <int BITS, class C>
+__device__ __forceinline__ void adamw_update(const AdamwEntry &E, long long group, int lane, const AdamwParams &P,
+                                             float scale, float rate, float spread, float decay, AdamwGroup<BITS> &X)
+{
+    using M = typename MomentOf<BITS>::T;
+    float root[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float g = __fmul_rn(X.g[j], scale);
+        float m = X.m[j], v = X.v[j];
+        if (BITS == 8) {
+            m = __fmul_rn(m, X.m_scale);
+            v = __fmul_rn(v, X.v_scale);
+            v = __fmul_rn(v, v);
+        }
+        m = __fadd_rn(__fmul_rn(m, P.b1), __fmul_rn(g, P.b1c));
+        v = __fadd_rn(__fmul_rn(v, P.b2), __fmul_rn(__fmul_rn(g, g), P.b2c));
+        root[j] = __fsqrt_rn(v);
+        const float step = __fdiv_rn(__fmul_rn(m, rate), __fadd_rn(__fmul_rn(root[j], spread), P.eps));
+        X.p[j] = __fsub_rn(__fmul_rn(X.p[j], decay), step);
+        X.m[j] = m;
+        X.v[j] = v;
+    }
+    store_lane(E.p, X.L, X.p);
+    if (!__is_same(C, void)) {
+        if (E.copy != nullptr) {
+            using CT = typename std::conditional<__is_same(C, void), __half, C>::type;
+            store_lane((CT *)E.copy, X.L, X.p);
+        }
+    }
+    if (BITS == 32) {
+        store_lane((M *)E.m, X.L, X.m);
+        store_lane((M *)E.v, X.L, X.v);
+    } else {
+        // elements that do not exist were read as zeros and stay zeros: they do not raise a block's top
+        const float tm = top_of(X.m), tr = top_of(root);
+        const bool some_m = tm >= 0x1p-100f, some_r = tr >= 0x1p-100f;
+        const float inv_m = some_m ? __fdiv_rn(448.0f, tm) : 0.0f, inv_r = some_r ? __fdiv_rn(448.0f, tr) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            X.m[j] = __fmul_rn(X.m[j], inv_m);
+            const float r = __fmul_rn(root[j], inv_r);
+            X.v[j] = root[j] > 0.0f ? fmaxf(r, 0x1p-9f) : r;      // 2^-9: the smallest e4m3 number
+        }
+        store_lane((M *)E.m, X.L, X.m);
+        store_lane((M *)E.v, X.L, X.v);
+        if (lane == 0 && group < E.hi) {
+            E.m_scale[group / kGroup] = some_m ? __fdiv_rn(tm, 448.0f) : 0.0f;
+            E.v_scale[group / kGroup] = some_r ? __fdiv_rn(tr, 448.0f) : 0.0f;
+        }
+    }
+}
+
+constexpr int kAdamwGroups = 2;                                     // groups of a warp per chunk, loaded together
+constexpr int kAdamwChunk = kOptWarps * kGroup * kAdamwGroups;      // elements
+
+// One step of AdamW (the formula is in psops.h).  What bounds it is HBM
+// traffic: 28 bytes per element with fp32 moments and gradients, 14 to 16 with
+// 8-bit moments and 16-bit gradients.
+template <int BITS, class G, class C>
+__global__ void __launch_bounds__(kOptThreads) psops_adamw_kernel(const AdamwParams P)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float scale = P.scale != nullptr ? *P.scale : 1.0f;
+    if (!(fabsf(scale) < INFINITY)) return;                         // skipped: nothing changes, t stays
+    const double pow1 = P.state->pow1, pow2 = P.state->pow2;
+    const float rate = (float)(P.lr * P.state->inv_bias1), spread = P.state->spread;
+    for (unsigned c = blockIdx.x; c < P.n_chunks; c += gridDim.x) {
+        const uint2 chunk = P.chunks[c];
+        const AdamwEntry E = P.entries[chunk.x];
+        const float decay = (float)(1.0 - P.lr * E.weight_decay);
+        const long long base = (long long)chunk.y * kAdamwChunk + warp * kGroup;
+        AdamwGroup<BITS> X[kAdamwGroups];
+#pragma unroll
+        for (int i = 0; i < kAdamwGroups; ++i)
+            adamw_load<BITS, G>(E, base + i * kOptWarps * kGroup, lane, X[i]);
+#pragma unroll
+        for (int i = 0; i < kAdamwGroups; ++i)
+            adamw_update<BITS, C>(E, base + i * kOptWarps * kGroup, lane, P, scale, rate, spread, decay, X[i]);
+    }
+    // The block that comes last -- every block has read the state by then --
+    // moves it on to the next step.
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(&P.state->tickets, 1u) == gridDim.x - 1) {
+            const double n1 = pow1 * P.beta1, n2 = pow2 * P.beta2;
+            P.state->pow1 = n1;
+            P.state->pow2 = n2;
+            P.state->inv_bias1 = 1.0 / (1.0 - n1 * P.beta1);
+            P.state->spread = (float)(1.0 / sqrt(1.0 - n2 * P.beta2));
+            P.state->steps += 1;
+            P.state->tickets = 0;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// 2-norm
+// ---------------------------------------------------------------------------
+
+struct NormEntry {
+    const void *g;                              // moved back by lo elements, so that the address is a multiple of 32
+    long long lo, hi;
+};
+
+struct NormParams {
+    const NormEntry *entries;
+    const uint2 *chunks;
+    double *partials;                           // one per block
+    unsigned *tickets;
+    float *out;
+    float max_norm;
+    unsigned n_chunks;
+};
+
+template <class G> struct NormShape {
+    static constexpr int kPer = 32 / (int)sizeof(G);                // elements of a 32-byte access
+    static constexpr int kDeep = 4;                                 // accesses of a thread in flight
+    static constexpr int kChunk = kOptThreads * kPer * kDeep;       // elements
+};
+
+__device__ __forceinline__ float sum_squares(const float *, const uint4 a, const uint4 b)
+{
+    const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf(__uint_as_float(w[i]), __uint_as_float(w[i]), s);
+    return s;
+}
+template <class T2>
+__device__ __forceinline__ float sum_squares_16(const uint4 a, const uint4 b)
+{
+    const unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        T2 h;
+        memcpy(&h, &w[i], 4);
+        const float2 f = widen(h);
+        s = fmaf(f.x, f.x, s);
+        s = fmaf(f.y, f.y, s);
+    }
+    return s;
+}
+__device__ __forceinline__ float sum_squares(const __half *, const uint4 a, const uint4 b) { return sum_squares_16<__half2>(a, b); }
+__device__ __forceinline__ float sum_squares(const __nv_bfloat16 *, const uint4 a, const uint4 b) { return sum_squares_16<__nv_bfloat162>(a, b); }
+
+__device__ __forceinline__ void load_32(const void *p, uint4 &a, uint4 &b)
+{
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w)
+                 : "l"(p));
+}
+
+// Sum over a block in a fixed order; the result is in thread 0.
+__device__ __forceinline__ double block_sum(double x, double *shared)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = x;
+    __syncthreads();
+    double s = 0.0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < kOptWarps; ++w) s += shared[w];
+    return s;
+}
+
+// Each block adds up the squares of its chunks; the block that draws the last
+// ticket adds the blocks' sums, always in the same order, and writes the norm
+// and the factor.  Bound by reading the gradients once.
+template <class G>
+__global__ void __launch_bounds__(kOptThreads) psops_gradnorm_kernel(const NormParams P)
+{
+    using S = NormShape<G>;
+    __shared__ double shared[kOptWarps];
+    __shared__ bool last;
+    double sum = 0.0;
+    for (unsigned c = blockIdx.x; c < P.n_chunks; c += gridDim.x) {
+        const uint2 chunk = P.chunks[c];
+        const NormEntry E = P.entries[chunk.x];
+        const G *g = (const G *)E.g;
+        const long long first = (long long)chunk.y * S::kChunk + (long long)threadIdx.x * S::kPer;
+        uint4 a[S::kDeep], b[S::kDeep];
+#pragma unroll
+        for (int i = 0; i < S::kDeep; ++i) {
+            const long long at = first + (long long)i * kOptThreads * S::kPer;
+            if (at >= E.lo && at + S::kPer <= E.hi) load_32(g + at, a[i], b[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < S::kDeep; ++i) {
+            const long long at = first + (long long)i * kOptThreads * S::kPer;
+            if (at >= E.lo && at + S::kPer <= E.hi) {
+                sum += (double)sum_squares((const G *)nullptr, a[i], b[i]);
+            } else {
+                float s = 0.0f;
+                for (int j = 0; j < S::kPer; ++j)
+                    if (at + j >= E.lo && at + j < E.hi) {
+                        const float x = one_in(g + at + j);
+                        s = fmaf(x, x, s);
+                    }
+                sum += (double)s;
+            }
+        }
+    }
+    const double mine = block_sum(sum, shared);
+    if (threadIdx.x == 0) {
+        P.partials[blockIdx.x] = mine;
+        __threadfence();
+        last = atomicAdd(P.tickets, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double total = 0.0;
+    for (unsigned b = threadIdx.x; b < gridDim.x; b += kOptThreads) total += __ldcg(P.partials + b);
+    total = block_sum(total, shared);
+    if (threadIdx.x == 0) {
+        const float norm = (float)sqrt(total);
+        const bool finite = norm < INFINITY;
+        P.out[0] = norm;
+        P.out[1] = finite ? fminf(1.0f, P.max_norm / (norm + 1e-6f)) : NAN;
+        *P.tickets = 0;
+    }
+}
+
+} // namespace

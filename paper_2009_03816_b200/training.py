@@ -1,0 +1,232 @@
+"""Operators of the training steps between two synchronisations.
+
+Holders of the device tensors (torch) that the library's training-operator
+contexts borrow, in the manner of :class:`binding.Swarm`: they check arguments,
+allocate workspaces and outputs, and forward to the C entry points; every
+computation runs in the CUDA library.
+
+  AdamW        one AdamW step over many tensors, moments in 32 or in 8 bits
+  GradNorm     2-norm of many gradients and the factor that clips it
+
+A context belongs to one stream, the current one of its GPU when the holder is
+made (or the one given); its calls enqueue there, whatever the current stream
+is later.  Tensors that were produced on another stream have to be ordered
+before the call by the caller, as for any kernel.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from . import binding
+from .binding import PSOPS_BF16, PSOPS_EINVAL, PSOPS_F16, PSOPS_F32, PSOPS_NONE, PsopsError
+
+_TYPES = {torch.float32: PSOPS_F32, torch.float16: PSOPS_F16, torch.bfloat16: PSOPS_BF16}
+MOMENT_BLOCK = 256               # elements that share one scale of an 8-bit moment
+
+
+def _refuse(where: str, why: str):
+    raise PsopsError(PSOPS_EINVAL, where, why)
+
+
+def _flat_list(where, what, tensors, dtypes, device, count=None, sizes=None):
+    """A list of contiguous device tensors of one of `dtypes`."""
+    tensors = list(tensors)
+    if count is not None and len(tensors) != count:
+        _refuse(where, f"{len(tensors)} tensors in `{what}`, {count} parameters")
+    for i, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor) or t.device != device:
+            _refuse(where, f"{what}[{i}] is not a tensor on {device}")
+        if t.dtype not in dtypes:
+            _refuse(where, f"{what}[{i}] is {t.dtype}, not one of {[str(d) for d in dtypes]}")
+        if not t.is_contiguous():
+            _refuse(where, f"{what}[{i}] is not contiguous")
+        if sizes is not None and t.numel() != sizes[i]:
+            _refuse(where, f"{what}[{i}] has {t.numel()} elements, not {sizes[i]}")
+    return tensors
+
+
+def _device_of(where, tensors):
+    if not tensors:
+        _refuse(where, "no tensors")
+    t = tensors[0]
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        _refuse(where, "the tensors have to be on a GPU")
+    return t.device
+
+
+def _stream_on(device, stream):
+    return torch.cuda.current_stream(device).cuda_stream if stream is None else stream
+
+
+def _workspace(nbytes, device, where):
+    if nbytes == 0:
+        _refuse(where, "sizes out of range")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+class AdamW:
+    """AdamW over a list of parameter tensors, in one launch per step.
+
+    params        fp32 device tensors, contiguous (views of a swarm's row, for instance)
+    grads         their gradients, all fp32, all fp16 or all bf16
+    bits          32: fp32 moments (m, v); 8: moments (m, sqrt v) of 8 bits with a
+                  scale for every 256 elements of a tensor
+    moments       state to go on with, else zeros: (m, v), lists of fp32 tensors, or for
+                  8 bits (m, m_scale, root, root_scale), lists of torch.float8_e4m3fn
+                  (or uint8) tensors of the parameters' sizes and of fp32 tensors of
+                  ceil(n / 256) scales
+    copies        16-bit tensors (None for a parameter without one) that receive the new
+                  weights, rounded to nearest
+    weight_decay  one number, or one for each parameter
+    steps_done    steps that the given moments have already seen
+
+    A step whose grad_scale is not finite is skipped on the device.
+    """
+
+    def __init__(self, params, grads, *, bits=32, moments=None, copies=None, betas=(0.9, 0.999), eps=1e-8,
+                 weight_decay=0.01, steps_done=0, stream=None):
+        where = "AdamW"
+        params = list(params)
+        device = _device_of(where, params)
+        self.params = _flat_list(where, "params", params, (torch.float32,), device)
+        n, sizes = len(params), [p.numel() for p in params]
+        self._sizes = sizes
+        self.grads = _flat_list(where, "grads", grads, tuple(_TYPES), device, n, sizes)
+        if len({g.dtype for g in self.grads}) != 1:
+            _refuse(where, "gradients of more than one type")
+        if bits not in (8, 32):
+            _refuse(where, f"moments of {bits} bits")
+        blocks = [-(-s // MOMENT_BLOCK) for s in sizes]
+        held = (torch.float32,) if bits == 32 else (torch.float8_e4m3fn, torch.uint8)
+        if moments is None:
+            zeros = lambda counts, dtype: [torch.zeros(c, dtype=torch.uint8 if dtype != torch.float32 else dtype,
+                                                       device=device).view(dtype) for c in counts]
+            moments = (zeros(sizes, held[0]), zeros(sizes, held[0])) if bits == 32 else \
+                (zeros(sizes, held[0]), zeros(blocks, torch.float32), zeros(sizes, held[0]), zeros(blocks, torch.float32))
+        if len(moments) != (2 if bits == 32 else 4):
+            _refuse(where, "`moments` is (m, v), or (m, m_scale, root, root_scale) for 8 bits")
+        if bits == 32:
+            self.moments = tuple(_flat_list(where, k, x, held, device, n, sizes) for k, x in zip(("m", "v"), moments))
+            m, v, ms, vs = self.moments[0], self.moments[1], [None] * n, [None] * n
+        else:
+            names = (("m", held, sizes), ("m_scale", (torch.float32,), blocks), ("root", held, sizes),
+                     ("root_scale", (torch.float32,), blocks))
+            self.moments = tuple(_flat_list(where, k, x, d, device, n, s) for (k, d, s), x in zip(names, moments))
+            m, ms, v, vs = self.moments
+        copy_type = PSOPS_NONE
+        if copies is not None:
+            copies = list(copies)
+            if len(copies) != n:
+                _refuse(where, f"{len(copies)} copies, {n} parameters")
+            there = [i for i, c in enumerate(copies) if c is not None]
+            _flat_list(where, "copies", [copies[i] for i in there], (torch.float16, torch.bfloat16), device,
+                       len(there), [sizes[i] for i in there])
+            kinds = {copies[i].dtype for i in there}
+            if len(kinds) > 1:
+                _refuse(where, "copies of more than one type")
+            copy_type = _TYPES[kinds.pop()] if kinds else PSOPS_NONE
+        self.copies = copies
+        decay = [float(weight_decay)] * n if not isinstance(weight_decay, (list, tuple)) else [float(d) for d in weight_decay]
+        if len(decay) != n:
+            _refuse(where, f"{len(decay)} weight decays, {n} parameters")
+        self.bits, self.device = bits, device
+        cfg = binding.psops_adamw_config(float(betas[0]), float(betas[1]), float(eps), int(steps_done), bits,
+                                         _TYPES[self.grads[0].dtype], copy_type, n)
+        at = lambda t: t.data_ptr() if t is not None and t.numel() else None
+        table = (binding.psops_adamw_tensor * n)(*[
+            binding.psops_adamw_tensor(at(self.params[i]), at(self.grads[i]),
+                                       at(copies[i]) if copies is not None else None, at(m[i]), at(v[i]), at(ms[i]),
+                                       at(vs[i]), sizes[i], decay[i]) for i in range(n)])
+        self.ctx = None
+        with torch.cuda.device(device):
+            self._workspace = _workspace(binding.psops_adamw_workspace_bytes(cfg, table), device, where)
+            self.stream = _stream_on(device, stream)
+            self.ctx = binding.psops_adamw_create(cfg, table, self._workspace, None, self.stream)
+        self._scale = None
+
+    def set_grads(self, grads):
+        """Other gradient tensors for the steps to come, of the type given at first."""
+        grads = _flat_list("AdamW.set_grads", "grads", grads, (self.grads[0].dtype,), self.device, len(self._sizes),
+                           self._sizes)
+        binding.psops_adamw_set_grads(self.ctx, grads)
+        self.grads = grads
+
+    def step(self, lr, grad_scale=None):
+        """One step; grad_scale: a device fp32 scalar that multiplies every gradient."""
+        if grad_scale is not None and not (isinstance(grad_scale, torch.Tensor) and grad_scale.device == self.device
+                                           and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1):
+            _refuse("AdamW.step", f"grad_scale has to be one fp32 number on {self.device}")
+        self._scale = grad_scale               # read by the kernel: keep it alive
+        binding.psops_adamw_step(self.ctx, lr, grad_scale)
+
+    @property
+    def steps(self) -> int:
+        """Steps taken so far (waits for the stream)."""
+        return binding.psops_adamw_steps(self.ctx)
+
+    @property
+    def launches(self) -> int:
+        return binding.psops_adamw_launch_count(self.ctx)
+
+    def close(self):
+        if self.ctx is not None:
+            binding.psops_adamw_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class GradNorm:
+    """2-norm of a list of gradient tensors (all of one type) together."""
+
+    def __init__(self, grads, *, stream=None):
+        where = "GradNorm"
+        grads = list(grads)
+        self.device = _device_of(where, grads)
+        self.grads = _flat_list(where, "grads", grads, tuple(_TYPES), self.device)
+        if len({g.dtype for g in grads}) != 1:
+            _refuse(where, "gradients of more than one type")
+        self._sizes = [g.numel() for g in grads]
+        self.ctx = None
+        with torch.cuda.device(self.device):
+            self._workspace = _workspace(binding.psops_gradnorm_workspace_bytes(self._sizes), self.device, where)
+            self.stream = _stream_on(self.device, stream)
+            self.ctx = binding.psops_gradnorm_create([g if g.numel() else None for g in grads], self._sizes,
+                                                     _TYPES[grads[0].dtype], self._workspace, None, self.stream)
+
+    def set_grads(self, grads):
+        grads = _flat_list("GradNorm.set_grads", "grads", grads, (self.grads[0].dtype,), self.device,
+                           len(self._sizes), self._sizes)
+        binding.psops_gradnorm_set_grads(self.ctx, [g if g.numel() else None for g in grads])
+        self.grads = grads
+
+    def norm(self, max_norm=math.inf, out=None):
+        """(norm, factor), two device scalars: factor = min(1, max_norm / (norm + 1e-6)), NaN
+        if the norm is not finite.  `out`: an fp32 device tensor of 2 elements to hold them."""
+        if out is None:
+            out = torch.empty(2, dtype=torch.float32, device=self.device)
+        elif out.device != self.device or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
+            _refuse("GradNorm.norm", f"`out` has to be 2 fp32 numbers on {self.device}")
+        binding.psops_gradnorm_run(self.ctx, max_norm, out)
+        return out[0], out[1]
+
+    @property
+    def launches(self) -> int:
+        return binding.psops_gradnorm_launch_count(self.ctx)
+
+    def close(self):
+        if self.ctx is not None:
+            binding.psops_gradnorm_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
