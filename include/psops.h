@@ -484,6 +484,83 @@ int64_t psops_gradnorm_launch_count(const psops_gradnorm *gn);
 const char *psops_gradnorm_last_error(const psops_gradnorm *gn);
 int psops_gradnorm_destroy(psops_gradnorm *gn);
 
+/*
+ * Softmax cross entropy of a linear head over a large vocabulary, without
+ * keeping the logits.  h: tokens x dim hidden states, w: vocab x dim weights
+ * (both of one 16-bit type), targets: one label per token.
+ *   logits[t, v] = sum_d h[t, d] w[v, d]
+ *   lse[t]       = log sum_v exp(logits[t, v])
+ *   rows[t]      = lse[t] - logits[t, targets[t]]
+ *   loss         = sum_t rows[t] / n  (PSOPS_MEAN)  or  sum_t rows[t]  (PSOPS_SUM)
+ * A token whose label lies outside [0, vocab) -- -100, say -- is left out: its
+ * rows and lse are 0, it gets no gradient and gives none, whatever its hidden
+ * state holds (NaN and infinities included); n counts the others.  With n = 0
+ * the loss is 0.
+ *   dlogits[t, v] = (exp(logits[t, v] - lse[t]) - [v == targets[t]]) * grad_t
+ *   dh = dlogits w,  dw = dlogits^T h
+ * with grad_t = *d_grad / n (PSOPS_MEAN), *d_grad (PSOPS_SUM) or d_grad[t]
+ * (PSOPS_PER_TOKEN).  The gradient pass computes the logits once more, a piece
+ * of the vocabulary at a time.
+ *
+ * Rounding: products are summed in fp32, softmax statistics are fp32, the loss
+ * is summed in double.  dlogits enters the two gradient products rounded to
+ * the 16-bit type (that is what the tensor cores multiply), scaled by a power
+ * of two that keeps small probabilities inside fp16's range; dh and dw are
+ * rounded to the 16-bit type once, at the end.
+ * Rows: row t of h, w, dh, dw starts at t * its stride (in elements, at least
+ * dim).  dim a multiple of 8 with 16-byte aligned rows of w is read in place;
+ * any other w, and any other dw, passes through the workspace
+ * (PSOPS_XENT_STAGED).
+ */
+#define PSOPS_MEAN       0
+#define PSOPS_SUM        1
+#define PSOPS_PER_TOKEN  2
+
+#define PSOPS_XENT_GRADS   1u   /* reserve workspace for psops_xent_backward                    */
+#define PSOPS_XENT_STAGED  2u   /* reserve workspace for rows of w / dw that are not 16-byte
+                                   aligned although dim is a multiple of 8                      */
+
+typedef struct {
+    int64_t  max_tokens;     /* most tokens of a call, 1 .. 2^24                       */
+    int64_t  dim;            /* 1 .. 2^20                                              */
+    int64_t  vocab;          /* 1 .. 2^31 - 2^16                                       */
+    int32_t  type;           /* PSOPS_F16 or PSOPS_BF16                                */
+    uint32_t flags;
+} psops_xent_config;
+
+typedef struct psops_xent psops_xent;  /* opaque */
+
+size_t psops_xent_workspace_bytes(const psops_xent_config *cfg);
+int psops_xent_create(psops_xent **out, const psops_xent_config *cfg, void *d_workspace, size_t workspace_bytes,
+                      void *cuda_stream);
+
+/*
+ * Loss only (the fitness of a worker's weights, or the first half of a training
+ * step).  d_loss: one float (it can be the element of a device loss vector
+ * given to psops_set_losses) or NULL; d_rows, d_lse: `tokens` floats each, or
+ * NULL.  reduction: PSOPS_MEAN or PSOPS_SUM.  0 <= tokens <= max_tokens.
+ * Errors: EINVAL, EALIGN (a pointer not aligned to its element; w not 16-byte
+ * aligned without PSOPS_XENT_STAGED), ECUDA.
+ */
+int psops_xent_forward(psops_xent *x, const void *d_h, int64_t h_ld, const void *d_w, int64_t w_ld,
+                       const int64_t *d_targets, int64_t tokens, int32_t reduction,
+                       float *d_loss, float *d_rows, float *d_lse);
+
+/*
+ * Gradients, from the same h, w, targets and the lse of psops_xent_forward.
+ * d_grad: the upstream gradient, see above.  d_dh or d_dw may be NULL (not
+ * wanted).  Both are overwritten, not added to.  Errors: as forward, and ESTATE
+ * without PSOPS_XENT_GRADS.
+ */
+int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void *d_w, int64_t w_ld,
+                        const int64_t *d_targets, int64_t tokens, const float *d_lse,
+                        const float *d_grad, int32_t reduction,
+                        void *d_dh, int64_t dh_ld, void *d_dw, int64_t dw_ld);
+
+int64_t psops_xent_launch_count(const psops_xent *x);
+const char *psops_xent_last_error(const psops_xent *x);
+int psops_xent_destroy(psops_xent *x);
+
 #ifdef __cplusplus
 }
 #endif

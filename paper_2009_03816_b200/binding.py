@@ -24,6 +24,8 @@ PSOPS_MAX_K = 1024
 PSOPS_KEEP_GBEST, PSOPS_QUADRATIC, PSOPS_GBEST_HISTORY, PSOPS_SEPARATE_SELECT = 1, 2, 4, 8
 PSOPS_X, PSOPS_V, PSOPS_PBEST, PSOPS_GBEST = 0, 1, 2, 3
 PSOPS_NONE, PSOPS_F32, PSOPS_F16, PSOPS_BF16 = 0, 1, 2, 3
+PSOPS_MEAN, PSOPS_SUM, PSOPS_PER_TOKEN = 0, 1, 2
+PSOPS_XENT_GRADS, PSOPS_XENT_STAGED = 1, 2
 
 EXPORTS = [
     "psops_workspace_bytes", "psops_create", "psops_set_losses", "psops_sync",
@@ -38,6 +40,8 @@ EXPORTS = [
     "psops_adamw_steps", "psops_adamw_launch_count", "psops_adamw_last_error", "psops_adamw_destroy",
     "psops_gradnorm_workspace_bytes", "psops_gradnorm_create", "psops_gradnorm_set_grads", "psops_gradnorm_run",
     "psops_gradnorm_launch_count", "psops_gradnorm_last_error", "psops_gradnorm_destroy",
+    "psops_xent_workspace_bytes", "psops_xent_create", "psops_xent_forward", "psops_xent_backward",
+    "psops_xent_launch_count", "psops_xent_last_error", "psops_xent_destroy",
 ]
 
 
@@ -58,6 +62,11 @@ class psops_adamw_tensor(ctypes.Structure):
     _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("m", ctypes.c_void_p),
                 ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
                 ("n", ctypes.c_int64), ("weight_decay", ctypes.c_double)]
+
+
+class psops_xent_config(ctypes.Structure):
+    _fields_ = [("max_tokens", ctypes.c_int64), ("dim", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
 
 class PsopsError(RuntimeError):
@@ -85,6 +94,7 @@ def load() -> ctypes.CDLL:
             "There is no CPU fallback.")
     lib = ctypes.CDLL(LIBRARY)
     cfgp = ctypes.POINTER(psops_config)
+    xcfgp = ctypes.POINTER(psops_xent_config)
     acfgp, atensp = ctypes.POINTER(psops_adamw_config), ctypes.POINTER(psops_adamw_tensor)
     sig = {
         "psops_workspace_bytes": (ctypes.c_size_t, [cfgp]),
@@ -136,6 +146,16 @@ def load() -> ctypes.CDLL:
         "psops_gradnorm_launch_count": (ctypes.c_int64, [_vp]),
         "psops_gradnorm_last_error": (ctypes.c_char_p, [_vp]),
         "psops_gradnorm_destroy": (ctypes.c_int, [_vp]),
+        "psops_xent_workspace_bytes": (ctypes.c_size_t, [xcfgp]),
+        "psops_xent_create": (ctypes.c_int, [ctypes.POINTER(_vp), xcfgp, _vp, ctypes.c_size_t, _vp]),
+        "psops_xent_forward": (ctypes.c_int, [_vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, ctypes.c_int64,
+                                              ctypes.c_int32, _f32p, _f32p, _f32p]),
+        "psops_xent_backward": (ctypes.c_int, [_vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, ctypes.c_int64,
+                                               _f32p, _f32p, ctypes.c_int32, _vp, ctypes.c_int64, _vp,
+                                               ctypes.c_int64]),
+        "psops_xent_launch_count": (ctypes.c_int64, [_vp]),
+        "psops_xent_last_error": (ctypes.c_char_p, [_vp]),
+        "psops_xent_destroy": (ctypes.c_int, [_vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)            # AttributeError if a symbol is missing
@@ -399,6 +419,42 @@ def psops_gradnorm_launch_count(gn) -> int:
 
 def psops_gradnorm_destroy(gn) -> None:
     _check(load().psops_gradnorm_destroy(gn), "psops_gradnorm_destroy")
+
+
+def psops_xent_workspace_bytes(cfg: psops_xent_config) -> int:
+    return int(load().psops_xent_workspace_bytes(ctypes.byref(cfg)))
+
+
+def psops_xent_create(cfg, d_workspace, workspace_bytes=None, stream=None):
+    handle = _vp()
+    if workspace_bytes is None:
+        workspace_bytes = d_workspace.numel() * d_workspace.element_size() if d_workspace is not None else 0
+    rc = load().psops_xent_create(ctypes.byref(handle), ctypes.byref(cfg), _ptr(d_workspace), int(workspace_bytes),
+                                  int(stream) if stream else None)
+    _check(rc, "psops_xent_create")
+    return handle
+
+
+def psops_xent_forward(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, reduction, d_loss, d_rows, d_lse) -> None:
+    _check(load().psops_xent_forward(x, _ptr(d_h), int(h_ld), _ptr(d_w), int(w_ld), _ptr(d_targets), int(tokens),
+                                     int(reduction), _ptr(d_loss), _ptr(d_rows), _ptr(d_lse)),
+           "psops_xent_forward", x, "psops_xent_last_error")
+
+
+def psops_xent_backward(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, d_lse, d_grad, reduction, d_dh, dh_ld, d_dw,
+                        dw_ld) -> None:
+    _check(load().psops_xent_backward(x, _ptr(d_h), int(h_ld), _ptr(d_w), int(w_ld), _ptr(d_targets), int(tokens),
+                                      _ptr(d_lse), _ptr(d_grad), int(reduction), _ptr(d_dh), int(dh_ld), _ptr(d_dw),
+                                      int(dw_ld)),
+           "psops_xent_backward", x, "psops_xent_last_error")
+
+
+def psops_xent_launch_count(x) -> int:
+    return int(load().psops_xent_launch_count(x))
+
+
+def psops_xent_destroy(x) -> None:
+    _check(load().psops_xent_destroy(x), "psops_xent_destroy")
 
 
 # ---- convenience holder of the tensors a context borrows ------------------

@@ -11,9 +11,10 @@ import sys
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
-SOURCES = [os.path.join(_HERE, "csrc", name) for name in ("psops.cu", "psops_optim.cu")]
+SOURCES = [os.path.join(_HERE, "csrc", name) for name in ("psops.cu", "psops_optim.cu", "psops_xent.cu")]
 HEADERS = [os.path.join(_ROOT, "include", "psops.h")] + [
-    os.path.join(_HERE, "csrc", name) for name in ("psops_kernels.cuh", "psops_host.cuh", "psops_optim_kernels.cuh")]
+    os.path.join(_HERE, "csrc", name) for name in ("psops_kernels.cuh", "psops_host.cuh", "psops_optim_kernels.cuh",
+                                              "psops_xent_kernels.cuh")]
 LIBRARY = os.path.join(_HERE, "libpsops.so")
 
 NVCC_FLAGS = [

@@ -5,6 +5,8 @@ contexts borrow, in the manner of :class:`binding.Swarm`: they check arguments,
 allocate workspaces and outputs, and forward to the C entry points; every
 computation runs in the CUDA library.
 
+  LinearXent   softmax cross entropy of a linear head without keeping the logits,
+               with its gradients; its loss alone is a worker's fitness
   AdamW        one AdamW step over many tensors, moments in 32 or in 8 bits
   GradNorm     2-norm of many gradients and the factor that clips it
 
@@ -20,7 +22,8 @@ import math
 import torch
 
 from . import binding
-from .binding import PSOPS_BF16, PSOPS_EINVAL, PSOPS_F16, PSOPS_F32, PSOPS_NONE, PsopsError
+from .binding import (PSOPS_BF16, PSOPS_EINVAL, PSOPS_F16, PSOPS_F32, PSOPS_MEAN, PSOPS_NONE, PSOPS_PER_TOKEN,
+                      PSOPS_SUM, PSOPS_XENT_GRADS, PSOPS_XENT_STAGED, PsopsError)
 
 _TYPES = {torch.float32: PSOPS_F32, torch.float16: PSOPS_F16, torch.bfloat16: PSOPS_BF16}
 MOMENT_BLOCK = 256               # elements that share one scale of an 8-bit moment
@@ -64,6 +67,160 @@ def _workspace(nbytes, device, where):
     if nbytes == 0:
         _refuse(where, "sizes out of range")
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+class LinearXent:
+    """Cross entropy of logits = h w^T against one label per token.
+
+    tokens, dim, vocab   the most tokens of a call, and the sizes of w (vocab x dim)
+    dtype                torch.bfloat16 or torch.float16, the type of h and w
+    gradients            False: no workspace for backward (the loss alone)
+
+    h may have any leading dimensions, with rows of `dim` consecutive elements; `targets`
+    (int64) has those leading dimensions.  A label outside [0, vocab) leaves its token out.
+    Calling the object gives the loss as a torch value with gradients::
+
+        loss = xent(h, w, targets)            # reduction="mean", "sum" or "none"
+        loss.backward()
+    """
+
+    def __init__(self, tokens, dim, vocab, *, dtype=torch.bfloat16, device="cuda", gradients=True, stream=None):
+        device = torch.device(device)
+        if device.type != "cuda":
+            _refuse("LinearXent", "needs a GPU")
+        if dtype not in (torch.float16, torch.bfloat16):
+            _refuse("LinearXent", f"h and w of {dtype}: torch.bfloat16 or torch.float16")
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+        self.tokens, self.dim, self.vocab, self.dtype = int(tokens), int(dim), int(vocab), dtype
+        self.ctx, self._launched = None, 0
+        self._flags = PSOPS_XENT_GRADS if gradients else 0
+        self.stream = _stream_on(self.device, stream)
+        self._open()
+
+    def _open(self):
+        cfg = binding.psops_xent_config(self.tokens, self.dim, self.vocab, _TYPES[self.dtype], self._flags)
+        nbytes = binding.psops_xent_workspace_bytes(cfg)
+        with torch.cuda.device(self.device):
+            self.close()
+            self._workspace = _workspace(nbytes, self.device, "LinearXent")
+            self.ctx = binding.psops_xent_create(cfg, self._workspace, None, self.stream)
+
+    def _rows(self, where, name, t, dtype=None):
+        """(tensor as rows, stride) of a matrix with consecutive elements in each row."""
+        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != (dtype or self.dtype):
+            _refuse(where, f"{name} is not a {dtype or self.dtype} tensor on {self.device}")
+        if t.dim() < 1 or t.shape[-1] != self.dim:
+            _refuse(where, f"{name} has no last dimension of {self.dim}")
+        if t.dim() != 2:
+            try:
+                t = t.view(-1, self.dim)
+            except RuntimeError:
+                _refuse(where, f"{name}: its leading dimensions cannot be seen as one")
+        if t.shape[1] > 1 and t.stride(1) != 1:
+            _refuse(where, f"{name}: the elements of a row are not consecutive")
+        ld = t.stride(0) if t.shape[0] > 1 else self.dim
+        if ld < self.dim:
+            _refuse(where, f"{name}: rows overlap")
+        return t, ld
+
+    def _arguments(self, where, h, w, targets):
+        h2, h_ld = self._rows(where, "h", h)
+        w2, w_ld = self._rows(where, "w", w)
+        if w.dim() != 2 or w2.shape[0] != self.vocab:
+            _refuse(where, f"w is not {self.vocab} x {self.dim}")
+        if not isinstance(targets, torch.Tensor) or targets.device != self.device or targets.dtype != torch.int64:
+            _refuse(where, f"targets is not an int64 tensor on {self.device}")
+        if targets.shape != h.shape[:-1] or not targets.is_contiguous():
+            _refuse(where, f"targets has to be contiguous and of shape {tuple(h.shape[:-1])}")
+        if h2.shape[0] > self.tokens:
+            _refuse(where, f"{h2.shape[0]} tokens, made for {self.tokens}")
+        self._stage_if_needed(w2, w_ld)
+        return h2, h_ld, w2, w_ld
+
+    def _stage_if_needed(self, t, ld):
+        """Rows that are not 16-byte aligned pass through a larger workspace, made when first met."""
+        if self.dim % 8 == 0 and (t.data_ptr() % 16 or ld % 8) and not self._flags & PSOPS_XENT_STAGED:
+            self._flags |= PSOPS_XENT_STAGED
+            self._open()
+
+    def forward(self, h, w, targets, reduction="mean"):
+        """(loss, rows, lse): the loss of all tokens ("mean" or "sum"), and each token's loss and log-sum-exp."""
+        if reduction not in ("mean", "sum"):
+            _refuse("LinearXent.forward", f"reduction {reduction!r}")
+        h2, h_ld, w2, w_ld = self._arguments("LinearXent.forward", h, w, targets)
+        loss = torch.empty((), dtype=torch.float32, device=self.device)
+        rows, lse = (torch.empty(targets.shape, dtype=torch.float32, device=self.device) for _ in range(2))
+        binding.psops_xent_forward(self.ctx, h2, h_ld, w2, w_ld, targets, h2.shape[0],
+                                   PSOPS_MEAN if reduction == "mean" else PSOPS_SUM, loss, rows, lse)
+        return loss, rows, lse
+
+    def backward(self, h, w, targets, lse, grad, reduction="mean", *, dh=None, dw=None, want=(True, True)):
+        """(dh, dw) from the upstream gradient: one fp32 number, or one per token for reduction "none".
+        dh, dw: tensors to hold them; want: which of the two is computed."""
+        where = "LinearXent.backward"
+        codes = {"mean": PSOPS_MEAN, "sum": PSOPS_SUM, "none": PSOPS_PER_TOKEN}
+        if reduction not in codes:
+            _refuse(where, f"reduction {reduction!r}")
+        h2, h_ld, w2, w_ld = self._arguments(where, h, w, targets)
+        for name, t, shape in (("lse", lse, targets.shape), ("grad", grad, targets.shape if reduction == "none" else None)):
+            if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != torch.float32 or \
+                    not t.is_contiguous() or (t.shape != shape if shape is not None else t.numel() != 1):
+                _refuse(where, f"{name} has to be contiguous, fp32, on {self.device}, of shape "
+                               f"{tuple(shape) if shape is not None else ()}")
+        out = []
+        for name, t, like, wanted in (("dh", dh, h, want[0]), ("dw", dw, w, want[1])):
+            if not wanted:
+                out.append((None, None, 0))
+                continue
+            t = torch.empty(like.shape, dtype=self.dtype, device=self.device) if t is None else t
+            rows, ld = self._rows(where, name, t)
+            if t.shape != like.shape:
+                _refuse(where, f"{name} is not of shape {tuple(like.shape)}")
+            out.append((t, rows, ld))
+        if out[1][0] is not None:
+            self._stage_if_needed(out[1][1], out[1][2])
+        binding.psops_xent_backward(self.ctx, h2, h_ld, w2, w_ld, targets, h2.shape[0], lse, grad, codes[reduction],
+                                    out[0][1], out[0][2], out[1][1], out[1][2])
+        return out[0][0], out[1][0]
+
+    def __call__(self, h, w, targets, reduction="mean"):
+        return _LinearXentFunction.apply(h, w, targets, self, reduction)
+
+    @property
+    def launches(self) -> int:
+        return self._launched + (binding.psops_xent_launch_count(self.ctx) if self.ctx is not None else 0)
+
+    def close(self):
+        if self.ctx is not None:
+            self._launched += binding.psops_xent_launch_count(self.ctx)
+            binding.psops_xent_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class _LinearXentFunction(torch.autograd.Function):
+    """LinearXent.forward and .backward as one differentiable step."""
+
+    @staticmethod
+    def forward(ctx, h, w, targets, op, reduction):
+        if reduction not in ("mean", "sum", "none"):
+            _refuse("LinearXent", f"reduction {reduction!r}")
+        loss, rows, lse = op.forward(h, w, targets, "mean" if reduction == "mean" else "sum")
+        ctx.save_for_backward(h, w, targets, lse)
+        ctx.op, ctx.reduction = op, reduction
+        return rows if reduction == "none" else loss
+
+    @staticmethod
+    def backward(ctx, grad):
+        h, w, targets, lse = ctx.saved_tensors
+        dh, dw = ctx.op.backward(h, w, targets, lse, grad.float().contiguous(), ctx.reduction,
+                                 want=(ctx.needs_input_grad[0], ctx.needs_input_grad[1]))
+        return dh, dw, None, None, None
 
 
 class AdamW:

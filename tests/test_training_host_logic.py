@@ -78,3 +78,28 @@ def test_gradnorm_refuses_before_touching_cuda(lib):
         assert e.value.code == code
     assert lib.psops_gradnorm_run(None, 1.0, None) == binding.PSOPS_EINVAL
     assert lib.psops_gradnorm_destroy(None) == binding.PSOPS_EINVAL
+
+
+def test_xent_config_and_workspace(lib):
+    assert ctypes.sizeof(binding.psops_xent_config) == 32
+    make = lambda T=64, D=32, V=100, kind=binding.PSOPS_BF16, flags=0: \
+        binding.psops_xent_workspace_bytes(binding.psops_xent_config(T, D, V, kind, flags))
+    assert make() > 0 and make(flags=binding.PSOPS_XENT_GRADS) > make()
+    assert make(flags=binding.PSOPS_XENT_STAGED) > make() and make(D=33) > make(D=40)
+    # the gradients' workspace stays far below the logits of a large call
+    assert make(8192, 4096, 131072, flags=binding.PSOPS_XENT_GRADS) < 8192 * 131072 * 2 / 2
+    for kw in ({"T": 0}, {"T": 1 << 25}, {"D": 0}, {"D": 1 << 21}, {"V": 0}, {"V": 1 << 31}, {"kind": binding.PSOPS_F32},
+               {"kind": 0}, {"flags": 4}):
+        assert make(**kw) == 0, kw
+
+
+def test_xent_refuses_before_touching_cuda(lib):
+    out = ctypes.c_void_p(1)
+    cfg = binding.psops_xent_config(64, 32, 100, binding.PSOPS_BF16, 0)
+    for ws, size in ((None, 1 << 30), (0x101, 1 << 30), (0x100, 64)):
+        assert lib.psops_xent_create(ctypes.byref(out), ctypes.byref(cfg), ws, size, None) == binding.PSOPS_EWORKSPACE
+        assert not out.value
+    assert lib.psops_xent_create(ctypes.byref(out), None, 0x100, 1 << 30, None) == binding.PSOPS_EINVAL
+    assert lib.psops_xent_forward(None, None, 0, None, 0, None, 0, 0, None, None, None) == binding.PSOPS_EINVAL
+    assert lib.psops_xent_backward(None, None, 0, None, 0, None, 0, None, None, 0, None, 0, None, 0) == binding.PSOPS_EINVAL
+    assert lib.psops_xent_destroy(None) == binding.PSOPS_EINVAL
