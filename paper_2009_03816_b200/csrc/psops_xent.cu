@@ -3,6 +3,7 @@
 
 #include "psops.h"
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -21,6 +22,8 @@ namespace {
 // Bytes that the logits' gradients of one piece of the vocabulary may take.
 constexpr int64_t kPieceBytes = 512ll << 20;
 constexpr int64_t kMinPiece = 2048;
+// Pairs of CTAs that run at once on a B200 (148 SMs).
+constexpr int64_t kPairs = 74;
 
 bool config_ok(const psops_xent_config *c)
 {
@@ -29,12 +32,20 @@ bool config_ok(const psops_xent_config *c)
            (c->flags & ~(PSOPS_XENT_GRADS | PSOPS_XENT_STAGED)) == 0;
 }
 
+// dh has few tiles where there are few rows: its sum over the vocabulary is then
+// split into shares, so that all SMs have a tile.
+int64_t shares_of(int64_t rows, int64_t padded)
+{
+    return std::max<int64_t>(1, kPairs / (rows / kTileRows * ceil_div(padded, kTile)));
+}
+
 struct Layout {
     int64_t rows;                               // compact rows, whole tiles
     int64_t padded;                             // dim, a multiple of 8
     int64_t piece;                              // vocabulary entries of a piece, a multiple of the tile
     bool staged;                                // w and dw may pass through the workspace
     int64_t parts;                              // softmax statistics per row
+    int64_t sum_rows;                           // rows of the fp32 sums of dh, all shares together
     size_t control, row_of, compact_of, label, row_scale, row_lse, label_logit, partials, hidden, stats, w, dw, dlogits, sums, total;
 };
 
@@ -46,7 +57,8 @@ Layout make_layout(const psops_xent_config *c)
     const int64_t whole = (int64_t)round_up((size_t)c->vocab, kTileCols);
     L.piece = std::min(whole, std::max(kMinPiece, kPieceBytes / (2 * L.rows) / kTileCols * kTileCols));
     L.staged = c->dim % 8 != 0 || (c->flags & PSOPS_XENT_STAGED) != 0;
-    L.parts = ceil_div(c->vocab, kSimple);
+    L.parts = whole / kHalf;
+    L.sum_rows = L.rows * shares_of(L.rows, L.padded);
     size_t at = 0;
     auto take = [&at](size_t bytes) {
         const size_t here = at;
@@ -68,7 +80,7 @@ Layout make_layout(const psops_xent_config *c)
     if (c->flags & PSOPS_XENT_GRADS) {
         if (L.staged) L.dw = take(2 * (size_t)L.piece * (size_t)L.padded);
         L.dlogits = take(2 * n * (size_t)L.piece);
-        L.sums = take(4 * n * (size_t)L.padded);
+        L.sums = take(4 * (size_t)L.sum_rows * (size_t)L.padded);
     }
     L.total = at;
     return L;
@@ -76,10 +88,15 @@ Layout make_layout(const psops_xent_config *c)
 
 } // namespace
 
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 struct psops_xent : Base {
     psops_xent_config cfg;
     Layout lay;
     char *ws;
+    EncodeTiled encode;
     template <class T> T *at(size_t offset) const { return (T *)(ws + offset); }
     XentControl *control() const { return at<XentControl>(lay.control); }
 };
@@ -147,37 +164,97 @@ int piece_of_w(psops_xent *x, const void *w, int64_t w_ld, int64_t first, int64_
     return x->launched("psops_xent_pack_kernel");
 }
 
-LogitsParams logits_params(const psops_xent *x)
+// A matrix of `height` rows of `width` consecutive elements as the tensor
+// copies see it: boxes of 128 bytes by `box_rows` rows, swizzled; outside, reads give zeros.
+int make_map(psops_xent *x, CUtensorMap *map, int type, const void *base, int64_t width, int64_t height, int64_t ld, int box_rows)
 {
-    LogitsParams P{};
-    P.h = x->at<void>(x->lay.hidden);
-    P.h_ld = (int)x->lay.padded;
-    P.dim = (int)x->lay.padded;
+    const int bytes = type == PSOPS_F32 ? 4 : 2;
+    const cuuint64_t size[2] = {(cuuint64_t)width, (cuuint64_t)height};
+    const cuuint64_t stride[1] = {(cuuint64_t)(ld * bytes)};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / bytes), (cuuint32_t)box_rows}, step[2] = {1, 1};
+    const CUtensorMapDataType kind = type == PSOPS_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                     : type == PSOPS_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    const CUresult r = x->encode(map, kind, 2, const_cast<void *>(base), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return PSOPS_OK;
+    std::snprintf(x->err, sizeof(x->err), "cuTensorMapEncodeTiled: error %d", (int)r);
+    return PSOPS_ECUDA;
+}
+
+using ProductKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ProductParams);
+template <class T>
+ProductKernel product_of(int job)
+{
+    return job == kLoss ? psops_xent_product_kernel<T, kLoss> : job == kDlogits ? psops_xent_product_kernel<T, kDlogits>
+           : job == kDh ? psops_xent_product_kernel<T, kDh> : psops_xent_product_kernel<T, kDw>;
+}
+ProductKernel product_of(const psops_xent *x, int job)
+{
+    return x->cfg.type == PSOPS_F16 ? product_of<__half>(job) : product_of<__nv_bfloat16>(job);
+}
+
+// `works`: tiles (times shares) if every token counts.
+int product(psops_xent *x, int job, int64_t works, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const ProductParams &P)
+{
+    const unsigned grid = 2u * (unsigned)std::max<int64_t>(1, std::min<int64_t>(works, x->sms / 2));
+    product_of(x, job)<<<grid, kProductThreads, kProductShared, x->stream>>>(a, b, out, P);
+    return x->launched("psops_xent_product_kernel");
+}
+
+ProductParams product_params(const psops_xent *x)
+{
+    ProductParams P{};
     P.control = x->control();
+    P.splits = 1;
     P.label = x->at<int>(x->lay.label);
+    P.row_lse = x->at<float>(x->lay.row_lse);
+    P.row_scale = x->at<float>(x->lay.row_scale);
     P.stats = x->at<float2>(x->lay.stats);
     P.stats_ld = x->lay.rows;
     P.label_logit = x->at<float>(x->lay.label_logit);
-    P.row_lse = x->at<float>(x->lay.row_lse);
-    P.row_scale = x->at<float>(x->lay.row_scale);
-    P.dlogits = x->at<void>(x->lay.dlogits);
-    P.dlogits_ld = x->lay.piece;
     return P;
 }
 
-template <class T>
+#define PSOPS_DO(call)                       \
+    do {                                     \
+        const int rc_ = (call);              \
+        if (rc_ != PSOPS_OK) return rc_;     \
+    } while (0)
+
+// What a call's products have in common.
+struct Call {
+    int64_t padded, rows, some_rows, tiles_m;   // rows: if every token counts, whole tiles; some_rows: whole steps
+    CUtensorMap hidden;                         // rows by dim, summed over dim
+};
+
+int open_call(psops_xent *x, int64_t tokens, Call *c)
+{
+    c->padded = x->lay.padded;
+    c->rows = (int64_t)round_up((size_t)std::max<int64_t>(1, tokens), kTileRows);
+    c->some_rows = (int64_t)round_up((size_t)std::max<int64_t>(1, tokens), kStepK);
+    c->tiles_m = c->rows / kTile;
+    return make_map(x, &c->hidden, x->cfg.type, x->at<void>(x->lay.hidden), c->padded, c->some_rows, c->padded, kHalf);
+}
+
 int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinParams J)
 {
-    const unsigned tiles_m = (unsigned)(round_up((size_t)std::max<int64_t>(1, tokens), kTileRows) / kSimple);
-    for (int64_t first = 0; first < x->cfg.vocab; first += x->lay.piece) {
-        LogitsParams P = logits_params(x);
-        const int64_t count = std::min(x->lay.piece, x->cfg.vocab - first);
-        const int rc = piece_of_w(x, w, w_ld, first, count, &P.w, &P.w_ld);
-        if (rc != PSOPS_OK) return rc;
+    Call c;
+    PSOPS_DO(open_call(x, tokens, &c));
+    // w in place is one piece
+    const bool in_place = x->cfg.dim % 8 == 0 && aligned16(w, w_ld);
+    const int64_t piece = in_place ? x->cfg.vocab : x->lay.piece;
+    for (int64_t first = 0; first < x->cfg.vocab; first += piece) {
+        const int64_t count = std::min(piece, x->cfg.vocab - first);
+        const void *rows_of_w;
+        int64_t ld;
+        CUtensorMap weights;
+        PSOPS_DO(piece_of_w(x, w, w_ld, first, count, &rows_of_w, &ld));
+        PSOPS_DO(make_map(x, &weights, x->cfg.type, rows_of_w, c.padded, count, ld, kHalf));
+        ProductParams P = product_params(x);
+        P.columns = (int)count;
+        P.depth = (int)c.padded;
         P.first = (int)first;
-        P.count = (int)count;
-        psops_xent_logits_kernel<T, false><<<dim3((unsigned)ceil_div(count, kSimple), tiles_m), kSimpleThreads, 0, x->stream>>>(P);
-        if (x->launched("psops_xent_logits_kernel") != PSOPS_OK) return PSOPS_ECUDA;
+        PSOPS_DO(product(x, kLoss, c.tiles_m * ceil_div(count, kTile), c.hidden, weights, weights, P));
     }
     J.stats = x->at<float2>(x->lay.stats);
     J.stats_ld = x->lay.rows;
@@ -190,55 +267,71 @@ int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinPara
     return x->launched("psops_xent_join_kernel");
 }
 
-template <class T>
 int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *dh, int64_t dh_ld, void *dw, int64_t dw_ld)
 {
-    const unsigned tiles_m = (unsigned)(round_up((size_t)std::max<int64_t>(1, tokens), kTileRows) / kSimple);
-    const unsigned tiles_d = (unsigned)ceil_div(x->cfg.dim, kSimple);
+    const int type = x->cfg.type;
     const bool direct = x->cfg.dim % 8 == 0 && aligned16(dw, dw_ld);
-    int rc;
+    Call c;
+    PSOPS_DO(open_call(x, tokens, &c));
+    const int64_t tiles_d = ceil_div(c.padded, kTile);
+    CUtensorMap hidden_across, dlogits_out, dlogits_along, dlogits_across, sums;
+    void *dlogits = x->at<void>(x->lay.dlogits);
+    PSOPS_DO(make_map(x, &hidden_across, type, x->at<void>(x->lay.hidden), c.padded, c.some_rows, c.padded, kStepK));
+    PSOPS_DO(make_map(x, &dlogits_out, type, dlogits, x->lay.piece, c.some_rows, x->lay.piece, 32));
+    PSOPS_DO(make_map(x, &dlogits_along, type, dlogits, x->lay.piece, c.some_rows, x->lay.piece, kHalf));
+    PSOPS_DO(make_map(x, &dlogits_across, type, dlogits, x->lay.piece, c.some_rows, x->lay.piece, kStepK));
+    PSOPS_DO(make_map(x, &sums, PSOPS_F32, x->at<void>(x->lay.sums), c.padded, x->lay.sum_rows, c.padded, 32));
+    // every piece gives every share something to add up, but the last piece may be short
+    const int64_t last = x->cfg.vocab - (x->cfg.vocab - 1) / x->lay.piece * x->lay.piece;
+    const int64_t shares = std::max<int64_t>(1, std::min({x->lay.sum_rows / c.rows, shares_of(c.rows, c.padded), ceil_div(last, kStepK)}));
     for (int64_t first = 0; first < x->cfg.vocab; first += x->lay.piece) {
-        LogitsParams P = logits_params(x);
         const int64_t count = std::min(x->lay.piece, x->cfg.vocab - first);
-        rc = piece_of_w(x, w, w_ld, first, count, &P.w, &P.w_ld);
-        if (rc != PSOPS_OK) return rc;
+        const void *rows_of_w;
+        int64_t ld;
+        CUtensorMap weights;
+        PSOPS_DO(piece_of_w(x, w, w_ld, first, count, &rows_of_w, &ld));
+        PSOPS_DO(make_map(x, &weights, type, rows_of_w, c.padded, count, ld, kHalf));
+        ProductParams P = product_params(x);
+        P.columns = (int)count;
+        P.depth = (int)c.padded;
         P.first = (int)first;
-        P.count = (int)count;
-        psops_xent_logits_kernel<T, true><<<dim3((unsigned)ceil_div(count, kSimple), tiles_m), kSimpleThreads, 0, x->stream>>>(P);
-        if (x->launched("psops_xent_logits_kernel") != PSOPS_OK) return PSOPS_ECUDA;
+        PSOPS_DO(product(x, kDlogits, c.tiles_m * ceil_div(count, kTile), c.hidden, weights, dlogits_out, P));
         if (dh != nullptr) {
-            DhParams Q{};
-            Q.dlogits = P.dlogits; Q.dlogits_ld = P.dlogits_ld; Q.w = P.w; Q.w_ld = P.w_ld;
-            Q.dim = (int)x->lay.padded; Q.count = (int)count; Q.add = first > 0; Q.control = x->control();
-            Q.sums = x->at<float>(x->lay.sums); Q.sums_ld = x->lay.padded;
-            psops_xent_dh_kernel<T><<<dim3(tiles_d, tiles_m), kSimpleThreads, 0, x->stream>>>(Q);
-            if (x->launched("psops_xent_dh_kernel") != PSOPS_OK) return PSOPS_ECUDA;
+            PSOPS_DO(make_map(x, &weights, type, rows_of_w, c.padded, count, ld, kStepK));
+            P.columns = (int)c.padded;
+            P.depth = (int)count;
+            P.splits = (int)shares;
+            P.split_rows = (int)c.rows;
+            P.add = first > 0;
+            PSOPS_DO(product(x, kDh, c.tiles_m * tiles_d * shares, dlogits_along, weights, sums, P));
         }
         if (dw != nullptr) {
-            DwParams Q{};
-            Q.dlogits = P.dlogits; Q.dlogits_ld = P.dlogits_ld; Q.h = P.h; Q.h_ld = P.h_ld;
-            Q.dim = (int)x->lay.padded; Q.count = (int)count; Q.control = x->control();
-            Q.dw = direct ? (void *)((uint16_t *)dw + first * dw_ld) : x->at<void>(x->lay.dw);
-            Q.dw_ld = direct ? dw_ld : x->lay.padded;
-            psops_xent_dw_kernel<T><<<dim3(tiles_d, (unsigned)ceil_div(count, kSimple)), kSimpleThreads, 0, x->stream>>>(Q);
-            if (x->launched("psops_xent_dw_kernel") != PSOPS_OK) return PSOPS_ECUDA;
+            uint16_t *to = direct ? (uint16_t *)dw + first * dw_ld : x->at<uint16_t>(x->lay.dw);
+            CUtensorMap dw_out;
+            PSOPS_DO(make_map(x, &dw_out, type, to, c.padded, count, direct ? dw_ld : c.padded, 32));
+            P.columns = (int)c.padded;
+            P.result_rows = (int)count;
+            PSOPS_DO(product(x, kDw, ceil_div(count, kTile) * tiles_d, dlogits_across, hidden_across, dw_out, P));
             if (!direct) {
                 const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(count, kCopyThreads / 32), (int64_t)x->sms * 8);
-                psops_xent_unpack_kernel<<<grid, kCopyThreads, 0, x->stream>>>(x->at<uint16_t>(x->lay.dw), (int)x->lay.padded, count,
-                                                                              (int)x->cfg.dim, (uint16_t *)dw + first * dw_ld, dw_ld);
-                if (x->launched("psops_xent_unpack_kernel") != PSOPS_OK) return PSOPS_ECUDA;
+                psops_xent_unpack_kernel<<<grid, kCopyThreads, 0, x->stream>>>(to, (int)c.padded, count, (int)x->cfg.dim,
+                                                                              (uint16_t *)dw + first * dw_ld, dw_ld);
+                PSOPS_DO(x->launched("psops_xent_unpack_kernel"));
             }
         }
     }
-    if (dh != nullptr && tokens > 0) {
-        const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(tokens, kCopyThreads / 32), (int64_t)x->sms * 8);
-        psops_xent_dh_out_kernel<T><<<grid, kCopyThreads, 0, x->stream>>>(x->at<float>(x->lay.sums), x->lay.padded, x->control(),
-                                                                         x->at<int>(x->lay.compact_of), (int)tokens,
-                                                                         (int)x->cfg.dim, (T *)dh, dh_ld);
-        rc = x->launched("psops_xent_dh_out_kernel");
-        if (rc != PSOPS_OK) return rc;
-    }
-    return PSOPS_OK;
+    if (dh == nullptr || tokens == 0) return PSOPS_OK;
+    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(tokens, kCopyThreads / 32), (int64_t)x->sms * 8);
+    const bool aligned = ((uintptr_t)dh & 7u) == 0 && dh_ld % 4 == 0;
+    if (type == PSOPS_F16)
+        psops_xent_dh_out_kernel<__half><<<grid, kCopyThreads, 0, x->stream>>>(x->at<float>(x->lay.sums), c.padded, (int)shares, c.rows,
+                                                                              x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
+                                                                              (int)x->cfg.dim, aligned, (__half *)dh, dh_ld);
+    else
+        psops_xent_dh_out_kernel<__nv_bfloat16><<<grid, kCopyThreads, 0, x->stream>>>(x->at<float>(x->lay.sums), c.padded, (int)shares, c.rows,
+                                                                                     x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
+                                                                                     (int)x->cfg.dim, aligned, (__nv_bfloat16 *)dh, dh_ld);
+    return x->launched("psops_xent_dh_out_kernel");
 }
 
 } // namespace
@@ -263,6 +356,13 @@ int psops_xent_create(psops_xent **out, const psops_xent_config *cfg, void *d_wo
     x->stream = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaGetDevice(&x->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&x->sms, cudaDevAttrMultiProcessorCount, x->device);
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    if (e == cudaSuccess)
+        e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", (void **)&x->encode, 12000, cudaEnableDefault, &found);
+    if (e == cudaSuccess && found != cudaDriverEntryPointSuccess) e = cudaErrorNotSupported;
+    for (int job = kLoss; e == cudaSuccess && job <= kDw; ++job)
+        e = cudaFuncSetAttribute((const void *)product_of(x, job), cudaFuncAttributeMaxDynamicSharedMemorySize, kProductShared);
+    if (e == cudaSuccess) e = cudaMemsetAsync(x->control(), 0, sizeof(XentControl), x->stream);
     if (e != cudaSuccess) {
         delete x;
         return PSOPS_ECUDA;
@@ -292,7 +392,7 @@ int psops_xent_forward(psops_xent *x, const void *d_h, int64_t h_ld, const void 
     J.lse_out = d_lse;
     J.loss = d_loss;
     J.reduction = reduction;
-    return x->cfg.type == PSOPS_F16 ? forward<__half>(x, d_w, w_ld, tokens, J) : forward<__nv_bfloat16>(x, d_w, w_ld, tokens, J);
+    return forward(x, d_w, w_ld, tokens, J);
 }
 
 int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void *d_w, int64_t w_ld,
@@ -317,8 +417,7 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
     P.reduction = reduction;
     rc = gather(x, P, d_h, h_ld);
     if (rc != PSOPS_OK) return rc;
-    return x->cfg.type == PSOPS_F16 ? backward<__half>(x, d_w, w_ld, tokens, d_dh, dh_ld, d_dw, dw_ld)
-                                    : backward<__nv_bfloat16>(x, d_w, w_ld, tokens, d_dh, dh_ld, d_dw, dw_ld);
+    return backward(x, d_w, w_ld, tokens, d_dh, dh_ld, d_dw, dw_ld);
 }
 
 int64_t psops_xent_launch_count(const psops_xent *x) { return x ? x->launches : 0; }

@@ -14,10 +14,12 @@
 
 #include <cstdint>
 
+#include "psops_umma.cuh"
+
 namespace {
 
 constexpr int kTileRows = 256;                   // compact rows are padded to this
-constexpr int kTileCols = 256;                   // vocabulary entries of a logits tile
+constexpr int kTileCols = 256;                   // a piece of the vocabulary is a multiple of this
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -27,13 +29,6 @@ struct XentControl {
     float unscale;                               // power of two: gradient sums * unscale = gradients
     int error;
 };
-
-template <class T> __device__ __forceinline__ float widen16(T x);
-template <> __device__ __forceinline__ float widen16(__half x) { return __half2float(x); }
-template <> __device__ __forceinline__ float widen16(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <class T> __device__ __forceinline__ T narrow16(float x);
-template <> __device__ __forceinline__ __half narrow16(float x) { return __float2half_rn(x); }
-template <> __device__ __forceinline__ __nv_bfloat16 narrow16(float x) { return __float2bfloat16_rn(x); }
 
 struct IndexParams {
     const long long *targets;
@@ -178,146 +173,377 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const u
 }
 
 // ---------------------------------------------------------------------------
-// Products: 64 x 64 tiles of fp32 sums, 256 threads with 4 x 4 sums each
+// Products on the tensor cores
+//
+// One kernel does all of them, persistent, a pair of CTAs to a 256 x 256 tile
+// of the result, 64 of the summed axis a step:
+//
+//   job       rows of the result   columns        summed over    what becomes of a tile
+//   kLoss     compact rows         vocabulary     dim            softmax maxima and sums
+//   kDlogits  compact rows         vocabulary     dim            the logits' gradient, 16 bits
+//   kDh       compact rows         dim            vocabulary     fp32 sums, added up over pieces
+//   kDw       vocabulary           dim            compact rows   dw, 16 bits
+//
+// Warp 0 of each CTA copies its half of both operands (128 rows of A, 128 of
+// B: 32 KB a step, kStages in flight), one thread of the first CTA issues the
+// products, warps 4 to 11 of each CTA turn the other one of two 256-column
+// accumulators into the job's output meanwhile.  kDh and kDw read operands whose
+// summed axis runs across the rows in memory: the copies bring 64 x 64 boxes,
+// and the product's descriptors say so; nothing is transposed.
 // ---------------------------------------------------------------------------
-constexpr int kSimple = 64, kSimpleK = 16, kSimpleThreads = 256;
+enum Job { kLoss = 0, kDlogits = 1, kDh = 2, kDw = 3 };
 
-template <class LoadA, class LoadB>
-__device__ __forceinline__ void simple_tile(LoadA a, LoadB b, int depth, float (&acc)[4][4])
-{
-    __shared__ float sa[kSimpleK][kSimple + 1], sb[kSimpleK][kSimple + 1];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
-    for (int k0 = 0; k0 < depth; k0 += kSimpleK) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < kSimple * kSimpleK; i += kSimpleThreads) {
-            const int k = i % kSimpleK, m = i / kSimpleK;
-            sa[k][m] = k0 + k < depth ? a(m, k0 + k) : 0.0f;
-            sb[k][m] = k0 + k < depth ? b(m, k0 + k) : 0.0f;
-        }
-        __syncthreads();
-        for (int k = 0; k < kSimpleK; ++k)
-            for (int i = 0; i < 4; ++i)
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(sa[k][ty * 4 + i], sb[k][tx * 4 + j], acc[i][j]);
-    }
-}
+constexpr int kTile = 256, kHalf = 128, kStepK = 64;
+constexpr int kStages = 6;
+constexpr int kStageBytes = 2 * kHalf * kStepK * 2;              // this CTA's halves of A and B
+constexpr int kOutBytes = 32 * 128;                              // a warp's 32 rows of 128 bytes on their way out
+constexpr int kOutWarps = 8;
+constexpr int kProductThreads = 384;
+constexpr int kProductShared = kStages * kStageBytes + kOutWarps * kOutBytes + 1024;   // 1024: alignment
+constexpr int kChainSteps = 8;                                   // steps of a logit summed by the tensor cores in one go
+constexpr int kGroupTiles = 8;                                   // row tiles that share columns in L2
 
-struct LogitsParams {
-    const void *h, *w;                           // compact hidden states; the piece's rows of w
-    int64_t w_ld;
-    int h_ld, dim;
-    int first, count;                            // the piece: vocabulary entries [first, first + count)
-    const XentControl *control;
+struct ProductParams {
+    XentControl *control;
+    int columns;                                 // kLoss, kDlogits: entries of the piece; kDh, kDw: padded dim
+    int depth;                                   // kLoss, kDlogits: padded dim; kDh: entries of the piece
+    int result_rows;                             // kDw: entries of the piece
+    int splits;                                  // kDh: the summed axis in so many shares, sums apart
+    int split_rows;                              // kDh: rows between the shares' sums
+    int first;                                   // first vocabulary entry of the piece
+    bool add;                                    // kDh: add to the sums of the pieces before
     const int *label;
-    float2 *stats;                               // (max, sum of exp2) by part of the vocabulary and compact row, base 2
+    const float *row_lse, *row_scale;
+    float2 *stats;                               // (max, sum of exp2) by 128 vocabulary entries and compact row, base 2
     long long stats_ld;
     float *label_logit;
-    const float *row_lse, *row_scale;
-    void *dlogits;                               // compact rows x piece
-    long long dlogits_ld;
 };
 
-template <class T, bool GRADS>
-__global__ void __launch_bounds__(kSimpleThreads) psops_xent_logits_kernel(const LogitsParams P)
+__device__ __forceinline__ float exp2_fast(float x)
 {
-    const int rows = P.control->rows;
-    const int whole = max(1, (rows + kTileRows - 1) / kTileRows) * kTileRows;
-    const int m0 = blockIdx.y * kSimple, n0 = blockIdx.x * kSimple;
-    if (m0 >= whole) return;
-    const T *h = (const T *)P.h, *w = (const T *)P.w;
-    float acc[4][4];
-    simple_tile([&](int m, int k) { return widen16(h[(long long)(m0 + m) * P.h_ld + k]); },
-                [&](int n, int k) { return n0 + n < P.count ? widen16(w[(n0 + n) * P.w_ld + k]) : 0.0f; }, P.dim, acc);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int i = 0; i < 4; ++i) {
-        const int r = m0 + ty * 4 + i;
-        const int y = r < rows ? P.label[r] - P.first : -1;
-        float top = -INFINITY;
-        for (int j = 0; j < 4; ++j) {
-            const int c = n0 + tx * 4 + j;
-            if (c == y && !GRADS) P.label_logit[r] = acc[i][j];
-            acc[i][j] *= kLog2e;
-            if (c >= P.count) acc[i][j] = -INFINITY;
-            top = fmaxf(top, acc[i][j]);
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <class T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    uint32_t u;
+    memcpy(&u, &h, 4);
+    return u;
+}
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    uint32_t u;
+    memcpy(&u, &h, 4);
+    return u;
+}
+
+// x = value where at == j; written out so that the registers of a row are not put into memory to be indexed
+__device__ __forceinline__ void take_if(float &x, int at, int j, uint32_t value)
+{
+    asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, %2;\n\t@p mov.b32 %0, %3;\n\t}" : "+f"(x) : "r"(at), "r"(j), "r"(value));
+}
+
+struct Work { int m, n, split; };                // tile of the result, share of the summed axis
+
+// Tiles in bands of kGroupTiles row tiles, column by column, so that the pairs
+// running at one time share both operands in L2.
+__device__ __forceinline__ Work work_of(int i, int tiles_m, int tiles_n)
+{
+    const int tiles = tiles_m * tiles_n;
+    Work w;
+    w.split = i / tiles;
+    i -= w.split * tiles;
+    const int band = i / (kGroupTiles * tiles_n);
+    const int in_band = i - band * kGroupTiles * tiles_n;
+    const int high = min(kGroupTiles, tiles_m - band * kGroupTiles);
+    w.n = in_band / high;
+    w.m = band * kGroupTiles + in_band - w.n * high;
+    return w;
+}
+
+template <class T, int JOB>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
+psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                          const __grid_constant__ CUtensorMap map_out, const ProductParams P)
+{
+    constexpr bool kAAcross = JOB == kDw, kBAcross = JOB == kDh || JOB == kDw;
+    constexpr bool kChained = JOB == kLoss || JOB == kDlogits;
+    constexpr int kChain = kChained ? kChainSteps : 1 << 30;
+    constexpr uint32_t kInstruction = umma::instruction(__is_same(T, __nv_bfloat16), kAAcross, kBAcross, kTile, kTile);
+
+    extern __shared__ uint8_t raw[];
+    __shared__ alignas(8) uint64_t bar_full[kStages], bar_empty[kStages], bar_sum[2], bar_free[2];
+    __shared__ uint32_t tensor_base_slot;
+    __shared__ int failed_slot;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = umma::cta_rank();
+    volatile int *failed = &failed_slot;
+    const uint32_t stages = (umma::shared_address(raw) + 1023u) & ~1023u;
+    const uint32_t outs = stages + kStages * kStageBytes;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            umma::barrier_init(umma::shared_address(&bar_full[s]), 1);
+            umma::barrier_init(umma::shared_address(&bar_empty[s]), 1);
         }
-        if (!GRADS) {
-            for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            const float ref = top > -INFINITY ? top : 0.0f;
-            float s = 0.0f;
-            for (int j = 0; j < 4; ++j) s += exp2f(acc[i][j] - ref);
-            for (int off = 8; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-            if (tx == 0) P.stats[(long long)((P.first + n0) / kSimple) * P.stats_ld + r] = make_float2(top, s);
-        } else {
-            const float lse = r < rows ? P.row_lse[r] : 0.0f, g = r < rows ? P.row_scale[r] : 0.0f;
-            for (int j = 0; j < 4; ++j) {
-                const int c = n0 + tx * 4 + j;
-                float d = 0.0f;
-                if (r < rows && c < P.count) d = (exp2f(acc[i][j] - lse) - (c == y ? 1.0f : 0.0f)) * g;
-                if (c < P.dlogits_ld) ((T *)P.dlogits)[r * P.dlogits_ld + c] = narrow16<T>(d);
-            }
+        for (int b = 0; b < 2; ++b) {
+            umma::barrier_init(umma::shared_address(&bar_sum[b]), 1);
+            umma::barrier_init(umma::shared_address(&bar_free[b]), 2 * kOutWarps);
         }
+        failed_slot = 0;
+        umma::barrier_init_done();
+        umma::prefetch_map(&map_a);
+        umma::prefetch_map(&map_b);
     }
-}
+    if (warp == 2) umma::tensor_memory_take(umma::shared_address(&tensor_base_slot));
+    umma::fence_before();
+    __syncthreads();
+    umma::cluster_sync();
+    umma::fence_after();
+    const uint32_t tensor_base = tensor_base_slot;
 
-struct DhParams {
-    const void *dlogits, *w;
-    long long dlogits_ld, w_ld;
-    int dim, count;
-    bool add;
-    const XentControl *control;
-    float *sums;
-    long long sums_ld;
-};
-
-template <class T>
-__global__ void __launch_bounds__(kSimpleThreads) psops_xent_dh_kernel(const DhParams P)
-{
     const int rows = P.control->rows;
-    const int m0 = blockIdx.y * kSimple, n0 = blockIdx.x * kSimple;
-    if (m0 >= rows) return;
-    const T *d = (const T *)P.dlogits, *w = (const T *)P.w;
-    float acc[4][4];
-    simple_tile([&](int m, int k) { return widen16(d[(m0 + m) * P.dlogits_ld + k]); },
-                [&](int n, int k) { return n0 + n < P.dim ? widen16(w[k * P.w_ld + n0 + n]) : 0.0f; }, P.count, acc);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const int r = m0 + ty * 4 + i, c = n0 + tx * 4 + j;
-            if (r < rows && c < P.dim) {
-                float *at = P.sums + r * P.sums_ld + c;
-                *at = P.add ? *at + acc[i][j] : acc[i][j];
+    const int some_rows = max(1, rows);
+    const int tiles_m = JOB == kDw ? (P.result_rows + kTile - 1) / kTile : JOB == kDh ? (rows + kTile - 1) / kTile : (some_rows + kTile - 1) / kTile;
+    const int tiles_n = (P.columns + kTile - 1) / kTile;
+    const int steps = ((JOB == kDw ? some_rows : P.depth) + kStepK - 1) / kStepK;
+    const int splits = JOB == kDh ? P.splits : 1;
+    const int works = tiles_m * tiles_n * splits;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+
+    if (warp == 0 && lane == 0) {
+        // ---- copies in
+        int s = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int i = pair; i < works && ok; i += pairs) {
+            const Work w = work_of(i, tiles_m, tiles_n);
+            const int k_first = (int)((long long)steps * w.split / splits), k_last = (int)((long long)steps * (w.split + 1) / splits);
+            const int m0 = w.m * kTile + (int)rank * kHalf, n0 = w.n * kTile + (int)rank * kHalf;
+            for (int k = k_first; k < k_last; ++k) {
+                if (!umma::barrier_wait(umma::shared_address(&bar_empty[s]), phase ^ 1u, failed)) { ok = false; break; }
+                const uint32_t full = umma::in_cta(umma::shared_address(&bar_full[s]), 0);
+                if (rank == 0) umma::barrier_expect(umma::shared_address(&bar_full[s]), 2 * kStageBytes);
+                const uint32_t a = stages + s * kStageBytes, b = a + kStageBytes / 2;
+                if (kAAcross) {
+                    umma::tensor_load(a, &map_a, m0, k * kStepK, full);
+                    umma::tensor_load(a + umma::kAcross, &map_a, m0 + 64, k * kStepK, full);
+                } else {
+                    umma::tensor_load(a, &map_a, k * kStepK, m0, full);
+                }
+                if (kBAcross) {
+                    umma::tensor_load(b, &map_b, n0, k * kStepK, full);
+                    umma::tensor_load(b + umma::kAcross, &map_b, n0 + 64, k * kStepK, full);
+                } else {
+                    umma::tensor_load(b, &map_b, k * kStepK, n0, full);
+                }
+                if (++s == kStages) { s = 0; phase ^= 1u; }
             }
         }
-}
-
-struct DwParams {
-    const void *dlogits, *h;
-    long long dlogits_ld;
-    int h_ld, dim, count;
-    const XentControl *control;
-    void *dw;
-    long long dw_ld;
-};
-
-template <class T>
-__global__ void __launch_bounds__(kSimpleThreads) psops_xent_dw_kernel(const DwParams P)
-{
-    const int rows = P.control->rows;
-    const float unscale = P.control->unscale;
-    const long long m0 = (long long)blockIdx.y * kSimple;
-    const int n0 = blockIdx.x * kSimple;
-    const T *d = (const T *)P.dlogits, *h = (const T *)P.h;
-    float acc[4][4];
-    simple_tile([&](int m, int k) { return m0 + m < P.count ? widen16(d[k * P.dlogits_ld + m0 + m]) : 0.0f; },
-                [&](int n, int k) { return n0 + n < P.dim ? widen16(h[(long long)k * P.h_ld + n0 + n]) : 0.0f; }, rows, acc);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) {
-            const long long r = m0 + ty * 4 + i;
-            const int c = n0 + tx * 4 + j;
-            if (r < P.count && c < P.dim) ((T *)P.dw)[r * P.dw_ld + c] = narrow16<T>(acc[i][j] * unscale);
+        if (!ok) __nanosleep(1000000);               // copies in flight land long before
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        // ---- products
+        int s = 0, buffer = 0;
+        uint32_t phase = 0, buffer_phase = 0;
+        bool ok = true;
+        for (int i = pair; i < works && ok; i += pairs) {
+            const Work w = work_of(i, tiles_m, tiles_n);
+            const int k_first = (int)((long long)steps * w.split / splits), k_last = (int)((long long)steps * (w.split + 1) / splits);
+            for (int k = k_first; k < k_last; ++k) {
+                const int link = (k - k_first) % kChain;           // place within a chain of sums
+                if (link == 0) {
+                    if (!umma::barrier_wait(umma::shared_address(&bar_free[buffer]), buffer_phase ^ 1u, failed)) { ok = false; break; }
+                    umma::fence_after();
+                }
+                const uint32_t sums = tensor_base + buffer * kTile;
+                if (!umma::barrier_wait(umma::shared_address(&bar_full[s]), phase, failed)) { ok = false; break; }
+                umma::fence_after();
+                const uint32_t a = stages + s * kStageBytes, b = a + kStageBytes / 2;
+                const uint64_t da = umma::operand(a, kAAcross), db = umma::operand(b, kBAcross);
+#pragma unroll
+                for (int j = 0; j < kStepK / 16; ++j)      // 16 of the summed axis: 32 bytes along a row, or two groups of 8 rows
+                    umma::multiply(sums, da + (kAAcross ? j * 128 : j * 2), db + (kBAcross ? j * 128 : j * 2), kInstruction, link > 0 || j > 0);
+                umma::products_arrive(umma::shared_address(&bar_empty[s]));
+                if (++s == kStages) { s = 0; phase ^= 1u; }
+                if (link == kChain - 1 || k == k_last - 1) {
+                    umma::products_arrive(umma::shared_address(&bar_sum[buffer]));
+                    if (++buffer == 2) { buffer = 0; buffer_phase ^= 1u; }
+                }
+            }
         }
+    } else if (warp >= 4) {
+        // ---- results: this warp has 32 rows (its quarter of tensor memory) and 128 columns
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t out = outs + (warp - 4) * kOutBytes;
+        const float unscale = JOB == kDw ? P.control->unscale : 1.0f;
+        int buffer = 0;
+        uint32_t phase = 0;
+        for (int i = pair; i < works; i += pairs) {
+            const Work w = work_of(i, tiles_m, tiles_n);
+            const int row0 = w.m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
+            const int col0 = w.n * kTile + half * kHalf;
+            int y = -1;
+            float lse = 0.0f, g = 0.0f;
+            if (JOB == kLoss || JOB == kDlogits) {
+                if (row < rows) y = P.label[row] - P.first - col0;
+                if (JOB == kDlogits && row < rows) {
+                    lse = P.row_lse[row];
+                    g = P.row_scale[row];
+                }
+            }
+            const uint32_t quarter_base = tensor_base + ((uint32_t)(quarter * 32) << 16) + half * kHalf;
+            float top = -INFINITY, sum = 0.0f;
+            // 64 columns from column c of this warp's, as bit patterns in u
+            auto finish = [&](int c, uint32_t *u) {
+                const int left = P.columns - (col0 + c);       // columns that exist from here on
+                if (JOB == kLoss) {
+                    if (left < 64) {
+#pragma unroll
+                        for (int j = 0; j < 64; ++j)
+                            if (j >= left) u[j] = 0xff800000u;       // -inf
+                    }
+                    if (y >= c && y < c + 64) {
+                        float mine = 0.0f;
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) take_if(mine, y - c, j, u[j]);
+                        P.label_logit[row] = mine;
+                    }
+                    float high = top;
+#pragma unroll
+                    for (int j = 0; j < 64; ++j) high = fmaxf(high, __uint_as_float(u[j]));
+                    const float ref = high > -INFINITY ? high * kLog2e : 0.0f;
+                    sum *= exp2_fast((top > -INFINITY ? top * kLog2e : -INFINITY) - ref);
+#pragma unroll
+                    for (int j = 0; j < 64; ++j) sum += exp2_fast(fmaf(__uint_as_float(u[j]), kLog2e, -ref));
+                    top = high;
+                } else {
+                    if (JOB == kDlogits) {
+                        const int hit = y - c;
+#pragma unroll
+                        for (int j = 0; j < 64; ++j)
+                            u[j] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(u[j]), kLog2e, -lse)));
+                        if (hit >= 0 && hit < 64) {
+#pragma unroll
+                            for (int j = 0; j < 64; ++j)
+                                if (j == hit) u[j] = __float_as_uint(__uint_as_float(u[j]) - 1.0f);
+                        }
+                        // rows and columns that are only padding become zeros
+                        const int mine = row < rows ? left : 0;
+#pragma unroll
+                        for (int j = 0; j < 64; ++j)
+                            u[j] = j < mine ? __float_as_uint(__uint_as_float(u[j]) * g) : 0u;
+                    } else if (JOB == kDw) {
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) * unscale);
+                    }
+                    const bool wanted = JOB == kDlogits ? row0 < (some_rows + kStepK - 1) / kStepK * kStepK
+                                        : JOB == kDh ? row0 < rows : row0 < P.result_rows;
+                    constexpr int kBoxes = JOB == kDh ? 2 : 1;         // 128 bytes a row: 32 fp32 or 64 16-bit columns
+#pragma unroll
+                    for (int box = 0; box < kBoxes; ++box) {
+                        if (lane == 0) umma::stores_read<0>();
+                        __syncwarp();
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            uint4 v;
+                            if (JOB == kDh)
+                                v = make_uint4(u[32 * box + 4 * j], u[32 * box + 4 * j + 1], u[32 * box + 4 * j + 2], u[32 * box + 4 * j + 3]);
+                            else {
+                                uint32_t p[4];
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    const int at = 8 * j + 2 * q;
+                                    p[q] = pack2<T>(__uint_as_float(u[at]), __uint_as_float(u[at + 1]));
+                                }
+                                v = make_uint4(p[0], p[1], p[2], p[3]);
+                            }
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(out + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(v.x),
+                                         "r"(v.y), "r"(v.z), "r"(v.w)
+                                         : "memory");
+                        }
+                        umma::copies_see_shared();
+                        __syncwarp();
+                        if (lane == 0) {
+                            const int x = col0 + c + box * 32;
+                            if (wanted && (JOB == kDlogits || x < P.columns)) {
+                                if (JOB == kDh && P.add) umma::tensor_add(&map_out, x, w.split * P.split_rows + row0, out);
+                                else umma::tensor_store(&map_out, x, (JOB == kDh ? w.split * P.split_rows : 0) + row0, out);
+                            }
+                            umma::stores_commit();
+                        }
+                    }
+                }
+            };
+            bool ok = true;
+            if constexpr (kChained) {
+                uint32_t total[kHalf];
+                const int chains = (steps + kChain - 1) / kChain;
+#pragma unroll 1
+                for (int q = 0; q < chains; ++q) {
+                    ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_sum[buffer]), phase, failed));
+                    if (!ok) break;
+                    umma::fence_after();
+                    const uint32_t sums = quarter_base + buffer * kTile;
+                    if (q == 0) {
+#pragma unroll
+                        for (int c = 0; c < kHalf; c += 32) umma::tensor_memory_load(sums + c, total + c);
+                        umma::tensor_memory_loaded<kHalf>(total);
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < kHalf; c += 16) {
+                            uint32_t t[16];
+                            umma::tensor_memory_load16(sums + c, t);
+                            umma::tensor_memory_loaded<16>(t);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                total[c + j] = __float_as_uint(__uint_as_float(total[c + j]) + __uint_as_float(t[j]));
+                        }
+                    }
+                    umma::fence_before();
+                    __syncwarp();
+                    if (lane == 0) umma::barrier_arrive_at(umma::in_cta(umma::shared_address(&bar_free[buffer]), 0));
+                    if (++buffer == 2) { buffer = 0; phase ^= 1u; }
+                }
+                if (!ok) break;
+                finish(0, total);
+                finish(64, total + 64);
+            } else {
+                ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_sum[buffer]), phase, failed));
+                if (!ok) break;
+                umma::fence_after();
+                const uint32_t sums = quarter_base + buffer * kTile;
+#pragma unroll 1
+                for (int c = 0; c < kHalf; c += 64) {
+                    uint32_t u[64];
+                    umma::tensor_memory_load(sums + c, u);
+                    umma::tensor_memory_load(sums + c + 32, u + 32);
+                    umma::tensor_memory_loaded<64>(u);
+                    if (c == kHalf - 64) {           // the last of this warp's sums are in registers
+                        umma::fence_before();
+                        __syncwarp();
+                        if (lane == 0) umma::barrier_arrive_at(umma::in_cta(umma::shared_address(&bar_free[buffer]), 0));
+                    }
+                    finish(c, u);
+                }
+                if (++buffer == 2) { buffer = 0; phase ^= 1u; }
+            }
+            if (JOB == kLoss && row < rows)
+                P.stats[(long long)((P.first + col0) / kHalf) * P.stats_ld + row] = make_float2(top > -INFINITY ? top * kLog2e : -INFINITY, sum);
+        }
+        if (lane == 0) umma::stores_done();
+    }
+    __syncwarp();
+    umma::fence_before();
+    __syncthreads();
+    umma::cluster_sync();                        // nobody reads the other's shared or tensor memory any more
+    umma::fence_after();
+    if (warp == 2) umma::tensor_memory_give(tensor_base);
+    if (threadIdx.x == 0 && *failed) atomicExch(&P.control->error, 1);
 }
 
 // ---------------------------------------------------------------------------
@@ -368,7 +594,7 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) psops_xent_join_kernel
         double loss = 0.0;
         if (r < rows) {
             for (int k = 1; k < kJoinParts; ++k) join(top, sum, tops[k][lane], sums[k][lane]);
-            const float lse = (top + log2f(sum)) * kLn2, mine = lse - P.label_logit[r];
+            const float lse = P.control->error ? NAN : (top + log2f(sum)) * kLn2, mine = lse - P.label_logit[r];
             const int t = P.row_of[r];
             if (P.rows_out != nullptr) P.rows_out[t] = mine;
             if (P.lse_out != nullptr) P.lse_out[t] = lse;
@@ -395,15 +621,35 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) psops_xent_join_kernel
 
 // dh in the caller's rows from the compact sums, rounded once; zero where a token is left out.
 template <class T>
-__global__ void __launch_bounds__(kCopyThreads) psops_xent_dh_out_kernel(const float *sums, long long sums_ld, const XentControl *control,
-                                                                         const int *compact_of, int tokens, int dim, T *dh, long long ld)
+__global__ void __launch_bounds__(kCopyThreads) psops_xent_dh_out_kernel(const float *sums, long long sums_ld, int splits,
+                                                                         long long split_rows, const XentControl *control,
+                                                                         const int *compact_of, int tokens, int dim, bool aligned,
+                                                                         T *dh, long long ld)
 {
-    const float unscale = control->unscale;
+    const float unscale = control->error ? NAN : control->unscale;      // a product gave up: no numbers rather than wrong ones
     const int warps = gridDim.x * (kCopyThreads / 32);
     for (int t = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); t < tokens; t += warps) {
         const int r = compact_of[t];
-        for (int d = threadIdx.x & 31; d < dim; d += 32)
-            dh[t * ld + d] = r < 0 ? narrow16<T>(0.0f) : narrow16<T>(sums[r * sums_ld + d] * unscale);
+        const float *in = sums + r * sums_ld;
+        T *out = dh + t * ld;
+        for (int d = (threadIdx.x & 31) * 4; d < dim; d += 128) {
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (r >= 0)
+                for (int s = 0; s < splits; ++s) {
+                    const float4 a = *reinterpret_cast<const float4 *>(in + s * split_rows * sums_ld + d);
+                    v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
+                }
+            const uint2 u = make_uint2(pack2<T>(v.x * unscale, v.y * unscale), pack2<T>(v.z * unscale, v.w * unscale));
+            if (aligned && d + 4 <= dim) {
+                *reinterpret_cast<uint2 *>(out + d) = u;
+            } else {
+                T e[4];
+                memcpy(e, &u, 8);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (d + j < dim) out[d + j] = e[j];
+            }
+        }
     }
 }
 
