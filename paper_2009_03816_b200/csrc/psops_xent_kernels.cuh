@@ -316,8 +316,8 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     const int works = tiles_m * tiles_n * splits;
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
-    if (warp == 0 && lane == 0) {
-        // ---- copies in
+    if (warp == 0) {
+        // ---- copies in (all lanes wait, one issues)
         int s = 0;
         uint32_t phase = 0;
         bool ok = true;
@@ -326,54 +326,62 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
             const int k_first = (int)((long long)steps * w.split / splits), k_last = (int)((long long)steps * (w.split + 1) / splits);
             const int m0 = w.m * kTile + (int)rank * kHalf, n0 = w.n * kTile + (int)rank * kHalf;
             for (int k = k_first; k < k_last; ++k) {
-                if (!umma::barrier_wait(umma::shared_address(&bar_empty[s]), phase ^ 1u, failed)) { ok = false; break; }
-                const uint32_t full = umma::in_cta(umma::shared_address(&bar_full[s]), 0);
-                if (rank == 0) umma::barrier_expect(umma::shared_address(&bar_full[s]), 2 * kStageBytes);
-                const uint32_t a = stages + s * kStageBytes, b = a + kStageBytes / 2;
-                if (kAAcross) {
-                    umma::tensor_load(a, &map_a, m0, k * kStepK, full);
-                    umma::tensor_load(a + umma::kAcross, &map_a, m0 + 64, k * kStepK, full);
-                } else {
-                    umma::tensor_load(a, &map_a, k * kStepK, m0, full);
+                ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_empty[s]), phase ^ 1u, failed));
+                if (!ok) break;
+                if (umma::elected()) {
+                    const uint32_t full = umma::in_cta(umma::shared_address(&bar_full[s]), 0);
+                    if (rank == 0) umma::barrier_expect(umma::shared_address(&bar_full[s]), 2 * kStageBytes);
+                    const uint32_t a = stages + s * kStageBytes, b = a + kStageBytes / 2;
+                    if (kAAcross) {
+                        umma::tensor_load(a, &map_a, m0, k * kStepK, full);
+                        umma::tensor_load(a + umma::kAcross, &map_a, m0 + 64, k * kStepK, full);
+                    } else {
+                        umma::tensor_load(a, &map_a, k * kStepK, m0, full);
+                    }
+                    if (kBAcross) {
+                        umma::tensor_load(b, &map_b, n0, k * kStepK, full);
+                        umma::tensor_load(b + umma::kAcross, &map_b, n0 + 64, k * kStepK, full);
+                    } else {
+                        umma::tensor_load(b, &map_b, k * kStepK, n0, full);
+                    }
                 }
-                if (kBAcross) {
-                    umma::tensor_load(b, &map_b, n0, k * kStepK, full);
-                    umma::tensor_load(b + umma::kAcross, &map_b, n0 + 64, k * kStepK, full);
-                } else {
-                    umma::tensor_load(b, &map_b, k * kStepK, n0, full);
-                }
+                __syncwarp();
                 if (++s == kStages) { s = 0; phase ^= 1u; }
             }
         }
         if (!ok) __nanosleep(1000000);               // copies in flight land long before
-    } else if (warp == 1 && lane == 0 && rank == 0) {
-        // ---- products
+    } else if (warp == 1 && rank == 0) {
+        // ---- products (all lanes wait, one issues)
         int s = 0, buffer = 0;
         uint32_t phase = 0, buffer_phase = 0;
         bool ok = true;
+        const uint64_t first_a = umma::operand(stages, kAAcross), first_b = umma::operand(stages + kStageBytes / 2, kBAcross);
         for (int i = pair; i < works && ok; i += pairs) {
             const Work w = work_of(i, tiles_m, tiles_n);
             const int k_first = (int)((long long)steps * w.split / splits), k_last = (int)((long long)steps * (w.split + 1) / splits);
             for (int k = k_first; k < k_last; ++k) {
                 const int link = (k - k_first) % kChain;           // place within a chain of sums
                 if (link == 0) {
-                    if (!umma::barrier_wait(umma::shared_address(&bar_free[buffer]), buffer_phase ^ 1u, failed)) { ok = false; break; }
+                    ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_free[buffer]), buffer_phase ^ 1u, failed));
+                    if (!ok) break;
                     umma::fence_after();
                 }
-                const uint32_t sums = tensor_base + buffer * kTile;
-                if (!umma::barrier_wait(umma::shared_address(&bar_full[s]), phase, failed)) { ok = false; break; }
+                ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_full[s]), phase, failed));
+                if (!ok) break;
                 umma::fence_after();
-                const uint32_t a = stages + s * kStageBytes, b = a + kStageBytes / 2;
-                const uint64_t da = umma::operand(a, kAAcross), db = umma::operand(b, kBAcross);
+                const bool ends = link == kChain - 1 || k == k_last - 1;
+                if (umma::elected()) {
+                    const uint32_t sums = tensor_base + buffer * kTile;
+                    const uint64_t da = first_a + (uint32_t)s * (kStageBytes >> 4), db = first_b + (uint32_t)s * (kStageBytes >> 4);
 #pragma unroll
-                for (int j = 0; j < kStepK / 16; ++j)      // 16 of the summed axis: 32 bytes along a row, or two groups of 8 rows
-                    umma::multiply(sums, da + (kAAcross ? j * 128 : j * 2), db + (kBAcross ? j * 128 : j * 2), kInstruction, link > 0 || j > 0);
-                umma::products_arrive(umma::shared_address(&bar_empty[s]));
-                if (++s == kStages) { s = 0; phase ^= 1u; }
-                if (link == kChain - 1 || k == k_last - 1) {
-                    umma::products_arrive(umma::shared_address(&bar_sum[buffer]));
-                    if (++buffer == 2) { buffer = 0; buffer_phase ^= 1u; }
+                    for (int j = 0; j < kStepK / 16; ++j)  // 16 of the summed axis: 32 bytes along a row, or two groups of 8 rows
+                        umma::multiply(sums, da + (kAAcross ? j * 128 : j * 2), db + (kBAcross ? j * 128 : j * 2), kInstruction, link > 0 || j > 0);
+                    umma::products_arrive(umma::shared_address(&bar_empty[s]));
+                    if (ends) umma::products_arrive(umma::shared_address(&bar_sum[buffer]));
                 }
+                __syncwarp();
+                if (++s == kStages) { s = 0; phase ^= 1u; }
+                if (ends && ++buffer == 2) { buffer = 0; buffer_phase ^= 1u; }
             }
         }
     } else if (warp >= 4) {
