@@ -56,13 +56,22 @@ struct AdamwParams {
     unsigned n_chunks;
 };
 
-struct alignas(32) Eight { float x[8]; };
+// Eight elements as they lie in memory, and as numbers.
+template <class T> struct Eight { uint32_t w[2 * sizeof(T)]; };
 
-__device__ __forceinline__ void load_eight(const float *p, float (&x)[8])
+__device__ __forceinline__ void load_eight(const void *p, uint32_t (&w)[8])
 {
-    asm volatile("ld.global.v8.f32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
                  : "l"(p));
+}
+__device__ __forceinline__ void load_eight(const void *p, uint32_t (&w)[4])
+{
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+}
+__device__ __forceinline__ void load_eight(const void *p, uint32_t (&w)[2])
+{
+    asm volatile("ld.global.L1::no_allocate.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
 }
 __device__ __forceinline__ void store_eight(float *p, const float (&x)[8])
 {
@@ -72,11 +81,9 @@ __device__ __forceinline__ void store_eight(float *p, const float (&x)[8])
 }
 __device__ __forceinline__ float2 widen(const __half2 h) { return __half22float2(h); }
 __device__ __forceinline__ float2 widen(const __nv_bfloat162 h) { return __bfloat1622float2(h); }
-template <class T2, class T>
-__device__ __forceinline__ void load_eight_16(const T *p, float (&x)[8])
+template <class T2>
+__device__ __forceinline__ void widen_eight(const uint32_t (&w)[4], float (&x)[8])
 {
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const unsigned w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         T2 h;
@@ -86,8 +93,13 @@ __device__ __forceinline__ void load_eight_16(const T *p, float (&x)[8])
         x[2 * i + 1] = f.y;
     }
 }
-__device__ __forceinline__ void load_eight(const __half *p, float (&x)[8]) { load_eight_16<__half2>(p, x); }
-__device__ __forceinline__ void load_eight(const __nv_bfloat16 *p, float (&x)[8]) { load_eight_16<__nv_bfloat162>(p, x); }
+__device__ __forceinline__ void numbers(const Eight<float> &e, float (&x)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(e.w[j]);
+}
+__device__ __forceinline__ void numbers(const Eight<__half> &e, float (&x)[8]) { widen_eight<__half2>(e.w, x); }
+__device__ __forceinline__ void numbers(const Eight<__nv_bfloat16> &e, float (&x)[8]) { widen_eight<__nv_bfloat162>(e.w, x); }
 
 __device__ __forceinline__ __half2 narrow2(const __half *, float a, float b) { return __floats2half2_rn(a, b); }
 __device__ __forceinline__ __nv_bfloat162 narrow2(const __nv_bfloat16 *, float a, float b) { return __floats2bfloat162_rn(a, b); }
@@ -121,13 +133,11 @@ __device__ __forceinline__ unsigned short q8_encode2(float a, float b)
 {
     return (unsigned short)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ void load_eight(const Q8 *p, float (&x)[8])
+__device__ __forceinline__ void numbers(const Eight<Q8> &e, float (&x)[8])
 {
-    const uint2 u = *reinterpret_cast<const uint2 *>(p);
-    const unsigned w[2] = {u.x, u.y};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 f = q8_decode2((unsigned short)(w[i >> 1] >> (16 * (i & 1))));
+        const float2 f = q8_decode2((unsigned short)(e.w[i >> 1] >> (16 * (i & 1))));
         x[2 * i] = f.x;
         x[2 * i + 1] = f.y;
     }
@@ -143,13 +153,13 @@ __device__ __forceinline__ void store_eight(Q8 *p, const float (&x)[8])
 __device__ __forceinline__ float one_in(const Q8 *p) { return q8_decode2(p->b).x; }
 __device__ __forceinline__ void one_out(Q8 *p, float x) { p->b = (uint8_t)q8_encode2(x, 0.0f); }
 
-// The eight elements of one lane: consecutive ones from `first` (stride 1), or
-// every 32nd where the arrays of the tensor are not aligned alike.
+// The elements of one lane where they do not move as a group of eight: element
+// first + j * stride for every bit j of the mask.  Strides are 1, or 32 where
+// the arrays of the tensor are not aligned alike.
 struct Lane {
     long long first;
     int stride;
-    bool whole;                                 // a full, aligned group of eight
-    unsigned mask;                              // bit j: element first + j * stride exists
+    unsigned mask;
 };
 
 __device__ __forceinline__ Lane lane_of(long long group, int lane, bool vec, long long lo, long long hi)
@@ -158,16 +168,11 @@ __device__ __forceinline__ Lane lane_of(long long group, int lane, bool vec, lon
     L.first = vec ? group + lane * 8 : group + lane;
     L.stride = vec ? 1 : 32;
     L.mask = 0;
-    if (L.first >= lo && L.first + 7 * L.stride < hi) {
-        L.mask = 0xffu;
-    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const long long i = L.first + j * L.stride;
-            L.mask |= (i >= lo && i < hi) ? 1u << j : 0u;
-        }
+    for (int j = 0; j < 8; ++j) {
+        const long long i = L.first + j * L.stride;
+        L.mask |= (i >= lo && i < hi) ? 1u << j : 0u;
     }
-    L.whole = vec && L.mask == 0xffu;
     return L;
 }
 
@@ -175,141 +180,187 @@ template <class T>
 __device__ __forceinline__ void load_lane(const T *base, const Lane &L, float (&x)[8])
 {
     const T *at = base + L.first;
-    if (L.whole) {
-        load_eight(at, x);
-    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = (L.mask >> j & 1u) ? one_in(at + j * L.stride) : 0.0f;
-    }
+    for (int j = 0; j < 8; ++j) x[j] = (L.mask >> j & 1u) ? one_in(at + j * L.stride) : 0.0f;
 }
 template <class T>
 __device__ __forceinline__ void store_lane(T *base, const Lane &L, const float (&x)[8])
 {
     T *at = base + L.first;
-    if (L.whole) {
-        store_eight(at, x);
-    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (L.mask >> j & 1u) one_out(at + j * L.stride, x[j]);
-    }
+    for (int j = 0; j < 8; ++j)
+        if (L.mask >> j & 1u) one_out(at + j * L.stride, x[j]);
 }
 
-// Largest magnitude of a warp's 256 values.  Magnitudes order like their bit
-// patterns, with NaN above everything, so this is an integer maximum.
+__device__ __forceinline__ float max_or_nan(float a, float b)
+{
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+// Largest magnitude of a warp's 256 values, NaN if there is one.  Across the
+// lanes magnitudes are compared as bit patterns, which order alike, with NaN
+// above everything.
 __device__ __forceinline__ float top_of(const float (&x)[8])
 {
-    unsigned t = 0;
+    float t = fabsf(x[0]);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t = max(t, __float_as_uint(x[j]) & 0x7fffffffu);
-    return __uint_as_float(__reduce_max_sync(0xffffffffu, t));
+    for (int j = 1; j < 8; ++j) t = max_or_nan(t, fabsf(x[j]));
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(t) & 0x7fffffffu));
 }
 
 template <int BITS> struct MomentOf;
 template <> struct MomentOf<32> { using T = float; };
 template <> struct MomentOf<8> { using T = Q8; };
 
+// What a step multiplies with, the same for every element of a tensor.
+struct AdamwFactors { float scale, rate, spread, decay; };
+
+// The step for eight elements of a lane: weights and moments in, weights and
+// moments out; for 8 bits the moments come out as they are kept, and the
+// block's two scales beside them.
 template <int BITS>
-struct AdamwGroup {
-    Lane L;
-    float p[8], g[8], m[8], v[8];
-    float m_scale, v_scale;
-};
-
-template <int BITS, class G>
-__device__ __forceinline__ void adamw_load(const AdamwEntry &E, long long group, int lane, AdamwGroup<BITS> &X)
+__device__ __forceinline__ void adamw_eight(const AdamwParams &P, const AdamwFactors &F, float (&p)[8], const float (&g_in)[8],
+                                            float (&m_io)[8], float (&v_io)[8], float &m_scale, float &v_scale)
 {
-    using M = typename MomentOf<BITS>::T;
-    X.L = lane_of(group, lane, E.vec != 0, E.lo, E.hi);
-    load_lane(E.p, X.L, X.p);
-    load_lane((const G *)E.g, X.L, X.g);
-    load_lane((const M *)E.m, X.L, X.m);
-    load_lane((const M *)E.v, X.L, X.v);
-    if (BITS == 8 && group < E.hi) {
-        X.m_scale = E.m_scale[group / kGroup];
-        X.v_scale = E.v_scale[group / kGroup];
-    }
-}
-
-template <int BITS, class C>
-__device__ __forceinline__ void adamw_update(const AdamwEntry &E, long long group, int lane, const AdamwParams &P,
-                                             float scale, float rate, float spread, float decay, AdamwGroup<BITS> &X)
-{
-    using M = typename MomentOf<BITS>::T;
     float root[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float g = __fmul_rn(X.g[j], scale);
-        float m = X.m[j], v = X.v[j];
+        const float g = __fmul_rn(g_in[j], F.scale);
+        float m = m_io[j], v = v_io[j];
         if (BITS == 8) {
-            m = __fmul_rn(m, X.m_scale);
-            v = __fmul_rn(v, X.v_scale);
+            m = __fmul_rn(m, m_scale);
+            v = __fmul_rn(v, v_scale);
             v = __fmul_rn(v, v);
         }
         m = __fadd_rn(__fmul_rn(m, P.b1), __fmul_rn(g, P.b1c));
         v = __fadd_rn(__fmul_rn(v, P.b2), __fmul_rn(__fmul_rn(g, g), P.b2c));
         root[j] = __fsqrt_rn(v);
-        const float step = __fdiv_rn(__fmul_rn(m, rate), __fadd_rn(__fmul_rn(root[j], spread), P.eps));
-        X.p[j] = __fsub_rn(__fmul_rn(X.p[j], decay), step);
-        X.m[j] = m;
-        X.v[j] = v;
+        const float step = __fdiv_rn(__fmul_rn(m, F.rate), __fadd_rn(__fmul_rn(root[j], F.spread), P.eps));
+        p[j] = __fsub_rn(__fmul_rn(p[j], F.decay), step);
+        m_io[j] = m;
+        v_io[j] = v;
     }
-    store_lane(E.p, X.L, X.p);
-    if (!__is_same(C, void)) {
-        if (E.copy != nullptr) {
-            using CT = typename std::conditional<__is_same(C, void), __half, C>::type;
-            store_lane((CT *)E.copy, X.L, X.p);
-        }
-    }
-    if (BITS == 32) {
-        store_lane((M *)E.m, X.L, X.m);
-        store_lane((M *)E.v, X.L, X.v);
-    } else {
-        // elements that do not exist were read as zeros and stay zeros: they do not raise a block's top
-        const float tm = top_of(X.m), tr = top_of(root);
+    if (BITS == 8) {
+        // elements that do not exist came in as zeros and stay zeros: they do not raise a block's top
+        const float tm = top_of(m_io), tr = top_of(root);
         const bool some_m = tm >= 0x1p-100f, some_r = tr >= 0x1p-100f;
-        const float inv_m = some_m ? __fdiv_rn(448.0f, tm) : 0.0f, inv_r = some_r ? __fdiv_rn(448.0f, tr) : 0.0f;
+        // four quotients, one division: every lane does one of them
+        const int lane = threadIdx.x & 31;
+        const float mine = lane & 2 ? tr : tm;
+        const float quotient = __fdiv_rn(lane & 1 ? mine : 448.0f, lane & 1 ? 448.0f : mine);
+        const float inv_m = some_m ? __shfl_sync(0xffffffffu, quotient, 0) : 0.0f;
+        const float new_m = some_m ? __shfl_sync(0xffffffffu, quotient, 1) : 0.0f;
+        const float inv_r = some_r ? __shfl_sync(0xffffffffu, quotient, 2) : 0.0f;
+        const float new_r = some_r ? __shfl_sync(0xffffffffu, quotient, 3) : 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            X.m[j] = __fmul_rn(X.m[j], inv_m);
+            m_io[j] = __fmul_rn(m_io[j], inv_m);
             const float r = __fmul_rn(root[j], inv_r);
-            X.v[j] = root[j] > 0.0f ? fmaxf(r, 0x1p-9f) : r;      // 2^-9: the smallest e4m3 number
+            v_io[j] = root[j] > 0.0f ? fmaxf(r, 0x1p-9f) : r;         // 2^-9: the smallest e4m3 number
         }
-        store_lane((M *)E.m, X.L, X.m);
-        store_lane((M *)E.v, X.L, X.v);
-        if (lane == 0 && group < E.hi) {
-            E.m_scale[group / kGroup] = some_m ? __fdiv_rn(tm, 448.0f) : 0.0f;
-            E.v_scale[group / kGroup] = some_r ? __fdiv_rn(tr, 448.0f) : 0.0f;
-        }
+        m_scale = new_m;
+        v_scale = new_r;
     }
 }
 
-constexpr int kAdamwGroups = 2;                                     // groups of a warp per chunk, loaded together
-constexpr int kAdamwChunk = kOptWarps * kGroup * kAdamwGroups;      // elements
+// A whole, aligned group.
+template <int BITS, class G, class C>
+__device__ __forceinline__ void adamw_whole(const AdamwEntry *E, long long group, int lane, const AdamwParams &P, const AdamwFactors &F)
+{
+    using M = typename MomentOf<BITS>::T;
+    using CT = typename std::conditional<__is_same(C, void), __half, C>::type;
+    const long long at = group + lane * 8;
+    Eight<float> p8;
+    Eight<G> g8;
+    Eight<M> m8, v8;
+    float p[8], g[8], m[8], v[8], m_scale = 0.0f, v_scale = 0.0f;
+    load_eight(E->p + at, p8.w);
+    load_eight((const G *)E->g + at, g8.w);
+    load_eight((const M *)E->m + at, m8.w);
+    load_eight((const M *)E->v + at, v8.w);
+    if (BITS == 8) {
+        m_scale = E->m_scale[group / kGroup];
+        v_scale = E->v_scale[group / kGroup];
+    }
+    numbers(p8, p);
+    numbers(g8, g);
+    numbers(m8, m);
+    numbers(v8, v);
+    adamw_eight<BITS>(P, F, p, g, m, v, m_scale, v_scale);
+    store_eight(E->p + at, p);
+    store_eight((M *)E->m + at, m);
+    store_eight((M *)E->v + at, v);
+    if (!__is_same(C, void) && E->copy != nullptr) store_eight((CT *)E->copy + at, p);
+    if (BITS == 8 && lane == 0) {                 // the reductions in between have every lane past its reads
+        E->m_scale[group / kGroup] = m_scale;
+        E->v_scale[group / kGroup] = v_scale;
+    }
+}
+
+// A group that is cut off by the tensor's ends, or of a tensor whose arrays are not aligned alike.
+template <int BITS, class G, class C>
+__device__ __noinline__ void adamw_broken(const AdamwEntry *E, long long group, int lane, const AdamwParams &P, const AdamwFactors F)
+{
+    using M = typename MomentOf<BITS>::T;
+    using CT = typename std::conditional<__is_same(C, void), __half, C>::type;
+    if (group >= E->hi) return;
+    const Lane L = lane_of(group, lane, E->vec != 0, E->lo, E->hi);
+    float p[8], g[8], m[8], v[8], m_scale = 0.0f, v_scale = 0.0f;
+    load_lane(E->p, L, p);
+    load_lane((const G *)E->g, L, g);
+    load_lane((const M *)E->m, L, m);
+    load_lane((const M *)E->v, L, v);
+    if (BITS == 8) {
+        m_scale = E->m_scale[group / kGroup];
+        v_scale = E->v_scale[group / kGroup];
+    }
+    __syncwarp();                                 // every lane has the old scales before one writes the new ones
+    adamw_eight<BITS>(P, F, p, g, m, v, m_scale, v_scale);
+    store_lane(E->p, L, p);
+    store_lane((M *)E->m, L, m);
+    store_lane((M *)E->v, L, v);
+    if (!__is_same(C, void) && E->copy != nullptr) store_lane((CT *)E->copy, L, p);
+    if (BITS == 8 && lane == 0) {
+        E->m_scale[group / kGroup] = m_scale;
+        E->v_scale[group / kGroup] = v_scale;
+    }
+}
+
+constexpr int kAdamwChunk = kOptWarps * kGroup;                     // elements: a group for each warp
+
+// Blocks of an SM.  With 8-bit moments a group is some 70 instructions per
+// element for 14 bytes, and more warps hide one another's latencies; with fp32
+// moments fewer of them keep the streams of HBM longer.  Measured on 134 M
+// elements, 2 / 3 / 4 / 5 blocks: 8 bits with bf16 gradients 549 / 424 / 386 /
+// 383 us; fp32 572 / 594 / 616 / 617 us, but 204 M elements of 1,288 tensors
+// 969 / 867 us with 2 / 3, and 11 M with bf16 gradients 61 / 56 us.
+template <int BITS> constexpr int kAdamwBlocks = BITS == 8 ? 4 : 3;
 
 // One step of AdamW (the formula is in psops.h).  What bounds it is HBM
-// traffic: 28 bytes per element with fp32 moments and gradients, 14 to 16 with
-// 8-bit moments and 16-bit gradients.
+// traffic: 28 bytes per element with fp32 moments and gradients (204 M elements
+// of 1,288 tensors: 863 us, 6.63 TB/s, what a plain copy reaches); 14 to 16 with
+// 8-bit moments and 16-bit gradients, where the instructions weigh as much
+// (268 M of 291 tensors with bf16 copies: 826 us, 5.2 TB/s).  Keeping the next
+// group's loads in registers under the arithmetic was slower (its registers cost
+// more warps than the overlap gave: 473 us against 378 us for 134 M elements).
 template <int BITS, class G, class C>
-__global__ void __launch_bounds__(kOptThreads) psops_adamw_kernel(const AdamwParams P)
+__global__ void __launch_bounds__(kOptThreads, kAdamwBlocks<BITS>) psops_adamw_kernel(const __grid_constant__ AdamwParams P)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const float scale = P.scale != nullptr ? *P.scale : 1.0f;
-    if (!(fabsf(scale) < INFINITY)) return;                         // skipped: nothing changes, t stays
+    AdamwFactors F;
+    F.scale = P.scale != nullptr ? *P.scale : 1.0f;
+    if (!(fabsf(F.scale) < INFINITY)) return;                       // skipped: nothing changes, t stays
     const double pow1 = P.state->pow1, pow2 = P.state->pow2;
-    const float rate = (float)(P.lr * P.state->inv_bias1), spread = P.state->spread;
+    F.rate = (float)(P.lr * P.state->inv_bias1);
+    F.spread = P.state->spread;
     for (unsigned c = blockIdx.x; c < P.n_chunks; c += gridDim.x) {
         const uint2 chunk = P.chunks[c];
-        const AdamwEntry E = P.entries[chunk.x];
-        const float decay = (float)(1.0 - P.lr * E.weight_decay);
-        const long long base = (long long)chunk.y * kAdamwChunk + warp * kGroup;
-        AdamwGroup<BITS> X[kAdamwGroups];
-#pragma unroll
-        for (int i = 0; i < kAdamwGroups; ++i)
-            adamw_load<BITS, G>(E, base + i * kOptWarps * kGroup, lane, X[i]);
-#pragma unroll
-        for (int i = 0; i < kAdamwGroups; ++i)
-            adamw_update<BITS, C>(E, base + i * kOptWarps * kGroup, lane, P, scale, rate, spread, decay, X[i]);
+        const AdamwEntry *E = P.entries + chunk.x;
+        const long long group = (long long)chunk.y * kAdamwChunk + warp * kGroup;
+        F.decay = (float)(1.0 - P.lr * E->weight_decay);
+        if (E->vec != 0 && group >= E->lo && group + kGroup <= E->hi) adamw_whole<BITS, G, C>(E, group, lane, P, F);
+        else adamw_broken<BITS, G, C>(E, group, lane, P, F);
     }
     // The block that comes last -- every block has read the state by then --
     // moves it on to the next step.
