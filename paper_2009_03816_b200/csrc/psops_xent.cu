@@ -103,6 +103,35 @@ struct psops_xent : Base {
 
 namespace {
 
+// All launches of a call but the first are programmatic (see after_the_kernel_before).
+template <typename... Params, typename... Args>
+int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), int64_t grid, int threads, size_t shared, Args &&...args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)std::max<int64_t>(1, grid));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = x->stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = follows ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+    if (e != cudaSuccess) return x->fail(e, name);
+    x->launches += 1;
+    return PSOPS_OK;
+}
+
+// Blocks of a copy of so many 16-byte pieces, one or more a thread.
+int64_t copy_grid(const psops_xent *x, int64_t pieces) { return std::min<int64_t>(ceil_div(pieces, kCopyThreads), (int64_t)x->sms * 8); }
+
+#define PSOPS_DO(call)                       \
+    do {                                     \
+        const int rc_ = (call);              \
+        if (rc_ != PSOPS_OK) return rc_;     \
+    } while (0)
+
 bool aligned16(const void *p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && ld % 8 == 0; }
 
 int check_matrix(const void *p, int64_t ld, int64_t rows, int64_t dim)
@@ -136,15 +165,11 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
     P.row_lse = x->at<float>(x->lay.row_lse);
     P.vocab = (int)x->cfg.vocab;
     P.headroom = x->cfg.type == PSOPS_F16 ? 32768.0f : 1.0f;
-    psops_xent_index_kernel<<<1, kIndexThreads, 0, x->stream>>>(P);
-    int rc = x->launched("psops_xent_index_kernel");
-    if (rc != PSOPS_OK) return rc;
-    const int64_t rows = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kTileRows);
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(rows, kCopyThreads / 32), (int64_t)x->sms * 8);
-    psops_xent_gather_kernel<<<grid, kCopyThreads, 0, x->stream>>>((const uint16_t *)h, h_ld, (int)x->cfg.dim, (int)x->lay.padded,
-                                                                  aligned16(h, h_ld), P.control, P.row_of,
-                                                                  x->at<uint16_t>(x->lay.hidden));
-    return x->launched("psops_xent_gather_kernel");
+    PSOPS_DO(launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel, 1, kIndexThreads, 0, P));
+    const int64_t rows = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kStepK);
+    return launch(x, "psops_xent_gather_kernel", true, psops_xent_gather_kernel, copy_grid(x, rows * x->lay.padded / 8), kCopyThreads, 0,
+                  (const uint16_t *)h, h_ld, (int)x->cfg.dim, (int)x->lay.padded, aligned16(h, h_ld), P.control, P.row_of,
+                  x->at<uint16_t>(x->lay.hidden));
 }
 
 // The rows of w of one piece as the products read them: in place, or packed into the workspace.
@@ -157,11 +182,10 @@ int piece_of_w(psops_xent *x, const void *w, int64_t w_ld, int64_t first, int64_
         return PSOPS_OK;
     }
     uint16_t *to = x->at<uint16_t>(x->lay.w);
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(count, kCopyThreads / 32), (int64_t)x->sms * 8);
-    psops_xent_pack_kernel<<<grid, kCopyThreads, 0, x->stream>>>(from, w_ld, count, (int)x->cfg.dim, (int)x->lay.padded, to);
     *out = to;
     *out_ld = x->lay.padded;
-    return x->launched("psops_xent_pack_kernel");
+    return launch(x, "psops_xent_pack_kernel", true, psops_xent_pack_kernel, copy_grid(x, count * x->lay.padded / 8), kCopyThreads, 0, from,
+                  w_ld, count, (int)x->cfg.dim, (int)x->lay.padded, aligned16(w, w_ld), to);
 }
 
 // A matrix of `height` rows of `width` consecutive elements as the tensor
@@ -197,8 +221,7 @@ ProductKernel product_of(const psops_xent *x, int job)
 int product(psops_xent *x, int job, int64_t works, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const ProductParams &P)
 {
     const unsigned grid = 2u * (unsigned)std::max<int64_t>(1, std::min<int64_t>(works, x->sms / 2));
-    product_of(x, job)<<<grid, kProductThreads, kProductShared, x->stream>>>(a, b, out, P);
-    return x->launched("psops_xent_product_kernel");
+    return launch(x, "psops_xent_product_kernel", true, product_of(x, job), grid, kProductThreads, kProductShared, a, b, out, P);
 }
 
 ProductParams product_params(const psops_xent *x)
@@ -214,12 +237,6 @@ ProductParams product_params(const psops_xent *x)
     P.label_logit = x->at<float>(x->lay.label_logit);
     return P;
 }
-
-#define PSOPS_DO(call)                       \
-    do {                                     \
-        const int rc_ = (call);              \
-        if (rc_ != PSOPS_OK) return rc_;     \
-    } while (0)
 
 // What a call's products have in common.
 struct Call {
@@ -263,8 +280,7 @@ int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinPara
     J.row_of = x->at<int>(x->lay.row_of);
     J.label_logit = x->at<float>(x->lay.label_logit);
     J.partials = x->at<double>(x->lay.partials);
-    psops_xent_join_kernel<<<(unsigned)ceil_div(std::max<int64_t>(1, tokens), kJoinRows), kJoinRows * kJoinParts, 0, x->stream>>>(J);
-    return x->launched("psops_xent_join_kernel");
+    return launch(x, "psops_xent_join_kernel", true, psops_xent_join_kernel, ceil_div(tokens, kJoinRows), kJoinRows * kJoinParts, 0, J);
 }
 
 int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *dh, int64_t dh_ld, void *dw, int64_t dw_ld)
@@ -313,25 +329,20 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             P.result_rows = (int)count;
             PSOPS_DO(product(x, kDw, ceil_div(count, kTile) * tiles_d, dlogits_across, hidden_across, dw_out, P));
             if (!direct) {
-                const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(count, kCopyThreads / 32), (int64_t)x->sms * 8);
-                psops_xent_unpack_kernel<<<grid, kCopyThreads, 0, x->stream>>>(to, (int)c.padded, count, (int)x->cfg.dim,
-                                                                              (uint16_t *)dw + first * dw_ld, dw_ld);
-                PSOPS_DO(x->launched("psops_xent_unpack_kernel"));
+                const int64_t grid = std::min<int64_t>(ceil_div(count, kCopyThreads / 32), (int64_t)x->sms * 8);
+                PSOPS_DO(launch(x, "psops_xent_unpack_kernel", true, psops_xent_unpack_kernel, grid, kCopyThreads, 0, to, (int)c.padded, count,
+                                (int)x->cfg.dim, (uint16_t *)dw + first * dw_ld, dw_ld));
             }
         }
     }
     if (dh == nullptr || tokens == 0) return PSOPS_OK;
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(tokens, kCopyThreads / 32), (int64_t)x->sms * 8);
     const bool aligned = ((uintptr_t)dh & 7u) == 0 && dh_ld % 4 == 0;
-    if (type == PSOPS_F16)
-        psops_xent_dh_out_kernel<__half><<<grid, kCopyThreads, 0, x->stream>>>(x->at<float>(x->lay.sums), c.padded, (int)shares, c.rows,
-                                                                              x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
-                                                                              (int)x->cfg.dim, aligned, (__half *)dh, dh_ld);
-    else
-        psops_xent_dh_out_kernel<__nv_bfloat16><<<grid, kCopyThreads, 0, x->stream>>>(x->at<float>(x->lay.sums), c.padded, (int)shares, c.rows,
-                                                                                     x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
-                                                                                     (int)x->cfg.dim, aligned, (__nv_bfloat16 *)dh, dh_ld);
-    return x->launched("psops_xent_dh_out_kernel");
+    auto out = [&](auto *typed, auto kernel) {
+        return launch(x, "psops_xent_dh_out_kernel", true, kernel, copy_grid(x, tokens * ceil_div(x->cfg.dim, 4)), kCopyThreads, 0,
+                      x->at<float>(x->lay.sums), c.padded, (int)shares, c.rows, x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
+                      (int)x->cfg.dim, aligned, typed, dh_ld);
+    };
+    return type == PSOPS_F16 ? out((__half *)dh, psops_xent_dh_out_kernel<__half>) : out((__nv_bfloat16 *)dh, psops_xent_dh_out_kernel<__nv_bfloat16>);
 }
 
 } // namespace

@@ -20,6 +20,7 @@ namespace {
 
 constexpr int kTileRows = 256;                   // compact rows are padded to this
 constexpr int kTileCols = 256;                   // a piece of the vocabulary is a multiple of this
+constexpr int kStepK = 64;                       // of the summed axis, a step of a product
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -49,38 +50,47 @@ struct IndexParams {
 
 constexpr int kIndexThreads = 1024;
 
-// One block lists the tokens that count, in order.
+// Kernels of one call follow each other with programmatic launches: the next
+// one may set itself up while this one runs, and waits here before it reads
+// anything; what it needs is complete then, and so is everything before.
+__device__ __forceinline__ void after_the_kernel_before()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// One block lists the tokens that count, in order: each warp a stretch of them.
 __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const IndexParams P)
 {
     __shared__ int warp_sum[32];
     __shared__ float warp_top[32];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = (P.tokens + kIndexThreads - 1) / kIndexThreads;
-    const int first = tid * per, last = min(P.tokens, first + per);
+    after_the_kernel_before();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per = (P.tokens + kIndexThreads - 1) / kIndexThreads * 32;
+    const int first = min(P.tokens, warp * per), last = min(P.tokens, first + per);
     int mine = 0;
     float top = 0.0f;
-    for (int t = first; t < last; ++t) {
+#pragma unroll 4
+    for (int t = first + lane; t < last; t += 32) {
         const long long y = P.targets[t];
         if (y >= 0 && y < P.vocab) {
             ++mine;
             if (P.grad != nullptr && P.reduction == PSOPS_PER_TOKEN) top = fmaxf(top, fabsf(P.grad[t]));
         }
     }
-    int upto = mine;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, upto, off);
-        if (lane >= off) upto += v;
-    }
+    mine = __reduce_add_sync(0xffffffffu, mine);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    if (lane == 31) warp_sum[warp] = upto;
-    if (lane == 0) warp_top[warp] = top;
+    if (lane == 0) {
+        warp_sum[warp] = mine;
+        warp_top[warp] = top;
+    }
     __syncthreads();
-    int before = 0, total = 0;
+    int at = 0, total = 0;
     top = 0.0f;
+#pragma unroll
     for (int w = 0; w < 32; ++w) {
-        if (w < warp) before += warp_sum[w];
+        if (w < warp) at += warp_sum[w];
         total += warp_sum[w];
         top = fmaxf(top, warp_top[w]);
     }
@@ -94,81 +104,86 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
         int e = 0;
         if (top > 0.0f && top < INFINITY) e = min(120, max(-100, ilogbf(top) + 1));
         up = ldexpf(P.headroom, -e);
-        if (tid == 0) P.control->unscale = 1.0f / up;
+        if (threadIdx.x == 0) P.control->unscale = 1.0f / up;
     }
-    int at = before + upto - mine;
-    for (int t = first; t < last; ++t) {
-        const long long y = P.targets[t];
-        if (y >= 0 && y < P.vocab) {
-            P.row_of[at] = t;
-            P.label[at] = (int)y;
-            P.compact_of[t] = at;
+#pragma unroll 2
+    for (int t0 = first; t0 < last; t0 += 32) {
+        const int t = t0 + lane;
+        const long long y = t < last ? P.targets[t] : -1;
+        const bool in = y >= 0 && y < P.vocab;
+        const unsigned votes = __ballot_sync(0xffffffffu, in);
+        if (in) {
+            const int r = at + __popc(votes & ((1u << lane) - 1u));
+            P.row_of[r] = t;
+            P.label[r] = (int)y;
+            P.compact_of[t] = r;
             if (P.grad != nullptr) {
-                P.row_scale[at] = (P.reduction == PSOPS_PER_TOKEN ? P.grad[t] : common) * up;
-                P.row_lse[at] = P.lse[t] * kLog2e;
+                P.row_scale[r] = (P.reduction == PSOPS_PER_TOKEN ? P.grad[t] : common) * up;
+                P.row_lse[r] = P.lse[t] * kLog2e;
             }
-            ++at;
-        } else {
+        } else if (t < last) {
             P.compact_of[t] = -1;
             if (P.rows_out != nullptr) P.rows_out[t] = 0.0f;
             if (P.lse_out != nullptr) P.lse_out[t] = 0.0f;
         }
+        at += __popc(votes);
     }
-    if (tid == 0) {
+    if (threadIdx.x == 0) {
         P.control->rows = total;
         P.control->tickets = 0;
     }
 }
 
-// A row of 16-bit values, `n` of them, into a row of `padded` (a multiple of
-// 8, 16-byte aligned) with zeros behind; src == nullptr: all zeros.
-__device__ __forceinline__ void copy_row(uint16_t *dst, const uint16_t *src, int n, int padded, bool aligned, int lane, int lanes)
+// Elements [8 g, 8 g + 8) of a row of `n` 16-bit values, zeros beyond its end.
+__device__ __forceinline__ uint4 eight_of_row(const uint16_t *row, int g, int n, bool aligned)
 {
-    for (int g = lane; g < padded / 8; g += lanes) {
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (src != nullptr) {
-            if (aligned && g * 8 + 8 <= n) {
-                u = *reinterpret_cast<const uint4 *>(src + g * 8);
-            } else {
-                uint16_t e[8];
+    if (aligned && g * 8 + 8 <= n) return *reinterpret_cast<const uint4 *>(row + g * 8);
+    uint32_t e[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) e[j] = g * 8 + j < n ? src[g * 8 + j] : (uint16_t)0;
-                u = make_uint4(e[0] | (unsigned)e[1] << 16, e[2] | (unsigned)e[3] << 16, e[4] | (unsigned)e[5] << 16, e[6] | (unsigned)e[7] << 16);
-            }
-        }
-        *reinterpret_cast<uint4 *>(dst + g * 8) = u;
-    }
+    for (int j = 0; j < 8; ++j) e[j] = g * 8 + j < n ? row[g * 8 + j] : 0u;
+    return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
 }
 
 constexpr int kCopyThreads = 256;
 
-// Hidden states of the tokens that count, one warp per row; zero rows up to a whole tile.
+// Hidden states of the tokens that count, in rows of `padded` (a multiple of 8)
+// elements; zero rows up to a whole step of the products.  A thread per 16 bytes.
 __global__ void __launch_bounds__(kCopyThreads) psops_xent_gather_kernel(const uint16_t *h, long long ld, int dim, int padded,
                                                                          bool aligned, const XentControl *control,
                                                                          const int *row_of, uint16_t *out)
 {
+    after_the_kernel_before();
     const int rows = control->rows;
-    const int whole = max(1, (rows + kTileRows - 1) / kTileRows) * kTileRows;
-    const int warps = gridDim.x * (kCopyThreads / 32);
-    for (int r = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); r < whole; r += warps)
-        copy_row(out + (long long)r * padded, r < rows ? h + row_of[r] * ld : nullptr, dim, padded, aligned, threadIdx.x & 31, 32);
+    const unsigned groups = padded / 8;
+    const long long whole = (long long)(max(1, rows) + kStepK - 1) / kStepK * kStepK * groups;
+    for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < whole; i += (long long)gridDim.x * kCopyThreads) {
+        const int r = (int)(i / groups), g = (int)(i - (long long)r * groups);
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (r < rows) u = eight_of_row(h + row_of[r] * ld, g, dim, aligned);
+        reinterpret_cast<uint4 *>(out)[i] = u;
+    }
 }
 
 // Rows of w that cannot be read in place.
 __global__ void __launch_bounds__(kCopyThreads) psops_xent_pack_kernel(const uint16_t *w, long long ld, long long rows, int dim,
-                                                                       int padded, uint16_t *out)
+                                                                       int padded, bool aligned, uint16_t *out)
 {
-    const long long warps = (long long)gridDim.x * (kCopyThreads / 32);
-    for (long long r = (long long)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); r < rows; r += warps)
-        copy_row(out + r * padded, w + r * ld, dim, padded, false, threadIdx.x & 31, 32);
+    after_the_kernel_before();
+    const unsigned groups = padded / 8;
+    for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < rows * groups; i += (long long)gridDim.x * kCopyThreads) {
+        const long long r = i / groups;
+        reinterpret_cast<uint4 *>(out)[i] = eight_of_row(w + r * ld, (int)(i - r * groups), dim, aligned);
+    }
 }
 
 // Rows of dw that could not be written in place.
 __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const uint16_t *in, int padded, long long rows, int dim,
                                                                          uint16_t *dw, long long ld)
 {
+    after_the_kernel_before();
     const long long warps = (long long)gridDim.x * (kCopyThreads / 32);
     for (long long r = (long long)blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); r < rows; r += warps)
+#pragma unroll 4
         for (int d = threadIdx.x & 31; d < dim; d += 32) dw[r * ld + d] = in[r * padded + d];
 }
 
@@ -193,7 +208,7 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const u
 // ---------------------------------------------------------------------------
 enum Job { kLoss = 0, kDlogits = 1, kDh = 2, kDw = 3 };
 
-constexpr int kTile = 256, kHalf = 128, kStepK = 64;
+constexpr int kTile = 256, kHalf = 128;
 constexpr int kStages = 6;
 constexpr int kStageBytes = 2 * kHalf * kStepK * 2;              // this CTA's halves of A and B
 constexpr int kOutBytes = 32 * 128;                              // a warp's 32 rows of 128 bytes on their way out
@@ -307,6 +322,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     umma::fence_after();
     const uint32_t tensor_base = tensor_base_slot;
 
+    after_the_kernel_before();
     const int rows = P.control->rows;
     const int some_rows = max(1, rows);
     const int tiles_m = JOB == kDw ? (P.result_rows + kTile - 1) / kTile : JOB == kDh ? (rows + kTile - 1) / kTile : (some_rows + kTile - 1) / kTile;
@@ -557,7 +573,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
 // ---------------------------------------------------------------------------
 // Joining the pieces
 // ---------------------------------------------------------------------------
-constexpr int kJoinRows = 32, kJoinParts = 8;    // a block: 32 compact rows, each joined by 8 threads
+constexpr int kJoinRows = 32, kJoinParts = 32;   // a block: 32 compact rows, each joined by 32 threads
 
 struct JoinParams {
     const float2 *stats;
@@ -583,17 +599,22 @@ __device__ __forceinline__ void join(float &top, float &sum, float top2, float s
 // comes last adds up the loss, always in the same order.
 __global__ void __launch_bounds__(kJoinRows * kJoinParts) psops_xent_join_kernel(const JoinParams P)
 {
-    __shared__ float tops[kJoinParts][kJoinRows], sums[kJoinParts][kJoinRows];
+    __shared__ float tops[kJoinParts][kJoinRows + 1], sums[kJoinParts][kJoinRows + 1];
     __shared__ double row_loss[kJoinRows];
     __shared__ bool last;
+    after_the_kernel_before();
     const int rows = P.control->rows;
     const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
     const int r = blockIdx.x * kJoinRows + lane;
     float top = -INFINITY, sum = 0.0f;
     if (r < rows)
-        for (int k = part; k < P.parts; k += kJoinParts) {
-            const float2 s = P.stats[k * P.stats_ld + r];
-            join(top, sum, s.x, s.y);
+        for (int k = part; k < P.parts; k += 8 * kJoinParts) {
+            float2 s[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                s[j] = k + j * kJoinParts < P.parts ? P.stats[(k + j * kJoinParts) * P.stats_ld + r] : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) join(top, sum, s[j].x, s[j].y);
         }
     tops[part][lane] = top;
     sums[part][lane] = sum;
@@ -634,29 +655,31 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_dh_out_kernel(const f
                                                                          const int *compact_of, int tokens, int dim, bool aligned,
                                                                          T *dh, long long ld)
 {
+    after_the_kernel_before();
     const float unscale = control->error ? NAN : control->unscale;      // a product gave up: no numbers rather than wrong ones
-    const int warps = gridDim.x * (kCopyThreads / 32);
-    for (int t = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); t < tokens; t += warps) {
+    const unsigned groups = (dim + 3) / 4;
+    for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < (long long)tokens * groups; i += (long long)gridDim.x * kCopyThreads) {
+        const int t = (int)(i / groups), d = (int)(i - (long long)t * groups) * 4;
         const int r = compact_of[t];
-        const float *in = sums + r * sums_ld;
-        T *out = dh + t * ld;
-        for (int d = (threadIdx.x & 31) * 4; d < dim; d += 128) {
-            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (r >= 0)
-                for (int s = 0; s < splits; ++s) {
-                    const float4 a = *reinterpret_cast<const float4 *>(in + s * split_rows * sums_ld + d);
-                    v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
-                }
-            const uint2 u = make_uint2(pack2<T>(v.x * unscale, v.y * unscale), pack2<T>(v.z * unscale, v.w * unscale));
-            if (aligned && d + 4 <= dim) {
-                *reinterpret_cast<uint2 *>(out + d) = u;
-            } else {
-                T e[4];
-                memcpy(e, &u, 8);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (d + j < dim) out[d + j] = e[j];
+        T *out = dh + t * ld + d;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (r >= 0) {
+            const float *in = sums + r * sums_ld + d;
+#pragma unroll 4
+            for (int s = 0; s < splits; ++s) {
+                const float4 a = *reinterpret_cast<const float4 *>(in + s * split_rows * sums_ld);
+                v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
             }
+        }
+        const uint2 u = make_uint2(pack2<T>(v.x * unscale, v.y * unscale), pack2<T>(v.z * unscale, v.w * unscale));
+        if (aligned && d + 4 <= dim) {
+            *reinterpret_cast<uint2 *>(out) = u;
+        } else {
+            T e[4];
+            memcpy(e, &u, 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (d + j < dim) out[j] = e[j];
         }
     }
 }
