@@ -22,21 +22,14 @@ namespace {
 // Bytes that the logits' gradients of one piece of the vocabulary may take.
 constexpr int64_t kPieceBytes = 512ll << 20;
 constexpr int64_t kMinPiece = 2048;
-// Pairs of CTAs that run at once on a B200 (148 SMs).
-constexpr int64_t kPairs = 74;
+// Bytes that the fp32 sums of dh may take in more than one share.
+constexpr int64_t kShareBytes = 256ll << 20;
 
 bool config_ok(const psops_xent_config *c)
 {
     return c != nullptr && c->max_tokens >= 1 && c->max_tokens <= (1 << 24) && c->dim >= 1 && c->dim <= (1 << 20) &&
            c->vocab >= 1 && c->vocab <= (1ll << 31) - (1 << 16) && (c->type == PSOPS_F16 || c->type == PSOPS_BF16) &&
            (c->flags & ~(PSOPS_XENT_GRADS | PSOPS_XENT_STAGED)) == 0;
-}
-
-// dh has few tiles where there are few rows: its sum over the vocabulary is then
-// split into shares, so that all SMs have a tile.
-int64_t shares_of(int64_t rows, int64_t padded)
-{
-    return std::max<int64_t>(1, kPairs / (rows / kTileRows * ceil_div(padded, kTile)));
 }
 
 struct Layout {
@@ -58,7 +51,7 @@ Layout make_layout(const psops_xent_config *c)
     L.piece = std::min(whole, std::max(kMinPiece, kPieceBytes / (2 * L.rows) / kTileCols * kTileCols));
     L.staged = c->dim % 8 != 0 || (c->flags & PSOPS_XENT_STAGED) != 0;
     L.parts = whole / kHalf;
-    L.sum_rows = L.rows * shares_of(L.rows, L.padded);
+    L.sum_rows = L.rows * std::max<int64_t>(1, std::min<int64_t>(kMostShares, kShareBytes / (4 * L.rows * L.padded)));
     size_t at = 0;
     auto take = [&at](size_t bytes) {
         const size_t here = at;
@@ -165,6 +158,12 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
     P.row_lse = x->at<float>(x->lay.row_lse);
     P.vocab = (int)x->cfg.vocab;
     P.headroom = x->cfg.type == PSOPS_F16 ? 32768.0f : 1.0f;
+    // every piece of the vocabulary gives every share of dh something to add up, the shortest piece too
+    const int64_t last = x->cfg.vocab - (x->cfg.vocab - 1) / x->lay.piece * x->lay.piece;
+    P.steps = (int)ceil_div(last, kStepK);
+    P.tiles_across = (int)ceil_div(x->lay.padded, kTile);
+    P.sum_rows = (int)x->lay.sum_rows;
+    P.pairs = x->sms / 2;
     PSOPS_DO(launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel, 1, kIndexThreads, 0, P));
     const int64_t rows = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kStepK);
     return launch(x, "psops_xent_gather_kernel", true, psops_xent_gather_kernel, copy_grid(x, rows * x->lay.padded / 8), kCopyThreads, 0,
@@ -228,7 +227,6 @@ ProductParams product_params(const psops_xent *x)
 {
     ProductParams P{};
     P.control = x->control();
-    P.splits = 1;
     P.label = x->at<int>(x->lay.label);
     P.row_lse = x->at<float>(x->lay.row_lse);
     P.row_scale = x->at<float>(x->lay.row_scale);
@@ -297,9 +295,6 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
     PSOPS_DO(make_map(x, &dlogits_along, type, dlogits, x->lay.piece, c.some_rows, x->lay.piece, kHalf));
     PSOPS_DO(make_map(x, &dlogits_across, type, dlogits, x->lay.piece, c.some_rows, x->lay.piece, kStepK));
     PSOPS_DO(make_map(x, &sums, PSOPS_F32, x->at<void>(x->lay.sums), c.padded, x->lay.sum_rows, c.padded, 32));
-    // every piece gives every share something to add up, but the last piece may be short
-    const int64_t last = x->cfg.vocab - (x->cfg.vocab - 1) / x->lay.piece * x->lay.piece;
-    const int64_t shares = std::max<int64_t>(1, std::min({x->lay.sum_rows / c.rows, shares_of(c.rows, c.padded), ceil_div(last, kStepK)}));
     for (int64_t first = 0; first < x->cfg.vocab; first += x->lay.piece) {
         const int64_t count = std::min(x->lay.piece, x->cfg.vocab - first);
         const void *rows_of_w;
@@ -316,10 +311,8 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             PSOPS_DO(make_map(x, &weights, type, rows_of_w, c.padded, count, ld, kStepK));
             P.columns = (int)c.padded;
             P.depth = (int)count;
-            P.splits = (int)shares;
-            P.split_rows = (int)c.rows;
             P.add = first > 0;
-            PSOPS_DO(product(x, kDh, c.tiles_m * tiles_d * shares, dlogits_along, weights, sums, P));
+            PSOPS_DO(product(x, kDh, c.tiles_m * tiles_d * kMostShares, dlogits_along, weights, sums, P));
         }
         if (dw != nullptr) {
             uint16_t *to = direct ? (uint16_t *)dw + first * dw_ld : x->at<uint16_t>(x->lay.dw);
@@ -339,7 +332,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
     const bool aligned = ((uintptr_t)dh & 7u) == 0 && dh_ld % 4 == 0;
     auto out = [&](auto *typed, auto kernel) {
         return launch(x, "psops_xent_dh_out_kernel", true, kernel, copy_grid(x, tokens * ceil_div(x->cfg.dim, 4)), kCopyThreads, 0,
-                      x->at<float>(x->lay.sums), c.padded, (int)shares, c.rows, x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
+                      x->at<float>(x->lay.sums), c.padded, x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
                       (int)x->cfg.dim, aligned, typed, dh_ld);
     };
     return type == PSOPS_F16 ? out((__half *)dh, psops_xent_dh_out_kernel<__half>) : out((__nv_bfloat16 *)dh, psops_xent_dh_out_kernel<__nv_bfloat16>);

@@ -29,6 +29,8 @@ struct XentControl {
     unsigned tickets;
     float unscale;                               // power of two: gradient sums * unscale = gradients
     int error;
+    int shares;                                  // dh: its sum over the vocabulary in so many shares
+    int share_rows;                              // rows between the shares' sums
 };
 
 struct IndexParams {
@@ -46,7 +48,27 @@ struct IndexParams {
     int vocab;
     int reduction;
     float headroom;                              // largest |dlogits| that the 16-bit type should see
+    int tiles_across, steps, sum_rows, pairs;    // dh: tiles of its columns, steps of the shortest piece, room for sums, pairs of CTAs
 };
+
+constexpr int kMostShares = 16;
+constexpr int kShareCost = 4;                    // a tile's start and end, in steps
+constexpr int kShareJoin = 6;                    // a tile's sums written and read once more, that many tiles to a step
+
+// dh has few tiles where there are few rows, and its sum over the vocabulary is
+// long: it is split into shares, as many as bring the rounds of tiles to the
+// least time (8 x 4 tiles on 74 pairs: one share leaves 42 pairs idle, two
+// shares ten; measured 183 -> 100 us for 1,950 rows, 32,003 entries, dim 1000).
+__device__ __forceinline__ int best_shares(int tiles, int steps, int most, int pairs)
+{
+    int best = 1;
+    long long least = 1ll << 62;
+    for (int s = 1; s <= most; ++s) {
+        const long long t = (long long)((tiles * s + pairs - 1) / pairs) * ((steps + s - 1) / s + kShareCost) + (long long)tiles * s / kShareJoin;
+        if (t < least) { least = t; best = s; }
+    }
+    return best;
+}
 
 constexpr int kIndexThreads = 1024;
 
@@ -131,6 +153,11 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
     if (threadIdx.x == 0) {
         P.control->rows = total;
         P.control->tickets = 0;
+        if (P.grad != nullptr) {
+            const int tiles = max(1, (total + kTileRows - 1) / kTileRows);
+            P.control->share_rows = tiles * kTileRows;
+            P.control->shares = best_shares(tiles * P.tiles_across, P.steps, min(min(kMostShares, P.steps), P.sum_rows / (tiles * kTileRows)), P.pairs);
+        }
     }
 }
 
@@ -209,13 +236,13 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const u
 enum Job { kLoss = 0, kDlogits = 1, kDh = 2, kDw = 3 };
 
 constexpr int kTile = 256, kHalf = 128;
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr int kStageBytes = 2 * kHalf * kStepK * 2;              // this CTA's halves of A and B
 constexpr int kOutBytes = 32 * 128;                              // a warp's 32 rows of 128 bytes on their way out
 constexpr int kOutWarps = 8;
 constexpr int kProductThreads = 384;
-constexpr int kProductShared = kStages * kStageBytes + kOutWarps * kOutBytes + 1024;   // 1024: alignment
-constexpr int kChainSteps = 8;                                   // steps of a logit summed by the tensor cores in one go
+constexpr int kProductShared = kStages * kStageBytes + kOutWarps * 2 * kOutBytes + 1024;   // two outputs a warp; 1024: alignment
+constexpr int kChainSteps = 12;                                  // most steps of a logit summed by the tensor cores in one go
 constexpr int kGroupTiles = 8;                                   // row tiles that share columns in L2
 
 struct ProductParams {
@@ -223,8 +250,6 @@ struct ProductParams {
     int columns;                                 // kLoss, kDlogits: entries of the piece; kDh, kDw: padded dim
     int depth;                                   // kLoss, kDlogits: padded dim; kDh: entries of the piece
     int result_rows;                             // kDw: entries of the piece
-    int splits;                                  // kDh: the summed axis in so many shares, sums apart
-    int split_rows;                              // kDh: rows between the shares' sums
     int first;                                   // first vocabulary entry of the piece
     bool add;                                    // kDh: add to the sums of the pieces before
     const int *label;
@@ -287,7 +312,6 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
 {
     constexpr bool kAAcross = JOB == kDw, kBAcross = JOB == kDh || JOB == kDw;
     constexpr bool kChained = JOB == kLoss || JOB == kDlogits;
-    constexpr int kChain = kChained ? kChainSteps : 1 << 30;
     constexpr uint32_t kInstruction = umma::instruction(__is_same(T, __nv_bfloat16), kAAcross, kBAcross, kTile, kTile);
 
     extern __shared__ uint8_t raw[];
@@ -328,7 +352,10 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     const int tiles_m = JOB == kDw ? (P.result_rows + kTile - 1) / kTile : JOB == kDh ? (rows + kTile - 1) / kTile : (some_rows + kTile - 1) / kTile;
     const int tiles_n = (P.columns + kTile - 1) / kTile;
     const int steps = ((JOB == kDw ? some_rows : P.depth) + kStepK - 1) / kStepK;
-    const int splits = JOB == kDh ? P.splits : 1;
+    const int fewest = (steps + kChainSteps - 1) / kChainSteps;                        // chains of a logit, of like length
+    const int chain = kChained ? (steps + fewest - 1) / fewest : steps;
+    const int chains = (steps + chain - 1) / chain;
+    const int splits = JOB == kDh ? P.control->shares : 1;
     const int works = tiles_m * tiles_n * splits;
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
@@ -375,8 +402,8 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
         for (int i = pair; i < works && ok; i += pairs) {
             const Work w = work_of(i, tiles_m, tiles_n);
             const int k_first = (int)((long long)steps * w.split / splits), k_last = (int)((long long)steps * (w.split + 1) / splits);
+            int link = 0;                                          // place within a chain of sums
             for (int k = k_first; k < k_last; ++k) {
-                const int link = (k - k_first) % kChain;           // place within a chain of sums
                 if (link == 0) {
                     ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_free[buffer]), buffer_phase ^ 1u, failed));
                     if (!ok) break;
@@ -385,7 +412,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                 ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_full[s]), phase, failed));
                 if (!ok) break;
                 umma::fence_after();
-                const bool ends = link == kChain - 1 || k == k_last - 1;
+                const bool ends = link == chain - 1 || k == k_last - 1;
                 if (umma::elected()) {
                     const uint32_t sums = tensor_base + buffer * kTile;
                     const uint64_t da = first_a + (uint32_t)s * (kStageBytes >> 4), db = first_b + (uint32_t)s * (kStageBytes >> 4);
@@ -397,14 +424,17 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                 }
                 __syncwarp();
                 if (++s == kStages) { s = 0; phase ^= 1u; }
+                link = ends ? 0 : link + 1;
                 if (ends && ++buffer == 2) { buffer = 0; buffer_phase ^= 1u; }
             }
         }
     } else if (warp >= 4) {
         // ---- results: this warp has 32 rows (its quarter of tensor memory) and 128 columns
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        const uint32_t out = outs + (warp - 4) * kOutBytes;
+        const uint32_t both_outs = outs + (warp - 4) * 2 * kOutBytes;
+        int turn = 0;                                // which of the two is written next
         const float unscale = JOB == kDw ? P.control->unscale : 1.0f;
+        const int share_rows = JOB == kDh ? P.control->share_rows : 0;
         int buffer = 0;
         uint32_t phase = 0;
         for (int i = pair; i < works; i += pairs) {
@@ -470,7 +500,9 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                     constexpr int kBoxes = JOB == kDh ? 2 : 1;         // 128 bytes a row: 32 fp32 or 64 16-bit columns
 #pragma unroll
                     for (int box = 0; box < kBoxes; ++box) {
-                        if (lane == 0) umma::stores_read<0>();
+                        const uint32_t out = both_outs + turn * kOutBytes;
+                        turn ^= 1;
+                        if (lane == 0) umma::stores_read<1>();
                         __syncwarp();
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -495,8 +527,8 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                         if (lane == 0) {
                             const int x = col0 + c + box * 32;
                             if (wanted && (JOB == kDlogits || x < P.columns)) {
-                                if (JOB == kDh && P.add) umma::tensor_add(&map_out, x, w.split * P.split_rows + row0, out);
-                                else umma::tensor_store(&map_out, x, (JOB == kDh ? w.split * P.split_rows : 0) + row0, out);
+                                if (JOB == kDh && P.add) umma::tensor_add(&map_out, x, w.split * share_rows + row0, out);
+                                else umma::tensor_store(&map_out, x, w.split * share_rows + row0, out);
                             }
                             umma::stores_commit();
                         }
@@ -506,7 +538,6 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
             bool ok = true;
             if constexpr (kChained) {
                 uint32_t total[kHalf];
-                const int chains = (steps + kChain - 1) / kChain;
 #pragma unroll 1
                 for (int q = 0; q < chains; ++q) {
                     ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_sum[buffer]), phase, failed));
@@ -650,13 +681,14 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) psops_xent_join_kernel
 
 // dh in the caller's rows from the compact sums, rounded once; zero where a token is left out.
 template <class T>
-__global__ void __launch_bounds__(kCopyThreads) psops_xent_dh_out_kernel(const float *sums, long long sums_ld, int splits,
-                                                                         long long split_rows, const XentControl *control,
+__global__ void __launch_bounds__(kCopyThreads) psops_xent_dh_out_kernel(const float *sums, long long sums_ld, const XentControl *control,
                                                                          const int *compact_of, int tokens, int dim, bool aligned,
                                                                          T *dh, long long ld)
 {
     after_the_kernel_before();
     const float unscale = control->error ? NAN : control->unscale;      // a product gave up: no numbers rather than wrong ones
+    const int shares = control->shares;
+    const long long share = control->share_rows * sums_ld;
     const unsigned groups = (dim + 3) / 4;
     for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < (long long)tokens * groups; i += (long long)gridDim.x * kCopyThreads) {
         const int t = (int)(i / groups), d = (int)(i - (long long)t * groups) * 4;
@@ -666,8 +698,8 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_dh_out_kernel(const f
         if (r >= 0) {
             const float *in = sums + r * sums_ld + d;
 #pragma unroll 4
-            for (int s = 0; s < splits; ++s) {
-                const float4 a = *reinterpret_cast<const float4 *>(in + s * split_rows * sums_ld);
+            for (int s = 0; s < shares; ++s) {
+                const float4 a = *reinterpret_cast<const float4 *>(in + s * share);
                 v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
             }
         }

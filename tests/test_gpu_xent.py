@@ -106,7 +106,7 @@ def _run(T, D, V, dtype, seed=1, masked=0.0, reduction="mean"):
 
 SHAPES = [(1, 1, 1), (1, 8, 2), (2, 3, 5), (256, 84, 10), (3, 64, 257), (65, 72, 255), (255, 128, 256), (256, 64, 512),
           (257, 200, 1000), (31, 1000, 3001), (513, 264, 700), (1, 512, 4097), (129, 65, 129), (300, 520, 2049),
-          (1024, 256, 8193), (64, 4096, 640)]
+          (1024, 256, 8193), (64, 4096, 640), (5, 13_000, 300)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
