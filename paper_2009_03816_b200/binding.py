@@ -181,10 +181,10 @@ def _check(rc: int, where: str, ctx=None, last_error="psops_last_error") -> None
 
 def _ptr(buf) -> int:
     """Address of a torch tensor or numpy array (0 for None)."""
-    if buf is None:
-        return 0
     if isinstance(buf, torch.Tensor):
         return buf.data_ptr()
+    if buf is None:
+        return 0
     if isinstance(buf, np.ndarray):
         return buf.ctypes.data
     if isinstance(buf, int):

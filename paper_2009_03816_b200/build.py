@@ -14,7 +14,8 @@ _ROOT = os.path.dirname(_HERE)
 SOURCES = [os.path.join(_HERE, "csrc", name) for name in ("psops.cu", "psops_optim.cu", "psops_xent.cu")]
 HEADERS = [os.path.join(_ROOT, "include", "psops.h")] + [
     os.path.join(_HERE, "csrc", name) for name in ("psops_kernels.cuh", "psops_host.cuh", "psops_optim_kernels.cuh",
-                                              "psops_xent_kernels.cuh", "psops_umma.cuh")]
+                                              "psops_xent_kernels.cuh", "psops_xent_small.cuh",
+                                              "psops_umma.cuh")]
 LIBRARY = os.path.join(_HERE, "libpsops.so")
 
 NVCC_FLAGS = [

@@ -8,9 +8,11 @@
 
 #include <algorithm>
 #include <new>
+#include <utility>
 
 #include "psops_host.cuh"
 #include "psops_xent_kernels.cuh"
+#include "psops_xent_small.cuh"
 
 using psops_host::Base;
 using psops_host::OnDevice;
@@ -22,6 +24,8 @@ namespace {
 // Bytes that the logits' gradients of one piece of the vocabulary may take.
 constexpr int64_t kPieceBytes = 512ll << 20;
 constexpr int64_t kMinPiece = 2048;
+// Most blocks of the small kernels' launches (they have a partial result each).
+constexpr int64_t kMostBlocks = 1024;
 // Bytes that the fp32 sums of dh may take in more than one share.
 constexpr int64_t kShareBytes = 256ll << 20;
 
@@ -66,9 +70,9 @@ Layout make_layout(const psops_xent_config *c)
     L.row_scale = take(4 * n);
     L.row_lse = take(4 * n);
     L.label_logit = take(4 * n);
-    L.partials = take(8 * (n / kJoinRows));
+    L.partials = take(std::max<size_t>(8 * (n / kJoinRows), sizeof(double2) * kMostBlocks));
     L.hidden = take(2 * n * (size_t)L.padded);
-    L.stats = take(8 * n * (size_t)L.parts);
+    L.stats = take(std::max<size_t>(8 * n * (size_t)L.parts, 8 * kFewTokens * kMostBlocks));
     if (L.staged) L.w = take(2 * (size_t)L.piece * (size_t)L.padded);
     if (c->flags & PSOPS_XENT_GRADS) {
         if (L.staged) L.dw = take(2 * (size_t)L.piece * (size_t)L.padded);
@@ -98,10 +102,10 @@ namespace {
 
 // All launches of a call but the first are programmatic (see after_the_kernel_before).
 template <typename... Params, typename... Args>
-int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), int64_t grid, int threads, size_t shared, Args &&...args)
+int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), dim3 grid, int threads, size_t shared, Args &&...args)
 {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)std::max<int64_t>(1, grid));
+    cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = x->stream;
@@ -114,6 +118,12 @@ int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params.
     if (e != cudaSuccess) return x->fail(e, name);
     x->launches += 1;
     return PSOPS_OK;
+}
+
+template <typename... Params, typename... Args>
+int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), int64_t grid, int threads, size_t shared, Args &&...args)
+{
+    return launch(x, name, follows, kernel, dim3((unsigned)std::max<int64_t>(1, grid)), threads, shared, std::forward<Args>(args)...);
 }
 
 // Blocks of a copy of so many 16-byte pieces, one or more a thread.
@@ -251,6 +261,57 @@ int open_call(psops_xent *x, int64_t tokens, Call *c)
     return make_map(x, &c->hidden, x->cfg.type, x->at<void>(x->lay.hidden), c->padded, c->some_rows, c->padded, kHalf);
 }
 
+HeadParams head_params(const psops_xent *x, const void *h, int64_t h_ld, const void *w, int64_t w_ld, const int64_t *targets,
+                       int64_t tokens, int32_t reduction)
+{
+    HeadParams P{};
+    P.h = h; P.h_ld = h_ld; P.w = w; P.w_ld = w_ld;
+    P.targets = (const long long *)targets;
+    P.tokens = (int)tokens; P.dim = (int)x->cfg.dim; P.vocab = (int)x->cfg.vocab; P.reduction = reduction;
+    P.control = x->control();
+    P.partials = x->at<double2>(x->lay.partials);
+    return P;
+}
+
+// Passes of few classes, and the forward pass of few tokens.
+template <class T>
+int forward_head(psops_xent *x, HeadParams P)
+{
+    const int64_t grid = std::min<int64_t>(ceil_div(P.tokens, kSmallWarps), std::min<int64_t>(x->sms, kMostBlocks));
+    return launch(x, "psops_xent_head_kernel", false, psops_xent_head_kernel<T, false>, grid, kSmallThreads, head_shared(P.vocab, P.dim), P);
+}
+
+template <class T>
+int backward_head(psops_xent *x, HeadParams P, void *dw, int64_t dw_ld)
+{
+    const int64_t grid = std::min<int64_t>(ceil_div(P.tokens, kSmallWarps), std::min<int64_t>(x->sms, kMostBlocks));
+    PSOPS_DO(launch(x, "psops_xent_head_kernel", false, psops_xent_head_kernel<T, true>, grid, kSmallThreads, head_shared(P.vocab, P.dim), P));
+    if (dw == nullptr) return PSOPS_OK;
+    return launch(x, "psops_xent_head_dw_kernel", true, psops_xent_head_dw_kernel<T>,
+                  dim3((unsigned)ceil_div(P.dim, 32), (unsigned)ceil_div(P.vocab, kHeadDwClasses)), kHeadDwThreads, 0, (const T *)P.h, P.h_ld,
+                  P.targets, (const float *)P.dlogits, P.tokens, P.dim, P.vocab, (T *)dw, dw_ld);
+}
+
+template <class T, bool ALIGNED>
+void (*few_kernel(int few))(const FewParams)
+{
+    return few == 1 ? psops_xent_few_kernel<T, 1, ALIGNED> : few == 2 ? psops_xent_few_kernel<T, 2, ALIGNED>
+           : psops_xent_few_kernel<T, 4, ALIGNED>;
+}
+template <class T>
+void (*few_kernel(int few, bool aligned))(const FewParams)
+{
+    return aligned ? few_kernel<T, true>(few) : few_kernel<T, false>(few);
+}
+
+template <class T>
+int forward_few(psops_xent *x, FewParams P)
+{
+    const auto kernel = few_kernel<T>(few_of(P.tokens), P.w_aligned && P.dim % 8 == 0);
+    const int64_t grid = std::min<int64_t>(std::min<int64_t>((int64_t)x->sms * kFewBlocks, kMostBlocks), ceil_div(P.vocab, kSmallWarps));
+    return launch(x, "psops_xent_few_kernel", false, kernel, grid, kSmallThreads, few_shared(P.tokens, P.dim), P);
+}
+
 int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinParams J)
 {
     Call c;
@@ -366,6 +427,15 @@ int psops_xent_create(psops_xent **out, const psops_xent_config *cfg, void *d_wo
     if (e == cudaSuccess && found != cudaDriverEntryPointSuccess) e = cudaErrorNotSupported;
     for (int job = kLoss; e == cudaSuccess && job <= kDw; ++job)
         e = cudaFuncSetAttribute((const void *)product_of(x, job), cudaFuncAttributeMaxDynamicSharedMemorySize, kProductShared);
+    const bool half = cfg->type == PSOPS_F16;
+    const void *heads[2] = {half ? (const void *)psops_xent_head_kernel<__half, false> : (const void *)psops_xent_head_kernel<__nv_bfloat16, false>,
+                            half ? (const void *)psops_xent_head_kernel<__half, true> : (const void *)psops_xent_head_kernel<__nv_bfloat16, true>};
+    for (const void *k : heads)
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadShared);
+    for (int few = 1; few <= kFewTokens; few *= 2)
+        for (int aligned = 0; aligned < 2 && e == cudaSuccess; ++aligned)
+            e = cudaFuncSetAttribute(half ? (const void *)few_kernel<__half>(few, aligned != 0) : (const void *)few_kernel<__nv_bfloat16>(few, aligned != 0),
+                                     cudaFuncAttributeMaxDynamicSharedMemorySize, kFewShared);
     if (e == cudaSuccess) e = cudaMemsetAsync(x->control(), 0, sizeof(XentControl), x->stream);
     if (e != cudaSuccess) {
         delete x;
@@ -384,6 +454,26 @@ int psops_xent_forward(psops_xent *x, const void *d_h, int64_t h_ld, const void 
     if (rc != PSOPS_OK) return rc;
     if (((uintptr_t)d_loss | (uintptr_t)d_rows | (uintptr_t)d_lse) & 3u) return PSOPS_EALIGN;
     OnDevice guard(x);
+    const bool half = x->cfg.type == PSOPS_F16;
+    if (is_head(x->cfg.vocab, x->cfg.dim, tokens)) {
+        HeadParams H = head_params(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, reduction);
+        H.loss = d_loss;
+        H.rows = d_rows;
+        H.lse_out = d_lse;
+        return half ? forward_head<__half>(x, H) : forward_head<__nv_bfloat16>(x, H);
+    }
+    if (is_few(tokens, x->cfg.dim)) {
+        FewParams F{};
+        F.h = (const uint16_t *)d_h; F.h_ld = h_ld; F.h_aligned = aligned16(d_h, h_ld);
+        F.w = (const uint16_t *)d_w; F.w_ld = w_ld; F.w_aligned = aligned16(d_w, w_ld);
+        F.targets = (const long long *)d_targets;
+        F.tokens = (int)tokens; F.dim = (int)x->cfg.dim; F.vocab = (int)x->cfg.vocab; F.reduction = reduction;
+        F.control = x->control();
+        F.stats = x->at<float2>(x->lay.stats);
+        F.label_logit = x->at<float>(x->lay.label_logit);
+        F.loss = d_loss; F.rows = d_rows; F.lse_out = d_lse;
+        return half ? forward_few<__half>(x, F) : forward_few<__nv_bfloat16>(x, F);
+    }
     IndexParams P{};
     P.targets = (const long long *)d_targets;
     P.rows_out = d_rows;
@@ -413,6 +503,15 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
     if (((uintptr_t)d_lse | (uintptr_t)d_grad) & 3u) return PSOPS_EALIGN;
     if (d_dw != nullptr && !x->lay.staged && !aligned16(d_dw, dw_ld)) return PSOPS_EALIGN;
     OnDevice guard(x);
+    if (is_head(x->cfg.vocab, x->cfg.dim, tokens)) {
+        HeadParams H = head_params(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, reduction);
+        H.lse = d_lse;
+        H.grad = d_grad;
+        H.dlogits = x->at<float>(x->lay.dlogits);
+        H.dh = d_dh;
+        H.dh_ld = dh_ld;
+        return x->cfg.type == PSOPS_F16 ? backward_head<__half>(x, H, d_dw, dw_ld) : backward_head<__nv_bfloat16>(x, H, d_dw, dw_ld);
+    }
     IndexParams P{};
     P.targets = (const long long *)d_targets;
     P.grad = d_grad;

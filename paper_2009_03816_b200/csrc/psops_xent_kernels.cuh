@@ -670,8 +670,10 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) psops_xent_join_kernel
         }
     }
     __syncthreads();
-    if (!last || threadIdx.x >= 32 || P.loss == nullptr) return;
+    if (!last || threadIdx.x >= 32) return;
     __threadfence();
+    if (lane == 0) P.control->tickets = 0;
+    if (P.loss == nullptr) return;
     double total = 0.0;
     for (unsigned b = lane; b < gridDim.x; b += 32) total += __ldcg(P.partials + b);
 #pragma unroll

@@ -26,6 +26,7 @@ from .binding import (PSOPS_BF16, PSOPS_EINVAL, PSOPS_F16, PSOPS_F32, PSOPS_MEAN
                       PSOPS_SUM, PSOPS_XENT_GRADS, PSOPS_XENT_STAGED, PsopsError)
 
 _TYPES = {torch.float32: PSOPS_F32, torch.float16: PSOPS_F16, torch.bfloat16: PSOPS_BF16}
+_REDUCTIONS = {"mean": PSOPS_MEAN, "sum": PSOPS_SUM, "none": PSOPS_PER_TOKEN}
 MOMENT_BLOCK = 256               # elements that share one scale of an 8-bit moment
 
 
@@ -92,6 +93,7 @@ class LinearXent:
             _refuse("LinearXent", f"h and w of {dtype}: torch.bfloat16 or torch.float16")
         self.device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
         self.tokens, self.dim, self.vocab, self.dtype = int(tokens), int(dim), int(vocab), dtype
+        self._w_shape = torch.Size((self.vocab, self.dim)) if min(self.vocab, self.dim) >= 0 else None
         self.ctx, self._launched = None, 0
         self._flags = PSOPS_XENT_GRADS if gradients else 0
         self.stream = _stream_on(self.device, stream)
@@ -105,83 +107,90 @@ class LinearXent:
             self._workspace = _workspace(nbytes, self.device, "LinearXent")
             self.ctx = binding.psops_xent_create(cfg, self._workspace, None, self.stream)
 
-    def _rows(self, where, name, t, dtype=None):
-        """(tensor as rows, stride) of a matrix with consecutive elements in each row."""
-        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != (dtype or self.dtype):
-            _refuse(where, f"{name} is not a {dtype or self.dtype} tensor on {self.device}")
-        if t.dim() < 1 or t.shape[-1] != self.dim:
+    def _rows(self, where, name, t):
+        """Stride of a matrix that has consecutive elements in each row, its leading dimensions seen as one."""
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype is not self.dtype:
+            _refuse(where, f"{name} is not a {self.dtype} tensor on {self.device}")
+        shape = t.shape
+        if len(shape) < 1 or shape[-1] != self.dim:
             _refuse(where, f"{name} has no last dimension of {self.dim}")
-        if t.dim() != 2:
+        if t.is_contiguous():
+            return self.dim
+        if len(shape) != 2:
             try:
                 t = t.view(-1, self.dim)
             except RuntimeError:
                 _refuse(where, f"{name}: its leading dimensions cannot be seen as one")
-        if t.shape[1] > 1 and t.stride(1) != 1:
+        if self.dim > 1 and t.stride(1) != 1:
             _refuse(where, f"{name}: the elements of a row are not consecutive")
         ld = t.stride(0) if t.shape[0] > 1 else self.dim
         if ld < self.dim:
             _refuse(where, f"{name}: rows overlap")
-        return t, ld
+        return ld
 
     def _arguments(self, where, h, w, targets):
-        h2, h_ld = self._rows(where, "h", h)
-        w2, w_ld = self._rows(where, "w", w)
-        if w.dim() != 2 or w2.shape[0] != self.vocab:
+        """(tokens, strides of h and w)."""
+        h_ld, w_ld = self._rows(where, "h", h), self._rows(where, "w", w)
+        if w.shape != self._w_shape:
             _refuse(where, f"w is not {self.vocab} x {self.dim}")
-        if not isinstance(targets, torch.Tensor) or targets.device != self.device or targets.dtype != torch.int64:
+        if not isinstance(targets, torch.Tensor) or targets.get_device() != self.device.index or \
+                targets.dtype is not torch.int64:
             _refuse(where, f"targets is not an int64 tensor on {self.device}")
         if targets.shape != h.shape[:-1] or not targets.is_contiguous():
             _refuse(where, f"targets has to be contiguous and of shape {tuple(h.shape[:-1])}")
-        if h2.shape[0] > self.tokens:
-            _refuse(where, f"{h2.shape[0]} tokens, made for {self.tokens}")
-        self._stage_if_needed(w2, w_ld)
-        return h2, h_ld, w2, w_ld
+        tokens = targets.numel()
+        if tokens > self.tokens:
+            _refuse(where, f"{tokens} tokens, made for {self.tokens}")
+        self._stage_if_needed(w, w_ld)
+        return tokens, h_ld, w_ld
 
     def _stage_if_needed(self, t, ld):
         """Rows that are not 16-byte aligned pass through a larger workspace, made when first met."""
-        if self.dim % 8 == 0 and (t.data_ptr() % 16 or ld % 8) and not self._flags & PSOPS_XENT_STAGED:
+        if (t.data_ptr() % 16 or ld % 8) and self.dim % 8 == 0 and not self._flags & PSOPS_XENT_STAGED:
             self._flags |= PSOPS_XENT_STAGED
             self._open()
 
     def forward(self, h, w, targets, reduction="mean"):
         """(loss, rows, lse): the loss of all tokens ("mean" or "sum"), and each token's loss and log-sum-exp."""
-        if reduction not in ("mean", "sum"):
+        if reduction != "mean" and reduction != "sum":
             _refuse("LinearXent.forward", f"reduction {reduction!r}")
-        h2, h_ld, w2, w_ld = self._arguments("LinearXent.forward", h, w, targets)
+        tokens, h_ld, w_ld = self._arguments("LinearXent.forward", h, w, targets)
         loss = torch.empty((), dtype=torch.float32, device=self.device)
-        rows, lse = (torch.empty(targets.shape, dtype=torch.float32, device=self.device) for _ in range(2))
-        binding.psops_xent_forward(self.ctx, h2, h_ld, w2, w_ld, targets, h2.shape[0],
-                                   PSOPS_MEAN if reduction == "mean" else PSOPS_SUM, loss, rows, lse)
+        rows = torch.empty(targets.shape, dtype=torch.float32, device=self.device)
+        lse = torch.empty_like(rows)
+        binding.psops_xent_forward(self.ctx, h, h_ld, w, w_ld, targets, tokens, _REDUCTIONS[reduction], loss, rows, lse)
         return loss, rows, lse
 
     def backward(self, h, w, targets, lse, grad, reduction="mean", *, dh=None, dw=None, want=(True, True)):
         """(dh, dw) from the upstream gradient: one fp32 number, or one per token for reduction "none".
         dh, dw: tensors to hold them; want: which of the two is computed."""
         where = "LinearXent.backward"
-        codes = {"mean": PSOPS_MEAN, "sum": PSOPS_SUM, "none": PSOPS_PER_TOKEN}
-        if reduction not in codes:
+        code = _REDUCTIONS.get(reduction)
+        if code is None:
             _refuse(where, f"reduction {reduction!r}")
-        h2, h_ld, w2, w_ld = self._arguments(where, h, w, targets)
-        for name, t, shape in (("lse", lse, targets.shape), ("grad", grad, targets.shape if reduction == "none" else None)):
-            if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != torch.float32 or \
-                    not t.is_contiguous() or (t.shape != shape if shape is not None else t.numel() != 1):
-                _refuse(where, f"{name} has to be contiguous, fp32, on {self.device}, of shape "
-                               f"{tuple(shape) if shape is not None else ()}")
-        out = []
-        for name, t, like, wanted in (("dh", dh, h, want[0]), ("dw", dw, w, want[1])):
-            if not wanted:
-                out.append((None, None, 0))
-                continue
-            t = torch.empty(like.shape, dtype=self.dtype, device=self.device) if t is None else t
-            rows, ld = self._rows(where, name, t)
-            if t.shape != like.shape:
-                _refuse(where, f"{name} is not of shape {tuple(like.shape)}")
-            out.append((t, rows, ld))
-        if out[1][0] is not None:
-            self._stage_if_needed(out[1][1], out[1][2])
-        binding.psops_xent_backward(self.ctx, h2, h_ld, w2, w_ld, targets, h2.shape[0], lse, grad, codes[reduction],
-                                    out[0][1], out[0][2], out[1][1], out[1][2])
-        return out[0][0], out[1][0]
+        tokens, h_ld, w_ld = self._arguments(where, h, w, targets)
+        self._numbers(where, "lse", lse, targets.shape)
+        self._numbers(where, "grad", grad, targets.shape if code == PSOPS_PER_TOKEN else None)
+        dh, dh_ld = self._gradient(where, "dh", dh, h) if want[0] else (None, 0)
+        dw, dw_ld = self._gradient(where, "dw", dw, w) if want[1] else (None, 0)
+        if dw is not None:
+            self._stage_if_needed(dw, dw_ld)
+        binding.psops_xent_backward(self.ctx, h, h_ld, w, w_ld, targets, tokens, lse, grad, code, dh, dh_ld, dw, dw_ld)
+        return dh, dw
+
+    def _numbers(self, where, name, t, shape):
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype is not torch.float32 or \
+                not t.is_contiguous() or (t.shape != shape if shape is not None else t.numel() != 1):
+            _refuse(where, f"{name} has to be contiguous, fp32, on {self.device}, of shape "
+                           f"{tuple(shape) if shape is not None else ()}")
+
+    def _gradient(self, where, name, t, like):
+        if t is None:
+            return torch.empty(like.shape, dtype=self.dtype, device=self.device), self.dim
+        ld = self._rows(where, name, t)
+        if t.shape != like.shape:
+            _refuse(where, f"{name} is not of shape {tuple(like.shape)}")
+        return t, ld
 
     def __call__(self, h, w, targets, reduction="mean"):
         return _LinearXentFunction.apply(h, w, targets, self, reduction)
@@ -312,8 +321,9 @@ class AdamW:
 
     def step(self, lr, grad_scale=None):
         """One step; grad_scale: a device fp32 scalar that multiplies every gradient."""
-        if grad_scale is not None and not (isinstance(grad_scale, torch.Tensor) and grad_scale.device == self.device
-                                           and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1):
+        if grad_scale is not None and not (isinstance(grad_scale, torch.Tensor)
+                                           and grad_scale.get_device() == self.device.index
+                                           and grad_scale.dtype is torch.float32 and grad_scale.numel() == 1):
             _refuse("AdamW.step", f"grad_scale has to be one fp32 number on {self.device}")
         self._scale = grad_scale               # read by the kernel: keep it alive
         binding.psops_adamw_step(self.ctx, lr, grad_scale)
@@ -371,7 +381,7 @@ class GradNorm:
         elif out.device != self.device or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
             _refuse("GradNorm.norm", f"`out` has to be 2 fp32 numbers on {self.device}")
         binding.psops_gradnorm_run(self.ctx, max_norm, out)
-        return out[0], out[1]
+        return out.unbind(0)
 
     @property
     def launches(self) -> int:

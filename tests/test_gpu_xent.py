@@ -122,6 +122,56 @@ def test_left_out_tokens(masked, reduction):
     _run(333, 136, 600, torch.float16, seed=4, masked=masked, reduction=reduction)
 
 
+HEADS = [(1, 2048, 8), (300, 100, 64), (77, 550, 50), (4096, 33, 17), (4097, 40, 17), (1000, 7, 33), (9, 1, 64), (130, 1600, 12)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,D,V", HEADS)
+def test_few_classes(T, D, V, dtype):
+    _run(T, D, V, dtype, seed=21, masked=0.2)
+    _run(T, D, V, dtype, seed=22, reduction="sum")
+
+
+FEW = [(1, 4096, 3000), (2, 1000, 70_001), (3, 61, 5000), (4, 256, 100), (7, 3000, 777), (8, 2056, 4096), (9, 64, 500)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,D,V", FEW)
+def test_few_tokens(T, D, V, dtype):
+    _run(T, D, V, dtype, seed=23)
+    _run(T, D, V, dtype, seed=24, masked=0.5, reduction="sum")
+
+
+@pytest.mark.parametrize("T,D,V", [(50, 30, 20), (6, 200, 900)])
+def test_small_forms_leave_out_and_weigh_like_the_others(T, D, V):
+    h, w, y = _inputs(T, D, V, torch.bfloat16, 31, masked=0.4)
+    y[0] = V - 1
+    op = training.LinearXent(T, D, V)
+    bad = h.clone()
+    bad[y < 0] = float("nan")
+    want, got = op.forward(h, w, y), op.forward(bad, w, y)
+    grad = torch.randn(T, device="cuda")
+    want_g, got_g = op.backward(h, w, y, want[2], grad, "none"), op.backward(bad, w, y, got[2], grad, "none")
+    for a, b in zip((*want, *want_g), (*got, *got_g)):
+        assert torch.equal(a, b)
+    x = _exact(h, w, y, grad)
+    _check_forward(x, *want)
+    _check_grads(x, *want_g, torch.bfloat16)
+    h[0] = float("nan")
+    loss, rows, lse = op.forward(h, w, y)
+    assert math.isnan(float(loss)) and math.isnan(float(rows[0])) and int(rows.isnan().sum()) == 1
+    # the large form after the small one on one context, and the small one again: counters start anew
+    if T == 6:
+        big = training.LinearXent(40, D, V)
+        h2, _, y2 = _inputs(40, D, V, torch.bfloat16, 32)
+        for _ in range(2):
+            first = big.forward(bad, w, y)
+            assert all(torch.equal(a, b) for a, b in zip(first, want))
+            _check_forward(_exact(h2, w, y2, grad.new_zeros(40)), *big.forward(h2, w, y2))
+        big.close()
+    op.close()
+
+
 def test_several_pieces_of_the_vocabulary():
     # 32,768 rows of workspace make a piece 8,192 entries: three pieces, the last one short
     T, D, V = 700, 128, 20_011
