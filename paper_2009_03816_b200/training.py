@@ -150,12 +150,16 @@ class LinearXent:
             self._flags |= PSOPS_XENT_STAGED
             self._open()
 
-    def forward(self, h, w, targets, reduction="mean"):
-        """(loss, rows, lse): the loss of all tokens ("mean" or "sum"), and each token's loss and log-sum-exp."""
+    def forward(self, h, w, targets, reduction="mean", *, loss=None):
+        """(loss, rows, lse): the loss of all tokens ("mean" or "sum"), and each token's loss and log-sum-exp.
+        `loss`: one fp32 number to hold it, such as an element of the loss vector a swarm reads."""
         if reduction != "mean" and reduction != "sum":
             _refuse("LinearXent.forward", f"reduction {reduction!r}")
         tokens, h_ld, w_ld = self._arguments("LinearXent.forward", h, w, targets)
-        loss = torch.empty((), dtype=torch.float32, device=self.device)
+        if loss is None:
+            loss = torch.empty((), dtype=torch.float32, device=self.device)
+        else:
+            self._numbers("LinearXent.forward", "loss", loss, None)
         rows = torch.empty(targets.shape, dtype=torch.float32, device=self.device)
         lse = torch.empty_like(rows)
         binding.psops_xent_forward(self.ctx, h, h_ld, w, w_ld, targets, tokens, _REDUCTIONS[reduction], loss, rows, lse)
