@@ -145,13 +145,15 @@ int open_base(Base *b, void *stream)
     return PSOPS_OK;
 }
 
-// Blocks of a persistent launch: as many as run at once, no more than there are chunks.
+// Blocks of a persistent launch: no more than run at once, and as many as have
+// the same number of chunks to do (but for the last ones).
 int grid_of(Base *b, const void *kernel, int64_t n_chunks, unsigned *grid)
 {
     int per_sm = 0;
     if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, kOptThreads, 0) != cudaSuccess) return PSOPS_ECUDA;
-    const int64_t most = (int64_t)b->sms * per_sm;
-    *grid = (unsigned)(n_chunks < 1 ? 1 : n_chunks < most ? n_chunks : most);
+    const int64_t most = (int64_t)b->sms * (per_sm < 1 ? 1 : per_sm);
+    const int64_t rounds = n_chunks < 1 ? 1 : ceil_div(n_chunks, most);
+    *grid = (unsigned)(n_chunks < 1 ? 1 : ceil_div(n_chunks, rounds));
     return PSOPS_OK;
 }
 
@@ -224,10 +226,8 @@ int psops_adamw_create(psops_adamw **out, const psops_adamw_config *cfg, const p
         for (int32_t i = 0; i < cfg->n_tensors; ++i)
             fill_chunks(list, i, chunks_of(tensors[i].n, kAdamwChunk, cfg->state_bits == 8 ? 0 : 7));
         AdamwState s{};
-        s.pow1 = std::pow(cfg->beta1, (double)cfg->steps_done);
-        s.pow2 = std::pow(cfg->beta2, (double)cfg->steps_done);
-        s.inv_bias1 = 1.0 / (1.0 - s.pow1 * cfg->beta1);
-        s.spread = (float)(1.0 / std::sqrt(1.0 - s.pow2 * cfg->beta2));
+        s.pow1 = std::pow(cfg->beta1, (double)(cfg->steps_done + 1));
+        s.pow2 = std::pow(cfg->beta2, (double)(cfg->steps_done + 1));
         s.steps = cfg->steps_done;
         rc = open_base(a, cuda_stream);
         if (rc == PSOPS_OK) rc = grid_of(a, (const void *)a->kernel, n_chunks, &a->grid);

@@ -39,11 +39,9 @@ struct AdamwEntry {
 };
 
 struct AdamwState {
-    double pow1, pow2;                          // beta^t of the steps taken
-    double inv_bias1;                           // 1 / (1 - beta1^(t+1)): the next step's
-    float spread;                               // 1 / sqrt(1 - beta2^(t+1)), rounded
+    double pow1, pow2;                          // beta^t with t the number of the next step
+    long long steps;                            // steps taken
     unsigned tickets;
-    long long steps;
 };
 
 struct AdamwParams {
@@ -352,8 +350,8 @@ __global__ void __launch_bounds__(kOptThreads, kAdamwBlocks<BITS>) psops_adamw_k
     F.scale = P.scale != nullptr ? *P.scale : 1.0f;
     if (!(fabsf(F.scale) < INFINITY)) return;                       // skipped: nothing changes, t stays
     const double pow1 = P.state->pow1, pow2 = P.state->pow2;
-    F.rate = (float)(P.lr * P.state->inv_bias1);
-    F.spread = P.state->spread;
+    F.rate = (float)(P.lr * (1.0 / (1.0 - pow1)));
+    F.spread = (float)(1.0 / sqrt(1.0 - pow2));
     for (unsigned c = blockIdx.x; c < P.n_chunks; c += gridDim.x) {
         const uint2 chunk = P.chunks[c];
         const AdamwEntry *E = P.entries + chunk.x;
@@ -362,20 +360,14 @@ __global__ void __launch_bounds__(kOptThreads, kAdamwBlocks<BITS>) psops_adamw_k
         if (E->vec != 0 && group >= E->lo && group + kGroup <= E->hi) adamw_whole<BITS, G, C>(E, group, lane, P, F);
         else adamw_broken<BITS, G, C>(E, group, lane, P, F);
     }
-    // The block that comes last -- every block has read the state by then --
-    // moves it on to the next step.
+    // The block that comes last moves the state on to the next step: every
+    // block has used the values it read by then.
     __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        if (atomicAdd(&P.state->tickets, 1u) == gridDim.x - 1) {
-            const double n1 = pow1 * P.beta1, n2 = pow2 * P.beta2;
-            P.state->pow1 = n1;
-            P.state->pow2 = n2;
-            P.state->inv_bias1 = 1.0 / (1.0 - n1 * P.beta1);
-            P.state->spread = (float)(1.0 / sqrt(1.0 - n2 * P.beta2));
-            P.state->steps += 1;
-            P.state->tickets = 0;
-        }
+    if (threadIdx.x == 0 && atomicAdd(&P.state->tickets, 1u) == gridDim.x - 1) {
+        P.state->pow1 = pow1 * P.beta1;
+        P.state->pow2 = pow2 * P.beta2;
+        P.state->steps += 1;
+        P.state->tickets = 0;
     }
 }
 
