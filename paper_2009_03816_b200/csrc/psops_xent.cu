@@ -38,7 +38,7 @@ bool config_ok(const psops_xent_config *c)
 
 struct Layout {
     int64_t rows;                               // compact rows, whole tiles
-    int64_t padded;                             // dim, a multiple of 8
+    int64_t padded;                             // dim in the workspace: a multiple of 64, so that rows are whole lines of 128 bytes
     int64_t piece;                              // vocabulary entries of a piece, a multiple of the tile
     bool staged;                                // w and dw may pass through the workspace
     int64_t parts;                              // softmax statistics per row
@@ -50,7 +50,7 @@ Layout make_layout(const psops_xent_config *c)
 {
     Layout L{};
     L.rows = (int64_t)round_up((size_t)c->max_tokens, kTileRows);
-    L.padded = (int64_t)round_up((size_t)c->dim, 8);
+    L.padded = (int64_t)round_up((size_t)c->dim, 64);
     const int64_t whole = (int64_t)round_up((size_t)c->vocab, kTileCols);
     L.piece = std::min(whole, std::max(kMinPiece, kPieceBytes / (2 * L.rows) / kTileCols * kTileCols));
     L.staged = c->dim % 8 != 0 || (c->flags & PSOPS_XENT_STAGED) != 0;
@@ -182,17 +182,18 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
 }
 
 // The rows of w of one piece as the products read them: in place, or packed into the workspace.
-int piece_of_w(psops_xent *x, const void *w, int64_t w_ld, int64_t first, int64_t count, const void **out, int64_t *out_ld)
+int piece_of_w(psops_xent *x, const void *w, int64_t w_ld, int64_t first, int64_t count, const void **out, int64_t *width, int64_t *out_ld)
 {
     const uint16_t *from = (const uint16_t *)w + first * w_ld;
     if (x->cfg.dim % 8 == 0 && aligned16(w, w_ld)) {
         *out = from;
+        *width = x->cfg.dim;
         *out_ld = w_ld;
         return PSOPS_OK;
     }
     uint16_t *to = x->at<uint16_t>(x->lay.w);
     *out = to;
-    *out_ld = x->lay.padded;
+    *width = *out_ld = x->lay.padded;
     return launch(x, "psops_xent_pack_kernel", true, psops_xent_pack_kernel, copy_grid(x, count * x->lay.padded / 8), kCopyThreads, 0, from,
                   w_ld, count, (int)x->cfg.dim, (int)x->lay.padded, aligned16(w, w_ld), to);
 }
@@ -322,10 +323,10 @@ int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinPara
     for (int64_t first = 0; first < x->cfg.vocab; first += piece) {
         const int64_t count = std::min(piece, x->cfg.vocab - first);
         const void *rows_of_w;
-        int64_t ld;
+        int64_t width, ld;
         CUtensorMap weights;
-        PSOPS_DO(piece_of_w(x, w, w_ld, first, count, &rows_of_w, &ld));
-        PSOPS_DO(make_map(x, &weights, x->cfg.type, rows_of_w, c.padded, count, ld, kHalf));
+        PSOPS_DO(piece_of_w(x, w, w_ld, first, count, &rows_of_w, &width, &ld));
+        PSOPS_DO(make_map(x, &weights, x->cfg.type, rows_of_w, width, count, ld, kHalf));
         ProductParams P = product_params(x);
         P.columns = (int)count;
         P.depth = (int)c.padded;
@@ -359,17 +360,17 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
     for (int64_t first = 0; first < x->cfg.vocab; first += x->lay.piece) {
         const int64_t count = std::min(x->lay.piece, x->cfg.vocab - first);
         const void *rows_of_w;
-        int64_t ld;
+        int64_t width, ld;
         CUtensorMap weights;
-        PSOPS_DO(piece_of_w(x, w, w_ld, first, count, &rows_of_w, &ld));
-        PSOPS_DO(make_map(x, &weights, type, rows_of_w, c.padded, count, ld, kHalf));
+        PSOPS_DO(piece_of_w(x, w, w_ld, first, count, &rows_of_w, &width, &ld));
+        PSOPS_DO(make_map(x, &weights, type, rows_of_w, width, count, ld, kHalf));
         ProductParams P = product_params(x);
         P.columns = (int)count;
         P.depth = (int)c.padded;
         P.first = (int)first;
         PSOPS_DO(product(x, kDlogits, c.tiles_m * ceil_div(count, kTile), c.hidden, weights, dlogits_out, P));
         if (dh != nullptr) {
-            PSOPS_DO(make_map(x, &weights, type, rows_of_w, c.padded, count, ld, kStepK));
+            PSOPS_DO(make_map(x, &weights, type, rows_of_w, width, count, ld, kStepK));
             P.columns = (int)c.padded;
             P.depth = (int)count;
             P.add = first > 0;
@@ -378,7 +379,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
         if (dw != nullptr) {
             uint16_t *to = direct ? (uint16_t *)dw + first * dw_ld : x->at<uint16_t>(x->lay.dw);
             CUtensorMap dw_out;
-            PSOPS_DO(make_map(x, &dw_out, type, to, c.padded, count, direct ? dw_ld : c.padded, 32));
+            PSOPS_DO(make_map(x, &dw_out, type, to, direct ? x->cfg.dim : c.padded, count, direct ? dw_ld : c.padded, 32));
             P.columns = (int)c.padded;
             P.result_rows = (int)count;
             PSOPS_DO(product(x, kDw, ceil_div(count, kTile) * tiles_d, dlogits_across, hidden_across, dw_out, P));

@@ -173,7 +173,7 @@ __device__ __forceinline__ uint4 eight_of_row(const uint16_t *row, int g, int n,
 
 constexpr int kCopyThreads = 256;
 
-// Hidden states of the tokens that count, in rows of `padded` (a multiple of 8)
+// Hidden states of the tokens that count, in rows of `padded` (a multiple of 64)
 // elements; zero rows up to a whole step of the products.  A thread per 16 bytes.
 __global__ void __launch_bounds__(kCopyThreads) psops_xent_gather_kernel(const uint16_t *h, long long ld, int dim, int padded,
                                                                          bool aligned, const XentControl *control,
