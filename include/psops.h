@@ -366,9 +366,13 @@ int psops_destroy(psops_ctx *ctx);
  * also the particle's fitness), the gradients, and an optimiser step.  The
  * operators below keep the conventions above: error codes, no device memory of
  * their own, a caller-owned 256-byte aligned workspace, work enqueued on the
- * stream given at creation, a context bound to the GPU current at creation and
- * used by one host thread at a time.  All of them are deterministic: the same
- * inputs give the same bits.
+ * context's stream, a context bound to the GPU current at creation and used by
+ * one host thread at a time.  All of them are deterministic: the same inputs
+ * give the same bits.  psops_*_set_stream moves a context to another stream of
+ * its GPU: what it enqueues there comes after what it has enqueued so far (but
+ * into a capturing stream no such wait can be recorded: order the streams
+ * before the capture).  Arrays written on yet other streams are the caller's to
+ * order, as for any kernel.
  * ---------------------------------------------------------------------------
  */
 
@@ -461,6 +465,7 @@ int psops_adamw_step(psops_adamw *opt, double lr, const float *d_scale);
 /* t, read from the device (waits for the stream). */
 int psops_adamw_steps(psops_adamw *opt, int64_t *steps);
 
+int psops_adamw_set_stream(psops_adamw *opt, void *cuda_stream);
 int64_t psops_adamw_launch_count(const psops_adamw *opt);
 const char *psops_adamw_last_error(const psops_adamw *opt);
 int psops_adamw_destroy(psops_adamw *opt);   /* waits for the stream; frees nothing of the caller's */
@@ -480,6 +485,7 @@ int psops_gradnorm_create(psops_gradnorm **out, int32_t n_tensors, const void *c
                           int32_t grad_type, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
 int psops_gradnorm_set_grads(psops_gradnorm *gn, const void *const *grads);
 int psops_gradnorm_run(psops_gradnorm *gn, float max_norm, float *d_out);
+int psops_gradnorm_set_stream(psops_gradnorm *gn, void *cuda_stream);
 int64_t psops_gradnorm_launch_count(const psops_gradnorm *gn);
 const char *psops_gradnorm_last_error(const psops_gradnorm *gn);
 int psops_gradnorm_destroy(psops_gradnorm *gn);
@@ -557,6 +563,7 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
                         const float *d_grad, int32_t reduction,
                         void *d_dh, int64_t dh_ld, void *d_dw, int64_t dw_ld);
 
+int psops_xent_set_stream(psops_xent *x, void *cuda_stream);
 int64_t psops_xent_launch_count(const psops_xent *x);
 const char *psops_xent_last_error(const psops_xent *x);
 int psops_xent_destroy(psops_xent *x);

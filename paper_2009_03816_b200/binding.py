@@ -37,11 +37,13 @@ EXPORTS = [
     "psops_shard_update_range", "psops_get_history", "psops_set_history", "psops_ssgd",
     "psops_host_register", "psops_host_unregister",
     "psops_adamw_workspace_bytes", "psops_adamw_create", "psops_adamw_set_grads", "psops_adamw_step",
-    "psops_adamw_steps", "psops_adamw_launch_count", "psops_adamw_last_error", "psops_adamw_destroy",
+    "psops_adamw_steps", "psops_adamw_set_stream", "psops_adamw_launch_count", "psops_adamw_last_error",
+    "psops_adamw_destroy",
     "psops_gradnorm_workspace_bytes", "psops_gradnorm_create", "psops_gradnorm_set_grads", "psops_gradnorm_run",
-    "psops_gradnorm_launch_count", "psops_gradnorm_last_error", "psops_gradnorm_destroy",
+    "psops_gradnorm_set_stream", "psops_gradnorm_launch_count", "psops_gradnorm_last_error",
+    "psops_gradnorm_destroy",
     "psops_xent_workspace_bytes", "psops_xent_create", "psops_xent_forward", "psops_xent_backward",
-    "psops_xent_launch_count", "psops_xent_last_error", "psops_xent_destroy",
+    "psops_xent_set_stream", "psops_xent_launch_count", "psops_xent_last_error", "psops_xent_destroy",
 ]
 
 
@@ -134,6 +136,7 @@ def load() -> ctypes.CDLL:
         "psops_adamw_set_grads": (ctypes.c_int, [_vp, ctypes.POINTER(_vp)]),
         "psops_adamw_step": (ctypes.c_int, [_vp, ctypes.c_double, _f32p]),
         "psops_adamw_steps": (ctypes.c_int, [_vp, ctypes.POINTER(ctypes.c_int64)]),
+        "psops_adamw_set_stream": (ctypes.c_int, [_vp, _vp]),
         "psops_adamw_launch_count": (ctypes.c_int64, [_vp]),
         "psops_adamw_last_error": (ctypes.c_char_p, [_vp]),
         "psops_adamw_destroy": (ctypes.c_int, [_vp]),
@@ -143,6 +146,7 @@ def load() -> ctypes.CDLL:
                                                  ctypes.c_size_t, _vp]),
         "psops_gradnorm_set_grads": (ctypes.c_int, [_vp, ctypes.POINTER(_vp)]),
         "psops_gradnorm_run": (ctypes.c_int, [_vp, ctypes.c_float, _f32p]),
+        "psops_gradnorm_set_stream": (ctypes.c_int, [_vp, _vp]),
         "psops_gradnorm_launch_count": (ctypes.c_int64, [_vp]),
         "psops_gradnorm_last_error": (ctypes.c_char_p, [_vp]),
         "psops_gradnorm_destroy": (ctypes.c_int, [_vp]),
@@ -153,6 +157,7 @@ def load() -> ctypes.CDLL:
         "psops_xent_backward": (ctypes.c_int, [_vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, ctypes.c_int64,
                                                _f32p, _f32p, ctypes.c_int32, _vp, ctypes.c_int64, _vp,
                                                ctypes.c_int64]),
+        "psops_xent_set_stream": (ctypes.c_int, [_vp, _vp]),
         "psops_xent_launch_count": (ctypes.c_int64, [_vp]),
         "psops_xent_last_error": (ctypes.c_char_p, [_vp]),
         "psops_xent_destroy": (ctypes.c_int, [_vp]),
@@ -380,6 +385,11 @@ def psops_adamw_steps(opt) -> int:
     return int(steps.value)
 
 
+def psops_adamw_set_stream(ctx, stream) -> None:
+    _check(load().psops_adamw_set_stream(ctx, int(stream) if stream else None), "psops_adamw_set_stream", ctx,
+           "psops_adamw_last_error")
+
+
 def psops_adamw_launch_count(opt) -> int:
     return int(load().psops_adamw_launch_count(opt))
 
@@ -410,6 +420,11 @@ def psops_gradnorm_set_grads(gn, grads) -> None:
 
 def psops_gradnorm_run(gn, max_norm: float, d_out) -> None:
     _check(load().psops_gradnorm_run(gn, float(max_norm), _ptr(d_out)), "psops_gradnorm_run", gn,
+           "psops_gradnorm_last_error")
+
+
+def psops_gradnorm_set_stream(ctx, stream) -> None:
+    _check(load().psops_gradnorm_set_stream(ctx, int(stream) if stream else None), "psops_gradnorm_set_stream", ctx,
            "psops_gradnorm_last_error")
 
 
@@ -447,6 +462,11 @@ def psops_xent_backward(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, d_lse, d_gra
                                       _ptr(d_lse), _ptr(d_grad), int(reduction), _ptr(d_dh), int(dh_ld), _ptr(d_dw),
                                       int(dw_ld)),
            "psops_xent_backward", x, "psops_xent_last_error")
+
+
+def psops_xent_set_stream(ctx, stream) -> None:
+    _check(load().psops_xent_set_stream(ctx, int(stream) if stream else None), "psops_xent_set_stream", ctx,
+           "psops_xent_last_error")
 
 
 def psops_xent_launch_count(x) -> int:

@@ -12,6 +12,12 @@ namespace psops_host {
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+#define PSOPS_TRY(base, call)                                             \
+    do {                                                                  \
+        const cudaError_t e_ = (call);                                    \
+        if (e_ != cudaSuccess) return (base)->fail(e_, #call);            \
+    } while (0)
+
 // What every training-operator context has: its GPU, its stream, its launch
 // count and the text of the last CUDA error.
 struct Base {
@@ -19,7 +25,13 @@ struct Base {
     int device = 0;
     int sms = 0;
     int64_t launches = 0;
+    cudaEvent_t moved = nullptr;       // orders a new stream behind the old one
     char err[256] = {0};
+
+    ~Base()
+    {
+        if (moved) cudaEventDestroy(moved);
+    }
 
     int fail(cudaError_t e, const char *what)
     {
@@ -57,6 +69,24 @@ private:
     int previous_;
 };
 
+inline int set_stream(Base *b, void *cuda_stream)
+{
+    if (b == nullptr) return PSOPS_EINVAL;
+    const cudaStream_t to = (cudaStream_t)cuda_stream;
+    if (to == b->stream) return PSOPS_OK;
+    OnDevice guard(b);
+    cudaStreamCaptureStatus from_capture = cudaStreamCaptureStatusNone, to_capture = cudaStreamCaptureStatusNone;
+    PSOPS_TRY(b, cudaStreamIsCapturing(to, &to_capture));
+    PSOPS_TRY(b, cudaStreamIsCapturing(b->stream, &from_capture));
+    if (to_capture == cudaStreamCaptureStatusNone && from_capture == cudaStreamCaptureStatusNone) {
+        if (b->moved == nullptr) PSOPS_TRY(b, cudaEventCreateWithFlags(&b->moved, cudaEventDisableTiming));
+        PSOPS_TRY(b, cudaEventRecord(b->moved, b->stream));
+        PSOPS_TRY(b, cudaStreamWaitEvent(to, b->moved, 0));
+    }
+    b->stream = to;
+    return PSOPS_OK;
+}
+
 // Page-locked staging of a small table that is sent to the device again and
 // again: the copy is asynchronous, and the staging is not overwritten before
 // the copy that read it has run.
@@ -90,9 +120,3 @@ private:
 };
 
 } // namespace psops_host
-
-#define PSOPS_TRY(base, call)                                             \
-    do {                                                                  \
-        const cudaError_t e_ = (call);                                    \
-        if (e_ != cudaSuccess) return (base)->fail(e_, #call);            \
-    } while (0)

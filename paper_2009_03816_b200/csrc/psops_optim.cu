@@ -309,6 +309,7 @@ int psops_adamw_steps(psops_adamw *a, int64_t *steps)
     return PSOPS_OK;
 }
 
+int psops_adamw_set_stream(psops_adamw *a, void *cuda_stream) { return psops_host::set_stream(a, cuda_stream); }
 int64_t psops_adamw_launch_count(const psops_adamw *a) { return a ? a->launches : 0; }
 const char *psops_adamw_last_error(const psops_adamw *a) { return a ? a->err : ""; }
 
@@ -468,6 +469,7 @@ int psops_gradnorm_run(psops_gradnorm *q, float max_norm, float *d_out)
     return q->launched("psops_gradnorm_kernel");
 }
 
+int psops_gradnorm_set_stream(psops_gradnorm *q, void *cuda_stream) { return psops_host::set_stream(q, cuda_stream); }
 int64_t psops_gradnorm_launch_count(const psops_gradnorm *q) { return q ? q->launches : 0; }
 const char *psops_gradnorm_last_error(const psops_gradnorm *q) { return q ? q->err : ""; }
 

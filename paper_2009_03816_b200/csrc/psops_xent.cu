@@ -524,6 +524,7 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
     return backward(x, d_w, w_ld, tokens, d_dh, dh_ld, d_dw, dw_ld);
 }
 
+int psops_xent_set_stream(psops_xent *x, void *cuda_stream) { return psops_host::set_stream(x, cuda_stream); }
 int64_t psops_xent_launch_count(const psops_xent *x) { return x ? x->launches : 0; }
 const char *psops_xent_last_error(const psops_xent *x) { return x ? x->err : ""; }
 

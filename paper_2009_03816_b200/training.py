@@ -10,10 +10,10 @@ computation runs in the CUDA library.
   AdamW        one AdamW step over many tensors, moments in 32 or in 8 bits
   GradNorm     2-norm of many gradients and the factor that clips it
 
-A context belongs to one stream, the current one of its GPU when the holder is
-made (or the one given); its calls enqueue there, whatever the current stream
-is later.  Tensors that were produced on another stream have to be ordered
-before the call by the caller, as for any kernel.
+Calls enqueue on the current stream of the holder's GPU, or always on the one
+given when it is made; a call on another stream than the one before comes after
+it.  Tensors that were produced on yet another stream have to be ordered before
+the call by the caller, as for any kernel.
 """
 from __future__ import annotations
 
@@ -60,8 +60,39 @@ def _device_of(where, tensors):
     return t.device
 
 
-def _stream_on(device, stream):
-    return torch.cuda.current_stream(device).cuda_stream if stream is None else stream
+class _Holder:
+    """What the three have in common: a context, its GPU and the stream its work goes to."""
+
+    ctx = None
+
+    def _on(self, device, stream):
+        self.device = device
+        self._follows = stream is None
+        self.stream = torch.cuda.current_stream(device).cuda_stream if stream is None else int(stream)
+        return self.stream
+
+    def _follow(self):
+        """Moves the context to the current stream, unless it was given one."""
+        if self._follows:
+            now = torch._C._cuda_getCurrentRawStream(self.device.index)
+            if now != self.stream:
+                self._set_stream(self.ctx, now)
+                self.stream = now
+
+    @property
+    def launches(self) -> int:
+        return self._launch_count(self.ctx) if self.ctx is not None else 0
+
+    def close(self):
+        if self.ctx is not None:
+            self._destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 def _workspace(nbytes, device, where):
@@ -70,7 +101,7 @@ def _workspace(nbytes, device, where):
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
-class LinearXent:
+class LinearXent(_Holder):
     """Cross entropy of logits = h w^T against one label per token.
 
     tokens, dim, vocab   the most tokens of a call, and the sizes of w (vocab x dim)
@@ -85,6 +116,10 @@ class LinearXent:
         loss.backward()
     """
 
+    _set_stream = staticmethod(binding.psops_xent_set_stream)
+    _launch_count = staticmethod(binding.psops_xent_launch_count)
+    _destroy = staticmethod(binding.psops_xent_destroy)
+
     def __init__(self, tokens, dim, vocab, *, dtype=torch.bfloat16, device="cuda", gradients=True, stream=None):
         device = torch.device(device)
         if device.type != "cuda":
@@ -94,9 +129,9 @@ class LinearXent:
         self.device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
         self.tokens, self.dim, self.vocab, self.dtype = int(tokens), int(dim), int(vocab), dtype
         self._w_shape = torch.Size((self.vocab, self.dim)) if min(self.vocab, self.dim) >= 0 else None
-        self.ctx, self._launched = None, 0
+        self._launched = 0
         self._flags = PSOPS_XENT_GRADS if gradients else 0
-        self.stream = _stream_on(self.device, stream)
+        self._on(self.device, stream)
         self._open()
 
     def _open(self):
@@ -141,6 +176,7 @@ class LinearXent:
         tokens = targets.numel()
         if tokens > self.tokens:
             _refuse(where, f"{tokens} tokens, made for {self.tokens}")
+        self._follow()
         self._stage_if_needed(w, w_ld)
         return tokens, h_ld, w_ld
 
@@ -197,23 +233,24 @@ class LinearXent:
         return t, ld
 
     def __call__(self, h, w, targets, reduction="mean"):
+        """The loss with gradients.  Here h, w and targets may have any strides (a slice of a sequence, say)."""
+        if isinstance(h, torch.Tensor) and h.dim() > 2:
+            h = h.contiguous()
+        elif isinstance(h, torch.Tensor) and h.dim() == 2 and h.shape[1] > 1 and (h.stride(1) != 1 or h.stride(0) < h.shape[1]):
+            h = h.contiguous()
+        if isinstance(w, torch.Tensor) and w.dim() == 2 and w.shape[1] > 1 and (w.stride(1) != 1 or w.stride(0) < w.shape[1]):
+            w = w.contiguous()
+        if isinstance(targets, torch.Tensor):
+            targets = targets.contiguous()
         return _LinearXentFunction.apply(h, w, targets, self, reduction)
 
     @property
     def launches(self) -> int:
-        return self._launched + (binding.psops_xent_launch_count(self.ctx) if self.ctx is not None else 0)
+        return self._launched + super().launches
 
     def close(self):
-        if self.ctx is not None:
-            self._launched += binding.psops_xent_launch_count(self.ctx)
-            binding.psops_xent_destroy(self.ctx)
-            self.ctx = None
-
-    def __del__(self):  # pragma: no cover
-        try:
-            self.close()
-        except Exception:
-            pass
+        self._launched += super().launches
+        super().close()
 
 
 class _LinearXentFunction(torch.autograd.Function):
@@ -236,7 +273,7 @@ class _LinearXentFunction(torch.autograd.Function):
         return dh, dw, None, None, None
 
 
-class AdamW:
+class AdamW(_Holder):
     """AdamW over a list of parameter tensors, in one launch per step.
 
     params        fp32 device tensors, contiguous (views of a swarm's row, for instance)
@@ -254,6 +291,10 @@ class AdamW:
 
     A step whose grad_scale is not finite is skipped on the device.
     """
+
+    _set_stream = staticmethod(binding.psops_adamw_set_stream)
+    _launch_count = staticmethod(binding.psops_adamw_launch_count)
+    _destroy = staticmethod(binding.psops_adamw_destroy)
 
     def __init__(self, params, grads, *, bits=32, moments=None, copies=None, betas=(0.9, 0.999), eps=1e-8,
                  weight_decay=0.01, steps_done=0, stream=None):
@@ -301,7 +342,7 @@ class AdamW:
         decay = [float(weight_decay)] * n if not isinstance(weight_decay, (list, tuple)) else [float(d) for d in weight_decay]
         if len(decay) != n:
             _refuse(where, f"{len(decay)} weight decays, {n} parameters")
-        self.bits, self.device = bits, device
+        self.bits = bits
         cfg = binding.psops_adamw_config(float(betas[0]), float(betas[1]), float(eps), int(steps_done), bits,
                                          _TYPES[self.grads[0].dtype], copy_type, n)
         at = lambda t: t.data_ptr() if t is not None and t.numel() else None
@@ -309,17 +350,16 @@ class AdamW:
             binding.psops_adamw_tensor(at(self.params[i]), at(self.grads[i]),
                                        at(copies[i]) if copies is not None else None, at(m[i]), at(v[i]), at(ms[i]),
                                        at(vs[i]), sizes[i], decay[i]) for i in range(n)])
-        self.ctx = None
         with torch.cuda.device(device):
             self._workspace = _workspace(binding.psops_adamw_workspace_bytes(cfg, table), device, where)
-            self.stream = _stream_on(device, stream)
-            self.ctx = binding.psops_adamw_create(cfg, table, self._workspace, None, self.stream)
+            self.ctx = binding.psops_adamw_create(cfg, table, self._workspace, None, self._on(device, stream))
         self._scale = None
 
     def set_grads(self, grads):
         """Other gradient tensors for the steps to come, of the type given at first."""
         grads = _flat_list("AdamW.set_grads", "grads", grads, (self.grads[0].dtype,), self.device, len(self._sizes),
                            self._sizes)
+        self._follow()
         binding.psops_adamw_set_grads(self.ctx, grads)
         self.grads = grads
 
@@ -330,6 +370,7 @@ class AdamW:
                                            and grad_scale.dtype is torch.float32 and grad_scale.numel() == 1):
             _refuse("AdamW.step", f"grad_scale has to be one fp32 number on {self.device}")
         self._scale = grad_scale               # read by the kernel: keep it alive
+        self._follow()
         binding.psops_adamw_step(self.ctx, lr, grad_scale)
 
     @property
@@ -337,24 +378,14 @@ class AdamW:
         """Steps taken so far (waits for the stream)."""
         return binding.psops_adamw_steps(self.ctx)
 
-    @property
-    def launches(self) -> int:
-        return binding.psops_adamw_launch_count(self.ctx)
-
-    def close(self):
-        if self.ctx is not None:
-            binding.psops_adamw_destroy(self.ctx)
-            self.ctx = None
-
-    def __del__(self):  # pragma: no cover
-        try:
-            self.close()
-        except Exception:
-            pass
 
 
-class GradNorm:
+class GradNorm(_Holder):
     """2-norm of a list of gradient tensors (all of one type) together."""
+
+    _set_stream = staticmethod(binding.psops_gradnorm_set_stream)
+    _launch_count = staticmethod(binding.psops_gradnorm_launch_count)
+    _destroy = staticmethod(binding.psops_gradnorm_destroy)
 
     def __init__(self, grads, *, stream=None):
         where = "GradNorm"
@@ -364,16 +395,16 @@ class GradNorm:
         if len({g.dtype for g in grads}) != 1:
             _refuse(where, "gradients of more than one type")
         self._sizes = [g.numel() for g in grads]
-        self.ctx = None
         with torch.cuda.device(self.device):
             self._workspace = _workspace(binding.psops_gradnorm_workspace_bytes(self._sizes), self.device, where)
-            self.stream = _stream_on(self.device, stream)
             self.ctx = binding.psops_gradnorm_create([g if g.numel() else None for g in grads], self._sizes,
-                                                     _TYPES[grads[0].dtype], self._workspace, None, self.stream)
+                                                     _TYPES[grads[0].dtype], self._workspace, None,
+                                                     self._on(self.device, stream))
 
     def set_grads(self, grads):
         grads = _flat_list("GradNorm.set_grads", "grads", grads, (self.grads[0].dtype,), self.device,
                            len(self._sizes), self._sizes)
+        self._follow()
         binding.psops_gradnorm_set_grads(self.ctx, [g if g.numel() else None for g in grads])
         self.grads = grads
 
@@ -384,20 +415,7 @@ class GradNorm:
             out = torch.empty(2, dtype=torch.float32, device=self.device)
         elif out.device != self.device or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
             _refuse("GradNorm.norm", f"`out` has to be 2 fp32 numbers on {self.device}")
+        self._follow()
         binding.psops_gradnorm_run(self.ctx, max_norm, out)
         return out.unbind(0)
 
-    @property
-    def launches(self) -> int:
-        return binding.psops_gradnorm_launch_count(self.ctx)
-
-    def close(self):
-        if self.ctx is not None:
-            binding.psops_gradnorm_destroy(self.ctx)
-            self.ctx = None
-
-    def __del__(self):  # pragma: no cover
-        try:
-            self.close()
-        except Exception:
-            pass

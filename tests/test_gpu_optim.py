@@ -267,6 +267,28 @@ def test_adamw_graph_replay_other_stream_and_new_gradients():
     opt.close(), opt2.close()
 
 
+def test_adamw_and_norm_follow_the_current_stream():
+    torch.manual_seed(1)
+    n = 300_007
+    p0, g = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    want, got = p0.clone(), p0.clone()
+    a, b, gn = training.AdamW([want], [g]), training.AdamW([got], [g]), training.GradNorm([g])
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for k in range(9):
+        a.step(1e-2, gn.norm(1.0)[1])
+    torch.cuda.synchronize()
+    norms = []
+    for k in range(9):
+        with torch.cuda.stream(streams[k % 3]):
+            norm, factor = gn.norm(1.0)
+            norms.append(norm)
+            b.step(1e-2, factor)
+    torch.cuda.synchronize()
+    assert torch.equal(want, got) and len({float(x) for x in norms}) == 1
+    a.close(), b.close(), gn.close()
+
+
 def test_adamw_many_tensors_and_past_32_bits():
     # 3,000 tensors of odd sizes, then one whose byte offsets pass 2^32
     sizes = [1 + (i * 37) % 301 for i in range(3000)]

@@ -310,6 +310,83 @@ def test_autograd_matches_and_batched_shapes():
     op.close()
 
 
+def test_autograd_of_slices_and_broadcast_inputs():
+    B, S, D, V = 5, 21, 64, 130
+    h, w, y = _inputs(B * S, D, V, torch.bfloat16, 41)
+    h, y = h.view(B, S, D), y.view(B, S)
+    op = training.LinearXent(B * S, D, V)
+    # next-token slices: neither h nor the labels can be seen as one run of rows
+    h1, w1 = h.clone().requires_grad_(), w.clone().requires_grad_()
+    op(h1[:, :-1], w1, y[:, 1:]).backward()
+    flat, labels = h[:, :-1].reshape(-1, D), y[:, 1:].reshape(-1)
+    loss, _, lse = op.forward(flat, w, labels)
+    dh, dw = op.backward(flat, w, labels, lse, torch.tensor(1.0, device="cuda"))
+    assert torch.equal(h1.grad[:, :-1].reshape(-1, D), dh) and torch.equal(w1.grad, dw)
+    assert bool((h1.grad[:, -1] == 0).all())
+    # one hidden state shared by all tokens, and weights that are a transposed view
+    one = h[0, 0].clone().requires_grad_()
+    wt = w.t().contiguous().requires_grad_()
+    op(one.expand(B * S, D), wt.t(), y.reshape(-1), "sum").backward()
+    full = h[0, 0].expand(B * S, D).contiguous()
+    _, _, lse = op.forward(full, w, y.reshape(-1), "sum")
+    dh, dw = op.backward(full, w, y.reshape(-1), lse, torch.tensor(1.0, device="cuda"), "sum")
+    assert torch.equal(wt.grad, dw.t())
+    want = dh.double().sum(0)
+    assert bool(((one.grad.double() - want).abs() <= HALF[torch.bfloat16] * (want.abs() + dh.double().abs().sum(0))).all())
+    op.close()
+
+
+def test_follows_the_current_stream():
+    T, D, V = 400, 64, 3000
+    h, w, y = _inputs(T, D, V, torch.bfloat16, 42)
+    grad = torch.tensor(1.0, device="cuda")
+    op = training.LinearXent(T, D, V)
+    want = op.forward(h, w, y)
+    want_g = op.backward(h, w, y, want[2], grad)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    for k in range(9):
+        with torch.cuda.stream(streams[k % 3]):
+            got = op.forward(h, w, y)
+            got_g = op.backward(h, w, y, got[2], grad)
+            same = [torch.equal(a, b) for a, b in zip((*want, *want_g), (*got, *got_g))]
+        assert all(same), k
+    fixed = training.LinearXent(T, D, V, stream=streams[0].cuda_stream)
+    got = fixed.forward(h, w, y)
+    assert fixed.stream == streams[0].cuda_stream
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    op.close(), fixed.close()
+
+
+def test_weights_past_32_bit_offsets():
+    # 2.4e9 elements of w: both the offset in elements and in bytes pass 32 bits
+    T, D, V = 6, 4096, 590_000
+    g = torch.Generator(device="cuda").manual_seed(5)
+    w = torch.empty(V, D, device="cuda", dtype=torch.bfloat16).normal_(0.0, 0.02, generator=g)
+    h = torch.empty(T, D, device="cuda", dtype=torch.bfloat16).normal_(generator=g)
+    y = torch.tensor([V - 1, 0, V // 2, V - 300, 2 ** 19 + 1, -5], device="cuda")
+    op = training.LinearXent(T, D, V)
+    for n in (T, 2):                                  # on the tensor cores, and as few tokens
+        loss, rows, lse = op.forward(h[:n], w, y[:n])
+        keep = y[:n] >= 0
+        s = torch.cat([h[:n].double() @ w[i:i + 100_000].double().T for i in range(0, V, 100_000)], 1)
+        want = torch.logsumexp(s, 1)
+        e = (2 * D + 8) * U * (h[:n].double().abs() @ w[:1000].double().abs().T).amax(1) * 1.5
+        assert bool(((lse.double() - want).abs()[keep] <= (2 * e + 64 * U * (1 + want))[keep]).all())
+        right = s.gather(1, y[:n].clamp(min=0)[:, None])[:, 0]
+        assert bool(((rows.double() - (want - right)).abs()[keep] <= (4 * e + 128 * U * (1 + want))[keep]).all())
+        dh, dw = op.backward(h[:n], w, y[:n], lse, torch.tensor(1.0, device="cuda"), "sum")
+        for v in (0, V - 1, V - 300, 2 ** 19 + 1, 2 ** 19):
+            d = torch.exp(s[:, v] - want) - (y[:n] == v).double()
+            d = torch.where(keep, d, torch.zeros_like(d))
+            exact = d @ h[:n].double()
+            tol = (d.abs() * (HALF[torch.bfloat16] + 1e-4)) @ h[:n].double().abs() + exact.abs() * HALF[torch.bfloat16] * 1.01 + 1e-9
+            assert bool(((dw[v].double() - exact).abs() <= tol).all()), v
+        assert bool(dh.isfinite().all()) and (n == 2 or bool((dh[5] == 0).all()))
+        del s, dw
+    op.close()
+
+
 def test_no_tokens_and_fewer_tokens_than_made_for():
     D, V = 40, 90
     h, w, y = _inputs(700, D, V, torch.bfloat16, 13)
