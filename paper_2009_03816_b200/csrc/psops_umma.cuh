@@ -87,12 +87,18 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
 }
 
 // ---- tensor copies -----------------------------------------------------------
-// Load into this CTA's shared memory; `cluster_bar` may lie in either CTA of the pair.
+// Load into this CTA's shared memory; the barrier may lie in either CTA of a pair.
+template <bool PAIR>
 __device__ __forceinline__ void tensor_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t cluster_bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
-                 "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+                     "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                     "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar)
+                     : "memory");
 }
 __device__ __forceinline__ void tensor_store(const CUtensorMap *map, int x, int y, uint32_t src)
 {
@@ -119,14 +125,22 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volat
 
 // ---- tensor memory -----------------------------------------------------------
 constexpr uint32_t kTensorColumns = 512;
+template <bool PAIR>
 __device__ __forceinline__ void tensor_memory_take(uint32_t where)
 {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "n"(kTensorColumns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    if constexpr (PAIR) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "n"(kTensorColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "n"(kTensorColumns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
 }
+template <bool PAIR>
 __device__ __forceinline__ void tensor_memory_give(uint32_t base)
 {
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "n"(kTensorColumns));
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "n"(kTensorColumns));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "n"(kTensorColumns));
 }
 // 32 columns of this warp's 32 lanes: register j of a lane is column j of its row.
 __device__ __forceinline__ void tensor_memory_load(uint32_t address, uint32_t *r)
@@ -173,24 +187,34 @@ __device__ __forceinline__ uint64_t operand(uint32_t address, bool k_across)
     d |= (uint64_t)2 << 61;                                  // 128-byte swizzle
     return d;
 }
-// fp32 sums; A and B bf16 or fp16; M x N of the pair of CTAs.
+// fp32 sums; A and B bf16 or fp16; M x N of the CTA or the pair of CTAs.
 __host__ __device__ constexpr uint32_t instruction(bool bf16, bool a_across, bool b_across, int m, int n)
 {
     return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (a_across ? 1u : 0u) << 15 | (b_across ? 1u : 0u) << 16 |
            (uint32_t)(n >> 3) << 17 | (uint32_t)(m >> 4) << 24;
 }
+template <bool PAIR>
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t instr, bool add)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"((uint32_t)add)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"((uint32_t)add)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"((uint32_t)add)
+                     : "memory");
 }
-// When the products issued so far are done: arrive at this barrier of both CTAs.
+// When the products issued so far are done: arrive at this barrier, of both CTAs of a pair.
+template <bool PAIR>
 __device__ __forceinline__ void products_arrive(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-                 "h"((uint16_t)3)
-                 : "memory");
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                     "h"((uint16_t)3)
+                     : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 } // namespace umma

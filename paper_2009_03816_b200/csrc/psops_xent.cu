@@ -102,24 +102,39 @@ namespace {
 
 // All launches of a call but the first are programmatic (see after_the_kernel_before).
 template <typename... Params, typename... Args>
-int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), dim3 grid, int threads, size_t shared, Args &&...args)
+int launch_clusters(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), dim3 grid, int threads, size_t shared, int cluster,
+                    Args &&...args)
 {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = x->stream;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = follows ? 1 : 0;
+    cudaLaunchAttribute attr[2] = {};
+    unsigned n = 0;
+    if (follows) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = (unsigned)cluster;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
     if (e != cudaSuccess) return x->fail(e, name);
     x->launches += 1;
     return PSOPS_OK;
 }
 
+template <typename... Params, typename... Args>
+int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), dim3 grid, int threads, size_t shared, Args &&...args)
+{
+    return launch_clusters(x, name, follows, kernel, grid, threads, shared, 1, std::forward<Args>(args)...);
+}
 template <typename... Params, typename... Args>
 int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), int64_t grid, int threads, size_t shared, Args &&...args)
 {
@@ -134,6 +149,9 @@ int64_t copy_grid(const psops_xent *x, int64_t pieces) { return std::min<int64_t
         const int rc_ = (call);              \
         if (rc_ != PSOPS_OK) return rc_;     \
     } while (0)
+
+// Which products run with pairs of CTAs.
+bool in_pairs(int job, int64_t tokens) { return job == kDw || tokens > kSingleTokens; }
 
 bool aligned16(const void *p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && ld % 8 == 0; }
 
@@ -173,7 +191,7 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
     P.steps = (int)ceil_div(last, kStepK);
     P.tiles_across = (int)ceil_div(x->lay.padded, kTile);
     P.sum_rows = (int)x->lay.sum_rows;
-    P.pairs = x->sms / 2;
+    P.pairs = in_pairs(kDh, P.tokens) ? x->sms / 2 : x->sms;
     PSOPS_DO(launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel, 1, kIndexThreads, 0, P));
     const int64_t rows = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kStepK);
     return launch(x, "psops_xent_gather_kernel", true, psops_xent_gather_kernel, copy_grid(x, rows * x->lay.padded / 8), kCopyThreads, 0,
@@ -217,21 +235,27 @@ int make_map(psops_xent *x, CUtensorMap *map, int type, const void *base, int64_
 
 using ProductKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ProductParams);
 template <class T>
-ProductKernel product_of(int job)
+ProductKernel product_of(int job, bool pair)
 {
-    return job == kLoss ? psops_xent_product_kernel<T, kLoss> : job == kDlogits ? psops_xent_product_kernel<T, kDlogits>
-           : job == kDh ? psops_xent_product_kernel<T, kDh> : psops_xent_product_kernel<T, kDw>;
+    return job == kDw        ? psops_xent_product_kernel<T, kDw, true>
+           : job == kLoss    ? (pair ? psops_xent_product_kernel<T, kLoss, true> : psops_xent_product_kernel<T, kLoss, false>)
+           : job == kDlogits ? (pair ? psops_xent_product_kernel<T, kDlogits, true> : psops_xent_product_kernel<T, kDlogits, false>)
+                             : (pair ? psops_xent_product_kernel<T, kDh, true> : psops_xent_product_kernel<T, kDh, false>);
 }
-ProductKernel product_of(const psops_xent *x, int job)
+ProductKernel product_of(const psops_xent *x, int job, bool pair)
 {
-    return x->cfg.type == PSOPS_F16 ? product_of<__half>(job) : product_of<__nv_bfloat16>(job);
+    return x->cfg.type == PSOPS_F16 ? product_of<__half>(job, pair) : product_of<__nv_bfloat16>(job, pair);
 }
 
-// `works`: tiles (times shares) if every token counts.
-int product(psops_xent *x, int job, int64_t works, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out, const ProductParams &P)
+// `tiles` (times shares): if every token counts.
+int product(psops_xent *x, int job, int64_t tokens, int64_t tiles, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &out,
+            const ProductParams &P)
 {
-    const unsigned grid = 2u * (unsigned)std::max<int64_t>(1, std::min<int64_t>(works, x->sms / 2));
-    return launch(x, "psops_xent_product_kernel", true, product_of(x, job), grid, kProductThreads, kProductShared, a, b, out, P);
+    const bool pair = in_pairs(job, tokens);
+    const int64_t ctas = pair ? 2 : 1;
+    const dim3 grid((unsigned)(ctas * std::max<int64_t>(1, std::min<int64_t>(tiles, x->sms / ctas))));
+    return launch_clusters(x, "psops_xent_product_kernel", true, product_of(x, job, pair), grid, kProductThreads,
+                  pair ? ProductShape<true>::kShared : ProductShape<false>::kShared, (int)ctas, a, b, out, P);
 }
 
 ProductParams product_params(const psops_xent *x)
@@ -331,7 +355,7 @@ int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinPara
         P.columns = (int)count;
         P.depth = (int)c.padded;
         P.first = (int)first;
-        PSOPS_DO(product(x, kLoss, c.tiles_m * ceil_div(count, kTile), c.hidden, weights, weights, P));
+        PSOPS_DO(product(x, kLoss, tokens, c.tiles_m * ceil_div(count, kTile), c.hidden, weights, weights, P));
     }
     J.stats = x->at<float2>(x->lay.stats);
     J.stats_ld = x->lay.rows;
@@ -368,13 +392,13 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
         P.columns = (int)count;
         P.depth = (int)c.padded;
         P.first = (int)first;
-        PSOPS_DO(product(x, kDlogits, c.tiles_m * ceil_div(count, kTile), c.hidden, weights, dlogits_out, P));
+        PSOPS_DO(product(x, kDlogits, tokens, c.tiles_m * ceil_div(count, kTile), c.hidden, weights, dlogits_out, P));
         if (dh != nullptr) {
             PSOPS_DO(make_map(x, &weights, type, rows_of_w, width, count, ld, kStepK));
             P.columns = (int)c.padded;
             P.depth = (int)count;
             P.add = first > 0;
-            PSOPS_DO(product(x, kDh, c.tiles_m * tiles_d * kMostShares, dlogits_along, weights, sums, P));
+            PSOPS_DO(product(x, kDh, tokens, c.tiles_m * tiles_d * kMostShares, dlogits_along, weights, sums, P));
         }
         if (dw != nullptr) {
             uint16_t *to = direct ? (uint16_t *)dw + first * dw_ld : x->at<uint16_t>(x->lay.dw);
@@ -382,7 +406,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             PSOPS_DO(make_map(x, &dw_out, type, to, direct ? x->cfg.dim : c.padded, count, direct ? dw_ld : c.padded, 32));
             P.columns = (int)c.padded;
             P.result_rows = (int)count;
-            PSOPS_DO(product(x, kDw, ceil_div(count, kTile) * tiles_d, dlogits_across, hidden_across, dw_out, P));
+            PSOPS_DO(product(x, kDw, tokens, ceil_div(count, kTile) * tiles_d, dlogits_across, hidden_across, dw_out, P));
             if (!direct) {
                 const int64_t grid = std::min<int64_t>(ceil_div(count, kCopyThreads / 32), (int64_t)x->sms * 8);
                 PSOPS_DO(launch(x, "psops_xent_unpack_kernel", true, psops_xent_unpack_kernel, grid, kCopyThreads, 0, to, (int)c.padded, count,
@@ -426,8 +450,10 @@ int psops_xent_create(psops_xent **out, const psops_xent_config *cfg, void *d_wo
     if (e == cudaSuccess)
         e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", (void **)&x->encode, 12000, cudaEnableDefault, &found);
     if (e == cudaSuccess && found != cudaDriverEntryPointSuccess) e = cudaErrorNotSupported;
-    for (int job = kLoss; e == cudaSuccess && job <= kDw; ++job)
-        e = cudaFuncSetAttribute((const void *)product_of(x, job), cudaFuncAttributeMaxDynamicSharedMemorySize, kProductShared);
+    for (int job = kLoss; job <= kDw; ++job)
+        for (int pair = 0; pair < 2 && e == cudaSuccess; ++pair)
+            e = cudaFuncSetAttribute((const void *)product_of(x, job, pair != 0), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     job == kDw || pair ? ProductShape<true>::kShared : ProductShape<false>::kShared);
     const bool half = cfg->type == PSOPS_F16;
     const void *heads[2] = {half ? (const void *)psops_xent_head_kernel<__half, false> : (const void *)psops_xent_head_kernel<__nv_bfloat16, false>,
                             half ? (const void *)psops_xent_head_kernel<__half, true> : (const void *)psops_xent_head_kernel<__nv_bfloat16, true>};

@@ -51,7 +51,7 @@ struct IndexParams {
     int tiles_across, steps, sum_rows, pairs;    // dh: tiles of its columns, steps of the shortest piece, room for sums, pairs of CTAs
 };
 
-constexpr int kMostShares = 16;
+constexpr int kMostShares = 32;
 constexpr int kShareCost = 4;                    // a tile's start and end, in steps
 constexpr int kShareJoin = 6;                    // a tile's sums written and read once more, that many tiles to a step
 
@@ -59,15 +59,16 @@ constexpr int kShareJoin = 6;                    // a tile's sums written and re
 // long: it is split into shares, as many as bring the rounds of tiles to the
 // least time (8 x 4 tiles on 74 pairs: one share leaves 42 pairs idle, two
 // shares ten; measured 183 -> 100 us for 1,950 rows, 32,003 entries, dim 1000).
+// By a whole warp, each lane looking at one number of shares; ties go to the fewest.
 __device__ __forceinline__ int best_shares(int tiles, int steps, int most, int pairs)
 {
-    int best = 1;
-    long long least = 1ll << 62;
-    for (int s = 1; s <= most; ++s) {
-        const long long t = (long long)((tiles * s + pairs - 1) / pairs) * ((steps + s - 1) / s + kShareCost) + (long long)tiles * s / kShareJoin;
-        if (t < least) { least = t; best = s; }
-    }
-    return best;
+    static_assert(kMostShares <= 32, "a lane for each");
+    const int s = (threadIdx.x & 31) + 1;
+    const long long rounds = ((long long)tiles * s + pairs - 1) / pairs;
+    const long long t = rounds * ((steps + s - 1) / s + kShareCost) + (long long)tiles * s / kShareJoin;
+    const unsigned mine = s > most || t >= 0xffffffffll ? 0xffffffffu : (unsigned)t;
+    const unsigned least = __reduce_min_sync(0xffffffffu, mine);
+    return least == 0xffffffffu ? 1 : __ffs((int)__ballot_sync(0xffffffffu, mine == least));
 }
 
 constexpr int kIndexThreads = 1024;
@@ -150,14 +151,15 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
         }
         at += __popc(votes);
     }
+    const int tiles = max(1, (total + kTileRows - 1) / kTileRows);
+    int shares = 1;
+    if (P.grad != nullptr && warp == 0)
+        shares = best_shares(tiles * P.tiles_across, P.steps, min(min(kMostShares, P.steps), P.sum_rows / (tiles * kTileRows)), P.pairs);
     if (threadIdx.x == 0) {
         P.control->rows = total;
         P.control->tickets = 0;
-        if (P.grad != nullptr) {
-            const int tiles = max(1, (total + kTileRows - 1) / kTileRows);
-            P.control->share_rows = tiles * kTileRows;
-            P.control->shares = best_shares(tiles * P.tiles_across, P.steps, min(min(kMostShares, P.steps), P.sum_rows / (tiles * kTileRows)), P.pairs);
-        }
+        P.control->share_rows = tiles * kTileRows;
+        P.control->shares = shares;
     }
 }
 
@@ -226,22 +228,32 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const u
 //   kDh       compact rows         dim            vocabulary     fp32 sums, added up over pieces
 //   kDw       vocabulary           dim            compact rows   dw, 16 bits
 //
-// Warp 0 of each CTA copies its half of both operands (128 rows of A, 128 of
-// B: 32 KB a step, kStages in flight), one thread of the first CTA issues the
+// Warp 0 of each CTA copies its share of both operands (of a pair: 128 rows of
+// A and 128 of B, 32 KB a step), one thread of the first CTA issues the
 // products, warps 4 to 11 of each CTA turn the other one of two 256-column
 // accumulators into the job's output meanwhile.  kDh and kDw read operands whose
 // summed axis runs across the rows in memory: the copies bring 64 x 64 boxes,
 // and the product's descriptors say so; nothing is transposed.
+//
+// With 128 tokens or fewer half of a pair's rows would be empty; the first
+// three jobs then run with single CTAs on 128 x 256 tiles.
 // ---------------------------------------------------------------------------
 enum Job { kLoss = 0, kDlogits = 1, kDh = 2, kDw = 3 };
 
 constexpr int kTile = 256, kHalf = 128;
-constexpr int kStages = 5;
-constexpr int kStageBytes = 2 * kHalf * kStepK * 2;              // this CTA's halves of A and B
+constexpr int kOperandBytes = kHalf * kStepK * 2;                // 128 rows of A or B
 constexpr int kOutBytes = 32 * 128;                              // a warp's 32 rows of 128 bytes on their way out
 constexpr int kOutWarps = 8;
 constexpr int kProductThreads = 384;
-constexpr int kProductShared = kStages * kStageBytes + kOutWarps * 2 * kOutBytes + 1024;   // two outputs a warp; 1024: alignment
+constexpr int kSingleTokens = kHalf;                             // up to here single CTAs
+// A pair: 32 KB a stage for each CTA, five of them, and two outputs a warp; a
+// single CTA: 48 KB a stage, four of them, one output.
+template <bool PAIR> struct ProductShape {
+    static constexpr int kCtas = PAIR ? 2 : 1, kRows = kHalf * kCtas;
+    static constexpr int kStages = PAIR ? 5 : 4, kOuts = PAIR ? 2 : 1;
+    static constexpr int kStageBytes = kOperandBytes * (PAIR ? 2 : 3);
+    static constexpr int kShared = kStages * kStageBytes + kOutWarps * kOuts * kOutBytes + 1024;       // 1024: alignment
+};
 constexpr int kChainSteps = 12;                                  // most steps of a logit summed by the tensor cores in one go
 constexpr int kGroupTiles = 8;                                   // row tiles that share columns in L2
 
@@ -305,14 +317,16 @@ __device__ __forceinline__ Work work_of(int i, int tiles_m, int tiles_n)
     return w;
 }
 
-template <class T, int JOB>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kProductThreads, 1)
+template <class T, int JOB, bool PAIR>
+__global__ void __launch_bounds__(kProductThreads, 1)
 psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                           const __grid_constant__ CUtensorMap map_out, const ProductParams P)
 {
     constexpr bool kAAcross = JOB == kDw, kBAcross = JOB == kDh || JOB == kDw;
     constexpr bool kChained = JOB == kLoss || JOB == kDlogits;
-    constexpr uint32_t kInstruction = umma::instruction(__is_same(T, __nv_bfloat16), kAAcross, kBAcross, kTile, kTile);
+    using S = ProductShape<PAIR>;
+    constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes, kRows = S::kRows;
+    constexpr uint32_t kInstruction = umma::instruction(__is_same(T, __nv_bfloat16), kAAcross, kBAcross, kRows, kTile);
 
     extern __shared__ uint8_t raw[];
     __shared__ alignas(8) uint64_t bar_full[kStages], bar_empty[kStages], bar_sum[2], bar_free[2];
@@ -320,7 +334,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     __shared__ int failed_slot;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = umma::cta_rank();
+    const uint32_t rank = PAIR ? umma::cta_rank() : 0;
     volatile int *failed = &failed_slot;
     const uint32_t stages = (umma::shared_address(raw) + 1023u) & ~1023u;
     const uint32_t outs = stages + kStages * kStageBytes;
@@ -332,14 +346,14 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
         }
         for (int b = 0; b < 2; ++b) {
             umma::barrier_init(umma::shared_address(&bar_sum[b]), 1);
-            umma::barrier_init(umma::shared_address(&bar_free[b]), 2 * kOutWarps);
+            umma::barrier_init(umma::shared_address(&bar_free[b]), S::kCtas * kOutWarps);
         }
         failed_slot = 0;
         umma::barrier_init_done();
         umma::prefetch_map(&map_a);
         umma::prefetch_map(&map_b);
     }
-    if (warp == 2) umma::tensor_memory_take(umma::shared_address(&tensor_base_slot));
+    if (warp == 2) umma::tensor_memory_take<PAIR>(umma::shared_address(&tensor_base_slot));
     umma::fence_before();
     __syncthreads();
     umma::cluster_sync();
@@ -349,7 +363,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     after_the_kernel_before();
     const int rows = P.control->rows;
     const int some_rows = max(1, rows);
-    const int tiles_m = JOB == kDw ? (P.result_rows + kTile - 1) / kTile : JOB == kDh ? (rows + kTile - 1) / kTile : (some_rows + kTile - 1) / kTile;
+    const int tiles_m = ((JOB == kDw ? P.result_rows : JOB == kDh ? rows : some_rows) + kRows - 1) / kRows;
     const int tiles_n = (P.columns + kTile - 1) / kTile;
     const int steps = ((JOB == kDw ? some_rows : P.depth) + kStepK - 1) / kStepK;
     const int fewest = (steps + kChainSteps - 1) / kChainSteps;                        // chains of a logit, of like length
@@ -357,7 +371,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     const int chains = (steps + chain - 1) / chain;
     const int splits = JOB == kDh ? P.control->shares : 1;
     const int works = tiles_m * tiles_n * splits;
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int pair = blockIdx.x / S::kCtas, pairs = gridDim.x / S::kCtas;
 
     if (warp == 0) {
         // ---- copies in (all lanes wait, one issues)
@@ -367,25 +381,30 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
         for (int i = pair; i < works && ok; i += pairs) {
             const Work w = work_of(i, tiles_m, tiles_n);
             const int k_first = (int)((long long)steps * w.split / splits), k_last = (int)((long long)steps * (w.split + 1) / splits);
-            const int m0 = w.m * kTile + (int)rank * kHalf, n0 = w.n * kTile + (int)rank * kHalf;
+            const int m0 = w.m * kRows + (int)rank * kHalf, n0 = w.n * kTile + (int)rank * kHalf;
             for (int k = k_first; k < k_last; ++k) {
                 ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_empty[s]), phase ^ 1u, failed));
                 if (!ok) break;
                 if (umma::elected()) {
                     const uint32_t full = umma::in_cta(umma::shared_address(&bar_full[s]), 0);
-                    if (rank == 0) umma::barrier_expect(umma::shared_address(&bar_full[s]), 2 * kStageBytes);
-                    const uint32_t a = stages + s * kStageBytes, b = a + kStageBytes / 2;
+                    if (rank == 0) umma::barrier_expect(umma::shared_address(&bar_full[s]), S::kCtas * kStageBytes);
+                    const uint32_t a = stages + s * kStageBytes, b = a + kOperandBytes;
                     if (kAAcross) {
-                        umma::tensor_load(a, &map_a, m0, k * kStepK, full);
-                        umma::tensor_load(a + umma::kAcross, &map_a, m0 + 64, k * kStepK, full);
+                        umma::tensor_load<PAIR>(a, &map_a, m0, k * kStepK, full);
+                        umma::tensor_load<PAIR>(a + umma::kAcross, &map_a, m0 + 64, k * kStepK, full);
                     } else {
-                        umma::tensor_load(a, &map_a, k * kStepK, m0, full);
+                        umma::tensor_load<PAIR>(a, &map_a, k * kStepK, m0, full);
                     }
-                    if (kBAcross) {
-                        umma::tensor_load(b, &map_b, n0, k * kStepK, full);
-                        umma::tensor_load(b + umma::kAcross, &map_b, n0 + 64, k * kStepK, full);
-                    } else {
-                        umma::tensor_load(b, &map_b, k * kStepK, n0, full);
+#pragma unroll
+                    for (int part = 0; part < (PAIR ? 1 : 2); ++part) {        // 128 rows of B each
+                        const uint32_t to = b + part * kOperandBytes;
+                        const int n = n0 + part * kHalf;
+                        if (kBAcross) {
+                            umma::tensor_load<PAIR>(to, &map_b, n, k * kStepK, full);
+                            umma::tensor_load<PAIR>(to + umma::kAcross, &map_b, n + 64, k * kStepK, full);
+                        } else {
+                            umma::tensor_load<PAIR>(to, &map_b, k * kStepK, n, full);
+                        }
                     }
                 }
                 __syncwarp();
@@ -398,7 +417,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
         int s = 0, buffer = 0;
         uint32_t phase = 0, buffer_phase = 0;
         bool ok = true;
-        const uint64_t first_a = umma::operand(stages, kAAcross), first_b = umma::operand(stages + kStageBytes / 2, kBAcross);
+        const uint64_t first_a = umma::operand(stages, kAAcross), first_b = umma::operand(stages + kOperandBytes, kBAcross);
         for (int i = pair; i < works && ok; i += pairs) {
             const Work w = work_of(i, tiles_m, tiles_n);
             const int k_first = (int)((long long)steps * w.split / splits), k_last = (int)((long long)steps * (w.split + 1) / splits);
@@ -418,9 +437,9 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                     const uint64_t da = first_a + (uint32_t)s * (kStageBytes >> 4), db = first_b + (uint32_t)s * (kStageBytes >> 4);
 #pragma unroll
                     for (int j = 0; j < kStepK / 16; ++j)  // 16 of the summed axis: 32 bytes along a row, or two groups of 8 rows
-                        umma::multiply(sums, da + (kAAcross ? j * 128 : j * 2), db + (kBAcross ? j * 128 : j * 2), kInstruction, link > 0 || j > 0);
-                    umma::products_arrive(umma::shared_address(&bar_empty[s]));
-                    if (ends) umma::products_arrive(umma::shared_address(&bar_sum[buffer]));
+                        umma::multiply<PAIR>(sums, da + (kAAcross ? j * 128 : j * 2), db + (kBAcross ? j * 128 : j * 2), kInstruction, link > 0 || j > 0);
+                    umma::products_arrive<PAIR>(umma::shared_address(&bar_empty[s]));
+                    if (ends) umma::products_arrive<PAIR>(umma::shared_address(&bar_sum[buffer]));
                 }
                 __syncwarp();
                 if (++s == kStages) { s = 0; phase ^= 1u; }
@@ -431,15 +450,15 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     } else if (warp >= 4) {
         // ---- results: this warp has 32 rows (its quarter of tensor memory) and 128 columns
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        const uint32_t both_outs = outs + (warp - 4) * 2 * kOutBytes;
-        int turn = 0;                                // which of the two is written next
+        const uint32_t own_outs = outs + (warp - 4) * S::kOuts * kOutBytes;
+        int turn = 0;                                // which of them is written next
         const float unscale = JOB == kDw ? P.control->unscale : 1.0f;
         const int share_rows = JOB == kDh ? P.control->share_rows : 0;
         int buffer = 0;
         uint32_t phase = 0;
         for (int i = pair; i < works; i += pairs) {
             const Work w = work_of(i, tiles_m, tiles_n);
-            const int row0 = w.m * kTile + (int)rank * kHalf + quarter * 32, row = row0 + lane;
+            const int row0 = w.m * kRows + (int)rank * kHalf + quarter * 32, row = row0 + lane;
             const int col0 = w.n * kTile + half * kHalf;
             int y = -1;
             float lse = 0.0f, g = 0.0f;
@@ -500,9 +519,9 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                     constexpr int kBoxes = JOB == kDh ? 2 : 1;         // 128 bytes a row: 32 fp32 or 64 16-bit columns
 #pragma unroll
                     for (int box = 0; box < kBoxes; ++box) {
-                        const uint32_t out = both_outs + turn * kOutBytes;
-                        turn ^= 1;
-                        if (lane == 0) umma::stores_read<1>();
+                        const uint32_t out = own_outs + turn * kOutBytes;
+                        turn = (turn + 1) % S::kOuts;
+                        if (lane == 0) umma::stores_read<S::kOuts - 1>();
                         __syncwarp();
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
@@ -597,7 +616,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     __syncthreads();
     umma::cluster_sync();                        // nobody reads the other's shared or tensor memory any more
     umma::fence_after();
-    if (warp == 2) umma::tensor_memory_give(tensor_base);
+    if (warp == 2) umma::tensor_memory_give<PAIR>(tensor_base);
     if (threadIdx.x == 0 && *failed) atomicExch(&P.control->error, 1);
 }
 
