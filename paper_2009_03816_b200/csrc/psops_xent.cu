@@ -192,11 +192,13 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
     P.tiles_across = (int)ceil_div(x->lay.padded, kTile);
     P.sum_rows = (int)x->lay.sum_rows;
     P.pairs = in_pairs(kDh, P.tokens) ? x->sms / 2 : x->sms;
-    PSOPS_DO(launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel, 1, kIndexThreads, 0, P));
-    const int64_t rows = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kStepK);
-    return launch(x, "psops_xent_gather_kernel", true, psops_xent_gather_kernel, copy_grid(x, rows * x->lay.padded / 8), kCopyThreads, 0,
-                  (const uint16_t *)h, h_ld, (int)x->cfg.dim, (int)x->lay.padded, aligned16(h, h_ld), P.control, P.row_of,
-                  x->at<uint16_t>(x->lay.hidden));
+    const GatherParams G{(const uint16_t *)h, h_ld, (int)x->cfg.dim, (int)x->lay.padded, aligned16(h, h_ld), x->at<uint16_t>(x->lay.hidden)};
+    const int64_t pieces = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kStepK) * x->lay.padded / 8;
+    if (P.tokens <= kIndexThreads)
+        return launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel<true>,
+                      std::min<int64_t>(ceil_div(pieces, kIndexThreads), (int64_t)x->sms), kIndexThreads, 0, P, G);
+    PSOPS_DO(launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel<false>, 1, kIndexThreads, 0, P, G));
+    return launch(x, "psops_xent_gather_kernel", true, psops_xent_gather_kernel, copy_grid(x, pieces), kCopyThreads, 0, G, P.control, P.row_of);
 }
 
 // The rows of w of one piece as the products read them: in place, or packed into the workspace.

@@ -82,12 +82,51 @@ __device__ __forceinline__ void after_the_kernel_before()
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// One block lists the tokens that count, in order: each warp a stretch of them.
-__global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const IndexParams P)
+// Elements [8 g, 8 g + 8) of a row of `n` 16-bit values, zeros beyond its end.
+__device__ __forceinline__ uint4 eight_of_row(const uint16_t *row, int g, int n, bool aligned)
 {
+    if (aligned && g * 8 + 8 <= n) return *reinterpret_cast<const uint4 *>(row + g * 8);
+    uint32_t e[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = g * 8 + j < n ? row[g * 8 + j] : 0u;
+    return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+}
+
+// Where the hidden states come from and go to.
+struct GatherParams {
+    const uint16_t *h;
+    long long ld;
+    int dim, padded;
+    bool aligned;
+    uint16_t *out;
+};
+
+// Hidden states of the tokens that count, in rows of `padded` (a multiple of 64)
+// elements; zero rows up to a whole step of the products.  A thread per 16 bytes.
+__device__ __forceinline__ void gather_rows(const GatherParams &G, int rows, const int *row_of)
+{
+    const unsigned groups = G.padded / 8;
+    const long long whole = (long long)(max(1, rows) + kStepK - 1) / kStepK * kStepK * groups;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < whole; i += (long long)gridDim.x * blockDim.x) {
+        const int r = (int)(i / groups), g = (int)(i - (long long)r * groups);
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (r < rows) u = eight_of_row(G.h + row_of[r] * G.ld, g, G.dim, G.aligned);
+        reinterpret_cast<uint4 *>(G.out)[i] = u;
+    }
+}
+
+// One block lists the tokens that count, in order: each warp a stretch of them.
+// GATHER: with no more tokens than threads every block makes the list for
+// itself, the first one also writes it down, and all of them gather: one launch
+// instead of two.
+template <bool GATHER>
+__global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const IndexParams P, const GatherParams G)
+{
+    __shared__ int own_row_of[GATHER ? kIndexThreads : 1];
     __shared__ int warp_sum[32];
     __shared__ float warp_top[32];
     after_the_kernel_before();
+    const bool writes = !GATHER || blockIdx.x == 0;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = (P.tokens + kIndexThreads - 1) / kIndexThreads * 32;
     const int first = min(P.tokens, warp * per), last = min(P.tokens, first + per);
@@ -127,7 +166,7 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
         int e = 0;
         if (top > 0.0f && top < INFINITY) e = min(120, max(-100, ilogbf(top) + 1));
         up = ldexpf(P.headroom, -e);
-        if (threadIdx.x == 0) P.control->unscale = 1.0f / up;
+        if (writes && threadIdx.x == 0) P.control->unscale = 1.0f / up;
     }
 #pragma unroll 2
     for (int t0 = first; t0 < last; t0 += 32) {
@@ -137,14 +176,17 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
         const unsigned votes = __ballot_sync(0xffffffffu, in);
         if (in) {
             const int r = at + __popc(votes & ((1u << lane) - 1u));
-            P.row_of[r] = t;
-            P.label[r] = (int)y;
-            P.compact_of[t] = r;
-            if (P.grad != nullptr) {
-                P.row_scale[r] = (P.reduction == PSOPS_PER_TOKEN ? P.grad[t] : common) * up;
-                P.row_lse[r] = P.lse[t] * kLog2e;
+            if (GATHER) own_row_of[r] = t;
+            if (writes) {
+                P.row_of[r] = t;
+                P.label[r] = (int)y;
+                P.compact_of[t] = r;
+                if (P.grad != nullptr) {
+                    P.row_scale[r] = (P.reduction == PSOPS_PER_TOKEN ? P.grad[t] : common) * up;
+                    P.row_lse[r] = P.lse[t] * kLog2e;
+                }
             }
-        } else if (t < last) {
+        } else if (writes && t < last) {
             P.compact_of[t] = -1;
             if (P.rows_out != nullptr) P.rows_out[t] = 0.0f;
             if (P.lse_out != nullptr) P.lse_out[t] = 0.0f;
@@ -153,44 +195,27 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
     }
     const int tiles = max(1, (total + kTileRows - 1) / kTileRows);
     int shares = 1;
-    if (P.grad != nullptr && warp == 0)
+    if (P.grad != nullptr && writes && warp == 0)
         shares = best_shares(tiles * P.tiles_across, P.steps, min(min(kMostShares, P.steps), P.sum_rows / (tiles * kTileRows)), P.pairs);
-    if (threadIdx.x == 0) {
+    if (writes && threadIdx.x == 0) {
         P.control->rows = total;
         P.control->tickets = 0;
         P.control->share_rows = tiles * kTileRows;
         P.control->shares = shares;
     }
-}
-
-// Elements [8 g, 8 g + 8) of a row of `n` 16-bit values, zeros beyond its end.
-__device__ __forceinline__ uint4 eight_of_row(const uint16_t *row, int g, int n, bool aligned)
-{
-    if (aligned && g * 8 + 8 <= n) return *reinterpret_cast<const uint4 *>(row + g * 8);
-    uint32_t e[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = g * 8 + j < n ? row[g * 8 + j] : 0u;
-    return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    if (GATHER) {
+        __syncthreads();
+        gather_rows(G, total, own_row_of);
+    }
 }
 
 constexpr int kCopyThreads = 256;
 
-// Hidden states of the tokens that count, in rows of `padded` (a multiple of 64)
-// elements; zero rows up to a whole step of the products.  A thread per 16 bytes.
-__global__ void __launch_bounds__(kCopyThreads) psops_xent_gather_kernel(const uint16_t *h, long long ld, int dim, int padded,
-                                                                         bool aligned, const XentControl *control,
-                                                                         const int *row_of, uint16_t *out)
+// The gathering alone, behind the list.
+__global__ void __launch_bounds__(kCopyThreads) psops_xent_gather_kernel(const GatherParams G, const XentControl *control, const int *row_of)
 {
     after_the_kernel_before();
-    const int rows = control->rows;
-    const unsigned groups = padded / 8;
-    const long long whole = (long long)(max(1, rows) + kStepK - 1) / kStepK * kStepK * groups;
-    for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < whole; i += (long long)gridDim.x * kCopyThreads) {
-        const int r = (int)(i / groups), g = (int)(i - (long long)r * groups);
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (r < rows) u = eight_of_row(h + row_of[r] * ld, g, dim, aligned);
-        reinterpret_cast<uint4 *>(out)[i] = u;
-    }
+    gather_rows(G, control->rows, row_of);
 }
 
 // Rows of w that cannot be read in place.
