@@ -27,7 +27,7 @@ constexpr float kLn2 = 0.6931471805599453f;
 struct XentControl {
     int rows;                                    // tokens that count
     unsigned tickets;
-    float unscale;                               // power of two: gradient sums * unscale = gradients
+    float unscale;                               // gradient sums * unscale = gradients
     int error;
     int shares;                                  // dh: its sum over the vocabulary in so many shares
     int share_rows;                              // rows between the shares' sums
@@ -40,7 +40,7 @@ struct IndexParams {
     int *row_of;                                 // compact row -> token
     int *compact_of;                             // token -> compact row, or -1
     int *label;                                  // compact row -> label
-    float *row_scale;                            // compact row -> grad_t times a power of two (backward)
+    float *row_scale;                            // compact row -> what its 16-bit gradients are multiplied with (backward)
     float *rows_out, *lse_out;                   // zeroed where a token is left out (forward)
     const float *lse;                            // (backward) by token
     float *row_lse;                              // (backward) by compact row, times log2 e
@@ -156,17 +156,22 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
         total += warp_sum[w];
         top = fmaxf(top, warp_top[w]);
     }
-    float common = 0.0f, up = 1.0f;
+    // What the 16-bit logits' gradients are multiplied with, and what undoes it in
+    // the fp32 sums.  One gradient for all tokens stays out of the 16 bits (its own
+    // rounding would be the same for every token and add up); gradients per token
+    // are scaled by a power of two that brings the largest to (1/2, 1] * headroom.
+    float up = P.headroom;
     if (P.grad != nullptr) {
+        float undo;
         if (P.reduction != PSOPS_PER_TOKEN) {
-            common = P.reduction == PSOPS_MEAN ? __fdiv_rn(P.grad[0], (float)max(1, total)) : P.grad[0];
-            top = fabsf(common);
+            undo = (P.reduction == PSOPS_MEAN ? __fdiv_rn(P.grad[0], (float)max(1, total)) : P.grad[0]) / P.headroom;
+        } else {
+            int e = 0;
+            if (top > 0.0f && top < INFINITY) e = min(120, max(-100, ilogbf(top) + 1));
+            up = ldexpf(P.headroom, -e);
+            undo = 1.0f / up;
         }
-        // gradients are normalised by a power of two, so that the largest |grad_t| lies in (1/2, 1] * headroom
-        int e = 0;
-        if (top > 0.0f && top < INFINITY) e = min(120, max(-100, ilogbf(top) + 1));
-        up = ldexpf(P.headroom, -e);
-        if (writes && threadIdx.x == 0) P.control->unscale = 1.0f / up;
+        if (writes && threadIdx.x == 0) P.control->unscale = undo;
     }
 #pragma unroll 2
     for (int t0 = first; t0 < last; t0 += 32) {
@@ -182,7 +187,7 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
                 P.label[r] = (int)y;
                 P.compact_of[t] = r;
                 if (P.grad != nullptr) {
-                    P.row_scale[r] = (P.reduction == PSOPS_PER_TOKEN ? P.grad[t] : common) * up;
+                    P.row_scale[r] = P.reduction == PSOPS_PER_TOKEN ? P.grad[t] * up : up;
                     P.row_lse[r] = P.lse[t] * kLog2e;
                 }
             }
@@ -530,11 +535,14 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                             for (int j = 0; j < 64; ++j)
                                 if (j == hit) u[j] = __float_as_uint(__uint_as_float(u[j]) - 1.0f);
                         }
-                        // rows and columns that are only padding become zeros
-                        const int mine = row < rows ? left : 0;
 #pragma unroll
-                        for (int j = 0; j < 64; ++j)
-                            u[j] = j < mine ? __float_as_uint(__uint_as_float(u[j]) * g) : 0u;
+                        for (int j = 0; j < 64; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) * g);
+                        if (left < 64 || row0 + 32 > rows) {           // rows and columns that are only padding become zeros
+                            const int mine = row < rows ? left : 0;
+#pragma unroll
+                            for (int j = 0; j < 64; ++j)
+                                if (j >= mine) u[j] = 0u;
+                        }
                     } else if (JOB == kDw) {
 #pragma unroll
                         for (int j = 0; j < 64; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) * unscale);
