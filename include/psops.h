@@ -506,7 +506,10 @@ int psops_gradnorm_destroy(psops_gradnorm *gn);
  *   dh = dlogits w,  dw = dlogits^T h
  * with grad_t = *d_grad / n (PSOPS_MEAN), *d_grad (PSOPS_SUM) or d_grad[t]
  * (PSOPS_PER_TOKEN).  The gradient pass computes the logits once more, a piece
- * of the vocabulary at a time.
+ * of the vocabulary at a time.  At a label the bracket is exp(-rows[t]) - 1; with
+ * the rows of the forward pass at hand it keeps its digits where the token is
+ * predicted with confidence, without them it is formed from the fp32 lse and
+ * loses them as rows[t] goes below some 1e-3.
  *
  * Rounding: products are summed in fp32, softmax statistics are fp32, the loss
  * is summed in double.  dlogits enters the two gradient products rounded to
@@ -553,13 +556,14 @@ int psops_xent_forward(psops_xent *x, const void *d_h, int64_t h_ld, const void 
                        float *d_loss, float *d_rows, float *d_lse);
 
 /*
- * Gradients, from the same h, w, targets and the lse of psops_xent_forward.
+ * Gradients, from the same h, w, targets and the lse of psops_xent_forward, and
+ * its rows or NULL.
  * d_grad: the upstream gradient, see above.  d_dh or d_dw may be NULL (not
  * wanted).  Both are overwritten, not added to.  Errors: as forward, and ESTATE
  * without PSOPS_XENT_GRADS.
  */
 int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void *d_w, int64_t w_ld,
-                        const int64_t *d_targets, int64_t tokens, const float *d_lse,
+                        const int64_t *d_targets, int64_t tokens, const float *d_lse, const float *d_rows,
                         const float *d_grad, int32_t reduction,
                         void *d_dh, int64_t dh_ld, void *d_dw, int64_t dw_ld);
 

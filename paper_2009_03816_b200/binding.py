@@ -155,7 +155,7 @@ def load() -> ctypes.CDLL:
         "psops_xent_forward": (ctypes.c_int, [_vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, ctypes.c_int64,
                                               ctypes.c_int32, _f32p, _f32p, _f32p]),
         "psops_xent_backward": (ctypes.c_int, [_vp, _vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, ctypes.c_int64,
-                                               _f32p, _f32p, ctypes.c_int32, _vp, ctypes.c_int64, _vp,
+                                               _f32p, _f32p, _f32p, ctypes.c_int32, _vp, ctypes.c_int64, _vp,
                                                ctypes.c_int64]),
         "psops_xent_set_stream": (ctypes.c_int, [_vp, _vp]),
         "psops_xent_launch_count": (ctypes.c_int64, [_vp]),
@@ -456,11 +456,11 @@ def psops_xent_forward(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, reduction, d_
            "psops_xent_forward", x, "psops_xent_last_error")
 
 
-def psops_xent_backward(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, d_lse, d_grad, reduction, d_dh, dh_ld, d_dw,
-                        dw_ld) -> None:
+def psops_xent_backward(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, d_lse, d_rows, d_grad, reduction, d_dh, dh_ld,
+                        d_dw, dw_ld) -> None:
     _check(load().psops_xent_backward(x, _ptr(d_h), int(h_ld), _ptr(d_w), int(w_ld), _ptr(d_targets), int(tokens),
-                                      _ptr(d_lse), _ptr(d_grad), int(reduction), _ptr(d_dh), int(dh_ld), _ptr(d_dw),
-                                      int(dw_ld)),
+                                      _ptr(d_lse), _ptr(d_rows), _ptr(d_grad), int(reduction), _ptr(d_dh), int(dh_ld),
+                                      _ptr(d_dw), int(dw_ld)),
            "psops_xent_backward", x, "psops_xent_last_error")
 
 

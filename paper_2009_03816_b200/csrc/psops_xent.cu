@@ -43,7 +43,7 @@ struct Layout {
     bool staged;                                // w and dw may pass through the workspace
     int64_t parts;                              // softmax statistics per row
     int64_t sum_rows;                           // rows of the fp32 sums of dh, all shares together
-    size_t control, row_of, compact_of, label, row_scale, row_lse, label_logit, partials, hidden, stats, w, dw, dlogits, sums, total;
+    size_t control, row_of, compact_of, label, row_scale, row_lse, row_label, label_logit, partials, hidden, stats, w, dw, dlogits, sums, total;
 };
 
 Layout make_layout(const psops_xent_config *c)
@@ -69,6 +69,7 @@ Layout make_layout(const psops_xent_config *c)
     L.label = take(4 * n);
     L.row_scale = take(4 * n);
     L.row_lse = take(4 * n);
+    L.row_label = take(4 * n);
     L.label_logit = take(4 * n);
     L.partials = take(std::max<size_t>(8 * (n / kJoinRows), sizeof(double2) * kMostBlocks));
     L.hidden = take(2 * n * (size_t)L.padded);
@@ -184,6 +185,7 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
     P.label = x->at<int>(x->lay.label);
     P.row_scale = x->at<float>(x->lay.row_scale);
     P.row_lse = x->at<float>(x->lay.row_lse);
+    P.row_label = x->at<float>(x->lay.row_label);
     P.vocab = (int)x->cfg.vocab;
     P.headroom = x->cfg.type == PSOPS_F16 ? 32768.0f : 1.0f;
     // every piece of the vocabulary gives every share of dh something to add up, the shortest piece too
@@ -267,6 +269,7 @@ ProductParams product_params(const psops_xent *x)
     P.label = x->at<int>(x->lay.label);
     P.row_lse = x->at<float>(x->lay.row_lse);
     P.row_scale = x->at<float>(x->lay.row_scale);
+    P.row_label = x->at<float>(x->lay.row_label);
     P.stats = x->at<float2>(x->lay.stats);
     P.stats_ld = x->lay.rows;
     P.label_logit = x->at<float>(x->lay.label_logit);
@@ -519,8 +522,8 @@ int psops_xent_forward(psops_xent *x, const void *d_h, int64_t h_ld, const void 
 }
 
 int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void *d_w, int64_t w_ld,
-                        const int64_t *d_targets, int64_t tokens, const float *d_lse, const float *d_grad, int32_t reduction,
-                        void *d_dh, int64_t dh_ld, void *d_dw, int64_t dw_ld)
+                        const int64_t *d_targets, int64_t tokens, const float *d_lse, const float *d_rows,
+                        const float *d_grad, int32_t reduction, void *d_dh, int64_t dh_ld, void *d_dw, int64_t dw_ld)
 {
     if (x == nullptr || reduction < PSOPS_MEAN || reduction > PSOPS_PER_TOKEN) return PSOPS_EINVAL;
     if (!(x->cfg.flags & PSOPS_XENT_GRADS)) return PSOPS_ESTATE;
@@ -529,12 +532,13 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
     if (rc == PSOPS_OK && d_dw != nullptr) rc = check_matrix(d_dw, dw_ld, x->cfg.vocab, x->cfg.dim);
     if (rc != PSOPS_OK) return rc;
     if (d_grad == nullptr || (tokens > 0 && d_lse == nullptr)) return PSOPS_EINVAL;
-    if (((uintptr_t)d_lse | (uintptr_t)d_grad) & 3u) return PSOPS_EALIGN;
+    if (((uintptr_t)d_lse | (uintptr_t)d_rows | (uintptr_t)d_grad) & 3u) return PSOPS_EALIGN;
     if (d_dw != nullptr && !x->lay.staged && !aligned16(d_dw, dw_ld)) return PSOPS_EALIGN;
     OnDevice guard(x);
     if (is_head(x->cfg.vocab, x->cfg.dim, tokens)) {
         HeadParams H = head_params(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, reduction);
         H.lse = d_lse;
+        H.known_rows = d_rows;
         H.grad = d_grad;
         H.dlogits = x->at<float>(x->lay.dlogits);
         H.dh = d_dh;
@@ -545,6 +549,7 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
     P.targets = (const long long *)d_targets;
     P.grad = d_grad;
     P.lse = d_lse;
+    P.rows = d_rows;
     P.tokens = (int)tokens;
     P.reduction = reduction;
     rc = gather(x, P, d_h, h_ld);

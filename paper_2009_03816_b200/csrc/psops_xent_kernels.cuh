@@ -42,7 +42,8 @@ struct IndexParams {
     int *label;                                  // compact row -> label
     float *row_scale;                            // compact row -> what its 16-bit gradients are multiplied with (backward)
     float *rows_out, *lse_out;                   // zeroed where a token is left out (forward)
-    const float *lse;                            // (backward) by token
+    const float *lse, *rows;                     // (backward) by token; rows may be NULL
+    float *row_label;                            // (backward) compact row -> exp(-rows) - 1, or 2 where rows are not given
     float *row_lse;                              // (backward) by compact row, times log2 e
     int tokens;
     int vocab;
@@ -189,6 +190,7 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
                 if (P.grad != nullptr) {
                     P.row_scale[r] = P.reduction == PSOPS_PER_TOKEN ? P.grad[t] * up : up;
                     P.row_lse[r] = P.lse[t] * kLog2e;
+                    P.row_label[r] = P.rows != nullptr ? expm1f(-P.rows[t]) : 2.0f;
                 }
             }
         } else if (writes && t < last) {
@@ -304,7 +306,7 @@ struct ProductParams {
     int first;                                   // first vocabulary entry of the piece
     bool add;                                    // kDh: add to the sums of the pieces before
     const int *label;
-    const float *row_lse, *row_scale;
+    const float *row_lse, *row_scale, *row_label;
     float2 *stats;                               // (max, sum of exp2) by 128 vocabulary entries and compact row, base 2
     long long stats_ld;
     float *label_logit;
@@ -501,12 +503,13 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
             const int row0 = w.m * kRows + (int)rank * kHalf + quarter * 32, row = row0 + lane;
             const int col0 = w.n * kTile + half * kHalf;
             int y = -1;
-            float lse = 0.0f, g = 0.0f;
+            float lse = 0.0f, g = 0.0f, at_label = 2.0f;
             if (JOB == kLoss || JOB == kDlogits) {
                 if (row < rows) y = P.label[row] - P.first - col0;
                 if (JOB == kDlogits && row < rows) {
                     lse = P.row_lse[row];
                     g = P.row_scale[row];
+                    at_label = P.row_label[row];
                 }
             }
             const uint32_t quarter_base = tensor_base + ((uint32_t)(quarter * 32) << 16) + half * kHalf;
@@ -543,7 +546,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                         if (hit >= 0 && hit < 64) {
 #pragma unroll
                             for (int j = 0; j < 64; ++j)
-                                if (j == hit) u[j] = __float_as_uint(__uint_as_float(u[j]) - 1.0f);
+                                if (j == hit) u[j] = __float_as_uint(at_label > 1.0f ? __uint_as_float(u[j]) - 1.0f : at_label);
                         }
 #pragma unroll
                         for (int j = 0; j < 64; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) * g);

@@ -36,7 +36,7 @@ struct HeadParams {
     XentControl *control;
     double2 *partials;                           // (loss, tokens that count) of each block
     float *loss, *rows, *lse_out;                // forward
-    const float *lse, *grad;                     // backward
+    const float *lse, *known_rows, *grad;        // backward; known_rows: the forward pass's, or NULL
     float *dlogits;                              // tokens x wide
     void *dh;
     long long dh_ld;
@@ -136,8 +136,11 @@ __global__ void __launch_bounds__(kSmallThreads) psops_xent_head_kernel(const He
             ++counted;
         } else {
             const float lse = P.lse[t], g = P.reduction == PSOPS_PER_TOKEN ? P.grad[t] : common;
-            const float d0 = there0 ? (expf(x0 - lse) - (v == y ? 1.0f : 0.0f)) * g : 0.0f;
-            const float d1 = there1 ? (expf(x1 - lse) - (lane + 32 == y ? 1.0f : 0.0f)) * g : 0.0f;
+            const bool known = P.known_rows != nullptr;
+            const float at_label = known ? expm1f(-P.known_rows[t]) : 0.0f;
+            auto bracket = [&](float x, bool label) { return !label ? expf(x - lse) : known ? at_label : expm1f(x - lse); };
+            const float d0 = there0 ? bracket(x0, v == y) * g : 0.0f;
+            const float d1 = there1 ? bracket(x1, lane + 32 == y) * g : 0.0f;
             if (lane < wide) {
                 mine[lane] = d0;
                 P.dlogits[(long long)t * wide + lane] = d0;

@@ -111,8 +111,8 @@ class Worker:
         de, dm, dw = self.grads
         h = self.hidden(x1, x2)
         h16 = h.to(torch.bfloat16)
-        _, _, lse = self.xent.forward(h16, w, y)
-        dh, _ = self.xent.backward(h16, w, y, lse, one, dw=dw)
+        _, rows, lse = self.xent.forward(h16, w, y)
+        dh, _ = self.xent.backward(h16, w, y, lse, one, rows=rows, dw=dw)
         du = (dh.float() * (1.0 - h * h)).to(torch.bfloat16)
         torch.mm(e[x2].T, du, out=dm)
         de.zero_()

@@ -201,21 +201,25 @@ class LinearXent(_Holder):
         binding.psops_xent_forward(self.ctx, h, h_ld, w, w_ld, targets, tokens, _REDUCTIONS[reduction], loss, rows, lse)
         return loss, rows, lse
 
-    def backward(self, h, w, targets, lse, grad, reduction="mean", *, dh=None, dw=None, want=(True, True)):
+    def backward(self, h, w, targets, lse, grad, reduction="mean", *, rows=None, dh=None, dw=None, want=(True, True)):
         """(dh, dw) from the upstream gradient: one fp32 number, or one per token for reduction "none".
-        dh, dw: tensors to hold them; want: which of the two is computed."""
+        rows: forward's, which keep the digits of the gradients of confident tokens; dh, dw: tensors to hold the
+        result; want: which of the two is computed."""
         where = "LinearXent.backward"
         code = _REDUCTIONS.get(reduction)
         if code is None:
             _refuse(where, f"reduction {reduction!r}")
         tokens, h_ld, w_ld = self._arguments(where, h, w, targets)
         self._numbers(where, "lse", lse, targets.shape)
+        if rows is not None:
+            self._numbers(where, "rows", rows, targets.shape)
         self._numbers(where, "grad", grad, targets.shape if code == PSOPS_PER_TOKEN else None)
         dh, dh_ld = self._gradient(where, "dh", dh, h) if want[0] else (None, 0)
         dw, dw_ld = self._gradient(where, "dw", dw, w) if want[1] else (None, 0)
         if dw is not None:
             self._stage_if_needed(dw, dw_ld)
-        binding.psops_xent_backward(self.ctx, h, h_ld, w, w_ld, targets, tokens, lse, grad, code, dh, dh_ld, dw, dw_ld)
+        binding.psops_xent_backward(self.ctx, h, h_ld, w, w_ld, targets, tokens, lse, rows, grad, code, dh, dh_ld, dw,
+                                    dw_ld)
         return dh, dw
 
     def _numbers(self, where, name, t, shape):
@@ -261,14 +265,14 @@ class _LinearXentFunction(torch.autograd.Function):
         if reduction not in ("mean", "sum", "none"):
             _refuse("LinearXent", f"reduction {reduction!r}")
         loss, rows, lse = op.forward(h, w, targets, "mean" if reduction == "mean" else "sum")
-        ctx.save_for_backward(h, w, targets, lse)
+        ctx.save_for_backward(h, w, targets, rows, lse)
         ctx.op, ctx.reduction = op, reduction
         return rows if reduction == "none" else loss
 
     @staticmethod
     def backward(ctx, grad):
-        h, w, targets, lse = ctx.saved_tensors
-        dh, dw = ctx.op.backward(h, w, targets, lse, grad.float().contiguous(), ctx.reduction,
+        h, w, targets, rows, lse = ctx.saved_tensors
+        dh, dw = ctx.op.backward(h, w, targets, lse, grad.float().contiguous(), ctx.reduction, rows=rows,
                                  want=(ctx.needs_input_grad[0], ctx.needs_input_grad[1]))
         return dh, dw, None, None, None
 

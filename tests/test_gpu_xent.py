@@ -270,6 +270,31 @@ def test_strides_offsets_and_untouched_gaps(D):
     op.close()
 
 
+@pytest.mark.parametrize("T,D,V", [(7, 64, 300), (40, 64, 300), (20, 32, 30)])
+def test_confident_tokens_keep_their_digits_with_rows(T, D, V):
+    # every token is all but certain: its loss, and with it its gradient, is about 1e-5 to 1e-3.  The loss itself is
+    # good to the fp32 error of a logit of about 20 (2e-6 and less); the gradient may add 16-bit roundings to that.
+    h, w, y = _inputs(T, D, V, torch.bfloat16, 51)
+    g = torch.Generator(device="cuda").manual_seed(52)
+    lean = 14 + 4 * torch.rand(T, 1, device="cuda", generator=g)
+    h = (h.float() * 0.1 + lean * w[y].float() / (w[y].float() ** 2).sum(1, keepdim=True)).to(torch.bfloat16)
+    op = training.LinearXent(T, D, V)
+    loss, rows, lse = op.forward(h, w, y)
+    x = _exact(h, w, y, torch.ones(T, device="cuda"))
+    assert float(x["rows"].median()) < 1e-3
+    dh, dw = op.backward(h, w, y, lse, torch.tensor(1.0, device="cuda"), "sum", rows=rows)
+    off = (rows.double() - x["rows"]).abs()                       # what the forward pass is off by
+    assert bool((off <= 4 * x["e_row"] + 64 * U * (1 + x["lse"].abs())).all())
+    spread = (HALF[torch.bfloat16] * x["d"].abs() + 2e-5 * x["p"])
+    spread.scatter_add_(1, y[:, None], (off + 4 * U * x["rows"])[:, None])
+    spread.scatter_add_(1, y[:, None], -2e-5 * x["p"].gather(1, y[:, None]))
+    tol = spread @ x["w"].abs() + x["dh"].abs() * HALF[torch.bfloat16] * 1.02 + 1e-9
+    assert bool(((dh.double() - x["dh"]).abs() <= tol).all())
+    tol = spread.T @ x["h"].abs() + x["dw"].abs() * HALF[torch.bfloat16] * 1.02 + 1e-9
+    assert bool(((dw.double() - x["dw"]).abs() <= tol).all())
+    op.close()
+
+
 def test_gradients_against_differences():
     T, D, V = 24, 32, 50
     h, w, y = _inputs(T, D, V, torch.bfloat16, 11, masked=0.2)
@@ -296,7 +321,7 @@ def test_autograd_matches_and_batched_shapes():
     h, w, y = _inputs(T, D, V, torch.bfloat16, 12, masked=0.3)
     op = training.LinearXent(T, D, V)
     loss, rows, lse = op.forward(h, w, y)
-    dh, dw = op.backward(h, w, y, lse, torch.tensor(2.0, device="cuda"))
+    dh, dw = op.backward(h, w, y, lse, torch.tensor(2.0, device="cuda"), rows=rows)
     h3 = h.view(6, 20, D).clone().requires_grad_()
     w3 = w.clone().requires_grad_()
     out = op(h3, w3, y.view(6, 20))
@@ -319,8 +344,8 @@ def test_autograd_of_slices_and_broadcast_inputs():
     h1, w1 = h.clone().requires_grad_(), w.clone().requires_grad_()
     op(h1[:, :-1], w1, y[:, 1:]).backward()
     flat, labels = h[:, :-1].reshape(-1, D), y[:, 1:].reshape(-1)
-    loss, _, lse = op.forward(flat, w, labels)
-    dh, dw = op.backward(flat, w, labels, lse, torch.tensor(1.0, device="cuda"))
+    loss, rows, lse = op.forward(flat, w, labels)
+    dh, dw = op.backward(flat, w, labels, lse, torch.tensor(1.0, device="cuda"), rows=rows)
     assert torch.equal(h1.grad[:, :-1].reshape(-1, D), dh) and torch.equal(w1.grad, dw)
     assert bool((h1.grad[:, -1] == 0).all())
     # one hidden state shared by all tokens, and weights that are a transposed view
@@ -328,8 +353,8 @@ def test_autograd_of_slices_and_broadcast_inputs():
     wt = w.t().contiguous().requires_grad_()
     op(one.expand(B * S, D), wt.t(), y.reshape(-1), "sum").backward()
     full = h[0, 0].expand(B * S, D).contiguous()
-    _, _, lse = op.forward(full, w, y.reshape(-1), "sum")
-    dh, dw = op.backward(full, w, y.reshape(-1), lse, torch.tensor(1.0, device="cuda"), "sum")
+    _, rows, lse = op.forward(full, w, y.reshape(-1), "sum")
+    dh, dw = op.backward(full, w, y.reshape(-1), lse, torch.tensor(1.0, device="cuda"), "sum", rows=rows)
     assert torch.equal(wt.grad, dw.t())
     want = dh.double().sum(0)
     assert bool(((one.grad.double() - want).abs() <= HALF[torch.bfloat16] * (want.abs() + dh.double().abs().sum(0))).all())

@@ -101,5 +101,5 @@ def test_xent_refuses_before_touching_cuda(lib):
         assert not out.value
     assert lib.psops_xent_create(ctypes.byref(out), None, 0x100, 1 << 30, None) == binding.PSOPS_EINVAL
     assert lib.psops_xent_forward(None, None, 0, None, 0, None, 0, 0, None, None, None) == binding.PSOPS_EINVAL
-    assert lib.psops_xent_backward(None, None, 0, None, 0, None, 0, None, None, 0, None, 0, None, 0) == binding.PSOPS_EINVAL
+    assert lib.psops_xent_backward(None, None, 0, None, 0, None, 0, None, None, None, 0, None, 0, None, 0) == binding.PSOPS_EINVAL
     assert lib.psops_xent_destroy(None) == binding.PSOPS_EINVAL
