@@ -196,7 +196,7 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
     P.pairs = in_pairs(kDh, P.tokens) ? x->sms / 2 : x->sms;
     const GatherParams G{(const uint16_t *)h, h_ld, (int)x->cfg.dim, (int)x->lay.padded, aligned16(h, h_ld), x->at<uint16_t>(x->lay.hidden)};
     const int64_t pieces = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kStepK) * x->lay.padded / 8;
-    if (P.tokens <= kIndexThreads)
+    if (P.tokens <= kListTokens)
         return launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel<true>,
                       std::min<int64_t>(ceil_div(pieces, kIndexThreads), (int64_t)x->sms), kIndexThreads, 0, P, G);
     PSOPS_DO(launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel<false>, 1, kIndexThreads, 0, P, G));

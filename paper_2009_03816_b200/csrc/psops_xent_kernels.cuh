@@ -117,13 +117,14 @@ __device__ __forceinline__ void gather_rows(const GatherParams &G, int rows, con
 }
 
 // One block lists the tokens that count, in order: each warp a stretch of them.
-// GATHER: with no more tokens than threads every block makes the list for
+// GATHER: with no more than kListTokens tokens every block makes the list for
 // itself, the first one also writes it down, and all of them gather: one launch
 // instead of two.
+constexpr int kListTokens = 8192;
 template <bool GATHER>
 __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const IndexParams P, const GatherParams G)
 {
-    __shared__ int own_row_of[GATHER ? kIndexThreads : 1];
+    __shared__ int own_row_of[GATHER ? kListTokens : 1];
     __shared__ int warp_sum[32];
     __shared__ float warp_top[32];
     after_the_kernel_before();
@@ -715,20 +716,32 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) psops_xent_join_kernel
     tops[part][lane] = top;
     sums[part][lane] = sum;
     __syncthreads();
-    if (part == 0) {
+    // warp `part` joins the parts of row `part`, a lane for each
+    top = tops[lane][part];
+    sum = sums[lane][part];
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        const float top2 = __shfl_xor_sync(0xffffffffu, top, off), sum2 = __shfl_xor_sync(0xffffffffu, sum, off);
+        join(top, sum, top2, sum2);
+    }
+    if (lane == 0) {
+        const int row = blockIdx.x * kJoinRows + part;
         double loss = 0.0;
-        if (r < rows) {
-            for (int k = 1; k < kJoinParts; ++k) join(top, sum, tops[k][lane], sums[k][lane]);
-            const float lse = P.control->error ? NAN : (top + log2f(sum)) * kLn2, mine = lse - P.label_logit[r];
-            const int t = P.row_of[r];
+        if (row < rows) {
+            const float lse = P.control->error ? NAN : (top + log2f(sum)) * kLn2, mine = lse - P.label_logit[row];
+            const int t = P.row_of[row];
             if (P.rows_out != nullptr) P.rows_out[t] = mine;
             if (P.lse_out != nullptr) P.lse_out[t] = lse;
             loss = mine;
         }
-        row_loss[lane] = loss;
-        __syncwarp();
+        row_loss[part] = loss;
+    }
+    __syncthreads();
+    if (part == 0) {
+        double loss = row_loss[lane];
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, off);
         if (lane == 0) {
-            for (int k = 1; k < kJoinRows; ++k) loss += row_loss[k];
             P.partials[blockIdx.x] = loss;
             __threadfence();
             last = atomicAdd(&P.control->tickets, 1u) == gridDim.x - 1;
