@@ -38,13 +38,6 @@ struct Base {
         std::snprintf(err, sizeof(err), "%s: %s", what, cudaGetErrorString(e));
         return PSOPS_ECUDA;
     }
-    int launched(const char *what)
-    {
-        const cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return fail(e, what);
-        launches += 1;
-        return PSOPS_OK;
-    }
 };
 
 // Work of a context belongs to the GPU that was current at its creation; the
@@ -68,6 +61,29 @@ public:
 private:
     int previous_;
 };
+
+// Launches a kernel that begins with umma::after_the_kernel_before.
+template <typename... Params, typename... Args>
+int launch(Base *b, const char *name, void (*kernel)(Params...), dim3 grid, int threads, size_t shared, int cluster, Args &&...args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = b->stream;
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+    if (e != cudaSuccess) return b->fail(e, name);
+    b->launches += 1;
+    return PSOPS_OK;
+}
 
 inline int set_stream(Base *b, void *cuda_stream)
 {

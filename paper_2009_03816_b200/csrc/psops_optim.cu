@@ -294,8 +294,7 @@ int psops_adamw_step(psops_adamw *a, double lr, const float *d_scale)
     P.b2c = (float)(1.0 - a->cfg.beta2);
     P.eps = (float)a->cfg.eps;
     P.n_chunks = (unsigned)a->n_chunks;
-    a->kernel<<<a->grid, kOptThreads, 0, a->stream>>>(P);
-    return a->launched("psops_adamw_kernel");
+    return psops_host::launch(a, "psops_adamw_kernel", a->kernel, dim3(a->grid), kOptThreads, 0, 1, P);
 }
 
 int psops_adamw_steps(psops_adamw *a, int64_t *steps)
@@ -465,8 +464,7 @@ int psops_gradnorm_run(psops_gradnorm *q, float max_norm, float *d_out)
     P.out = d_out;
     P.max_norm = max_norm;
     P.n_chunks = (unsigned)q->n_chunks;
-    q->kernel<<<q->grid, kOptThreads, 0, q->stream>>>(P);
-    return q->launched("psops_gradnorm_kernel");
+    return psops_host::launch(q, "psops_gradnorm_kernel", q->kernel, dim3(q->grid), kOptThreads, 0, 1, P);
 }
 
 int psops_gradnorm_set_stream(psops_gradnorm *q, void *cuda_stream) { return psops_host::set_stream(q, cuda_stream); }

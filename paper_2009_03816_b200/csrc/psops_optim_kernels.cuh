@@ -21,6 +21,8 @@
 
 #include <cstdint>
 
+#include "psops_umma.cuh"
+
 namespace {
 
 constexpr int kOptThreads = 256;
@@ -346,6 +348,7 @@ template <int BITS, class G, class C>
 __global__ void __launch_bounds__(kOptThreads, kAdamwBlocks<BITS>) psops_adamw_kernel(const __grid_constant__ AdamwParams P)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    umma::after_the_kernel_before();
     AdamwFactors F;
     F.scale = P.scale != nullptr ? *P.scale : 1.0f;
     if (!(fabsf(F.scale) < INFINITY)) return;                       // skipped: nothing changes, t stays
@@ -452,6 +455,7 @@ __global__ void __launch_bounds__(kOptThreads) psops_gradnorm_kernel(const NormP
     using S = NormShape<G>;
     __shared__ double shared[kOptWarps];
     __shared__ bool last;
+    umma::after_the_kernel_before();
     double sum = 0.0;
     for (unsigned c = blockIdx.x; c < P.n_chunks; c += gridDim.x) {
         const uint2 chunk = P.chunks[c];

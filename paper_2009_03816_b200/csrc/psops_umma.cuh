@@ -24,6 +24,14 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t address, uint32_t rank)
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(address), "r"(rank));
     return r;
 }
+// Programmatic launches: a kernel may set itself up while the one before it in
+// the stream still runs, and waits here before it reads or writes anything;
+// everything before is complete and visible then.
+__device__ __forceinline__ void after_the_kernel_before()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
 // True in one lane of a converged warp, the same one each time.
 __device__ __forceinline__ bool elected()
 {

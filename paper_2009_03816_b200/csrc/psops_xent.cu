@@ -101,45 +101,15 @@ struct psops_xent : Base {
 
 namespace {
 
-// All launches of a call but the first are programmatic (see after_the_kernel_before).
 template <typename... Params, typename... Args>
-int launch_clusters(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), dim3 grid, int threads, size_t shared, int cluster,
-                    Args &&...args)
+int launch(psops_xent *x, const char *name, void (*kernel)(Params...), dim3 grid, int threads, size_t shared, Args &&...args)
 {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = shared;
-    cfg.stream = x->stream;
-    cudaLaunchAttribute attr[2] = {};
-    unsigned n = 0;
-    if (follows) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n++].val.programmaticStreamSerializationAllowed = 1;
-    }
-    if (cluster > 1) {
-        attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = (unsigned)cluster;
-        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
-        ++n;
-    }
-    cfg.attrs = attr;
-    cfg.numAttrs = n;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
-    if (e != cudaSuccess) return x->fail(e, name);
-    x->launches += 1;
-    return PSOPS_OK;
-}
-
-template <typename... Params, typename... Args>
-int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), dim3 grid, int threads, size_t shared, Args &&...args)
-{
-    return launch_clusters(x, name, follows, kernel, grid, threads, shared, 1, std::forward<Args>(args)...);
+    return psops_host::launch(x, name, kernel, grid, threads, shared, 1, std::forward<Args>(args)...);
 }
 template <typename... Params, typename... Args>
-int launch(psops_xent *x, const char *name, bool follows, void (*kernel)(Params...), int64_t grid, int threads, size_t shared, Args &&...args)
+int launch(psops_xent *x, const char *name, void (*kernel)(Params...), int64_t grid, int threads, size_t shared, Args &&...args)
 {
-    return launch(x, name, follows, kernel, dim3((unsigned)std::max<int64_t>(1, grid)), threads, shared, std::forward<Args>(args)...);
+    return launch(x, name, kernel, dim3((unsigned)std::max<int64_t>(1, grid)), threads, shared, std::forward<Args>(args)...);
 }
 
 // Blocks of a copy of so many 16-byte pieces, one or more a thread.
@@ -197,10 +167,10 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
     const GatherParams G{(const uint16_t *)h, h_ld, (int)x->cfg.dim, (int)x->lay.padded, aligned16(h, h_ld), x->at<uint16_t>(x->lay.hidden)};
     const int64_t pieces = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kStepK) * x->lay.padded / 8;
     if (P.tokens <= kListTokens)
-        return launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel<true>,
+        return launch(x, "psops_xent_index_kernel", psops_xent_index_kernel<true>,
                       std::min<int64_t>(ceil_div(pieces, kIndexThreads), (int64_t)x->sms), kIndexThreads, 0, P, G);
-    PSOPS_DO(launch(x, "psops_xent_index_kernel", false, psops_xent_index_kernel<false>, 1, kIndexThreads, 0, P, G));
-    return launch(x, "psops_xent_gather_kernel", true, psops_xent_gather_kernel, copy_grid(x, pieces), kCopyThreads, 0, G, P.control, P.row_of);
+    PSOPS_DO(launch(x, "psops_xent_index_kernel", psops_xent_index_kernel<false>, 1, kIndexThreads, 0, P, G));
+    return launch(x, "psops_xent_gather_kernel", psops_xent_gather_kernel, copy_grid(x, pieces), kCopyThreads, 0, G, P.control, P.row_of);
 }
 
 // The rows of w of one piece as the products read them: in place, or packed into the workspace.
@@ -216,7 +186,7 @@ int piece_of_w(psops_xent *x, const void *w, int64_t w_ld, int64_t first, int64_
     uint16_t *to = x->at<uint16_t>(x->lay.w);
     *out = to;
     *width = *out_ld = x->lay.padded;
-    return launch(x, "psops_xent_pack_kernel", true, psops_xent_pack_kernel, copy_grid(x, count * x->lay.padded / 8), kCopyThreads, 0, from,
+    return launch(x, "psops_xent_pack_kernel", psops_xent_pack_kernel, copy_grid(x, count * x->lay.padded / 8), kCopyThreads, 0, from,
                   w_ld, count, (int)x->cfg.dim, (int)x->lay.padded, aligned16(w, w_ld), to);
 }
 
@@ -258,8 +228,8 @@ int product(psops_xent *x, int job, int64_t tokens, int64_t tiles, const CUtenso
     const bool pair = in_pairs(job, tokens);
     const int64_t ctas = pair ? 2 : 1;
     const dim3 grid((unsigned)(ctas * std::max<int64_t>(1, std::min<int64_t>(tiles, x->sms / ctas))));
-    return launch_clusters(x, "psops_xent_product_kernel", true, product_of(x, job, pair), grid, kProductThreads,
-                  pair ? ProductShape<true>::kShared : ProductShape<false>::kShared, (int)ctas, a, b, out, P);
+    return psops_host::launch(x, "psops_xent_product_kernel", product_of(x, job, pair), grid, kProductThreads,
+                              pair ? ProductShape<true>::kShared : ProductShape<false>::kShared, (int)ctas, a, b, out, P);
 }
 
 ProductParams product_params(const psops_xent *x)
@@ -308,16 +278,16 @@ template <class T>
 int forward_head(psops_xent *x, HeadParams P)
 {
     const int64_t grid = std::min<int64_t>(ceil_div(P.tokens, kSmallWarps), std::min<int64_t>(x->sms, kMostBlocks));
-    return launch(x, "psops_xent_head_kernel", false, psops_xent_head_kernel<T, false>, grid, kSmallThreads, head_shared(P.vocab, P.dim), P);
+    return launch(x, "psops_xent_head_kernel", psops_xent_head_kernel<T, false>, grid, kSmallThreads, head_shared(P.vocab, P.dim), P);
 }
 
 template <class T>
 int backward_head(psops_xent *x, HeadParams P, void *dw, int64_t dw_ld)
 {
     const int64_t grid = std::min<int64_t>(ceil_div(P.tokens, kSmallWarps), std::min<int64_t>(x->sms, kMostBlocks));
-    PSOPS_DO(launch(x, "psops_xent_head_kernel", false, psops_xent_head_kernel<T, true>, grid, kSmallThreads, head_shared(P.vocab, P.dim), P));
+    PSOPS_DO(launch(x, "psops_xent_head_kernel", psops_xent_head_kernel<T, true>, grid, kSmallThreads, head_shared(P.vocab, P.dim), P));
     if (dw == nullptr) return PSOPS_OK;
-    return launch(x, "psops_xent_head_dw_kernel", true, psops_xent_head_dw_kernel<T>,
+    return launch(x, "psops_xent_head_dw_kernel", psops_xent_head_dw_kernel<T>,
                   dim3((unsigned)ceil_div(P.dim, 32), (unsigned)ceil_div(P.vocab, kHeadDwClasses)), kHeadDwThreads, 0, (const T *)P.h, P.h_ld,
                   P.targets, (const float *)P.dlogits, P.tokens, P.dim, P.vocab, (T *)dw, dw_ld);
 }
@@ -339,7 +309,7 @@ int forward_few(psops_xent *x, FewParams P)
 {
     const auto kernel = few_kernel<T>(few_of(P.tokens), P.w_aligned && P.dim % 8 == 0);
     const int64_t grid = std::min<int64_t>(std::min<int64_t>((int64_t)x->sms * kFewBlocks, kMostBlocks), ceil_div(P.vocab, kSmallWarps));
-    return launch(x, "psops_xent_few_kernel", false, kernel, grid, kSmallThreads, few_shared(P.tokens, P.dim), P);
+    return launch(x, "psops_xent_few_kernel", kernel, grid, kSmallThreads, few_shared(P.tokens, P.dim), P);
 }
 
 int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinParams J)
@@ -369,7 +339,7 @@ int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinPara
     J.row_of = x->at<int>(x->lay.row_of);
     J.label_logit = x->at<float>(x->lay.label_logit);
     J.partials = x->at<double>(x->lay.partials);
-    return launch(x, "psops_xent_join_kernel", true, psops_xent_join_kernel, ceil_div(tokens, kJoinRows), kJoinRows * kJoinParts, 0, J);
+    return launch(x, "psops_xent_join_kernel", psops_xent_join_kernel, ceil_div(tokens, kJoinRows), kJoinRows * kJoinParts, 0, J);
 }
 
 int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *dh, int64_t dh_ld, void *dw, int64_t dw_ld)
@@ -414,7 +384,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             PSOPS_DO(product(x, kDw, tokens, ceil_div(count, kTile) * tiles_d, dlogits_across, hidden_across, dw_out, P));
             if (!direct) {
                 const int64_t grid = std::min<int64_t>(ceil_div(count, kCopyThreads / 32), (int64_t)x->sms * 8);
-                PSOPS_DO(launch(x, "psops_xent_unpack_kernel", true, psops_xent_unpack_kernel, grid, kCopyThreads, 0, to, (int)c.padded, count,
+                PSOPS_DO(launch(x, "psops_xent_unpack_kernel", psops_xent_unpack_kernel, grid, kCopyThreads, 0, to, (int)c.padded, count,
                                 (int)x->cfg.dim, (uint16_t *)dw + first * dw_ld, dw_ld));
             }
         }
@@ -422,7 +392,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
     if (dh == nullptr || tokens == 0) return PSOPS_OK;
     const bool aligned = ((uintptr_t)dh & 7u) == 0 && dh_ld % 4 == 0;
     auto out = [&](auto *typed, auto kernel) {
-        return launch(x, "psops_xent_dh_out_kernel", true, kernel, copy_grid(x, tokens * ceil_div(x->cfg.dim, 4)), kCopyThreads, 0,
+        return launch(x, "psops_xent_dh_out_kernel", kernel, copy_grid(x, tokens * ceil_div(x->cfg.dim, 4)), kCopyThreads, 0,
                       x->at<float>(x->lay.sums), c.padded, x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
                       (int)x->cfg.dim, aligned, typed, dh_ld);
     };

@@ -74,14 +74,7 @@ __device__ __forceinline__ int best_shares(int tiles, int steps, int most, int p
 
 constexpr int kIndexThreads = 1024;
 
-// Kernels of one call follow each other with programmatic launches: the next
-// one may set itself up while this one runs, and waits here before it reads
-// anything; what it needs is complete then, and so is everything before.
-__device__ __forceinline__ void after_the_kernel_before()
-{
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
+using umma::after_the_kernel_before;
 
 // Elements [8 g, 8 g + 8) of a row of `n` 16-bit values, zeros beyond its end.
 __device__ __forceinline__ uint4 eight_of_row(const uint16_t *row, int g, int n, bool aligned)

@@ -61,6 +61,7 @@ __global__ void __launch_bounds__(kSmallThreads) psops_xent_head_kernel(const He
     float *w = head_shared_memory;                                   // dim x pitch
     float *hidden = w + (size_t)P.dim * pitch + (size_t)warp * P.dim;
     float *mine = w + (size_t)P.dim * (pitch + kSmallWarps) + warp * kHeadClasses;
+    after_the_kernel_before();
     for (int i = threadIdx.x; i < P.vocab * P.dim; i += kSmallThreads) {
         const int v = i / P.dim, d = i - v * P.dim;
         w[d * pitch + v] = wide16(((const T *)P.w)[v * P.w_ld + d]);
@@ -288,6 +289,7 @@ __global__ void __launch_bounds__(kSmallThreads, kFewBlocks) psops_xent_few_kern
     __shared__ bool last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int chunks = (P.dim + 255) / 256;
+    after_the_kernel_before();
     for (int i = threadIdx.x; i < N * chunks * 32; i += kSmallThreads) {
         const int t = i / (chunks * 32), g = i - t * chunks * 32;    // group g of eight of token t
         uint4 u = make_uint4(0, 0, 0, 0);
