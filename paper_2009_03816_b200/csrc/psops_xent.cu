@@ -24,6 +24,12 @@ namespace {
 // Bytes that the logits' gradients of one piece of the vocabulary may take.
 constexpr int64_t kPieceBytes = 512ll << 20;
 constexpr int64_t kMinPiece = 2048;
+// Pairs of CTAs that run at once on a B200 (148 SMs), where a layout must not ask the GPU.
+constexpr int64_t kPairs = 74;
+// From so many tokens on, dw of a small vocabulary is summed in shares.  Gradients
+// in a CUDA graph, whole / in shares: 1,024 x 1,024 x 2,300: 41 / 46 us; 2,048 x 512
+// x 300: 40 / 36; 4,000 x 1,000 x 500: 60 / 52; 8,192 x 2,048 x 177: 132 / 111.
+constexpr int64_t kSplitTokens = 1536;
 // Most blocks of the small kernels' launches (they have a partial result each).
 constexpr int64_t kMostBlocks = 1024;
 // Bytes that the fp32 sums of dh may take in more than one share.
@@ -43,7 +49,8 @@ struct Layout {
     bool staged;                                // w and dw may pass through the workspace
     int64_t parts;                              // softmax statistics per row
     int64_t sum_rows;                           // rows of the fp32 sums of dh, all shares together
-    size_t control, row_of, compact_of, label, row_scale, row_lse, row_label, label_logit, partials, hidden, stats, w, dw, dlogits, sums, total;
+    int64_t dw_most;                            // most shares of dw's sum over the tokens; 1: not split
+    size_t control, row_of, compact_of, label, row_scale, row_lse, row_label, label_logit, partials, hidden, stats, w, dw, dlogits, sums, dw_sums, total;
 };
 
 Layout make_layout(const psops_xent_config *c)
@@ -79,6 +86,10 @@ Layout make_layout(const psops_xent_config *c)
         if (L.staged) L.dw = take(2 * (size_t)L.piece * (size_t)L.padded);
         L.dlogits = take(2 * n * (size_t)L.piece);
         L.sums = take(4 * (size_t)L.sum_rows * (size_t)L.padded);
+        // a small vocabulary gives dw few tiles: then its sum over the tokens is split
+        const int64_t tiles = whole / kTile * ceil_div(L.padded, kTile);
+        L.dw_most = std::max<int64_t>(1, std::min<int64_t>(kMostShares, kPairs / tiles));
+        if (L.dw_most > 1) L.dw_sums = take(4 * (size_t)(whole * L.dw_most) * (size_t)L.padded);
     }
     L.total = at;
     return L;
@@ -122,7 +133,7 @@ int64_t copy_grid(const psops_xent *x, int64_t pieces) { return std::min<int64_t
     } while (0)
 
 // Which products run with pairs of CTAs.
-bool in_pairs(int job, int64_t tokens) { return job == kDw || tokens > kSingleTokens; }
+bool in_pairs(int job, int64_t tokens) { return job == kDw || job == kDwSums || tokens > kSingleTokens; }
 
 bool aligned16(const void *p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && ld % 8 == 0; }
 
@@ -164,6 +175,9 @@ int gather(psops_xent *x, IndexParams P, const void *h, int64_t h_ld)
     P.tiles_across = (int)ceil_div(x->lay.padded, kTile);
     P.sum_rows = (int)x->lay.sum_rows;
     P.pairs = in_pairs(kDh, P.tokens) ? x->sms / 2 : x->sms;
+    P.dw_most = (int)x->lay.dw_most;
+    P.dw_tiles = (int)(ceil_div(x->cfg.vocab, kTile) * P.tiles_across);
+    P.dw_pairs = x->sms / 2;
     const GatherParams G{(const uint16_t *)h, h_ld, (int)x->cfg.dim, (int)x->lay.padded, aligned16(h, h_ld), x->at<uint16_t>(x->lay.hidden)};
     const int64_t pieces = (int64_t)round_up((size_t)std::max<int64_t>(1, P.tokens), kStepK) * x->lay.padded / 8;
     if (P.tokens <= kListTokens)
@@ -212,6 +226,7 @@ template <class T>
 ProductKernel product_of(int job, bool pair)
 {
     return job == kDw        ? psops_xent_product_kernel<T, kDw, true>
+           : job == kDwSums  ? psops_xent_product_kernel<T, kDwSums, true>
            : job == kLoss    ? (pair ? psops_xent_product_kernel<T, kLoss, true> : psops_xent_product_kernel<T, kLoss, false>)
            : job == kDlogits ? (pair ? psops_xent_product_kernel<T, kDlogits, true> : psops_xent_product_kernel<T, kDlogits, false>)
                              : (pair ? psops_xent_product_kernel<T, kDh, true> : psops_xent_product_kernel<T, kDh, false>);
@@ -342,6 +357,25 @@ int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinPara
     return launch(x, "psops_xent_join_kernel", psops_xent_join_kernel, ceil_div(tokens, kJoinRows), kJoinRows * kJoinParts, 0, J);
 }
 
+// dh, or dw from its shares, from fp32 sums.
+template <bool DW>
+int results(psops_xent *x, const float *sums, int dw_share_rows, int rows, void *out, int64_t ld)
+{
+    OutParams P{};
+    P.sums = sums;
+    P.sums_ld = x->lay.padded;
+    P.control = x->control();
+    P.compact_of = x->at<int>(x->lay.compact_of);
+    P.rows = rows;
+    P.dim = (int)x->cfg.dim;
+    P.dw_share_rows = dw_share_rows;
+    P.aligned = ((uintptr_t)out & 7u) == 0 && ld % 4 == 0;
+    P.out = out;
+    P.ld = ld;
+    return launch(x, "psops_xent_out_kernel", x->cfg.type == PSOPS_F16 ? psops_xent_out_kernel<__half, DW> : psops_xent_out_kernel<__nv_bfloat16, DW>,
+                  copy_grid(x, rows * ceil_div(x->cfg.dim, 4)), kCopyThreads, 0, P);
+}
+
 int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *dh, int64_t dh_ld, void *dw, int64_t dw_ld)
 {
     const int type = x->cfg.type;
@@ -375,7 +409,16 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             P.add = first > 0;
             PSOPS_DO(product(x, kDh, tokens, c.tiles_m * tiles_d * kMostShares, dlogits_along, weights, sums, P));
         }
-        if (dw != nullptr) {
+        if (dw != nullptr && x->lay.dw_most > 1 && tokens >= kSplitTokens) {      // one piece, then
+            CUtensorMap dw_sums;
+            const int64_t share_rows = (int64_t)round_up((size_t)count, kTile);
+            PSOPS_DO(make_map(x, &dw_sums, PSOPS_F32, x->at<void>(x->lay.dw_sums), c.padded, share_rows * x->lay.dw_most, c.padded, 32));
+            P.columns = (int)c.padded;
+            P.result_rows = (int)count;
+            P.dw_share_rows = (int)share_rows;
+            PSOPS_DO(product(x, kDwSums, tokens, ceil_div(count, kTile) * tiles_d * x->lay.dw_most, dlogits_across, hidden_across, dw_sums, P));
+            PSOPS_DO(results<true>(x, x->at<float>(x->lay.dw_sums), (int)share_rows, (int)count, dw, dw_ld));
+        } else if (dw != nullptr) {
             uint16_t *to = direct ? (uint16_t *)dw + first * dw_ld : x->at<uint16_t>(x->lay.dw);
             CUtensorMap dw_out;
             PSOPS_DO(make_map(x, &dw_out, type, to, direct ? x->cfg.dim : c.padded, count, direct ? dw_ld : c.padded, 32));
@@ -390,13 +433,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
         }
     }
     if (dh == nullptr || tokens == 0) return PSOPS_OK;
-    const bool aligned = ((uintptr_t)dh & 7u) == 0 && dh_ld % 4 == 0;
-    auto out = [&](auto *typed, auto kernel) {
-        return launch(x, "psops_xent_dh_out_kernel", kernel, copy_grid(x, tokens * ceil_div(x->cfg.dim, 4)), kCopyThreads, 0,
-                      x->at<float>(x->lay.sums), c.padded, x->control(), x->at<int>(x->lay.compact_of), (int)tokens,
-                      (int)x->cfg.dim, aligned, typed, dh_ld);
-    };
-    return type == PSOPS_F16 ? out((__half *)dh, psops_xent_dh_out_kernel<__half>) : out((__nv_bfloat16 *)dh, psops_xent_dh_out_kernel<__nv_bfloat16>);
+    return results<false>(x, x->at<float>(x->lay.sums), 0, (int)tokens, dh, dh_ld);
 }
 
 } // namespace
@@ -425,10 +462,10 @@ int psops_xent_create(psops_xent **out, const psops_xent_config *cfg, void *d_wo
     if (e == cudaSuccess)
         e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", (void **)&x->encode, 12000, cudaEnableDefault, &found);
     if (e == cudaSuccess && found != cudaDriverEntryPointSuccess) e = cudaErrorNotSupported;
-    for (int job = kLoss; job <= kDw; ++job)
+    for (int job = kLoss; job <= kDwSums; ++job)
         for (int pair = 0; pair < 2 && e == cudaSuccess; ++pair)
             e = cudaFuncSetAttribute((const void *)product_of(x, job, pair != 0), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     job == kDw || pair ? ProductShape<true>::kShared : ProductShape<false>::kShared);
+                                     job >= kDw || pair ? ProductShape<true>::kShared : ProductShape<false>::kShared);
     const bool half = cfg->type == PSOPS_F16;
     const void *heads[2] = {half ? (const void *)psops_xent_head_kernel<__half, false> : (const void *)psops_xent_head_kernel<__nv_bfloat16, false>,
                             half ? (const void *)psops_xent_head_kernel<__half, true> : (const void *)psops_xent_head_kernel<__nv_bfloat16, true>};

@@ -31,6 +31,7 @@ struct XentControl {
     int error;
     int shares;                                  // dh: its sum over the vocabulary in so many shares
     int share_rows;                              // rows between the shares' sums
+    int dw_shares;                               // dw, where it is split: its sum over the tokens in so many shares
 };
 
 struct IndexParams {
@@ -49,7 +50,8 @@ struct IndexParams {
     int vocab;
     int reduction;
     float headroom;                              // largest |dlogits| that the 16-bit type should see
-    int tiles_across, steps, sum_rows, pairs;    // dh: tiles of its columns, steps of the shortest piece, room for sums, pairs of CTAs
+    int tiles_across, steps, sum_rows, pairs;    // dh: tiles of its columns, steps of the shortest piece, room for sums, CTAs or pairs of them
+    int dw_tiles, dw_most, dw_pairs;             // dw, where it is split: tiles, most shares (0: not split), pairs of CTAs
 };
 
 constexpr int kMostShares = 32;
@@ -198,7 +200,13 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
     int shares = 1;
     if (P.grad != nullptr && writes && warp == 0)
         shares = best_shares(tiles * P.tiles_across, P.steps, min(min(kMostShares, P.steps), P.sum_rows / (tiles * kTileRows)), P.pairs);
+    int dw_shares = 1;
+    if (P.dw_most > 1 && writes && warp == 0) {
+        const int steps = (max(1, total) + kStepK - 1) / kStepK;
+        dw_shares = best_shares(P.dw_tiles, steps, min(P.dw_most, steps), P.dw_pairs);
+    }
     if (writes && threadIdx.x == 0) {
+        P.control->dw_shares = dw_shares;
         P.control->rows = total;
         P.control->tickets = 0;
         P.control->share_rows = tiles * kTileRows;
@@ -253,6 +261,7 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const u
 //   kDlogits  compact rows         vocabulary     dim            the logits' gradient, 16 bits
 //   kDh       compact rows         dim            vocabulary     fp32 sums, added up over pieces
 //   kDw       vocabulary           dim            compact rows   dw, 16 bits
+//   kDwSums   the same, the summed axis in shares                fp32 sums
 //
 // Warp 0 of each CTA copies its share of both operands (of a pair: 128 rows of
 // A and 128 of B, 32 KB a step), one thread of the first CTA issues the
@@ -264,7 +273,7 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const u
 // With 128 tokens or fewer half of a pair's rows would be empty; the first
 // three jobs then run with single CTAs on 128 x 256 tiles.
 // ---------------------------------------------------------------------------
-enum Job { kLoss = 0, kDlogits = 1, kDh = 2, kDw = 3 };
+enum Job { kLoss = 0, kDlogits = 1, kDh = 2, kDw = 3, kDwSums = 4 };
 
 constexpr int kTile = 256, kHalf = 128;
 constexpr int kOperandBytes = kHalf * kStepK * 2;                // 128 rows of A or B
@@ -296,7 +305,8 @@ struct ProductParams {
     XentControl *control;
     int columns;                                 // kLoss, kDlogits: entries of the piece; kDh, kDw: padded dim
     int depth;                                   // kLoss, kDlogits: padded dim; kDh: entries of the piece
-    int result_rows;                             // kDw: entries of the piece
+    int result_rows;                             // kDw, kDwSums: entries of the piece
+    int dw_share_rows;                           // kDwSums: rows between the shares' sums
     int first;                                   // first vocabulary entry of the piece
     bool add;                                    // kDh: add to the sums of the pieces before
     const int *label;
@@ -357,7 +367,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                           const __grid_constant__ CUtensorMap map_out, const ProductParams P)
 {
-    constexpr bool kAAcross = JOB == kDw, kBAcross = JOB == kDh || JOB == kDw;
+    constexpr bool kAAcross = JOB == kDw || JOB == kDwSums, kBAcross = JOB == kDh || kAAcross;
+    constexpr bool kSums = JOB == kDh || JOB == kDwSums;
     constexpr bool kChained = JOB == kLoss || JOB == kDlogits;
     using S = ProductShape<PAIR>;
     constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes, kRows = S::kRows;
@@ -398,14 +409,14 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     after_the_kernel_before();
     const int rows = P.control->rows;
     const int some_rows = max(1, rows);
-    const int tiles_m = ((JOB == kDw ? P.result_rows : JOB == kDh ? rows : some_rows) + kRows - 1) / kRows;
+    const int tiles_m = ((kAAcross ? P.result_rows : JOB == kDh ? rows : some_rows) + kRows - 1) / kRows;
     const int tiles_n = (P.columns + kTile - 1) / kTile;
-    const int steps = ((JOB == kDw ? some_rows : P.depth) + kStepK - 1) / kStepK;
+    const int steps = ((kAAcross ? some_rows : P.depth) + kStepK - 1) / kStepK;
     const int fewest = (steps + kChainSteps - 1) / kChainSteps;                        // chains of a logit, of like length
     const int chain = kChained ? (steps + fewest - 1) / fewest : steps;
     const int chains = (steps + chain - 1) / chain;
     const float put_back = 1.0f + kCutOff<T> * (float)(chain * (kStepK / 16)), unit = kLog2e * put_back;
-    const int splits = JOB == kDh ? P.control->shares : 1;
+    const int splits = JOB == kDh ? P.control->shares : JOB == kDwSums ? P.control->dw_shares : 1;
     const int works = tiles_m * tiles_n * splits;
     const int pair = blockIdx.x / S::kCtas, pairs = gridDim.x / S::kCtas;
 
@@ -489,7 +500,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
         const uint32_t own_outs = outs + (warp - 4) * S::kOuts * kOutBytes;
         int turn = 0;                                // which of them is written next
         const float unscale = JOB == kDw ? P.control->unscale : 1.0f;
-        const int share_rows = JOB == kDh ? P.control->share_rows : 0;
+        const int share_rows = JOB == kDh ? P.control->share_rows : JOB == kDwSums ? P.dw_share_rows : 0;
         int buffer = 0;
         uint32_t phase = 0;
         for (int i = pair; i < works; i += pairs) {
@@ -556,7 +567,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                     }
                     const bool wanted = JOB == kDlogits ? row0 < (some_rows + kStepK - 1) / kStepK * kStepK
                                         : JOB == kDh ? row0 < rows : row0 < P.result_rows;
-                    constexpr int kBoxes = JOB == kDh ? 2 : 1;         // 128 bytes a row: 32 fp32 or 64 16-bit columns
+                    constexpr int kBoxes = kSums ? 2 : 1;         // 128 bytes a row: 32 fp32 or 64 16-bit columns
 #pragma unroll
                     for (int box = 0; box < kBoxes; ++box) {
                         const uint32_t out = own_outs + turn * kOutBytes;
@@ -566,7 +577,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
 #pragma unroll
                         for (int j = 0; j < 8; ++j) {
                             uint4 v;
-                            if (JOB == kDh)
+                            if (kSums)
                                 v = make_uint4(u[32 * box + 4 * j], u[32 * box + 4 * j + 1], u[32 * box + 4 * j + 2], u[32 * box + 4 * j + 3]);
                             else {
                                 uint32_t p[4];
@@ -752,24 +763,34 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) psops_xent_join_kernel
     if (lane == 0) *P.loss = P.reduction == PSOPS_MEAN ? (float)(total / (double)max(1, rows)) : (float)total;
 }
 
-// dh in the caller's rows from the compact sums, rounded once; zero where a token is left out.
-template <class T>
-__global__ void __launch_bounds__(kCopyThreads) psops_xent_dh_out_kernel(const float *sums, long long sums_ld, const XentControl *control,
-                                                                         const int *compact_of, int tokens, int dim, bool aligned,
-                                                                         T *dh, long long ld)
+// dh in the caller's rows from the compact sums, rounded once; zero where a
+// token is left out.  DW: dw from its shares' sums (row for row).
+struct OutParams {
+    const float *sums;
+    long long sums_ld;
+    const XentControl *control;
+    const int *compact_of;
+    int rows, dim, dw_share_rows;
+    bool aligned;
+    void *out;
+    long long ld;
+};
+
+template <class T, bool DW>
+__global__ void __launch_bounds__(kCopyThreads) psops_xent_out_kernel(const OutParams P)
 {
     after_the_kernel_before();
-    const float unscale = control->error ? NAN : control->unscale;      // a product gave up: no numbers rather than wrong ones
-    const int shares = control->shares;
-    const long long share = control->share_rows * sums_ld;
+    const float unscale = P.control->error ? NAN : P.control->unscale;  // a product gave up: no numbers rather than wrong ones
+    const int shares = DW ? P.control->dw_shares : P.control->shares, dim = P.dim;
+    const long long share = (DW ? P.dw_share_rows : P.control->share_rows) * P.sums_ld;
     const unsigned groups = (dim + 3) / 4;
-    for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < (long long)tokens * groups; i += (long long)gridDim.x * kCopyThreads) {
+    for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < (long long)P.rows * groups; i += (long long)gridDim.x * kCopyThreads) {
         const int t = (int)(i / groups), d = (int)(i - (long long)t * groups) * 4;
-        const int r = compact_of[t];
-        T *out = dh + t * ld + d;
+        const int r = DW ? t : P.compact_of[t];
+        T *out = (T *)P.out + t * P.ld + d;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (r >= 0) {
-            const float *in = sums + r * sums_ld + d;
+            const float *in = P.sums + r * P.sums_ld + d;
 #pragma unroll 4
             for (int s = 0; s < shares; ++s) {
                 const float4 a = *reinterpret_cast<const float4 *>(in + s * share);
@@ -777,7 +798,7 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_dh_out_kernel(const f
             }
         }
         const uint2 u = make_uint2(pack2<T>(v.x * unscale, v.y * unscale), pack2<T>(v.z * unscale, v.w * unscale));
-        if (aligned && d + 4 <= dim) {
+        if (P.aligned && d + 4 <= dim) {
             *reinterpret_cast<uint2 *>(out) = u;
         } else {
             T e[4];

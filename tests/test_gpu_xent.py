@@ -115,6 +115,13 @@ def test_sizes(T, D, V, dtype):
     _run(T, D, V, dtype)
 
 
+@pytest.mark.parametrize("T,D,V", [(1600, 200, 700), (2500, 61, 130), (1536, 1024, 257), (9000, 72, 500)])
+def test_many_tokens_and_a_small_vocabulary(T, D, V):
+    # dw in shares of the tokens, and with most tokens left out fewer shares than there is room for
+    _run(T, D, V, torch.bfloat16, seed=61)
+    _run(T, D, V, torch.float16, seed=62, masked=0.97, reduction="sum")
+
+
 @pytest.mark.parametrize("masked", [0.3, 0.9, 1.0])
 @pytest.mark.parametrize("reduction", ["mean", "sum"])
 def test_left_out_tokens(masked, reduction):
