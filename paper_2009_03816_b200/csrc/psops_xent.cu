@@ -327,6 +327,29 @@ int forward_few(psops_xent *x, FewParams P)
     return launch(x, "psops_xent_few_kernel", kernel, grid, kSmallThreads, few_shared(P.tokens, P.dim), P);
 }
 
+template <class T, bool ALIGNED>
+void (*few_grads_kernel(int few))(const FewGradParams)
+{
+    return few == 1 ? psops_xent_few_grads_kernel<T, 1, ALIGNED> : few == 2 ? psops_xent_few_grads_kernel<T, 2, ALIGNED>
+           : psops_xent_few_grads_kernel<T, 4, ALIGNED>;
+}
+
+template <class T>
+int backward_few(psops_xent *x, FewGradParams P, bool aligned, void *dh, int64_t dh_ld)
+{
+    const int few = few_of(P.tokens), teams_of_block = kSmallWarps / P.team;
+    const int rows = few == 1 ? kFewGradRows<1> : few == 2 ? kFewGradRows<2> : kFewGradRows<4>;
+    const int blocks = few == 1 ? kFewGradBlocks<1> : few == 2 ? kFewGradBlocks<2> : kFewGradBlocks<4>;
+    // as many blocks as run at once, have rows to do and room for their parts of dh
+    const int64_t grid = std::max<int64_t>(1, std::min({(int64_t)x->sms * blocks, ceil_div(ceil_div(P.vocab, rows), teams_of_block),
+                                                        x->lay.sum_rows / (few * teams_of_block)}));
+    PSOPS_DO(launch(x, "psops_xent_few_grads_kernel", aligned ? few_grads_kernel<T, true>(few) : few_grads_kernel<T, false>(few), grid,
+                    kSmallThreads, 0, P));
+    if (dh == nullptr) return PSOPS_OK;
+    return launch(x, "psops_xent_few_dh_kernel", psops_xent_few_dh_kernel<T>, dim3((unsigned)ceil_div(P.dim, 32), (unsigned)P.tokens),
+                  kSmallThreads, 0, (const float *)P.parts, (int)grid * teams_of_block, few, P.padded, P.targets, P.vocab, P.dim, (T *)dh, dh_ld);
+}
+
 int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinParams J)
 {
     Call c;
@@ -551,6 +574,21 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
         H.dh = d_dh;
         H.dh_ld = dh_ld;
         return x->cfg.type == PSOPS_F16 ? backward_head<__half>(x, H, d_dw, dw_ld) : backward_head<__nv_bfloat16>(x, H, d_dw, dw_ld);
+    }
+    if (is_few(tokens, x->cfg.dim) && x->cfg.dim <= kFewGradDim) {
+        FewGradParams F{};
+        F.h = (const uint16_t *)d_h; F.h_ld = h_ld; F.h_aligned = aligned16(d_h, h_ld);
+        F.w = (const uint16_t *)d_w; F.w_ld = w_ld;
+        F.targets = (const long long *)d_targets;
+        F.tokens = (int)tokens; F.dim = (int)x->cfg.dim; F.vocab = (int)x->cfg.vocab; F.reduction = reduction;
+        F.team = few_team(x->cfg.dim);
+        F.lse = d_lse; F.known_rows = d_rows; F.grad = d_grad;
+        F.parts = x->at<float>(x->lay.sums);
+        F.padded = (int)x->lay.padded;
+        F.want_dh = d_dh != nullptr;
+        F.dw = (uint16_t *)d_dw; F.dw_ld = dw_ld;
+        const bool aligned = x->cfg.dim % 8 == 0 && aligned16(d_w, w_ld) && (d_dw == nullptr || aligned16(d_dw, dw_ld));
+        return x->cfg.type == PSOPS_F16 ? backward_few<__half>(x, F, aligned, d_dh, dh_ld) : backward_few<__nv_bfloat16>(x, F, aligned, d_dh, dh_ld);
     }
     IndexParams P{};
     P.targets = (const long long *)d_targets;

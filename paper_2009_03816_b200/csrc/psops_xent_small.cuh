@@ -410,4 +410,208 @@ __global__ void __launch_bounds__(kSmallThreads, kFewBlocks) psops_xent_few_kern
     }
 }
 
+// ---- gradients of few tokens ------------------------------------------------------
+// Up to 4 tokens: w is read once and dw written once, and that is all the
+// traffic.  A team of warps (one for each 512 features, up to the whole block)
+// takes a few rows of w at a time: the logits of the rows, then, with the rows still in registers, their part of dh and their rows
+// of dw.  The teams' parts of dh are added up by a kernel behind.  fp32
+// throughout, so nothing but the results is rounded to 16 bits.
+// Measured in a CUDA graph, this form / the tensor cores, 32,768 x 4,096: 1 token
+// 99 / 185 us (537 MB: 82 us), 2 tokens 122 / 182, 4 tokens 189 / 183; 32,003 x
+// 1,000: 3 tokens 59 / 68.  Rows at a time and blocks of an SM: what registers
+// allow, the best of 1, 2 and 4 rows with 1 to 4 blocks.
+constexpr int kFewGradDim = 4096;
+template <int N> constexpr int kFewGradRows = N == 2 ? 4 : 2;
+template <int N> constexpr int kFewGradBlocks = N == 1 ? 2 : 1;
+inline int few_team(int64_t dim) { return dim <= 512 ? 1 : dim <= 1024 ? 2 : dim <= 2048 ? 4 : 8; }
+
+struct FewGradParams {
+    const uint16_t *h, *w;
+    long long h_ld, w_ld;
+    bool h_aligned;
+    const long long *targets;
+    int tokens, dim, vocab, reduction, team;
+    const float *lse, *known_rows, *grad;
+    float *parts;                                // team x token x padded features
+    int padded;
+    bool want_dh;
+    uint16_t *dw;                                // or NULL
+    long long dw_ld;
+};
+
+__device__ __forceinline__ bool few_counts(const FewGradParams &P, int t)
+{
+    return t < P.tokens && P.targets[t] >= 0 && P.targets[t] < P.vocab;
+}
+__device__ __forceinline__ void team_sync(int team, int team_index)
+{
+    if (team == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(team_index + 1), "r"(team * 32) : "memory");
+}
+
+template <class T, int N, bool ALIGNED>
+__global__ void __launch_bounds__(kSmallThreads, kFewGradBlocks<N>) psops_xent_few_grads_kernel(const FewGradParams P)
+{
+    constexpr int R = kFewGradRows<N>;
+    __shared__ float sums[2][kSmallWarps][R * N];
+    after_the_kernel_before();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int team_index = warp / P.team, in_team = warp - team_index * P.team;
+    const int teams = gridDim.x * (kSmallWarps / P.team), me = blockIdx.x * (kSmallWarps / P.team) + team_index;
+    const int group[2] = {(in_team * 2) * 32 + lane, (in_team * 2 + 1) * 32 + lane};     // this lane's groups of eight features
+    const bool there[2] = {group[0] * 8 < P.dim, group[1] * 8 < P.dim};
+
+    uint4 hidden[N][2];
+    float dh[N][16];
+    int n = 0;
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        const bool counts = few_counts(P, t);
+        n += counts ? 1 : 0;
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            hidden[t][q] = counts && there[q] ? eight_of_row(P.h + t * P.h_ld, group[q], P.dim, P.h_aligned) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dh[t][e] = 0.0f;
+    }
+    // lane (r * N + t) turns the logit of row r and token t into its gradient
+    const int mt = lane % N, mr = lane / N;
+    const bool mine = lane < R * N && few_counts(P, mt);
+    const float lse = mine ? P.lse[mt] : 0.0f;
+    const float at_label = mine && P.known_rows != nullptr ? expm1f(-P.known_rows[mt]) : 2.0f;
+    const long long label = mine ? P.targets[mt] : -1;
+    const float g = !mine ? 0.0f : P.reduction == PSOPS_PER_TOKEN ? P.grad[mt] : P.reduction == PSOPS_MEAN ? __fdiv_rn(P.grad[0], (float)max(1, n)) : P.grad[0];
+
+    auto fetch = [&](long long v0, uint4 (&u)[R][2]) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                u[r][q] = make_uint4(0, 0, 0, 0);
+                if (v0 + r < P.vocab && there[q]) {
+                    const uint16_t *row = P.w + (v0 + r) * P.w_ld;
+                    u[r][q] = ALIGNED ? load_once(row + group[q] * 8) : eight_of_row(row, group[q], P.dim, false);
+                }
+            }
+    };
+    auto sixteen = [](const uint4 (&u)[2], float (&x)[16]) {
+        float a[8], b[8];
+        eight_numbers<T>(u[0], a);
+        eight_numbers<T>(u[1], b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            x[j] = a[j];
+            x[8 + j] = b[j];
+        }
+    };
+    uint4 now[R][2], next[R][2];
+    long long v0 = (long long)me * R;
+    fetch(v0, next);
+    for (int turn = 0; v0 < P.vocab; v0 += (long long)teams * R, turn ^= 1) {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) now[r][q] = next[r][q];
+        fetch(v0 + (long long)teams * R, next);
+        // logits: this lane's features, the warp's, the team's
+        float logit = 0.0f;                      // of row mr and token mt
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float x[16];
+            sixteen(now[r], x);
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                float k[16], s = 0.0f;
+                sixteen(hidden[t], k);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s = fmaf(x[e], k[e], s);
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+                if (lane == r * N + t) logit = s;
+            }
+        }
+        if (P.team > 1) {
+            if (lane < R * N) sums[turn][warp][lane] = logit;
+            team_sync(P.team, team_index);
+            if (lane < R * N) {
+                logit = 0.0f;
+                for (int k = 0; k < P.team; ++k) logit += sums[turn][team_index * P.team + k][lane];
+            }
+        }
+        float d = 0.0f;
+        if (mine && v0 + mr < P.vocab) {
+            if (v0 + mr != label) d = expf(logit - lse) * g;
+            else d = (at_label > 1.0f ? expm1f(logit - lse) : at_label) * g;
+        }
+        // dh and dw of these rows
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float row[16], x[16];
+            sixteen(now[r], x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) row[e] = 0.0f;
+#pragma unroll
+            for (int t = 0; t < N; ++t) {
+                const float dt = __shfl_sync(0xffffffffu, d, r * N + t);
+                float k[16];
+                sixteen(hidden[t], k);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    row[e] = fmaf(dt, k[e], row[e]);
+                    dh[t][e] = fmaf(dt, x[e], dh[t][e]);
+                }
+            }
+            if (P.dw != nullptr && v0 + r < P.vocab) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q)
+                    if (there[q]) {
+                        uint16_t *to = P.dw + (v0 + r) * P.dw_ld + group[q] * 8;
+                        const uint4 u = make_uint4(pack2<T>(row[q * 8], row[q * 8 + 1]), pack2<T>(row[q * 8 + 2], row[q * 8 + 3]),
+                                                   pack2<T>(row[q * 8 + 4], row[q * 8 + 5]), pack2<T>(row[q * 8 + 6], row[q * 8 + 7]));
+                        if (ALIGNED) {
+                            *reinterpret_cast<uint4 *>(to) = u;
+                        } else {
+                            uint16_t e[8];
+                            memcpy(e, &u, 16);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (group[q] * 8 + j < P.dim) to[j] = e[j];
+                        }
+                    }
+            }
+        }
+    }
+    if (!P.want_dh) return;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            if (there[q]) {
+                float4 *to = reinterpret_cast<float4 *>(P.parts + ((long long)me * N + t) * P.padded + group[q] * 8);
+                to[0] = make_float4(dh[t][q * 8], dh[t][q * 8 + 1], dh[t][q * 8 + 2], dh[t][q * 8 + 3]);
+                to[1] = make_float4(dh[t][q * 8 + 4], dh[t][q * 8 + 5], dh[t][q * 8 + 6], dh[t][q * 8 + 7]);
+            }
+}
+
+// dh from the teams' parts: a block has 32 features of a token, its warps share the teams.
+template <class T>
+__global__ void __launch_bounds__(kSmallThreads) psops_xent_few_dh_kernel(const float *parts, int teams, int few, int padded,
+                                                                          const long long *targets, int vocab, int dim, T *dh, long long ld)
+{
+    __shared__ float sums[kSmallWarps][33];
+    after_the_kernel_before();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = blockIdx.y, d = blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (d < dim)
+#pragma unroll 8
+        for (int k = warp; k < teams; k += kSmallWarps) s += parts[((long long)k * few + t) * padded + d];
+    sums[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && d < dim) {
+        for (int k = 1; k < kSmallWarps; ++k) s += sums[k][lane];
+        const long long y = targets[t];
+        dh[t * ld + d] = narrow16<T>(y >= 0 && y < vocab ? s : 0.0f);
+    }
+}
+
 } // namespace

@@ -139,7 +139,8 @@ def test_few_classes(T, D, V, dtype):
     _run(T, D, V, dtype, seed=22, reduction="sum")
 
 
-FEW = [(1, 4096, 3000), (2, 1000, 70_001), (3, 61, 5000), (4, 256, 100), (7, 3000, 777), (8, 2056, 4096), (9, 64, 500)]
+FEW = [(1, 4096, 3000), (2, 1000, 70_001), (3, 61, 5000), (4, 256, 100), (4, 2048, 1001), (1, 600, 66), (2, 4100, 300),
+       (1, 30_000, 70), (7, 3000, 777), (8, 2056, 4096), (9, 64, 500)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
@@ -149,10 +150,10 @@ def test_few_tokens(T, D, V, dtype):
     _run(T, D, V, dtype, seed=24, masked=0.5, reduction="sum")
 
 
-@pytest.mark.parametrize("T,D,V", [(50, 30, 20), (6, 200, 900)])
+@pytest.mark.parametrize("T,D,V", [(50, 30, 20), (6, 200, 900), (4, 200, 900), (3, 1500, 333), (2, 3001, 100)])
 def test_small_forms_leave_out_and_weigh_like_the_others(T, D, V):
     h, w, y = _inputs(T, D, V, torch.bfloat16, 31, masked=0.4)
-    y[0] = V - 1
+    y[0], y[1] = V - 1, -7
     op = training.LinearXent(T, D, V)
     bad = h.clone()
     bad[y < 0] = float("nan")
