@@ -1,10 +1,10 @@
 // psops_xent_small.cuh -- the linear cross entropy where tensor-core tiles do
 // not pay: few classes (a classifier's head), and few tokens.
 //
-// Both kernels do a whole forward pass in one launch; tokens that are left out
-// are simply passed over, so nothing is listed or gathered first.  Products and
-// sums are fp32, and the gradients of few classes are rounded to 16 bits only at
-// the end.
+// Each form does a whole forward pass in one launch and the gradients in two;
+// tokens that are left out are simply passed over, so nothing is listed or
+// gathered first.  Products and sums are fp32, and gradients are rounded to 16
+// bits only at the end.
 #pragma once
 
 #include "psops_xent_kernels.cuh"
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kHeadDwThreads) psops_xent_head_dw_kernel(cons
 // hidden states lie in shared memory as fp32; every warp has an equal share of
 // w's rows and takes four at a time; lane t keeps the softmax of token t.
 // Measured with 268 MB of w (32,768 x 4,096): 1 / 2 / 4 tokens 47 / 51 / 59 us
-// (5.7 TB/s down to 4.6) where the tensor-core form takes 68 us whatever their
+// (5.7 TB/s down to 4.6) where the tensor-core form takes 62 us whatever their
 // number; 8 tokens took 91 us, so from 5 on the tensor cores do it.
 constexpr int kFewTokens = 4, kFewRows = 4, kFewBlocks = 2;          // blocks of an SM
 // Pieces of a row (512 bytes) on their way under the arithmetic: four where the registers are there.
