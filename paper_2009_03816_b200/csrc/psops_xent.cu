@@ -88,7 +88,7 @@ Layout make_layout(const psops_xent_config *c)
         L.sums = take(4 * (size_t)L.sum_rows * (size_t)L.padded);
         // a small vocabulary gives dw few tiles: then its sum over the tokens is split
         const int64_t tiles = whole / kTile * ceil_div(L.padded, kTile);
-        L.dw_most = std::max<int64_t>(1, std::min<int64_t>(kMostShares, kPairs / tiles));
+        L.dw_most = c->max_tokens < kSplitTokens ? 1 : std::max<int64_t>(1, std::min<int64_t>(kMostShares, kPairs / tiles));
         if (L.dw_most > 1) L.dw_sums = take(4 * (size_t)(whole * L.dw_most) * (size_t)L.padded);
     }
     L.total = at;
@@ -432,7 +432,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             P.add = first > 0;
             PSOPS_DO(product(x, kDh, tokens, c.tiles_m * tiles_d * kMostShares, dlogits_along, weights, sums, P));
         }
-        if (dw != nullptr && x->lay.dw_most > 1 && tokens >= kSplitTokens) {      // one piece, then
+        if (dw != nullptr && x->lay.dw_most > 1 && tokens >= kSplitTokens) {
             CUtensorMap dw_sums;
             const int64_t share_rows = (int64_t)round_up((size_t)count, kTile);
             PSOPS_DO(make_map(x, &dw_sums, PSOPS_F32, x->at<void>(x->lay.dw_sums), c.padded, share_rows * x->lay.dw_most, c.padded, 32));
@@ -440,7 +440,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             P.result_rows = (int)count;
             P.dw_share_rows = (int)share_rows;
             PSOPS_DO(product(x, kDwSums, tokens, ceil_div(count, kTile) * tiles_d * x->lay.dw_most, dlogits_across, hidden_across, dw_sums, P));
-            PSOPS_DO(results<true>(x, x->at<float>(x->lay.dw_sums), (int)share_rows, (int)count, dw, dw_ld));
+            PSOPS_DO(results<true>(x, x->at<float>(x->lay.dw_sums), (int)share_rows, (int)count, (uint16_t *)dw + first * dw_ld, dw_ld));
         } else if (dw != nullptr) {
             uint16_t *to = direct ? (uint16_t *)dw + first * dw_ld : x->at<uint16_t>(x->lay.dw);
             CUtensorMap dw_out;

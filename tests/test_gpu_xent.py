@@ -193,6 +193,20 @@ def test_several_pieces_of_the_vocabulary():
     op.close()
 
 
+@pytest.mark.parametrize("D", [64, 61])
+def test_a_small_vocabulary_in_several_pieces(D):
+    # 200,192 rows of workspace make a piece 2,048 entries; dw is summed in shares, piece by piece
+    T, V = 2000, 2300
+    h, w, y = _inputs(T, D, V, torch.bfloat16, 71, masked=0.1)
+    x = _exact(h, w, y, torch.ones(T, device="cuda"))
+    op = training.LinearXent(200_000, D, V)
+    loss, rows, lse = op.forward(h, w, y, "sum")
+    dh, dw = op.backward(h, w, y, lse, torch.ones(1, device="cuda"), "sum")
+    _check_forward(x, loss, rows, lse, "sum")
+    _check_grads(x, dh, dw, torch.bfloat16)
+    op.close()
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_per_token_gradients(dtype):
     T, D, V = 150, 96, 777
