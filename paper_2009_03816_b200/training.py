@@ -22,8 +22,8 @@ import math
 import torch
 
 from . import binding
-from .binding import (PSOPS_BF16, PSOPS_EINVAL, PSOPS_F16, PSOPS_F32, PSOPS_MEAN, PSOPS_NONE, PSOPS_PER_TOKEN,
-                      PSOPS_SUM, PSOPS_XENT_GRADS, PSOPS_XENT_STAGED, PsopsError)
+from .binding import (PSOPS_BF16, PSOPS_EINVAL, PSOPS_ESTATE, PSOPS_F16, PSOPS_F32, PSOPS_MEAN, PSOPS_NONE,
+                      PSOPS_PER_TOKEN, PSOPS_SUM, PSOPS_XENT_GRADS, PSOPS_XENT_STAGED, PsopsError)
 
 _TYPES = {torch.float32: PSOPS_F32, torch.float16: PSOPS_F16, torch.bfloat16: PSOPS_BF16}
 _REDUCTIONS = {"mean": PSOPS_MEAN, "sum": PSOPS_SUM, "none": PSOPS_PER_TOKEN}
@@ -76,8 +76,19 @@ class _Holder:
         if self._follows:
             now = torch._C._cuda_getCurrentRawStream(self.device.index)
             if now != self.stream:
-                self._set_stream(self.ctx, now)
+                self._move(now)
                 self.stream = now
+
+    def _move(self, stream):
+        self._set_stream(self.ctx, stream)
+
+    def _capturing(self):
+        """Whether the stream of the next call is being captured."""
+        if not self._follows:
+            with torch.cuda.stream(torch.cuda.ExternalStream(self.stream, self.device)):
+                return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.device(self.device):
+            return torch.cuda.is_current_stream_capturing()
 
     @property
     def launches(self) -> int:
@@ -110,6 +121,10 @@ class LinearXent(_Holder):
 
     h may have any leading dimensions, with rows of `dim` consecutive elements; `targets`
     (int64) has those leading dimensions.  A label outside [0, vocab) leaves its token out.
+    A w or dw whose rows are not 16-byte aligned although dim is a multiple of 8 passes through
+    a second context with a larger workspace.  It is made when such rows are first met, which
+    cannot be inside a stream capture, and the first context stays as it is: CUDA graphs that
+    were captured through this object keep their workspace as long as the object lives.
     Calling the object gives the loss as a torch value with gradients::
 
         loss = xent(h, w, targets)            # reduction="mean", "sum" or "none"
@@ -119,6 +134,8 @@ class LinearXent(_Holder):
     _set_stream = staticmethod(binding.psops_xent_set_stream)
     _launch_count = staticmethod(binding.psops_xent_launch_count)
     _destroy = staticmethod(binding.psops_xent_destroy)
+    _launched = 0                   # by contexts that are closed
+    _staged = None                  # the second context
 
     def __init__(self, tokens, dim, vocab, *, dtype=torch.bfloat16, device="cuda", gradients=True, stream=None):
         device = torch.device(device)
@@ -129,18 +146,15 @@ class LinearXent(_Holder):
         self.device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
         self.tokens, self.dim, self.vocab, self.dtype = int(tokens), int(dim), int(vocab), dtype
         self._w_shape = torch.Size((self.vocab, self.dim)) if min(self.vocab, self.dim) >= 0 else None
-        self._launched = 0
         self._flags = PSOPS_XENT_GRADS if gradients else 0
         self._on(self.device, stream)
-        self._open()
+        self._workspace, self.ctx = self._open(self._flags)
 
-    def _open(self):
-        cfg = binding.psops_xent_config(self.tokens, self.dim, self.vocab, _TYPES[self.dtype], self._flags)
-        nbytes = binding.psops_xent_workspace_bytes(cfg)
+    def _open(self, flags):
+        cfg = binding.psops_xent_config(self.tokens, self.dim, self.vocab, _TYPES[self.dtype], flags)
         with torch.cuda.device(self.device):
-            self.close()
-            self._workspace = _workspace(nbytes, self.device, "LinearXent")
-            self.ctx = binding.psops_xent_create(cfg, self._workspace, None, self.stream)
+            workspace = _workspace(binding.psops_xent_workspace_bytes(cfg), self.device, "LinearXent")
+            return workspace, binding.psops_xent_create(cfg, workspace, None, self.stream)
 
     def _rows(self, where, name, t):
         """Stride of a matrix that has consecutive elements in each row, its leading dimensions seen as one."""
@@ -176,15 +190,26 @@ class LinearXent(_Holder):
         tokens = targets.numel()
         if tokens > self.tokens:
             _refuse(where, f"{tokens} tokens, made for {self.tokens}")
-        self._follow()
-        self._stage_if_needed(w, w_ld)
         return tokens, h_ld, w_ld
 
-    def _stage_if_needed(self, t, ld):
-        """Rows that are not 16-byte aligned pass through a larger workspace, made when first met."""
-        if (t.data_ptr() % 16 or ld % 8) and self.dim % 8 == 0 and not self._flags & PSOPS_XENT_STAGED:
-            self._flags |= PSOPS_XENT_STAGED
-            self._open()
+    def _context(self, where, w, w_ld, dw=None, dw_ld=0):
+        """The context for these rows, on the stream that it works on."""
+        if self.dim % 8 == 0 and self.ctx is not None and (
+                w.data_ptr() % 16 or w_ld % 8 or dw is not None and (dw.data_ptr() % 16 or dw_ld % 8)):
+            if self._staged is None and self._capturing():
+                raise PsopsError(PSOPS_ESTATE, where, "rows that are not 16-byte aligned, met for the first time inside a "
+                                                      "stream capture: make one such call before it")
+            self._follow()
+            if self._staged is None:
+                self._staged_workspace, self._staged = self._open(self._flags | PSOPS_XENT_STAGED)
+            return self._staged
+        self._follow()
+        return self.ctx
+
+    def _move(self, stream):
+        super()._move(stream)
+        if self._staged is not None:
+            self._set_stream(self._staged, stream)
 
     def forward(self, h, w, targets, reduction="mean", *, loss=None):
         """(loss, rows, lse): the loss of all tokens ("mean" or "sum"), and each token's loss and log-sum-exp.
@@ -198,7 +223,8 @@ class LinearXent(_Holder):
             self._numbers("LinearXent.forward", "loss", loss, None)
         rows = torch.empty(targets.shape, dtype=torch.float32, device=self.device)
         lse = torch.empty_like(rows)
-        binding.psops_xent_forward(self.ctx, h, h_ld, w, w_ld, targets, tokens, _REDUCTIONS[reduction], loss, rows, lse)
+        ctx = self._context("LinearXent.forward", w, w_ld)
+        binding.psops_xent_forward(ctx, h, h_ld, w, w_ld, targets, tokens, _REDUCTIONS[reduction], loss, rows, lse)
         return loss, rows, lse
 
     def backward(self, h, w, targets, lse, grad, reduction="mean", *, rows=None, dh=None, dw=None, want=(True, True)):
@@ -216,10 +242,8 @@ class LinearXent(_Holder):
         self._numbers(where, "grad", grad, targets.shape if code == PSOPS_PER_TOKEN else None)
         dh, dh_ld = self._gradient(where, "dh", dh, h) if want[0] else (None, 0)
         dw, dw_ld = self._gradient(where, "dw", dw, w) if want[1] else (None, 0)
-        if dw is not None:
-            self._stage_if_needed(dw, dw_ld)
-        binding.psops_xent_backward(self.ctx, h, h_ld, w, w_ld, targets, tokens, lse, rows, grad, code, dh, dh_ld, dw,
-                                    dw_ld)
+        ctx = self._context(where, w, w_ld, dw, dw_ld)
+        binding.psops_xent_backward(ctx, h, h_ld, w, w_ld, targets, tokens, lse, rows, grad, code, dh, dh_ld, dw, dw_ld)
         return dh, dw
 
     def _numbers(self, where, name, t, shape):
@@ -250,11 +274,16 @@ class LinearXent(_Holder):
 
     @property
     def launches(self) -> int:
-        return self._launched + super().launches
+        return self._launched + super().launches + (self._launch_count(self._staged) if self._staged is not None else 0)
 
     def close(self):
-        self._launched += super().launches
-        super().close()
+        self._launched = self.launches
+        try:
+            if self._staged is not None:
+                self._destroy(self._staged)
+                self._staged = None
+        finally:
+            super().close()
 
 
 class _LinearXentFunction(torch.autograd.Function):
