@@ -372,7 +372,8 @@ int psops_destroy(psops_ctx *ctx);
  * its GPU: what it enqueues there comes after what it has enqueued so far (but
  * into a capturing stream no such wait can be recorded: order the streams
  * before the capture).  Arrays written on yet other streams are the caller's to
- * order, as for any kernel.
+ * order, as for any kernel.  psops_*_destroy frees the context also where it
+ * returns an error.
  * ---------------------------------------------------------------------------
  */
 

@@ -571,9 +571,9 @@ class Swarm:
         return psops_launch_count(self.ctx)
 
     def close(self):
-        if self.ctx is not None:
-            psops_destroy(self.ctx)
-            self.ctx = None
+        ctx, self.ctx = self.ctx, None             # it is freed even where the entry reports an error
+        if ctx is not None:
+            psops_destroy(ctx)
 
     def __del__(self):  # pragma: no cover
         try:

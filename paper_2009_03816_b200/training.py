@@ -95,9 +95,9 @@ class _Holder:
         return self._launch_count(self.ctx) if self.ctx is not None else 0
 
     def close(self):
-        if self.ctx is not None:
-            self._destroy(self.ctx)
-            self.ctx = None
+        ctx, self.ctx = self.ctx, None             # it is freed even where the entry reports an error
+        if ctx is not None:
+            self._destroy(ctx)
 
     def __del__(self):  # pragma: no cover
         try:
@@ -278,10 +278,10 @@ class LinearXent(_Holder):
 
     def close(self):
         self._launched = self.launches
+        staged, self._staged = self._staged, None
         try:
-            if self._staged is not None:
-                self._destroy(self._staged)
-                self._staged = None
+            if staged is not None:
+                self._destroy(staged)
         finally:
             super().close()
 

@@ -71,3 +71,62 @@ def test_rows_that_are_not_aligned_get_a_context_beside_the_first(monkeypatch):
     assert op.launches == 30
     op.close()
     assert len(entries.calls) == 3
+
+
+def _holder(cls, destroy):
+    holder = cls.__new__(cls)
+    holder.ctx = object()
+    holder._destroy = destroy
+    holder._launch_count = lambda ctx: 3
+    return holder
+
+
+@pytest.mark.parametrize("cls", [training.LinearXent, training.AdamW, training.GradNorm])
+def test_a_context_is_destroyed_once_whatever_the_entry_answers(cls):
+    seen = []
+
+    def destroy(ctx):
+        seen.append(ctx)
+        raise binding.PsopsError(binding.PSOPS_ECUDA, "destroy", "the stream could not be waited for")
+
+    holder = _holder(cls, destroy)
+    ctx = holder.ctx
+    with pytest.raises(binding.PsopsError):
+        holder.close()
+    assert holder.ctx is None and seen == [ctx]       # the library has freed it: the handle is gone
+    holder.close()
+    holder.__del__()
+    assert seen == [ctx]
+
+
+def test_both_contexts_are_destroyed_once_whatever_the_entry_answers():
+    seen = []
+
+    def destroy(ctx):
+        seen.append(ctx)
+        raise binding.PsopsError(binding.PSOPS_ECUDA, "destroy")
+
+    op = _holder(training.LinearXent, destroy)
+    op.ctx, op._staged = 1, 2
+    with pytest.raises(binding.PsopsError):
+        op.close()
+    assert sorted(seen) == [1, 2] and op.ctx is None and op._staged is None
+    op.close()
+    assert len(seen) == 2
+
+
+def test_a_swarm_is_destroyed_once_whatever_the_entry_answers(monkeypatch):
+    seen = []
+
+    def destroy(ctx):
+        seen.append(ctx)
+        raise binding.PsopsError(binding.PSOPS_ECUDA, "psops_destroy")
+
+    monkeypatch.setattr(binding, "psops_destroy", destroy)
+    swarm = binding.Swarm.__new__(binding.Swarm)
+    swarm.ctx = 17
+    with pytest.raises(binding.PsopsError):
+        swarm.close()
+    assert swarm.ctx is None
+    swarm.close()
+    assert seen == [17]
