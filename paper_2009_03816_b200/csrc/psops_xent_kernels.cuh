@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
             up = ldexpf(P.headroom, -e);
             undo = 1.0f / up;
         }
+        if (total == 0) undo = 0.0f;                 // no token, no gradient, even if the upstream one is not finite
         if (writes && threadIdx.x == 0) P.control->unscale = undo;
     }
 #pragma unroll 2
@@ -780,7 +781,8 @@ template <class T, bool DW>
 __global__ void __launch_bounds__(kCopyThreads) psops_xent_out_kernel(const OutParams P)
 {
     after_the_kernel_before();
-    const float unscale = P.control->error ? NAN : P.control->unscale;  // a product gave up: no numbers rather than wrong ones
+    const bool error = P.control->error != 0;                           // a product gave up: no numbers rather than wrong ones
+    const float counts = error ? NAN : P.control->unscale, left_out = error ? NAN : 0.0f;      // an unscale that is not finite stays with the tokens that count
     const int shares = DW ? P.control->dw_shares : P.control->shares, dim = P.dim;
     const long long share = (DW ? P.dw_share_rows : P.control->share_rows) * P.sums_ld;
     const unsigned groups = (dim + 3) / 4;
@@ -789,6 +791,7 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_out_kernel(const OutP
         const int r = DW ? t : P.compact_of[t];
         T *out = (T *)P.out + t * P.ld + d;
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const float unscale = r >= 0 ? counts : left_out;
         if (r >= 0) {
             const float *in = P.sums + r * P.sums_ld + d;
 #pragma unroll 4

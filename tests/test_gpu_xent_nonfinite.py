@@ -1,0 +1,57 @@
+"""Linear cross entropy where something is not finite: upstream gradients that
+overflowed, and a context whose tensor-core products gave up."""
+import pytest
+import torch
+
+from paper_2009_03816_b200 import training
+
+import gpu_util
+
+pytestmark = pytest.mark.gpu
+
+# pairs of CTAs, single CTAs, dw in shares, rows of w through the workspace, few tokens, few classes
+FORMS = [(300, 64, 500), (100, 64, 300), (1600, 200, 700), (140, 61, 400), (4, 64, 300), (50, 32, 20)]
+
+
+def _inputs(T, D, V, dtype, seed=1):
+    gpu_util.ensure_library()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    h = torch.empty(T, D, device="cuda").normal_(generator=g).to(dtype)
+    w = (torch.empty(V, D, device="cuda").normal_(generator=g) * D ** -0.5).to(dtype)
+    y = torch.randint(0, V, (T,), device="cuda", generator=g)
+    return h, w, y
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,D,V", FORMS)
+def test_left_out_tokens_get_no_gradient_from_an_upstream_gradient_that_is_not_finite(T, D, V, dtype):
+    h, w, y = _inputs(T, D, V, dtype)
+    out = torch.arange(T, device="cuda") % 3 == 1
+    y[out] = -100
+    op = training.LinearXent(T, D, V, dtype=dtype)
+    _, rows, lse = op.forward(h, w, y)
+    for bad in (float("inf"), -float("inf"), float("nan")):
+        grad = torch.tensor(bad, device="cuda")
+        for reduction in ("mean", "sum"):
+            dh, dw = op.backward(h, w, y, lse, grad, reduction, rows=rows)
+            assert bool((dh[out] == 0).all()), (bad, reduction)
+            # the overflow itself stays to be seen by whoever looks at the gradients
+            assert not bool(dh[~out].isfinite().all()) and not bool(dw.isfinite().all())
+    op.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,D,V", FORMS)
+def test_no_token_left_and_an_upstream_gradient_that_is_not_finite(T, D, V, dtype):
+    h, w, y = _inputs(T, D, V, dtype)
+    y.fill_(-100)
+    op = training.LinearXent(T, D, V, dtype=dtype)
+    loss, rows, lse = op.forward(h, w, y)
+    assert float(loss) == 0.0
+    for bad in (float("inf"), float("nan")):
+        for reduction in ("mean", "sum"):
+            dh, dw = op.backward(h, w, y, lse, torch.tensor(bad, device="cuda"), reduction)
+            assert bool((dh == 0).all()) and bool((dw == 0).all()), (bad, reduction)
+        dh, dw = op.backward(h, w, y, lse, torch.full((T,), bad, device="cuda"), "none")
+        assert bool((dh == 0).all()) and bool((dw == 0).all()), bad
+    op.close()
