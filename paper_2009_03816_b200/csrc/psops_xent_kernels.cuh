@@ -134,7 +134,10 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
         const long long y = P.targets[t];
         if (y >= 0 && y < P.vocab) {
             ++mine;
-            if (P.grad != nullptr && P.reduction == PSOPS_PER_TOKEN) top = fmaxf(top, fabsf(P.grad[t]));
+            if (P.grad != nullptr && P.reduction == PSOPS_PER_TOKEN) {
+                const float g = fabsf(P.grad[t]);
+                if (g < INFINITY) top = fmaxf(top, g);       // one that overflowed must not scale the others out of range
+            }
         }
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
@@ -156,7 +159,7 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
     // What the 16-bit logits' gradients are multiplied with, and what undoes it in
     // the fp32 sums.  One gradient for all tokens stays out of the 16 bits (its own
     // rounding would be the same for every token and add up); gradients per token
-    // are scaled by a power of two that brings the largest to (1/2, 1] * headroom.
+    // are scaled by a power of two that brings the largest finite one to (1/2, 1] * headroom.
     float up = P.headroom;
     if (P.grad != nullptr) {
         float undo;
@@ -164,7 +167,7 @@ __global__ void __launch_bounds__(kIndexThreads) psops_xent_index_kernel(const I
             undo = (P.reduction == PSOPS_MEAN ? __fdiv_rn(P.grad[0], (float)max(1, total)) : P.grad[0]) / P.headroom;
         } else {
             int e = 0;
-            if (top > 0.0f && top < INFINITY) e = min(120, max(-100, ilogbf(top) + 1));
+            if (top > 0.0f) e = min(120, max(-100, ilogbf(top) + 1));
             up = ldexpf(P.headroom, -e);
             undo = 1.0f / up;
         }

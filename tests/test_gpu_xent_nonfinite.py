@@ -55,3 +55,20 @@ def test_no_token_left_and_an_upstream_gradient_that_is_not_finite(T, D, V, dtyp
         dh, dw = op.backward(h, w, y, lse, torch.full((T,), bad, device="cuda"), "none")
         assert bool((dh == 0).all()) and bool((dw == 0).all()), bad
     op.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,D,V", FORMS)
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_one_tokens_overflowed_gradient_stays_with_that_token(T, D, V, dtype, bad):
+    h, w, y = _inputs(T, D, V, dtype)
+    op = training.LinearXent(T, D, V, dtype=dtype)
+    _, rows, lse = op.forward(h, w, y)
+    grad = torch.full((T,), 7.5, device="cuda")
+    want, _ = op.backward(h, w, y, lse, grad, "none", rows=rows)
+    grad[2] = bad
+    got, dw = op.backward(h, w, y, lse, grad, "none", rows=rows)
+    others = torch.arange(T, device="cuda") != 2
+    assert bool(want.isfinite().all()) and torch.equal(got[others], want[others])
+    assert not bool(got[2].isfinite().all()) and not bool(dw.isfinite().all())
+    op.close()
