@@ -521,8 +521,9 @@ int psops_gradnorm_destroy(psops_gradnorm *gn);
  * dim).  dim a multiple of 8 with 16-byte aligned rows of w is read in place;
  * any other w, and any other dw, passes through the workspace
  * (PSOPS_XENT_STAGED).
- * Should a kernel ever wait in vain for its operands (four seconds), the loss,
- * rows, lse and dh of that call and of every later one of the context are NaN.
+ * Should a product on the tensor cores ever wait in vain for its operands (four
+ * seconds), the loss, the rows and lse of the tokens that count, dh and dw of
+ * that call, and of every later call of the context that runs there, are NaN.
  */
 #define PSOPS_MEAN       0
 #define PSOPS_SUM        1

@@ -380,11 +380,14 @@ int forward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, JoinPara
     return launch(x, "psops_xent_join_kernel", psops_xent_join_kernel, ceil_div(tokens, kJoinRows), kJoinRows * kJoinParts, 0, J);
 }
 
-// dh, or dw from its shares, from fp32 sums.
+// dh (and a look at dw), or dw from its shares, from fp32 sums.
 template <bool DW>
-int results(psops_xent *x, const float *sums, int dw_share_rows, int rows, void *out, int64_t ld)
+int results(psops_xent *x, const float *sums, int dw_share_rows, int rows, void *out, int64_t ld, void *dw = nullptr, int64_t dw_ld = 0)
 {
     OutParams P{};
+    P.dw = dw;
+    P.dw_ld = dw_ld;
+    P.dw_rows = x->cfg.vocab;
     P.sums = sums;
     P.sums_ld = x->lay.padded;
     P.control = x->control();
@@ -455,8 +458,8 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             }
         }
     }
-    if (dh == nullptr || tokens == 0) return PSOPS_OK;
-    return results<false>(x, x->at<float>(x->lay.sums), 0, (int)tokens, dh, dh_ld);
+    if ((dh == nullptr || tokens == 0) && dw == nullptr) return PSOPS_OK;
+    return results<false>(x, x->at<float>(x->lay.sums), 0, dh != nullptr ? (int)tokens : 0, dh, dh_ld, dw, dw_ld);
 }
 
 } // namespace

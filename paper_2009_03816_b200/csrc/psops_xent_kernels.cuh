@@ -764,11 +764,13 @@ __global__ void __launch_bounds__(kJoinRows * kJoinParts) psops_xent_join_kernel
     for (unsigned b = lane; b < gridDim.x; b += 32) total += __ldcg(P.partials + b);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xffffffffu, total, off);
-    if (lane == 0) *P.loss = P.reduction == PSOPS_MEAN ? (float)(total / (double)max(1, rows)) : (float)total;
+    if (lane == 0) *P.loss = P.control->error ? NAN : P.reduction == PSOPS_MEAN ? (float)(total / (double)max(1, rows)) : (float)total;
 }
 
 // dh in the caller's rows from the compact sums, rounded once; zero where a
-// token is left out.  DW: dw from its shares' sums (row for row).
+// token is left out.  DW: dw from its shares' sums (row for row).  The launch for
+// dh is a call's last one and runs for dw alone too (with no rows then): where a
+// product gave up it leaves no numbers in either rather than wrong ones.
 struct OutParams {
     const float *sums;
     long long sums_ld;
@@ -778,13 +780,15 @@ struct OutParams {
     bool aligned;
     void *out;
     long long ld;
+    void *dw;                                    // dh's launch: dw, or NULL
+    long long dw_ld, dw_rows;
 };
 
 template <class T, bool DW>
 __global__ void __launch_bounds__(kCopyThreads) psops_xent_out_kernel(const OutParams P)
 {
     after_the_kernel_before();
-    const bool error = P.control->error != 0;                           // a product gave up: no numbers rather than wrong ones
+    const bool error = P.control->error != 0;
     const float counts = error ? NAN : P.control->unscale, left_out = error ? NAN : 0.0f;      // an unscale that is not finite stays with the tokens that count
     const int shares = DW ? P.control->dw_shares : P.control->shares, dim = P.dim;
     const long long share = (DW ? P.dw_share_rows : P.control->share_rows) * P.sums_ld;
@@ -813,6 +817,12 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_out_kernel(const OutP
             for (int j = 0; j < 4; ++j)
                 if (d + j < dim) out[j] = e[j];
         }
+    }
+    if (DW || !error || P.dw == nullptr) return;
+    const uint16_t nothing = (uint16_t)pack2<T>(NAN, NAN);
+    for (long long i = (long long)blockIdx.x * kCopyThreads + threadIdx.x; i < P.dw_rows * dim; i += (long long)gridDim.x * kCopyThreads) {
+        const long long v = i / dim;
+        ((uint16_t *)P.dw)[v * P.dw_ld + (i - v * dim)] = nothing;
     }
 }
 

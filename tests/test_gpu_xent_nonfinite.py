@@ -72,3 +72,41 @@ def test_one_tokens_overflowed_gradient_stays_with_that_token(T, D, V, dtype, ba
     assert bool(want.isfinite().all()) and torch.equal(got[others], want[others])
     assert not bool(got[2].isfinite().all()) and not bool(dw.isfinite().all())
     op.close()
+
+
+def _give_up(workspace):
+    """Sets the error word that a product sets which waited in vain (the fourth of the control block)."""
+    workspace.view(torch.int32)[3] = 1
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,D,V", FORMS[:4] + [(700, 64, 9000)])
+def test_a_context_that_gave_up_leaves_no_numbers(T, D, V, dtype):
+    h, w, y = _inputs(T, D, V, dtype)
+    y[1] = -100
+    one = torch.tensor(1.0, device="cuda")
+    op = training.LinearXent(32_768 if V == 9000 else T, D, V, dtype=dtype)          # 9,000 entries: two pieces
+    _, rows, lse = op.forward(h, w, y)
+    assert bool(rows.isfinite().all())
+    flat = torch.full((V * (D + 3) + 9,), 3.25, device="cuda", dtype=dtype)
+    apart = flat[5:5 + V * (D + 3)].view(V, D + 3)[:, :D]                             # through the workspace
+    op.backward(h, w, y, lse, one, dw=apart)
+    assert bool(apart.isfinite().all())
+    _give_up(op._workspace)
+    if op._staged is not None:
+        _give_up(op._staged_workspace)
+    for reduction in ("mean", "sum"):
+        loss, rows1, lse1 = op.forward(h, w, y, reduction)
+        counts = y >= 0
+        assert bool(loss.isnan()) and bool(rows1[counts].isnan().all()) and bool(lse1[counts].isnan().all())
+        for want in ((True, True), (True, False), (False, True)):
+            for dw in (None, apart):
+                dh, dw = op.backward(h, w, y, lse, one, reduction, rows=rows, dw=dw, want=want)
+                assert (dh is None or bool(dh.isnan().all())) and (dw is None or bool(dw.isnan().all())), want
+    none = y.clone().fill_(-1)
+    assert bool(op.forward(h, w, none)[0].isnan())
+    assert all(bool(t.isnan().all()) for t in op.backward(h, w, none, lse, one))
+    assert bool(op.backward(h[:0], w, y[:0], lse[:0], one)[1].isnan().all())          # no tokens at all
+    apart.fill_(3.25)
+    assert bool((flat == 3.25).all()), "wrote beside the rows"
+    op.close()
