@@ -125,7 +125,7 @@ class LinearXent(_Holder):
     a second context with a larger workspace.  It is made when such rows are first met, which
     cannot be inside a stream capture, and the first context stays as it is: CUDA graphs that
     were captured through this object keep their workspace as long as the object lives.
-    Calling the object gives the loss as a torch value with gradients::
+    Calling the object gives the loss as a torch value with gradients (of the first order)::
 
         loss = xent(h, w, targets)            # reduction="mean", "sum" or "none"
         loss.backward()
@@ -287,7 +287,7 @@ class LinearXent(_Holder):
 
 
 class _LinearXentFunction(torch.autograd.Function):
-    """LinearXent.forward and .backward as one differentiable step."""
+    """LinearXent.forward and .backward as one differentiable step; a second derivative raises an error."""
 
     @staticmethod
     def forward(ctx, h, w, targets, op, reduction):
@@ -299,6 +299,7 @@ class _LinearXentFunction(torch.autograd.Function):
         return rows if reduction == "none" else loss
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
         h, w, targets, rows, lse = ctx.saved_tensors
         dh, dw = ctx.op.backward(h, w, targets, lse, grad.float().contiguous(), ctx.reduction, rows=rows,

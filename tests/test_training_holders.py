@@ -130,3 +130,33 @@ def test_a_swarm_is_destroyed_once_whatever_the_entry_answers(monkeypatch):
     assert swarm.ctx is None
     swarm.close()
     assert seen == [17]
+
+
+class _PlainXent:
+    """Forward and backward of the linear cross entropy in torch operations, unseen by autograd as the kernels are."""
+
+    def forward(self, h, w, targets, reduction):
+        logits = h.float() @ w.float().T
+        lse = torch.logsumexp(logits, 1)
+        rows = lse - logits.gather(1, targets[:, None])[:, 0]
+        return rows.mean() if reduction == "mean" else rows.sum(), rows, lse
+
+    @torch.no_grad()
+    def backward(self, h, w, targets, lse, grad, reduction, *, rows=None, want=(True, True)):
+        d = torch.exp(h.float() @ w.float().T - lse[:, None])
+        d[torch.arange(len(targets)), targets] -= 1.0
+        d = d * grad / len(targets)
+        return (d @ w.float()).to(h.dtype), (d.T @ h.float()).to(w.dtype)
+
+
+def test_a_second_derivative_is_refused_rather_than_left_out():
+    torch.manual_seed(0)
+    h, w = torch.randn(5, 8, requires_grad=True), torch.randn(7, 8)
+    y = torch.randint(0, 7, (5,))
+    loss = training._LinearXentFunction.apply(h, w, y, _PlainXent(), "mean")
+    (dh,) = torch.autograd.grad(loss, h, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        (loss + dh.pow(2).sum()).backward()              # a gradient penalty
+    loss = training._LinearXentFunction.apply(h, w, y, _PlainXent(), "mean")
+    loss.backward()
+    assert torch.equal(h.grad, dh)
