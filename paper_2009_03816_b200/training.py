@@ -299,12 +299,27 @@ class _LinearXentFunction(torch.autograd.Function):
         return rows if reduction == "none" else loss
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, grad):
         h, w, targets, rows, lse = ctx.saved_tensors
-        dh, dw = ctx.op.backward(h, w, targets, lse, grad.float().contiguous(), ctx.reduction, rows=rows,
-                                 want=(ctx.needs_input_grad[0], ctx.needs_input_grad[1]))
+        with torch.no_grad():
+            dh, dw = ctx.op.backward(h, w, targets, lse, grad.float().contiguous(), ctx.reduction, rows=rows,
+                                     want=(ctx.needs_input_grad[0], ctx.needs_input_grad[1]))
+        if torch.is_grad_enabled():                # create_graph: what is done with the gradients is recorded
+            dh, dw = (None if d is None else _FirstOrderOnly.apply(d, h, w, grad) for d in (dh, dw))
         return dh, dw, None, None, None
+
+
+class _FirstOrderOnly(torch.autograd.Function):
+    """A gradient as it is, dependent on all that it came from, with an error in place of its derivative."""
+
+    @staticmethod
+    def forward(ctx, gradient, *came_from):
+        return gradient.view_as(gradient)
+
+    @staticmethod
+    def backward(ctx, grad):
+        raise RuntimeError("LinearXent: gradients are of the first order only (once_differentiable); a function of them "
+                           "cannot be differentiated")
 
 
 class AdamW(_Holder):
