@@ -29,6 +29,10 @@ _TYPES = {torch.float32: PSOPS_F32, torch.float16: PSOPS_F16, torch.bfloat16: PS
 _REDUCTIONS = {"mean": PSOPS_MEAN, "sum": PSOPS_SUM, "none": PSOPS_PER_TOKEN}
 MOMENT_BLOCK = 256               # elements that share one scale of an 8-bit moment
 
+# The kernels write through addresses, which autograd does not see: what they change in a caller's tensor is told
+# it here, so that a backward pass that had saved the tensor raises an error as it does after torch's own operations.
+_changed = torch.autograd.graph.increment_version
+
 
 def _refuse(where: str, why: str):
     raise PsopsError(PSOPS_EINVAL, where, why)
@@ -217,6 +221,7 @@ class LinearXent(_Holder):
         if reduction != "mean" and reduction != "sum":
             _refuse("LinearXent.forward", f"reduction {reduction!r}")
         tokens, h_ld, w_ld = self._arguments("LinearXent.forward", h, w, targets)
+        given = [] if loss is None else [loss]
         if loss is None:
             loss = torch.empty((), dtype=torch.float32, device=self.device)
         else:
@@ -225,6 +230,8 @@ class LinearXent(_Holder):
         lse = torch.empty_like(rows)
         ctx = self._context("LinearXent.forward", w, w_ld)
         binding.psops_xent_forward(ctx, h, h_ld, w, w_ld, targets, tokens, _REDUCTIONS[reduction], loss, rows, lse)
+        if given:
+            _changed(given)
         return loss, rows, lse
 
     def backward(self, h, w, targets, lse, grad, reduction="mean", *, rows=None, dh=None, dw=None, want=(True, True)):
@@ -240,10 +247,13 @@ class LinearXent(_Holder):
         if rows is not None:
             self._numbers(where, "rows", rows, targets.shape)
         self._numbers(where, "grad", grad, targets.shape if code == PSOPS_PER_TOKEN else None)
+        given = [t for t, wanted in ((dh, want[0]), (dw, want[1])) if wanted and t is not None]
         dh, dh_ld = self._gradient(where, "dh", dh, h) if want[0] else (None, 0)
         dw, dw_ld = self._gradient(where, "dw", dw, w) if want[1] else (None, 0)
         ctx = self._context(where, w, w_ld, dw, dw_ld)
         binding.psops_xent_backward(ctx, h, h_ld, w, w_ld, targets, tokens, lse, rows, grad, code, dh, dh_ld, dw, dw_ld)
+        if given:
+            _changed(given)
         return dh, dw
 
     def _numbers(self, where, name, t, shape):
@@ -403,6 +413,9 @@ class AdamW(_Holder):
             self._workspace = _workspace(binding.psops_adamw_workspace_bytes(cfg, table), device, where)
             self.ctx = binding.psops_adamw_create(cfg, table, self._workspace, None, self._on(device, stream))
         self._scale = None
+        # parameters and copies as autograd counts their changes: views share the count of what they are views of
+        self._written = list({id(t): t for t in (t._base if t._is_view() else t for t in (
+            *self.params, *(c for c in copies or () if c is not None)))}.values())
 
     def set_grads(self, grads):
         """Other gradient tensors for the steps to come, of the type given at first."""
@@ -421,6 +434,7 @@ class AdamW(_Holder):
         self._scale = grad_scale               # read by the kernel: keep it alive
         self._follow()
         binding.psops_adamw_step(self.ctx, lr, grad_scale)
+        _changed(self._written)
 
     @property
     def steps(self) -> int:
@@ -460,11 +474,14 @@ class GradNorm(_Holder):
     def norm(self, max_norm=math.inf, out=None):
         """(norm, factor), two device scalars: factor = min(1, max_norm / (norm + 1e-6)), NaN
         if the norm is not finite.  `out`: an fp32 device tensor of 2 elements to hold them."""
+        given = out is not None
         if out is None:
             out = torch.empty(2, dtype=torch.float32, device=self.device)
         elif out.device != self.device or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
             _refuse("GradNorm.norm", f"`out` has to be 2 fp32 numbers on {self.device}")
         self._follow()
         binding.psops_gradnorm_run(self.ctx, max_norm, out)
+        if given:
+            _changed(out)
         return out.unbind(0)
 
