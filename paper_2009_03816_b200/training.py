@@ -12,8 +12,13 @@ computation runs in the CUDA library.
 
 Calls enqueue on the current stream of the holder's GPU, or always on the one
 given when it is made; a call on another stream than the one before comes after
-it.  Tensors that were produced on yet another stream have to be ordered before
-the call by the caller, as for any kernel.
+it.  A given stream waits in each call for what the current one has been given
+so far, and tensors that are let go of meanwhile are kept from other uses until
+it is done with them; its results are the caller's to wait for, but for the
+differentiable call, whose results the current stream waits for.  Inside a stream
+capture nothing of this is recorded: there the caller orders the two.  Tensors that
+were produced on yet another stream have to be ordered before the call by the
+caller, as for any kernel.
 """
 from __future__ import annotations
 
@@ -64,6 +69,11 @@ def _device_of(where, tensors):
     return t.device
 
 
+def _is_capturing(stream):
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class _Holder:
     """What the three have in common: a context, its GPU and the stream its work goes to."""
 
@@ -75,24 +85,38 @@ class _Holder:
         self.stream = torch.cuda.current_stream(device).cuda_stream if stream is None else int(stream)
         return self.stream
 
-    def _follow(self):
-        """Moves the context to the current stream, unless it was given one."""
+    def _follow(self, *tensors):
+        """Moves the context to the current stream; one that was given its stream lets that wait for the current one, and
+        has `tensors`, the ones of the call that the holder does not keep, not used for anything else before it is done."""
+        now = torch._C._cuda_getCurrentRawStream(self.device.index)
+        if now == self.stream:
+            return
         if self._follows:
-            now = torch._C._cuda_getCurrentRawStream(self.device.index)
-            if now != self.stream:
+            if self.ctx is not None:
                 self._move(now)
-                self.stream = now
+            self.stream = now
+            return
+        self._order(to_own=True)
+        own = self._own()
+        for t in tensors:
+            if t is not None:
+                t.record_stream(own)
 
     def _move(self, stream):
         self._set_stream(self.ctx, stream)
 
+    def _own(self):
+        return torch.cuda.ExternalStream(self.stream, self.device)
+
+    def _order(self, to_own):
+        """A given stream behind the current one, or the other way round (unless one of them is being captured)."""
+        now, own = torch.cuda.current_stream(self.device), self._own()
+        if now.cuda_stream != own.cuda_stream and not any(map(_is_capturing, (now, own))):
+            own.wait_stream(now) if to_own else now.wait_stream(own)
+
     def _capturing(self):
         """Whether the stream of the next call is being captured."""
-        if not self._follows:
-            with torch.cuda.stream(torch.cuda.ExternalStream(self.stream, self.device)):
-                return torch.cuda.is_current_stream_capturing()
-        with torch.cuda.device(self.device):
-            return torch.cuda.is_current_stream_capturing()
+        return _is_capturing(torch.cuda.current_stream(self.device) if self._follows else self._own())
 
     @property
     def launches(self) -> int:
@@ -158,6 +182,7 @@ class LinearXent(_Holder):
         cfg = binding.psops_xent_config(self.tokens, self.dim, self.vocab, _TYPES[self.dtype], flags)
         with torch.cuda.device(self.device):
             workspace = _workspace(binding.psops_xent_workspace_bytes(cfg), self.device, "LinearXent")
+            self._follow()
             return workspace, binding.psops_xent_create(cfg, workspace, None, self.stream)
 
     def _rows(self, where, name, t):
@@ -196,18 +221,18 @@ class LinearXent(_Holder):
             _refuse(where, f"{tokens} tokens, made for {self.tokens}")
         return tokens, h_ld, w_ld
 
-    def _context(self, where, w, w_ld, dw=None, dw_ld=0):
-        """The context for these rows, on the stream that it works on."""
+    def _context(self, where, tensors, w, w_ld, dw=None, dw_ld=0):
+        """The context for these rows, ready for a call with `tensors`."""
         if self.dim % 8 == 0 and self.ctx is not None and (
                 w.data_ptr() % 16 or w_ld % 8 or dw is not None and (dw.data_ptr() % 16 or dw_ld % 8)):
             if self._staged is None and self._capturing():
                 raise PsopsError(PSOPS_ESTATE, where, "rows that are not 16-byte aligned, met for the first time inside a "
                                                       "stream capture: make one such call before it")
-            self._follow()
+            self._follow(*tensors)
             if self._staged is None:
                 self._staged_workspace, self._staged = self._open(self._flags | PSOPS_XENT_STAGED)
             return self._staged
-        self._follow()
+        self._follow(*tensors)
         return self.ctx
 
     def _move(self, stream):
@@ -228,7 +253,7 @@ class LinearXent(_Holder):
             self._numbers("LinearXent.forward", "loss", loss, None)
         rows = torch.empty(targets.shape, dtype=torch.float32, device=self.device)
         lse = torch.empty_like(rows)
-        ctx = self._context("LinearXent.forward", w, w_ld)
+        ctx = self._context("LinearXent.forward", (h, w, targets, loss, rows, lse), w, w_ld)
         binding.psops_xent_forward(ctx, h, h_ld, w, w_ld, targets, tokens, _REDUCTIONS[reduction], loss, rows, lse)
         if given:
             _changed(given)
@@ -250,11 +275,16 @@ class LinearXent(_Holder):
         given = [t for t, wanted in ((dh, want[0]), (dw, want[1])) if wanted and t is not None]
         dh, dh_ld = self._gradient(where, "dh", dh, h) if want[0] else (None, 0)
         dw, dw_ld = self._gradient(where, "dw", dw, w) if want[1] else (None, 0)
-        ctx = self._context(where, w, w_ld, dw, dw_ld)
+        ctx = self._context(where, (h, w, targets, lse, rows, grad, dh, dw), w, w_ld, dw, dw_ld)
         binding.psops_xent_backward(ctx, h, h_ld, w, w_ld, targets, tokens, lse, rows, grad, code, dh, dh_ld, dw, dw_ld)
         if given:
             _changed(given)
         return dh, dw
+
+    def _join(self):
+        """The current stream behind a given one: autograd's own operations follow there."""
+        if not self._follows:
+            self._order(to_own=False)
 
     def _numbers(self, where, name, t, shape):
         if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype is not torch.float32 or \
@@ -304,6 +334,7 @@ class _LinearXentFunction(torch.autograd.Function):
         if reduction not in ("mean", "sum", "none"):
             _refuse("LinearXent", f"reduction {reduction!r}")
         loss, rows, lse = op.forward(h, w, targets, "mean" if reduction == "mean" else "sum")
+        op._join()
         ctx.save_for_backward(h, w, targets, rows, lse)
         ctx.op, ctx.reduction = op, reduction
         return rows if reduction == "none" else loss
@@ -314,6 +345,7 @@ class _LinearXentFunction(torch.autograd.Function):
         with torch.no_grad():
             dh, dw = ctx.op.backward(h, w, targets, lse, grad.float().contiguous(), ctx.reduction, rows=rows,
                                      want=(ctx.needs_input_grad[0], ctx.needs_input_grad[1]))
+            ctx.op._join()
         if torch.is_grad_enabled():                # create_graph: what is done with the gradients is recorded
             dh, dw = (None if d is None else _FirstOrderOnly.apply(d, h, w, grad) for d in (dh, dw))
         return dh, dw, None, None, None
@@ -411,8 +443,9 @@ class AdamW(_Holder):
                                        at(vs[i]), sizes[i], decay[i]) for i in range(n)])
         with torch.cuda.device(device):
             self._workspace = _workspace(binding.psops_adamw_workspace_bytes(cfg, table), device, where)
-            self.ctx = binding.psops_adamw_create(cfg, table, self._workspace, None, self._on(device, stream))
-        self._scale = None
+            self._on(device, stream)
+            self._follow()
+            self.ctx = binding.psops_adamw_create(cfg, table, self._workspace, None, self.stream)
         # parameters and copies as autograd counts their changes: views share the count of what they are views of
         self._written = list({id(t): t for t in (t._base if t._is_view() else t for t in (
             *self.params, *(c for c in copies or () if c is not None)))}.values())
@@ -421,7 +454,7 @@ class AdamW(_Holder):
         """Other gradient tensors for the steps to come, of the type given at first."""
         grads = _flat_list("AdamW.set_grads", "grads", grads, (self.grads[0].dtype,), self.device, len(self._sizes),
                            self._sizes)
-        self._follow()
+        self._follow(*self.grads)                  # the old ones: steps on their way still read them
         binding.psops_adamw_set_grads(self.ctx, grads)
         self.grads = grads
 
@@ -431,8 +464,8 @@ class AdamW(_Holder):
                                            and grad_scale.get_device() == self.device.index
                                            and grad_scale.dtype is torch.float32 and grad_scale.numel() == 1):
             _refuse("AdamW.step", f"grad_scale has to be one fp32 number on {self.device}")
-        self._scale = grad_scale               # read by the kernel: keep it alive
-        self._follow()
+        self._follow(grad_scale)
+        self._scale = grad_scale               # read by the kernel, and by a captured one again: keep it alive
         binding.psops_adamw_step(self.ctx, lr, grad_scale)
         _changed(self._written)
 
@@ -460,14 +493,15 @@ class GradNorm(_Holder):
         self._sizes = [g.numel() for g in grads]
         with torch.cuda.device(self.device):
             self._workspace = _workspace(binding.psops_gradnorm_workspace_bytes(self._sizes), self.device, where)
+            self._on(self.device, stream)
+            self._follow()
             self.ctx = binding.psops_gradnorm_create([g if g.numel() else None for g in grads], self._sizes,
-                                                     _TYPES[grads[0].dtype], self._workspace, None,
-                                                     self._on(self.device, stream))
+                                                     _TYPES[grads[0].dtype], self._workspace, None, self.stream)
 
     def set_grads(self, grads):
         grads = _flat_list("GradNorm.set_grads", "grads", grads, (self.grads[0].dtype,), self.device,
                            len(self._sizes), self._sizes)
-        self._follow()
+        self._follow(*self.grads)
         binding.psops_gradnorm_set_grads(self.ctx, [g if g.numel() else None for g in grads])
         self.grads = grads
 
@@ -479,7 +513,7 @@ class GradNorm(_Holder):
             out = torch.empty(2, dtype=torch.float32, device=self.device)
         elif out.device != self.device or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
             _refuse("GradNorm.norm", f"`out` has to be 2 fp32 numbers on {self.device}")
-        self._follow()
+        self._follow(out)
         binding.psops_gradnorm_run(self.ctx, max_norm, out)
         if given:
             _changed(out)

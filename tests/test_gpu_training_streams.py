@@ -78,3 +78,146 @@ def test_rows_that_are_not_aligned_are_refused_if_a_capture_meets_them_first():
         assert torch.equal(a, b) and torch.equal(a, c)
     del graph
     op.close()
+
+
+# ---- a stream of the holder's own beside the current one -------------------------
+# torch.cuda._sleep occupies a stream for some 50 ms: without the order between the two
+# streams, and without memory being kept for the one that still uses it, what follows on
+# the other stream runs long before it.
+
+def _busy():
+    torch.cuda._sleep(100_000_000)
+
+
+def _adamw(stream, p, g, **kw):
+    return training.AdamW([p], [g], stream=stream, **kw)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_default_moments_are_zero_before_the_first_step_on_a_given_stream(bits):
+    gpu_util.ensure_library()
+    torch.manual_seed(0)
+    n = 1 << 20
+    p0, g = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    want, got = p0.clone(), p0.clone()
+    opt = _adamw(None, want, g, bits=bits)
+    for _ in range(3):
+        opt.step(1e-2)
+    torch.cuda.synchronize()
+    own = torch.cuda.Stream()
+    dirt = [torch.full((n,), 7.0, device="cuda") for _ in range(8)]       # what the moments' memory holds before
+    del dirt
+    _busy()
+    opt2 = _adamw(own.cuda_stream, got, g, bits=bits)
+    for _ in range(3):
+        opt2.step(1e-2)
+    own.synchronize()
+    assert torch.equal(want, got) and opt2.steps == 3
+    for a, b in zip(opt.moments, opt2.moments):
+        assert torch.equal(a[0].view(torch.uint8), b[0].view(torch.uint8))
+    opt.close(), opt2.close()
+
+
+def test_a_given_stream_waits_for_what_the_current_one_has_been_given():
+    h, w, y = _inputs(300, 64, 500)
+    one = torch.ones((), device="cuda")
+    own = torch.cuda.Stream()
+    plain, op = training.LinearXent(300, 64, 500), training.LinearXent(300, 64, 500, stream=own.cuda_stream)
+    want = plain.forward(h, w, y)
+    want = (*want, *plain.backward(h, w, y, want[2], one, rows=want[1]))
+    torch.cuda.synchronize()
+    late = torch.zeros_like(h)
+    dirt = [torch.empty_like(t) for t in want for _ in range(4)]
+    _busy()
+    for t in dirt:
+        t.fill_(7.0)                                   # on their way when the outputs take over their memory
+    late.copy_(h)
+    del dirt, t
+    got = op.forward(late, w, y)
+    got = (*got, *op.backward(late, w, y, got[2], one, rows=got[1]))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    norm = training.GradNorm([got[4]], stream=own.cuda_stream)
+    _busy()
+    got[4].mul_(2.0)
+    n, factor = norm.norm(1.0)
+    own.synchronize()
+    assert float(n) == pytest.approx(2.0 * float(want[4].double().norm()), rel=1e-5)
+    plain.close(), op.close(), norm.close()
+
+
+def test_memory_let_go_of_is_not_used_again_before_a_given_stream_is_done():
+    h, w, y = _inputs(300, 64, 500)
+    own = torch.cuda.Stream()
+    op = training.LinearXent(300, 64, 500, stream=own.cuda_stream)
+    one = torch.ones((), device="cuda")
+    loss, rows, lse = op.forward(h, w, y)
+    dh, dw = op.backward(h, w, y, lse, one, rows=rows)
+    torch.cuda.synchronize()
+    h2, one2 = h.clone(), one.clone()
+    out = torch.zeros_like(dw)
+    with torch.cuda.stream(own):
+        _busy()
+    op.forward(h2, w, y)                               # results dropped at once
+    op.backward(h2, w, y, lse, one2, rows=rows, dw=out)
+    del h2, one2
+    taken = [torch.full(s, 1.5, device="cuda", dtype=d) for s, d in (((), torch.float32), ((300,), torch.float32),
+                                                                     (h.shape, h.dtype)) for _ in range(8)]
+    torch.cuda.synchronize()
+    assert all(bool((t == 1.5).all()) for t in taken)
+    assert torch.equal(out, dw)
+    # AdamW: the scale and the gradients of a step that still waits
+    p, g = torch.zeros(5000, device="cuda"), torch.ones(5000, device="cuda")
+    opt = _adamw(own.cuda_stream, p, g.clone(), weight_decay=0.0)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(own):
+        _busy()
+    scale = torch.full((), 0.5, device="cuda")
+    opt.step(1e-2, scale)
+    opt.set_grads([g])
+    del scale
+    taken = [torch.full((), float("nan"), device="cuda") for _ in range(8)] + [torch.full((5000,), float("nan"), device="cuda")
+                                                                             for _ in range(4)]
+    torch.cuda.synchronize()
+    assert opt.steps == 1 and bool((p < -0.0099).all()) and len(taken) == 12
+    op.close(), opt.close()
+
+
+def test_the_differentiable_call_on_a_given_stream():
+    h, w, y = _inputs(300, 64, 500)
+    own = torch.cuda.Stream()
+    plain, op = training.LinearXent(300, 64, 500), training.LinearXent(300, 64, 500, stream=own.cuda_stream)
+    grads = []
+    for x in (plain, op):
+        h1, w1 = h.clone().requires_grad_(), w.clone().requires_grad_()
+        with torch.cuda.stream(own):
+            _busy()
+        loss = 2.0 * x(h1, w1, y)
+        with torch.cuda.stream(own):
+            _busy()
+        loss.backward()
+        grads.append((loss.detach().clone(), h1.grad.clone(), w1.grad.clone()))
+    for a, b in zip(*grads):
+        assert torch.equal(a, b)
+    plain.close(), op.close()
+
+
+def test_a_given_stream_in_a_capture():
+    h, w, y = _inputs(300, 64, 500)
+    own = torch.cuda.Stream()
+    op = training.LinearXent(300, 64, 500, stream=own.cuda_stream)
+    want = op.forward(h, w, y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=own):
+        got = op.forward(h, w, y)
+    for t in got:
+        t.zero_()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    del graph
+    op.close()
