@@ -133,7 +133,7 @@ int64_t copy_grid(const psops_xent *x, int64_t pieces) { return std::min<int64_t
     } while (0)
 
 // Which products run with pairs of CTAs.
-bool in_pairs(int job, int64_t tokens) { return job == kDw || job == kDwSums || tokens > kSingleTokens; }
+bool in_pairs(int job, int64_t tokens) { return job >= kDw || tokens > kSingleTokens; }
 
 bool aligned16(const void *p, int64_t ld) { return ((uintptr_t)p & 15u) == 0 && ld % 8 == 0; }
 
@@ -226,6 +226,7 @@ template <class T>
 ProductKernel product_of(int job, bool pair)
 {
     return job == kDw        ? psops_xent_product_kernel<T, kDw, true>
+           : job == kDwLong  ? psops_xent_product_kernel<T, kDwLong, true>
            : job == kDwSums  ? psops_xent_product_kernel<T, kDwSums, true>
            : job == kLoss    ? (pair ? psops_xent_product_kernel<T, kLoss, true> : psops_xent_product_kernel<T, kLoss, false>)
            : job == kDlogits ? (pair ? psops_xent_product_kernel<T, kDlogits, true> : psops_xent_product_kernel<T, kDlogits, false>)
@@ -442,6 +443,7 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             P.columns = (int)c.padded;
             P.result_rows = (int)count;
             P.dw_share_rows = (int)share_rows;
+            P.add = false;
             PSOPS_DO(product(x, kDwSums, tokens, ceil_div(count, kTile) * tiles_d * x->lay.dw_most, dlogits_across, hidden_across, dw_sums, P));
             PSOPS_DO(results<true>(x, x->at<float>(x->lay.dw_sums), (int)share_rows, (int)count, (uint16_t *)dw + first * dw_ld, dw_ld));
         } else if (dw != nullptr) {
@@ -450,7 +452,8 @@ int backward(psops_xent *x, const void *w, int64_t w_ld, int64_t tokens, void *d
             PSOPS_DO(make_map(x, &dw_out, type, to, direct ? x->cfg.dim : c.padded, count, direct ? dw_ld : c.padded, 32));
             P.columns = (int)c.padded;
             P.result_rows = (int)count;
-            PSOPS_DO(product(x, kDw, tokens, ceil_div(count, kTile) * tiles_d, dlogits_across, hidden_across, dw_out, P));
+            PSOPS_DO(product(x, tokens > kChainTokens ? kDwLong : kDw, tokens, ceil_div(count, kTile) * tiles_d, dlogits_across, hidden_across,
+                             dw_out, P));
             if (!direct) {
                 const int64_t grid = std::min<int64_t>(ceil_div(count, kCopyThreads / 32), (int64_t)x->sms * 8);
                 PSOPS_DO(launch(x, "psops_xent_unpack_kernel", psops_xent_unpack_kernel, grid, kCopyThreads, 0, to, (int)c.padded, count,

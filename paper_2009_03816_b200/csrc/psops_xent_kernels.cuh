@@ -265,6 +265,7 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const u
 //   kDlogits  compact rows         vocabulary     dim            the logits' gradient, 16 bits
 //   kDh       compact rows         dim            vocabulary     fp32 sums, added up over pieces
 //   kDw       vocabulary           dim            compact rows   dw, 16 bits
+//   kDwLong   the same, from a call of more tokens than one chain of sums may have
 //   kDwSums   the same, the summed axis in shares                fp32 sums
 //
 // Warp 0 of each CTA copies its share of both operands (of a pair: 128 rows of
@@ -277,7 +278,7 @@ __global__ void __launch_bounds__(kCopyThreads) psops_xent_unpack_kernel(const u
 // With 128 tokens or fewer half of a pair's rows would be empty; the first
 // three jobs then run with single CTAs on 128 x 256 tiles.
 // ---------------------------------------------------------------------------
-enum Job { kLoss = 0, kDlogits = 1, kDh = 2, kDw = 3, kDwSums = 4 };
+enum Job { kLoss = 0, kDlogits = 1, kDh = 2, kDw = 3, kDwLong = 4, kDwSums = 5 };
 
 constexpr int kTile = 256, kHalf = 128;
 constexpr int kOperandBytes = kHalf * kStepK * 2;                // 128 rows of A or B
@@ -293,14 +294,25 @@ template <bool PAIR> struct ProductShape {
     static constexpr int kStageBytes = kOperandBytes * (PAIR ? 2 : 3);
     static constexpr int kShared = kStages * kStageBytes + kOutWarps * kOuts * kOutBytes + 1024;       // 1024: alignment
 };
-constexpr int kChainSteps = 12;                                  // most steps of a logit summed by the tensor cores in one go
 // The tensor cores cut off what does not fit into a running sum, so a chain of n
-// products of 16 elements each ends nearer to zero than it should: measured, by
-// 0.26 to 0.38 (bf16) and 0.35 to 0.97 (fp16, whose products have more bits to
-// lose) times n 2^-24 of its value for logits of 16 that lean to their label, up to
-// 0.49 and 1.5 where all products have one sign.  The middle of that is put back
-// with the factor that the logits are multiplied with anyway: what is left of the
-// loss's error is mostly below 5e-7.
+// products of 16 elements each ends nearer to zero than it should, by c n 2^-24 of
+// its value: at most a unit in the last place per product, c <= 2.  Measured for
+// logits of 16 that lean to their label: c = 0.26 to 0.38 (bf16) and 0.35 to 0.97
+// (fp16, whose products have more bits to lose); where all products have one sign
+// up to 0.49 and 1.5, and up to 1.6 in dw's sums over 300,000 tokens, of either type.
+// So sums are made of chains of at most so many steps, which are added up in fp32,
+// to nearest (logits and dw in registers, the fp32 sums where they lie; dw has a
+// variant for it, since the registers cost it 452 bytes of spills):
+//   a logit: 12 steps, n <= 48, since the loss is fp32;
+//   dh, dw: 128 steps, n <= 512: at most 6e-5 of the value, an eighth of fp16's unit
+//   roundoff.  One chain of 131,072 terms left dh 1.2e-4 too small, one of 300,000 dw
+//   1.8e-3.
+constexpr int kLogitSteps = 12, kSumSteps = 128;
+constexpr int kChainTokens = kSumSteps * kStepK;                 // a call of more takes kDwLong
+// For the logits the middle of the loss is also put back, with the factor that they
+// are multiplied with anyway: what is left of the loss's error is mostly below 5e-7.
+// Where nothing was cut off (a logit of one product), the factor itself is the
+// error: 0.3 and 0.6 of 48 2^-24, 9e-7 and 1.7e-6 of the logit.
 template <class T> constexpr float kCutOff = 0.3f * 0x1p-24f;
 template <> constexpr float kCutOff<__half> = 0.6f * 0x1p-24f;
 constexpr int kGroupTiles = 8;                                   // row tiles that share columns in L2
@@ -312,7 +324,7 @@ struct ProductParams {
     int result_rows;                             // kDw, kDwSums: entries of the piece
     int dw_share_rows;                           // kDwSums: rows between the shares' sums
     int first;                                   // first vocabulary entry of the piece
-    bool add;                                    // kDh: add to the sums of the pieces before
+    bool add;                                    // kDh: add to the sums of the pieces before (else false)
     const int *label;
     const float *row_lse, *row_scale, *row_label;
     float2 *stats;                               // (max, sum of exp2) by 128 vocabulary entries and compact row, base 2
@@ -371,9 +383,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                           const __grid_constant__ CUtensorMap map_out, const ProductParams P)
 {
-    constexpr bool kAAcross = JOB == kDw || JOB == kDwSums, kBAcross = JOB == kDh || kAAcross;
-    constexpr bool kSums = JOB == kDh || JOB == kDwSums;
-    constexpr bool kChained = JOB == kLoss || JOB == kDlogits;
+    constexpr bool kAAcross = JOB == kDw || JOB == kDwLong || JOB == kDwSums, kBAcross = JOB == kDh || kAAcross;
+    constexpr bool kSums = JOB == kDh || JOB == kDwSums, kLogits = JOB == kLoss || JOB == kDlogits;
+    constexpr int kChainSteps = kLogits ? kLogitSteps : kSumSteps;
     using S = ProductShape<PAIR>;
     constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes, kRows = S::kRows;
     constexpr uint32_t kInstruction = umma::instruction(__is_same(T, __nv_bfloat16), kAAcross, kBAcross, kRows, kTile);
@@ -416,11 +428,11 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
     const int tiles_m = ((kAAcross ? P.result_rows : JOB == kDh ? rows : some_rows) + kRows - 1) / kRows;
     const int tiles_n = (P.columns + kTile - 1) / kTile;
     const int steps = ((kAAcross ? some_rows : P.depth) + kStepK - 1) / kStepK;
-    const int fewest = (steps + kChainSteps - 1) / kChainSteps;                        // chains of a logit, of like length
-    const int chain = kChained ? (steps + fewest - 1) / fewest : steps;
-    const int chains = (steps + chain - 1) / chain;
-    const float put_back = 1.0f + kCutOff<T> * (float)(chain * (kStepK / 16)), unit = kLog2e * put_back;
     const int splits = JOB == kDh ? P.control->shares : JOB == kDwSums ? P.control->dw_shares : 1;
+    const int share = (steps + splits - 1) / splits;                                   // steps of the longest share
+    const int fewest = (share + kChainSteps - 1) / kChainSteps;                        // chains of like length
+    const int chain = (share + fewest - 1) / fewest;
+    const float put_back = 1.0f + kCutOff<T> * (float)(chain * (kStepK / 16)), unit = kLog2e * put_back;
     const int works = tiles_m * tiles_n * splits;
     const int pair = blockIdx.x / S::kCtas, pairs = gridDim.x / S::kCtas;
 
@@ -503,7 +515,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         const uint32_t own_outs = outs + (warp - 4) * S::kOuts * kOutBytes;
         int turn = 0;                                // which of them is written next
-        const float unscale = JOB == kDw ? P.control->unscale : 1.0f;
+        const float unscale = kAAcross && !kSums ? P.control->unscale : 1.0f;
         const int share_rows = JOB == kDh ? P.control->share_rows : JOB == kDwSums ? P.dw_share_rows : 0;
         int buffer = 0;
         uint32_t phase = 0;
@@ -513,7 +525,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
             const int col0 = w.n * kTile + half * kHalf;
             int y = -1;
             float lse = 0.0f, g = 0.0f, at_label = 2.0f;
-            if (JOB == kLoss || JOB == kDlogits) {
+            if (kLogits) {
                 if (row < rows) y = P.label[row] - P.first - col0;
                 if (JOB == kDlogits && row < rows) {
                     lse = P.row_lse[row];
@@ -523,6 +535,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
             }
             const uint32_t quarter_base = tensor_base + ((uint32_t)(quarter * 32) << 16) + half * kHalf;
             float top = -INFINITY, sum = 0.0f;
+            bool add = P.add;
             // 64 columns from column c of this warp's, as bit patterns in u
             auto finish = [&](int c, uint32_t *u) {
                 const int left = P.columns - (col0 + c);       // columns that exist from here on
@@ -565,7 +578,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                             for (int j = 0; j < 64; ++j)
                                 if (j >= mine) u[j] = 0u;
                         }
-                    } else if (JOB == kDw) {
+                    } else if (!kSums) {
 #pragma unroll
                         for (int j = 0; j < 64; ++j) u[j] = __float_as_uint(__uint_as_float(u[j]) * unscale);
                     }
@@ -601,7 +614,7 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                         if (lane == 0) {
                             const int x = col0 + c + box * 32;
                             if (wanted && (JOB == kDlogits || x < P.columns)) {
-                                if (JOB == kDh && P.add) umma::tensor_add(&map_out, x, w.split * share_rows + row0, out);
+                                if (kSums && add) umma::tensor_add(&map_out, x, w.split * share_rows + row0, out);
                                 else umma::tensor_store(&map_out, x, w.split * share_rows + row0, out);
                             }
                             umma::stores_commit();
@@ -609,14 +622,25 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                     }
                 }
             };
+            const int k_first = (int)((long long)steps * w.split / splits), k_last = (int)((long long)steps * (w.split + 1) / splits);
+            const int chains = (k_last - k_first + chain - 1) / chain;
             bool ok = true;
-            if constexpr (kChained) {
+            // the accumulator of the next chain: there, and given back when it is in registers
+            auto take = [&]() {
+                ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_sum[buffer]), phase, failed));
+                umma::fence_after();
+                return ok;
+            };
+            auto give = [&]() {
+                umma::fence_before();
+                __syncwarp();
+                if (lane == 0) umma::barrier_arrive_at(umma::in_cta(umma::shared_address(&bar_free[buffer]), 0));
+            };
+            if constexpr (kLogits || JOB == kDwLong) {
                 uint32_t total[kHalf];
 #pragma unroll 1
                 for (int q = 0; q < chains; ++q) {
-                    ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_sum[buffer]), phase, failed));
-                    if (!ok) break;
-                    umma::fence_after();
+                    if (!take()) break;
                     const uint32_t sums = quarter_base + buffer * kTile;
                     if (q == 0) {
 #pragma unroll
@@ -633,33 +657,33 @@ psops_xent_product_kernel(const __grid_constant__ CUtensorMap map_a, const __gri
                                 total[c + j] = __float_as_uint(__uint_as_float(total[c + j]) + __uint_as_float(t[j]));
                         }
                     }
-                    umma::fence_before();
-                    __syncwarp();
-                    if (lane == 0) umma::barrier_arrive_at(umma::in_cta(umma::shared_address(&bar_free[buffer]), 0));
+                    give();
                     if (++buffer == 2) { buffer = 0; phase ^= 1u; }
                 }
                 if (!ok) break;
                 finish(0, total);
                 finish(64, total + 64);
             } else {
-                ok = __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(&bar_sum[buffer]), phase, failed));
-                if (!ok) break;
-                umma::fence_after();
-                const uint32_t sums = quarter_base + buffer * kTile;
 #pragma unroll 1
-                for (int c = 0; c < kHalf; c += 64) {
-                    uint32_t u[64];
-                    umma::tensor_memory_load(sums + c, u);
-                    umma::tensor_memory_load(sums + c + 32, u + 32);
-                    umma::tensor_memory_loaded<64>(u);
-                    if (c == kHalf - 64) {           // the last of this warp's sums are in registers
-                        umma::fence_before();
-                        __syncwarp();
-                        if (lane == 0) umma::barrier_arrive_at(umma::in_cta(umma::shared_address(&bar_free[buffer]), 0));
+                for (int q = 0; q < chains; ++q) {
+                    if (!take()) break;
+                    if (q > 0) {                         // always in the same order: the chain before lies in memory
+                        add = true;
+                        if (lane == 0) umma::stores_done();
                     }
-                    finish(c, u);
+                    const uint32_t sums = quarter_base + buffer * kTile;
+#pragma unroll 1
+                    for (int c = 0; c < kHalf; c += 64) {
+                        uint32_t u[64];
+                        umma::tensor_memory_load(sums + c, u);
+                        umma::tensor_memory_load(sums + c + 32, u + 32);
+                        umma::tensor_memory_loaded<64>(u);
+                        if (c == kHalf - 64) give();
+                        finish(c, u);
+                    }
+                    if (++buffer == 2) { buffer = 0; phase ^= 1u; }
                 }
-                if (++buffer == 2) { buffer = 0; phase ^= 1u; }
+                if (!ok) break;
             }
             if (JOB == kLoss && row < rows)
                 P.stats[(long long)((P.first + col0) / kHalf) * P.stats_ld + row] = make_float2(top > -INFINITY ? top * unit : -INFINITY, sum);
