@@ -2,6 +2,15 @@
 
 The tolerances come from the sums.  u = 2^-24.
 
+* The tensor cores cut a running sum off after every 16 products: a chain of n such
+  blocks ends c n u of its value nearer to zero, c measured as 0.17 to 0.49 for bf16
+  and 0.35 to 1.5 for fp16.  A logit's chains have at most 48 blocks and 0.3 (bf16)
+  or 0.6 (fp16) of that is put back; inputs that lean to their label have c of 0.26
+  to 0.38 and 0.35 to 0.97, which leaves 0.08 and 0.37 of 48 u; the fp32 sums of up
+  to six chains and the base-2 softmax add some 4 u of rounding: 8 u and 22 u of the
+  logit.  Where all products have one sign, 0.19 and 0.9 of 48 u stay: 14 u and 48 u.
+  Where nothing is cut off, what is put back is the error: 0.3 and 0.6 of 48 u, and
+  rounding: 19 u and 33 u.
 * dh and dw: a chain has at most 512 blocks, each of which cuts off at most a unit in
   the last place, 2 u: a bias of at most 1024 u = 6.1e-5, and nothing is put back.
   The rounding of the logits' gradients to 16 bits has a bias of its own (a token's
@@ -12,6 +21,8 @@ The tolerances come from the sums.  u = 2^-24.
   and the results once more, each with the same relative spread at most, so that its
   norm is at most sqrt(2) of that of exact products rounded once.
 """
+import math
+
 import pytest
 import torch
 
@@ -46,6 +57,64 @@ def _leaning(T, D, V, dtype, seed):
 
 def _rounded(d, dtype):
     return (d * HEADROOM[dtype]).to(dtype).double() / HEADROOM[dtype]
+
+
+def _exact(h, w, y, grad):
+    logits = h.double() @ w.double().T
+    lse = torch.logsumexp(logits, 1)
+    at = torch.arange(len(y), device="cuda")
+    right = logits[at, y]
+    d = torch.exp(logits - lse[:, None])
+    d[at, y] -= 1.0
+    d16 = _rounded(d, h.dtype)
+    return lse, lse - right, right, [(x @ w.double() * grad, x.T @ h.double() * grad) for x in (d, d16)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,D,V", [(512, 1000, 3000), (256, 1536, 8192), (384, 2048, 5001), (256, 4096, 4096), (100, 4096, 2000)])
+def test_leaning_inputs(T, D, V, dtype):
+    h, w, y = _leaning(T, D, V, dtype, 5)
+    lse, rows, right, (exact, summed) = _exact(h, w, y, 1.0 / T)
+    op = training.LinearXent(T, D, V, dtype=dtype)
+    loss, rows1, lse1 = op.forward(h, w, y)
+    dh1, dw1 = op.backward(h, w, y, lse1, torch.tensor(1.0, device="cuda"), rows=rows1)
+    op.close()
+    tol = (8 if dtype == torch.bfloat16 else 22) * U
+    logit = lse1.double() - rows1.double()                 # what the label's logit came out as
+    size = float(right.norm())
+    assert abs(float(((logit - right) * right.sign()).sum() / right.abs().sum())) <= tol        # bias
+    assert float((logit - right).norm()) <= 2 * tol * size                                      # spread
+    assert abs(float((lse1.double() - lse).mean() / lse.mean())) <= tol
+    assert float((lse1.double() - lse).norm() / lse.norm()) <= 2 * tol
+    assert abs(float(loss) - float(rows.mean())) <= 2 * tol * float(lse.mean())
+    for got, want, sums in zip((dh1, dw1), exact, summed):
+        error, rounded = _projection(got, want)[1], _projection(want.to(dtype), want)[1]
+        bias = _projection(got, sums)[0]
+        assert error <= 1.5 * rounded and abs(bias) <= SUM_BIAS, (error / rounded, bias)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("D", [768, 2048])
+def test_logits_of_one_sign_and_logits_that_need_no_rounding(D, dtype):
+    T = V = 256
+    gpu_util.ensure_library()
+    g = torch.Generator(device="cuda").manual_seed(6)
+    y = torch.arange(T, device="cuda")
+    op = training.LinearXent(T, D, V, dtype=dtype, gradients=False)
+    w = torch.empty(V, D, device="cuda").normal_(0.0, 0.02, generator=g).to(dtype)
+    h = (w.float().sign() * torch.rand(T, D, device="cuda", generator=g)).to(dtype)
+    right = (h.double() * w.double()).sum(1)
+    _, rows, lse = op.forward(h, w, y)
+    bias = float((lse.double() - rows.double() - right).sum() / right.sum())
+    assert abs(bias) <= (14 if dtype == torch.bfloat16 else 48) * U, bias
+    # one feature in each: the logit 16 at the label and zeros elsewhere, exactly
+    h = torch.zeros(T, D, device="cuda")
+    h[y, y] = 16.0
+    w = torch.eye(V, D, device="cuda").to(dtype)
+    _, rows, lse = op.forward(h.to(dtype), w, y)
+    want = math.log(math.exp(16.0) + V - 1)
+    assert float((lse.double() - want).abs().max()) <= (19 if dtype == torch.bfloat16 else 33) * U * 16.0
+    op.close()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
