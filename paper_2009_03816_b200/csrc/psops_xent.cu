@@ -581,7 +581,8 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
         H.dh_ld = dh_ld;
         return x->cfg.type == PSOPS_F16 ? backward_head<__half>(x, H, d_dw, dw_ld) : backward_head<__nv_bfloat16>(x, H, d_dw, dw_ld);
     }
-    if (is_few(tokens, x->cfg.dim) && x->cfg.dim <= kFewGradDim) {
+    const bool aligned = x->cfg.dim % 8 == 0 && aligned16(d_w, w_ld) && (d_dw == nullptr || aligned16(d_dw, dw_ld));
+    if (is_few(tokens, x->cfg.dim) && x->cfg.dim <= kFewGradDim && few_grads_pay(tokens, x->cfg.dim, x->cfg.vocab, aligned)) {
         FewGradParams F{};
         F.h = (const uint16_t *)d_h; F.h_ld = h_ld; F.h_aligned = aligned16(d_h, h_ld);
         F.w = (const uint16_t *)d_w; F.w_ld = w_ld;
@@ -593,7 +594,6 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
         F.padded = (int)x->lay.padded;
         F.want_dh = d_dh != nullptr;
         F.dw = (uint16_t *)d_dw; F.dw_ld = dw_ld;
-        const bool aligned = x->cfg.dim % 8 == 0 && aligned16(d_w, w_ld) && (d_dw == nullptr || aligned16(d_dw, dw_ld));
         return x->cfg.type == PSOPS_F16 ? backward_few<__half>(x, F, aligned, d_dh, dh_ld) : backward_few<__nv_bfloat16>(x, F, aligned, d_dh, dh_ld);
     }
     IndexParams P{};

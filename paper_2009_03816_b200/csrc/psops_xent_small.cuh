@@ -416,14 +416,32 @@ __global__ void __launch_bounds__(kSmallThreads, kFewBlocks) psops_xent_few_kern
 // takes a few rows of w at a time: the logits of the rows, then, with the rows still in registers, their part of dh and their rows
 // of dw.  The teams' parts of dh are added up by a kernel behind.  fp32
 // throughout, so nothing but the results is rounded to 16 bits.
-// Measured in a CUDA graph, this form / the tensor cores, 32,768 x 4,096: 1 token
-// 99 / 185 us (537 MB: 82 us), 2 tokens 122 / 182, 4 tokens 189 / 183; 32,003 x
-// 1,000: 3 tokens 59 / 68.  Rows at a time and blocks of an SM: what registers
-// allow, the best of 1, 2 and 4 rows with 1 to 4 blocks.
+// Rows at a time and blocks of an SM: what registers allow, the best of 1, 2 and 4
+// rows with 1 to 4 blocks.
+// Measured in a CUDA graph, this form / the tensor cores, us:
+//   one token    32,768 x 4,096: 99 / 185 (537 MB: 82)    131,072 x 600: 89 / 157
+//   two          32,768 x 4,096: 122 / 183   131,072 x 4,096: 454 / 659   131,072 x 64: 65 / 73
+//   three, four  131,072 x 512: 98 / 126     32,768 x 1,024: 61 / 70      131,072 x 1,024: 193 / 200
+//                16,384 x 4,096: 102 / 114   4,096 x 3,000: 31 / 58       32,768 x 768: 59 / 59
+//                32,768 x 4,096: 190 / 185   131,072 x 2,048: 367 / 347   32,768 x 3,000: 187 / 158
+//                32,768 x 1,536: 100 / 90    65,536 x 768: 104 / 96       65,536 x 128: 56 / 50
+// From three tokens on the arithmetic bounds it, on whole warps of 512 features;
+// the tensor cores cost some 15 us more in launches, then less per feature that
+// is there and a little per row.  Where rows are not 16-byte aligned the element
+// by element loads bound it from two tokens on: 4,096 x 2,100 with four tokens
+// 61 / 70, 16,384 x 1,100 with two 90 / 90, 8,192 x 4,001 with two 177 / 159,
+// 65,536 x 1,100 with two 387 / 299; with one 16,384 x 1,100 63 / 89.
 constexpr int kFewGradDim = 4096;
 template <int N> constexpr int kFewGradRows = N == 2 ? 4 : 2;
 template <int N> constexpr int kFewGradBlocks = N == 1 ? 2 : 1;
 inline int few_team(int64_t dim) { return dim <= 512 ? 1 : dim <= 1024 ? 2 : dim <= 2048 ? 4 : 8; }
+
+inline bool few_grads_pay(int64_t tokens, int64_t dim, int64_t vocab, bool aligned)
+{
+    if (tokens == 1) return true;
+    if (!aligned) return vocab * dim <= 1 << 24;
+    return tokens == 2 || vocab * (9 * 512 * few_team(dim) - 8 * dim - 1024) < 3 << 25;
+}
 
 struct FewGradParams {
     const uint16_t *h, *w;
