@@ -523,7 +523,7 @@ int psops_xent_forward(psops_xent *x, const void *d_h, int64_t h_ld, const void 
     if (((uintptr_t)d_loss | (uintptr_t)d_rows | (uintptr_t)d_lse) & 3u) return PSOPS_EALIGN;
     OnDevice guard(x);
     const bool half = x->cfg.type == PSOPS_F16;
-    if (is_head(x->cfg.vocab, x->cfg.dim, tokens)) {
+    if (is_head(x->cfg.vocab, x->cfg.dim, tokens, false)) {
         HeadParams H = head_params(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, reduction);
         H.loss = d_loss;
         H.rows = d_rows;
@@ -571,7 +571,7 @@ int psops_xent_backward(psops_xent *x, const void *d_h, int64_t h_ld, const void
     if (((uintptr_t)d_lse | (uintptr_t)d_rows | (uintptr_t)d_grad) & 3u) return PSOPS_EALIGN;
     if (d_dw != nullptr && !x->lay.staged && !aligned16(d_dw, dw_ld)) return PSOPS_EALIGN;
     OnDevice guard(x);
-    if (is_head(x->cfg.vocab, x->cfg.dim, tokens)) {
+    if (is_head(x->cfg.vocab, x->cfg.dim, tokens, true)) {
         HeadParams H = head_params(x, d_h, h_ld, d_w, w_ld, d_targets, tokens, reduction);
         H.lse = d_lse;
         H.known_rows = d_rows;

@@ -17,15 +17,35 @@ constexpr int kSmallThreads = 256, kSmallWarps = kSmallThreads / 32;
 // Up to 64 classes whose weights fit into shared memory beside a hidden state
 // per warp.  A warp takes a token: 32 / `wide` slices of the features by `wide`
 // classes (the power of two above their number), then the softmax across lanes.
+// Every block loads all weights, element by element, and a warp's tokens come one
+// after the other; dw's few blocks walk through all tokens.  Measured in a CUDA
+// graph, this form / the tensor cores, us, dim x classes:
+//   tokens          256            1,024         2,048         4,096          8,192
+//   loss   84 x 10  7.4 / 17       7.4 / 17      9.4 / 18      13 / 20        19 / 22
+//          512 x 10 12 / 17        13 / 18       19 / 18       30 / 21        47 / 24
+//          84 x 64  9.8 / 17       10 / 17       14 / 18       21 / 20        33 / 22
+//          512 x 64 33 / 17        34 / 17       51 / 18       84 / 21        135 / 24
+//   grads  84 x 10  13 / 28        26 / 32       50 / 32       95 / 35        177 / 39
+//          512 x 10 20 / 27        37 / 32       64 / 34       123 / 38       234 / 47
+//          84 x 64  16 / 29        32 / 33       55 / 33       106 / 35       200 / 40
+//          512 x 64 42 / 28        60 / 32       102 / 34      186 / 39       337 / 48
+// (16 tokens take what 256 do, but for the gradients of 84 x 10: 7.4 / 25.)  Loading
+// grows with dim times `wide`, the tensor cores' time with dim alone: 64 tokens x
+// 192 x 64 16 / 17, 16 x 1,200 x 10 23 / 22, 64 x 2,000 x 4 22 / 26.
 constexpr int kHeadClasses = 64;
-constexpr int kHeadTokens = 4096;                // more are better off on the tensor cores: every block counts all labels
+constexpr int64_t kHeadWeights = 12000;                                  // dim times `wide` beyond 5.5
+constexpr int64_t kHeadLossTokens = 8192, kHeadLossWork = 1 << 24;       // work: tokens times dim times `wide`
+constexpr int64_t kHeadGradTokens = 1024, kHeadGradWork = 1 << 22;
 constexpr int kHeadShared = 200 * 1024;
 
 __host__ __device__ inline int head_wide(int vocab) { return vocab <= 8 ? 8 : vocab <= 16 ? 16 : vocab <= 32 ? 32 : 64; }
 inline size_t head_shared(int vocab, int dim) { return 4ull * (size_t)dim * (head_wide(vocab) + 1 + kSmallWarps) + 4ull * kSmallWarps * kHeadClasses; }
-inline bool is_head(int64_t vocab, int64_t dim, int64_t tokens)
+inline bool is_head(int64_t vocab, int64_t dim, int64_t tokens, bool grads)
 {
-    return vocab <= kHeadClasses && tokens <= kHeadTokens && dim <= kHeadShared / 4 && head_shared((int)vocab, (int)dim) <= (size_t)kHeadShared;
+    if (vocab > kHeadClasses) return false;
+    const int64_t wide = head_wide((int)vocab), weights = dim * wide;
+    return 2 * weights - 11 * dim <= 2 * kHeadWeights && tokens <= (grads ? kHeadGradTokens : kHeadLossTokens) &&
+           tokens * weights <= (grads ? kHeadGradWork : kHeadLossWork) && head_shared((int)vocab, (int)dim) <= (size_t)kHeadShared;
 }
 
 struct HeadParams {

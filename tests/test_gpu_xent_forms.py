@@ -43,3 +43,20 @@ def test_gradients_of_few_tokens_by_alignment():
 def test_values_of_few_tokens_on_both_sides(T, D, V, dtype):
     _run(T, D, V, dtype, seed=81)
     _run(T, D, V, dtype, seed=82, masked=0.4, reduction="sum")
+
+
+# few classes: one launch for the loss and two for the gradients, where those are faster
+@pytest.mark.parametrize("T,D,V,loss,grads", [(256, 84, 10, True, True), (1024, 84, 10, True, True), (4096, 84, 10, True, False),
+                                              (9000, 84, 10, False, False), (1024, 512, 10, True, False), (4096, 512, 10, False, False),
+                                              (256, 512, 64, False, False), (2048, 84, 64, True, False), (4096, 84, 64, False, False)])
+def test_few_classes_take_the_form_that_was_faster(T, D, V, loss, grads):
+    got = _launches(T, D, V)
+    assert (got[0] == 1) == loss and (got[1] == 2) == grads, got
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,D,V", [(1024, 84, 10), (1025, 84, 10), (8192, 84, 10), (8193, 84, 10), (700, 512, 10), (256, 193, 64), (256, 192, 64),
+                                   (300, 12_000, 1), (6, 4000, 3), (2049, 512, 10)])
+def test_values_of_few_classes_on_both_sides(T, D, V, dtype):
+    _run(T, D, V, dtype, seed=83)
+    _run(T, D, V, dtype, seed=84, masked=0.4, reduction="sum")
