@@ -511,11 +511,12 @@ class GradNorm(_Holder):
         given = out is not None
         if out is None:
             out = torch.empty(2, dtype=torch.float32, device=self.device)
-        elif out.device != self.device or out.dtype != torch.float32 or out.numel() != 2 or not out.is_contiguous():
+        elif not isinstance(out, torch.Tensor) or out.device != self.device or out.dtype != torch.float32 or \
+                out.numel() != 2 or not out.is_contiguous():
             _refuse("GradNorm.norm", f"`out` has to be 2 fp32 numbers on {self.device}")
         self._follow(out)
         binding.psops_gradnorm_run(self.ctx, max_norm, out)
         if given:
             _changed(out)
-        return out.unbind(0)
+        return out.view(2).unbind(0)
 
