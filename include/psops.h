@@ -449,7 +449,8 @@ int psops_adamw_create(psops_adamw **out, const psops_adamw_config *cfg, const p
 
 /* New gradient addresses, one per tensor (a framework that allocates gradients
  * anew for each step).  Enqueued on the stream: steps already enqueued keep the
- * old ones.  Not inside a stream capture.  EINVAL, EALIGN, ECUDA. */
+ * old ones; the host waits for the table sent before, if that is still on its way.
+ * EINVAL, EALIGN, ESTATE (inside a stream capture; nothing is changed), ECUDA. */
 int psops_adamw_set_grads(psops_adamw *opt, const void *const *grads);
 
 /*
@@ -484,7 +485,7 @@ typedef struct psops_gradnorm psops_gradnorm;  /* opaque */
 size_t psops_gradnorm_workspace_bytes(int32_t n_tensors, const int64_t *n);
 int psops_gradnorm_create(psops_gradnorm **out, int32_t n_tensors, const void *const *grads, const int64_t *n,
                           int32_t grad_type, void *d_workspace, size_t workspace_bytes, void *cuda_stream);
-int psops_gradnorm_set_grads(psops_gradnorm *gn, const void *const *grads);
+int psops_gradnorm_set_grads(psops_gradnorm *gn, const void *const *grads);  /* as psops_adamw_set_grads */
 int psops_gradnorm_run(psops_gradnorm *gn, float max_norm, float *d_out);
 int psops_gradnorm_set_stream(psops_gradnorm *gn, void *cuda_stream);
 int64_t psops_gradnorm_launch_count(const psops_gradnorm *gn);

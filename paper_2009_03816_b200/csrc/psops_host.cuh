@@ -103,6 +103,15 @@ inline int set_stream(Base *b, void *cuda_stream)
     return PSOPS_OK;
 }
 
+// A table that is sent from the staging below cannot be part of a captured graph:
+// every replay would send what the staging holds by then.
+inline int not_capturing(Base *b)
+{
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    PSOPS_TRY(b, cudaStreamIsCapturing(b->stream, &status));
+    return status == cudaStreamCaptureStatusNone ? PSOPS_OK : PSOPS_ESTATE;
+}
+
 // Page-locked staging of a small table that is sent to the device again and
 // again: the copy is asynchronous, and the staging is not overwritten before
 // the copy that read it has run.

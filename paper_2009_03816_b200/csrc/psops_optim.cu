@@ -266,6 +266,8 @@ int psops_adamw_set_grads(psops_adamw *a, const void *const *grads)
         const int rc = adamw_entry(&a->cfg, &t, &e);
         if (rc != PSOPS_OK) return rc;
     }
+    const int rc = psops_host::not_capturing(a);
+    if (rc != PSOPS_OK) return rc;
     PSOPS_TRY(a, a->staging.wait());
     for (int32_t i = 0; i < n; ++i) {
         a->tensors[(size_t)i].g = grads[i];
@@ -444,6 +446,8 @@ int psops_gradnorm_set_grads(psops_gradnorm *q, const void *const *grads)
         const int rc = norm_entry(grads[i], q->n[i], q->grad_type, &e);
         if (rc != PSOPS_OK) return rc;
     }
+    const int rc = psops_host::not_capturing(q);
+    if (rc != PSOPS_OK) return rc;
     PSOPS_TRY(q, q->staging.wait());
     for (size_t i = 0; i < q->n.size(); ++i)
         norm_entry(grads[i], q->n[i], q->grad_type, (NormEntry *)q->staging.host() + i);

@@ -221,3 +221,28 @@ def test_a_given_stream_in_a_capture():
         assert torch.equal(a, b)
     del graph
     op.close()
+
+
+def test_new_gradient_addresses_are_refused_inside_a_capture():
+    gpu_util.ensure_library()
+    n = 5000
+    p = torch.zeros(n, device="cuda")
+    a, b, c = (torch.full((n,), x, device="cuda") for x in (1.0, 2.0, 4.0))
+    opt, norm = training.AdamW([p], [a], weight_decay=0.0), training.GradNorm([a])
+    out = torch.zeros(2, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for holder in (opt, norm):
+            with pytest.raises(binding.PsopsError) as e:
+                holder.set_grads([b])
+            assert e.value.code == binding.PSOPS_ESTATE
+        norm.norm(1.0, out=out)
+        opt.step(1e-2)
+    graph.replay()
+    assert float(out[0]) == pytest.approx(n ** 0.5, rel=1e-6) and opt.steps == 1
+    norm.set_grads([c]), opt.set_grads([c])             # outside, and the graph reads them from then on
+    graph.replay()
+    assert float(out[0]) == pytest.approx(4 * n ** 0.5, rel=1e-6) and opt.steps == 2
+    assert opt.grads[0] is c and norm.grads[0] is c
+    del graph
+    opt.close(), norm.close()
