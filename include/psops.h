@@ -369,9 +369,12 @@ int psops_destroy(psops_ctx *ctx);
  * context's stream, a context bound to the GPU current at creation and used by
  * one host thread at a time.  All of them are deterministic: the same inputs
  * give the same bits.  psops_*_set_stream moves a context to another stream of
- * its GPU: what it enqueues there comes after what it has enqueued so far (but
- * into a capturing stream no such wait can be recorded: order the streams
- * before the capture).  Arrays written on yet other streams are the caller's to
+ * its GPU: what it enqueues there comes after what it has enqueued so far (also
+ * from one branch of a capture to another, but not into a capture or out of one,
+ * where no such wait can be recorded: order the streams before the capture).  A
+ * captured graph uses its context's workspace whenever it is replayed: order
+ * replays and other calls of the context, and keep context and workspace for as
+ * long as the graph.  Arrays written on yet other streams are the caller's to
  * order, as for any kernel.  psops_*_destroy frees the context also where it
  * returns an error.
  * ---------------------------------------------------------------------------

@@ -92,9 +92,11 @@ inline int set_stream(Base *b, void *cuda_stream)
     if (to == b->stream) return PSOPS_OK;
     OnDevice guard(b);
     cudaStreamCaptureStatus from_capture = cudaStreamCaptureStatusNone, to_capture = cudaStreamCaptureStatusNone;
-    PSOPS_TRY(b, cudaStreamIsCapturing(to, &to_capture));
-    PSOPS_TRY(b, cudaStreamIsCapturing(b->stream, &from_capture));
-    if (to_capture == cudaStreamCaptureStatusNone && from_capture == cudaStreamCaptureStatusNone) {
+    unsigned long long from_id = 0, to_id = 0;
+    PSOPS_TRY(b, cudaStreamGetCaptureInfo(to, &to_capture, &to_id));
+    PSOPS_TRY(b, cudaStreamGetCaptureInfo(b->stream, &from_capture, &from_id));
+    // both outside captures, or two branches of one
+    if (to_capture == from_capture && (to_capture == cudaStreamCaptureStatusNone || to_id == from_id)) {
         if (b->moved == nullptr) PSOPS_TRY(b, cudaEventCreateWithFlags(&b->moved, cudaEventDisableTiming));
         PSOPS_TRY(b, cudaEventRecord(b->moved, b->stream));
         PSOPS_TRY(b, cudaStreamWaitEvent(to, b->moved, 0));

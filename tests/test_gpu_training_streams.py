@@ -246,3 +246,33 @@ def test_new_gradient_addresses_are_refused_inside_a_capture():
     assert opt.grads[0] is c and norm.grads[0] is c
     del graph
     opt.close(), norm.close()
+
+
+def test_calls_on_two_branches_of_one_capture_come_after_one_another():
+    h, w, y = _inputs(2000, 128, 3000)
+    h2 = (h.float() * 0.5).bfloat16()
+    one = torch.ones((), device="cuda")
+    op = training.LinearXent(2000, 128, 3000)
+
+    def both(x):
+        loss, rows, lse = op.forward(x, w, y)
+        return loss, rows, lse, *op.backward(x, w, y, lse, one, rows=rows)
+
+    want = [both(x) for x in (h, h2, h, h2)]
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=first):
+        second.wait_stream(first)                        # the branch: nothing else orders the two
+        got = []
+        for k, x in enumerate((h, h2, h, h2)):
+            with torch.cuda.stream((first, second)[k % 2]):
+                got.append(both(x))
+        first.wait_stream(second)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for s, t in zip(a, b):
+            assert torch.equal(s, t)
+    op.close()
+    del graph
