@@ -21,7 +21,8 @@ using psops_host::round_up;
 
 namespace {
 
-// Bytes that the logits' gradients of one piece of the vocabulary may take.
+// Bytes that the logits' gradients of one piece of the vocabulary may take, and
+// those of its rows of w (and of dw) that pass through the workspace.
 constexpr int64_t kPieceBytes = 512ll << 20;
 constexpr int64_t kMinPiece = 2048;
 // Pairs of CTAs that run at once on a B200 (148 SMs), where a layout must not ask the GPU.
@@ -59,8 +60,9 @@ Layout make_layout(const psops_xent_config *c)
     L.rows = (int64_t)round_up((size_t)c->max_tokens, kTileRows);
     L.padded = (int64_t)round_up((size_t)c->dim, 64);
     const int64_t whole = (int64_t)round_up((size_t)c->vocab, kTileCols);
-    L.piece = std::min(whole, std::max(kMinPiece, kPieceBytes / (2 * L.rows) / kTileCols * kTileCols));
     L.staged = c->dim % 8 != 0 || (c->flags & PSOPS_XENT_STAGED) != 0;
+    const int64_t widest = L.staged ? std::max(L.rows, L.padded) : L.rows;
+    L.piece = std::min(whole, std::max(kMinPiece, kPieceBytes / (2 * widest) / kTileCols * kTileCols));
     L.parts = whole / kHalf;
     L.sum_rows = L.rows * std::max<int64_t>(1, std::min<int64_t>(kMostShares, kShareBytes / (4 * L.rows * L.padded)));
     size_t at = 0;
