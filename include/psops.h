@@ -374,9 +374,9 @@ int psops_destroy(psops_ctx *ctx);
  * where no such wait can be recorded: order the streams before the capture).  A
  * captured graph uses its context's workspace whenever it is replayed: order
  * replays and other calls of the context, and keep context and workspace for as
- * long as the graph.  Arrays written on yet other streams are the caller's to
- * order, as for any kernel.  psops_*_destroy frees the context also where it
- * returns an error.
+ * long as the graph.  Contexts are created outside captures (else ESTATE).
+ * Arrays written on yet other streams are the caller's to order, as for any
+ * kernel.  psops_*_destroy frees the context also where it returns an error.
  * ---------------------------------------------------------------------------
  */
 
@@ -467,7 +467,7 @@ int psops_adamw_set_grads(psops_adamw *opt, const void *const *grads);
  */
 int psops_adamw_step(psops_adamw *opt, double lr, const float *d_scale);
 
-/* t, read from the device (waits for the stream). */
+/* t, read from the device (waits for the stream; ESTATE inside a stream capture). */
 int psops_adamw_steps(psops_adamw *opt, int64_t *steps);
 
 int psops_adamw_set_stream(psops_adamw *opt, void *cuda_stream);

@@ -105,8 +105,9 @@ inline int set_stream(Base *b, void *cuda_stream)
     return PSOPS_OK;
 }
 
-// A table that is sent from the staging below cannot be part of a captured graph:
-// every replay would send what the staging holds by then.
+// What must not become part of a captured graph: a table that is sent from the
+// staging below (every replay would send what the staging holds by then), the
+// setting up of a context (it would be done at the replay only), a wait for the host.
 inline int not_capturing(Base *b)
 {
     cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;

@@ -142,7 +142,7 @@ int open_base(Base *b, void *stream)
     if (cudaGetDevice(&b->device) != cudaSuccess ||
         cudaDeviceGetAttribute(&b->sms, cudaDevAttrMultiProcessorCount, b->device) != cudaSuccess)
         return PSOPS_ECUDA;
-    return PSOPS_OK;
+    return psops_host::not_capturing(b);
 }
 
 // Blocks of a persistent launch: no more than run at once, and as many as have
@@ -303,6 +303,8 @@ int psops_adamw_steps(psops_adamw *a, int64_t *steps)
 {
     if (a == nullptr || steps == nullptr) return PSOPS_EINVAL;
     OnDevice guard(a);
+    const int rc = psops_host::not_capturing(a);
+    if (rc != PSOPS_OK) return rc;
     AdamwState s;
     PSOPS_TRY(a, cudaMemcpyAsync(&s, a->state, sizeof(s), cudaMemcpyDeviceToHost, a->stream));
     PSOPS_TRY(a, cudaStreamSynchronize(a->stream));

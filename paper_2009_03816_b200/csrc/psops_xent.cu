@@ -487,6 +487,11 @@ int psops_xent_create(psops_xent **out, const psops_xent_config *cfg, void *d_wo
     x->lay = lay;
     x->ws = (char *)d_workspace;
     x->stream = (cudaStream_t)cuda_stream;
+    const int rc = psops_host::not_capturing(x);
+    if (rc != PSOPS_OK) {
+        delete x;
+        return rc;
+    }
     cudaError_t e = cudaGetDevice(&x->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&x->sms, cudaDevAttrMultiProcessorCount, x->device);
     cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;

@@ -472,6 +472,7 @@ class AdamW(_Holder):
     @property
     def steps(self) -> int:
         """Steps taken so far (waits for the stream)."""
+        self._follow()
         return binding.psops_adamw_steps(self.ctx)
 
 

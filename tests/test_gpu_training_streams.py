@@ -276,3 +276,23 @@ def test_calls_on_two_branches_of_one_capture_come_after_one_another():
             assert torch.equal(s, t)
     op.close()
     del graph
+
+
+def test_setting_up_and_waiting_are_refused_inside_a_capture():
+    h, w, y = _inputs(60, 64, 40)
+    p, g = torch.zeros(100, device="cuda"), torch.ones(100, device="cuda")
+    opt = training.AdamW([p], [g], weight_decay=0.0)
+    graph = torch.cuda.CUDAGraph()
+    refused = [lambda: training.LinearXent(60, 64, 40), lambda: training.AdamW([p], [g], moments=([g.clone()], [g.clone()])),
+               lambda: training.GradNorm([g]), lambda: opt.steps]
+    with torch.cuda.graph(graph):
+        for k, f in enumerate(refused):
+            with pytest.raises(binding.PsopsError) as e:
+                f()
+            assert e.value.code == binding.PSOPS_ESTATE, k
+        opt.step(1e-2)
+    for _ in range(3):
+        graph.replay()
+    assert opt.steps == 3 and bool((p < -0.0299).all())
+    del graph
+    opt.close()
