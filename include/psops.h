@@ -518,16 +518,17 @@ int psops_gradnorm_destroy(psops_gradnorm *gn);
  *
  * Rounding: products are summed in fp32, softmax statistics are fp32, the loss
  * is summed in double.  The tensor cores cut sums off where fp32 would round to
- * nearest; they add up at most 768 terms of a logit and 8,192 of dh or dw before
- * fp32 registers take over, which keeps dh and dw within 6e-5 of their value,
- * whatever the length of the sum.  dlogits enters the two gradient products rounded to
+ * nearest; they add up at most 768 terms of a logit and 8,192 of dh or dw in one
+ * go, fp32 additions do the rest: 6e-5 of the largest partial sum at most in dh and
+ * dw, however long the sum.  dlogits enters the two gradient products rounded to
  * the 16-bit type (that is what the tensor cores multiply), scaled by a power
  * of two that keeps small probabilities inside fp16's range; dh and dw are
  * rounded to the 16-bit type once, at the end.
  * Rows: row t of h, w, dh, dw starts at t * its stride (in elements, at least
  * dim).  dim a multiple of 8 with 16-byte aligned rows of w is read in place;
  * any other w, and any other dw, passes through the workspace
- * (PSOPS_XENT_STAGED).
+ * (PSOPS_XENT_STAGED), 512 MB of rows of each at a time.  dh and dw must not
+ * overlap the inputs.
  * Should a product on the tensor cores ever wait in vain for its operands (four
  * seconds), the loss, the rows and lse of the tokens that count, dh and dw of
  * that call, and of every later call of the context that runs there, are NaN.

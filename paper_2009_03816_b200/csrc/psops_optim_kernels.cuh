@@ -339,9 +339,9 @@ template <int BITS> constexpr int kAdamwBlocks = BITS == 8 ? 4 : 3;
 
 // One step of AdamW (the formula is in psops.h).  What bounds it is HBM
 // traffic: 28 bytes per element with fp32 moments and gradients (204 M elements
-// of 1,288 tensors: 863 us, 6.63 TB/s, what a plain copy reaches); 14 to 16 with
-// 8-bit moments and 16-bit gradients, where the instructions weigh as much
-// (268 M of 291 tensors with bf16 copies: 826 us, 5.2 TB/s).  Keeping the next
+// of 1,288 tensors: 850 to 877 us, 6.5 to 6.7 TB/s, what a plain copy reaches);
+// 14 to 16 with 8-bit moments and 16-bit gradients, where the instructions weigh
+// as much (268 M of 291 tensors with bf16 copies: 797 to 839 us, 5.1 to 5.4 TB/s).  Keeping the next
 // group's loads in registers under the arithmetic was slower (its registers cost
 // more warps than the overlap gave: 473 us against 378 us for 134 M elements).
 template <int BITS, class G, class C>

@@ -332,6 +332,9 @@ struct ProductParams {
     float *label_logit;
 };
 
+// 32 bits, approximate: off by some units in the last place of the result, numbers
+// below 2^-126 as zero.  A probability's error from its logit, 16 times 2^-24 and
+// more, is larger, and one below 2^-126 adds nothing to a sum that has a 1 in it.
 __device__ __forceinline__ float exp2_fast(float x)
 {
     float y;

@@ -257,9 +257,10 @@ __global__ void __launch_bounds__(kHeadDwThreads) psops_xent_head_dw_kernel(cons
 // Up to 4 tokens against the whole vocabulary: bound by reading w once.  The
 // hidden states lie in shared memory as fp32; every warp has an equal share of
 // w's rows and takes four at a time; lane t keeps the softmax of token t.
-// Measured with 268 MB of w (32,768 x 4,096): 1 / 2 / 4 tokens 47 / 51 / 59 us
-// (5.7 TB/s down to 4.6) where the tensor-core form takes 62 us whatever their
-// number; 8 tokens took 91 us, so from 5 on the tensor cores do it.
+// Measured with 268 MB of w (32,768 x 4,096): 1 / 2 / 4 tokens 47 to 53 / 51 to 56
+// / 59 to 62 us by the box (5.7 TB/s down to 4.3) where the tensor-core form takes
+// 62 to 65 us whatever their number; 8 tokens took 91 us, so from 5 on the tensor
+// cores do it.
 constexpr int kFewTokens = 4, kFewRows = 4, kFewBlocks = 2;          // blocks of an SM
 // Pieces of a row (512 bytes) on their way under the arithmetic: four where the registers are there.
 template <int N> constexpr int kFewAhead = N == 1 ? 4 : 2;
