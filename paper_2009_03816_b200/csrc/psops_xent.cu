@@ -537,7 +537,7 @@ int psops_xent_forward(psops_xent *x, const void *d_h, int64_t h_ld, const void 
         H.lse_out = d_lse;
         return half ? forward_head<__half>(x, H) : forward_head<__nv_bfloat16>(x, H);
     }
-    if (is_few(tokens, x->cfg.dim)) {
+    if (is_few(tokens, x->cfg.dim) && few_loss_pays(x->cfg.dim, x->cfg.vocab)) {
         FewParams F{};
         F.h = (const uint16_t *)d_h; F.h_ld = h_ld; F.h_aligned = aligned16(d_h, h_ld);
         F.w = (const uint16_t *)d_w; F.w_ld = w_ld; F.w_aligned = aligned16(d_w, w_ld);

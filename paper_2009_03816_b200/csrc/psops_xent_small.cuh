@@ -260,7 +260,14 @@ __global__ void __launch_bounds__(kHeadDwThreads) psops_xent_head_dw_kernel(cons
 // Measured with 268 MB of w (32,768 x 4,096): 1 / 2 / 4 tokens 47 to 53 / 51 to 56
 // / 59 to 62 us by the box (5.7 TB/s down to 4.3) where the tensor-core form takes
 // 62 to 65 us whatever their number; 8 tokens took 91 us, so from 5 on the tensor
-// cores do it.
+// cores do it.  With short rows a warp's turn is mostly its reductions: four tokens in
+// a CUDA graph, this form / the tensor cores, us, by dim x entries:
+//          8,192        32,768       65,536       131,072
+//   64     9.0 / 15     17 / 16      25 / 20      42 / 28
+//   61     10 / 17      21 / 18      33 / 23      58 / 34
+//   192    9.4 / 16     17 / 17      25 / 21      42 / 32
+//   320    9.8 / 17     18 / 18      25 / 24      43 / 37
+//   512    9.8 / 18     18 / 21      26 / 27      43 / 45
 constexpr int kFewTokens = 4, kFewRows = 4, kFewBlocks = 2;          // blocks of an SM
 // Pieces of a row (512 bytes) on their way under the arithmetic: four where the registers are there.
 template <int N> constexpr int kFewAhead = N == 1 ? 4 : 2;
@@ -269,6 +276,7 @@ constexpr int kFewShared = 96 * 1024;
 inline int few_of(int64_t tokens) { return tokens <= 1 ? 1 : tokens <= 2 ? 2 : 4; }
 inline size_t few_shared(int64_t tokens, int64_t dim) { return 4ull * (size_t)few_of(tokens) * (size_t)((dim + 255) / 256 * 256); }
 inline bool is_few(int64_t tokens, int64_t dim) { return tokens >= 1 && tokens <= kFewTokens && dim <= kFewShared / 4 && few_shared(tokens, dim) <= (size_t)kFewShared; }
+inline bool few_loss_pays(int64_t dim, int64_t vocab) { return dim > 320 || vocab <= 1 << 15; }
 
 struct FewParams {
     const uint16_t *h, *w;

@@ -60,3 +60,17 @@ def test_few_classes_take_the_form_that_was_faster(T, D, V, loss, grads):
 def test_values_of_few_classes_on_both_sides(T, D, V, dtype):
     _run(T, D, V, dtype, seed=83)
     _run(T, D, V, dtype, seed=84, masked=0.4, reduction="sum")
+
+
+# the loss of few tokens in its own form: one launch
+@pytest.mark.parametrize("T,D,V,own", [(1, 4096, 32_768, True), (4, 64, 32_768, True), (4, 64, 65_536, False), (1, 320, 40_000, False),
+                                       (4, 512, 131_072, True)])
+def test_the_loss_of_few_tokens_takes_the_form_that_was_faster(T, D, V, own):
+    assert (_launches(T, D, V)[0] == 1) == own
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,D,V", [(1, 61, 32_768), (4, 61, 32_769), (2, 320, 33_000), (3, 321, 33_000)])
+def test_values_of_the_loss_of_few_tokens_on_both_sides(T, D, V, dtype):
+    _run(T, D, V, dtype, seed=85)
+    _run(T, D, V, dtype, seed=86, masked=0.4, reduction="sum")
