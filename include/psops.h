@@ -584,6 +584,98 @@ int64_t psops_xent_launch_count(const psops_xent *x);
 const char *psops_xent_last_error(const psops_xent *x);
 int psops_xent_destroy(psops_xent *x);
 
+/*
+ * Causal attention over packed sequences, with grouped heads and, if wanted, a
+ * learned bias by buckets of the distance.  q: tokens x heads x dim; k and v:
+ * tokens x kv_heads x dim; query head h reads key head h / (heads / kv_heads).
+ * Sequence b is tokens offsets[b] .. offsets[b + 1] - 1.  Within a sequence, for
+ * j <= i:
+ *   x[i, j] = scale * (q_i . k_j) + bias[bucket(i - j), h]
+ *   lse_i   = log sum_j exp(x[i, j])
+ *   out_i   = sum_j exp(x[i, j] - lse_i) v_j
+ * and from the gradient of out
+ *   dv_j = sum_i p[i, j] do_i,   ds[i, j] = p[i, j] (do_i . v_j - do_i . out_i)
+ *   dq_i = scale * sum_j ds[i, j] k_j,   dk_j = scale * sum_i ds[i, j] q_i
+ *   dbias[b, h] = sum of ds[i, j] over all pairs with bucket(i - j) = b
+ * dk and dv are summed over the heads that share them.  bucket(d) is the b with
+ * first[b] <= d < first[b + 1]; the last bucket has no end.  Neither scores nor
+ * probabilities are kept.
+ *
+ * A row reads nothing of another sequence, of later tokens or of tokens of no
+ * sequence, whatever these hold (NaN and infinities included).  A bias below
+ * -1e30 (the lowest number of a type, -inf) takes its pairs out; a row that is
+ * left with no pair, or whose scores are all -inf, has out 0, lse -inf and no
+ * gradient.  Sequences may be empty.  Rows of no sequence (in front of the first,
+ * behind the last) are left as they were in all results, or become zeros if
+ * zero_rest is not 0.
+ *
+ * Rounding: products are summed in fp32 by the tensor cores, softmax statistics
+ * are fp32.  The tensor cores multiply 16-bit numbers: p and ds enter their
+ * second products rounded to the type of q.  In fp16, p is kept scaled by a
+ * power of two, and ds by one that the largest norms of the rows of do and v
+ * allow, so that small ones keep their digits; results are rounded once, at the
+ * end.  delta = do . out is taken from out as it was rounded.
+ * Should a product ever wait in vain for its operands (four seconds), the
+ * results of its tile are NaN.
+ */
+#define PSOPS_ATTENTION_GRADS  1u   /* reserve workspace for psops_attention_backward           */
+
+typedef struct {
+    int64_t  max_tokens;     /* most tokens of a call, 1 .. 2^24                       */
+    int32_t  max_sequences;  /* most sequences of a call, 1 .. 2^24                    */
+    int32_t  heads;          /* 1 .. 1024                                              */
+    int32_t  kv_heads;       /* divides heads                                          */
+    int32_t  dim;            /* of a head: a multiple of 8, 8 .. 128                   */
+    int32_t  type;           /* PSOPS_F16 or PSOPS_BF16: q, k, v, out, gradients       */
+    int32_t  buckets;        /* of the bias, 0 (no bias) .. 64                         */
+    const int32_t *first;    /* host: first distance of each bucket, ascending from 0,
+                                the last at most 1024; copied                          */
+    float    scale;          /* > 0                                                    */
+    uint32_t flags;
+} psops_attention_config;
+
+/* tokens x heads x dim: the dim elements of a head are consecutive, strides in
+ * elements.  Rows have to be 16-byte aligned (strides multiples of 8); in results
+ * they must not overlap. */
+typedef struct {
+    void    *p;
+    int64_t  token_stride, head_stride;
+} psops_heads;
+
+typedef struct psops_attention psops_attention;  /* opaque */
+
+size_t psops_attention_workspace_bytes(const psops_attention_config *cfg);
+int psops_attention_create(psops_attention **out, const psops_attention_config *cfg, void *d_workspace, size_t workspace_bytes,
+                           void *cuda_stream);
+
+/*
+ * d_offsets: sequences + 1 device numbers that do not decrease, from >= 0 to
+ * <= tokens (they are read on the device; others are cut to that range, and a
+ * sequence that ends before it begins is empty).  d_bias: buckets x heads, of
+ * bias_type PSOPS_F32 or the type of q; NULL without buckets.  d_lse: heads x
+ * tokens.  0 <= tokens <= max_tokens, 0 <= sequences <= max_sequences.
+ * Errors: EINVAL, EALIGN, ECUDA.
+ */
+int psops_attention_forward(psops_attention *a, const psops_heads *q, const psops_heads *k, const psops_heads *v,
+                            const int32_t *d_offsets, int32_t sequences, int64_t tokens, const void *d_bias, int32_t bias_type,
+                            const psops_heads *out, float *d_lse, int32_t zero_rest);
+
+/*
+ * Gradients, from the inputs and results of psops_attention_forward and the
+ * gradient of out.  dq, dk, dv, d_dbias (buckets x heads, of bias_type) may be
+ * NULL (not wanted).  All are overwritten, not added to, and must not overlap the
+ * inputs.  Errors: as forward, and ESTATE without PSOPS_ATTENTION_GRADS.
+ */
+int psops_attention_backward(psops_attention *a, const psops_heads *q, const psops_heads *k, const psops_heads *v,
+                             const int32_t *d_offsets, int32_t sequences, int64_t tokens, const void *d_bias, int32_t bias_type,
+                             const psops_heads *out, const float *d_lse, const psops_heads *grad, const psops_heads *dq,
+                             const psops_heads *dk, const psops_heads *dv, void *d_dbias, int32_t zero_rest);
+
+int psops_attention_set_stream(psops_attention *a, void *cuda_stream);
+int64_t psops_attention_launch_count(const psops_attention *a);
+const char *psops_attention_last_error(const psops_attention *a);
+int psops_attention_destroy(psops_attention *a);
+
 #ifdef __cplusplus
 }
 #endif

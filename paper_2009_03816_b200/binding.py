@@ -26,6 +26,7 @@ PSOPS_X, PSOPS_V, PSOPS_PBEST, PSOPS_GBEST = 0, 1, 2, 3
 PSOPS_NONE, PSOPS_F32, PSOPS_F16, PSOPS_BF16 = 0, 1, 2, 3
 PSOPS_MEAN, PSOPS_SUM, PSOPS_PER_TOKEN = 0, 1, 2
 PSOPS_XENT_GRADS, PSOPS_XENT_STAGED = 1, 2
+PSOPS_ATTENTION_GRADS = 1
 
 EXPORTS = [
     "psops_workspace_bytes", "psops_create", "psops_set_losses", "psops_sync",
@@ -44,6 +45,9 @@ EXPORTS = [
     "psops_gradnorm_destroy",
     "psops_xent_workspace_bytes", "psops_xent_create", "psops_xent_forward", "psops_xent_backward",
     "psops_xent_set_stream", "psops_xent_launch_count", "psops_xent_last_error", "psops_xent_destroy",
+    "psops_attention_workspace_bytes", "psops_attention_create", "psops_attention_forward", "psops_attention_backward",
+    "psops_attention_set_stream", "psops_attention_launch_count", "psops_attention_last_error",
+    "psops_attention_destroy",
 ]
 
 
@@ -69,6 +73,17 @@ class psops_adamw_tensor(ctypes.Structure):
 class psops_xent_config(ctypes.Structure):
     _fields_ = [("max_tokens", ctypes.c_int64), ("dim", ctypes.c_int64), ("vocab", ctypes.c_int64),
                 ("type", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class psops_attention_config(ctypes.Structure):
+    _fields_ = [("max_tokens", ctypes.c_int64), ("max_sequences", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("dim", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("buckets", ctypes.c_int32), ("first", ctypes.POINTER(ctypes.c_int32)), ("scale", ctypes.c_float),
+                ("flags", ctypes.c_uint32)]
+
+
+class psops_heads(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class PsopsError(RuntimeError):
@@ -97,6 +112,7 @@ def load() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIBRARY)
     cfgp = ctypes.POINTER(psops_config)
     xcfgp = ctypes.POINTER(psops_xent_config)
+    tcfgp, hp = ctypes.POINTER(psops_attention_config), ctypes.POINTER(psops_heads)
     acfgp, atensp = ctypes.POINTER(psops_adamw_config), ctypes.POINTER(psops_adamw_tensor)
     sig = {
         "psops_workspace_bytes": (ctypes.c_size_t, [cfgp]),
@@ -161,6 +177,16 @@ def load() -> ctypes.CDLL:
         "psops_xent_launch_count": (ctypes.c_int64, [_vp]),
         "psops_xent_last_error": (ctypes.c_char_p, [_vp]),
         "psops_xent_destroy": (ctypes.c_int, [_vp]),
+        "psops_attention_workspace_bytes": (ctypes.c_size_t, [tcfgp]),
+        "psops_attention_create": (ctypes.c_int, [ctypes.POINTER(_vp), tcfgp, _vp, ctypes.c_size_t, _vp]),
+        "psops_attention_forward": (ctypes.c_int, [_vp, hp, hp, hp, _vp, ctypes.c_int32, ctypes.c_int64, _vp,
+                                                   ctypes.c_int32, hp, _f32p, ctypes.c_int32]),
+        "psops_attention_backward": (ctypes.c_int, [_vp, hp, hp, hp, _vp, ctypes.c_int32, ctypes.c_int64, _vp,
+                                                    ctypes.c_int32, hp, _f32p, hp, hp, hp, hp, _vp, ctypes.c_int32]),
+        "psops_attention_set_stream": (ctypes.c_int, [_vp, _vp]),
+        "psops_attention_launch_count": (ctypes.c_int64, [_vp]),
+        "psops_attention_last_error": (ctypes.c_char_p, [_vp]),
+        "psops_attention_destroy": (ctypes.c_int, [_vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)            # AttributeError if a symbol is missing
@@ -475,6 +501,49 @@ def psops_xent_launch_count(x) -> int:
 
 def psops_xent_destroy(x) -> None:
     _check(load().psops_xent_destroy(x), "psops_xent_destroy")
+
+
+def psops_attention_workspace_bytes(cfg: psops_attention_config) -> int:
+    return int(load().psops_attention_workspace_bytes(ctypes.byref(cfg)))
+
+
+def psops_attention_create(cfg, d_workspace, workspace_bytes=None, stream=None):
+    handle = _vp()
+    if workspace_bytes is None:
+        workspace_bytes = d_workspace.numel() * d_workspace.element_size() if d_workspace is not None else 0
+    rc = load().psops_attention_create(ctypes.byref(handle), ctypes.byref(cfg), _ptr(d_workspace), int(workspace_bytes),
+                                       int(stream) if stream else None)
+    _check(rc, "psops_attention_create")
+    return handle
+
+
+def psops_attention_forward(a, q, k, v, d_offsets, sequences, tokens, d_bias, bias_type, out, d_lse, zero_rest) -> None:
+    """q, k, v, out: psops_heads."""
+    _check(load().psops_attention_forward(a, q, k, v, _ptr(d_offsets), int(sequences), int(tokens), _ptr(d_bias),
+                                          int(bias_type), out, _ptr(d_lse), int(zero_rest)),
+           "psops_attention_forward", a, "psops_attention_last_error")
+
+
+def psops_attention_backward(a, q, k, v, d_offsets, sequences, tokens, d_bias, bias_type, out, d_lse, grad, dq, dk, dv,
+                             d_dbias, zero_rest) -> None:
+    """q, k, v, out, grad and, where not None, dq, dk, dv: psops_heads."""
+    _check(load().psops_attention_backward(a, q, k, v, _ptr(d_offsets), int(sequences), int(tokens), _ptr(d_bias),
+                                           int(bias_type), out, _ptr(d_lse), grad, dq, dk, dv, _ptr(d_dbias),
+                                           int(zero_rest)),
+           "psops_attention_backward", a, "psops_attention_last_error")
+
+
+def psops_attention_set_stream(ctx, stream) -> None:
+    _check(load().psops_attention_set_stream(ctx, int(stream) if stream else None), "psops_attention_set_stream", ctx,
+           "psops_attention_last_error")
+
+
+def psops_attention_launch_count(a) -> int:
+    return int(load().psops_attention_launch_count(a))
+
+
+def psops_attention_destroy(a) -> None:
+    _check(load().psops_attention_destroy(a), "psops_attention_destroy")
 
 
 # ---- convenience holder of the tensors a context borrows ------------------

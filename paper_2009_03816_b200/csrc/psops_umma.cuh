@@ -54,6 +54,10 @@ __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void barrier_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ void barrier_arrive_at(uint32_t cluster_bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
@@ -108,6 +112,13 @@ __device__ __forceinline__ void tensor_load(uint32_t dst, const CUtensorMap *map
                      "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar)
                      : "memory");
 }
+// The same from an array of three axes, into this CTA's own shared memory.
+__device__ __forceinline__ void tensor_load3(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
 __device__ __forceinline__ void tensor_store(const CUtensorMap *map, int x, int y, uint32_t src)
 {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src)
@@ -133,6 +144,18 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volat
 
 // ---- tensor memory -----------------------------------------------------------
 constexpr uint32_t kTensorColumns = 512;
+// COLUMNS of them for this CTA alone; two CTAs share an SM if both take half.
+template <uint32_t COLUMNS>
+__device__ __forceinline__ void tensor_columns_take(uint32_t where)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(where), "n"(COLUMNS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+template <uint32_t COLUMNS>
+__device__ __forceinline__ void tensor_columns_give(uint32_t base)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(base), "n"(COLUMNS));
+}
 template <bool PAIR>
 __device__ __forceinline__ void tensor_memory_take(uint32_t where)
 {
@@ -168,6 +191,24 @@ __device__ __forceinline__ void tensor_memory_load16(uint32_t address, uint32_t 
                    "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(address));
 }
+// 16 or 32 columns of this warp's 32 lanes, written.
+__device__ __forceinline__ void tensor_memory_store16(uint32_t address, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(address),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+__device__ __forceinline__ void tensor_memory_store(uint32_t address, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(address),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+                 "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+                 : "memory");
+}
+__device__ __forceinline__ void tensor_memory_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // The loads above are complete; their N registers are tied to this point, so
 // that nothing the compiler does with them can move in front of it.
 template <int N>
@@ -184,12 +225,13 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 // Operands lie in shared memory in rows of 128 bytes, 128-byte swizzle, groups
 // of 8 rows 1024 bytes apart.  Where the summed axis runs along the rows
 // ("k along"), rows are the other axis.  Where it runs across them, a row holds
-// 64 elements of the other axis, and the next 64 elements lie `kAcross` bytes on.
+// 64 elements of the other axis, and the next 64 elements lie `across` bytes on
+// (kAcross in tiles of 64 rows).
 constexpr uint32_t kAcross = 8192;
-__device__ __forceinline__ uint64_t operand(uint32_t address, bool k_across)
+__device__ __forceinline__ uint64_t operand(uint32_t address, bool k_across, uint32_t across = kAcross)
 {
     uint64_t d = (uint64_t)((address & 0x3ffffu) >> 4);
-    d |= (uint64_t)(k_across ? kAcross >> 4 : 1u) << 16;     // from one 64-element column of rows to the next
+    d |= (uint64_t)(k_across ? across >> 4 : 1u) << 16;     // from one 64-element column of rows to the next
     d |= (uint64_t)(1024u >> 4) << 32;                       // from one group of 8 rows to the next
     d |= (uint64_t)1 << 46;                                  // descriptor version of sm_100
     d |= (uint64_t)2 << 61;                                  // 128-byte swizzle
@@ -212,6 +254,13 @@ __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uin
         asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
                      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(instr), "r"((uint32_t)add)
                      : "memory");
+}
+// The same with A in tensor memory: row i of A in lane i, two elements of the summed axis in a column.
+__device__ __forceinline__ void multiply_from_tensor_memory(uint32_t d, uint32_t a, uint64_t b, uint32_t instr, bool add)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(instr), "r"((uint32_t)add)
+                 : "memory");
 }
 // When the products issued so far are done: arrive at this barrier, of both CTAs of a pair.
 template <bool PAIR>

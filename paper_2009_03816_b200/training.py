@@ -7,6 +7,8 @@ computation runs in the CUDA library.
 
   LinearXent   softmax cross entropy of a linear head without keeping the logits,
                with its gradients; its loss alone is a worker's fitness
+  Attention    causal attention over packed sequences, with grouped heads and a learned
+               bias by buckets of the distance, with its gradients
   AdamW        one AdamW step over many tensors, moments in 32 or in 8 bits
   GradNorm     2-norm of many gradients and the factor that clips it
 
@@ -22,12 +24,13 @@ caller, as for any kernel.
 """
 from __future__ import annotations
 
+import ctypes
 import math
 
 import torch
 
 from . import binding
-from .binding import (PSOPS_BF16, PSOPS_EINVAL, PSOPS_ESTATE, PSOPS_F16, PSOPS_F32, PSOPS_MEAN, PSOPS_NONE,
+from .binding import (PSOPS_ATTENTION_GRADS, PSOPS_BF16, PSOPS_EINVAL, PSOPS_ESTATE, PSOPS_F16, PSOPS_F32, PSOPS_MEAN, PSOPS_NONE,
                       PSOPS_PER_TOKEN, PSOPS_SUM, PSOPS_XENT_GRADS, PSOPS_XENT_STAGED, PsopsError)
 
 _TYPES = {torch.float32: PSOPS_F32, torch.float16: PSOPS_F16, torch.bfloat16: PSOPS_BF16}
@@ -75,7 +78,7 @@ def _is_capturing(stream):
 
 
 class _Holder:
-    """What the three have in common: a context, its GPU and the stream its work goes to."""
+    """What the holders have in common: a context, its GPU and the stream its work goes to."""
 
     ctx = None
 
@@ -360,8 +363,216 @@ class _FirstOrderOnly(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
-        raise RuntimeError("LinearXent: gradients are of the first order only (once_differentiable); a function of them "
+        raise RuntimeError("LinearXent, Attention: gradients are of the first order only (once_differentiable); a function of them "
                            "cannot be differentiated")
+
+
+def distance_buckets(count, far):
+    """The first distance of each of `count` buckets: the lower half holds one distance each, the others grow by a
+    common ratio up to `far`, and the last holds all that is farther."""
+    count, far = int(count), int(far)
+    near = count // 2
+    if not 1 <= count <= 64 or not count <= far <= 1024:
+        _refuse("distance_buckets", f"{count} buckets up to {far}: 1 to 64, and no more than distances, 1024 at most")
+    first = list(range(near))
+    for k in range(count - near):
+        # the smallest d with (d / near)^(count - near) >= (far / near)^k, in whole numbers
+        d = near
+        if near:
+            low, high, n = near, far, count - near
+            while low < high:
+                mid = (low + high) // 2
+                if mid ** n * near ** k >= far ** k * near ** n:
+                    high = mid
+                else:
+                    low = mid + 1
+            d = low
+        first.append(max(d, first[-1] + 1) if first else 0)
+    return first
+
+
+class Attention(_Holder):
+    """Causal attention over packed sequences.
+
+    tokens, sequences       the most of a call
+    heads, kv_heads, dim    query heads, key heads (a divisor of them) and elements of a head (a multiple of 8, to 128)
+    dtype                   torch.bfloat16 or torch.float16, the type of q, k and v
+    buckets                 None, or the first distance of each bucket of a learned bias, ascending from 0 (such as
+                            :func:`distance_buckets` gives)
+    scale                   of the products of q and k, 1 / sqrt(dim) if not given
+    gradients               False: no workspace for backward
+
+    q is tokens x heads x dim, k and v are tokens x kv_heads x dim, with consecutive elements in each head and rows on
+    multiples of 16 bytes (views of one projection's output, for instance); `offsets` (int32, on the GPU, one more than
+    there are sequences) has each sequence's first token, and behind the last one its end; `bias` is buckets x heads, fp32
+    or of q's type.  Rows of no sequence are zeros in results that a call makes, and left as they were in given ones.
+    Calling the object gives the output as a torch value with gradients (of the first order)::
+
+        out = attention(q, k, v, offsets, bias)
+    """
+
+    _set_stream = staticmethod(binding.psops_attention_set_stream)
+    _launch_count = staticmethod(binding.psops_attention_launch_count)
+    _destroy = staticmethod(binding.psops_attention_destroy)
+
+    def __init__(self, tokens, sequences, heads, kv_heads, dim, *, dtype=torch.bfloat16, buckets=None, scale=None,
+                 device="cuda", gradients=True, stream=None):
+        device = torch.device(device)
+        if device.type != "cuda":
+            _refuse("Attention", "needs a GPU")
+        if dtype not in (torch.float16, torch.bfloat16):
+            _refuse("Attention", f"q, k and v of {dtype}: torch.bfloat16 or torch.float16")
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+        self.tokens, self.sequences, self.dtype = int(tokens), int(sequences), dtype
+        self.heads, self.kv_heads, self.dim = int(heads), int(kv_heads), int(dim)
+        self.buckets = [] if buckets is None else [int(b) for b in buckets]
+        self.scale = self.dim ** -0.5 if scale is None and self.dim > 0 else float(scale or 0.0)
+        first = (ctypes.c_int32 * len(self.buckets))(*self.buckets) if self.buckets else None
+        cfg = binding.psops_attention_config(self.tokens, self.sequences, self.heads, self.kv_heads, self.dim,
+                                             _TYPES[dtype], len(self.buckets), first, self.scale,
+                                             PSOPS_ATTENTION_GRADS if gradients else 0)
+        self._on(self.device, stream)
+        with torch.cuda.device(self.device):
+            self._workspace = _workspace(binding.psops_attention_workspace_bytes(cfg), self.device, "Attention")
+            self._follow()
+            self.ctx = binding.psops_attention_create(cfg, self._workspace, None, self.stream)
+
+    def _tensor(self, where, name, t, heads, tokens=None):
+        """The tensor as the library takes it."""
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype is not self.dtype:
+            _refuse(where, f"{name} is not a {self.dtype} tensor on {self.device}")
+        shape = t.shape
+        if len(shape) != 3 or shape[1] != heads or shape[2] != self.dim or tokens is not None and shape[0] != tokens:
+            _refuse(where, f"{name} is not {'tokens' if tokens is None else tokens} x {heads} x {self.dim}")
+        stride = t.stride()
+        if stride[2] != 1:
+            _refuse(where, f"{name}: the elements of a head are not consecutive")
+        return binding.psops_heads(t.data_ptr() or None, stride[0], stride[1])
+
+    def _arguments(self, where, q, k, v, offsets, bias):
+        Q = self._tensor(where, "q", q, self.heads)
+        tokens = q.shape[0]
+        if tokens > self.tokens:
+            _refuse(where, f"{tokens} tokens, made for {self.tokens}")
+        K, V = self._tensor(where, "k", k, self.kv_heads, tokens), self._tensor(where, "v", v, self.kv_heads, tokens)
+        if not isinstance(offsets, torch.Tensor) or offsets.get_device() != self.device.index or \
+                offsets.dtype is not torch.int32 or offsets.dim() != 1 or not offsets.is_contiguous() or offsets.numel() < 1:
+            _refuse(where, f"offsets has to be contiguous, int32, of one axis, on {self.device}")
+        sequences = offsets.numel() - 1
+        if sequences > self.sequences:
+            _refuse(where, f"{sequences} sequences, made for {self.sequences}")
+        if bool(self.buckets) != (bias is not None):
+            _refuse(where, "a bias goes with buckets")
+        if bias is not None:
+            self._bias(where, "bias", bias, (self.dtype, torch.float32))
+        return Q, K, V, tokens, sequences, _TYPES[bias.dtype] if bias is not None else PSOPS_NONE
+
+    def _bias(self, where, name, t, types):
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype not in types or \
+                t.shape != (len(self.buckets), self.heads) or not t.is_contiguous():
+            _refuse(where, f"{name} has to be contiguous, {len(self.buckets)} x {self.heads}, of "
+                           f"{' or '.join(map(str, types))}, on {self.device}")
+
+    def _lse(self, where, t, tokens):
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype is not torch.float32 or \
+                t.shape != (self.heads, tokens) or not t.is_contiguous():
+            _refuse(where, f"lse has to be contiguous, fp32, {self.heads} x {tokens}, on {self.device}")
+
+    def forward(self, q, k, v, offsets, bias=None, *, out=None):
+        """(out, lse): the output, and heads x tokens log-sum-exps.  `out`: a tensor to hold the output."""
+        where = "Attention.forward"
+        Q, K, V, tokens, sequences, bias_type = self._arguments(where, q, k, v, offsets, bias)
+        given = out is not None
+        if not given:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        O = self._tensor(where, "out", out, self.heads, tokens)
+        lse = (torch.zeros if given else torch.empty)((self.heads, tokens), dtype=torch.float32, device=self.device)
+        self._follow(q, k, v, offsets, bias, out, lse)
+        binding.psops_attention_forward(self.ctx, Q, K, V, offsets, sequences, tokens, bias, bias_type, O, lse, not given)
+        if given:
+            _changed([out])
+        return out, lse
+
+    def backward(self, q, k, v, offsets, out, lse, grad, bias=None, *, dq=None, dk=None, dv=None, dbias=None,
+                 want=(True, True, True, True)):
+        """(dq, dk, dv, dbias) from forward's inputs and results and the gradient of its output.
+        dq, dk, dv, dbias: tensors to hold the results; want: which of them are computed."""
+        where = "Attention.backward"
+        Q, K, V, tokens, sequences, bias_type = self._arguments(where, q, k, v, offsets, bias)
+        O, G = self._tensor(where, "out", out, self.heads, tokens), self._tensor(where, "grad", grad, self.heads, tokens)
+        self._lse(where, lse, tokens)
+        held, results, given = [], [], []
+        for name, t, like, heads, wanted in (("dq", dq, q, self.heads, want[0]), ("dk", dk, k, self.kv_heads, want[1]),
+                                             ("dv", dv, v, self.kv_heads, want[2])):
+            if not wanted:
+                results.append(None)
+                held.append(None)
+                continue
+            if t is None:
+                # what is given keeps its rows of no sequence, what is made here does not
+                t = (torch.empty if dq is None and dk is None and dv is None else torch.zeros)(
+                    like.shape, dtype=self.dtype, device=self.device)
+            else:
+                given.append(t)
+            results.append(t)
+            held.append(self._tensor(where, name, t, heads, tokens))
+        if not want[3] or bias is None:
+            dbias = None
+        elif dbias is None:
+            dbias = torch.empty_like(bias)
+        else:
+            self._bias(where, "dbias", dbias, (bias.dtype,))
+            given.append(dbias)
+        self._follow(q, k, v, offsets, bias, out, lse, grad, *results, dbias)
+        binding.psops_attention_backward(self.ctx, Q, K, V, offsets, sequences, tokens, bias, bias_type, O, lse, G, *held,
+                                         dbias, dq is None and dk is None and dv is None)
+        if given:
+            _changed(given)
+        return (*results, dbias)
+
+    def _fitting(self, t):
+        """The tensor, or a copy of it where its rows do not lie as the library reads them."""
+        if not isinstance(t, torch.Tensor) or t.dim() != 3 or not t.is_cuda:
+            return t
+        (a, b, c), (n, h, _) = t.stride(), t.shape
+        if c == 1 and t.data_ptr() % 16 == 0 and (n <= 1 or a % 8 == 0 and a >= self.dim) and \
+                (h <= 1 or b % 8 == 0 and b >= self.dim):
+            return t
+        return t.contiguous() if not t.is_contiguous() else t.clone()
+
+    def _join(self):
+        if not self._follows:
+            self._order(to_own=False)
+
+    def __call__(self, q, k, v, offsets, bias=None):
+        """The output with gradients.  Here q, k and v may have any strides."""
+        q, k, v = map(self._fitting, (q, k, v))
+        if isinstance(bias, torch.Tensor):
+            bias = bias.contiguous()
+        return _AttentionFunction.apply(q, k, v, bias, offsets, self)
+
+
+class _AttentionFunction(torch.autograd.Function):
+    """Attention.forward and .backward as one differentiable step; a second derivative raises an error."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, bias, offsets, op):
+        out, lse = op.forward(q, k, v, offsets, bias)
+        op._join()
+        ctx.save_for_backward(q, k, v, bias, offsets, out, lse)
+        ctx.op = op
+        return out
+
+    @staticmethod
+    def backward(ctx, grad):
+        q, k, v, bias, offsets, out, lse = ctx.saved_tensors
+        with torch.no_grad():
+            results = ctx.op.backward(q, k, v, offsets, out, lse, ctx.op._fitting(grad), bias, want=ctx.needs_input_grad[:4])
+            ctx.op._join()
+        if torch.is_grad_enabled():                # create_graph: what is done with the gradients is recorded
+            came_from = [t for t in (q, k, v, bias, grad) if t is not None]
+            results = [None if d is None else _FirstOrderOnly.apply(d, *came_from) for d in results]
+        return (*results, None, None)
 
 
 class AdamW(_Holder):
