@@ -676,6 +676,59 @@ int64_t psops_attention_launch_count(const psops_attention *a);
 const char *psops_attention_last_error(const psops_attention *a);
 int psops_attention_destroy(psops_attention *a);
 
+/*
+ * Activations kept in 8 bits between the forward and the backward pass.  A row of
+ * `cols` 16-bit numbers is cut into blocks of 128 (the last may be short); with top
+ * the largest magnitude of a block
+ *   scale = top / 127,   code = x / scale rounded to the nearest, ties away from zero
+ * (fp32 division, correctly rounded; codes are signed bytes, value = code * scale).
+ * A block with top < 2^-100 is kept as zeros with scale 0; one with a number that is
+ * not finite has scale NaN, so that all its values are.
+ * Codes: rows of cols rounded up to a multiple of 16 bytes, 16-byte aligned; the
+ * bytes behind a row's last code are set to 0.  Scales: ceil(cols / 128) for each
+ * row, row after row.
+ *
+ * psops_keep8_activate: y = f(a), or f(a) * b where d_b is not NULL, from the inputs
+ * as they are, and the inputs in 8 bits.  psops_keep8_activate_backward, from the
+ * values A, B that these stand for and the gradient of y:
+ *   da = dy * B * f'(A),  db = dy * f(A),  y = f(A) * B   (B = 1 where d_b_codes is NULL)
+ * each of which may be NULL (not wanted); y is for a backward pass that needs it
+ * again, as the next product's does, so that it need not be kept either.
+ *   PSOPS_RELU  f(x) = max(x, 0), f'(0) = 0
+ *   PSOPS_SILU  f(x) = x / (1 + exp(-x))
+ *   PSOPS_GELU  f(x) = x / 2 (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3)))
+ * All arithmetic is fp32, numbers below 2^-126 count as zero, results are rounded once.
+ *
+ * type: PSOPS_F16 or PSOPS_BF16.  Rows start at multiples of their stride (in
+ * elements, at least cols) and may lie anywhere; 16-byte aligned ones are fastest.
+ * Results must not overlap the inputs.  rows >= 0, cols >= 1, at most 2^30 blocks in a call.  A
+ * context has no workspace: calls share nothing but its stream.
+ * Errors: EINVAL, EALIGN (an array not aligned to its element, codes not to 16
+ * bytes), ECUDA.
+ */
+#define PSOPS_RELU       0
+#define PSOPS_SILU       1
+#define PSOPS_GELU       2
+
+typedef struct psops_keep8 psops_keep8;  /* opaque */
+
+int psops_keep8_create(psops_keep8 **out, void *cuda_stream);
+int psops_keep8_pack(psops_keep8 *k, int32_t type, int64_t rows, int64_t cols, const void *d_x, int64_t x_ld,
+                     void *d_codes, float *d_scales);
+int psops_keep8_unpack(psops_keep8 *k, int32_t type, int64_t rows, int64_t cols, const void *d_codes,
+                       const float *d_scales, void *d_x, int64_t x_ld);
+int psops_keep8_activate(psops_keep8 *k, int32_t kind, int32_t type, int64_t rows, int64_t cols, const void *d_a,
+                         int64_t a_ld, const void *d_b, int64_t b_ld, void *d_y, int64_t y_ld, void *d_a_codes,
+                         float *d_a_scales, void *d_b_codes, float *d_b_scales);
+int psops_keep8_activate_backward(psops_keep8 *k, int32_t kind, int32_t type, int64_t rows, int64_t cols,
+                                  const void *d_a_codes, const float *d_a_scales, const void *d_b_codes,
+                                  const float *d_b_scales, const void *d_dy, int64_t dy_ld, void *d_da, int64_t da_ld,
+                                  void *d_db, int64_t db_ld, void *d_y, int64_t y_ld);
+int psops_keep8_set_stream(psops_keep8 *k, void *cuda_stream);
+int64_t psops_keep8_launch_count(const psops_keep8 *k);
+const char *psops_keep8_last_error(const psops_keep8 *k);
+int psops_keep8_destroy(psops_keep8 *k);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,6 +9,8 @@ computation runs in the CUDA library.
                with its gradients; its loss alone is a worker's fitness
   Attention    causal attention over packed sequences, with grouped heads and a learned
                bias by buckets of the distance, with its gradients
+  Keep8        activations kept in 8 bits for the backward pass, and the (gated) activation
+               whose backward pass reads them
   AdamW        one AdamW step over many tensors, moments in 32 or in 8 bits
   GradNorm     2-norm of many gradients and the factor that clips it
 
@@ -30,11 +32,13 @@ import math
 import torch
 
 from . import binding
-from .binding import (PSOPS_ATTENTION_GRADS, PSOPS_BF16, PSOPS_EINVAL, PSOPS_ESTATE, PSOPS_F16, PSOPS_F32, PSOPS_MEAN, PSOPS_NONE,
+from .binding import (PSOPS_ATTENTION_GRADS, PSOPS_BF16, PSOPS_GELU, PSOPS_RELU, PSOPS_SILU, PSOPS_EINVAL, PSOPS_ESTATE, PSOPS_F16, PSOPS_F32, PSOPS_MEAN, PSOPS_NONE,
                       PSOPS_PER_TOKEN, PSOPS_SUM, PSOPS_XENT_GRADS, PSOPS_XENT_STAGED, PsopsError)
 
 _TYPES = {torch.float32: PSOPS_F32, torch.float16: PSOPS_F16, torch.bfloat16: PSOPS_BF16}
 _REDUCTIONS = {"mean": PSOPS_MEAN, "sum": PSOPS_SUM, "none": PSOPS_PER_TOKEN}
+_KINDS = {"relu": PSOPS_RELU, "silu": PSOPS_SILU, "gelu": PSOPS_GELU}
+KEPT_BLOCK = 128                 # elements of a row that share one scale of a kept activation
 MOMENT_BLOCK = 256               # elements that share one scale of an 8-bit moment
 
 # The kernels write through addresses, which autograd does not see: what they change in a caller's tensor is told
@@ -363,7 +367,7 @@ class _FirstOrderOnly(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad):
-        raise RuntimeError("LinearXent, Attention: gradients are of the first order only (once_differentiable); a function of them "
+        raise RuntimeError("LinearXent, Attention, Keep8: gradients are of the first order only (once_differentiable); a function of them "
                            "cannot be differentiated")
 
 
@@ -573,6 +577,221 @@ class _AttentionFunction(torch.autograd.Function):
             came_from = [t for t in (q, k, v, bias, grad) if t is not None]
             results = [None if d is None else _FirstOrderOnly.apply(d, *came_from) for d in results]
         return (*results, None, None)
+
+
+class Keep8(_Holder):
+    """Activations kept in 8 bits between the forward and the backward pass.
+
+    A tensor of a 16-bit type becomes codes (int8, its last dimension padded to a multiple of 16) and
+    scales (fp32, one for every 128 elements of a row), 1.03 bytes an element; psops.h has the rule.  Three ways:
+
+      pack, unpack    any tensor there and back
+      hooks           a context in which autograd keeps what it saves in 8 bits, whatever the operation::
+
+          with keep.hooks():
+              y = block(x)
+
+      calling it      y = f(a) or f(a) * b with f one of "relu", "silu", "gelu" (tanh form), differentiable, the
+                      inputs kept in 8 bits: keep(a, b, "silu")
+    """
+
+    _set_stream = staticmethod(binding.psops_keep8_set_stream)
+    _launch_count = staticmethod(binding.psops_keep8_launch_count)
+    _destroy = staticmethod(binding.psops_keep8_destroy)
+
+    def __init__(self, *, device="cuda", stream=None):
+        device = torch.device(device)
+        if device.type != "cuda":
+            _refuse("Keep8", "needs a GPU")
+        self.device = torch.device("cuda", torch.cuda.current_device()) if device.index is None else device
+        self._on(self.device, stream)
+        with torch.cuda.device(self.device):
+            self._follow()
+            self.ctx = binding.psops_keep8_create(self.stream)
+
+    def _rows(self, where, name, t, like=None):
+        """(rows, elements of a row, stride) of a tensor with consecutive elements in each row, its leading dimensions
+        seen as one."""
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or \
+                t.dtype is not torch.bfloat16 and t.dtype is not torch.float16:
+            _refuse(where, f"{name} is not a 16-bit floating-point tensor on {self.device}")
+        shape = t.shape
+        if len(shape) < 1 or shape[-1] < 1:
+            _refuse(where, f"{name} has no elements in its rows")
+        if like is not None and (shape != like.shape or t.dtype is not like.dtype):
+            _refuse(where, f"{name} is not {like.dtype} of shape {tuple(like.shape)}")
+        cols = shape[-1]
+        rows = t.numel() // cols
+        if t.is_contiguous():
+            return rows, cols, cols
+        if len(shape) != 2:
+            try:
+                t = t.view(-1, cols)
+            except RuntimeError:
+                _refuse(where, f"{name}: its leading dimensions cannot be seen as one")
+        if cols > 1 and t.stride(1) != 1:
+            _refuse(where, f"{name}: the elements of a row are not consecutive")
+        ld = t.stride(0) if rows > 1 else cols
+        if ld < cols:
+            _refuse(where, f"{name}: rows overlap")
+        return rows, cols, ld
+
+    def _room(self, shape):
+        """Codes and scales for a tensor of this shape."""
+        cols = shape[-1]
+        return (torch.empty((*shape[:-1], -(-cols // 16) * 16), dtype=torch.int8, device=self.device),
+                torch.empty((*shape[:-1], -(-cols // KEPT_BLOCK)), dtype=torch.float32, device=self.device))
+
+    def _kept(self, where, name, codes, scales, shape):
+        room = (torch.Size((*shape[:-1], -(-shape[-1] // 16) * 16)), torch.Size((*shape[:-1], -(-shape[-1] // KEPT_BLOCK))))
+        for what, t, size, dtype in (("codes", codes, room[0], torch.int8), ("scales", scales, room[1], torch.float32)):
+            if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype is not dtype or \
+                    t.shape != size or not t.is_contiguous():
+                _refuse(where, f"{what} of {name} have to be contiguous, {dtype}, of shape {tuple(size)}, on {self.device}")
+
+    def pack(self, x):
+        """(codes, scales)."""
+        rows, cols, ld = self._rows("Keep8.pack", "x", x)
+        codes, scales = self._room(x.shape)
+        self._follow(x, codes, scales)
+        binding.psops_keep8_pack(self.ctx, _TYPES[x.dtype], rows, cols, x, ld, codes, scales)
+        return codes, scales
+
+    def unpack(self, codes, scales, shape, dtype, *, out=None):
+        """The tensor of this shape and type that pack was given, each element half a scale off at most.
+        `out`: a tensor to hold it."""
+        where = "Keep8.unpack"
+        shape = torch.Size(shape)
+        if dtype not in (torch.float16, torch.bfloat16) or len(shape) < 1 or shape[-1] < 1:
+            _refuse(where, f"{dtype} of shape {tuple(shape)}")
+        self._kept(where, "x", codes, scales, shape)
+        given = out is not None
+        if not given:
+            out = torch.empty(shape, dtype=dtype, device=self.device)
+        rows, cols, ld = self._rows(where, "out", out)
+        if out.shape != shape or out.dtype is not dtype:
+            _refuse(where, f"out is not {dtype} of shape {tuple(shape)}")
+        self._follow(codes, scales, out)
+        binding.psops_keep8_unpack(self.ctx, _TYPES[dtype], rows, cols, codes, scales, out, ld)
+        if given:
+            _changed([out])
+        return out
+
+    def _kind(self, where, kind):
+        code = _KINDS.get(kind)
+        if code is None:
+            _refuse(where, f"activation {kind!r}: one of {', '.join(_KINDS)}")
+        return code
+
+    def activate(self, a, b=None, kind="silu", *, out=None):
+        """(y, kept): f(a), or f(a) * b, and (codes, scales) of a, or (codes, scales, codes, scales) of a and b, for the
+        backward pass.  `out`: a tensor to hold y."""
+        where = "Keep8.activate"
+        code = self._kind(where, kind)
+        rows, cols, a_ld = self._rows(where, "a", a)
+        b_ld = self._rows(where, "b", b, a)[2] if b is not None else 0
+        given = out is not None
+        if not given:
+            out = torch.empty(a.shape, dtype=a.dtype, device=self.device)
+        y_ld = self._rows(where, "out", out, a)[2]
+        kept = self._room(a.shape) + (self._room(a.shape) if b is not None else ())
+        self._follow(a, b, out, *kept)
+        binding.psops_keep8_activate(self.ctx, code, _TYPES[a.dtype], rows, cols, a, a_ld, b, b_ld, out, y_ld,
+                                     *kept, *((None, None) if b is None else ()))
+        if given:
+            _changed([out])
+        return out, kept
+
+    def activate_backward(self, kept, grad, kind="silu", *, again=False, da=None, db=None, want=(True, True)):
+        """(da, db) from what activate kept and the gradient of y, or (da, db, y) with `again`: y from the kept inputs,
+        for a product's gradient that needs it.  da, db: tensors to hold the results (views of one gradient, for
+        instance); want: which of the two are computed.  db is None without b."""
+        where = "Keep8.activate_backward"
+        code = self._kind(where, kind)
+        rows, cols, ld = self._rows(where, "grad", grad)
+        if len(kept) not in (2, 4):
+            _refuse(where, "`kept` is (codes, scales) of a, or of a and b")
+        gated = len(kept) == 4
+        for i in range(0, len(kept), 2):
+            self._kept(where, "ab"[i // 2], kept[i], kept[i + 1], grad.shape)
+        results, strides, given = [], [], []
+        for name, t, wanted in (("da", da, want[0]), ("db", db, want[1] and gated), ("y", None, again)):
+            if not wanted:
+                t = None
+            elif t is None:
+                t = torch.empty(grad.shape, dtype=grad.dtype, device=self.device)
+            else:
+                given.append(t)
+            results.append(t)
+            strides.append(self._rows(where, name, t, grad)[2] if t is not None else 0)
+        self._follow(grad, *kept, *results)
+        binding.psops_keep8_activate_backward(self.ctx, code, _TYPES[grad.dtype], rows, cols, *kept,
+                                              *(() if gated else (None, None)), grad, ld, results[0], strides[0],
+                                              results[1], strides[1], results[2], strides[2])
+        if given:
+            _changed(given)
+        return tuple(results) if again else tuple(results[:2])
+
+    def _join(self):
+        if not self._follows:
+            self._order(to_own=False)
+
+    @staticmethod
+    def _fitting(t):
+        """The tensor, or a copy of it where the elements of its rows are not consecutive or its rows overlap."""
+        if not isinstance(t, torch.Tensor) or t.dim() < 1 or t.is_contiguous() or \
+                t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1]):
+            return t
+        return t.contiguous()
+
+    def __call__(self, a, b=None, kind="silu"):
+        """f(a), or f(a) * b, with gradients.  Here a and b may have any strides."""
+        return _Keep8Function.apply(self._fitting(a), self._fitting(b), kind, self)
+
+    def hooks(self, least=4096):
+        """A context in which autograd keeps the 16-bit tensors that it saves in 8 bits: those of `least` elements or
+        more on this GPU, but for leaves that have gradients (weights) and views of them, which are there anyway."""
+        def pack(t):
+            base = t._base if t._is_view() else t
+            if t.get_device() != self.device.index or t.dtype not in (torch.float16, torch.bfloat16) or \
+                    t.numel() < max(1, least) or t.dim() < 1 or base.is_leaf and base.requires_grad:
+                return t
+            with torch.no_grad():
+                codes, scales = self.pack(self._fitting(t.detach()))
+                self._join()
+            return codes, scales, t.shape, t.dtype
+
+        def unpack(kept):
+            if isinstance(kept, torch.Tensor):
+                return kept
+            with torch.no_grad():
+                x = self.unpack(*kept)
+                self._join()
+            return x
+
+        return torch.autograd.graph.saved_tensors_hooks(pack, unpack)
+
+
+class _Keep8Function(torch.autograd.Function):
+    """Keep8.activate and .activate_backward as one differentiable step; a second derivative raises an error."""
+
+    @staticmethod
+    def forward(ctx, a, b, kind, op):
+        y, kept = op.activate(a, b, kind)
+        op._join()
+        ctx.save_for_backward(*kept)
+        ctx.op, ctx.kind = op, kind
+        return y
+
+    @staticmethod
+    def backward(ctx, grad):
+        kept = ctx.saved_tensors
+        with torch.no_grad():
+            da, db = ctx.op.activate_backward(kept, ctx.op._fitting(grad), ctx.kind, want=ctx.needs_input_grad[:2])
+            ctx.op._join()
+        if torch.is_grad_enabled():                # create_graph: what is done with the gradients is recorded
+            da, db = (None if d is None else _FirstOrderOnly.apply(d, grad) for d in (da, db))
+        return da, db, None, None
 
 
 class AdamW(_Holder):
