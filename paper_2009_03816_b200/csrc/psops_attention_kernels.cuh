@@ -96,6 +96,41 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
+// Two fp32 numbers in one instruction, each as by itself.
+__device__ __forceinline__ uint64_t pair_of(uint32_t low, uint32_t high)
+{
+    uint64_t x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(low), "r"(high));
+    return x;
+}
+__device__ __forceinline__ uint64_t both(float x) { return pair_of(__float_as_uint(x), __float_as_uint(x)); }
+__device__ __forceinline__ float low_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float high_of(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ uint64_t fma_both(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
+}
+__device__ __forceinline__ uint64_t add_both(uint64_t a, uint64_t b)
+{
+    uint64_t x;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+__device__ __forceinline__ uint64_t mul_both(uint64_t a, uint64_t b)
+{
+    uint64_t x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float x;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(b), "f"(c));
+    return x;
+}
+
 // ---------------------------------------------------------------------------
 // The list of tiles, most work first; rows of no sequence; delta
 // ---------------------------------------------------------------------------
@@ -306,16 +341,6 @@ struct Bias {
     int first[kMostBuckets];                 // the first distance of each bucket
 };
 
-__device__ __forceinline__ int bucket_of(const Bias &B, int distance)
-{
-    int low = 0, high = B.buckets;           // first[low] <= distance < first[high]
-    while (high - low > 1) {
-        const int mid = (low + high) / 2;
-        if (B.first[mid] <= distance) low = mid;
-        else high = mid;
-    }
-    return low;
-}
 // In base 2.  What lies below -1e30, such as the lowest number of a type, takes its
 // pairs out as -inf does: no row's lse could hold it beside a logarithm.
 template <class T>
@@ -326,12 +351,41 @@ __device__ __forceinline__ float bias_at(const Bias &B, int bucket, int heads, i
     const float x = b * kLog2e;
     return x < -1e30f ? -INFINITY : x;
 }
-// table[kBefore + d]: the bias of distance d, up to a tile's reach beyond the last bucket's beginning.
-template <class T>
-__device__ __forceinline__ void make_table(const Bias &B, int heads, int head, float *table, int threads)
+__device__ __forceinline__ void barrier_named(int id, int threads)
 {
-    for (int i = threadIdx.x; i < kBefore + B.last + 2 * kTile; i += threads)
-        table[i] = i < kBefore ? 0.0f : bias_at<T>(B, bucket_of(B, i - kBefore), heads, head);
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// What the softmax threads of a CTA keep of the bias; distances up to a tile's
+// reach beyond the last bucket's beginning.
+struct Tables {
+    float value[kMostBuckets];               // of the head at hand
+    int first[kMostBuckets];
+    uint8_t bucket[kMostDistance + 2 * kTile];
+    float distance[kTableFloats];            // [kBefore + d]: the bias of distance d
+};
+// By THREADS threads that share barrier 1, after each has put its part of `value` in place.
+template <int THREADS, bool BUCKETS>
+__device__ __forceinline__ void make_tables(const Bias &B, Tables &t)
+{
+    const int many = B.last + 2 * kTile;
+    if (BUCKETS && threadIdx.x < kMostBuckets) t.first[threadIdx.x] = threadIdx.x < B.buckets ? B.first[threadIdx.x] : INT32_MAX;
+    barrier_named(1, THREADS);
+    if (BUCKETS && threadIdx.x < kBefore) t.distance[threadIdx.x] = 0.0f;
+    for (int d = threadIdx.x; d < many; d += THREADS) {
+        int bucket;
+        if (BUCKETS) {
+            bucket = 0;
+#pragma unroll
+            for (int step = kMostBuckets / 2; step > 0; step /= 2)           // the last one that begins at d or before
+                if (t.first[bucket + step] <= d) bucket += step;
+            t.bucket[d] = (uint8_t)bucket;
+        } else {
+            bucket = t.bucket[d];
+        }
+        t.distance[kBefore + d] = t.value[bucket];
+    }
+    barrier_named(1, THREADS);
 }
 
 // Numbers that are not finite in a row of a tile (two boxes of 64 elements for
@@ -382,10 +436,6 @@ __device__ __forceinline__ bool wait_all(const uint64_t *bar, uint32_t parity, v
 {
     return __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(bar), parity, failed));
 }
-__device__ __forceinline__ void barrier_named(int id, int threads)
-{
-    asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
 
 // Eight results of a row, rounded to the 16-bit type.
 template <class T>
@@ -397,6 +447,10 @@ __device__ __forceinline__ void put8(uint16_t *to, const float *x)
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
+
+struct None {};
+template <bool BIAS> struct Choose { using Type = Tables; };
+template <> struct Choose<false> { using Type = None; };
 
 struct ForwardParams {
     const Item *items;
@@ -412,13 +466,15 @@ constexpr int kForwardThreads = 192;         // four warps of softmax, one of co
 constexpr float kLazy = 8.0f;                // a maximum moves only when it grows by more than this (base 2)
 
 template <int HALVES>
-constexpr int forward_shared() { return 1024 + 3 * HALVES * kHalfBytes; }
+constexpr int forward_shared() { return 1024 + (HALVES == 1 ? 5 : 3) * HALVES * kHalfBytes; }
 
 // A CTA has 128 queries of one head; two CTAs share an SM, so that one's softmax
 // runs under the other's products.  Per tile of 128 keys: S = Q K^T into tensor
 // memory; each thread has one row of it, twice read (maximum; probabilities),
-// which needs no word from another thread; P goes back into tensor memory in
-// place of S, as the left operand of O += P V.
+// which needs no word from another thread; P goes back into tensor memory as the
+// left operand of O += P V.  For dim <= 64 the half of an SM's tensor memory that
+// a CTA has holds P beside S: the next scores are computed as soon as S has been
+// read, with two tiles of K and V under way.  For more, P takes the place of S.
 template <class T, int HALVES, bool BIAS>
 __global__ void __launch_bounds__(kForwardThreads, 2)
 psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -426,13 +482,16 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
 {
     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
     constexpr int kTileBytes = HALVES * kHalfBytes;
+    constexpr bool kAhead = HALVES == 1;
+    constexpr int kStages = kAhead ? 2 : 1;
     // fp16 has no numbers below 2^-24: probabilities, at most 2^kLazy, are kept higher up
     constexpr float kShift = kBf16 ? 0.0f : 7.0f;
     extern __shared__ uint8_t raw[];
-    __shared__ alignas(8) uint64_t bar_q, bar_k_full, bar_k_empty, bar_v_full, bar_v_empty, bar_s, bar_p, bar_o;
+    __shared__ alignas(8) uint64_t bar_q, bar_k_full[kStages], bar_k_empty[kStages], bar_v_full[kStages], bar_v_empty[kStages], bar_s,
+        bar_read, bar_p, bar_o;
     __shared__ uint32_t tensor_base_slot;
     __shared__ int failed_slot, dirty;
-    __shared__ float table[BIAS ? kTableFloats : 1];
+    __shared__ typename Choose<BIAS>::Type tables;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &failed_slot;
@@ -444,21 +503,22 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
     if (item.length <= 0) return;
     const int tile = item.level, first = item.first + tile * kTile;
     uint8_t *tiles = raw + (((umma::shared_address(raw) + 1023u) & ~1023u) - umma::shared_address(raw));
-    const uint32_t q_at = umma::shared_address(tiles), k_at = q_at + kTileBytes, v_at = k_at + kTileBytes;
+    const uint32_t q_at = umma::shared_address(tiles), k_at = q_at + kTileBytes, v_at = k_at + kStages * kTileBytes;
 
     if (threadIdx.x == 0) {
-        for (uint64_t *b : {&bar_q, &bar_k_full, &bar_k_empty, &bar_v_full, &bar_v_empty, &bar_s, &bar_o})
-            umma::barrier_init(umma::shared_address(b), 1);
+        for (uint64_t *b : {&bar_q, &bar_s, &bar_o}) umma::barrier_init(umma::shared_address(b), 1);
+        for (int i = 0; i < kStages; ++i)
+            for (uint64_t *b : {&bar_k_full[i], &bar_k_empty[i], &bar_v_full[i], &bar_v_empty[i]}) umma::barrier_init(umma::shared_address(b), 1);
+        umma::barrier_init(umma::shared_address(&bar_read), 4);
         umma::barrier_init(umma::shared_address(&bar_p), 4);
         failed_slot = dirty = 0;
         umma::barrier_init_done();
     }
     if (warp == 5) umma::tensor_columns_take<256>(umma::shared_address(&tensor_base_slot));
-    if (BIAS) make_table<T>(P.bias, P.heads, head, table, kForwardThreads);
     umma::fence_before();
     __syncthreads();
     umma::fence_after();
-    const uint32_t s_at = tensor_base_slot, o_at = s_at + kTile;
+    const uint32_t s_at = tensor_base_slot, o_at = s_at + kTile, p_at = kAhead ? o_at + 64 : s_at;
 
     if (warp == 4) {
         // ---- copies in; the tile on the diagonal comes first
@@ -471,22 +531,22 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         }
         __syncwarp();
         for (int j = 0; j <= tile && ok; ++j) {
-            const int token = first - j * kTile;
-            const uint32_t phase = (j & 1) ^ 1;
-            ok = wait_all(&bar_k_empty, phase, failed);
+            const int token = first - j * kTile, stage = j % kStages;
+            const uint32_t phase = (j / kStages & 1) ^ 1;
+            ok = wait_all(&bar_k_empty[stage], phase, failed);
             if (!ok) break;
             if (umma::elected()) {
-                umma::barrier_expect(umma::shared_address(&bar_k_full), kTileBytes);
+                umma::barrier_expect(umma::shared_address(&bar_k_full[stage]), kTileBytes);
                 for (int h = 0; h < HALVES; ++h)
-                    umma::tensor_load3(k_at + h * kHalfBytes, &map_k, h * 64, kv, token, umma::shared_address(&bar_k_full));
+                    umma::tensor_load3(k_at + stage * kTileBytes + h * kHalfBytes, &map_k, h * 64, kv, token, umma::shared_address(&bar_k_full[stage]));
             }
             __syncwarp();
-            ok = wait_all(&bar_v_empty, phase, failed);
+            ok = wait_all(&bar_v_empty[stage], phase, failed);
             if (!ok) break;
             if (umma::elected()) {
-                umma::barrier_expect(umma::shared_address(&bar_v_full), kTileBytes);
+                umma::barrier_expect(umma::shared_address(&bar_v_full[stage]), kTileBytes);
                 for (int h = 0; h < HALVES; ++h)
-                    umma::tensor_load3(v_at + h * kHalfBytes, &map_v, h * 64, kv, token, umma::shared_address(&bar_v_full));
+                    umma::tensor_load3(v_at + stage * kTileBytes + h * kHalfBytes, &map_v, h * 64, kv, token, umma::shared_address(&bar_v_full[stage]));
             }
             __syncwarp();
         }
@@ -497,38 +557,51 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         const uint32_t instr_s = umma::instruction(kBf16, false, false, kTile, kTile);
         const uint32_t instr_o = umma::instruction(kBf16, false, true, kTile, steps * 16);
         const uint64_t dq = umma::operand(q_at, false), dk = umma::operand(k_at, false), dv = umma::operand(v_at, true, kHalfBytes);
-        bool ok = wait_all(&bar_q, 0, failed);
-        for (int j = 0; j <= tile && ok; ++j) {
-            const uint32_t phase = j & 1;
-            ok = wait_all(&bar_k_full, phase, failed);
-            if (!ok) break;
+        auto scores = [&](int j) {
+            const int stage = j % kStages;
+            if (!wait_all(&bar_k_full[stage], j / kStages & 1, failed)) return false;
+            if (kAhead && j > 0 && !wait_all(&bar_read, (j & 1) ^ 1, failed)) return false;
             umma::fence_after();
             if (umma::elected()) {
                 for (int s = 0; s < steps; ++s) {
                     const uint32_t on = (s >> 2) * (kHalfBytes >> 4) + (s & 3) * 2;
-                    umma::multiply<false>(s_at, dq + on, dk + on, instr_s, s > 0);
+                    umma::multiply<false>(s_at, dq + on, dk + stage * (kTileBytes >> 4) + on, instr_s, s > 0);
                 }
                 umma::products_arrive<false>(umma::shared_address(&bar_s));
-                umma::products_arrive<false>(umma::shared_address(&bar_k_empty));
+                umma::products_arrive<false>(umma::shared_address(&bar_k_empty[stage]));
             }
             __syncwarp();
-            ok = wait_all(&bar_v_full, phase, failed) && wait_all(&bar_p, phase, failed);
+            return true;
+        };
+        bool ok = wait_all(&bar_q, 0, failed) && scores(0);
+        for (int j = 0; j <= tile && ok; ++j) {
+            const int stage = j % kStages;
+            if (kAhead && j < tile && !scores(j + 1)) break;
+            ok = wait_all(&bar_v_full[stage], j / kStages & 1, failed) && wait_all(&bar_p, j & 1, failed);
             if (!ok) break;
             umma::fence_after();
             if (umma::elected()) {
 #pragma unroll
                 for (int s = 0; s < kTile / 16; ++s)
-                    umma::multiply_from_tensor_memory(o_at, s_at + s * 8, dv + s * 128, instr_o, j > 0 || s > 0);
-                umma::products_arrive<false>(umma::shared_address(&bar_v_empty));
-                if (j == tile) umma::products_arrive<false>(umma::shared_address(&bar_o));
+                    umma::multiply_from_tensor_memory(o_at, p_at + s * 8, dv + stage * (kTileBytes >> 4) + s * 128, instr_o, j > 0 || s > 0);
+                umma::products_arrive<false>(umma::shared_address(&bar_v_empty[stage]));
+                umma::products_arrive<false>(umma::shared_address(&bar_o));
             }
             __syncwarp();
+            if (!kAhead && j < tile) ok = scores(j + 1);
         }
     } else {
         // ---- softmax: one query a thread
         const int row = threadIdx.x;
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        const float far = BIAS ? table[kBefore + P.bias.last] : 0.0f;
+        float far = 0.0f;
+        const float *table = nullptr;
+        if constexpr (BIAS) {
+            if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, head) : 0.0f;
+            make_tables<kTile, true>(P.bias, tables);
+            table = tables.distance + kBefore;
+            far = tables.value[P.bias.buckets - 1];
+        }
         float top = -INFINITY, sum = 0.0f;       // top: what is subtracted, base 2
         bool ok = true;
         for (int j = 0; j <= tile; ++j) {
@@ -536,29 +609,47 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
             if (!ok) break;
             umma::fence_after();
             const bool diagonal = j == 0, near = BIAS && j * kTile - (kTile - 1) < P.bias.last;
-            const float *distance = table + kBefore + j * kTile + row;        // - column
-            float most = -INFINITY;
+            const float *distance = table + j * kTile + row;                  // - column
+            // the row, in two halves so that the second is on its way under the first's maximum; with a bias it becomes
+            // the whole exponent here, else scale and bias come with the exponential
+            uint32_t s[kTile];
+            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            umma::tensor_memory_load(s_at + lanes, s);
+            umma::tensor_memory_load(s_at + lanes + 32, s + 32);
+            umma::tensor_memory_loaded<64>(s);
+            umma::tensor_memory_load(s_at + lanes + 64, s + 64);
+            umma::tensor_memory_load(s_at + lanes + 96, s + 96);
 #pragma unroll
-            for (int c = 0; c < kTile; c += 32) {
-                uint32_t u[32];
-                umma::tensor_memory_load(s_at + lanes + c, u);
-                umma::tensor_memory_loaded<32>(u);
+            for (int c = 0; c < kTile; c += 64) {
+                if (c > 0) umma::tensor_memory_loaded<64>(s + c);
                 if (near) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (!diagonal || c + i <= row) most = fmaxf(most, __fmaf_rn(__uint_as_float(u[i]), P.scale2, distance[-(c + i)]));
-                } else if (diagonal) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c + i <= row) most = fmaxf(most, __uint_as_float(u[i]));
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) most = fmaxf(most, __uint_as_float(u[i]));
+                    for (int i = c; i < c + 64; ++i) s[i] = __float_as_uint(__fmaf_rn(__uint_as_float(s[i]), P.scale2, distance[-i]));
                 }
+                if (diagonal) {
+#pragma unroll
+                    for (int i = c; i < c + 64; ++i)
+                        if (i > row) s[i] = 0xff800000u;                     // -inf
+                }
+#pragma unroll
+                for (int i = c; i < c + 64; i += 8)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) most[n] = max3(most[n], __uint_as_float(s[i + 2 * n]), __uint_as_float(s[i + 2 * n + 1]));
             }
-            if (!near) most = __fmaf_rn(most, P.scale2, far);
-            if (__any_sync(0xffffffffu, most > top + kLazy)) {
-                const float higher = fmaxf(most, top);
+            if (kAhead) {
+                umma::fence_before();
+                __syncwarp();
+                if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_read));
+            }
+            float higher = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            if (!near) higher = __fmaf_rn(higher, P.scale2, far);
+            if (kAhead && j > 0) {               // else bar_s has said so: the sums of the tile before are complete
+                ok = wait_all(&bar_o, (j & 1) ^ 1, failed);
+                if (!ok) break;
+                umma::fence_after();
+            }
+            if (__any_sync(0xffffffffu, higher > top + kLazy)) {
+                higher = fmaxf(higher, top);
                 const float factor = higher > -INFINITY ? exp2_fast(top - higher) : 1.0f;
                 top = higher;
                 sum *= factor;
@@ -574,41 +665,28 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
                 }
             }
             const float base = (near ? 0.0f : far) + kShift - (top > -INFINITY ? top : 0.0f);
-            float here = 0.0f;
+            const uint64_t times = both(near ? 1.0f : P.scale2), plus = both(base);
+            uint64_t parts[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < kTile; c += 32) {
-                uint32_t u[32], p[16];
-                umma::tensor_memory_load(s_at + lanes + c, u);
-                umma::tensor_memory_loaded<32>(u);
-                float x[32];
-                if (near) {
+                uint32_t p[16];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        x[i] = exp2_fast(__fmaf_rn(__uint_as_float(u[i]), P.scale2, distance[-(c + i)]) + base);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) x[i] = exp2_fast(__fmaf_rn(__uint_as_float(u[i]), P.scale2, base));
+                for (int i = 0; i < 16; ++i) {
+                    const uint64_t x = fma_both(pair_of(s[c + 2 * i], s[c + 2 * i + 1]), times, plus);
+                    const float2 e = make_float2(exp2_fast(low_of(x)), exp2_fast(high_of(x)));
+                    parts[i & 3] = add_both(parts[i & 3], pair_of(__float_as_uint(e.x), __float_as_uint(e.y)));
+                    p[i] = pack2<T>(e.x, e.y);
                 }
-                if (diagonal) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c + i > row) x[i] = 0.0f;
-                }
-                float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    part[i / 2 & 3] += x[i] + x[i + 1];
-                    p[i / 2] = pack2<T>(x[i], x[i + 1]);
-                }
-                here += (part[0] + part[1]) + (part[2] + part[3]);
-                umma::tensor_memory_store16(s_at + lanes + c / 2, p);
+                umma::tensor_memory_store16(p_at + lanes + c / 2, p);
             }
+            const uint64_t all = add_both(add_both(parts[0], parts[1]), add_both(parts[2], parts[3]));
+            const float here = low_of(all) + high_of(all);
             sum += here;
             if (diagonal) {
                 // keys that are masked here may hold anything: rows of the next sequence, or of none
-                ok = wait_all(&bar_v_full, 0, failed);
+                ok = wait_all(&bar_v_full[0], 0, failed);
                 if (!ok) break;
-                if (clean_row<T>(tiles + 2 * kTileBytes, row, HALVES)) dirty = 1;
+                if (clean_row<T>(tiles + (1 + kStages) * kTileBytes, row, HALVES)) dirty = 1;
                 umma::copies_see_shared();
             }
             umma::tensor_memory_stored();
@@ -616,7 +694,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
             __syncwarp();
             if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_p));
         }
-        if (ok) ok = wait_all(&bar_o, 0, failed);
+        if (ok) ok = wait_all(&bar_o, tile & 1, failed);
         umma::fence_after();
         barrier_named(1, kTile);
         const bool poisoned = *(volatile int *)&dirty != 0;
@@ -710,7 +788,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
     __shared__ int failed_slot, dirty0, dirty1;
     __shared__ float2 most[kBackwardThreads / 32];
     __shared__ float by_column[KEYS ? 2 : 1][2][kTile];                     // lse and delta of the queries
-    __shared__ float table[BIAS ? kTableFloats : 1];
+    __shared__ typename Choose<BIAS>::Type tables;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &failed_slot;
@@ -739,10 +817,8 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
         umma::barrier_init_done();
     }
     if (warp == 9) umma::tensor_columns_take<512>(umma::shared_address(&tensor_base_slot));
-    if (BIAS && !KEYS) {
-        make_table<T>(P.bias, P.heads, head, table, kBackwardThreads);
+    if (BIAS && !KEYS)
         for (int i = threadIdx.x; i < 8 * kMostBuckets; i += kBackwardThreads) bucket_sums[i] = 0.0f;
-    }
     if (!kBf16) {
         float2 m = make_float2(0.0f, 0.0f);
         for (int i = threadIdx.x; i < P.blocks; i += kBackwardThreads) m = make_float2(fmaxf(m.x, P.norms[i].x), fmaxf(m.y, P.norms[i].y));
@@ -858,20 +934,29 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
             }
         }
         const float unit_p = kBf16 ? 1.0f : unit * 0x1p-14f;
-        float far = BIAS && !KEYS ? table[kBefore + P.bias.last] : 0.0f;
+        // the bias of the (first) query head
+        float far = 0.0f, next_value = 0.0f;
+        const float *table = nullptr;
+        auto value = [&](int q_head) { return threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, q_head) : 0.0f; };
+        if constexpr (BIAS) {
+            if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = value(KEYS ? head * P.group : head);
+            make_tables<kSoftmaxThreads, true>(P.bias, tables);
+            table = tables.distance + kBefore;
+            far = tables.value[P.bias.buckets - 1];
+        }
         float row_lse = 0.0f, row_delta = 0.0f, far_sum = 0.0f;
         // a row whose scores are all -inf has no probabilities
         auto base2 = [](float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; };
         if (!KEYS && row < left) {
             const long long at = (long long)head * P.tokens + first + row;
             row_lse = base2(P.lse[at]);
-            row_delta = P.delta[at] * unit_p;
+            row_delta = -P.delta[at] * unit_p;
         }
         auto fetch = [&](int j) {                                            // this thread's part of by_column
             const int token = token_of(j) + row, q_head = head * P.group + j / meets;
             if (token >= item.first + item.length) return 0.0f;
             const long long at = (long long)q_head * P.tokens + token;
-            return half == 0 ? base2(P.lse[at]) : P.delta[at] * unit_p;
+            return half == 0 ? base2(P.lse[at]) : -P.delta[at] * unit_p;
         };
         float coming = KEYS ? fetch(0) : 0.0f;
         bool ok = true;                          // where it is not, all rounds are gone through all the same, for the barriers in them
@@ -881,18 +966,22 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
             const int columns = KEYS ? min(item.length - (tile + apart) * kTile, kTile) : kTile;   // columns that exist
             if (KEYS) {
                 by_column[j & 1][half][row] = coming;
-                if (BIAS && j % meets == 0) {
-                    barrier_named(1, kSoftmaxThreads);                      // nobody reads the table of the head before
-                    make_table<T>(P.bias, P.heads, head * P.group + j / meets, table, kSoftmaxThreads);
+                if constexpr (BIAS) {
+                    if (j > 0 && j % meets == 0) {
+                        barrier_named(1, kSoftmaxThreads);                  // nobody reads the tables of the head before
+                        if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = next_value;
+                        make_tables<kSoftmaxThreads, false>(P.bias, tables);
+                        far = tables.value[P.bias.buckets - 1];
+                    }
+                    if (j % meets == 0 && j + meets < rounds) next_value = value(head * P.group + j / meets + 1);
                 }
                 barrier_named(1, kSoftmaxThreads);
-                if (BIAS) far = table[kBefore + P.bias.last];
                 if (j + 1 < rounds) coming = fetch(j + 1);
             }
             const bool near = BIAS && apart * kTile - (kTile - 1) < P.bias.last;
             const bool masked = diagonal || columns < kTile;
             // distance of column c: of a query row to keys it falls with c, of a key row to queries it grows
-            const float *distance = table + kBefore + apart * kTile + (KEYS ? col0 - row : row - col0);
+            const float *distance = table + apart * kTile + (KEYS ? col0 - row : row - col0);
             ok &= wait_all(&bar_s, j & 1, failed);
             if (masked) {
                 // what is masked may hold anything: it must not meet a zero in a product to come
@@ -907,26 +996,37 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
             umma::fence_after();
             float p[64];
             auto counts = [&](int c) { return KEYS ? (!diagonal || col0 + c >= row) && col0 + c < columns : !diagonal || col0 + c <= row; };
+            uint32_t s[64];
+            umma::tensor_memory_load(s_at + lanes, s);
+            umma::tensor_memory_load(s_at + lanes + 32, s + 32);
+            umma::tensor_memory_loaded<64>(s);
+            const uint64_t times = both(P.scale2);
 #pragma unroll
             for (int c = 0; c < 64; c += 32) {
-                uint32_t u[32];
-                umma::tensor_memory_load(s_at + lanes + c, u);
-                umma::tensor_memory_loaded<32>(u);
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    float4 lse = make_float4(row_lse, row_lse, row_lse, row_lse);
-                    if (KEYS) lse = *(const float4 *)&by_column[j & 1][0][col0 + c + i];
-                    const float of[4] = {lse.x, lse.y, lse.z, lse.w};
+                for (int i = c; i < c + 32; i += 4) {
+                    uint64_t plus[2] = {both(far + (kShift - row_lse)), 0};
+                    plus[1] = plus[0];
+                    if (KEYS || near) {
+                        float4 lse = make_float4(row_lse, row_lse, row_lse, row_lse);
+                        if (KEYS) lse = *(const float4 *)&by_column[j & 1][0][col0 + i];
+                        float of[4] = {kShift - lse.x, kShift - lse.y, kShift - lse.z, kShift - lse.w};
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const float b = near ? distance[KEYS ? c + i + n : -(c + i + n)] : far;
-                        p[c + i + n] = exp2_fast(__fmaf_rn(__uint_as_float(u[i + n]), P.scale2, b + (kShift - of[n])));
+                        for (int n = 0; n < 4; ++n) of[n] += near ? distance[KEYS ? i + n : -(i + n)] : far;
+                        plus[0] = pair_of(__float_as_uint(of[0]), __float_as_uint(of[1]));
+                        plus[1] = pair_of(__float_as_uint(of[2]), __float_as_uint(of[3]));
+                    }
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) {
+                        const uint64_t x = fma_both(pair_of(s[i + 2 * n], s[i + 2 * n + 1]), times, plus[n]);
+                        p[i + 2 * n] = exp2_fast(low_of(x));
+                        p[i + 2 * n + 1] = exp2_fast(high_of(x));
                     }
                 }
                 if (masked) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (!counts(c + i)) p[c + i] = 0.0f;
+                    for (int i = c; i < c + 32; ++i)
+                        if (!counts(i)) p[i] = 0.0f;
                 }
                 if (KEYS) {
                     uint32_t w[16];
@@ -948,13 +1048,21 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                 umma::tensor_memory_loaded<32>(u);
 #pragma unroll
                 for (int i = 0; i < 32; i += 4) {
-                    float4 delta = make_float4(row_delta, row_delta, row_delta, row_delta);
-                    if (KEYS) delta = *(const float4 *)&by_column[j & 1][1][col0 + c + i];
-                    const float of[4] = {delta.x, delta.y, delta.z, delta.w};
+                    // delta has its sign turned
+                    uint64_t minus[2] = {both(row_delta), both(row_delta)};
+                    if (KEYS) {
+                        const uint4 delta = *(const uint4 *)&by_column[j & 1][1][col0 + c + i];
+                        minus[0] = pair_of(delta.x, delta.y);
+                        minus[1] = pair_of(delta.z, delta.w);
+                    }
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) {
-                        const float dp = kBf16 ? __uint_as_float(u[i + n]) - of[n] : __fmaf_rn(__uint_as_float(u[i + n]), unit_p, -of[n]);
-                        p[c + i + n] *= dp;
+                    for (int n = 0; n < 2; ++n) {
+                        const int at = c + i + 2 * n;
+                        const uint64_t dp = pair_of(u[i + 2 * n], u[i + 2 * n + 1]);
+                        const uint64_t x = mul_both(kBf16 ? add_both(dp, minus[n]) : fma_both(dp, both(unit_p), minus[n]),
+                                                    pair_of(__float_as_uint(p[at]), __float_as_uint(p[at + 1])));
+                        p[at] = low_of(x);
+                        p[at + 1] = high_of(x);
                     }
                 }
                 if (masked) {
@@ -973,41 +1081,49 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
             if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_ds));
             if (BIAS && !KEYS && P.partials != nullptr) {
                 if (!near) {
-                    float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    uint64_t part[4] = {0, 0, 0, 0};
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) part[c & 3] += p[c];
-                    far_sum += (part[0] + part[1]) + (part[2] + part[3]);
-                } else {
-                    // 32 rows x 16 columns at a time: lane l adds up diagonals l and l + 32 of the 47; equal buckets are
-                    // neighbours, summed across lanes in a fixed order
+                    for (int c = 0; c < 64; c += 2) part[c / 2 & 3] = add_both(part[c / 2 & 3], pair_of(__float_as_uint(p[c]), __float_as_uint(p[c + 1])));
+                    const uint64_t all = add_both(add_both(part[0], part[1]), add_both(part[2], part[3]));
+                    far_sum += low_of(all) + high_of(all);
+                } else if constexpr (BIAS) {
+                    // The warp's 32 rows x 64 columns have 95 diagonals, one distance each: lane l sums those of numbers l,
+                    // l + 32 and l + 64, read askew from shared memory 16 columns at a time (row r, column c: number
+                    // r - c + 63).  Then equal buckets are neighbours, summed across lanes in a fixed order.
                     float *stripe = stripes + warp * kStripeFloats, *mine = bucket_sums + warp * kMostBuckets;
+                    float sums[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int c = 0; c < 64; c += kStripe) {
 #pragma unroll
                         for (int i = 0; i < kStripe; ++i) stripe[lane * (kStripe + 1) + i] = row < left ? p[c + i] : 0.0f;
                         __syncwarp();
-                        // row r, column i: diagonal r - i + 15, distance apart * 128 + 32 quarter + r - (col0 + c + i)
-                        const int zero = apart * kTile + (warp & 3) * 32 - col0 - c - (kStripe - 1);
+                        // in columns 32 k .. 32 k + 31, row l + (c - 32 k) - 31 of lane l has number l + 32 (1 - k), and
+                        // 32 rows further down (where that is negative) number l + 32 (2 - k)
+                        const int high = c < 32 ? 2 : 1;
 #pragma unroll
-                        for (int turn = 0; turn < 2; ++turn) {
-                            const int diagonal_at = lane + turn * 32;
-                            float sum = 0.0f;
-                            for (int i = 0; i < kStripe; ++i) {
-                                const int r = diagonal_at + i - (kStripe - 1);
-                                if (r >= 0 && r < 32) sum += stripe[r * (kStripe + 1) + i];
-                            }
-                            const int d = zero + diagonal_at;
-                            const int bucket = d < 0 ? -1 : bucket_of(P.bias, d);
-#pragma unroll
-                            for (int n = 1; n < 32; n *= 2) {
-                                const float other = __shfl_down_sync(0xffffffffu, sum, n);
-                                const int its = __shfl_down_sync(0xffffffffu, bucket, n);
-                                if (lane + n < 32 && its == bucket) sum += other;
-                            }
-                            const int before = __shfl_up_sync(0xffffffffu, bucket, 1);
-                            if (bucket >= 0 && (lane == 0 || before != bucket)) mine[bucket] += sum;
-                            __syncwarp();
+                        for (int i = 0; i < kStripe; ++i) {
+                            const int r = lane + (c & 31) + i - 31;
+                            const float x = stripe[(r & 31) * (kStripe + 1) + i];
+                            if (r >= 0) sums[high - 1] += x;
+                            else sums[high] += x;
                         }
+                        __syncwarp();
+                    }
+                    const int zero = apart * kTile + (warp & 3) * 32 - col0 - 63;            // distance of diagonal 0
+#pragma unroll
+                    for (int n = 0; n < 3; ++n) {
+                        const int d = zero + lane + n * 32;
+                        const int bucket = d < 0 || n == 2 && lane == 31 ? -1 : tables.bucket[d];
+                        float sum = sums[n];
+#pragma unroll
+                        for (int k = 1; k < 32; k *= 2) {
+                            const float other = __shfl_down_sync(0xffffffffu, sum, k);
+                            const int its = __shfl_down_sync(0xffffffffu, bucket, k);
+                            if (lane + k < 32 && its == bucket) sum += other;
+                        }
+                        const int before = __shfl_up_sync(0xffffffffu, bucket, 1);
+                        if (bucket >= 0 && (lane == 0 || before != bucket)) mine[bucket] += sum;
+                        __syncwarp();
                     }
                 }
             }
