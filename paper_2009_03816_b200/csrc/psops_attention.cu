@@ -195,6 +195,19 @@ BackwardKernel backward_kernel(const psops_attention *a, size_t *shared)
     return a->cfg.type == PSOPS_F16 ? backward_kernel<__half, KEYS>(wide, bias) : backward_kernel<__nv_bfloat16, KEYS>(wide, bias);
 }
 
+Divisor divisor(uint32_t by)
+{
+    uint32_t shift = 0;
+    while (((uint32_t)1 << shift) < by) ++shift;
+    return Divisor{by, (uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by), 31 + shift};
+}
+
+// As many CTAs as run at once, or as there can be tiles.
+dim3 works_grid(const psops_attention *a, const PrepParams &L, int heads, int to_an_sm)
+{
+    return dim3((unsigned)std::min<int64_t>((int64_t)(L.capacity - 1) * heads, (int64_t)a->sms * to_an_sm));
+}
+
 Bias bias_of(const psops_attention *a, const void *bias, int32_t bias_type)
 {
     Bias b = a->bias;
@@ -287,7 +300,8 @@ int psops_attention_forward(psops_attention *a, const psops_heads *q, const psop
     P.count = L.count;
     P.tokens = (int)tokens;
     P.heads = H;
-    P.group = H / G;
+    P.by_heads = divisor(H);
+    P.by_group = divisor(H / G);
     P.dim = a->cfg.dim;
     P.scale2 = a->cfg.scale * kLog2e;
     P.out = O;
@@ -296,7 +310,7 @@ int psops_attention_forward(psops_attention *a, const psops_heads *q, const psop
     P.bias = bias_of(a, d_bias, bias_type);
     size_t shared;
     ForwardKernel kernel = forward_kernel(a, &shared);
-    return launch(a, "psops_attention_forward_kernel", kernel, dim3((unsigned)((L.capacity - 1) * H)), kForwardThreads, shared, 1, mq, mk, mv, P);
+    return launch(a, "psops_attention_forward_kernel", kernel, works_grid(a, L, H, 2), kForwardThreads, shared, 1, mq, mk, mv, P);
 }
 
 int psops_attention_backward(psops_attention *a, const psops_heads *q, const psops_heads *k, const psops_heads *v, const int32_t *d_offsets,
@@ -349,6 +363,7 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         P.tokens = (int)tokens;
         P.heads = H;
         P.group = H / G;
+        P.by_group = divisor(H / G);
         P.dim = a->cfg.dim;
         P.scale = a->cfg.scale;
         P.scale2 = a->cfg.scale * kLog2e;
@@ -364,16 +379,18 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         if (dk != nullptr || dv != nullptr) {
             if (dk != nullptr) P.out0 = heads_of(a, dk, tokens, G);
             if (dv != nullptr) P.out1 = heads_of(a, dv, tokens, G);
+            P.by_heads = divisor(G);
             BackwardKernel kernel = backward_kernel<true>(a, &shared);
-            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, dim3((unsigned)((L.capacity - 1) * G)), kBackwardThreads, shared, 1, mk, mv,
+            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, G, 1), kBackwardThreads, shared, 1, mk, mv,
                             mq, mg, P));
         }
         if (dq != nullptr || d_dbias != nullptr) {
             P.out0 = dq != nullptr ? heads_of(a, dq, tokens, H) : Heads{};
             P.out1 = Heads{};
             P.partials = d_dbias != nullptr ? a->at<float>(a->lay.partials) : nullptr;
+            P.by_heads = divisor(H);
             BackwardKernel kernel = backward_kernel<false>(a, &shared);
-            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, dim3((unsigned)((L.capacity - 1) * H)), kBackwardThreads, shared, 1, mq, mg,
+            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, H, 1), kBackwardThreads, shared, 1, mq, mg,
                             mk, mv, P));
         }
     }

@@ -31,8 +31,14 @@ constexpr int kTableFloats = kBefore + kMostDistance + 2 * kTile;
 constexpr int kPrepThreads = 512, kBins = 1024;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
+// Division of numbers below 2^31 by a number that the host knows.
+struct Divisor {
+    uint32_t by, factor, shift;
+};
+__device__ __forceinline__ uint32_t divide(uint32_t x, const Divisor &d) { return (uint32_t)(((uint64_t)x * d.factor) >> d.shift); }
+
 // A tile of a sequence.
-struct Item {
+struct alignas(16) Item {
     int first, length;       // first token and tokens of its sequence
     int level;               // its number, counted so that its work grows with it
     int slot;                // the same for the same tile of the same batch in any call
@@ -96,6 +102,20 @@ __device__ __forceinline__ float exp2_fast(float x)
     return y;
 }
 
+// Both to about 2^-23, relative and, of the logarithm of numbers near 1, absolute.
+__device__ __forceinline__ float reciprocal(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float log2_fast(float x)
+{
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // Two fp32 numbers in one instruction, each as by itself.
 __device__ __forceinline__ uint64_t pair_of(uint32_t low, uint32_t high)
 {
@@ -123,6 +143,35 @@ __device__ __forceinline__ uint64_t mul_both(uint64_t a, uint64_t b)
     uint64_t x;
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
     return x;
+}
+// 2^x of two numbers without the special-function unit, which has 16 results a clock
+// where a tile of products of dim 128 takes 16 scores a clock: 2^n times a
+// polynomial for 2^f, f in [-1/2, 1/2] (least largest relative error at degree 5, by
+// Remez's exchange: 1.5e-7 with these coefficients).  Below 2^-126 it is zero; NaN
+// stays NaN.
+__device__ __forceinline__ uint64_t exp2_both(uint64_t x)
+{
+    float a = low_of(x), b = high_of(x);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-127.0f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-127.0f));
+    x = pair_of(__float_as_uint(a), __float_as_uint(b));
+    const uint64_t t = add_both(x, both(12582912.0f));                       // 1.5 2^23 + n
+    const uint64_t f = fma_both(add_both(t, both(-12582912.0f)), both(-1.0f), x);
+    uint64_t p = both(0x1.5c08e6p-10f);
+    p = fma_both(p, f, both(0x1.3d0c52p-7f));
+    p = fma_both(p, f, both(0x1.c6b6e4p-5f));
+    p = fma_both(p, f, both(0x1.ebf918p-3f));
+    p = fma_both(p, f, both(0x1.62e428p-1f));
+    p = fma_both(p, f, both(1.0f));
+    return mul_both(p, pair_of(((uint32_t)t << 23) + 0x3f800000u, ((uint32_t)(t >> 32) << 23) + 0x3f800000u));
+}
+// Two probabilities; every OWN-th pair of a row by the polynomial (0: none).
+template <int OWN>
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x, int i)
+{
+    if constexpr (OWN > 0)
+        if (i % OWN == OWN - 1) return exp2_both(x);
+    return pair_of(__float_as_uint(exp2_fast(low_of(x))), __float_as_uint(exp2_fast(high_of(x))));
 }
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
@@ -197,20 +246,13 @@ __device__ __forceinline__ void make_list(const PrepParams &P)
             P.items[at] = Item{0, 0, 0, 0};                  // offsets that decrease
         }
     };
-    const int lane = threadIdx.x & 31;
-    for (int b0 = threadIdx.x & ~31; b0 < P.sequences; b0 += kPrepThreads) {
-        const int b = b0 + lane;
-        int first = 0, length = 0;
-        if (b < P.sequences) bounds(b, first, length);
-        const int tiles = (length + kTile - 1) / kTile, slot = first / kTile + b;
-        if (tiles <= 2)
-            for (int l = 0; l < tiles; ++l) place(first, length, slot, l);
-        for (uint32_t left = __ballot_sync(0xffffffffu, tiles > 2); left != 0; left &= left - 1) {
-            const int of = __ffs(left) - 1;
-            const int f = __shfl_sync(0xffffffffu, first, of), n = __shfl_sync(0xffffffffu, length, of);
-            const int s = __shfl_sync(0xffffffffu, slot, of), many = (n + kTile - 1) / kTile;
-            for (int l = lane; l < many; l += 32) place(f, n, s, l);
-        }
+    // a team of threads for each sequence: as many as there are for each, a warp at most
+    int team = 32;
+    while (team > 1 && team * P.sequences > kPrepThreads) team /= 2;
+    for (int b = threadIdx.x / team; b < P.sequences; b += kPrepThreads / team) {
+        int first, length;
+        bounds(b, first, length);
+        for (int l = threadIdx.x % team; l * kTile < length; l += team) place(first, length, first / kTile + b, l);
     }
 }
 
@@ -388,37 +430,36 @@ __device__ __forceinline__ void make_tables(const Bias &B, Tables &t)
     barrier_named(1, THREADS);
 }
 
-// Numbers that are not finite in a row of a tile (two boxes of 64 elements for
-// dim > 64) become zeros, so that a probability of zero meets none.  True if
-// there were any.  The row's eight 16-byte words are taken in the swizzle's order.
-template <class T>
-__device__ __forceinline__ bool clean_row(uint8_t *tile, int row, int halves)
+// acc + 0 x: stays zero as long as both halves of x are finite.
+template <class T> __device__ __forceinline__ uint32_t add_nothing(uint32_t acc, uint32_t x)
 {
-    bool any = false;
-    for (int h = 0; h < halves; ++h) {
-        uint8_t *at = tile + h * kHalfBytes + row * 128;
+    if (__is_same(T, __half)) asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(x), "r"(0u));
+    else asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(x), "r"(0u));
+    return acc;
+}
+// Numbers that are not finite among 64 elements of a row of a tile become zeros,
+// so that a probability of zero meets none.  True if there were any.  The eight
+// 16-byte words are taken in the swizzle's order.
+template <class T>
+__device__ __forceinline__ bool clean_row(uint8_t *half_tile, int row)
+{
+    uint4 *at = (uint4 *)(half_tile + row * 128);
+    uint32_t acc = 0;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            uint4 *word = (uint4 *)(at + ((c ^ (row & 7)) << 4));
-            uint4 w = *word;
-            uint32_t x[4] = {w.x, w.y, w.z, w.w};
-            constexpr uint32_t kExponent = __is_same(T, __half) ? 0x7c00u : 0x7f80u;
-            bool bad = false;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                bad |= (x[j] & kExponent) == kExponent || ((x[j] >> 16) & kExponent) == kExponent;
-            if (bad) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if ((x[j] & kExponent) == kExponent) x[j] &= 0xffff0000u;
-                    if (((x[j] >> 16) & kExponent) == kExponent) x[j] &= 0xffffu;
-                }
-                *word = make_uint4(x[0], x[1], x[2], x[3]);
-                any = true;
-            }
-        }
+    for (int c = 0; c < 8; ++c) {
+        const uint4 w = at[c ^ (row & 7)];
+        acc = add_nothing<T>(add_nothing<T>(add_nothing<T>(add_nothing<T>(acc, w.x), w.y), w.z), w.w);
     }
-    return any;
+    if ((acc & 0x7fff7fffu) == 0) return false;
+    constexpr uint32_t kExponent = __is_same(T, __half) ? 0x7c00u : 0x7f80u;
+#pragma unroll 1
+    for (int c = 0; c < 32; ++c) {
+        uint32_t &x = ((uint32_t *)at)[c];
+        if ((x & kExponent) == kExponent) x &= 0xffff0000u;
+        if (((x >> 16) & kExponent) == kExponent) x &= 0xffffu;
+    }
+    umma::copies_see_shared();
+    return true;
 }
 // What clean_row took away and a sum over rows from..to-1 should have met.
 template <class T>
@@ -437,11 +478,70 @@ __device__ __forceinline__ bool wait_all(const uint64_t *bar, uint32_t parity, v
     return __all_sync(0xffffffffu, umma::barrier_wait(umma::shared_address(bar), parity, failed));
 }
 
-// Eight results of a row, rounded to the 16-bit type.
-template <class T>
-__device__ __forceinline__ void put8(uint16_t *to, const float *x)
+// What a CTA does in turn k: tiles of the list, each with all heads before the
+// next, dealt out to the CTAs to and fro.  The list is in order of work, so that
+// all get about the same.
+struct Work {
+    Item item;
+    int head;
+    bool some;
+};
+__device__ __forceinline__ Work work_at(const Item *items, int total, const Divisor &heads, int k)
 {
-    *(uint4 *)to = make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
+    const uint32_t many = gridDim.x, i = k * many + (k & 1 ? many - 1 - blockIdx.x : blockIdx.x);
+    Work w{};
+    w.some = i < (uint32_t)total;
+    if (w.some) {
+        const uint32_t of = divide(i, heads);
+        const int4 x = *(const int4 *)(items + of);
+        w.item = Item{x.x, x.y, x.z, x.w};
+        w.head = (int)(i - of * heads.by);
+    }
+    return w;
+}
+
+// 32 columns from column c of a warp's 32 rows, out of tensor memory into rows of
+// 16-bit numbers.  A lane has a row; after four lanes have traded their quarters
+// of it (a transposition of 4 x 4 words of 16 bytes) they store 64 consecutive
+// bytes of one row together.  Row r is at to + r stride, `rows` of them exist.
+// fix(x): what else becomes of the lane's own row.
+template <class T, class Fix>
+__device__ __forceinline__ void put_rows(uint32_t from, float times, uint16_t *to, long long stride, int c, int dim, int rows, Fix &&fix)
+{
+    const int lane = threadIdx.x & 31;
+    uint32_t u[32];
+    umma::tensor_memory_load(from + c, u);
+    umma::tensor_memory_loaded<32>(u);
+    float x[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(u[i]) * times;
+    fix(x);
+    uint32_t w[4][4];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i / 4][i % 4] = pack2<T>(x[2 * i], x[2 * i + 1]);
+#pragma unroll
+    for (int bit = 1; bit <= 2; bit *= 2) {
+        const bool upper = lane & bit;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (q & bit) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t theirs = __shfl_xor_sync(0xffffffffu, upper ? w[q][i] : w[q | bit][i], bit);
+                if (upper) w[q][i] = theirs;
+                else w[q | bit][i] = theirs;
+            }
+        }
+    }
+    const int column = c + (lane & 3) * 8;
+    if (column < dim) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int r = (lane & ~3) + q;
+            if (r < rows) *(uint4 *)(to + r * stride + column) = make_uint4(w[q][0], w[q][1], w[q][2], w[q][3]);
+        }
+    }
+    __syncwarp();
 }
 
 // ---------------------------------------------------------------------------
@@ -455,24 +555,25 @@ template <> struct Choose<false> { using Type = None; };
 struct ForwardParams {
     const Item *items;
     const int *count;
-    int tokens, heads, group, dim;
+    int tokens, heads, dim;
+    Divisor by_heads, by_group;
     float scale2;                            // scale, base 2
     Heads out, v;
     float *lse;
     Bias bias;
 };
 
-constexpr int kForwardThreads = 192;         // four warps of softmax, one of copies, one of products
+constexpr int kForwardThreads = 320;         // eight warps of softmax, one of copies, one of products
+constexpr int kSoftmaxThreads = 256;
 constexpr float kLazy = 8.0f;                // a maximum moves only when it grows by more than this (base 2)
 
 template <int HALVES>
-constexpr int forward_shared() { return 1024 + (HALVES == 1 ? 5 : 3) * HALVES * kHalfBytes; }
+constexpr int forward_shared() { return 1024 + (HALVES == 1 ? 6 : 3) * HALVES * kHalfBytes; }
 
 // A CTA has 128 queries of one head; two CTAs share an SM, so that one's softmax
 // runs under the other's products.  Per tile of 128 keys: S = Q K^T into tensor
-// memory; each thread has one row of it, twice read (maximum; probabilities),
-// which needs no word from another thread; P goes back into tensor memory as the
-// left operand of O += P V.  For dim <= 64 the half of an SM's tensor memory that
+// memory; two threads have a row of it, 64 columns each, and tell one another
+// their maxima; P goes back into tensor memory as the left operand of O += P V.  For dim <= 64 the half of an SM's tensor memory that
 // a CTA has holds P beside S: the next scores are computed as soon as S has been
 // read, with two tiles of K and V under way.  For more, P takes the place of S.
 template <class T, int HALVES, bool BIAS>
@@ -484,250 +585,310 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
     constexpr int kTileBytes = HALVES * kHalfBytes;
     constexpr bool kAhead = HALVES == 1;
     constexpr int kStages = kAhead ? 2 : 1;
+    constexpr int kOwn = kAhead ? 8 : 0;
     // fp16 has no numbers below 2^-24: probabilities, at most 2^kLazy, are kept higher up
     constexpr float kShift = kBf16 ? 0.0f : 7.0f;
     extern __shared__ uint8_t raw[];
-    __shared__ alignas(8) uint64_t bar_q, bar_k_full[kStages], bar_k_empty[kStages], bar_v_full[kStages], bar_v_empty[kStages], bar_s,
-        bar_read, bar_p, bar_o;
+    __shared__ alignas(8) uint64_t bar_q_full[kStages], bar_q_empty[kStages], bar_k_full[kStages], bar_k_empty[kStages], bar_v_full[kStages],
+        bar_v_empty[kStages], bar_s, bar_read, bar_p[2], bar_o;
     __shared__ uint32_t tensor_base_slot;
-    __shared__ int failed_slot, dirty;
+    __shared__ int failed_slot, dirty[2];
+    __shared__ float other[2][2][kTile], other_sum[2][kTile];       // maxima (by parity of the tile) and sums of the rows' halves
     __shared__ typename Choose<BIAS>::Type tables;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &failed_slot;
-    umma::after_the_kernel_before();
-    const int head = blockIdx.x % P.heads;
-    const int index = blockIdx.x / P.heads;
-    if (index >= *P.count) return;
-    const Item item = P.items[index];
-    if (item.length <= 0) return;
-    const int tile = item.level, first = item.first + tile * kTile;
     uint8_t *tiles = raw + (((umma::shared_address(raw) + 1023u) & ~1023u) - umma::shared_address(raw));
-    const uint32_t q_at = umma::shared_address(tiles), k_at = q_at + kTileBytes, v_at = k_at + kStages * kTileBytes;
+    const uint32_t q_at = umma::shared_address(tiles), k_at = q_at + kStages * kTileBytes, v_at = k_at + kStages * kTileBytes;
 
     if (threadIdx.x == 0) {
-        for (uint64_t *b : {&bar_q, &bar_s, &bar_o}) umma::barrier_init(umma::shared_address(b), 1);
         for (int i = 0; i < kStages; ++i)
-            for (uint64_t *b : {&bar_k_full[i], &bar_k_empty[i], &bar_v_full[i], &bar_v_empty[i]}) umma::barrier_init(umma::shared_address(b), 1);
-        umma::barrier_init(umma::shared_address(&bar_read), 4);
-        umma::barrier_init(umma::shared_address(&bar_p), 4);
-        failed_slot = dirty = 0;
+            for (uint64_t *b : {&bar_q_full[i], &bar_q_empty[i], &bar_k_full[i], &bar_k_empty[i], &bar_v_full[i], &bar_v_empty[i]})
+                umma::barrier_init(umma::shared_address(b), 1);
+        umma::barrier_init(umma::shared_address(&bar_s), 1);
+        umma::barrier_init(umma::shared_address(&bar_o), 1);
+        umma::barrier_init(umma::shared_address(&bar_read), 8);
+        for (int i = 0; i < 2; ++i) umma::barrier_init(umma::shared_address(&bar_p[i]), 8);
+        failed_slot = dirty[0] = dirty[1] = 0;
         umma::barrier_init_done();
+        umma::prefetch_map(&map_q);
+        umma::prefetch_map(&map_k);
+        umma::prefetch_map(&map_v);
     }
-    if (warp == 5) umma::tensor_columns_take<256>(umma::shared_address(&tensor_base_slot));
+    if (warp == 9) umma::tensor_columns_take<256>(umma::shared_address(&tensor_base_slot));
     umma::fence_before();
     __syncthreads();
     umma::fence_after();
     const uint32_t s_at = tensor_base_slot, o_at = s_at + kTile, p_at = kAhead ? o_at + 64 : s_at;
 
-    if (warp == 4) {
+    umma::after_the_kernel_before();
+    const int total = *P.count * P.heads;
+    auto kv_of = [&](int head) { return (int)divide(head, P.by_group); };
+    Work coming = work_at(P.items, total, P.by_heads, 0);
+
+    if (warp == 8) {
         // ---- copies in; the tile on the diagonal comes first
-        const int kv = head / P.group;
         bool ok = true;
-        if (umma::elected()) {
-            umma::barrier_expect(umma::shared_address(&bar_q), kTileBytes);
-            for (int h = 0; h < HALVES; ++h)
-                umma::tensor_load3(q_at + h * kHalfBytes, &map_q, h * 64, head, first, umma::shared_address(&bar_q));
-        }
-        __syncwarp();
-        for (int j = 0; j <= tile && ok; ++j) {
-            const int token = first - j * kTile, stage = j % kStages;
-            const uint32_t phase = (j / kStages & 1) ^ 1;
-            ok = wait_all(&bar_k_empty[stage], phase, failed);
+        int t = 0, n = 0;                        // tiles and works before this one
+        for (int turn = 1; coming.some && ok; ++turn) {
+            const Work w = coming;
+            coming = work_at(P.items, total, P.by_heads, turn);
+            if (w.item.length <= 0) continue;
+            const int first = w.item.first + w.item.level * kTile, kv = kv_of(w.head), q_stage = n % kStages;
+            ok = wait_all(&bar_q_empty[q_stage], (n / kStages & 1) ^ 1, failed);
             if (!ok) break;
             if (umma::elected()) {
-                umma::barrier_expect(umma::shared_address(&bar_k_full[stage]), kTileBytes);
+                umma::barrier_expect(umma::shared_address(&bar_q_full[q_stage]), kTileBytes);
                 for (int h = 0; h < HALVES; ++h)
-                    umma::tensor_load3(k_at + stage * kTileBytes + h * kHalfBytes, &map_k, h * 64, kv, token, umma::shared_address(&bar_k_full[stage]));
+                    umma::tensor_load3(q_at + q_stage * kTileBytes + h * kHalfBytes, &map_q, h * 64, w.head, first, umma::shared_address(&bar_q_full[q_stage]));
             }
             __syncwarp();
-            ok = wait_all(&bar_v_empty[stage], phase, failed);
-            if (!ok) break;
-            if (umma::elected()) {
-                umma::barrier_expect(umma::shared_address(&bar_v_full[stage]), kTileBytes);
-                for (int h = 0; h < HALVES; ++h)
-                    umma::tensor_load3(v_at + stage * kTileBytes + h * kHalfBytes, &map_v, h * 64, kv, token, umma::shared_address(&bar_v_full[stage]));
+            ++n;
+            for (int j = 0; j <= w.item.level; ++j, ++t) {
+                const int token = first - j * kTile, stage = t % kStages;
+                const uint32_t phase = (t / kStages & 1) ^ 1;
+                ok = wait_all(&bar_k_empty[stage], phase, failed);
+                if (!ok) break;
+                if (umma::elected()) {
+                    umma::barrier_expect(umma::shared_address(&bar_k_full[stage]), kTileBytes);
+                    for (int h = 0; h < HALVES; ++h)
+                        umma::tensor_load3(k_at + stage * kTileBytes + h * kHalfBytes, &map_k, h * 64, kv, token, umma::shared_address(&bar_k_full[stage]));
+                }
+                __syncwarp();
+                ok = wait_all(&bar_v_empty[stage], phase, failed);
+                if (!ok) break;
+                if (umma::elected()) {
+                    umma::barrier_expect(umma::shared_address(&bar_v_full[stage]), kTileBytes);
+                    for (int h = 0; h < HALVES; ++h)
+                        umma::tensor_load3(v_at + stage * kTileBytes + h * kHalfBytes, &map_v, h * 64, kv, token, umma::shared_address(&bar_v_full[stage]));
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
         if (!ok) __nanosleep(1000000);           // copies in flight land long before
-    } else if (warp == 5) {
+    } else if (warp == 9) {
         // ---- products; they run in the order in which they are issued, so S may follow P V without a wait
         const int steps = (P.dim + 15) / 16;
         const uint32_t instr_s = umma::instruction(kBf16, false, false, kTile, kTile);
         const uint32_t instr_o = umma::instruction(kBf16, false, true, kTile, steps * 16);
         const uint64_t dq = umma::operand(q_at, false), dk = umma::operand(k_at, false), dv = umma::operand(v_at, true, kHalfBytes);
-        auto scores = [&](int j) {
-            const int stage = j % kStages;
-            if (!wait_all(&bar_k_full[stage], j / kStages & 1, failed)) return false;
-            if (kAhead && j > 0 && !wait_all(&bar_read, (j & 1) ^ 1, failed)) return false;
+        constexpr uint32_t kNext = kTileBytes >> 4;
+        // scores of tile t, the `j`th of work n
+        auto scores = [&](int t, int n, int j, int last) {
+            const int stage = t % kStages, q_stage = n % kStages;
+            if (j == 0 && !wait_all(&bar_q_full[q_stage], n / kStages & 1, failed)) return false;
+            if (!wait_all(&bar_k_full[stage], t / kStages & 1, failed)) return false;
+            if (kAhead && t > 0 && !wait_all(&bar_read, (t & 1) ^ 1, failed)) return false;
             umma::fence_after();
             if (umma::elected()) {
                 for (int s = 0; s < steps; ++s) {
                     const uint32_t on = (s >> 2) * (kHalfBytes >> 4) + (s & 3) * 2;
-                    umma::multiply<false>(s_at, dq + on, dk + stage * (kTileBytes >> 4) + on, instr_s, s > 0);
+                    umma::multiply<false>(s_at, dq + q_stage * kNext + on, dk + stage * kNext + on, instr_s, s > 0);
                 }
                 umma::products_arrive<false>(umma::shared_address(&bar_s));
                 umma::products_arrive<false>(umma::shared_address(&bar_k_empty[stage]));
+                if (j == last) umma::products_arrive<false>(umma::shared_address(&bar_q_empty[q_stage]));
             }
             __syncwarp();
             return true;
         };
-        bool ok = wait_all(&bar_q, 0, failed) && scores(0);
-        for (int j = 0; j <= tile && ok; ++j) {
-            const int stage = j % kStages;
-            if (kAhead && j < tile && !scores(j + 1)) break;
-            ok = wait_all(&bar_v_full[stage], j / kStages & 1, failed) && wait_all(&bar_p, j & 1, failed);
-            if (!ok) break;
-            umma::fence_after();
-            if (umma::elected()) {
-#pragma unroll
-                for (int s = 0; s < kTile / 16; ++s)
-                    umma::multiply_from_tensor_memory(o_at, p_at + s * 8, dv + stage * (kTileBytes >> 4) + s * 128, instr_o, j > 0 || s > 0);
-                umma::products_arrive<false>(umma::shared_address(&bar_v_empty[stage]));
-                umma::products_arrive<false>(umma::shared_address(&bar_o));
+        int t = 0, n = 0, turn = 1;
+        auto next_work = [&]() {                 // the next one with tokens
+            Work w = coming;
+            while (w.some) {
+                coming = work_at(P.items, total, P.by_heads, turn++);
+                if (w.item.length > 0) break;
+                w = coming;
             }
-            __syncwarp();
-            if (!kAhead && j < tile) ok = scores(j + 1);
+            return w;
+        };
+        Work w = next_work();
+        bool ok = !w.some || scores(0, 0, 0, w.item.level);
+        while (w.some && ok) {
+            const Work then = next_work();
+            for (int j = 0; j <= w.item.level; ++j, ++t) {
+                const int stage = t % kStages;
+                // the scores after these: of the next tile, or of the next work's first one
+                auto ahead = [&]() {
+                    return j < w.item.level ? scores(t + 1, n, j + 1, w.item.level) : !then.some || scores(t + 1, n + 1, 0, then.item.level);
+                };
+                if (kAhead) ok = ahead();
+                ok = ok && wait_all(&bar_v_full[stage], t / kStages & 1, failed);
+                // the first 32 columns of both halves of a row, then the others
+                for (int part = 0; part < 2 && ok; ++part) {
+                    ok = wait_all(&bar_p[part], t & 1, failed);
+                    if (!ok) break;
+                    umma::fence_after();
+                    if (umma::elected()) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            // 16 keys s of the tile; P's columns are 0-63, or 0-31 and 64-95 where it lies in S
+                            const int s = (i >> 1) * 4 + part * 2 + (i & 1);
+                            umma::multiply_from_tensor_memory(o_at, p_at + (i >> 1) * (kAhead ? 32 : 64) + (part * 2 + (i & 1)) * 8,
+                                                              dv + stage * kNext + s * 128, instr_o, j > 0 || part > 0 || i > 0);
+                        }
+                        if (part == 1) {
+                            umma::products_arrive<false>(umma::shared_address(&bar_v_empty[stage]));
+                            umma::products_arrive<false>(umma::shared_address(&bar_o));
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (!ok) break;
+                if (!kAhead && !(ok = ahead())) break;
+            }
+            ++n;
+            w = then;
         }
     } else {
-        // ---- softmax: one query a thread
-        const int row = threadIdx.x;
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        // ---- softmax: half a row a thread
+        const int half = warp >> 2, row = threadIdx.x & (kTile - 1), col0 = half * 64;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const int o_begin = half * 32 * HALVES, o_end = min(o_begin + 32 * HALVES, P.dim);      // its columns of O
         float far = 0.0f;
         const float *table = nullptr;
-        if constexpr (BIAS) {
-            if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, head) : 0.0f;
-            make_tables<kTile, true>(P.bias, tables);
-            table = tables.distance + kBefore;
-            far = tables.value[P.bias.buckets - 1];
-        }
-        float top = -INFINITY, sum = 0.0f;       // top: what is subtracted, base 2
+        if constexpr (BIAS) table = tables.distance + kBefore;
+        // where it is not, all works are gone through all the same, without waits, for the barriers in them
         bool ok = true;
-        for (int j = 0; j <= tile; ++j) {
-            ok = wait_all(&bar_s, j & 1, failed);
-            if (!ok) break;
-            umma::fence_after();
-            const bool diagonal = j == 0, near = BIAS && j * kTile - (kTile - 1) < P.bias.last;
-            const float *distance = table + j * kTile + row;                  // - column
-            // the row, in two halves so that the second is on its way under the first's maximum; with a bias it becomes
-            // the whole exponent here, else scale and bias come with the exponential
-            uint32_t s[kTile];
-            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            umma::tensor_memory_load(s_at + lanes, s);
-            umma::tensor_memory_load(s_at + lanes + 32, s + 32);
-            umma::tensor_memory_loaded<64>(s);
-            umma::tensor_memory_load(s_at + lanes + 64, s + 64);
-            umma::tensor_memory_load(s_at + lanes + 96, s + 96);
-#pragma unroll
-            for (int c = 0; c < kTile; c += 64) {
-                if (c > 0) umma::tensor_memory_loaded<64>(s + c);
+        int t = 0, n = 0, head_before = -1;
+        for (int turn = 1; coming.some; ++turn) {
+            const Work w = coming;
+            coming = work_at(P.items, total, P.by_heads, turn);
+            if (w.item.length <= 0) continue;
+            const int tile = w.item.level, first = w.item.first + tile * kTile;
+            if constexpr (BIAS) {
+                if (w.head != head_before) {
+                    if (threadIdx.x < kMostBuckets)
+                        tables.value[threadIdx.x] = threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, w.head) : 0.0f;
+                    if (n == 0) make_tables<kSoftmaxThreads, true>(P.bias, tables);
+                    else make_tables<kSoftmaxThreads, false>(P.bias, tables);
+                    far = tables.value[P.bias.buckets - 1];
+                    head_before = w.head;
+                }
+            }
+            float top = -INFINITY, sum = 0.0f;   // top: what is subtracted, base 2
+            for (int j = 0; j <= tile; ++j, ++t) {
+                ok = ok && wait_all(&bar_s, t & 1, failed);
+                umma::fence_after();
+                const bool diagonal = j == 0, near = BIAS && j * kTile - (kTile - 1) < P.bias.last;
+                const float *distance = table + j * kTile + row - col0;           // - column
+                // half a row; with a bias it becomes the whole exponent here, else scale and bias come with the exponential
+                uint32_t s[64];
+                float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                umma::tensor_memory_load(s_at + lanes + col0, s);
+                umma::tensor_memory_load(s_at + lanes + col0 + 32, s + 32);
+                umma::tensor_memory_loaded<64>(s);
                 if (near) {
 #pragma unroll
-                    for (int i = c; i < c + 64; ++i) s[i] = __float_as_uint(__fmaf_rn(__uint_as_float(s[i]), P.scale2, distance[-i]));
+                    for (int i = 0; i < 64; ++i) s[i] = __float_as_uint(__fmaf_rn(__uint_as_float(s[i]), P.scale2, distance[-i]));
                 }
                 if (diagonal) {
 #pragma unroll
-                    for (int i = c; i < c + 64; ++i)
-                        if (i > row) s[i] = 0xff800000u;                     // -inf
+                    for (int i = 0; i < 64; ++i)
+                        if (col0 + i > row) s[i] = 0xff800000u;              // -inf
                 }
 #pragma unroll
-                for (int i = c; i < c + 64; i += 8)
+                for (int i = 0; i < 64; i += 8)
 #pragma unroll
-                    for (int n = 0; n < 4; ++n) most[n] = max3(most[n], __uint_as_float(s[i + 2 * n]), __uint_as_float(s[i + 2 * n + 1]));
-            }
-            if (kAhead) {
-                umma::fence_before();
-                __syncwarp();
-                if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_read));
-            }
-            float higher = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-            if (!near) higher = __fmaf_rn(higher, P.scale2, far);
-            if (kAhead && j > 0) {               // else bar_s has said so: the sums of the tile before are complete
-                ok = wait_all(&bar_o, (j & 1) ^ 1, failed);
-                if (!ok) break;
-                umma::fence_after();
-            }
-            if (__any_sync(0xffffffffu, higher > top + kLazy)) {
-                higher = fmaxf(higher, top);
-                const float factor = higher > -INFINITY ? exp2_fast(top - higher) : 1.0f;
-                top = higher;
-                sum *= factor;
-                if (j > 0) {
-                    for (int c = 0; c < P.dim; c += 16) {
-                        uint32_t u[16];
-                        umma::tensor_memory_load16(o_at + lanes + c, u);
-                        umma::tensor_memory_loaded<16>(u);
+                    for (int m = 0; m < 4; ++m) most[m] = max3(most[m], __uint_as_float(s[i + 2 * m]), __uint_as_float(s[i + 2 * m + 1]));
+                if (kAhead) {
+                    umma::fence_before();
+                    __syncwarp();
+                    if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_read));
+                }
+                float higher = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+                other[t & 1][half][row] = higher;
+                barrier_named(2 + (warp & 3), 64);                           // the two warps that have these rows
+                higher = fmaxf(higher, other[t & 1][half ^ 1][row]);
+                if (!near) higher = __fmaf_rn(higher, P.scale2, far);
+                if (kAhead && t > 0) {           // else bar_s has said so: the product of the tile before is complete
+                    ok = ok && wait_all(&bar_o, (t & 1) ^ 1, failed);
+                    umma::fence_after();
+                }
+                if (__any_sync(0xffffffffu, higher > top + kLazy)) {
+                    higher = fmaxf(higher, top);
+                    const float factor = higher > -INFINITY ? exp2_fast(top - higher) : 1.0f;
+                    top = higher;
+                    sum *= factor;
+                    if (j > 0) {
+                        for (int c = o_begin; c < o_end; c += 16) {
+                            uint32_t u[16];
+                            umma::tensor_memory_load16(o_at + lanes + c, u);
+                            umma::tensor_memory_loaded<16>(u);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * factor);
-                        umma::tensor_memory_store16(o_at + lanes + c, u);
+                            for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * factor);
+                            umma::tensor_memory_store16(o_at + lanes + c, u);
+                        }
                     }
                 }
-            }
-            const float base = (near ? 0.0f : far) + kShift - (top > -INFINITY ? top : 0.0f);
-            const uint64_t times = both(near ? 1.0f : P.scale2), plus = both(base);
-            uint64_t parts[4] = {0, 0, 0, 0};
+                const float base = (near ? 0.0f : far) + kShift - (top > -INFINITY ? top : 0.0f);
+                const uint64_t times = both(near ? 1.0f : P.scale2), plus = both(base);
+                uint64_t parts[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int c = 0; c < kTile; c += 32) {
-                uint32_t p[16];
+                for (int c = 0; c < 64; c += 32) {
+                    uint32_t p[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint64_t x = fma_both(pair_of(s[c + 2 * i], s[c + 2 * i + 1]), times, plus);
-                    const float2 e = make_float2(exp2_fast(low_of(x)), exp2_fast(high_of(x)));
-                    parts[i & 3] = add_both(parts[i & 3], pair_of(__float_as_uint(e.x), __float_as_uint(e.y)));
-                    p[i] = pack2<T>(e.x, e.y);
+                    for (int i = 0; i < 16; ++i) {
+                        const uint64_t x = fma_both(pair_of(s[c + 2 * i], s[c + 2 * i + 1]), times, plus);
+                        const uint64_t e = exp2_pair<kOwn>(x, i);
+                        parts[i & 3] = add_both(parts[i & 3], e);
+                        p[i] = pack2<T>(low_of(e), high_of(e));
+                    }
+                    umma::tensor_memory_store16(p_at + lanes + (kAhead ? half * 32 : col0) + c / 2, p);
+                    if (!diagonal) {
+                        umma::tensor_memory_stored();
+                        umma::fence_before();
+                        __syncwarp();
+                        if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_p[c / 32]));
+                    }
                 }
-                umma::tensor_memory_store16(p_at + lanes + c / 2, p);
-            }
-            const uint64_t all = add_both(add_both(parts[0], parts[1]), add_both(parts[2], parts[3]));
-            const float here = low_of(all) + high_of(all);
-            sum += here;
-            if (diagonal) {
-                // keys that are masked here may hold anything: rows of the next sequence, or of none
-                ok = wait_all(&bar_v_full[0], 0, failed);
-                if (!ok) break;
-                if (clean_row<T>(tiles + (1 + kStages) * kTileBytes, row, HALVES)) dirty = 1;
-                umma::copies_see_shared();
-            }
-            umma::tensor_memory_stored();
-            umma::fence_before();
-            __syncwarp();
-            if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_p));
-        }
-        if (ok) ok = wait_all(&bar_o, tile & 1, failed);
-        umma::fence_after();
-        barrier_named(1, kTile);
-        const bool poisoned = *(volatile int *)&dirty != 0;
-        const int left = item.length - tile * kTile;                          // queries of this tile
-        const float unit = !ok || *failed ? NAN : sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-        const long long token = first + row;
-        uint16_t *out = (uint16_t *)P.out.p + token * P.out.token + head * P.out.head;
-        const uint16_t *v = (const uint16_t *)P.v.p + (long long)first * P.v.token + head / P.group * P.v.head;
-        for (int c = 0; c < P.dim; c += 16) {
-            uint32_t u[16];
-            umma::tensor_memory_load16(o_at + lanes + c, u);
-            umma::tensor_memory_loaded<16>(u);
-            if (row < left) {
-                float x[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(u[i]) * unit;
-                if (poisoned) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (c + i < P.dim) x[i] += taken_away<T>(v + c + i, P.v.token, 0, row + 1);
+                const uint64_t all = add_both(add_both(parts[0], parts[1]), add_both(parts[2], parts[3]));
+                sum += low_of(all) + high_of(all);
+                if (diagonal) {
+                    // keys that are masked here may hold anything: rows of the next sequence, or of none
+                    ok = ok && wait_all(&bar_v_full[t % kStages], t / kStages & 1, failed);
+                    if (half < HALVES && clean_row<T>(tiles + (2 * kStages + t % kStages) * kTileBytes + half * kHalfBytes, row)) dirty[n & 1] = 1;
+                    umma::tensor_memory_stored();
+                    umma::fence_before();
+                    __syncwarp();
+                    if (lane == 0)
+                        for (int i = 0; i < 2; ++i) umma::barrier_arrive(umma::shared_address(&bar_p[i]));
                 }
-                put8<T>(out + c, x);
-                if (c + 8 < P.dim) put8<T>(out + c + 8, x + 8);
             }
-            __syncwarp();
+            // while the last product runs: the sum, and all that does not need O
+            const int left = w.item.length - tile * kTile;                        // queries of this tile
+            uint16_t *out = (uint16_t *)P.out.p + (long long)(first + (warp & 3) * 32) * P.out.token + w.head * P.out.head;
+            other_sum[half][row] = sum;
+            barrier_named(2 + (warp & 3), 64);
+            sum += other_sum[half ^ 1][row];
+            float unit = sum > 0.0f || sum != sum ? reciprocal(sum) : 0.0f;
+            if (half == 0 && row < left)
+                P.lse[(long long)w.head * P.tokens + first + row] = sum == 0.0f ? -INFINITY : (top + (log2_fast(sum) - kShift)) * kLn2;
+            ok = ok && wait_all(&bar_o, (t & 1) ^ 1, failed);
+            umma::fence_after();
+            if (threadIdx.x == 0) dirty[(n & 1) ^ 1] = 0;                         // read by all in the work before
+            barrier_named(1, kSoftmaxThreads);
+            const bool poisoned = *(volatile int *)&dirty[n & 1] != 0;
+            if (!ok || *failed) {
+                unit = NAN;
+                if (half == 0 && row < left) P.lse[(long long)w.head * P.tokens + first + row] = NAN;
+            }
+            for (int c = o_begin; c < o_end; c += 32)
+                put_rows<T>(o_at + lanes, unit, out, P.out.token, c, P.dim, left - (warp & 3) * 32, [&](float *x) {
+                    if (!poisoned) return;
+                    const uint16_t *v = (const uint16_t *)P.v.p + (long long)first * P.v.token + kv_of(w.head) * P.v.head;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c + i < o_end && row < left) x[i] += taken_away<T>(v + c + i, P.v.token, 0, row + 1);
+                });
+            ++n;
         }
-        if (row < left) P.lse[(long long)head * P.tokens + token] = !ok || *failed ? NAN : sum == 0.0f ? -INFINITY : (top + (log2f(sum) - kShift)) * kLn2;
     }
     __syncwarp();
     umma::fence_before();
     __syncthreads();
     umma::fence_after();
-    if (warp == 5) umma::tensor_columns_give<256>(tensor_base_slot);
+    if (warp == 9) umma::tensor_columns_give<256>(tensor_base_slot);
 }
 
 // ---------------------------------------------------------------------------
@@ -738,6 +899,7 @@ struct BackwardParams {
     const Item *items;
     const int *count;
     int tokens, heads, group, dim;
+    Divisor by_heads, by_group;              // the heads of A0
     float scale, scale2;
     Heads q, k, grad;                        // read where numbers are not finite
     Heads out0, out1;                        // dq; or dk and dv
@@ -748,8 +910,7 @@ struct BackwardParams {
     float *partials;                         // dbias by slot, head and bucket; NULL: not wanted
 };
 
-constexpr int kBackwardThreads = 320;        // eight warps of softmax, one of copies, one of products
-constexpr int kSoftmaxThreads = 256;
+constexpr int kBackwardThreads = 320;        // as above
 constexpr int kStripe = 16;                  // columns of ds that are summed along their diagonals at a time
 constexpr int kStripeFloats = 32 * (kStripe + 1);
 
@@ -780,45 +941,43 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
 {
     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
     constexpr int kTileBytes = HALVES * kHalfBytes;
+    constexpr int kOwn = 4;
+    // scores in two places by turns, where tensor memory has room for them: the next ones need not wait for these
+    constexpr bool kTwice = !KEYS || HALVES == 1;
+    constexpr uint32_t kSecond = 3 * kTile;                                 // columns 384 to 511
     // fp16: probabilities are kept 2^14 times as large (dv is scaled back), ds by a power of two from the norms
     constexpr float kShift = kBf16 ? 0.0f : 14.0f;
     extern __shared__ uint8_t raw[];
-    __shared__ alignas(8) uint64_t bar_a, bar_b_full[2], bar_b_empty[2], bar_s, bar_t, bar_p, bar_ds, bar_sums;
+    __shared__ alignas(8) uint64_t bar_a_full, bar_a_empty, bar_b_full[2], bar_b_empty[2], bar_s[2], bar_t, bar_p, bar_ds, bar_sums;
     __shared__ uint32_t tensor_base_slot;
-    __shared__ int failed_slot, dirty0, dirty1;
+    __shared__ int failed_slot, dirty[2][2];                                // by parity of the work, and which of B
     __shared__ float2 most[kBackwardThreads / 32];
-    __shared__ float by_column[KEYS ? 2 : 1][2][kTile];                     // lse and delta of the queries
+    __shared__ alignas(16) float by_column[KEYS ? 2 : 1][2][kTile];         // lse and delta of the queries
     __shared__ typename Choose<BIAS>::Type tables;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int *failed = &failed_slot;
-    umma::after_the_kernel_before();
-    const int kv_heads = P.heads / P.group;
-    const int grid_heads = KEYS ? kv_heads : P.heads;
-    const int head = blockIdx.x % grid_heads;                               // of A0
-    const int index = blockIdx.x / grid_heads;
-    if (index >= *P.count) return;
-    const Item item = P.items[index];
-    if (item.length <= 0) return;
-    const int tiles_of = (item.length + kTile - 1) / kTile;
-    const int tile = KEYS ? tiles_of - 1 - item.level : item.level;         // the work is level + 1 tiles (of each head)
-    const int first = item.first + tile * kTile;
-    const int meets = item.level + 1, rounds = KEYS ? meets * P.group : meets;
     uint8_t *tiles = raw + (((umma::shared_address(raw) + 1023u) & ~1023u) - umma::shared_address(raw));
     const uint32_t a_at = umma::shared_address(tiles), b_at = a_at + 2 * kTileBytes;
     float *stripes = (float *)(tiles + 6 * kTileBytes), *bucket_sums = stripes + 8 * kStripeFloats;
 
     if (threadIdx.x == 0) {
-        for (uint64_t *b : {&bar_a, &bar_b_full[0], &bar_b_full[1], &bar_b_empty[0], &bar_b_empty[1], &bar_s, &bar_t, &bar_sums})
+        for (uint64_t *b : {&bar_a_full, &bar_a_empty, &bar_b_full[0], &bar_b_full[1], &bar_b_empty[0], &bar_b_empty[1], &bar_s[0], &bar_s[1], &bar_t, &bar_sums})
             umma::barrier_init(umma::shared_address(b), 1);
         umma::barrier_init(umma::shared_address(&bar_p), 8);
         umma::barrier_init(umma::shared_address(&bar_ds), 8);
-        failed_slot = dirty0 = dirty1 = 0;
+        failed_slot = 0;
+        dirty[0][0] = dirty[0][1] = dirty[1][0] = dirty[1][1] = 0;
         umma::barrier_init_done();
+        umma::prefetch_map(&map_a0);
+        umma::prefetch_map(&map_a1);
+        umma::prefetch_map(&map_b0);
+        umma::prefetch_map(&map_b1);
     }
     if (warp == 9) umma::tensor_columns_take<512>(umma::shared_address(&tensor_base_slot));
     if (BIAS && !KEYS)
         for (int i = threadIdx.x; i < 8 * kMostBuckets; i += kBackwardThreads) bucket_sums[i] = 0.0f;
+    umma::after_the_kernel_before();
     if (!kBf16) {
         float2 m = make_float2(0.0f, 0.0f);
         for (int i = threadIdx.x; i < P.blocks; i += kBackwardThreads) m = make_float2(fmaxf(m.x, P.norms[i].x), fmaxf(m.y, P.norms[i].y));
@@ -831,33 +990,48 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
     __syncthreads();
     umma::fence_after();
     const uint32_t s_at = tensor_base_slot, t_at = s_at + kTile, sum0_at = t_at + kTile, sum1_at = sum0_at + HALVES * 64;
-    // the tile of B in round j: !KEYS from the diagonal down, KEYS from the diagonal up, head after head
-    auto token_of = [&](int j) { return KEYS ? first + (j % meets) * kTile : first - j * kTile; };
+
+    const int total = *P.count * (int)P.by_heads.by;
+    auto kv_of = [&](int head) { return (int)divide(head, P.by_group); };
+    Work coming = work_at(P.items, total, P.by_heads, 0);
+    // A tile meets level + 1 tiles of B (of each head): !KEYS from the diagonal down, KEYS from the diagonal up.
+    auto tile_of = [](const Work &w) { return KEYS ? (w.item.length + kTile - 1) / kTile - 1 - w.item.level : w.item.level; };
+    auto token_of = [](int first, int meets, int j) { return KEYS ? first + (j % meets) * kTile : first - j * kTile; };
 
     if (warp == 8) {
         // ---- copies in
         bool ok = true;
-        if (umma::elected()) {
-            umma::barrier_expect(umma::shared_address(&bar_a), 2 * kTileBytes);
-            for (int h = 0; h < HALVES; ++h) {
-                umma::tensor_load3(a_at + h * kHalfBytes, &map_a0, h * 64, head, first, umma::shared_address(&bar_a));
-                umma::tensor_load3(a_at + kTileBytes + h * kHalfBytes, &map_a1, h * 64, head, first, umma::shared_address(&bar_a));
-            }
-        }
-        __syncwarp();
-        for (int j = 0; j < rounds && ok; ++j) {
-            const int stage = j & 1, token = token_of(j), b_head = KEYS ? head * P.group + j / meets : head / P.group;
-            ok = wait_all(&bar_b_empty[stage], (j >> 1 & 1) ^ 1, failed);
+        int r = 0, n = 0;                        // rounds and works before this one
+        for (int turn = 1; coming.some && ok; ++turn) {
+            const Work w = coming;
+            coming = work_at(P.items, total, P.by_heads, turn);
+            if (w.item.length <= 0) continue;
+            const int first = w.item.first + tile_of(w) * kTile, meets = w.item.level + 1, rounds = KEYS ? meets * P.group : meets;
+            ok = wait_all(&bar_a_empty, (n & 1) ^ 1, failed);
             if (!ok) break;
             if (umma::elected()) {
-                const uint32_t to = b_at + stage * 2 * kTileBytes, full = umma::shared_address(&bar_b_full[stage]);
-                umma::barrier_expect(full, 2 * kTileBytes);
+                umma::barrier_expect(umma::shared_address(&bar_a_full), 2 * kTileBytes);
                 for (int h = 0; h < HALVES; ++h) {
-                    umma::tensor_load3(to + h * kHalfBytes, &map_b0, h * 64, b_head, token, full);
-                    umma::tensor_load3(to + kTileBytes + h * kHalfBytes, &map_b1, h * 64, b_head, token, full);
+                    umma::tensor_load3(a_at + h * kHalfBytes, &map_a0, h * 64, w.head, first, umma::shared_address(&bar_a_full));
+                    umma::tensor_load3(a_at + kTileBytes + h * kHalfBytes, &map_a1, h * 64, w.head, first, umma::shared_address(&bar_a_full));
                 }
             }
             __syncwarp();
+            ++n;
+            for (int j = 0; j < rounds; ++j, ++r) {
+                const int stage = r & 1, token = token_of(first, meets, j), b_head = KEYS ? w.head * P.group + j / meets : kv_of(w.head);
+                ok = wait_all(&bar_b_empty[stage], (r >> 1 & 1) ^ 1, failed);
+                if (!ok) break;
+                if (umma::elected()) {
+                    const uint32_t to = b_at + stage * 2 * kTileBytes, full = umma::shared_address(&bar_b_full[stage]);
+                    umma::barrier_expect(full, 2 * kTileBytes);
+                    for (int h = 0; h < HALVES; ++h) {
+                        umma::tensor_load3(to + h * kHalfBytes, &map_b0, h * 64, b_head, token, full);
+                        umma::tensor_load3(to + kTileBytes + h * kHalfBytes, &map_b1, h * 64, b_head, token, full);
+                    }
+                }
+                __syncwarp();
+            }
         }
         if (!ok) __nanosleep(1000000);           // copies in flight land long before
     } else if (warp == 9) {
@@ -869,59 +1043,84 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
         const uint64_t db_across = umma::operand(b_at, true, kHalfBytes);
         constexpr uint32_t kNext = kTileBytes >> 4;                          // from A0 to A1, from B0 to B1
         // which: 0 scores, 1 dp
-        auto scores = [&](int j, int which) {
-            const uint32_t stage = (j & 1) * 2 * kNext + which * kNext;
+        auto scores = [&](int r, int which) {
+            const uint32_t stage = (r & 1) * 2 * kNext + which * kNext;
             if (umma::elected()) {
                 for (int s = 0; s < steps; ++s) {
                     const uint32_t on = (s >> 2) * (kHalfBytes >> 4) + (s & 3) * 2;
-                    umma::multiply<false>(which ? t_at : s_at, da + which * kNext + on, db + stage + on, instr_s, s > 0);
+                    umma::multiply<false>(which ? t_at : s_at + (kTwice && (r & 1) ? kSecond : 0), da + which * kNext + on, db + stage + on, instr_s, s > 0);
                 }
-                umma::products_arrive<false>(umma::shared_address(which ? &bar_t : &bar_s));
+                umma::products_arrive<false>(umma::shared_address(which ? &bar_t : &bar_s[kTwice ? r & 1 : 0]));
             }
             __syncwarp();
         };
-        auto add = [&](int j, int which, uint32_t from, uint32_t to) {
+        auto add = [&](int r, int j, int which, uint32_t from, uint32_t to) {
             if (umma::elected()) {
 #pragma unroll
                 for (int s = 0; s < kTile / 16; ++s)        // columns 0-31 and 64-95 hold the halves
-                    umma::multiply_from_tensor_memory(to, from + (s >> 2) * 64 + (s & 3) * 8, db_across + (j & 1) * 2 * kNext + which * kNext + s * 128,
+                    umma::multiply_from_tensor_memory(to, from + (s >> 2) * 64 + (s & 3) * 8, db_across + (r & 1) * 2 * kNext + which * kNext + s * 128,
                                                       instr_sum, j > 0 || s > 0);
             }
             __syncwarp();
         };
-        bool ok = wait_all(&bar_a, 0, failed) && wait_all(&bar_b_full[0], 0, failed);
-        if (ok) {
-            umma::fence_after();
-            scores(0, 0);
-            scores(0, 1);
-        }
-        for (int j = 0; j < rounds && ok; ++j) {
-            ok = wait_all(&bar_p, j & 1, failed);
+        bool ok = true;
+        int r = 0, n = 0;
+        for (int turn = 1; coming.some && ok; ++turn) {
+            const Work w = coming;
+            coming = work_at(P.items, total, P.by_heads, turn);
+            if (w.item.length <= 0) continue;
+            const int meets = w.item.level + 1, rounds = KEYS ? meets * P.group : meets;
+            auto loaded = [&](int r) { return wait_all(&bar_b_full[r & 1], r >> 1 & 1, failed); };
+            auto last_scores = [&](int j) {                                  // A is read no more
+                if (j == rounds - 1 && umma::elected()) umma::products_arrive<false>(umma::shared_address(&bar_a_empty));
+                __syncwarp();
+            };
+            ok = wait_all(&bar_a_full, n & 1, failed) && loaded(r);
             if (!ok) break;
             umma::fence_after();
-            if (KEYS) add(j, 1, s_at, sum1_at);
-            if (j + 1 < rounds) {
-                ok = wait_all(&bar_b_full[(j + 1) & 1], (j + 1) >> 1 & 1, failed);
+            scores(r, 0);
+            scores(r, 1);
+            last_scores(0);
+            for (int j = 0; j < rounds; ++j, ++r) {
+                auto next_scores = [&]() {
+                    if (j + 1 == rounds) return true;
+                    if (!loaded(r + 1)) return false;
+                    umma::fence_after();
+                    scores(r + 1, 0);
+                    return true;
+                };
+                // the place of the next scores has been read: bar_ds of the round before says so
+                if (kTwice && !(ok = next_scores())) break;
+                if (KEYS) {
+                    ok = wait_all(&bar_p, r & 1, failed);
+                    if (!ok) break;
+                    umma::fence_after();
+                    add(r, j, 1, s_at + (kTwice && (r & 1) ? kSecond : 0), sum1_at);
+                }
+                if (!kTwice) {
+                    // ... or follows in the order of the products
+                    if (!(ok = next_scores())) break;
+                }
+                ok = wait_all(&bar_ds, r & 1, failed);
                 if (!ok) break;
                 umma::fence_after();
-                scores(j + 1, 0);
+                add(r, j, 0, t_at, sum0_at);
+                if (umma::elected()) {
+                    umma::products_arrive<false>(umma::shared_address(&bar_b_empty[r & 1]));
+                    if (j + 1 == rounds) umma::products_arrive<false>(umma::shared_address(&bar_sums));
+                }
+                __syncwarp();
+                if (j + 1 < rounds) {
+                    scores(r + 1, 1);
+                    last_scores(j + 1);
+                }
             }
-            ok = wait_all(&bar_ds, j & 1, failed);
-            if (!ok) break;
-            umma::fence_after();
-            add(j, 0, t_at, sum0_at);
-            if (umma::elected()) {
-                umma::products_arrive<false>(umma::shared_address(&bar_b_empty[j & 1]));
-                if (j + 1 == rounds) umma::products_arrive<false>(umma::shared_address(&bar_sums));
-            }
-            __syncwarp();
-            if (j + 1 < rounds) scores(j + 1, 1);
+            ++n;
         }
     } else {
         // ---- softmax: row and 64 columns of each tile
         const int half = warp >> 2, row = threadIdx.x & (kTile - 1), col0 = half * 64;
         const uint32_t lanes = ((uint32_t)((warp & 3) * 32) << 16) + col0;
-        const int left = item.length - tile * kTile;                        // rows of A that exist
         float unit = 1.0f;                                                  // of ds
         if (!kBf16) {
             float2 m = make_float2(0.0f, 0.0f);
@@ -934,249 +1133,283 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
             }
         }
         const float unit_p = kBf16 ? 1.0f : unit * 0x1p-14f;
-        // the bias of the (first) query head
-        float far = 0.0f, next_value = 0.0f;
-        const float *table = nullptr;
-        auto value = [&](int q_head) { return threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, q_head) : 0.0f; };
-        if constexpr (BIAS) {
-            if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = value(KEYS ? head * P.group : head);
-            make_tables<kSoftmaxThreads, true>(P.bias, tables);
-            table = tables.distance + kBefore;
-            far = tables.value[P.bias.buckets - 1];
-        }
-        float row_lse = 0.0f, row_delta = 0.0f, far_sum = 0.0f;
         // a row whose scores are all -inf has no probabilities
         auto base2 = [](float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; };
-        if (!KEYS && row < left) {
-            const long long at = (long long)head * P.tokens + first + row;
-            row_lse = base2(P.lse[at]);
-            row_delta = -P.delta[at] * unit_p;
-        }
-        auto fetch = [&](int j) {                                            // this thread's part of by_column
-            const int token = token_of(j) + row, q_head = head * P.group + j / meets;
-            if (token >= item.first + item.length) return 0.0f;
-            const long long at = (long long)q_head * P.tokens + token;
-            return half == 0 ? base2(P.lse[at]) : -P.delta[at] * unit_p;
-        };
-        float coming = KEYS ? fetch(0) : 0.0f;
-        bool ok = true;                          // where it is not, all rounds are gone through all the same, for the barriers in them
-        for (int j = 0; j < rounds; ++j) {
-            const int apart = KEYS ? j % meets : j;                         // tiles between queries and keys
-            const bool diagonal = apart == 0;
-            const int columns = KEYS ? min(item.length - (tile + apart) * kTile, kTile) : kTile;   // columns that exist
-            if (KEYS) {
-                by_column[j & 1][half][row] = coming;
-                if constexpr (BIAS) {
-                    if (j > 0 && j % meets == 0) {
-                        barrier_named(1, kSoftmaxThreads);                  // nobody reads the tables of the head before
-                        if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = next_value;
-                        make_tables<kSoftmaxThreads, false>(P.bias, tables);
-                        far = tables.value[P.bias.buckets - 1];
-                    }
-                    if (j % meets == 0 && j + meets < rounds) next_value = value(head * P.group + j / meets + 1);
-                }
-                barrier_named(1, kSoftmaxThreads);
-                if (j + 1 < rounds) coming = fetch(j + 1);
+        float far = 0.0f;
+        const float *table = nullptr;
+        if constexpr (BIAS) table = tables.distance + kBefore;
+        // where it is not, all works are gone through all the same, without waits, for the barriers in them
+        bool ok = true;
+        int r = 0, n = 0, head_before = -1;
+        for (int turn = 1; coming.some; ++turn) {
+            const Work w = coming;
+            coming = work_at(P.items, total, P.by_heads, turn);
+            if (w.item.length <= 0) continue;
+            const Item item = w.item;
+            const int head = w.head, tile = tile_of(w), first = item.first + tile * kTile, meets = item.level + 1;
+            const int rounds = KEYS ? meets * P.group : meets;
+            const int left = item.length - tile * kTile;                        // rows of A that exist
+            float row_base = 0.0f, row_delta = 0.0f, far_sum = 0.0f, next_value = 0.0f;
+            if (!KEYS && row < left) {
+                const long long at = (long long)head * P.tokens + first + row;
+                row_base = kShift - base2(P.lse[at]);
+                row_delta = -P.delta[at] * unit_p;
             }
-            const bool near = BIAS && apart * kTile - (kTile - 1) < P.bias.last;
-            const bool masked = diagonal || columns < kTile;
-            // distance of column c: of a query row to keys it falls with c, of a key row to queries it grows
-            const float *distance = table + apart * kTile + (KEYS ? col0 - row : row - col0);
-            ok &= wait_all(&bar_s, j & 1, failed);
-            if (masked) {
-                // what is masked may hold anything: it must not meet a zero in a product to come
-                ok &= wait_all(&bar_t, j & 1, failed);
-                uint8_t *b = tiles + (2 + (j & 1) * 2 + (KEYS ? half : 0)) * kTileBytes;
-                if ((KEYS || half == 0) && (diagonal || row >= columns) && clean_row<T>(b, row, HALVES) && diagonal) {
-                    if (KEYS && half == 1) dirty1 = 1;
-                    else dirty0 = 1;
+            // KEYS: lse or delta of one query of a round, as it is in memory, a round ahead; 0 where there is none
+            auto fetch = [&](int apart, int q_head) {
+                const int token = first + apart * kTile + row;
+                if (token >= item.first + item.length) return 0.0f;
+                return (half == 0 ? P.lse : P.delta)[(long long)q_head * P.tokens + token];
+            };
+            int apart = 0, q_head = KEYS ? head * P.group : head;               // tiles between queries and keys; KEYS: the query head
+            float column = KEYS ? fetch(0, q_head) : 0.0f;
+            // the bias of the (first) query head
+            auto value = [&](int q_head) { return threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, q_head) : 0.0f; };
+            if constexpr (BIAS) {
+                if (q_head != head_before) {
+                    if (n > 0) barrier_named(1, kSoftmaxThreads);               // nobody reads the tables of the head before
+                    if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = value(q_head);
+                    if (n == 0) make_tables<kSoftmaxThreads, true>(P.bias, tables);
+                    else make_tables<kSoftmaxThreads, false>(P.bias, tables);
+                    far = tables.value[P.bias.buckets - 1];
+                    head_before = q_head;
                 }
-                umma::copies_see_shared();
             }
-            umma::fence_after();
-            float p[64];
-            auto counts = [&](int c) { return KEYS ? (!diagonal || col0 + c >= row) && col0 + c < columns : !diagonal || col0 + c <= row; };
-            uint32_t s[64];
-            umma::tensor_memory_load(s_at + lanes, s);
-            umma::tensor_memory_load(s_at + lanes + 32, s + 32);
-            umma::tensor_memory_loaded<64>(s);
-            const uint64_t times = both(P.scale2);
-#pragma unroll
-            for (int c = 0; c < 64; c += 32) {
-#pragma unroll
-                for (int i = c; i < c + 32; i += 4) {
-                    uint64_t plus[2] = {both(far + (kShift - row_lse)), 0};
-                    plus[1] = plus[0];
-                    if (KEYS || near) {
-                        float4 lse = make_float4(row_lse, row_lse, row_lse, row_lse);
-                        if (KEYS) lse = *(const float4 *)&by_column[j & 1][0][col0 + i];
-                        float of[4] = {kShift - lse.x, kShift - lse.y, kShift - lse.z, kShift - lse.w};
-#pragma unroll
-                        for (int n = 0; n < 4; ++n) of[n] += near ? distance[KEYS ? i + n : -(i + n)] : far;
-                        plus[0] = pair_of(__float_as_uint(of[0]), __float_as_uint(of[1]));
-                        plus[1] = pair_of(__float_as_uint(of[2]), __float_as_uint(of[3]));
+            for (int j = 0; j < rounds; ++j, ++r) {
+                const bool diagonal = apart == 0;
+                const bool near = BIAS && apart * kTile - (kTile - 1) < P.bias.last;
+                const int columns = KEYS ? min(item.length - (tile + apart) * kTile, kTile) : kTile;   // columns that exist
+                if (KEYS) {
+                    if constexpr (BIAS) {
+                        if (j > 0 && diagonal) {
+                            barrier_named(1, kSoftmaxThreads);                  // nobody reads the tables of the head before
+                            if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = next_value;
+                            make_tables<kSoftmaxThreads, false>(P.bias, tables);
+                            far = tables.value[P.bias.buckets - 1];
+                            head_before = q_head;
+                        }
+                        if (diagonal && j + meets < rounds) next_value = value(q_head + 1);
                     }
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const uint64_t x = fma_both(pair_of(s[i + 2 * n], s[i + 2 * n + 1]), times, plus[n]);
-                        p[i + 2 * n] = exp2_fast(low_of(x));
-                        p[i + 2 * n + 1] = exp2_fast(high_of(x));
-                    }
+                    by_column[r & 1][half][row] = half == 0 ? kShift - base2(column) + (near ? 0.0f : far) : -column * unit_p;
+                    barrier_named(1, kSoftmaxThreads);
+                    const bool last = apart + 1 == meets;
+                    if (j + 1 < rounds) column = fetch(last ? 0 : apart + 1, last ? q_head + 1 : q_head);
                 }
+                const bool masked = diagonal || columns < kTile;
+                // distance of column c: of a query row to keys it falls with c, of a key row to queries it grows
+                const float *distance = table + apart * kTile + (KEYS ? col0 - row : row - col0);
+                ok = ok && wait_all(&bar_s[kTwice ? r & 1 : 0], (kTwice ? r >> 1 : r) & 1, failed);
                 if (masked) {
+                    // what is masked may hold anything: it must not meet a zero in a product to come
+                    ok = ok && wait_all(&bar_t, r & 1, failed);
+                    // KEYS: q by one half of the threads, do by the other; else k alone, by both
+                    uint8_t *b = tiles + (2 + (r & 1) * 2 + (KEYS ? half : 0)) * kTileBytes;
+                    bool any = false;
+                    if (diagonal || row >= columns)
 #pragma unroll
-                    for (int i = c; i < c + 32; ++i)
-                        if (!counts(i)) p[i] = 0.0f;
+                        for (int h = 0; h < HALVES; ++h)
+                            if (KEYS || h == half) any |= clean_row<T>(b + h * kHalfBytes, row);
+                    if (any && diagonal) dirty[n & 1][KEYS ? half : 0] = 1;
+                }
+                umma::fence_after();
+                float p[64];
+                auto counts = [&](int c) { return KEYS ? (!diagonal || col0 + c >= row) && col0 + c < columns : !diagonal || col0 + c <= row; };
+                const uint32_t here = s_at + lanes + (kTwice && (r & 1) ? kSecond : 0);
+                uint32_t s[64];
+                umma::tensor_memory_load(here, s);
+                umma::tensor_memory_load(here + 32, s + 32);
+                umma::tensor_memory_loaded<64>(s);
+                const uint64_t times = both(P.scale2), even = both(row_base + far);
+#pragma unroll
+                for (int c = 0; c < 64; c += 32) {
+                    // what a score's product is added to: shift, bias, -lse
+                    if (KEYS && near) {
+#pragma unroll
+                        for (int i = c; i < c + 32; i += 4) {
+                            const float4 of = *(const float4 *)&by_column[r & 1][0][col0 + i];
+                            p[i] = of.x + distance[i];
+                            p[i + 1] = of.y + distance[i + 1];
+                            p[i + 2] = of.z + distance[i + 2];
+                            p[i + 3] = of.w + distance[i + 3];
+                        }
+                    } else if (KEYS) {
+#pragma unroll
+                        for (int i = c; i < c + 32; i += 4) {
+                            const float4 of = *(const float4 *)&by_column[r & 1][0][col0 + i];
+                            p[i] = of.x;
+                            p[i + 1] = of.y;
+                            p[i + 2] = of.z;
+                            p[i + 3] = of.w;
+                        }
+                    } else if (near) {
+#pragma unroll
+                        for (int i = c; i < c + 32; ++i) p[i] = row_base + distance[-i];
+                    } else {
+#pragma unroll
+                        for (int i = c; i < c + 32; ++i) p[i] = low_of(even);
+                    }
+#pragma unroll
+                    for (int i = c; i < c + 32; i += 2) {
+                        const uint64_t x = fma_both(pair_of(s[i], s[i + 1]), times, pair_of(__float_as_uint(p[i]), __float_as_uint(p[i + 1])));
+                        const uint64_t e = exp2_pair<kOwn>(x, i / 2);
+                        p[i] = low_of(e);
+                        p[i + 1] = high_of(e);
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int i = c; i < c + 32; ++i)
+                            if (!counts(i)) p[i] = 0.0f;
+                    }
+                    if (KEYS) {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[c + 2 * i], p[c + 2 * i + 1]);
+                        umma::tensor_memory_store16(here + c / 2, w);
+                    }
                 }
                 if (KEYS) {
+                    umma::tensor_memory_stored();
+                    umma::fence_before();
+                    __syncwarp();
+                    if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_p));
+                }
+                ok = ok && wait_all(&bar_t, r & 1, failed);
+                umma::fence_after();
+#pragma unroll
+                for (int c = 0; c < 64; c += 32) {
+                    uint32_t u[32];
+                    umma::tensor_memory_load(t_at + lanes + c, u);
+                    umma::tensor_memory_loaded<32>(u);
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        // delta has its sign turned
+                        uint64_t minus[2] = {both(row_delta), both(row_delta)};
+                        if (KEYS) {
+                            const uint4 delta = *(const uint4 *)&by_column[r & 1][1][col0 + c + i];
+                            minus[0] = pair_of(delta.x, delta.y);
+                            minus[1] = pair_of(delta.z, delta.w);
+                        }
+#pragma unroll
+                        for (int n = 0; n < 2; ++n) {
+                            const int at = c + i + 2 * n;
+                            const uint64_t dp = pair_of(u[i + 2 * n], u[i + 2 * n + 1]);
+                            const uint64_t x = mul_both(kBf16 ? add_both(dp, minus[n]) : fma_both(dp, both(unit_p), minus[n]),
+                                                        pair_of(__float_as_uint(p[at]), __float_as_uint(p[at + 1])));
+                            p[at] = low_of(x);
+                            p[at + 1] = high_of(x);
+                        }
+                    }
+                    if (masked) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!counts(c + i)) p[c + i] = 0.0f;
+                    }
                     uint32_t w[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[c + 2 * i], p[c + 2 * i + 1]);
-                    umma::tensor_memory_store16(s_at + lanes + c / 2, w);
+                    umma::tensor_memory_store16(t_at + lanes + c / 2, w);
+                }
+                umma::tensor_memory_stored();
+                umma::fence_before();
+                __syncwarp();
+                if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_ds));
+                if (BIAS && !KEYS && P.partials != nullptr) {
+                    if (!near) {
+                        uint64_t part[4] = {0, 0, 0, 0};
+#pragma unroll
+                        for (int c = 0; c < 64; c += 2) part[c / 2 & 3] = add_both(part[c / 2 & 3], pair_of(__float_as_uint(p[c]), __float_as_uint(p[c + 1])));
+                        const uint64_t all = add_both(add_both(part[0], part[1]), add_both(part[2], part[3]));
+                        far_sum += low_of(all) + high_of(all);
+                    } else if constexpr (BIAS) {
+                        // The warp's 32 rows x 64 columns have 95 diagonals, one distance each: lane l sums those of numbers l,
+                        // l + 32 and l + 64, read askew from shared memory 16 columns at a time (row r, column c: number
+                        // r - c + 63).  Then equal buckets are neighbours, summed across lanes in a fixed order.
+                        float *stripe = stripes + warp * kStripeFloats, *mine = bucket_sums + warp * kMostBuckets;
+                        float sums[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int c = 0; c < 64; c += kStripe) {
+#pragma unroll
+                            for (int i = 0; i < kStripe; ++i) stripe[lane * (kStripe + 1) + i] = row < left ? p[c + i] : 0.0f;
+                            __syncwarp();
+                            // in columns 32 k .. 32 k + 31, row l + (c - 32 k) - 31 of lane l has number l + 32 (1 - k), and
+                            // 32 rows further down (where that is negative) number l + 32 (2 - k)
+                            const int high = c < 32 ? 2 : 1;
+#pragma unroll
+                            for (int i = 0; i < kStripe; ++i) {
+                                const int r = lane + (c & 31) + i - 31;
+                                const float x = stripe[(r & 31) * (kStripe + 1) + i];
+                                if (r >= 0) sums[high - 1] += x;
+                                else sums[high] += x;
+                            }
+                            __syncwarp();
+                        }
+                        const int zero = apart * kTile + (warp & 3) * 32 - col0 - 63;            // distance of diagonal 0
+#pragma unroll
+                        for (int n = 0; n < 3; ++n) {
+                            const int d = zero + lane + n * 32;
+                            const int bucket = d < 0 || n == 2 && lane == 31 ? -1 : tables.bucket[d];
+                            float sum = sums[n];
+#pragma unroll
+                            for (int k = 1; k < 32; k *= 2) {
+                                const float other = __shfl_down_sync(0xffffffffu, sum, k);
+                                const int its = __shfl_down_sync(0xffffffffu, bucket, k);
+                                if (lane + k < 32 && its == bucket) sum += other;
+                            }
+                            const int before = __shfl_up_sync(0xffffffffu, bucket, 1);
+                            if (bucket >= 0 && (lane == 0 || before != bucket)) mine[bucket] += sum;
+                            __syncwarp();
+                        }
+                    }
+                }
+                if (++apart == meets) {
+                    apart = 0;
+                    ++q_head;
                 }
             }
-            if (KEYS) umma::tensor_memory_stored();
-            umma::fence_before();
-            __syncwarp();
-            if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_p));
-            ok &= wait_all(&bar_t, j & 1, failed);
+            ok = ok && wait_all(&bar_sums, n & 1, failed);
             umma::fence_after();
+            if (threadIdx.x < 2) dirty[(n & 1) ^ 1][threadIdx.x] = 0;           // read by all in the work before
+            barrier_named(1, kSoftmaxThreads);
+            const bool gone = !ok || *failed;
+            // half of the columns of each sum
+            const int begin = half * 32 * HALVES, end = min(begin + 32 * HALVES, P.dim);
 #pragma unroll
-            for (int c = 0; c < 64; c += 32) {
-                uint32_t u[32];
-                umma::tensor_memory_load(t_at + lanes + c, u);
-                umma::tensor_memory_loaded<32>(u);
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    // delta has its sign turned
-                    uint64_t minus[2] = {both(row_delta), both(row_delta)};
-                    if (KEYS) {
-                        const uint4 delta = *(const uint4 *)&by_column[j & 1][1][col0 + c + i];
-                        minus[0] = pair_of(delta.x, delta.y);
-                        minus[1] = pair_of(delta.z, delta.w);
-                    }
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) {
-                        const int at = c + i + 2 * n;
-                        const uint64_t dp = pair_of(u[i + 2 * n], u[i + 2 * n + 1]);
-                        const uint64_t x = mul_both(kBf16 ? add_both(dp, minus[n]) : fma_both(dp, both(unit_p), minus[n]),
-                                                    pair_of(__float_as_uint(p[at]), __float_as_uint(p[at + 1])));
-                        p[at] = low_of(x);
-                        p[at + 1] = high_of(x);
-                    }
-                }
-                if (masked) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (!counts(c + i)) p[c + i] = 0.0f;
-                }
-                uint32_t w[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[c + 2 * i], p[c + 2 * i + 1]);
-                umma::tensor_memory_store16(t_at + lanes + c / 2, w);
-            }
-            umma::tensor_memory_stored();
-            umma::fence_before();
-            __syncwarp();
-            if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_ds));
-            if (BIAS && !KEYS && P.partials != nullptr) {
-                if (!near) {
-                    uint64_t part[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int c = 0; c < 64; c += 2) part[c / 2 & 3] = add_both(part[c / 2 & 3], pair_of(__float_as_uint(p[c]), __float_as_uint(p[c + 1])));
-                    const uint64_t all = add_both(add_both(part[0], part[1]), add_both(part[2], part[3]));
-                    far_sum += low_of(all) + high_of(all);
-                } else if constexpr (BIAS) {
-                    // The warp's 32 rows x 64 columns have 95 diagonals, one distance each: lane l sums those of numbers l,
-                    // l + 32 and l + 64, read askew from shared memory 16 columns at a time (row r, column c: number
-                    // r - c + 63).  Then equal buckets are neighbours, summed across lanes in a fixed order.
-                    float *stripe = stripes + warp * kStripeFloats, *mine = bucket_sums + warp * kMostBuckets;
-                    float sums[3] = {0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int c = 0; c < 64; c += kStripe) {
-#pragma unroll
-                        for (int i = 0; i < kStripe; ++i) stripe[lane * (kStripe + 1) + i] = row < left ? p[c + i] : 0.0f;
-                        __syncwarp();
-                        // in columns 32 k .. 32 k + 31, row l + (c - 32 k) - 31 of lane l has number l + 32 (1 - k), and
-                        // 32 rows further down (where that is negative) number l + 32 (2 - k)
-                        const int high = c < 32 ? 2 : 1;
-#pragma unroll
-                        for (int i = 0; i < kStripe; ++i) {
-                            const int r = lane + (c & 31) + i - 31;
-                            const float x = stripe[(r & 31) * (kStripe + 1) + i];
-                            if (r >= 0) sums[high - 1] += x;
-                            else sums[high] += x;
-                        }
-                        __syncwarp();
-                    }
-                    const int zero = apart * kTile + (warp & 3) * 32 - col0 - 63;            // distance of diagonal 0
-#pragma unroll
-                    for (int n = 0; n < 3; ++n) {
-                        const int d = zero + lane + n * 32;
-                        const int bucket = d < 0 || n == 2 && lane == 31 ? -1 : tables.bucket[d];
-                        float sum = sums[n];
-#pragma unroll
-                        for (int k = 1; k < 32; k *= 2) {
-                            const float other = __shfl_down_sync(0xffffffffu, sum, k);
-                            const int its = __shfl_down_sync(0xffffffffu, bucket, k);
-                            if (lane + k < 32 && its == bucket) sum += other;
-                        }
-                        const int before = __shfl_up_sync(0xffffffffu, bucket, 1);
-                        if (bucket >= 0 && (lane == 0 || before != bucket)) mine[bucket] += sum;
-                        __syncwarp();
-                    }
-                }
-            }
-        }
-        if (ok) ok = wait_all(&bar_sums, 0, failed);
-        umma::fence_after();
-        barrier_named(1, kSoftmaxThreads);
-        const bool gone = !ok || *failed;
-        const long long token = first + row;
-        // half of the columns of each sum
-        const int begin = half * 32 * HALVES, end = min(begin + 32 * HALVES, P.dim);
-#pragma unroll
-        for (int which = 0; which < (KEYS ? 2 : 1); ++which) {
-            const bool poisoned = *(volatile int *)(which ? &dirty1 : &dirty0) != 0;
-            const Heads &O = which ? P.out1 : P.out0;
-            if (O.p == nullptr) continue;
-            const float times = gone ? NAN : which ? (kBf16 ? 1.0f : 0x1p-14f) : P.scale / unit;
-            uint16_t *out = (uint16_t *)O.p + token * O.token + head * O.head;
-            for (int c = begin; c < end; c += 16) {
-                uint32_t u[16];
-                umma::tensor_memory_load16((which ? sum1_at : sum0_at) + lanes - col0 + c, u);
-                umma::tensor_memory_loaded<16>(u);
-                if (row < left) {
-                    float x[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = __uint_as_float(u[i]) * times;
-                    if (poisoned) {
+            for (int which = 0; which < (KEYS ? 2 : 1); ++which) {
+                const bool poisoned = *(volatile int *)&dirty[n & 1][which] != 0;
+                const Heads &O = which ? P.out1 : P.out0;
+                if (O.p == nullptr) continue;
+                const float times = gone ? NAN : which ? (kBf16 ? 1.0f : 0x1p-14f) : P.scale / unit;
+                uint16_t *out = (uint16_t *)O.p + (long long)(first + (warp & 3) * 32) * O.token + head * O.head;
+                for (int c = begin; c < end; c += 32)
+                    put_rows<T>((which ? sum1_at : sum0_at) + lanes - col0, times, out, O.token, c, P.dim, left - (warp & 3) * 32, [&](float *x) {
+                        if (!poisoned || row >= left) return;
                         // !KEYS: the keys of this tile up to the query; KEYS: queries (do) of this tile from the key on, all heads
                         for (int g = 0; g < (KEYS ? P.group : 1); ++g) {
                             const Heads &B = !KEYS ? P.k : which ? P.grad : P.q;
-                            const uint16_t *b = (const uint16_t *)B.p + (long long)first * B.token + (KEYS ? head * P.group + g : head / P.group) * B.head;
+                            const uint16_t *b = (const uint16_t *)B.p + (long long)first * B.token + (KEYS ? head * P.group + g : kv_of(head)) * B.head;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i)
+                            for (int i = 0; i < 32; ++i)
                                 if (c + i < end) x[i] += taken_away<T>(b + c + i, B.token, KEYS ? row : 0, KEYS ? min(left, kTile) : row + 1);
                         }
-                    }
-                    put8<T>(out + c, x);
-                    if (c + 8 < end) put8<T>(out + c + 8, x + 8);
-                }
-                __syncwarp();
+                    });
             }
-        }
-        if (BIAS && !KEYS && P.partials != nullptr) {
-            if (row >= left) far_sum = 0.0f;
+            if (BIAS && !KEYS && P.partials != nullptr) {
+                if (row >= left) far_sum = 0.0f;
 #pragma unroll
-            for (int d = 16; d > 0; d /= 2) far_sum += __shfl_xor_sync(0xffffffffu, far_sum, d);
-            if (lane == 0) bucket_sums[warp * kMostBuckets + P.bias.buckets - 1] += far_sum;
-            barrier_named(1, kSoftmaxThreads);
-            if (threadIdx.x < P.bias.buckets) {
-                float sum = 0.0f;
-                for (int w = 0; w < 8; ++w) sum += bucket_sums[w * kMostBuckets + threadIdx.x];
-                P.partials[((long long)item.slot * P.heads + head) * P.bias.buckets + threadIdx.x] = gone ? NAN : sum / unit;
+                for (int d = 16; d > 0; d /= 2) far_sum += __shfl_xor_sync(0xffffffffu, far_sum, d);
+                if (lane == 0) bucket_sums[warp * kMostBuckets + P.bias.buckets - 1] += far_sum;
+                barrier_named(1, kSoftmaxThreads);
+                if (threadIdx.x < P.bias.buckets) {
+                    float sum = 0.0f;
+                    for (int of = 0; of < 8; ++of) {
+                        sum += bucket_sums[of * kMostBuckets + threadIdx.x];
+                        bucket_sums[of * kMostBuckets + threadIdx.x] = 0.0f;
+                    }
+                    P.partials[((long long)item.slot * P.heads + head) * P.bias.buckets + threadIdx.x] = gone ? NAN : sum / unit;
+                }
+                barrier_named(1, kSoftmaxThreads);                              // the sums of the next work start from zero
             }
+            ++n;
         }
     }
     __syncwarp();
