@@ -461,6 +461,9 @@ __device__ __forceinline__ bool clean_row(uint8_t *half_tile, int row)
     umma::copies_see_shared();
     return true;
 }
+// Bits 0 to n - 1 of 32.
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
+
 // What clean_row took away and a sum over rows from..to-1 should have met.
 template <class T>
 __device__ __noinline__ float taken_away(const uint16_t *column, long long stride, int from, int to)
@@ -784,8 +787,12 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
                 }
                 if (diagonal) {
 #pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        if (col0 + i > row) s[i] = 0xff800000u;              // -inf
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t keep = below(row - col0 + 1 - 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!(keep >> i & 1)) s[32 * c + i] = 0xff800000u;   // -inf
+                    }
                 }
 #pragma unroll
                 for (int i = 0; i < 64; i += 8)
@@ -911,13 +918,14 @@ struct BackwardParams {
 };
 
 constexpr int kBackwardThreads = 320;        // as above
-constexpr int kStripe = 16;                  // columns of ds that are summed along their diagonals at a time
-constexpr int kStripeFloats = 32 * (kStripe + 1);
+// columns of ds that are summed along their diagonals at a time: as many as there is shared memory for
+template <int HALVES> constexpr int kStripe = HALVES == 1 ? 32 : 16;
+template <int HALVES> constexpr int kStripeFloats = 32 * (kStripe<HALVES> + 1);
 
 template <int HALVES, bool KEYS, bool BIAS>
 constexpr int backward_shared()
 {
-    return 1024 + 6 * HALVES * kHalfBytes + (BIAS && !KEYS ? 8 * (kStripeFloats + kMostBuckets) * 4 : 0);
+    return 1024 + 6 * HALVES * kHalfBytes + (BIAS && !KEYS ? 8 * (kStripeFloats<HALVES> + kMostBuckets) * 4 : 0);
 }
 
 // One kernel, two uses.  A CTA keeps two tiles of 128 rows (A0, A1) and meets
@@ -959,7 +967,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
     volatile int *failed = &failed_slot;
     uint8_t *tiles = raw + (((umma::shared_address(raw) + 1023u) & ~1023u) - umma::shared_address(raw));
     const uint32_t a_at = umma::shared_address(tiles), b_at = a_at + 2 * kTileBytes;
-    float *stripes = (float *)(tiles + 6 * kTileBytes), *bucket_sums = stripes + 8 * kStripeFloats;
+    float *stripes = (float *)(tiles + 6 * kTileBytes), *bucket_sums = stripes + 8 * kStripeFloats<HALVES>;
 
     if (threadIdx.x == 0) {
         for (uint64_t *b : {&bar_a_full, &bar_a_empty, &bar_b_full[0], &bar_b_full[1], &bar_b_empty[0], &bar_b_empty[1], &bar_s[0], &bar_s[1], &bar_t, &bar_sums})
@@ -1213,7 +1221,13 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                 }
                 umma::fence_after();
                 float p[64];
-                auto counts = [&](int c) { return KEYS ? (!diagonal || col0 + c >= row) && col0 + c < columns : !diagonal || col0 + c <= row; };
+                // the columns that count, a bit each: !KEYS up to the row, KEYS from the row on, and those that exist
+                uint32_t keep[2] = {~0u, ~0u};
+                if (masked) {
+                    const int from = KEYS && diagonal ? row - col0 : 0, to = KEYS ? columns - col0 : row - col0 + 1;
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) keep[c] = below(to - 32 * c) & ~below(from - 32 * c);
+                }
                 const uint32_t here = s_at + lanes + (kTwice && (r & 1) ? kSecond : 0);
                 uint32_t s[64];
                 umma::tensor_memory_load(here, s);
@@ -1258,7 +1272,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                     if (masked) {
 #pragma unroll
                         for (int i = c; i < c + 32; ++i)
-                            if (!counts(i)) p[i] = 0.0f;
+                            if (!(keep[c / 32] >> (i - c) & 1)) p[i] = 0.0f;
                     }
                     if (KEYS) {
                         uint32_t w[16];
@@ -1302,7 +1316,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                     if (masked) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (!counts(c + i)) p[c + i] = 0.0f;
+                            if (!(keep[c / 32] >> i & 1)) p[c + i] = 0.0f;
                     }
                     uint32_t w[16];
 #pragma unroll
@@ -1322,41 +1336,46 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                         far_sum += low_of(all) + high_of(all);
                     } else if constexpr (BIAS) {
                         // The warp's 32 rows x 64 columns have 95 diagonals, one distance each: lane l sums those of numbers l,
-                        // l + 32 and l + 64, read askew from shared memory 16 columns at a time (row r, column c: number
+                        // l + 32 and l + 64, read askew from shared memory some columns at a time (row r, column c: number
                         // r - c + 63).  Then equal buckets are neighbours, summed across lanes in a fixed order.
-                        float *stripe = stripes + warp * kStripeFloats, *mine = bucket_sums + warp * kMostBuckets;
+                        float *stripe = stripes + warp * kStripeFloats<HALVES>, *mine = bucket_sums + warp * kMostBuckets;
                         float sums[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int c = 0; c < 64; c += kStripe) {
+                        for (int c = 0; c < 64; c += kStripe<HALVES>) {
 #pragma unroll
-                            for (int i = 0; i < kStripe; ++i) stripe[lane * (kStripe + 1) + i] = row < left ? p[c + i] : 0.0f;
+                            for (int i = 0; i < kStripe<HALVES>; ++i) stripe[lane * (kStripe<HALVES> + 1) + i] = row < left ? p[c + i] : 0.0f;
                             __syncwarp();
                             // in columns 32 k .. 32 k + 31, row l + (c - 32 k) - 31 of lane l has number l + 32 (1 - k), and
                             // 32 rows further down (where that is negative) number l + 32 (2 - k)
                             const int high = c < 32 ? 2 : 1;
 #pragma unroll
-                            for (int i = 0; i < kStripe; ++i) {
+                            for (int i = 0; i < kStripe<HALVES>; ++i) {
                                 const int r = lane + (c & 31) + i - 31;
-                                const float x = stripe[(r & 31) * (kStripe + 1) + i];
+                                const float x = stripe[(r & 31) * (kStripe<HALVES> + 1) + i];
                                 if (r >= 0) sums[high - 1] += x;
                                 else sums[high] += x;
                             }
                             __syncwarp();
                         }
                         const int zero = apart * kTile + (warp & 3) * 32 - col0 - 63;            // distance of diagonal 0
+                        int bucket[3], before[3];
 #pragma unroll
                         for (int n = 0; n < 3; ++n) {
                             const int d = zero + lane + n * 32;
-                            const int bucket = d < 0 || n == 2 && lane == 31 ? -1 : tables.bucket[d];
-                            float sum = sums[n];
+                            bucket[n] = d < 0 || n == 2 && lane == 31 ? -1 : tables.bucket[d];
+                            before[n] = __shfl_up_sync(0xffffffffu, bucket[n], 1);
+                        }
 #pragma unroll
-                            for (int k = 1; k < 32; k *= 2) {
-                                const float other = __shfl_down_sync(0xffffffffu, sum, k);
-                                const int its = __shfl_down_sync(0xffffffffu, bucket, k);
-                                if (lane + k < 32 && its == bucket) sum += other;
+                        for (int k = 1; k < 32; k *= 2)
+#pragma unroll
+                            for (int n = 0; n < 3; ++n) {
+                                const float theirs = __shfl_down_sync(0xffffffffu, sums[n], k);
+                                const int its = __shfl_down_sync(0xffffffffu, bucket[n], k);
+                                if (lane + k < 32 && its == bucket[n]) sums[n] += theirs;
                             }
-                            const int before = __shfl_up_sync(0xffffffffu, bucket, 1);
-                            if (bucket >= 0 && (lane == 0 || before != bucket)) mine[bucket] += sum;
+#pragma unroll
+                        for (int n = 0; n < 3; ++n) {
+                            if (bucket[n] >= 0 && (lane == 0 || before[n] != bucket[n])) mine[bucket[n]] += sums[n];
                             __syncwarp();
                         }
                     }

@@ -488,9 +488,9 @@ class Attention(_Holder):
         Q, K, V, tokens, sequences, bias_type = self._arguments(where, q, k, v, offsets, bias)
         given = out is not None
         if not given:
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+            out = torch.empty_like(q)
         O = self._tensor(where, "out", out, self.heads, tokens)
-        lse = (torch.zeros if given else torch.empty)((self.heads, tokens), dtype=torch.float32, device=self.device)
+        lse = (q.new_zeros if given else q.new_empty)((self.heads, tokens), dtype=torch.float32)
         self._follow(q, k, v, offsets, bias, out, lse)
         binding.psops_attention_forward(self.ctx, Q, K, V, offsets, sequences, tokens, bias, bias_type, O, lse, not given)
         if given:
@@ -506,20 +506,18 @@ class Attention(_Holder):
         O, G = self._tensor(where, "out", out, self.heads, tokens), self._tensor(where, "grad", grad, self.heads, tokens)
         self._lse(where, lse, tokens)
         held, results, given = [], [], []
+        mine = dq is None and dk is None and dv is None
         for name, t, like, heads, wanted in (("dq", dq, q, self.heads, want[0]), ("dk", dk, k, self.kv_heads, want[1]),
                                              ("dv", dv, v, self.kv_heads, want[2])):
             if not wanted:
-                results.append(None)
-                held.append(None)
-                continue
-            if t is None:
-                # what is given keeps its rows of no sequence, what is made here does not
-                t = (torch.empty if dq is None and dk is None and dv is None else torch.zeros)(
-                    like.shape, dtype=self.dtype, device=self.device)
+                t = None
+            elif t is None:
+                # what is given keeps its rows of no sequence, what is made here has zeros there
+                t = torch.empty_like(like) if mine else torch.zeros_like(like)
             else:
                 given.append(t)
             results.append(t)
-            held.append(self._tensor(where, name, t, heads, tokens))
+            held.append(self._tensor(where, name, t, heads, tokens) if t is not None else None)
         if not want[3] or bias is None:
             dbias = None
         elif dbias is None:
@@ -529,7 +527,7 @@ class Attention(_Holder):
             given.append(dbias)
         self._follow(q, k, v, offsets, bias, out, lse, grad, *results, dbias)
         binding.psops_attention_backward(self.ctx, Q, K, V, offsets, sequences, tokens, bias, bias_type, O, lse, G, *held,
-                                         dbias, dq is None and dk is None and dv is None)
+                                         dbias, mine)
         if given:
             _changed(given)
         return (*results, dbias)
@@ -636,11 +634,17 @@ class Keep8(_Holder):
             _refuse(where, f"{name}: rows overlap")
         return rows, cols, ld
 
-    def _room(self, shape):
-        """Codes and scales for a tensor of this shape."""
-        cols = shape[-1]
-        return (torch.empty((*shape[:-1], -(-cols // 16) * 16), dtype=torch.int8, device=self.device),
-                torch.empty((*shape[:-1], -(-cols // KEPT_BLOCK)), dtype=torch.float32, device=self.device))
+    @staticmethod
+    def _like(t):
+        """A contiguous tensor like this one."""
+        return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+    @staticmethod
+    def _room(t):
+        """Codes and scales for a tensor like this one."""
+        *leading, cols = t.shape
+        return (t.new_empty((*leading, -(-cols // 16) * 16), dtype=torch.int8),
+                t.new_empty((*leading, -(-cols // KEPT_BLOCK)), dtype=torch.float32))
 
     def _kept(self, where, name, codes, scales, shape):
         room = (torch.Size((*shape[:-1], -(-shape[-1] // 16) * 16)), torch.Size((*shape[:-1], -(-shape[-1] // KEPT_BLOCK))))
@@ -652,7 +656,7 @@ class Keep8(_Holder):
     def pack(self, x):
         """(codes, scales)."""
         rows, cols, ld = self._rows("Keep8.pack", "x", x)
-        codes, scales = self._room(x.shape)
+        codes, scales = self._room(x)
         self._follow(x, codes, scales)
         binding.psops_keep8_pack(self.ctx, _TYPES[x.dtype], rows, cols, x, ld, codes, scales)
         return codes, scales
@@ -667,7 +671,7 @@ class Keep8(_Holder):
         self._kept(where, "x", codes, scales, shape)
         given = out is not None
         if not given:
-            out = torch.empty(shape, dtype=dtype, device=self.device)
+            out = scales.new_empty(shape, dtype=dtype)
         rows, cols, ld = self._rows(where, "out", out)
         if out.shape != shape or out.dtype is not dtype:
             _refuse(where, f"out is not {dtype} of shape {tuple(shape)}")
@@ -692,9 +696,9 @@ class Keep8(_Holder):
         b_ld = self._rows(where, "b", b, a)[2] if b is not None else 0
         given = out is not None
         if not given:
-            out = torch.empty(a.shape, dtype=a.dtype, device=self.device)
+            out = self._like(a)
         y_ld = self._rows(where, "out", out, a)[2]
-        kept = self._room(a.shape) + (self._room(a.shape) if b is not None else ())
+        kept = self._room(a) + (self._room(a) if b is not None else ())
         self._follow(a, b, out, *kept)
         binding.psops_keep8_activate(self.ctx, code, _TYPES[a.dtype], rows, cols, a, a_ld, b, b_ld, out, y_ld,
                                      *kept, *((None, None) if b is None else ()))
@@ -719,7 +723,7 @@ class Keep8(_Holder):
             if not wanted:
                 t = None
             elif t is None:
-                t = torch.empty(grad.shape, dtype=grad.dtype, device=self.device)
+                t = self._like(grad)
             else:
                 given.append(t)
             results.append(t)
