@@ -21,9 +21,11 @@ namespace {
 
 constexpr int kMostFillBlocks = 592;             // blocks of the preparing kernel beside the list's
 
+constexpr int64_t kJoinWithin = 8192;            // so few sums of dbias are joined by the last CTA, more by a kernel of its own
+
 struct Layout {
     int64_t capacity;                            // tiles of a call at most
-    size_t count, items, used, norms, delta, partials, total;
+    size_t count, ticket, items, used, norms, delta, partials, total;
 };
 
 using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -76,6 +78,7 @@ Layout make_layout(const psops_attention_config *c)
         return here;
     };
     l.count = take(sizeof(int));
+    l.ticket = take(sizeof(int));
     l.items = take((size_t)l.capacity * sizeof(Item));
     if (c->flags & PSOPS_ATTENTION_GRADS) {
         l.used = take((size_t)l.capacity * sizeof(int));
@@ -180,19 +183,17 @@ ForwardKernel forward_kernel(const psops_attention *a, size_t *shared)
     *shared = wide ? forward_shared<2>() : forward_shared<1>();
     return a->cfg.type == PSOPS_F16 ? forward_kernel<__half>(wide, bias) : forward_kernel<__nv_bfloat16>(wide, bias);
 }
-template <class T, bool KEYS>
+template <class T>
 BackwardKernel backward_kernel(bool wide, bool bias)
 {
-    return wide ? (bias ? psops_attention_backward_kernel<T, 2, KEYS, true> : psops_attention_backward_kernel<T, 2, KEYS, false>)
-                : (bias ? psops_attention_backward_kernel<T, 1, KEYS, true> : psops_attention_backward_kernel<T, 1, KEYS, false>);
+    return wide ? (bias ? psops_attention_backward_kernel<T, 2, true> : psops_attention_backward_kernel<T, 2, false>)
+                : (bias ? psops_attention_backward_kernel<T, 1, true> : psops_attention_backward_kernel<T, 1, false>);
 }
-template <bool KEYS>
 BackwardKernel backward_kernel(const psops_attention *a, size_t *shared)
 {
     const bool wide = a->cfg.dim > 64, bias = a->cfg.buckets > 0;
-    *shared = wide ? (bias ? backward_shared<2, KEYS, true>() : backward_shared<2, KEYS, false>())
-                   : (bias ? backward_shared<1, KEYS, true>() : backward_shared<1, KEYS, false>());
-    return a->cfg.type == PSOPS_F16 ? backward_kernel<__half, KEYS>(wide, bias) : backward_kernel<__nv_bfloat16, KEYS>(wide, bias);
+    *shared = wide ? (bias ? backward_shared<2, true>() : backward_shared<2, false>()) : (bias ? backward_shared<1, true>() : backward_shared<1, false>());
+    return a->cfg.type == PSOPS_F16 ? backward_kernel<__half>(wide, bias) : backward_kernel<__nv_bfloat16>(wide, bias);
 }
 
 Divisor divisor(uint32_t by)
@@ -202,7 +203,7 @@ Divisor divisor(uint32_t by)
     return Divisor{by, (uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by), 31 + shift};
 }
 
-// As many CTAs as run at once, or as there can be tiles.
+// As many CTAs as run at once, or as there can be works: tiles with all of `heads` heads.
 dim3 works_grid(const psops_attention *a, const PrepParams &L, int heads, int to_an_sm)
 {
     return dim3((unsigned)std::min<int64_t>((int64_t)(L.capacity - 1) * heads, (int64_t)a->sms * to_an_sm));
@@ -252,13 +253,10 @@ int psops_attention_create(psops_attention **out, const psops_attention_config *
         e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", (void **)&a->encode, 12000, cudaEnableDefault, &found);
     if (e == cudaSuccess && found != cudaDriverEntryPointSuccess) e = cudaErrorNotSupported;
     size_t shared = 0;
-    const void *kernels[3] = {};
-    size_t sizes[3] = {};
-    kernels[0] = (const void *)forward_kernel(a, &shared); sizes[0] = shared;
-    kernels[1] = (const void *)backward_kernel<false>(a, &shared); sizes[1] = shared;
-    kernels[2] = (const void *)backward_kernel<true>(a, &shared); sizes[2] = shared;
-    for (int i = 0; i < 3 && e == cudaSuccess; ++i)
-        e = cudaFuncSetAttribute(kernels[i], cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizes[i]);
+    const void *kernel = (const void *)forward_kernel(a, &shared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    kernel = (const void *)backward_kernel(a, &shared);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
     if (e != cudaSuccess) {
         delete a;
         return PSOPS_ECUDA;
@@ -349,6 +347,16 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         }
     }
     const int64_t blocks = tokens > 0 ? std::min<int64_t>({(int64_t)a->sms * 4, kMostFillBlocks, ceil_div(tokens * H, kPrepThreads / 16)}) : 0;
+    JoinParams J{};
+    J.partials = a->at<float>(a->lay.partials);
+    J.used = L.used;
+    J.slots = tokens > 0 && sequences > 0 ? L.capacity : 0;
+    J.heads = H;
+    J.buckets = a->cfg.buckets;
+    J.fp32 = bias_type == PSOPS_F32;
+    J.out = d_dbias;
+    const bool join_within = d_dbias != nullptr && J.slots > 0 && (int64_t)J.slots * H * a->cfg.buckets <= kJoinWithin;
+    if (join_within) J.ticket = L.ticket = a->at<int>(a->lay.ticket);
     PSOPS_DO(prepare(a, L, blocks));
     if (tokens > 0 && sequences > 0) {
         CUtensorMap mq, mk, mv, mg;
@@ -375,34 +383,22 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         P.norms = L.norms;
         P.blocks = (int)blocks;
         P.bias = bias_of(a, d_bias, bias_type);
+        P.by_heads = divisor(H);
+        P.by_kv_heads = divisor(G);
+        P.want_keys = dk != nullptr || dv != nullptr;
+        P.want_queries = dq != nullptr || d_dbias != nullptr;
+        if (dq != nullptr) P.dq = heads_of(a, dq, tokens, H);
+        if (dk != nullptr) P.dk = heads_of(a, dk, tokens, G);
+        if (dv != nullptr) P.dv = heads_of(a, dv, tokens, G);
+        P.partials = d_dbias != nullptr ? a->at<float>(a->lay.partials) : nullptr;
+        if (join_within) P.join = J;
         size_t shared;
-        if (dk != nullptr || dv != nullptr) {
-            if (dk != nullptr) P.out0 = heads_of(a, dk, tokens, G);
-            if (dv != nullptr) P.out1 = heads_of(a, dv, tokens, G);
-            P.by_heads = divisor(G);
-            BackwardKernel kernel = backward_kernel<true>(a, &shared);
-            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, G, 1), kBackwardThreads, shared, 1, mk, mv,
-                            mq, mg, P));
-        }
-        if (dq != nullptr || d_dbias != nullptr) {
-            P.out0 = dq != nullptr ? heads_of(a, dq, tokens, H) : Heads{};
-            P.out1 = Heads{};
-            P.partials = d_dbias != nullptr ? a->at<float>(a->lay.partials) : nullptr;
-            P.by_heads = divisor(H);
-            BackwardKernel kernel = backward_kernel<false>(a, &shared);
-            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, H, 1), kBackwardThreads, shared, 1, mq, mg,
-                            mk, mv, P));
-        }
+        BackwardKernel kernel = backward_kernel(a, &shared);
+        const int works = (P.want_keys ? G : 0) + (P.want_queries ? H : 0);
+        if (works > 0)
+            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, works, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
     }
-    if (d_dbias == nullptr) return PSOPS_OK;
-    JoinParams J{};
-    J.partials = a->at<float>(a->lay.partials);
-    J.used = L.used;
-    J.slots = tokens > 0 && sequences > 0 ? L.capacity : 0;
-    J.heads = H;
-    J.buckets = a->cfg.buckets;
-    J.fp32 = bias_type == PSOPS_F32;
-    J.out = d_dbias;
+    if (d_dbias == nullptr || join_within) return PSOPS_OK;
     return launch(a, "psops_attention_join_kernel",
                   a->cfg.type == PSOPS_F16 ? psops_attention_join_kernel<__half> : psops_attention_join_kernel<__nv_bfloat16>,
                   dim3((unsigned)ceil_div(H * a->cfg.buckets, 32)), 32 * kJoinParts, 0, 1, J);

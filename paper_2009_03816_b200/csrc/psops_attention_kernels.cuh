@@ -55,6 +55,7 @@ struct PrepParams {
     Item *items;
     int *count;
     int *used;               // NULL, or by slot whether a tile has it
+    int *ticket;             // NULL, or becomes zero
     int heads, kv_heads, dim;
     int fill;                // how many of `rest` are to be zeroed where no sequence is
     Heads rest[3];
@@ -195,6 +196,7 @@ __device__ __forceinline__ void make_list(const PrepParams &P)
     while ((most >> shift) >= kBins) ++shift;
     const int bins = (most >> shift) + 1;
     for (int i = threadIdx.x; i <= bins; i += kPrepThreads) sequences_at[i] = rest_at[i] = 0;
+    if (P.ticket != nullptr && threadIdx.x == 0) *P.ticket = 0;
     if (P.used != nullptr)
         for (int i = threadIdx.x; i < P.capacity; i += kPrepThreads) P.used[i] = 0;
     __syncthreads();
@@ -489,9 +491,9 @@ struct Work {
     int head;
     bool some;
 };
-__device__ __forceinline__ Work work_at(const Item *items, int total, const Divisor &heads, int k)
+__device__ __forceinline__ Work work_at(const Item *items, int total, const Divisor &heads, uint32_t cta, int k)
 {
-    const uint32_t many = gridDim.x, i = k * many + (k & 1 ? many - 1 - blockIdx.x : blockIdx.x);
+    const uint32_t many = gridDim.x, i = k * many + (k & 1 ? many - 1 - cta : cta);
     Work w{};
     w.some = i < (uint32_t)total;
     if (w.some) {
@@ -627,7 +629,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
     umma::after_the_kernel_before();
     const int total = *P.count * P.heads;
     auto kv_of = [&](int head) { return (int)divide(head, P.by_group); };
-    Work coming = work_at(P.items, total, P.by_heads, 0);
+    Work coming = work_at(P.items, total, P.by_heads, blockIdx.x, 0);
 
     if (warp == 8) {
         // ---- copies in; the tile on the diagonal comes first
@@ -635,7 +637,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         int t = 0, n = 0;                        // tiles and works before this one
         for (int turn = 1; coming.some && ok; ++turn) {
             const Work w = coming;
-            coming = work_at(P.items, total, P.by_heads, turn);
+            coming = work_at(P.items, total, P.by_heads, blockIdx.x, turn);
             if (w.item.length <= 0) continue;
             const int first = w.item.first + w.item.level * kTile, kv = kv_of(w.head), q_stage = n % kStages;
             ok = wait_all(&bar_q_empty[q_stage], (n / kStages & 1) ^ 1, failed);
@@ -699,7 +701,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         auto next_work = [&]() {                 // the next one with tokens
             Work w = coming;
             while (w.some) {
-                coming = work_at(P.items, total, P.by_heads, turn++);
+                coming = work_at(P.items, total, P.by_heads, blockIdx.x, turn++);
                 if (w.item.length > 0) break;
                 w = coming;
             }
@@ -756,7 +758,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         int t = 0, n = 0, head_before = -1;
         for (int turn = 1; coming.some; ++turn) {
             const Work w = coming;
-            coming = work_at(P.items, total, P.by_heads, turn);
+            coming = work_at(P.items, total, P.by_heads, blockIdx.x, turn);
             if (w.item.length <= 0) continue;
             const int tile = w.item.level, first = w.item.first + tile * kTile;
             if constexpr (BIAS) {
@@ -902,19 +904,38 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
 // Backward
 // ---------------------------------------------------------------------------
 
+// dbias's sums: by slot (only used ones count), head and bucket.
+constexpr int kJoinParts = 16;
+struct JoinParams {
+    const float *partials;
+    const int *used;
+    int slots, heads, buckets, fp32;
+    void *out;                               // buckets x heads
+    int *ticket;
+};
+template <class T>
+__device__ __forceinline__ void put_dbias(const JoinParams &P, int at, double sum)
+{
+    const long long to = (long long)(at % P.buckets) * P.heads + at / P.buckets;
+    if (P.fp32) ((float *)P.out)[to] = (float)sum;
+    else ((T *)P.out)[to] = (T)(float)sum;
+}
+
 struct BackwardParams {
     const Item *items;
     const int *count;
     int tokens, heads, group, dim;
-    Divisor by_heads, by_group;              // the heads of A0
+    Divisor by_heads, by_kv_heads, by_group;
+    int want_keys, want_queries;
     float scale, scale2;
     Heads q, k, grad;                        // read where numbers are not finite
-    Heads out0, out1;                        // dq; or dk and dv
+    Heads dq, dk, dv;                        // an address is NULL where the result is not wanted
     const float *lse, *delta;
     const float2 *norms;                     // NULL, or `blocks` of them
     int blocks;
     Bias bias;
     float *partials;                         // dbias by slot, head and bucket; NULL: not wanted
+    JoinParams join;                         // ticket NULL: a kernel of its own joins them
 };
 
 constexpr int kBackwardThreads = 320;        // as above
@@ -922,17 +943,25 @@ constexpr int kBackwardThreads = 320;        // as above
 template <int HALVES> constexpr int kStripe = HALVES == 1 ? 32 : 16;
 template <int HALVES> constexpr int kStripeFloats = 32 * (kStripe<HALVES> + 1);
 
-template <int HALVES, bool KEYS, bool BIAS>
-constexpr int backward_shared()
-{
-    return 1024 + 6 * HALVES * kHalfBytes + (BIAS && !KEYS ? 8 * (kStripeFloats<HALVES> + kMostBuckets) * 4 : 0);
-}
+template <int HALVES, bool BIAS>
+constexpr int backward_shared() { return 1024 + 6 * HALVES * kHalfBytes + (BIAS ? 8 * (kStripeFloats<HALVES> + kMostBuckets) * 4 : 0); }
 
-// One kernel, two uses.  A CTA keeps two tiles of 128 rows (A0, A1) and meets
-// pairs of tiles of 128 rows (B0, B1) one after the other:
+struct Barriers {
+    uint64_t a_full, a_empty, b_full[2], b_empty[2], s[2], t, p, ds, sums;
+};
+template <bool BIAS>
+struct BackwardShared {
+    Barriers bars[2];                        // of the first use and of the second
+    int dirty[2][2];                         // by parity of the work, and which of B
+    alignas(16) float by_column[2][2][kTile];        // lse and delta of the queries
+    typename Choose<BIAS>::Type tables;
+};
+
+// One kernel, two uses, one after the other.  A CTA keeps two tiles of 128 rows
+// (A0, A1) and meets pairs of tiles of 128 rows (B0, B1) one after the other:
 //              A0  A1  B0  B1     S = A0 B0^T   T = A1 B1^T   sums
-//   !KEYS      q   do  k   v      scores        dp            dq += ds B0
 //   KEYS       k   v   q   do     scores^T      dp^T          dk += ds^T B0, dv += p^T B1
+//   !KEYS      q   do  k   v      scores        dp            dq += ds B0
 // The scores are computed in both: seven products instead of the five that a
 // single pass needs, and in exchange no sum passes between CTAs, so that all
 // gradients are the same in every run and dq needs no fp32 sums in memory.
@@ -942,10 +971,9 @@ constexpr int backward_shared()
 // ds of the tile before and of dp run; while they form ds, those of p and of the
 // next scores.
 template <class T, int HALVES, bool KEYS, bool BIAS>
-__global__ void __launch_bounds__(kBackwardThreads, 1)
-psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_constant__ CUtensorMap map_a1,
-                                const __grid_constant__ CUtensorMap map_b0, const __grid_constant__ CUtensorMap map_b1,
-                                const __grid_constant__ BackwardParams P)
+__device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const CUtensorMap &map_a1, const CUtensorMap &map_b0, const CUtensorMap &map_b1,
+                                              const BackwardParams &P, BackwardShared<BIAS> &M, uint8_t *tiles, uint32_t tensor_base, float unit,
+                                              volatile int *failed)
 {
     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
     constexpr int kTileBytes = HALVES * kHalfBytes;
@@ -955,53 +983,34 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
     constexpr uint32_t kSecond = 3 * kTile;                                 // columns 384 to 511
     // fp16: probabilities are kept 2^14 times as large (dv is scaled back), ds by a power of two from the norms
     constexpr float kShift = kBf16 ? 0.0f : 14.0f;
-    extern __shared__ uint8_t raw[];
-    __shared__ alignas(8) uint64_t bar_a_full, bar_a_empty, bar_b_full[2], bar_b_empty[2], bar_s[2], bar_t, bar_p, bar_ds, bar_sums;
-    __shared__ uint32_t tensor_base_slot;
-    __shared__ int failed_slot, dirty[2][2];                                // by parity of the work, and which of B
-    __shared__ float2 most[kBackwardThreads / 32];
-    __shared__ alignas(16) float by_column[KEYS ? 2 : 1][2][kTile];         // lse and delta of the queries
-    __shared__ typename Choose<BIAS>::Type tables;
-
+    Barriers &bars = M.bars[KEYS ? 0 : 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    volatile int *failed = &failed_slot;
-    uint8_t *tiles = raw + (((umma::shared_address(raw) + 1023u) & ~1023u) - umma::shared_address(raw));
     const uint32_t a_at = umma::shared_address(tiles), b_at = a_at + 2 * kTileBytes;
     float *stripes = (float *)(tiles + 6 * kTileBytes), *bucket_sums = stripes + 8 * kStripeFloats<HALVES>;
 
     if (threadIdx.x == 0) {
-        for (uint64_t *b : {&bar_a_full, &bar_a_empty, &bar_b_full[0], &bar_b_full[1], &bar_b_empty[0], &bar_b_empty[1], &bar_s[0], &bar_s[1], &bar_t, &bar_sums})
+        for (uint64_t *b : {&bars.a_full, &bars.a_empty, &bars.b_full[0], &bars.b_full[1], &bars.b_empty[0], &bars.b_empty[1], &bars.s[0],
+                            &bars.s[1], &bars.t, &bars.sums})
             umma::barrier_init(umma::shared_address(b), 1);
-        umma::barrier_init(umma::shared_address(&bar_p), 8);
-        umma::barrier_init(umma::shared_address(&bar_ds), 8);
-        failed_slot = 0;
-        dirty[0][0] = dirty[0][1] = dirty[1][0] = dirty[1][1] = 0;
+        umma::barrier_init(umma::shared_address(&bars.p), 8);
+        umma::barrier_init(umma::shared_address(&bars.ds), 8);
+        M.dirty[0][0] = M.dirty[0][1] = M.dirty[1][0] = M.dirty[1][1] = 0;
         umma::barrier_init_done();
-        umma::prefetch_map(&map_a0);
-        umma::prefetch_map(&map_a1);
-        umma::prefetch_map(&map_b0);
-        umma::prefetch_map(&map_b1);
     }
-    if (warp == 9) umma::tensor_columns_take<512>(umma::shared_address(&tensor_base_slot));
     if (BIAS && !KEYS)
         for (int i = threadIdx.x; i < 8 * kMostBuckets; i += kBackwardThreads) bucket_sums[i] = 0.0f;
-    umma::after_the_kernel_before();
-    if (!kBf16) {
-        float2 m = make_float2(0.0f, 0.0f);
-        for (int i = threadIdx.x; i < P.blocks; i += kBackwardThreads) m = make_float2(fmaxf(m.x, P.norms[i].x), fmaxf(m.y, P.norms[i].y));
-#pragma unroll
-        for (int d = 16; d > 0; d /= 2)
-            m = make_float2(fmaxf(m.x, __shfl_xor_sync(0xffffffffu, m.x, d)), fmaxf(m.y, __shfl_xor_sync(0xffffffffu, m.y, d)));
-        if (lane == 0) most[warp] = m;
-    }
     umma::fence_before();
     __syncthreads();
     umma::fence_after();
-    const uint32_t s_at = tensor_base_slot, t_at = s_at + kTile, sum0_at = t_at + kTile, sum1_at = sum0_at + HALVES * 64;
+    const uint32_t s_at = tensor_base, t_at = s_at + kTile, sum0_at = t_at + kTile, sum1_at = sum0_at + HALVES * 64;
 
-    const int total = *P.count * (int)P.by_heads.by;
+    // those that got less of the first part come first in the second
+    const Divisor &heads = KEYS ? P.by_kv_heads : P.by_heads;               // of A0
+    const uint32_t cta = KEYS ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
+    const int total = *P.count * (int)heads.by;
+    auto work_of = [&](int turn) { return work_at(P.items, total, heads, cta, turn); };
+    Work coming = work_of(0);
     auto kv_of = [&](int head) { return (int)divide(head, P.by_group); };
-    Work coming = work_at(P.items, total, P.by_heads, 0);
     // A tile meets level + 1 tiles of B (of each head): !KEYS from the diagonal down, KEYS from the diagonal up.
     auto tile_of = [](const Work &w) { return KEYS ? (w.item.length + kTile - 1) / kTile - 1 - w.item.level : w.item.level; };
     auto token_of = [](int first, int meets, int j) { return KEYS ? first + (j % meets) * kTile : first - j * kTile; };
@@ -1012,26 +1021,26 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
         int r = 0, n = 0;                        // rounds and works before this one
         for (int turn = 1; coming.some && ok; ++turn) {
             const Work w = coming;
-            coming = work_at(P.items, total, P.by_heads, turn);
+            coming = work_of(turn);
             if (w.item.length <= 0) continue;
             const int first = w.item.first + tile_of(w) * kTile, meets = w.item.level + 1, rounds = KEYS ? meets * P.group : meets;
-            ok = wait_all(&bar_a_empty, (n & 1) ^ 1, failed);
+            ok = wait_all(&bars.a_empty, (n & 1) ^ 1, failed);
             if (!ok) break;
             if (umma::elected()) {
-                umma::barrier_expect(umma::shared_address(&bar_a_full), 2 * kTileBytes);
+                umma::barrier_expect(umma::shared_address(&bars.a_full), 2 * kTileBytes);
                 for (int h = 0; h < HALVES; ++h) {
-                    umma::tensor_load3(a_at + h * kHalfBytes, &map_a0, h * 64, w.head, first, umma::shared_address(&bar_a_full));
-                    umma::tensor_load3(a_at + kTileBytes + h * kHalfBytes, &map_a1, h * 64, w.head, first, umma::shared_address(&bar_a_full));
+                    umma::tensor_load3(a_at + h * kHalfBytes, &map_a0, h * 64, w.head, first, umma::shared_address(&bars.a_full));
+                    umma::tensor_load3(a_at + kTileBytes + h * kHalfBytes, &map_a1, h * 64, w.head, first, umma::shared_address(&bars.a_full));
                 }
             }
             __syncwarp();
             ++n;
             for (int j = 0; j < rounds; ++j, ++r) {
                 const int stage = r & 1, token = token_of(first, meets, j), b_head = KEYS ? w.head * P.group + j / meets : kv_of(w.head);
-                ok = wait_all(&bar_b_empty[stage], (r >> 1 & 1) ^ 1, failed);
+                ok = wait_all(&bars.b_empty[stage], (r >> 1 & 1) ^ 1, failed);
                 if (!ok) break;
                 if (umma::elected()) {
-                    const uint32_t to = b_at + stage * 2 * kTileBytes, full = umma::shared_address(&bar_b_full[stage]);
+                    const uint32_t to = b_at + stage * 2 * kTileBytes, full = umma::shared_address(&bars.b_full[stage]);
                     umma::barrier_expect(full, 2 * kTileBytes);
                     for (int h = 0; h < HALVES; ++h) {
                         umma::tensor_load3(to + h * kHalfBytes, &map_b0, h * 64, b_head, token, full);
@@ -1058,7 +1067,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                     const uint32_t on = (s >> 2) * (kHalfBytes >> 4) + (s & 3) * 2;
                     umma::multiply<false>(which ? t_at : s_at + (kTwice && (r & 1) ? kSecond : 0), da + which * kNext + on, db + stage + on, instr_s, s > 0);
                 }
-                umma::products_arrive<false>(umma::shared_address(which ? &bar_t : &bar_s[kTwice ? r & 1 : 0]));
+                umma::products_arrive<false>(umma::shared_address(which ? &bars.t : &bars.s[kTwice ? r & 1 : 0]));
             }
             __syncwarp();
         };
@@ -1075,15 +1084,15 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
         int r = 0, n = 0;
         for (int turn = 1; coming.some && ok; ++turn) {
             const Work w = coming;
-            coming = work_at(P.items, total, P.by_heads, turn);
+            coming = work_of(turn);
             if (w.item.length <= 0) continue;
             const int meets = w.item.level + 1, rounds = KEYS ? meets * P.group : meets;
-            auto loaded = [&](int r) { return wait_all(&bar_b_full[r & 1], r >> 1 & 1, failed); };
+            auto loaded = [&](int r) { return wait_all(&bars.b_full[r & 1], r >> 1 & 1, failed); };
             auto last_scores = [&](int j) {                                  // A is read no more
-                if (j == rounds - 1 && umma::elected()) umma::products_arrive<false>(umma::shared_address(&bar_a_empty));
+                if (j == rounds - 1 && umma::elected()) umma::products_arrive<false>(umma::shared_address(&bars.a_empty));
                 __syncwarp();
             };
-            ok = wait_all(&bar_a_full, n & 1, failed) && loaded(r);
+            ok = wait_all(&bars.a_full, n & 1, failed) && loaded(r);
             if (!ok) break;
             umma::fence_after();
             scores(r, 0);
@@ -1100,7 +1109,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                 // the place of the next scores has been read: bar_ds of the round before says so
                 if (kTwice && !(ok = next_scores())) break;
                 if (KEYS) {
-                    ok = wait_all(&bar_p, r & 1, failed);
+                    ok = wait_all(&bars.p, r & 1, failed);
                     if (!ok) break;
                     umma::fence_after();
                     add(r, j, 1, s_at + (kTwice && (r & 1) ? kSecond : 0), sum1_at);
@@ -1109,13 +1118,13 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                     // ... or follows in the order of the products
                     if (!(ok = next_scores())) break;
                 }
-                ok = wait_all(&bar_ds, r & 1, failed);
+                ok = wait_all(&bars.ds, r & 1, failed);
                 if (!ok) break;
                 umma::fence_after();
                 add(r, j, 0, t_at, sum0_at);
                 if (umma::elected()) {
-                    umma::products_arrive<false>(umma::shared_address(&bar_b_empty[r & 1]));
-                    if (j + 1 == rounds) umma::products_arrive<false>(umma::shared_address(&bar_sums));
+                    umma::products_arrive<false>(umma::shared_address(&bars.b_empty[r & 1]));
+                    if (j + 1 == rounds) umma::products_arrive<false>(umma::shared_address(&bars.sums));
                 }
                 __syncwarp();
                 if (j + 1 < rounds) {
@@ -1129,29 +1138,18 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
         // ---- softmax: row and 64 columns of each tile
         const int half = warp >> 2, row = threadIdx.x & (kTile - 1), col0 = half * 64;
         const uint32_t lanes = ((uint32_t)((warp & 3) * 32) << 16) + col0;
-        float unit = 1.0f;                                                  // of ds
-        if (!kBf16) {
-            float2 m = make_float2(0.0f, 0.0f);
-            for (int w = 0; w < kBackwardThreads / 32; ++w) m = make_float2(fmaxf(m.x, most[w].x), fmaxf(m.y, most[w].y));
-            const float bound = 2.0f * sqrtf(m.x) * sqrtf(m.y);             // |ds| <= p (|dp| + |delta|)
-            if (bound > 0.0f && bound < INFINITY) {
-                int e;
-                frexpf(bound, &e);
-                unit = ldexpf(1.0f, min(max(14 - e, -100), 100));
-            }
-        }
         const float unit_p = kBf16 ? 1.0f : unit * 0x1p-14f;
         // a row whose scores are all -inf has no probabilities
         auto base2 = [](float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; };
         float far = 0.0f;
         const float *table = nullptr;
-        if constexpr (BIAS) table = tables.distance + kBefore;
+        if constexpr (BIAS) table = M.tables.distance + kBefore;
         // where it is not, all works are gone through all the same, without waits, for the barriers in them
         bool ok = true;
         int r = 0, n = 0, head_before = -1;
         for (int turn = 1; coming.some; ++turn) {
             const Work w = coming;
-            coming = work_at(P.items, total, P.by_heads, turn);
+            coming = work_of(turn);
             if (w.item.length <= 0) continue;
             const Item item = w.item;
             const int head = w.head, tile = tile_of(w), first = item.first + tile * kTile, meets = item.level + 1;
@@ -1175,11 +1173,11 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
             auto value = [&](int q_head) { return threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, q_head) : 0.0f; };
             if constexpr (BIAS) {
                 if (q_head != head_before) {
-                    if (n > 0) barrier_named(1, kSoftmaxThreads);               // nobody reads the tables of the head before
-                    if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = value(q_head);
-                    if (n == 0) make_tables<kSoftmaxThreads, true>(P.bias, tables);
-                    else make_tables<kSoftmaxThreads, false>(P.bias, tables);
-                    far = tables.value[P.bias.buckets - 1];
+                    if (n > 0) barrier_named(1, kSoftmaxThreads);               // nobody reads the M.tables of the head before
+                    if (threadIdx.x < kMostBuckets) M.tables.value[threadIdx.x] = value(q_head);
+                    if (n == 0) make_tables<kSoftmaxThreads, true>(P.bias, M.tables);
+                    else make_tables<kSoftmaxThreads, false>(P.bias, M.tables);
+                    far = M.tables.value[P.bias.buckets - 1];
                     head_before = q_head;
                 }
             }
@@ -1190,15 +1188,15 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                 if (KEYS) {
                     if constexpr (BIAS) {
                         if (j > 0 && diagonal) {
-                            barrier_named(1, kSoftmaxThreads);                  // nobody reads the tables of the head before
-                            if (threadIdx.x < kMostBuckets) tables.value[threadIdx.x] = next_value;
-                            make_tables<kSoftmaxThreads, false>(P.bias, tables);
-                            far = tables.value[P.bias.buckets - 1];
+                            barrier_named(1, kSoftmaxThreads);                  // nobody reads the M.tables of the head before
+                            if (threadIdx.x < kMostBuckets) M.tables.value[threadIdx.x] = next_value;
+                            make_tables<kSoftmaxThreads, false>(P.bias, M.tables);
+                            far = M.tables.value[P.bias.buckets - 1];
                             head_before = q_head;
                         }
                         if (diagonal && j + meets < rounds) next_value = value(q_head + 1);
                     }
-                    by_column[r & 1][half][row] = half == 0 ? kShift - base2(column) + (near ? 0.0f : far) : -column * unit_p;
+                    M.by_column[r & 1][half][row] = half == 0 ? kShift - base2(column) + (near ? 0.0f : far) : -column * unit_p;
                     barrier_named(1, kSoftmaxThreads);
                     const bool last = apart + 1 == meets;
                     if (j + 1 < rounds) column = fetch(last ? 0 : apart + 1, last ? q_head + 1 : q_head);
@@ -1206,10 +1204,10 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                 const bool masked = diagonal || columns < kTile;
                 // distance of column c: of a query row to keys it falls with c, of a key row to queries it grows
                 const float *distance = table + apart * kTile + (KEYS ? col0 - row : row - col0);
-                ok = ok && wait_all(&bar_s[kTwice ? r & 1 : 0], (kTwice ? r >> 1 : r) & 1, failed);
+                ok = ok && wait_all(&bars.s[kTwice ? r & 1 : 0], (kTwice ? r >> 1 : r) & 1, failed);
                 if (masked) {
                     // what is masked may hold anything: it must not meet a zero in a product to come
-                    ok = ok && wait_all(&bar_t, r & 1, failed);
+                    ok = ok && wait_all(&bars.t, r & 1, failed);
                     // KEYS: q by one half of the threads, do by the other; else k alone, by both
                     uint8_t *b = tiles + (2 + (r & 1) * 2 + (KEYS ? half : 0)) * kTileBytes;
                     bool any = false;
@@ -1217,7 +1215,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
 #pragma unroll
                         for (int h = 0; h < HALVES; ++h)
                             if (KEYS || h == half) any |= clean_row<T>(b + h * kHalfBytes, row);
-                    if (any && diagonal) dirty[n & 1][KEYS ? half : 0] = 1;
+                    if (any && diagonal) M.dirty[n & 1][KEYS ? half : 0] = 1;
                 }
                 umma::fence_after();
                 float p[64];
@@ -1240,7 +1238,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                     if (KEYS && near) {
 #pragma unroll
                         for (int i = c; i < c + 32; i += 4) {
-                            const float4 of = *(const float4 *)&by_column[r & 1][0][col0 + i];
+                            const float4 of = *(const float4 *)&M.by_column[r & 1][0][col0 + i];
                             p[i] = of.x + distance[i];
                             p[i + 1] = of.y + distance[i + 1];
                             p[i + 2] = of.z + distance[i + 2];
@@ -1249,7 +1247,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                     } else if (KEYS) {
 #pragma unroll
                         for (int i = c; i < c + 32; i += 4) {
-                            const float4 of = *(const float4 *)&by_column[r & 1][0][col0 + i];
+                            const float4 of = *(const float4 *)&M.by_column[r & 1][0][col0 + i];
                             p[i] = of.x;
                             p[i + 1] = of.y;
                             p[i + 2] = of.z;
@@ -1285,9 +1283,9 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                     umma::tensor_memory_stored();
                     umma::fence_before();
                     __syncwarp();
-                    if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_p));
+                    if (lane == 0) umma::barrier_arrive(umma::shared_address(&bars.p));
                 }
-                ok = ok && wait_all(&bar_t, r & 1, failed);
+                ok = ok && wait_all(&bars.t, r & 1, failed);
                 umma::fence_after();
 #pragma unroll
                 for (int c = 0; c < 64; c += 32) {
@@ -1299,7 +1297,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                         // delta has its sign turned
                         uint64_t minus[2] = {both(row_delta), both(row_delta)};
                         if (KEYS) {
-                            const uint4 delta = *(const uint4 *)&by_column[r & 1][1][col0 + c + i];
+                            const uint4 delta = *(const uint4 *)&M.by_column[r & 1][1][col0 + c + i];
                             minus[0] = pair_of(delta.x, delta.y);
                             minus[1] = pair_of(delta.z, delta.w);
                         }
@@ -1326,7 +1324,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                 umma::tensor_memory_stored();
                 umma::fence_before();
                 __syncwarp();
-                if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_ds));
+                if (lane == 0) umma::barrier_arrive(umma::shared_address(&bars.ds));
                 if (BIAS && !KEYS && P.partials != nullptr) {
                     if (!near) {
                         uint64_t part[4] = {0, 0, 0, 0};
@@ -1362,7 +1360,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
 #pragma unroll
                         for (int n = 0; n < 3; ++n) {
                             const int d = zero + lane + n * 32;
-                            bucket[n] = d < 0 || n == 2 && lane == 31 ? -1 : tables.bucket[d];
+                            bucket[n] = d < 0 || n == 2 && lane == 31 ? -1 : M.tables.bucket[d];
                             before[n] = __shfl_up_sync(0xffffffffu, bucket[n], 1);
                         }
 #pragma unroll
@@ -1385,17 +1383,17 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
                     ++q_head;
                 }
             }
-            ok = ok && wait_all(&bar_sums, n & 1, failed);
+            ok = ok && wait_all(&bars.sums, n & 1, failed);
             umma::fence_after();
-            if (threadIdx.x < 2) dirty[(n & 1) ^ 1][threadIdx.x] = 0;           // read by all in the work before
+            if (threadIdx.x < 2) M.dirty[(n & 1) ^ 1][threadIdx.x] = 0;           // read by all in the work before
             barrier_named(1, kSoftmaxThreads);
             const bool gone = !ok || *failed;
             // half of the columns of each sum
             const int begin = half * 32 * HALVES, end = min(begin + 32 * HALVES, P.dim);
 #pragma unroll
             for (int which = 0; which < (KEYS ? 2 : 1); ++which) {
-                const bool poisoned = *(volatile int *)&dirty[n & 1][which] != 0;
-                const Heads &O = which ? P.out1 : P.out0;
+                const bool poisoned = *(volatile int *)&M.dirty[n & 1][which] != 0;
+                const Heads &O = !KEYS ? P.dq : which ? P.dv : P.dk;
                 if (O.p == nullptr) continue;
                 const float times = gone ? NAN : which ? (kBf16 ? 1.0f : 0x1p-14f) : P.scale / unit;
                 uint16_t *out = (uint16_t *)O.p + (long long)(first + (warp & 3) * 32) * O.token + head * O.head;
@@ -1431,21 +1429,86 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_a0, cons
             ++n;
         }
     }
+}
+
+template <class T, int HALVES, bool BIAS>
+__global__ void __launch_bounds__(kBackwardThreads, 1)
+psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                                const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_grad,
+                                const __grid_constant__ BackwardParams P)
+{
+    extern __shared__ uint8_t raw[];
+    __shared__ BackwardShared<BIAS> shared;
+    __shared__ uint32_t tensor_base_slot;
+    __shared__ int failed_slot;
+    __shared__ float2 most[kBackwardThreads / 32];
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t *tiles = raw + (((umma::shared_address(raw) + 1023u) & ~1023u) - umma::shared_address(raw));
+    if (threadIdx.x == 0) {
+        failed_slot = 0;
+        umma::prefetch_map(&map_q);
+        umma::prefetch_map(&map_k);
+        umma::prefetch_map(&map_v);
+        umma::prefetch_map(&map_grad);
+    }
+    if (warp == 9) umma::tensor_columns_take<512>(umma::shared_address(&tensor_base_slot));
+    umma::after_the_kernel_before();
+    float unit = 1.0f;                                                      // of ds
+    if (__is_same(T, __half)) {
+        float2 m = make_float2(0.0f, 0.0f);
+        for (int i = threadIdx.x; i < P.blocks; i += kBackwardThreads) m = make_float2(fmaxf(m.x, P.norms[i].x), fmaxf(m.y, P.norms[i].y));
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2)
+            m = make_float2(fmaxf(m.x, __shfl_xor_sync(0xffffffffu, m.x, d)), fmaxf(m.y, __shfl_xor_sync(0xffffffffu, m.y, d)));
+        if (lane == 0) most[warp] = m;
+    }
+    umma::fence_before();
+    __syncthreads();
+    umma::fence_after();
+    if (__is_same(T, __half)) {
+        float2 m = make_float2(0.0f, 0.0f);
+        for (int w = 0; w < kBackwardThreads / 32; ++w) m = make_float2(fmaxf(m.x, most[w].x), fmaxf(m.y, most[w].y));
+        const float bound = 2.0f * sqrtf(m.x) * sqrtf(m.y);                 // |ds| <= p (|dp| + |delta|)
+        if (bound > 0.0f && bound < INFINITY) {
+            int e;
+            frexpf(bound, &e);
+            unit = ldexpf(1.0f, min(max(14 - e, -100), 100));
+        }
+    }
+    const uint32_t tensor_base = tensor_base_slot;
+    if (P.want_keys) backward_part<T, HALVES, true, BIAS>(map_k, map_v, map_q, map_grad, P, shared, tiles, tensor_base, unit, &failed_slot);
+    if (P.want_queries) {
+        __syncwarp();
+        umma::fence_before();
+        __syncthreads();                                                    // tiles and sums of the first part are done with
+        umma::fence_after();
+        backward_part<T, HALVES, false, BIAS>(map_q, map_grad, map_k, map_v, P, shared, tiles, tensor_base, unit, &failed_slot);
+    }
     __syncwarp();
     umma::fence_before();
     __syncthreads();
     umma::fence_after();
-    if (warp == 9) umma::tensor_columns_give<512>(tensor_base_slot);
+    if (warp == 9) umma::tensor_columns_give<512>(tensor_base);
+    if (P.join.ticket == nullptr) return;
+    // few sums: the CTA that is done last joins them
+    __shared__ int last;
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(P.join.ticket, 1) == (int)gridDim.x - 1;
+        __threadfence();
+    }
+    __syncthreads();
+    if (last)
+        for (int at = threadIdx.x; at < P.join.heads * P.join.buckets; at += kBackwardThreads) {
+            double sum = 0.0;
+            for (int s = 0; s < P.join.slots; ++s)
+                if (P.join.used[s]) sum += (double)__ldcg(P.join.partials + (long long)s * P.join.heads * P.join.buckets + at);
+            put_dbias<T>(P.join, at, sum);
+        }
 }
 
 // dbias: the slots of all tiles joined in their order, in double.
-constexpr int kJoinParts = 16;
-struct JoinParams {
-    const float *partials;
-    const int *used;
-    int slots, heads, buckets, fp32;
-    void *out;                               // buckets x heads
-};
 template <class T>
 __global__ void __launch_bounds__(32 * kJoinParts) psops_attention_join_kernel(const JoinParams P)
 {
@@ -1460,10 +1523,7 @@ __global__ void __launch_bounds__(32 * kJoinParts) psops_attention_join_kernel(c
     __syncthreads();
     if (part != 0 || at >= per_slot) return;
     for (int p = 1; p < kJoinParts; ++p) sum += sums[p][threadIdx.x];
-    const int head = at / P.buckets, bucket = at % P.buckets;
-    const long long to = (long long)bucket * P.heads + head;
-    if (P.fp32) ((float *)P.out)[to] = (float)sum;
-    else ((T *)P.out)[to] = (T)(float)sum;
+    put_dbias<T>(P, at, sum);
 }
 
 } // namespace psops_attention_k
