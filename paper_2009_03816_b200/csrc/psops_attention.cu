@@ -286,7 +286,9 @@ int psops_attention_forward(psops_attention *a, const psops_heads *q, const psop
         L.rest_heads[0] = H;
         L.rest_lse = d_lse;
     }
-    PSOPS_DO(prepare(a, L, zero_rest ? std::min<int64_t>(a->sms, ceil_div(tokens * H * (a->cfg.dim / 8), kPrepThreads)) : 0));
+    // no more tiles than CTAs run at once: they need no list (short batches, where a launch counts)
+    const bool own = sequences > 0 && (L.capacity - 1) * H <= 2 * a->sms;
+    if (!own) PSOPS_DO(prepare(a, L, zero_rest ? std::min<int64_t>(a->sms, ceil_div(tokens * H * (a->cfg.dim / 8), kPrepThreads)) : 0));
     if (sequences == 0) return PSOPS_OK;
     CUtensorMap mq, mk, mv;
     const Heads V = heads_of(a, v, tokens, G);
@@ -306,6 +308,8 @@ int psops_attention_forward(psops_attention *a, const psops_heads *q, const psop
     P.v = V;
     P.lse = d_lse;
     P.bias = bias_of(a, d_bias, bias_type);
+    P.own = own;
+    P.prep = L;
     size_t shared;
     ForwardKernel kernel = forward_kernel(a, &shared);
     return launch(a, "psops_attention_forward_kernel", kernel, works_grid(a, L, H, 2), kForwardThreads, shared, 1, mq, mk, mv, P);

@@ -185,6 +185,12 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 // The list of tiles, most work first; rows of no sequence; delta
 // ---------------------------------------------------------------------------
 
+__device__ __forceinline__ void bounds_of(const PrepParams &P, int b, int &first, int &length)
+{
+    first = clamped(P.offsets[b], 0, P.tokens);
+    length = max(clamped(P.offsets[b + 1], 0, P.tokens) - first, 0);
+}
+
 // One block.  Tiles go into bins by level (several levels to a bin only beyond
 // kBins of them); within a bin the order is left to chance, which changes when
 // a tile is done and nothing else.
@@ -200,13 +206,9 @@ __device__ __forceinline__ void make_list(const PrepParams &P)
     if (P.used != nullptr)
         for (int i = threadIdx.x; i < P.capacity; i += kPrepThreads) P.used[i] = 0;
     __syncthreads();
-    auto bounds = [&](int b, int &first, int &length) {
-        first = clamped(P.offsets[b], 0, P.tokens);
-        length = max(clamped(P.offsets[b + 1], 0, P.tokens) - first, 0);
-    };
     for (int b = threadIdx.x; b < P.sequences; b += kPrepThreads) {
         int first, length;
-        bounds(b, first, length);
+        bounds_of(P, b, first, length);
         const int tiles = (length + kTile - 1) / kTile;
         atomicAdd(&sequences_at[tiles >> shift], 1);
         atomicAdd(&rest_at[tiles >> shift], tiles & ((1 << shift) - 1));
@@ -253,12 +255,13 @@ __device__ __forceinline__ void make_list(const PrepParams &P)
     while (team > 1 && team * P.sequences > kPrepThreads) team /= 2;
     for (int b = threadIdx.x / team; b < P.sequences; b += kPrepThreads / team) {
         int first, length;
-        bounds(b, first, length);
+        bounds_of(P, b, first, length);
         for (int l = threadIdx.x % team; l * kTile < length; l += team) place(first, length, first / kTile + b, l);
     }
 }
 
 // Zeroes what the call's own tensors hold where no sequence is.
+template <int THREADS>
 __device__ __forceinline__ void fill_rest(const PrepParams &P, int block, int blocks)
 {
     const int low = P.sequences > 0 ? clamped(P.offsets[0], 0, P.tokens) : 0;
@@ -266,14 +269,14 @@ __device__ __forceinline__ void fill_rest(const PrepParams &P, int block, int bl
     const int count = low + P.tokens - high, words = P.dim / 8;
     for (int t = 0; t < P.fill; ++t) {
         const int per_token = P.rest_heads[t] * words;
-        for (long long i = (long long)block * kPrepThreads + threadIdx.x; i < (long long)count * per_token; i += (long long)blocks * kPrepThreads) {
+        for (long long i = (long long)block * THREADS + threadIdx.x; i < (long long)count * per_token; i += (long long)blocks * THREADS) {
             const int n = (int)(i / per_token), w = (int)(i % per_token), token = n < low ? n : high + n - low;
             uint16_t *row = (uint16_t *)P.rest[t].p + token * P.rest[t].token + (w / words) * P.rest[t].head;
             *(uint4 *)(row + (w % words) * 8) = make_uint4(0, 0, 0, 0);
         }
     }
     if (P.rest_lse != nullptr)
-        for (long long i = (long long)block * kPrepThreads + threadIdx.x; i < (long long)count * P.heads; i += (long long)blocks * kPrepThreads) {
+        for (long long i = (long long)block * THREADS + threadIdx.x; i < (long long)count * P.heads; i += (long long)blocks * THREADS) {
             const int n = (int)(i % count), token = n < low ? n : high + n - low;
             P.rest_lse[i / count * P.tokens + token] = 0.0f;
         }
@@ -370,7 +373,7 @@ __global__ void __launch_bounds__(kPrepThreads) psops_attention_prepare_kernel(c
         return;
     }
     const int block = blockIdx.x - 1, blocks = gridDim.x - 1;
-    if (P.fill > 0) fill_rest(P, block, blocks);
+    if (P.fill > 0) fill_rest<kPrepThreads>(P, block, blocks);
     if (P.delta != nullptr) make_delta<T>(P, block, blocks);
 }
 
@@ -505,6 +508,38 @@ __device__ __forceinline__ Work work_at(const Item *items, int total, const Divi
     return w;
 }
 
+// The same without a list, where there are no more works than CTAs: each warp
+// looks for its CTA's one itself.
+__device__ __forceinline__ Work own_work(const PrepParams &P, const Divisor &heads)
+{
+    const int lane = threadIdx.x & 31;
+    const uint32_t of = divide(blockIdx.x, heads);
+    Work w{};
+    w.head = (int)(blockIdx.x - of * heads.by);
+    int before = 0;                          // tiles of the sequences before
+    for (int b = 0; b < P.sequences && !w.some; b += 32) {
+        int first = 0, length = 0;
+        if (b + lane < P.sequences) bounds_of(P, b + lane, first, length);
+        const int tiles = (length + kTile - 1) / kTile;
+        int up_to = tiles;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int n = __shfl_up_sync(0xffffffffu, up_to, d);
+            if (lane >= d) up_to += n;
+        }
+        const uint32_t found = __ballot_sync(0xffffffffu, before + up_to > (int)of);
+        if (found != 0) {
+            const int at = __ffs(found) - 1;
+            w.some = true;
+            w.item.first = __shfl_sync(0xffffffffu, first, at);
+            w.item.length = __shfl_sync(0xffffffffu, length, at);
+            w.item.level = (int)of - before - __shfl_sync(0xffffffffu, up_to - tiles, at);
+        }
+        before += __shfl_sync(0xffffffffu, up_to, 31);
+    }
+    return w;
+}
+
 // 32 columns from column c of a warp's 32 rows, out of tensor memory into rows of
 // 16-bit numbers.  A lane has a row; after four lanes have traded their quarters
 // of it (a transposition of 4 x 4 words of 16 bytes) they store 64 consecutive
@@ -566,6 +601,8 @@ struct ForwardParams {
     Heads out, v;
     float *lse;
     Bias bias;
+    int own;                                 // works without a list, and rows of no sequence zeroed here
+    PrepParams prep;
 };
 
 constexpr int kForwardThreads = 320;         // eight warps of softmax, one of copies, one of products
@@ -627,9 +664,16 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
     const uint32_t s_at = tensor_base_slot, o_at = s_at + kTile, p_at = kAhead ? o_at + 64 : s_at;
 
     umma::after_the_kernel_before();
-    const int total = *P.count * P.heads;
     auto kv_of = [&](int head) { return (int)divide(head, P.by_group); };
-    Work coming = work_at(P.items, total, P.by_heads, blockIdx.x, 0);
+    int total = 0;
+    Work coming;
+    if (P.own) {
+        coming = own_work(P.prep, P.by_heads);
+        if (P.prep.fill > 0) fill_rest<kForwardThreads>(P.prep, blockIdx.x, gridDim.x);
+    } else {
+        total = *P.count * P.heads;
+        coming = work_at(P.items, total, P.by_heads, blockIdx.x, 0);
+    }
 
     if (warp == 8) {
         // ---- copies in; the tile on the diagonal comes first
