@@ -18,6 +18,7 @@ struct psops_keep8 : psops_host::Base {};
 
 namespace {
 
+constexpr int64_t kCtasOfSm = 64;                            // dealt out as they end, beyond what runs at once
 constexpr int64_t kMostBlocksOfRows = (int64_t)1 << 30;      // blocks of 128 in a call, so that numbers of blocks stay below 2^31
 
 using Kernel = void (*)(const KeepParams);
@@ -25,8 +26,10 @@ using Kernel = void (*)(const KeepParams);
 template <class T, int JOB, int KIND, bool GATED>
 Kernel by_width(int width)
 {
-    return width == 8 ? psops_keep8_kernel<T, JOB, KIND, GATED, 8> : width == 2 ? psops_keep8_kernel<T, JOB, KIND, GATED, 2>
-                                                                  : psops_keep8_kernel<T, JOB, KIND, GATED, 1>;
+    return width == 16  ? psops_keep8_kernel<T, JOB, KIND, GATED, 8, true>
+           : width == 8 ? psops_keep8_kernel<T, JOB, KIND, GATED, 8, false>
+           : width == 4 ? psops_keep8_kernel<T, JOB, KIND, GATED, 4, false>
+           : width == 2 ? psops_keep8_kernel<T, JOB, KIND, GATED, 2, false> : psops_keep8_kernel<T, JOB, KIND, GATED, 1, false>;
 }
 template <class T, int JOB>
 Kernel by_kind(int kind, bool gated, int width)
@@ -54,12 +57,15 @@ int run(psops_keep8 *k, int job, int kind, int32_t type, int64_t rows, int64_t c
     int width = 8;
     auto look = [&](const void *p, int64_t ld) {
         if (p == nullptr) return;
-        if (((uintptr_t)p & 15u) || (rows > 1 && ld % 8)) width = std::min(width, 2);
-        if (((uintptr_t)p & 3u) || (rows > 1 && ld % 2)) width = 1;
+        while (width > 1 && (((uintptr_t)p & (2 * width - 1)) || (rows > 1 && ld % width))) width /= 2;
     };
     for (int i = 0; i < 2; ++i) look(P.x[i], P.x_ld[i]);
     for (int i = 0; i < 3; ++i) look(P.y[i], P.y_ld[i]);
-    const int64_t grid = std::min<int64_t>(ceil_div(rows * of_row, kTeams), (int64_t)k->sms * 16);
+    if (width == 8 && cols % kBlock == 0) width = 16;            // and no block is short
+    const int times = job == kPack ? kTimes<kPack, false> : job == kUnpack ? kTimes<kUnpack, false> : job == kForward ? kTimes<kForward, false>
+                      : width == 16 ? kTimes<kBackward, true> : kTimes<kBackward, false>;
+    const int64_t of_cta = kThreads / (width >= 4 ? kLanes<4> : kLanes<1>) * times;
+    const int64_t grid = std::min<int64_t>(ceil_div(rows * of_row, of_cta), (int64_t)k->sms * kCtasOfSm);
     return launch(k, "psops_keep8_kernel",
                   type == PSOPS_F16 ? kernel_of<__half>(job, kind, gated, width) : kernel_of<__nv_bfloat16>(job, kind, gated, width),
                   dim3((unsigned)grid), kThreads, 0, 1, P);

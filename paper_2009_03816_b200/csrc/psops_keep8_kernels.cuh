@@ -2,8 +2,8 @@
 //
 // A row's blocks of 128 elements share a scale: s = top / 127 with top the largest
 // magnitude, code = x / s rounded to the nearest, ties away from zero.
-// All of it is bound by memory: a warp does two blocks at a time, 16 lanes with 8
-// elements each, several blocks in flight.
+// All of it is bound by memory, and close to it by instructions: a warp does four
+// blocks at a time (two where rows are not aligned to 8 bytes).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -18,7 +18,7 @@
 namespace psops_keep8_k {
 
 constexpr int kBlock = 128;
-constexpr int kThreads = 256, kTeams = kThreads / 16;
+constexpr int kThreads = 256;
 constexpr int kPitch = 16;                       // rows of codes begin on multiples of it
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kGeluA = 1.5957691216057308f, kGeluB = 0.044715f;     // 2 sqrt(2 / pi)
@@ -65,143 +65,139 @@ template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, fl
     return u;
 }
 
-// The eight elements of a lane, as four pairs.  W consecutive ones lie together,
-// (lane + 16 k) W on: with W = 8 all of them (16-byte aligned rows), with W = 2 or 1
-// (4-byte or 2-byte aligned ones) every access of 16 lanes is still to consecutive
-// memory.
-struct Eight { uint32_t pair[4]; };
+// The elements of a lane, as pairs.  W consecutive ones lie together, (lane +
+// lanes k) W on: with W = 8 16-byte accesses (rows aligned to that), with W = 4, 2 or
+// 1 (rows aligned to 8, 4 or 2 bytes) every access of a block's lanes is still to
+// consecutive memory.  Eight lanes a block spread what a block costs over 16 elements
+// each (6.4 TB/s of a copy's 6.5 where 16 lanes gave 4.9); with narrow accesses 16
+// lanes touch fewer sectors at a time (odd widths: 3.4 TB/s, with eight 2.3).
+template <int W> constexpr int kLanes = W >= 4 ? 8 : 16;
+template <int W> constexpr int kOf = kBlock / kLanes<W>;
+template <int W> struct Some { uint32_t pair[kOf<W> / 2]; };
+template <int W> struct Codes { uint32_t four[kOf<W> / 4]; };
 
-template <int W>
-__device__ __forceinline__ Eight load(const uint16_t *p, int lane, int n)
+template <int BYTES> struct Word;
+template <> struct Word<16> { using Type = uint4; };
+template <> struct Word<8> { using Type = uint2; };
+template <> struct Word<4> { using Type = uint32_t; };
+
+// n: elements of the block that exist; WHOLE: all of them do.
+template <int W, bool WHOLE>
+__device__ __forceinline__ Some<W> load(const uint16_t *p, int lane, int n)
 {
-    Eight e{};
-    if constexpr (W == 8) {
-        const int at = lane * 8;
-        if (at + 8 <= n) {
-            const uint4 w = __ldcs((const uint4 *)(p + at));
-            e = Eight{{w.x, w.y, w.z, w.w}};
-        } else {
+    Some<W> e{};
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (at + i < n) e.pair[i / 2] |= (uint32_t)p[at + i] << (i % 2 * 16);
+    for (int k = 0; k < kOf<W> / W; ++k) {
+        const int at = (lane + kLanes<W> * k) * W;
+        if constexpr (W > 1) {
+            if (WHOLE || at + W <= n) {
+                const auto w = __ldcs((const typename Word<2 * W>::Type *)(p + at));
+                memcpy(&e.pair[k * W / 2], &w, 2 * W);
+                continue;
+            }
         }
-    } else if constexpr (W == 2) {
+        if (!WHOLE) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int at = (lane + 16 * k) * 2;
-            if (at + 2 <= n) e.pair[k] = __ldcs((const uint32_t *)(p + at));
-            else if (at < n) e.pair[k] = p[at];
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int at = lane + 16 * k;
-            if (at < n) e.pair[k / 2] |= (uint32_t)__ldcs(p + at) << (k % 2 * 16);
+            for (int i = 0; i < W; ++i)
+                if (at + i < n) e.pair[(k * W + i) / 2] |= (uint32_t)__ldcs(p + at + i) << ((k * W + i) % 2 * 16);
         }
     }
     return e;
 }
-template <int W>
-__device__ __forceinline__ void store(uint16_t *p, int lane, int n, const Eight &e)
+template <int W, bool WHOLE>
+__device__ __forceinline__ void store(uint16_t *p, int lane, int n, const Some<W> &e)
 {
-    if constexpr (W == 8) {
-        const int at = lane * 8;
-        if (at + 8 <= n) {
-            *(uint4 *)(p + at) = make_uint4(e.pair[0], e.pair[1], e.pair[2], e.pair[3]);
-        } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (at + i < n) p[at + i] = (uint16_t)(e.pair[i / 2] >> (i % 2 * 16));
+    for (int k = 0; k < kOf<W> / W; ++k) {
+        const int at = (lane + kLanes<W> * k) * W;
+        if constexpr (W > 1) {
+            if (WHOLE || at + W <= n) {
+                typename Word<2 * W>::Type w;
+                memcpy(&w, &e.pair[k * W / 2], 2 * W);
+                *(typename Word<2 * W>::Type *)(p + at) = w;
+                continue;
+            }
         }
-    } else if constexpr (W == 2) {
+        if (!WHOLE) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int at = (lane + 16 * k) * 2;
-            if (at + 2 <= n) *(uint32_t *)(p + at) = e.pair[k];
-            else if (at < n) p[at] = (uint16_t)e.pair[k];
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int at = lane + 16 * k;
-            if (at < n) p[at] = (uint16_t)(e.pair[k / 2] >> (k % 2 * 16));
+            for (int i = 0; i < W; ++i)
+                if (at + i < n) p[at + i] = (uint16_t)(e.pair[(k * W + i) / 2] >> ((k * W + i) % 2 * 16));
         }
     }
 }
-// Codes of the same eight: x is elements 0-3, y is 4-7.  Rows of codes are padded
-// to whole groups of 16, which a block's stores fill with zeros.
-template <int W>
-__device__ __forceinline__ void store_codes(uint8_t *p, int lane, int padded, uint2 c)
+// Codes of the same sixteen.  Rows of codes are padded to whole groups of 16, which
+// a block's stores fill with zeros.
+template <int W, bool WHOLE>
+__device__ __forceinline__ void store_codes(uint8_t *p, int lane, int padded, const Codes<W> &c)
 {
-    if constexpr (W == 8) {
-        if (lane * 8 < padded) *(uint2 *)(p + lane * 8) = c;
-    } else if constexpr (W == 2) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int at = (lane + 16 * k) * 2;
-            if (at < padded) *(uint16_t *)(p + at) = (uint16_t)((k < 2 ? c.x : c.y) >> (k % 2 * 16));
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (lane + 16 * k < padded) p[lane + 16 * k] = (uint8_t)((k < 4 ? c.x : c.y) >> (k % 4 * 8));
+    for (int k = 0; k < kOf<W> / W; ++k) {
+        const int at = (lane + kLanes<W> * k) * W;
+        if (!WHOLE && at >= padded) continue;
+        if constexpr (W == 8) *(uint2 *)(p + at) = make_uint2(c.four[2 * k], c.four[2 * k + 1]);
+        if constexpr (W == 4) *(uint32_t *)(p + at) = c.four[k];
+        if constexpr (W == 2) *(uint16_t *)(p + at) = (uint16_t)(c.four[k / 2] >> (k % 2 * 16));
+        if constexpr (W == 1) p[at] = (uint8_t)(c.four[k / 4] >> (k % 4 * 8));
     }
 }
-template <int W>
-__device__ __forceinline__ uint2 load_codes(const uint8_t *p, int lane, int padded)
+template <int W, bool WHOLE>
+__device__ __forceinline__ Codes<W> load_codes(const uint8_t *p, int lane, int padded)
 {
-    uint2 c = make_uint2(0, 0);
-    if constexpr (W == 8) {
-        if (lane * 8 < padded) c = __ldcs((const uint2 *)(p + lane * 8));
-    } else if constexpr (W == 2) {
+    Codes<W> c{};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int at = (lane + 16 * k) * 2;
-            if (at < padded) (k < 2 ? c.x : c.y) |= (uint32_t)__ldcs((const uint16_t *)(p + at)) << (k % 2 * 16);
+    for (int k = 0; k < kOf<W> / W; ++k) {
+        const int at = (lane + kLanes<W> * k) * W;
+        if (!WHOLE && at >= padded) continue;
+        if constexpr (W == 8) {
+            const uint2 w = __ldcs((const uint2 *)(p + at));
+            c.four[2 * k] = w.x;
+            c.four[2 * k + 1] = w.y;
         }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (lane + 16 * k < padded) (k < 4 ? c.x : c.y) |= (uint32_t)__ldcs(p + lane + 16 * k) << (k % 4 * 8);
+        if constexpr (W == 4) c.four[k] = __ldcs((const uint32_t *)(p + at));
+        if constexpr (W == 2) c.four[k / 2] |= (uint32_t)__ldcs((const uint16_t *)(p + at)) << (k % 2 * 16);
+        if constexpr (W == 1) c.four[k / 4] |= (uint32_t)__ldcs(p + at) << (k % 4 * 8);
     }
     return c;
 }
 
-// Codes and scale of a block, 16 lanes.  Ties are exact quotients of two numbers
-// of 11 bits at most by 127; any other quotient is 2^-19 off a tie or more, so the
-// factor 1 + 2^-21 moves ties away from zero and nothing else across one.  A block
-// with a number that is not finite has the scale NaN; one below 2^-100 is zeros.
-template <class T>
-__device__ __forceinline__ uint2 quantise(const Eight &e, float *scale)
+// Codes and scale of a block, by its lanes.  Ties are exact quotients of two numbers
+// of 11 bits at most by 127; any other quotient is 2^-19 off a tie or more.  The
+// factor 1 + 2^-21 moves ties away from zero, since the reciprocal, its factor and
+// their product are off by 2^-22 together at most, and moves nothing else across one.
+// A block with a number that is not finite has the scale NaN; one below 2^-100 is zeros.
+template <class T, int W>
+__device__ __forceinline__ Codes<W> quantise(const Some<W> &e, float *scale)
 {
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = __vmaxu2(top, e.pair[i] & 0x7fff7fffu);
+    for (int i = 0; i < kOf<W> / 2; ++i) top = __vmaxu2(top, e.pair[i] & 0x7fff7fffu);
 #pragma unroll
-    for (int d = 8; d > 0; d /= 2) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, d));
+    for (int d = kLanes<W> / 2; d > 0; d /= 2) top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, d));
     const uint32_t bits = max(top & 0xffffu, top >> 16);
     const float most = to_float<T>(bits);
     const bool some = most >= 0x1p-100f, finite = most < INFINITY;
     *scale = finite ? (some ? __fdiv_rn(most, 127.0f) : 0.0f) : NAN;
-    const float inverse = some && finite ? __fmul_rn(__fdiv_rn(127.0f, most), 1.0f + 0x1p-21f) : 0.0f;
-    uint32_t code[8];
+    float inverse;                           // 2^8 / top, within 2^-23, is a normal number for any top
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(most * 0x1p-8f));
+    inverse = some ? inverse * (127.0f * 0x1p-8f * (1.0f + 0x1p-21f)) : 0.0f;
+    Codes<W> c;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 x = unpack2<T>(e.pair[i]);
+    for (int i = 0; i < kOf<W> / 4; ++i) {
+        const float2 x = unpack2<T>(e.pair[2 * i]), y = unpack2<T>(e.pair[2 * i + 1]);
         // the sum's low byte is the nearest whole number
-        code[2 * i] = __float_as_uint(__fmaf_rn(x.x, inverse, 12582912.0f));
-        code[2 * i + 1] = __float_as_uint(__fmaf_rn(x.y, inverse, 12582912.0f));
+        const uint32_t code[4] = {__float_as_uint(__fmaf_rn(x.x, inverse, 12582912.0f)), __float_as_uint(__fmaf_rn(x.y, inverse, 12582912.0f)),
+                                  __float_as_uint(__fmaf_rn(y.x, inverse, 12582912.0f)), __float_as_uint(__fmaf_rn(y.y, inverse, 12582912.0f))};
+        c.four[i] = __byte_perm(__byte_perm(code[0], code[1], 0x0040), __byte_perm(code[2], code[3], 0x0040), 0x5410);
+        if (!finite) c.four[i] = 0;
     }
-    uint2 c;
-    c.x = __byte_perm(__byte_perm(code[0], code[1], 0x0040), __byte_perm(code[2], code[3], 0x0040), 0x5410);
-    c.y = __byte_perm(__byte_perm(code[4], code[5], 0x0040), __byte_perm(code[6], code[7], 0x0040), 0x5410);
-    return finite ? c : make_uint2(0, 0);
+    return c;
 }
-__device__ __forceinline__ void values(uint2 c, float scale, float *x)
+template <int W>
+__device__ __forceinline__ void values(const Codes<W> &c, float scale, float *x)
 {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const uint32_t w = (h ? c.y : c.x) ^ 0x80808080u;                  // code + 128
+    for (int h = 0; h < kOf<W> / 4; ++h) {
+        const uint32_t w = c.four[h] ^ 0x80808080u;                         // code + 128
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             x[4 * h + i] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + i)) - 8388736.0f) * scale;
@@ -250,61 +246,70 @@ struct KeepParams {
     float *scales[2];
 };
 constexpr int kPack = 0, kUnpack = 1, kForward = 2, kBackward = 3;
+template <int JOB, bool WHOLE> constexpr int kTimes = JOB == kPack || JOB == kUnpack || (JOB == kBackward && WHOLE) ? 2 : 1;
 
-// `GATED` doubles the inputs.  U blocks of a team are in flight at a time.
-template <class T, int JOB, int KIND, bool GATED, int W>
+// `GATED` doubles the inputs.  A warp has a few blocks, U times over.  U: what kept
+// most bytes under way without costing warps their registers.
+template <class T, int JOB, int KIND, bool GATED, int W, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) psops_keep8_kernel(const KeepParams P)
 {
     constexpr int N = GATED ? 2 : 1;
-    constexpr int U = JOB == kPack || JOB == kUnpack ? 4 : 2;
+    constexpr int U = kTimes<JOB, WHOLE>;
+    constexpr int kOfWarp = 32 / kLanes<W>;
     umma::after_the_kernel_before();
-    const int lane = threadIdx.x & 15;
-    const uint32_t teams = gridDim.x * kTeams;
+    const int lane = threadIdx.x % kLanes<W>;
     const long long pitch = (P.cols + kPitch - 1) / kPitch * kPitch;
-    // whole warps go round together: both teams take part in every shuffle
-    for (uint32_t first = blockIdx.x * kTeams + (threadIdx.x >> 5) * 2; first < P.blocks.count; first += teams * U) {
+    const uint32_t step = gridDim.x * (kThreads / kLanes<W>) * U;
+    // whole warps go round together: all lanes take part in every shuffle; what a warp does at a time lies together
+    for (uint32_t first = (blockIdx.x * (kThreads / 32) + threadIdx.x / 32) * kOfWarp * U; first < P.blocks.count; first += step) {
         uint32_t row[U];
         int col[U], n[U];
-        Eight in[U][N];
-        uint2 code[U][N];
+        Some<W> in[U][N];
+        Codes<W> code[U][N];
         float scale[U][N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint32_t i = first + u * teams + (threadIdx.x >> 4 & 1);
-            row[u] = row_of(P.blocks, i);
-            col[u] = (int)(i - row[u] * P.blocks.of_row) * kBlock;
-            n[u] = i < P.blocks.count ? min(P.cols - col[u], kBlock) : 0;
-            if (n[u] == 0) row[u] = 0, col[u] = 0;
+            const uint32_t i = first + u * kOfWarp + threadIdx.x % 32 / kLanes<W>;
+            const bool there = i < P.blocks.count;
+            row[u] = there ? row_of(P.blocks, i) : 0;
+            const uint32_t of = there ? i - row[u] * P.blocks.of_row : 0;
+            col[u] = (int)of * kBlock;
+            n[u] = there ? (WHOLE ? kBlock : min(P.cols - col[u], kBlock)) : 0;
             if (JOB != kUnpack) {
 #pragma unroll
-                for (int t = 0; t < (JOB == kForward ? N : 1); ++t) in[u][t] = load<W>(P.x[t] + row[u] * P.x_ld[t] + col[u], lane, n[u]);
+                for (int t = 0; t < (JOB == kForward ? N : 1); ++t)
+                    in[u][t] = load<W, WHOLE>(P.x[t] + row[u] * P.x_ld[t] + col[u], lane, n[u]);
             }
             if (JOB == kUnpack || JOB == kBackward) {
 #pragma unroll
                 for (int t = 0; t < N; ++t) {
-                    code[u][t] = load_codes<W>(P.codes[t] + row[u] * pitch + col[u], lane, n[u]);
-                    scale[u][t] = n[u] > 0 ? __ldcs(P.scales[t] + (long long)row[u] * P.blocks.of_row + col[u] / kBlock) : 0.0f;
+                    code[u][t] = load_codes<W, WHOLE>(P.codes[t] + row[u] * pitch + col[u], lane, n[u]);
+                    scale[u][t] = __ldcs(P.scales[t] + (long long)row[u] * P.blocks.of_row + of);
                 }
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int padded = (n[u] + kPitch - 1) / kPitch * kPitch;
+            const bool there = n[u] > 0;
+            Codes<W> kept[N];
+            float s[N];
             if (JOB == kPack || JOB == kForward) {
 #pragma unroll
+                for (int t = 0; t < N; ++t) kept[t] = quantise<T, W>(in[u][t], &s[t]);
+            }
+            if (!there) continue;
+            if (JOB == kPack || JOB == kForward) {
+                const int padded = (n[u] + kPitch - 1) / kPitch * kPitch;
+#pragma unroll
                 for (int t = 0; t < N; ++t) {
-                    float s;
-                    const uint2 c = quantise<T>(in[u][t], &s);
-                    if (n[u] > 0) {
-                        store_codes<W>(P.codes[t] + row[u] * pitch + col[u], lane, padded, c);
-                        if (lane == 0) P.scales[t][(long long)row[u] * P.blocks.of_row + col[u] / kBlock] = s;
-                    }
+                    store_codes<W, WHOLE>(P.codes[t] + row[u] * pitch + col[u], lane, padded, kept[t]);
+                    if (lane == 0) P.scales[t][(long long)row[u] * P.blocks.of_row + col[u] / kBlock] = s[t];
                 }
             }
             if (JOB == kForward) {
-                Eight y;
+                Some<W> y;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < kOf<W> / 2; ++i) {
                     const float2 a = unpack2<T>(in[u][0].pair[i]);
                     float2 f = make_float2(activation<KIND, false>(a.x, nullptr), activation<KIND, false>(a.y, nullptr));
                     if (GATED) {
@@ -313,23 +318,23 @@ __global__ void __launch_bounds__(kThreads) psops_keep8_kernel(const KeepParams 
                     }
                     y.pair[i] = pack2<T>(f.x, f.y);
                 }
-                store<W>(P.y[0] + row[u] * P.y_ld[0] + col[u], lane, n[u], y);
+                store<W, WHOLE>(P.y[0] + row[u] * P.y_ld[0] + col[u], lane, n[u], y);
             }
             if (JOB == kUnpack) {
-                float x[8];
-                values(code[u][0], scale[u][0], x);
-                Eight y;
+                float x[kOf<W>];
+                values<W>(code[u][0], scale[u][0], x);
+                Some<W> y;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y.pair[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
-                store<W>(P.y[0] + row[u] * P.y_ld[0] + col[u], lane, n[u], y);
+                for (int i = 0; i < kOf<W> / 2; ++i) y.pair[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+                store<W, WHOLE>(P.y[0] + row[u] * P.y_ld[0] + col[u], lane, n[u], y);
             }
             if (JOB == kBackward) {
-                float a[8], b[8];
-                values(code[u][0], scale[u][0], a);
-                if (GATED) values(code[u][N - 1], scale[u][N - 1], b);
-                Eight da, db, y;
+                float a[kOf<W>], b[kOf<W>];
+                values<W>(code[u][0], scale[u][0], a);
+                if (GATED) values<W>(code[u][N - 1], scale[u][N - 1], b);
+                Some<W> da, db, y;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < kOf<W> / 2; ++i) {
                     const float2 g = unpack2<T>(in[u][0].pair[i]);
                     float2 slope, f;
                     f.x = activation<KIND, true>(a[2 * i], &slope.x);
@@ -342,9 +347,9 @@ __global__ void __launch_bounds__(kThreads) psops_keep8_kernel(const KeepParams 
                     da.pair[i] = pack2<T>(g.x * slope.x, g.y * slope.y);
                     y.pair[i] = pack2<T>(f.x, f.y);
                 }
-                if (P.y[0] != nullptr) store<W>(P.y[0] + row[u] * P.y_ld[0] + col[u], lane, n[u], da);
-                if (GATED && P.y[1] != nullptr) store<W>(P.y[1] + row[u] * P.y_ld[1] + col[u], lane, n[u], db);
-                if (P.y[2] != nullptr) store<W>(P.y[2] + row[u] * P.y_ld[2] + col[u], lane, n[u], y);
+                if (P.y[0] != nullptr) store<W, WHOLE>(P.y[0] + row[u] * P.y_ld[0] + col[u], lane, n[u], da);
+                if (GATED && P.y[1] != nullptr) store<W, WHOLE>(P.y[1] + row[u] * P.y_ld[1] + col[u], lane, n[u], db);
+                if (P.y[2] != nullptr) store<W, WHOLE>(P.y[2] + row[u] * P.y_ld[2] + col[u], lane, n[u], y);
             }
         }
     }

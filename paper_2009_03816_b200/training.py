@@ -453,6 +453,11 @@ class Attention(_Holder):
             _refuse(where, f"{name}: the elements of a head are not consecutive")
         return binding.psops_heads(t.data_ptr() or None, stride[0], stride[1])
 
+    def _result(self, like):
+        """A new tensor of this shape, and as the library takes it."""
+        t = torch.empty_like(like, memory_format=torch.contiguous_format)
+        return t, binding.psops_heads(t.data_ptr() or None, like.shape[1] * self.dim, self.dim)
+
     def _arguments(self, where, q, k, v, offsets, bias):
         Q = self._tensor(where, "q", q, self.heads)
         tokens = q.shape[0]
@@ -487,9 +492,10 @@ class Attention(_Holder):
         where = "Attention.forward"
         Q, K, V, tokens, sequences, bias_type = self._arguments(where, q, k, v, offsets, bias)
         given = out is not None
-        if not given:
-            out = torch.empty_like(q)
-        O = self._tensor(where, "out", out, self.heads, tokens)
+        if given:
+            O = self._tensor(where, "out", out, self.heads, tokens)
+        else:
+            out, O = self._result(q)
         lse = (q.new_zeros if given else q.new_empty)((self.heads, tokens), dtype=torch.float32)
         self._follow(q, k, v, offsets, bias, out, lse)
         binding.psops_attention_forward(self.ctx, Q, K, V, offsets, sequences, tokens, bias, bias_type, O, lse, not given)
@@ -510,14 +516,16 @@ class Attention(_Holder):
         for name, t, like, heads, wanted in (("dq", dq, q, self.heads, want[0]), ("dk", dk, k, self.kv_heads, want[1]),
                                              ("dv", dv, v, self.kv_heads, want[2])):
             if not wanted:
-                t = None
+                t = as_taken = None
             elif t is None:
-                # what is given keeps its rows of no sequence, what is made here has zeros there
-                t = torch.empty_like(like) if mine else torch.zeros_like(like)
+                t, as_taken = self._result(like)
+                if not mine:               # what is given keeps its rows of no sequence, what is made here has zeros there
+                    t.zero_()
             else:
+                as_taken = self._tensor(where, name, t, heads, tokens)
                 given.append(t)
             results.append(t)
-            held.append(self._tensor(where, name, t, heads, tokens) if t is not None else None)
+            held.append(as_taken)
         if not want[3] or bias is None:
             dbias = None
         elif dbias is None:
@@ -637,7 +645,7 @@ class Keep8(_Holder):
     @staticmethod
     def _like(t):
         """A contiguous tensor like this one."""
-        return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
 
     @staticmethod
     def _room(t):
@@ -647,11 +655,12 @@ class Keep8(_Holder):
                 t.new_empty((*leading, -(-cols // KEPT_BLOCK)), dtype=torch.float32))
 
     def _kept(self, where, name, codes, scales, shape):
-        room = (torch.Size((*shape[:-1], -(-shape[-1] // 16) * 16)), torch.Size((*shape[:-1], -(-shape[-1] // KEPT_BLOCK))))
-        for what, t, size, dtype in (("codes", codes, room[0], torch.int8), ("scales", scales, room[1], torch.float32)):
-            if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype is not dtype or \
-                    t.shape != size or not t.is_contiguous():
-                _refuse(where, f"{what} of {name} have to be contiguous, {dtype}, of shape {tuple(size)}, on {self.device}")
+        *leading, cols = shape
+        for what, t, width, dtype in (("codes", codes, -(-cols // 16) * 16, torch.int8),
+                                      ("scales", scales, -(-cols // KEPT_BLOCK), torch.float32)):
+            if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() != self.device.index or \
+                    t.shape != (*leading, width) or not t.is_contiguous():
+                _refuse(where, f"{what} of {name} have to be contiguous, {dtype}, of shape {(*leading, width)}, on {self.device}")
 
     def pack(self, x):
         """(codes, scales)."""
@@ -670,11 +679,13 @@ class Keep8(_Holder):
             _refuse(where, f"{dtype} of shape {tuple(shape)}")
         self._kept(where, "x", codes, scales, shape)
         given = out is not None
-        if not given:
-            out = scales.new_empty(shape, dtype=dtype)
-        rows, cols, ld = self._rows(where, "out", out)
-        if out.shape != shape or out.dtype is not dtype:
-            _refuse(where, f"out is not {dtype} of shape {tuple(shape)}")
+        if given:
+            rows, cols, ld = self._rows(where, "out", out)
+            if out.shape != shape or out.dtype is not dtype:
+                _refuse(where, f"out is not {dtype} of shape {tuple(shape)}")
+        else:
+            out, cols = scales.new_empty(shape, dtype=dtype), shape[-1]
+            rows, ld = shape.numel() // cols, cols
         self._follow(codes, scales, out)
         binding.psops_keep8_unpack(self.ctx, _TYPES[dtype], rows, cols, codes, scales, out, ld)
         if given:
@@ -695,9 +706,10 @@ class Keep8(_Holder):
         rows, cols, a_ld = self._rows(where, "a", a)
         b_ld = self._rows(where, "b", b, a)[2] if b is not None else 0
         given = out is not None
-        if not given:
-            out = self._like(a)
-        y_ld = self._rows(where, "out", out, a)[2]
+        if given:
+            y_ld = self._rows(where, "out", out, a)[2]
+        else:
+            out, y_ld = self._like(a), cols
         kept = self._room(a) + (self._room(a) if b is not None else ())
         self._follow(a, b, out, *kept)
         binding.psops_keep8_activate(self.ctx, code, _TYPES[a.dtype], rows, cols, a, a_ld, b, b_ld, out, y_ld,
@@ -720,14 +732,16 @@ class Keep8(_Holder):
             self._kept(where, "ab"[i // 2], kept[i], kept[i + 1], grad.shape)
         results, strides, given = [], [], []
         for name, t, wanted in (("da", da, want[0]), ("db", db, want[1] and gated), ("y", None, again)):
+            ld_of = cols
             if not wanted:
                 t = None
             elif t is None:
                 t = self._like(grad)
             else:
+                ld_of = self._rows(where, name, t, grad)[2]
                 given.append(t)
             results.append(t)
-            strides.append(self._rows(where, name, t, grad)[2] if t is not None else 0)
+            strides.append(ld_of)
         self._follow(grad, *kept, *results)
         binding.psops_keep8_activate_backward(self.ctx, code, _TYPES[grad.dtype], rows, cols, *kept,
                                               *(() if gated else (None, None)), grad, ld, results[0], strides[0],
