@@ -442,29 +442,32 @@ template <class T> __device__ __forceinline__ uint32_t add_nothing(uint32_t acc,
     else asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(acc) : "r"(x), "r"(0u));
     return acc;
 }
-// Numbers that are not finite among 64 elements of a row of a tile become zeros,
-// so that a probability of zero meets none.  True if there were any.  The eight
-// 16-byte words are taken in the swizzle's order.
+// Whether there are numbers that are not finite among 64 elements of a row of a
+// tile.  The eight 16-byte words are taken in the swizzle's order.
 template <class T>
-__device__ __forceinline__ bool clean_row(uint8_t *half_tile, int row)
+__device__ __forceinline__ bool not_clean(const uint8_t *half_tile, int row)
 {
-    uint4 *at = (uint4 *)(half_tile + row * 128);
+    const uint4 *at = (const uint4 *)(half_tile + row * 128);
     uint32_t acc = 0;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         const uint4 w = at[c ^ (row & 7)];
         acc = add_nothing<T>(add_nothing<T>(add_nothing<T>(add_nothing<T>(acc, w.x), w.y), w.z), w.w);
     }
-    if ((acc & 0x7fff7fffu) == 0) return false;
+    return (acc & 0x7fff7fffu) != 0;
+}
+// Makes zeros of them, so that a probability of zero meets none.
+template <class T>
+__device__ __noinline__ void clean_row(uint8_t *half_tile, int row)
+{
     constexpr uint32_t kExponent = __is_same(T, __half) ? 0x7c00u : 0x7f80u;
 #pragma unroll 1
     for (int c = 0; c < 32; ++c) {
-        uint32_t &x = ((uint32_t *)at)[c];
+        uint32_t &x = ((uint32_t *)(half_tile + row * 128))[c];
         if ((x & kExponent) == kExponent) x &= 0xffff0000u;
         if (((x >> 16) & kExponent) == kExponent) x &= 0xffffu;
     }
     umma::copies_see_shared();
-    return true;
 }
 // Bits 0 to n - 1 of 32.
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
@@ -900,7 +903,11 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
                 if (diagonal) {
                     // keys that are masked here may hold anything: rows of the next sequence, or of none
                     ok = ok && wait_all(&bar_v_full[t % kStages], t / kStages & 1, failed);
-                    if (half < HALVES && clean_row<T>(tiles + (2 * kStages + t % kStages) * kTileBytes + half * kHalfBytes, row)) dirty[n & 1] = 1;
+                    uint8_t *v = tiles + (2 * kStages + t % kStages) * kTileBytes + half * kHalfBytes;
+                    if (half < HALVES && not_clean<T>(v, row)) {
+                        clean_row<T>(v, row);
+                        dirty[n & 1] = 1;
+                    }
                     umma::tensor_memory_stored();
                     umma::fence_before();
                     __syncwarp();
@@ -985,6 +992,7 @@ struct BackwardParams {
 constexpr int kBackwardThreads = 320;        // as above
 // columns of ds that are summed along their diagonals at a time: as many as there is shared memory for
 template <int HALVES> constexpr int kStripe = HALVES == 1 ? 32 : 16;
+constexpr int kFewBuckets = 3;               // up to so many buckets in a warp's part of a tile are summed one by one
 template <int HALVES> constexpr int kStripeFloats = 32 * (kStripe<HALVES> + 1);
 
 template <int HALVES, bool BIAS>
@@ -1250,16 +1258,23 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                 const float *distance = table + apart * kTile + (KEYS ? col0 - row : row - col0);
                 ok = ok && wait_all(&bars.s[kTwice ? r & 1 : 0], (kTwice ? r >> 1 : r) & 1, failed);
                 if (masked) {
-                    // what is masked may hold anything: it must not meet a zero in a product to come
-                    ok = ok && wait_all(&bars.t, r & 1, failed);
-                    // KEYS: q by one half of the threads, do by the other; else k alone, by both
+                    // What is masked may hold anything: it must not meet a zero in a product to come.  KEYS: one half of the
+                    // threads looks at q, the other at do; else both at k.
                     uint8_t *b = tiles + (2 + (r & 1) * 2 + (KEYS ? half : 0)) * kTileBytes;
                     bool any = false;
                     if (diagonal || row >= columns)
 #pragma unroll
                         for (int h = 0; h < HALVES; ++h)
-                            if (KEYS || h == half) any |= clean_row<T>(b + h * kHalfBytes, row);
-                    if (any && diagonal) M.dirty[n & 1][KEYS ? half : 0] = 1;
+                            if (KEYS || h == half) any |= not_clean<T>(b + h * kHalfBytes, row);
+                    if (__any_sync(0xffffffffu, any)) {
+                        ok = ok && wait_all(&bars.t, r & 1, failed);            // the scores' products have read them
+                        if (any) {
+                            for (int h = 0; h < HALVES; ++h)
+                                if (KEYS || h == half) clean_row<T>(b + h * kHalfBytes, row);
+                            if (diagonal) M.dirty[n & 1][KEYS ? half : 0] = 1;
+                        }
+                        __syncwarp();
+                    }
                 }
                 umma::fence_after();
                 float p[64];
@@ -1377,48 +1392,73 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                         const uint64_t all = add_both(add_both(part[0], part[1]), add_both(part[2], part[3]));
                         far_sum += low_of(all) + high_of(all);
                     } else if constexpr (BIAS) {
-                        // The warp's 32 rows x 64 columns have 95 diagonals, one distance each: lane l sums those of numbers l,
-                        // l + 32 and l + 64, read askew from shared memory some columns at a time (row r, column c: number
-                        // r - c + 63).  Then equal buckets are neighbours, summed across lanes in a fixed order.
-                        float *stripe = stripes + warp * kStripeFloats<HALVES>, *mine = bucket_sums + warp * kMostBuckets;
-                        float sums[3] = {0.0f, 0.0f, 0.0f};
+                        // the warp's 32 rows x 64 columns have 95 diagonals, one distance each; diagonal 0's, and the buckets of all
+                        const int zero = apart * kTile + (warp & 3) * 32 - col0 - 63;
+                        const int low = M.tables.bucket[max(zero, 0)], high = zero + 94 < 0 ? low - 1 : M.tables.bucket[max(zero + 94, 0)];
+                        float *mine = bucket_sums + warp * kMostBuckets;
+                        if (high - low < kFewBuckets) {
+                            // farther out a bucket is wide: its part of each row, as bits, one bucket after the other
+                            for (int bucket = low; bucket <= high; ++bucket) {
+                                // distance of column c: row_zero - c
+                                const int row_zero = zero + 63 + lane;
+                                const int from = bucket == P.bias.buckets - 1 ? 0 : row_zero - M.tables.first[bucket + 1] + 1;
+                                const int to = row_zero - M.tables.first[bucket] + 1;
+                                float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int c = 0; c < 64; c += kStripe<HALVES>) {
+                                for (int c = 0; c < 64; c += 32) {
+                                    const uint32_t of = row < left ? below(to - c) & ~below(from - c) : 0u;
 #pragma unroll
-                            for (int i = 0; i < kStripe<HALVES>; ++i) stripe[lane * (kStripe<HALVES> + 1) + i] = row < left ? p[c + i] : 0.0f;
-                            __syncwarp();
-                            // in columns 32 k .. 32 k + 31, row l + (c - 32 k) - 31 of lane l has number l + 32 (1 - k), and
-                            // 32 rows further down (where that is negative) number l + 32 (2 - k)
-                            const int high = c < 32 ? 2 : 1;
+                                    for (int i = 0; i < 32; ++i)
+                                        if (of >> i & 1) part[i & 3] += p[c + i];
+                                }
+                                float sum = (part[0] + part[1]) + (part[2] + part[3]);
 #pragma unroll
-                            for (int i = 0; i < kStripe<HALVES>; ++i) {
-                                const int r = lane + (c & 31) + i - 31;
-                                const float x = stripe[(r & 31) * (kStripe<HALVES> + 1) + i];
-                                if (r >= 0) sums[high - 1] += x;
-                                else sums[high] += x;
+                                for (int k = 16; k > 0; k /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+                                if (lane == 0) mine[bucket] += sum;
+                                __syncwarp();
                             }
-                            __syncwarp();
-                        }
-                        const int zero = apart * kTile + (warp & 3) * 32 - col0 - 63;            // distance of diagonal 0
-                        int bucket[3], before[3];
+                        } else {
+                            // lane l sums the diagonals of numbers l, l + 32 and l + 64, read askew from shared memory some columns at a time (row r, column c: number
+                            // r - c + 63).  Then equal buckets are neighbours, summed across lanes in a fixed order.
+                            float *stripe = stripes + warp * kStripeFloats<HALVES>;
+                            float sums[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int n = 0; n < 3; ++n) {
-                            const int d = zero + lane + n * 32;
-                            bucket[n] = d < 0 || n == 2 && lane == 31 ? -1 : M.tables.bucket[d];
-                            before[n] = __shfl_up_sync(0xffffffffu, bucket[n], 1);
-                        }
+                            for (int c = 0; c < 64; c += kStripe<HALVES>) {
 #pragma unroll
-                        for (int k = 1; k < 32; k *= 2)
+                                for (int i = 0; i < kStripe<HALVES>; ++i) stripe[lane * (kStripe<HALVES> + 1) + i] = row < left ? p[c + i] : 0.0f;
+                                __syncwarp();
+                                // in columns 32 k .. 32 k + 31, row l + (c - 32 k) - 31 of lane l has number l + 32 (1 - k), and
+                                // 32 rows further down (where that is negative) number l + 32 (2 - k)
+                                const int high = c < 32 ? 2 : 1;
+#pragma unroll
+                                for (int i = 0; i < kStripe<HALVES>; ++i) {
+                                    const int r = lane + (c & 31) + i - 31;
+                                    const float x = stripe[(r & 31) * (kStripe<HALVES> + 1) + i];
+                                    if (r >= 0) sums[high - 1] += x;
+                                    else sums[high] += x;
+                                }
+                                __syncwarp();
+                            }
+                            int bucket[3], before[3];
 #pragma unroll
                             for (int n = 0; n < 3; ++n) {
-                                const float theirs = __shfl_down_sync(0xffffffffu, sums[n], k);
-                                const int its = __shfl_down_sync(0xffffffffu, bucket[n], k);
-                                if (lane + k < 32 && its == bucket[n]) sums[n] += theirs;
+                                const int d = zero + lane + n * 32;
+                                bucket[n] = d < 0 || n == 2 && lane == 31 ? -1 : M.tables.bucket[d];
+                                before[n] = __shfl_up_sync(0xffffffffu, bucket[n], 1);
                             }
 #pragma unroll
-                        for (int n = 0; n < 3; ++n) {
-                            if (bucket[n] >= 0 && (lane == 0 || before[n] != bucket[n])) mine[bucket[n]] += sums[n];
-                            __syncwarp();
+                            for (int k = 1; k < 32; k *= 2)
+#pragma unroll
+                                for (int n = 0; n < 3; ++n) {
+                                    const float theirs = __shfl_down_sync(0xffffffffu, sums[n], k);
+                                    const int its = __shfl_down_sync(0xffffffffu, bucket[n], k);
+                                    if (lane + k < 32 && its == bucket[n]) sums[n] += theirs;
+                                }
+#pragma unroll
+                            for (int n = 0; n < 3; ++n) {
+                                if (bucket[n] >= 0 && (lane == 0 || before[n] != bucket[n])) mine[bucket[n]] += sums[n];
+                                __syncwarp();
+                            }
                         }
                     }
                 }
