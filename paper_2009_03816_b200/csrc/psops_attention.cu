@@ -21,11 +21,12 @@ namespace {
 
 constexpr int kMostFillBlocks = 592;             // blocks of the preparing kernel beside the list's
 
+constexpr int kMostCtas = 320;                   // two for each SM forward; half as many, with twice the room, backward
 constexpr int64_t kJoinWithin = 8192;            // so few sums of dbias are joined by the last CTA, more by a kernel of its own
 
 struct Layout {
     int64_t capacity;                            // tiles of a call at most
-    size_t count, ticket, items, used, norms, delta, partials, total;
+    size_t count, ticket, items, fold, used, norms, delta, partials, total;
 };
 
 using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -80,7 +81,10 @@ Layout make_layout(const psops_attention_config *c)
     l.count = take(sizeof(int));
     l.ticket = take(sizeof(int));
     l.items = take((size_t)l.capacity * sizeof(Item));
-    if (c->flags & PSOPS_ATTENTION_GRADS) {
+    const bool grads = c->flags & PSOPS_ATTENTION_GRADS;
+    if (c->max_tokens * (grads ? c->heads / c->kv_heads : 1) > (int64_t)kChain * kTile)
+        l.fold = take((size_t)kMostCtas * kFoldFloats * sizeof(float));
+    if (grads) {
         l.used = take((size_t)l.capacity * sizeof(int));
         l.norms = take(kMostFillBlocks * sizeof(float2));
         l.delta = take((size_t)c->max_tokens * c->heads * sizeof(float));
@@ -206,7 +210,7 @@ Divisor divisor(uint32_t by)
 // As many CTAs as run at once, or as there can be works: tiles with all of `heads` heads.
 dim3 works_grid(const psops_attention *a, const PrepParams &L, int heads, int to_an_sm)
 {
-    return dim3((unsigned)std::min<int64_t>((int64_t)(L.capacity - 1) * heads, (int64_t)a->sms * to_an_sm));
+    return dim3((unsigned)std::min<int64_t>((int64_t)(L.capacity - 1) * heads, std::min(a->sms * to_an_sm, kMostCtas / 2 * to_an_sm)));
 }
 
 Bias bias_of(const psops_attention *a, const void *bias, int32_t bias_type)
@@ -287,7 +291,7 @@ int psops_attention_forward(psops_attention *a, const psops_heads *q, const psop
         L.rest_lse = d_lse;
     }
     // no more tiles than CTAs run at once: they need no list (short batches, where a launch counts)
-    const bool own = sequences > 0 && (L.capacity - 1) * H <= 2 * a->sms;
+    const bool own = sequences > 0 && (L.capacity - 1) * H <= std::min(2 * a->sms, kMostCtas);
     if (!own) PSOPS_DO(prepare(a, L, zero_rest ? std::min<int64_t>(a->sms, ceil_div(tokens * H * (a->cfg.dim / 8), kPrepThreads)) : 0));
     if (sequences == 0) return PSOPS_OK;
     CUtensorMap mq, mk, mv;
@@ -308,6 +312,7 @@ int psops_attention_forward(psops_attention *a, const psops_heads *q, const psop
     P.v = V;
     P.lse = d_lse;
     P.bias = bias_of(a, d_bias, bias_type);
+    P.fold = a->at<float>(a->lay.fold);
     P.own = own;
     P.prep = L;
     size_t shared;
@@ -395,6 +400,7 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         if (dk != nullptr) P.dk = heads_of(a, dk, tokens, G);
         if (dv != nullptr) P.dv = heads_of(a, dv, tokens, G);
         P.partials = d_dbias != nullptr ? a->at<float>(a->lay.partials) : nullptr;
+        P.fold = a->at<float>(a->lay.fold);
         if (join_within) P.join = J;
         size_t shared;
         BackwardKernel kernel = backward_kernel(a, &shared);

@@ -29,6 +29,10 @@ constexpr int kHalfBytes = kTile * 128;          // 64 elements of each of 128 t
 constexpr int kBefore = 128;                     // places of the distance table for pairs above the diagonal
 constexpr int kTableFloats = kBefore + kMostDistance + 2 * kTile;
 constexpr int kPrepThreads = 512, kBins = 1024;
+// The tensor cores cut off what does not fit into a running sum.  After so many
+// tiles (16,384 terms) a sum goes to memory, where fp32 additions carry it on.
+constexpr int kChain = 128;
+constexpr int kFoldFloats = kTile * kMostDim;    // room of a CTA for one of them
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // Division of numbers below 2^31 by a number that the host knows.
@@ -591,6 +595,26 @@ __device__ __forceinline__ void put_rows(uint32_t from, float times, uint16_t *t
 // Forward
 // ---------------------------------------------------------------------------
 
+// The place of a thread's row in a CTA's room; column c is at [c * kTile].
+__device__ __forceinline__ float *room_of(float *fold, int which, int row) { return fold + (long long)which * kFoldFloats + row; }
+
+// Columns begin to end of this thread's row in tensor memory are added to what is
+// in its room, times a factor, or put there.
+__device__ __noinline__ void add_to_room(float *room, uint32_t from, int begin, int end, float factor, bool add)
+{
+#pragma unroll 1
+    for (int c = begin; c < end; c += 16) {
+        uint32_t u[16];
+        umma::tensor_memory_load16(from + c, u);
+        umma::tensor_memory_loaded<16>(u);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float *at = room + (c + i) * kTile;
+            *at = add ? __fmaf_rn(*at, factor, __uint_as_float(u[i])) : __uint_as_float(u[i]);
+        }
+    }
+}
+
 struct None {};
 template <bool BIAS> struct Choose { using Type = Tables; };
 template <> struct Choose<false> { using Type = None; };
@@ -604,6 +628,7 @@ struct ForwardParams {
     Heads out, v;
     float *lse;
     Bias bias;
+    float *fold;                             // room for sums of more than kChain tiles, kFoldFloats for each CTA
     int own;                                 // works without a list, and rows of no sequence zeroed here
     PrepParams prep;
 };
@@ -638,7 +663,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         bar_v_empty[kStages], bar_s, bar_read, bar_p[2], bar_o;
     __shared__ uint32_t tensor_base_slot;
     __shared__ int failed_slot, dirty[2];
-    __shared__ float other[2][2][kTile], other_sum[2][kTile];       // maxima (by parity of the tile) and sums of the rows' halves
+    __shared__ float other[2][2][kTile], other_sum[2][kTile], fold_top[2][kTile];      // maxima (by parity of the tile) and sums of the rows' halves
     __shared__ typename Choose<BIAS>::Type tables;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -777,7 +802,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
                             // 16 keys s of the tile; P's columns are 0-63, or 0-31 and 64-95 where it lies in S
                             const int s = (i >> 1) * 4 + part * 2 + (i & 1);
                             umma::multiply_from_tensor_memory(o_at, p_at + (i >> 1) * (kAhead ? 32 : 64) + (part * 2 + (i & 1)) * 8,
-                                                              dv + stage * kNext + s * 128, instr_o, j > 0 || part > 0 || i > 0);
+                                                              dv + stage * kNext + s * 128, instr_o, j % kChain > 0 || part > 0 || i > 0);
                         }
                         if (part == 1) {
                             umma::products_arrive<false>(umma::shared_address(&bar_v_empty[stage]));
@@ -822,6 +847,17 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
             for (int j = 0; j <= tile; ++j, ++t) {
                 ok = ok && wait_all(&bar_s, t & 1, failed);
                 umma::fence_after();
+                if (j > 0 && j % kChain == 0) {
+                    // a chain of sums ends: what lies in memory, of another maximum, and this one
+                    if (kAhead) {
+                        ok = ok && wait_all(&bar_o, (t & 1) ^ 1, failed);
+                        umma::fence_after();
+                    }
+                    float *folded = room_of(P.fold, blockIdx.x, row);
+                    const float factor = top > -INFINITY ? exp2_fast(fold_top[half][row] - top) : 1.0f;
+                    add_to_room(folded, o_at + lanes, o_begin, o_end, factor, j > kChain);
+                    fold_top[half][row] = top;
+                }
                 const bool diagonal = j == 0, near = BIAS && j * kTile - (kTile - 1) < P.bias.last;
                 const float *distance = table + j * kTile + row - col0;           // - column
                 // half a row; with a bias it becomes the whole exponent here, else scale and bias come with the exponential
@@ -866,7 +902,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
                     const float factor = higher > -INFINITY ? exp2_fast(top - higher) : 1.0f;
                     top = higher;
                     sum *= factor;
-                    if (j > 0) {
+                    if (j % kChain > 0) {
                         for (int c = o_begin; c < o_end; c += 16) {
                             uint32_t u[16];
                             umma::tensor_memory_load16(o_at + lanes + c, u);
@@ -935,6 +971,13 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
             }
             for (int c = o_begin; c < o_end; c += 32)
                 put_rows<T>(o_at + lanes, unit, out, P.out.token, c, P.dim, left - (warp & 3) * 32, [&](float *x) {
+                    if (tile >= kChain) {
+                        const float *folded = room_of(P.fold, blockIdx.x, row);
+                        const float factor = top > -INFINITY ? exp2_fast(fold_top[half][row] - top) * unit : unit;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (c + i < o_end) x[i] = __fmaf_rn(folded[(c + i) * kTile], factor, x[i]);
+                    }
                     if (!poisoned) return;
                     const uint16_t *v = (const uint16_t *)P.v.p + (long long)first * P.v.token + kv_of(w.head) * P.v.head;
 #pragma unroll
@@ -986,6 +1029,7 @@ struct BackwardParams {
     int blocks;
     Bias bias;
     float *partials;                         // dbias by slot, head and bucket; NULL: not wanted
+    float *fold;                             // room for sums of more than kChain tiles, twice kFoldFloats for each CTA
     JoinParams join;                         // ticket NULL: a kernel of its own joins them
 };
 
@@ -1128,7 +1172,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
 #pragma unroll
                 for (int s = 0; s < kTile / 16; ++s)        // columns 0-31 and 64-95 hold the halves
                     umma::multiply_from_tensor_memory(to, from + (s >> 2) * 64 + (s & 3) * 8, db_across + (r & 1) * 2 * kNext + which * kNext + s * 128,
-                                                      instr_sum, j > 0 || s > 0);
+                                                      instr_sum, j % kChain > 0 || s > 0);
             }
             __syncwarp();
         };
@@ -1176,7 +1220,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                 add(r, j, 0, t_at, sum0_at);
                 if (umma::elected()) {
                     umma::products_arrive<false>(umma::shared_address(&bars.b_empty[r & 1]));
-                    if (j + 1 == rounds) umma::products_arrive<false>(umma::shared_address(&bars.sums));
+                    if (j + 1 == rounds || (j + 1) % kChain == 0) umma::products_arrive<false>(umma::shared_address(&bars.sums));
                 }
                 __syncwarp();
                 if (j + 1 < rounds) {
@@ -1198,7 +1242,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
         if constexpr (BIAS) table = M.tables.distance + kBefore;
         // where it is not, all works are gone through all the same, without waits, for the barriers in them
         bool ok = true;
-        int r = 0, n = 0, head_before = -1;
+        int r = 0, n = 0, chains = 0, head_before = -1;                     // rounds, works and chains of sums before
         for (int turn = 1; coming.some; ++turn) {
             const Work w = coming;
             coming = work_of(turn);
@@ -1234,6 +1278,15 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                 }
             }
             for (int j = 0; j < rounds; ++j, ++r) {
+                if (j > 0 && j % kChain == 0) {
+                    // before p and ds of this round let the next chain begin
+                    ok = ok && wait_all(&bars.sums, chains++ & 1, failed);
+                    umma::fence_after();
+                    for (int which = 0; which < (KEYS ? 2 : 1); ++which)
+                        add_to_room(room_of(P.fold, blockIdx.x * 2 + which, row), (which ? sum1_at : sum0_at) + lanes - col0, half * 32 * HALVES,
+                                    min((half + 1) * 32 * HALVES, P.dim), 1.0f, j > kChain);
+                    umma::fence_before();
+                }
                 const bool diagonal = apart == 0;
                 const bool near = BIAS && apart * kTile - (kTile - 1) < P.bias.last;
                 const int columns = KEYS ? min(item.length - (tile + apart) * kTile, kTile) : kTile;   // columns that exist
@@ -1467,7 +1520,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                     ++q_head;
                 }
             }
-            ok = ok && wait_all(&bars.sums, n & 1, failed);
+            ok = ok && wait_all(&bars.sums, chains++ & 1, failed);
             umma::fence_after();
             if (threadIdx.x < 2) M.dirty[(n & 1) ^ 1][threadIdx.x] = 0;           // read by all in the work before
             barrier_named(1, kSoftmaxThreads);
@@ -1483,6 +1536,12 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                 uint16_t *out = (uint16_t *)O.p + (long long)(first + (warp & 3) * 32) * O.token + head * O.head;
                 for (int c = begin; c < end; c += 32)
                     put_rows<T>((which ? sum1_at : sum0_at) + lanes - col0, times, out, O.token, c, P.dim, left - (warp & 3) * 32, [&](float *x) {
+                        if (rounds > kChain) {
+                            const float *folded = room_of(P.fold, blockIdx.x * 2 + which, row);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (c + i < end) x[i] = __fmaf_rn(folded[(c + i) * kTile], times, x[i]);
+                        }
                         if (!poisoned || row >= left) return;
                         // !KEYS: the keys of this tile up to the query; KEYS: queries (do) of this tile from the key on, all heads
                         for (int g = 0; g < (KEYS ? P.group : 1); ++g) {
