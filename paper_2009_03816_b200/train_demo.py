@@ -15,7 +15,13 @@ copies.  A local step is, all of it on the device:
   AdamW with the clipping factor   training.AdamW, one launch, which also rewrites
                                    the bf16 copies
 
-and every `step` iterations each worker's loss on a common held-out batch --
+With --model block the worker's model is one transformer layer instead, fed with
+packed sequences of uneven lengths from the same source: embedding, causal
+attention with grouped heads and a learned bias by distance (training.Attention),
+a gated activation that keeps its inputs in 8 bits (training.Keep8, which also holds
+what autograd saves of the layer), residual connections, and the same head.
+
+And every `step` iterations each worker's loss on a common held-out batch --
 LinearXent's forward alone, written straight into the swarm's loss vector -- is
 its fitness for one synchronisation (binding.Swarm: psops_sync, or psops_average
 for the averaging baseline).  The result is one JSON object with the best and the
@@ -51,10 +57,35 @@ class TrainConfig:
     m_min: float = 0.3
     c1: float = 0.2
     c2: float = 0.9
+    model: str = "pairs"         # or "block"; the rest is the block's
+    heads: int = 4
+    kv_heads: int = 2
+    ff: int = 512                # width of the gated activation
+    buckets: int = 16            # of the bias, up to a distance of
+    far: int = 64
+
+    @property
+    def shapes(self) -> tuple:
+        """Of the weight matrices, in the order in which a row holds them; the last one is the head's."""
+        V, D = self.vocab, self.dim
+        if self.model == "pairs":
+            return (V, D), (D, D), (V, D)
+        of_head = D // self.heads
+        return ((V, D), (D, D + 2 * self.kv_heads * of_head), (self.buckets, self.heads), (D, D), (D, 2 * self.ff), (self.ff, D), (V, D))
+
+    @property
+    def lengths(self) -> tuple:
+        """Of the packed sequences of a batch, uneven, `tokens` together."""
+        out, left, at = [], self.tokens, 0
+        while left > 0:
+            n = min(left, (90, 17, 128, 1, 200, 64)[at % 6])
+            out.append(n)
+            left, at = left - n, at + 1
+        return tuple(out)
 
     @property
     def N(self) -> int:
-        return 2 * self.vocab * self.dim + self.dim * self.dim
+        return sum(a * b for a, b in self.shapes)
 
     @property
     def ld(self) -> int:
@@ -70,7 +101,7 @@ class Source:
 
     def __init__(self, cfg: TrainConfig, device):
         self.gen = torch.Generator(device=device).manual_seed(cfg.seed)
-        self.vocab, self.device = cfg.vocab, device
+        self.vocab, self.device, self.lengths = cfg.vocab, device, cfg.lengths
         self.after, self.later = (torch.randperm(cfg.vocab, device=device, generator=self.gen) for _ in range(2))
 
     def _draw(self, tokens):
@@ -84,21 +115,37 @@ class Source:
         return x1, x2, torch.where(u < 0.7, self.after[x1], torch.where(u < 0.9, self.later[x2], free))
 
 
+    def packed(self, tokens):
+        """(token, next token) of `tokens` places of packed sequences, as the configuration cuts them."""
+        lengths = self.lengths
+        longest = max(lengths)
+        last, before, free = (self._draw(len(lengths) * n).view(-1, n) for n in (1, 1, longest + 1))
+        u = torch.rand(len(lengths), longest + 1, device=self.device, generator=self.gen)
+        line = [last[:, 0]]
+        before = before[:, 0]
+        for t in range(longest):
+            now = torch.where(u[:, t] < 0.7, self.after[line[-1]], torch.where(u[:, t] < 0.9, self.later[before], free[:, t]))
+            before = line[-1]
+            line.append(now)
+        line = torch.stack(line, 1)
+        x = torch.cat([line[i, :n] for i, n in enumerate(lengths)])
+        y = torch.cat([line[i, 1:n + 1] for i, n in enumerate(lengths)])
+        return x, y
+
+
 class Worker:
     """One particle's model: views of its row, their bf16 copies, gradients and optimiser."""
 
     def __init__(self, cfg: TrainConfig, row, xent):
-        V, D = cfg.vocab, cfg.dim
-        shapes = ((V, D), (D, D), (V, D))
         at, self.weights = 0, []
-        for a, b in shapes:
+        for a, b in cfg.shapes:
             self.weights.append(row[at:at + a * b].view(a, b))
             at += a * b
         self.copies = [w.to(torch.bfloat16) for w in self.weights]
         self.grads = [torch.zeros_like(c) for c in self.copies]
         self.xent = xent
         self.opt = training.AdamW(self.weights, self.grads, bits=cfg.state_bits, copies=self.copies,
-                                  weight_decay=[0.0, cfg.weight_decay, cfg.weight_decay])
+                                  weight_decay=[0.0] + [cfg.weight_decay] * (len(self.weights) - 1))
         self.clip = training.GradNorm(self.grads)
         self.cfg = cfg
 
@@ -133,8 +180,57 @@ class Worker:
         self.clip.close()
 
 
+class BlockWorker(Worker):
+    """A worker whose model is a transformer layer."""
+
+    def __init__(self, cfg: TrainConfig, row, xent):
+        super().__init__(cfg, row, xent)
+        device = row.device
+        self.attention = training.Attention(cfg.tokens, len(cfg.lengths), cfg.heads, cfg.kv_heads, cfg.dim // cfg.heads, device=device,
+                                            buckets=training.distance_buckets(cfg.buckets, cfg.far))
+        self.keep = training.Keep8(device=device)
+        ends = torch.tensor((0,) + cfg.lengths).cumsum(0)
+        self.offsets = ends.to(device=device, dtype=torch.int32)
+        for c, g in zip(self.copies, self.grads):
+            c.requires_grad_(True)
+            c.grad = g
+
+    def hidden(self, x):
+        cfg = self.cfg
+        e, qkv, bias, out, up, down, _ = self.copies
+        h = e[x]
+        # queries, keys and values side by side, as one product leaves them
+        p = (h @ qkv).view(-1, cfg.heads + 2 * cfg.kv_heads, cfg.dim // cfg.heads)
+        q, k, v = p.split([cfg.heads, cfg.kv_heads, cfg.kv_heads], 1)
+        h = h + self.attention(q, k, v, self.offsets, bias).reshape(-1, cfg.dim) @ out
+        a, b = (h @ up).chunk(2, -1)
+        return h + self.keep(a, b, "silu") @ down
+
+    def local_step(self, x, y, one):
+        for g in self.grads:
+            g.zero_()
+        with self.keep.hooks():
+            h = self.hidden(x)
+        self.xent(h, self.copies[-1], y).backward(one)
+        _, factor = self.clip.norm(self.cfg.max_norm)
+        self.opt.step(self.cfg.lr, factor)
+
+    def loss_into(self, out, x, y):
+        with torch.no_grad():
+            self.xent.forward(self.hidden(x), self.copies[-1], y, loss=out)
+
+    def reread(self):
+        with torch.no_grad():
+            super().reread()
+
+    def close(self):
+        super().close()
+        self.attention.close()
+        self.keep.close()
+
+
 def run(method: str, cfg: TrainConfig = TrainConfig(), device="cuda:0") -> dict:
-    assert method in ("pso", "pa")
+    assert method in ("pso", "pa") and cfg.model in ("pairs", "block")
     _build.build_library()
     device = torch.device(device)
     gen = torch.Generator(device=device).manual_seed(cfg.seed + 1)
@@ -144,9 +240,10 @@ def run(method: str, cfg: TrainConfig = TrainConfig(), device="cuda:0") -> dict:
     swarm = binding.Swarm(x, v, p, N=cfg.N, m_max=cfg.m_max, m_min=cfg.m_min, t_max=cfg.t_max, c1=cfg.c1, c2=cfg.c2,
                           seed=cfg.seed)
     xent = training.LinearXent(cfg.tokens, cfg.dim, cfg.vocab, device=device)
-    workers = [Worker(cfg, x[k], xent) for k in range(cfg.K)]
+    workers = [(Worker if cfg.model == "pairs" else BlockWorker)(cfg, x[k], xent) for k in range(cfg.K)]
     source = Source(cfg, device)
-    held_out = source.batch(cfg.tokens)
+    draw = source.batch if cfg.model == "pairs" else source.packed
+    held_out = draw(cfg.tokens)
     one = torch.ones((), device=device)
     losses = torch.zeros(cfg.K, device=device)
 
@@ -159,7 +256,7 @@ def run(method: str, cfg: TrainConfig = TrainConfig(), device="cuda:0") -> dict:
     best, mean, chosen = [], [], []
     for it in range(1, cfg.t_max + 1):
         for worker in workers:
-            worker.local_step(*source.batch(cfg.tokens), one)
+            worker.local_step(*draw(cfg.tokens), one)
         if it % cfg.step:
             continue
         if method == "pa":

@@ -1,0 +1,454 @@
+"""Attention where it can go wrong: what lies in masked places, biases that mask, strides, given results, streams and
+graphs, large offsets, long sums; refusals of the C entries; the differentiable form."""
+import math
+
+import pytest
+import torch
+
+from attention_util import compare, inputs, lengths_to_offsets, reference
+from paper_2009_03816_b200 import binding, training
+from paper_2009_03816_b200 import build as _build
+
+pytestmark = pytest.mark.gpu
+BF16, F16 = torch.bfloat16, torch.float16
+NAMES = ("out", "lse", "dq", "dk", "dv")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _library():
+    _build.build_library()
+
+
+def both(op, x, offsets, **kw):
+    """Results of both passes by name."""
+    bias = x.get("bias")
+    out, lse = op.forward(x["q"], x["k"], x["v"], offsets, bias)
+    dq, dk, dv, dbias = op.backward(x["q"], x["k"], x["v"], offsets, out, lse, x["grad"], bias)
+    return dict(out=out, lse=lse, dq=dq, dk=dk, dv=dv, **({"dbias": dbias} if bias is not None else {}))
+
+
+def make(lengths, heads=2, kv_heads=1, dim=64, dtype=BF16, first=0, rest=0, buckets=None, seed=0, **kw):
+    T = first + sum(lengths) + rest
+    x = inputs(T, heads, kv_heads, dim, dtype, seed, True, buckets)
+    op = training.Attention(T, max(1, len(lengths)), heads, kv_heads, dim, dtype=dtype, buckets=buckets, **kw)
+    return op, x, lengths_to_offsets(lengths, first)
+
+
+def same(a, b, rows=slice(None)):
+    for name in a:
+        p, q = (a[name][:, rows], b[name][:, rows]) if name == "lse" else (a[name][rows], b[name][rows])
+        if name != "dbias":
+            assert torch.equal(p, q), name
+
+
+# ---- masked places -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("dim", [64, 80])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+def test_other_sequences_and_rows_of_none_reach_nothing(what, dim, dtype):
+    lengths, first, rest = [70, 130, 200], 20, 60
+    op, x, offsets = make(lengths, 2, 1, dim, dtype, first, rest, buckets=[0, 1, 2, 8])
+    clean = both(op, x, offsets)
+    for lo, hi in ((0, 20), (420, 480), (90, 220)):          # in front, behind, the middle sequence
+        y = {k: v.clone() if k != "bias" else v for k, v in x.items()}
+        for name in ("q", "k", "v", "grad"):
+            y[name][lo:hi] = what
+        got = both(op, y, offsets)
+        for a, b in ((20, 90), (90, 220), (220, 420)):
+            if (a, b) != (lo, hi):
+                # ds of fp16 is scaled by what is finite of do and v: other rows' norms may move it by a power of two
+                same(got, clean, slice(a, b)) if dtype == BF16 else [
+                    torch.testing.assert_close(got[n][a:b], clean[n][a:b], rtol=2e-2, atol=2e-3) for n in ("out", "dq", "dk", "dv")]
+        if (lo, hi) == (90, 220):
+            assert not torch.isfinite(got["out"][90:220]).any()
+        else:
+            assert torch.isfinite(got["dbias"]).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("at", [0, 37, 127, 128, 200, 299])
+@pytest.mark.parametrize("name", ["k", "v"])
+def test_later_tokens_reach_nothing(name, at, dim):
+    op, x, offsets = make([300], 2, 1, dim, BF16)
+    clean = both(op, x, offsets)
+    y = {k: v.clone() for k, v in x.items()}
+    y[name][at, 0, 3] = math.inf if name == "v" else math.nan
+    got = both(op, y, offsets)
+    # rows before `at` see none of it, forward and in dq; rows from `at` on do
+    assert torch.equal(got["out"][:at], clean["out"][:at]) and torch.equal(got["lse"][:, :at], clean["lse"][:, :at])
+    assert torch.equal(got["dq"][:at], clean["dq"][:at])
+    if name == "v":
+        assert (got["out"][at:, :, 3] == math.inf).all() and torch.equal(got["out"][at:, :, :3], clean["out"][at:, :, :3])
+    else:
+        assert got["out"][at:].isnan().all() and got["lse"][:, at:].isnan().all()
+    assert not torch.isfinite(got["dq"][at:]).all(-1).any()
+
+
+@pytest.mark.parametrize("at", [0, 64, 128, 255, 299])
+def test_earlier_keys_see_none_of_an_earlier_gradient(at):
+    """do of token `at` reaches dk and dv of keys up to it, none behind it."""
+    op, x, offsets = make([300], 2, 1, 64, BF16)
+    clean = both(op, x, offsets)
+    y = {k: v.clone() for k, v in x.items()}
+    y["grad"][at, 1, 7] = math.inf
+    got = both(op, y, offsets)
+    for name in ("dk", "dv"):
+        assert torch.equal(got[name][at + 1:], clean[name][at + 1:]), name
+    assert not torch.isfinite(got["dv"][:at + 1, :, 7]).any()
+    assert torch.equal(got["dq"][:at], clean["dq"][:at]) and torch.equal(got["dq"][at + 1:], clean["dq"][at + 1:])
+
+
+@pytest.mark.parametrize("lowest", [-math.inf, torch.finfo(torch.float32).min, -1e31])
+def test_biases_that_mask(lowest):
+    """Distances of a masked bucket count for nothing; a row with none left is zeros with lse -inf."""
+    buckets = [0, 1, 40, 200]
+    op, x, offsets = make([500, 30], 2, 2, 64, BF16, buckets=buckets)
+    x["bias"] = x["bias"].float()
+    op2 = training.Attention(530, 2, 2, 2, 64, buckets=buckets)
+    x["bias"][2] = lowest                                          # distances 40 to 199
+    y = dict(x, bias=x["bias"].clone())
+    y["bias"][2] = -math.inf
+    got = both(op2, x, offsets)
+    compare(got, reference(x["q"], x["k"], x["v"], [500, 30], 0, x["grad"], y["bias"], buckets))
+    assert not got["dbias"][2].any()
+    y["bias"][:, 0] = lowest                                       # all of one head
+    got = both(op, y, offsets)
+    assert not got["out"][:, 0].any() and (got["lse"][0] == -math.inf).all()
+    assert not got["dq"][:, 0].any() and not got["dk"][:, 0].any() and not got["dv"][:, 0].any() and not got["dbias"][:, 0].any()
+    assert torch.isfinite(got["out"]).all() and torch.isfinite(got["dk"]).all()
+    y["bias"][1:, 1] = lowest                                      # the token itself alone
+    got = both(op, y, offsets)
+    assert torch.equal(got["out"][:, 1], x["v"][:, 1])
+
+
+def test_empty_calls():
+    op = training.Attention(50, 4, 2, 1, 16, buckets=[0, 3])
+    x = inputs(40, 2, 1, 16, BF16, buckets=[0, 3])
+    for offsets in (torch.tensor([0], dtype=torch.int32, device="cuda"), lengths_to_offsets([0, 0, 0], 7)):
+        got = both(op, x, offsets)
+        for name, t in got.items():
+            assert not t.any(), name
+    y = {k: v[:0] if k != "bias" else v for k, v in x.items()}
+    got = both(op, y, lengths_to_offsets([0, 0]))
+    assert got["out"].shape == (0, 2, 16) and got["lse"].shape == (2, 0) and not got["dbias"].any()
+
+
+def test_offsets_out_of_order_stay_in_bounds():
+    """Whatever the offsets hold, nothing outside the tensors is touched and the call ends."""
+    room = torch.full((300 * 64 + 200,), 7.0, dtype=BF16, device="cuda")
+    op = training.Attention(100, 6, 3, 3, 64)
+    x = inputs(100, 3, 3, 64, BF16)
+    out = room[104:104 + 300 * 64].view(100, 3, 64)
+    for bad in ([5, 90, 10, 100, 0, 100, 100], [-50, 30, 1000, 2 ** 31 - 1, -2 ** 31, 60, 80], [100, 0, 100, 0, 100, 0, 100]):
+        offsets = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        _, lse = op.forward(x["q"], x["k"], x["v"], offsets, out=out)
+        op.backward(x["q"], x["k"], x["v"], offsets, out, lse, x["grad"])
+        torch.cuda.synchronize()
+        assert (room[:104] == 7.0).all() and (room[104 + 300 * 64:] == 7.0).all()
+    # and the holder still works
+    offsets = lengths_to_offsets([60, 40])
+    compare(both(op, x, offsets), reference(x["q"], x["k"], x["v"], [60, 40], 0, x["grad"]))
+
+
+# ---- layouts ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_layouts(dtype):
+    """Head-major tensors, gaps between rows, given results in views of one buffer; the same bits each time."""
+    lengths, H, G, D = [150, 90], 4, 2, 40
+    op, x, offsets = make(lengths, H, G, D, dtype, first=5, rest=9)
+    want = both(op, x, offsets)
+    T = 254
+    head_major = {n: t.transpose(0, 1).contiguous().transpose(0, 1) for n, t in x.items()}
+    assert head_major["q"].stride() == (D, T * D, 1)
+    for name, t in both(op, head_major, offsets).items():
+        assert torch.equal(t, want[name]), name
+    wide = {}
+    for n, t in x.items():
+        room = torch.full((T, t.shape[1] + 1, D + 8), math.nan, dtype=dtype, device="cuda")
+        room[:, :t.shape[1], :D] = t
+        wide[n] = room[:, :t.shape[1], :D]
+    for name, t in both(op, wide, offsets).items():
+        assert torch.equal(t, want[name]), name
+    joint = torch.full((T, H + 2 * G, D), 3.0, dtype=dtype, device="cuda")
+    dq, dk, dv = joint[:, :H], joint[:, H:H + G], joint[:, H + G:]
+    op.backward(x["q"], x["k"], x["v"], offsets, want["out"], want["lse"], x["grad"], dq=dq, dk=dk, dv=dv)
+    for name, t in (("dq", dq), ("dk", dk), ("dv", dv)):
+        assert torch.equal(t[5:245], want[name][5:245])
+    assert (joint[:5] == 3.0).all() and (joint[245:] == 3.0).all()                # rows of no sequence as they were
+    out = torch.full((H, T, D), 3.0, dtype=dtype, device="cuda").transpose(0, 1)
+    op.forward(x["q"], x["k"], x["v"], offsets, out=out)
+    assert torch.equal(out[5:245], want["out"][5:245]) and (out[:5] == 3.0).all() and (out[245:] == 3.0).all()
+
+
+def test_what_is_wanted():
+    op, x, offsets = make([200], 2, 2, 64, BF16, buckets=[0, 2, 50])
+    want = both(op, x, offsets)
+    for wanted in ((True, False, False, False), (False, True, False, False), (False, False, True, False), (False, False, False, True),
+                   (True, False, True, False), (False, False, False, False)):
+        got = op.backward(x["q"], x["k"], x["v"], offsets, want["out"], want["lse"], x["grad"], x["bias"], want=wanted)
+        for name, t, w in zip(("dq", "dk", "dv", "dbias"), got, wanted):
+            assert torch.equal(t, want[name]) if w else t is None
+
+
+def test_the_same_bits_again():
+    lengths = [300, 5, 128, 77, 600, 1, 1, 250]
+    op, x, offsets = make(lengths, 4, 2, 128, BF16, buckets=training.distance_buckets(16, 100))
+    want = both(op, x, offsets)
+    for _ in range(5):
+        for name, t in both(op, x, offsets).items():
+            assert torch.equal(t, want[name]), name
+    # nor does it matter what else is in the batch: the sequence of 600 alone
+    at = sum(lengths[:4])
+    rows = slice(at, at + 600)
+    alone = training.Attention(600, 1, 4, 2, 128, buckets=training.distance_buckets(16, 100))
+    y = {n: t[rows] if n != "bias" else t for n, t in x.items()}
+    got = both(alone, y, lengths_to_offsets([600]))
+    for name in ("out", "dq", "dk", "dv"):
+        assert torch.equal(got[name], want[name][rows]), name
+
+
+@pytest.mark.parametrize("case", ["many short", "one long", "few sums", "many sums"])
+def test_lists_of_tiles(case):
+    """The list's kernel and the search without it; dbias joined within and by a kernel of its own."""
+    buckets = [0, 1, 2, 30]
+    lengths = {"many short": [1 + i % 5 for i in range(1500)], "one long": [5000], "few sums": [100, 40], "many sums": [129] * 60}[case]
+    op, x, offsets = make(lengths, 1 if case != "few sums" else 2, 1, 32, BF16, buckets=buckets)
+    compare(both(op, x, offsets), reference(x["q"], x["k"], x["v"], lengths, 0, x["grad"], x["bias"], buckets), case)
+
+
+@pytest.mark.parametrize("kv_heads", [1, 2])
+def test_sums_of_more_terms_than_go_at_a_time(kv_heads):
+    """A row of 17,000 keys and keys of 34,000 queries, all numbers of one sign: cut-off sums must not add up."""
+    T = 17000
+    x = inputs(T, 2, kv_heads, 32, F16)
+    x = {n: (t.abs() + 0.5).contiguous() if n in ("v", "grad") else (t * 0.1).contiguous() for n, t in x.items()}
+    op = training.Attention(T, 1, 2, kv_heads, 32, dtype=F16)
+    got = both(op, x, lengths_to_offsets([T]))
+    want = reference(x["q"], x["k"], x["v"], [T], 0, x["grad"])
+    compare(got, want)
+    # 16,384 terms are 1,024 cut sums, each off by 2^-23 of the sum at most; half of that on average, and results are rounded
+    for name in ("out", "dv"):
+        exact = want[name][0]
+        bias = float(((got[name].double() - exact) * exact).sum() / (exact * exact).sum())
+        assert abs(bias) < 1024 * 2.0 ** -23 + 2.0 ** -13, (name, bias)
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements of q: the last sequences of a large batch."""
+    T, H = 140_000, 128
+    lengths = [100] * 1400
+    q = torch.empty(T, H, 128, dtype=BF16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(3))
+    assert q.numel() > 2 ** 31
+    k, v = q[:, :1].clone(), q[:, 1:2].clone()
+    grad = torch.empty_like(q).normal_()
+    op = training.Attention(T, 1400, H, 1, 128)
+    offsets = lengths_to_offsets(lengths)
+    out, lse = op.forward(q, k, v, offsets)
+    dq, dk, dv, _ = op.backward(q, k, v, offsets, out, lse, grad)
+    rows = slice(T - 200, T)
+    want = reference(q[rows], k[rows], v[rows], [100, 100], 0, grad[rows])
+    compare(dict(out=out[rows], lse=lse[:, rows], dq=dq[rows], dk=dk[rows], dv=dv[rows]), want)
+
+
+# ---- streams, graphs, the context ------------------------------------------------------------------------
+
+def test_streams_and_graphs():
+    lengths = [300, 40, 128]
+    op, x, offsets = make(lengths, 2, 1, 64, BF16, buckets=[0, 1, 60])
+    want = both(op, x, offsets)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, torch.cuda.current_stream(), side):
+        with torch.cuda.stream(stream):
+            got = both(op, x, offsets)
+        stream.synchronize()
+        for name, t in got.items():
+            assert torch.equal(t, want[name]), name
+    y = {n: t.clone() for n, t in x.items()}
+    lengths_held = offsets.clone()
+    with torch.cuda.stream(side):
+        both(op, y, lengths_held)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        held = both(op, y, lengths_held)
+    for seed, other in ((1, [300, 40, 128]), (2, [1, 467, 0]), (3, [200, 200, 60])):
+        z = inputs(468, 2, 1, 64, BF16, seed, True, [0, 1, 60])
+        for n in y:
+            y[n].copy_(z[n])
+        lengths_held.copy_(lengths_to_offsets(other))
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = training.Attention(468, 3, 2, 1, 64, buckets=[0, 1, 60])
+        for name, t in both(eager, z, lengths_to_offsets(other)).items():
+            rows = slice(0, sum(other))
+            assert torch.equal(t, held[name]), (seed, name)
+    # a captured backward pass while an eager graph of the same leaves lives
+    leaves = [t.clone().requires_grad_() for t in (x["q"], x["k"], x["v"])]
+    alive = op(*leaves, offsets, x["bias"])
+    with torch.cuda.stream(side):
+        op(*leaves, offsets, x["bias"]).backward(x["grad"])
+    side.synchronize()
+    graph2 = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph2, stream=side):
+        captured = both(op, x, offsets)
+    graph2.replay()
+    torch.cuda.synchronize()
+    for name, t in captured.items():
+        assert torch.equal(t, want[name]), name
+    alive.backward(x["grad"])
+    torch.cuda.synchronize()
+
+
+def test_a_stream_of_its_own():
+    side = torch.cuda.Stream()
+    op, x, offsets = make([300, 40], 2, 1, 64, BF16, stream=side.cuda_stream)
+    plain, _, _ = make([300, 40], 2, 1, 64, BF16)
+    want = both(plain, x, offsets)
+    leaves = [t.clone().requires_grad_() for t in (x["q"], x["k"], x["v"])]
+    out = op(*leaves, offsets)                           # the differentiable call's results are the current stream's
+    out.backward(x["grad"])
+    for name, t in (("out", out), ("dq", leaves[0].grad), ("dk", leaves[1].grad), ("dv", leaves[2].grad)):
+        assert torch.equal(t, want[name]), name
+
+
+def test_creation_inside_a_capture_is_refused():
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        for make_one in (lambda: training.Attention(10, 1, 1, 1, 8), lambda: training.Keep8()):
+            with pytest.raises(binding.PsopsError) as e:
+                make_one()
+            assert e.value.code == binding.PSOPS_ESTATE
+
+
+def test_refusals_of_the_entries():
+    lib = binding.load()
+    op = training.Attention(64, 2, 4, 2, 16, buckets=[0, 5])
+    plain = training.Attention(64, 2, 4, 2, 16, gradients=False)
+    x = inputs(64, 4, 2, 16, BF16, buckets=[0, 5])
+    offsets = lengths_to_offsets([60, 4])
+    h = lambda t, a=None, b=None, off=0: binding.psops_heads(t.data_ptr() + off, t.stride(0) if a is None else a, t.stride(1) if b is None else b)
+    q, k, v, out = h(x["q"]), h(x["k"]), h(x["v"]), h(torch.empty(64, 4, 16, dtype=BF16, device="cuda"))
+    lse = torch.zeros(4, 64, device="cuda")
+    bias, kind = x["bias"].data_ptr(), binding.PSOPS_BF16
+    at = offsets.data_ptr()
+
+    def forward(q=q, k=k, v=v, at=at, n=2, T=64, bias=bias, kind=kind, out=out, lse=lse.data_ptr(), ctx=op.ctx):
+        return lib.psops_attention_forward(ctx, q, k, v, at, n, T, bias, kind, out, lse, 0)
+
+    assert forward() == binding.PSOPS_OK
+    for kw in (dict(T=65), dict(T=-1), dict(n=3), dict(n=-1), dict(q=None), dict(out=None), dict(at=None), dict(bias=None), dict(kind=F16),
+               dict(kind=binding.PSOPS_F16), dict(lse=None), dict(q=h(x["q"], a=8)), dict(q=h(x["q"], b=8)), dict(k=binding.psops_heads(None, 32, 16)),
+               dict(out=h(x["q"], a=40, b=16)), dict(v=h(x["v"], a=1 << 39)), dict(ctx=plain.ctx)):
+        if kw.get("kind") is F16:
+            kw = dict(kind=7)
+        assert forward(**kw) == binding.PSOPS_EINVAL, kw
+    for kw in (dict(q=h(x["q"], off=2)), dict(q=h(x["q"], a=132)), dict(k=h(x["k"], b=20)), dict(at=at + 2), dict(bias=bias + 1),
+               dict(lse=lse.data_ptr() + 2), dict(out=h(x["q"], off=8))):
+        assert forward(**kw) == binding.PSOPS_EALIGN, kw
+    back = lambda ctx=op.ctx, dq=out, db=None, grad=out: lib.psops_attention_backward(ctx, q, k, v, at, 2, 64, bias if ctx is op.ctx else None, kind, out,
+                                                                                      lse.data_ptr(), grad, dq, None, None, db, 0)
+    assert back(ctx=plain.ctx) == binding.PSOPS_ESTATE
+    assert back(grad=None) == binding.PSOPS_EINVAL
+    assert back(dq=h(x["q"], a=40, b=16)) == binding.PSOPS_EINVAL
+    assert back(db=lse.data_ptr() + 1) == binding.PSOPS_EALIGN
+    torch.cuda.synchronize()
+    with pytest.raises(binding.PsopsError) as e:
+        training.Attention(64, 2, 4, 2, 12)
+    assert e.value.code == binding.PSOPS_EINVAL
+
+
+# ---- the differentiable form --------------------------------------------------------------------------------
+
+def test_autograd_with_any_strides_and_shared_inputs():
+    T, H, D = 200, 4, 24
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    base = torch.empty(H, D, T, device="cuda").normal_(generator=gen).to(BF16)
+    q = base.permute(2, 0, 1).detach().requires_grad_()                       # elements of a head T apart
+    kv = torch.empty(T, 1, D, device="cuda").normal_(generator=gen).to(BF16).requires_grad_()
+    k = kv.expand(T, 2, D)                                                    # one head broadcast to two: its gradient is their sum
+    table = torch.empty(8, 3, device="cuda").normal_(generator=gen).requires_grad_()
+    bias = table.T[:, :H]                                                     # a slice of a transposed table
+    op = training.Attention(T, 2, H, 2, D, buckets=[0, 4, 20])
+    offsets = lengths_to_offsets([120, 80])
+    out = op(q, k, kv.expand(T, 2, D), offsets, bias)
+    grad = torch.empty(T, H, D, device="cuda").normal_(generator=gen).to(BF16)
+    out.backward(grad)
+    full = k.detach().contiguous()
+    want = reference(q.detach().contiguous(), full, full, [120, 80], 0, grad, bias.detach().contiguous(), [0, 4, 20])
+    compare({"out": out.detach(), "dq": q.grad}, want)
+    exact = (want["dk"][0] + want["dv"][0]).sum(1, keepdim=True)
+    size = (want["dk"][0].abs() + want["dv"][0].abs()).sum(1, keepdim=True)
+    bound = (want["dk"][1] + want["dv"][1]).sum(1, keepdim=True)
+    # torch adds the heads and the two uses in bf16: three more roundings of sums no larger than `size`
+    assert bool(((kv.grad.double() - exact).abs() <= bound + 3 * 2.0 ** -8 * (size + bound)).all())
+    assert bool(((table.grad.double()[:4].T - want["dbias"][0]).abs() <= want["dbias"][1] + 2.0 ** -23 * want["dbias"][0].abs()).all())
+    assert not table.grad[4:].any()
+    # an upstream gradient that is broadcast
+    q2 = q.detach().clone().requires_grad_()
+    op(q2, full, full, offsets, bias.detach()).sum().backward()
+    ones = reference(q2.detach().contiguous(), full, full, [120, 80], 0, torch.ones_like(grad), bias.detach().contiguous(), [0, 4, 20])
+    compare({"dq": q2.grad}, ones)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_gradients_against_differences(dtype):
+    """d/dt of sum(grad out) along a direction, by differences of the formula in 64 bits, against the kernel's gradients."""
+    lengths, buckets = [90, 170], [0, 1, 3, 10, 40]
+    op, x, offsets = make(lengths, 4, 2, 40, dtype, buckets=buckets, seed=9)
+    got = both(op, x, offsets)
+    want = reference(x["q"], x["k"], x["v"], lengths, 0, x["grad"], x["bias"], buckets)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    for name, of in (("dq", "q"), ("dk", "k"), ("dv", "v"), ("dbias", "bias")):
+        direction = torch.empty(x[of].shape, dtype=torch.float64, device="cuda").normal_(generator=gen)
+        def value(t):
+            y = {n: v.double() for n, v in x.items()}
+            y[of] = y[of] + t * direction
+            out = reference64(y, lengths, buckets)
+            return float((out * x["grad"].double()).sum())
+        step = 1e-4
+        slope = (value(step) - value(-step)) / (2 * step)
+        mine = float((got[name].double() * direction).sum())
+        bound = float((want[name][1] * direction.abs()).sum())
+        assert abs(mine - slope) <= bound + 1e-5 * (1 + abs(slope)), (name, mine, slope, bound)
+
+
+def reference64(y, lengths, buckets):
+    out = torch.zeros_like(y["q"])
+    at, g = 0, y["q"].shape[1] // y["k"].shape[1]
+    for n in lengths:
+        r = slice(at, at + n)
+        at += n
+        d = torch.arange(n, device="cuda")[:, None] - torch.arange(n, device="cuda")
+        of = torch.bucketize(d.clamp(min=0), torch.tensor(buckets, device="cuda"), right=True) - 1
+        for h in range(out.shape[1]):
+            s = y["q"][r, h] @ y["k"][r, h // g].T / y["q"].shape[2] ** 0.5 + y["bias"][:, h][of]
+            out[r, h] = torch.softmax(torch.where(d >= 0, s, -math.inf), -1) @ y["v"][r, h // g]
+    return out
+
+
+def test_second_derivatives_raise():
+    op, x, offsets = make([20], 1, 1, 16, BF16)
+    q = x["q"].detach().contiguous().requires_grad_()
+    (dq,) = torch.autograd.grad(op(q, x["k"], x["v"], offsets).float().pow(2).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dq.float().sum().backward()
+
+
+def test_given_results_count_as_changes():
+    op, x, offsets = make([20], 1, 1, 16, BF16)
+    out = torch.zeros(20, 1, 16, dtype=BF16, device="cuda")
+    leaf = torch.ones(1, device="cuda", dtype=BF16, requires_grad=True)
+    loss = (leaf * out).sum()
+    op.forward(x["q"], x["k"], x["v"], offsets, out=out)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        loss.backward()
+
+
+def test_launches_are_counted():
+    op, x, offsets = make([100], 1, 1, 16, BF16)
+    both(op, x, offsets)
+    assert op.launches == 1 + 2                            # a short batch: no list forward; two kernels backward
