@@ -688,8 +688,8 @@ int psops_attention_destroy(psops_attention *a);
  * bytes behind a row's last code are set to 0.  Scales: ceil(cols / 128) for each
  * row, row after row.
  *
- * psops_keep8_activate: y = f(a), or f(a) * b where d_b is not NULL, from the inputs
- * as they are, and the inputs in 8 bits.  psops_keep8_activate_backward, from the
+ * psops_keep_activate: y = f(a), or f(a) * b where d_b is not NULL, from the inputs
+ * as they are, and the inputs in 8 bits.  psops_keep_activate_backward, from the
  * values A, B that these stand for and the gradient of y:
  *   da = dy * B * f'(A),  db = dy * f(A),  y = f(A) * B   (B = 1 where d_b_codes is NULL)
  * each of which may be NULL (not wanted); y is for a backward pass that needs it
@@ -710,24 +710,24 @@ int psops_attention_destroy(psops_attention *a);
 #define PSOPS_SILU       1
 #define PSOPS_GELU       2
 
-typedef struct psops_keep8 psops_keep8;  /* opaque */
+typedef struct psops_keep psops_keep;  /* opaque */
 
-int psops_keep8_create(psops_keep8 **out, void *cuda_stream);
-int psops_keep8_pack(psops_keep8 *k, int32_t type, int64_t rows, int64_t cols, const void *d_x, int64_t x_ld,
+int psops_keep_create(psops_keep **out, void *cuda_stream);
+int psops_keep_pack(psops_keep *k, int32_t type, int64_t rows, int64_t cols, const void *d_x, int64_t x_ld,
                      void *d_codes, float *d_scales);
-int psops_keep8_unpack(psops_keep8 *k, int32_t type, int64_t rows, int64_t cols, const void *d_codes,
+int psops_keep_unpack(psops_keep *k, int32_t type, int64_t rows, int64_t cols, const void *d_codes,
                        const float *d_scales, void *d_x, int64_t x_ld);
-int psops_keep8_activate(psops_keep8 *k, int32_t kind, int32_t type, int64_t rows, int64_t cols, const void *d_a,
+int psops_keep_activate(psops_keep *k, int32_t kind, int32_t type, int64_t rows, int64_t cols, const void *d_a,
                          int64_t a_ld, const void *d_b, int64_t b_ld, void *d_y, int64_t y_ld, void *d_a_codes,
                          float *d_a_scales, void *d_b_codes, float *d_b_scales);
-int psops_keep8_activate_backward(psops_keep8 *k, int32_t kind, int32_t type, int64_t rows, int64_t cols,
+int psops_keep_activate_backward(psops_keep *k, int32_t kind, int32_t type, int64_t rows, int64_t cols,
                                   const void *d_a_codes, const float *d_a_scales, const void *d_b_codes,
                                   const float *d_b_scales, const void *d_dy, int64_t dy_ld, void *d_da, int64_t da_ld,
                                   void *d_db, int64_t db_ld, void *d_y, int64_t y_ld);
-int psops_keep8_set_stream(psops_keep8 *k, void *cuda_stream);
-int64_t psops_keep8_launch_count(const psops_keep8 *k);
-const char *psops_keep8_last_error(const psops_keep8 *k);
-int psops_keep8_destroy(psops_keep8 *k);
+int psops_keep_set_stream(psops_keep *k, void *cuda_stream);
+int64_t psops_keep_launch_count(const psops_keep *k);
+const char *psops_keep_last_error(const psops_keep *k);
+int psops_keep_destroy(psops_keep *k);
 
 #ifdef __cplusplus
 }

@@ -49,9 +49,9 @@ EXPORTS = [
     "psops_attention_workspace_bytes", "psops_attention_create", "psops_attention_forward", "psops_attention_backward",
     "psops_attention_set_stream", "psops_attention_launch_count", "psops_attention_last_error",
     "psops_attention_destroy",
-    "psops_keep8_create", "psops_keep8_pack", "psops_keep8_unpack", "psops_keep8_activate",
-    "psops_keep8_activate_backward", "psops_keep8_set_stream", "psops_keep8_launch_count", "psops_keep8_last_error",
-    "psops_keep8_destroy",
+    "psops_keep_create", "psops_keep_pack", "psops_keep_unpack", "psops_keep_activate",
+    "psops_keep_activate_backward", "psops_keep_set_stream", "psops_keep_launch_count", "psops_keep_last_error",
+    "psops_keep_destroy",
 ]
 
 
@@ -192,17 +192,17 @@ def load() -> ctypes.CDLL:
         "psops_attention_launch_count": (ctypes.c_int64, [_vp]),
         "psops_attention_last_error": (ctypes.c_char_p, [_vp]),
         "psops_attention_destroy": (ctypes.c_int, [_vp]),
-        "psops_keep8_create": (ctypes.c_int, [ctypes.POINTER(_vp), _vp]),
-        "psops_keep8_pack": (ctypes.c_int, [_vp, _i32, _i64, _i64, _vp, _i64, _vp, _f32p]),
-        "psops_keep8_unpack": (ctypes.c_int, [_vp, _i32, _i64, _i64, _vp, _f32p, _vp, _i64]),
-        "psops_keep8_activate": (ctypes.c_int, [_vp, _i32, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _f32p,
+        "psops_keep_create": (ctypes.c_int, [ctypes.POINTER(_vp), _vp]),
+        "psops_keep_pack": (ctypes.c_int, [_vp, _i32, _i64, _i64, _vp, _i64, _vp, _f32p]),
+        "psops_keep_unpack": (ctypes.c_int, [_vp, _i32, _i64, _i64, _vp, _f32p, _vp, _i64]),
+        "psops_keep_activate": (ctypes.c_int, [_vp, _i32, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _f32p,
                                                 _vp, _f32p]),
-        "psops_keep8_activate_backward": (ctypes.c_int, [_vp, _i32, _i32, _i64, _i64, _vp, _f32p, _vp, _f32p, _vp, _i64,
+        "psops_keep_activate_backward": (ctypes.c_int, [_vp, _i32, _i32, _i64, _i64, _vp, _f32p, _vp, _f32p, _vp, _i64,
                                                          _vp, _i64, _vp, _i64, _vp, _i64]),
-        "psops_keep8_set_stream": (ctypes.c_int, [_vp, _vp]),
-        "psops_keep8_launch_count": (ctypes.c_int64, [_vp]),
-        "psops_keep8_last_error": (ctypes.c_char_p, [_vp]),
-        "psops_keep8_destroy": (ctypes.c_int, [_vp]),
+        "psops_keep_set_stream": (ctypes.c_int, [_vp, _vp]),
+        "psops_keep_launch_count": (ctypes.c_int64, [_vp]),
+        "psops_keep_last_error": (ctypes.c_char_p, [_vp]),
+        "psops_keep_destroy": (ctypes.c_int, [_vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)            # AttributeError if a symbol is missing
@@ -562,48 +562,48 @@ def psops_attention_destroy(a) -> None:
     _check(load().psops_attention_destroy(a), "psops_attention_destroy")
 
 
-def psops_keep8_create(stream=None):
+def psops_keep_create(stream=None):
     handle = _vp()
-    _check(load().psops_keep8_create(ctypes.byref(handle), int(stream) if stream else None), "psops_keep8_create")
+    _check(load().psops_keep_create(ctypes.byref(handle), int(stream) if stream else None), "psops_keep_create")
     return handle
 
 
-def psops_keep8_pack(k, type_, rows, cols, d_x, x_ld, d_codes, d_scales) -> None:
-    _check(load().psops_keep8_pack(k, type_, rows, cols, _ptr(d_x), x_ld, _ptr(d_codes), _ptr(d_scales)),
-           "psops_keep8_pack", k, "psops_keep8_last_error")
+def psops_keep_pack(k, type_, rows, cols, d_x, x_ld, d_codes, d_scales) -> None:
+    _check(load().psops_keep_pack(k, type_, rows, cols, _ptr(d_x), x_ld, _ptr(d_codes), _ptr(d_scales)),
+           "psops_keep_pack", k, "psops_keep_last_error")
 
 
-def psops_keep8_unpack(k, type_, rows, cols, d_codes, d_scales, d_x, x_ld) -> None:
-    _check(load().psops_keep8_unpack(k, type_, rows, cols, _ptr(d_codes), _ptr(d_scales), _ptr(d_x), x_ld),
-           "psops_keep8_unpack", k, "psops_keep8_last_error")
+def psops_keep_unpack(k, type_, rows, cols, d_codes, d_scales, d_x, x_ld) -> None:
+    _check(load().psops_keep_unpack(k, type_, rows, cols, _ptr(d_codes), _ptr(d_scales), _ptr(d_x), x_ld),
+           "psops_keep_unpack", k, "psops_keep_last_error")
 
 
-def psops_keep8_activate(k, kind, type_, rows, cols, d_a, a_ld, d_b, b_ld, d_y, y_ld, d_a_codes, d_a_scales, d_b_codes,
+def psops_keep_activate(k, kind, type_, rows, cols, d_a, a_ld, d_b, b_ld, d_y, y_ld, d_a_codes, d_a_scales, d_b_codes,
                          d_b_scales) -> None:
-    _check(load().psops_keep8_activate(k, kind, type_, rows, cols, _ptr(d_a), a_ld, _ptr(d_b), b_ld, _ptr(d_y), y_ld,
+    _check(load().psops_keep_activate(k, kind, type_, rows, cols, _ptr(d_a), a_ld, _ptr(d_b), b_ld, _ptr(d_y), y_ld,
                                        _ptr(d_a_codes), _ptr(d_a_scales), _ptr(d_b_codes), _ptr(d_b_scales)),
-           "psops_keep8_activate", k, "psops_keep8_last_error")
+           "psops_keep_activate", k, "psops_keep_last_error")
 
 
-def psops_keep8_activate_backward(k, kind, type_, rows, cols, d_a_codes, d_a_scales, d_b_codes, d_b_scales, d_dy, dy_ld,
+def psops_keep_activate_backward(k, kind, type_, rows, cols, d_a_codes, d_a_scales, d_b_codes, d_b_scales, d_dy, dy_ld,
                                   d_da, da_ld, d_db, db_ld, d_y, y_ld) -> None:
-    _check(load().psops_keep8_activate_backward(k, kind, type_, rows, cols, _ptr(d_a_codes), _ptr(d_a_scales),
+    _check(load().psops_keep_activate_backward(k, kind, type_, rows, cols, _ptr(d_a_codes), _ptr(d_a_scales),
                                                 _ptr(d_b_codes), _ptr(d_b_scales), _ptr(d_dy), dy_ld, _ptr(d_da), da_ld,
                                                 _ptr(d_db), db_ld, _ptr(d_y), y_ld),
-           "psops_keep8_activate_backward", k, "psops_keep8_last_error")
+           "psops_keep_activate_backward", k, "psops_keep_last_error")
 
 
-def psops_keep8_set_stream(ctx, stream) -> None:
-    _check(load().psops_keep8_set_stream(ctx, int(stream) if stream else None), "psops_keep8_set_stream", ctx,
-           "psops_keep8_last_error")
+def psops_keep_set_stream(ctx, stream) -> None:
+    _check(load().psops_keep_set_stream(ctx, int(stream) if stream else None), "psops_keep_set_stream", ctx,
+           "psops_keep_last_error")
 
 
-def psops_keep8_launch_count(k) -> int:
-    return int(load().psops_keep8_launch_count(k))
+def psops_keep_launch_count(k) -> int:
+    return int(load().psops_keep_launch_count(k))
 
 
-def psops_keep8_destroy(k) -> None:
-    _check(load().psops_keep8_destroy(k), "psops_keep8_destroy")
+def psops_keep_destroy(k) -> None:
+    _check(load().psops_keep_destroy(k), "psops_keep_destroy")
 
 
 # ---- convenience holder of the tensors a context borrows ------------------

@@ -12,11 +12,11 @@ import sys
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 SOURCES = [os.path.join(_HERE, "csrc", name) for name in ("psops.cu", "psops_optim.cu", "psops_xent.cu", "psops_attention.cu",
-                                                        "psops_keep8.cu")]
+                                                        "psops_keep.cu")]
 HEADERS = [os.path.join(_ROOT, "include", "psops.h")] + [
     os.path.join(_HERE, "csrc", name) for name in ("psops_kernels.cuh", "psops_host.cuh", "psops_optim_kernels.cuh",
                                               "psops_xent_kernels.cuh", "psops_xent_small.cuh",
-                                              "psops_umma.cuh", "psops_attention_kernels.cuh", "psops_keep8_kernels.cuh")]
+                                              "psops_umma.cuh", "psops_attention_kernels.cuh", "psops_keep_kernels.cuh")]
 LIBRARY = os.path.join(_HERE, "libpsops.so")
 
 NVCC_FLAGS = [

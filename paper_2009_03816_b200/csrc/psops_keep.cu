@@ -1,4 +1,4 @@
-// psops_keep8.cu -- C entries of activations kept in 8 bits.
+// psops_keep.cu -- C entries of activations kept in 8 bits.
 #include "psops.h"
 
 #include <cuda_runtime.h>
@@ -7,14 +7,14 @@
 #include <new>
 
 #include "psops_host.cuh"
-#include "psops_keep8_kernels.cuh"
+#include "psops_keep_kernels.cuh"
 
-using namespace psops_keep8_k;
+using namespace psops_keep_k;
 using psops_host::ceil_div;
 using psops_host::launch;
 using psops_host::OnDevice;
 
-struct psops_keep8 : psops_host::Base {};
+struct psops_keep : psops_host::Base {};
 
 namespace {
 
@@ -26,10 +26,10 @@ using Kernel = void (*)(const KeepParams);
 template <class T, int JOB, int KIND, bool GATED>
 Kernel by_width(int width)
 {
-    return width == 16  ? psops_keep8_kernel<T, JOB, KIND, GATED, 8, true>
-           : width == 8 ? psops_keep8_kernel<T, JOB, KIND, GATED, 8, false>
-           : width == 4 ? psops_keep8_kernel<T, JOB, KIND, GATED, 4, false>
-           : width == 2 ? psops_keep8_kernel<T, JOB, KIND, GATED, 2, false> : psops_keep8_kernel<T, JOB, KIND, GATED, 1, false>;
+    return width == 16  ? psops_keep_kernel<T, JOB, KIND, GATED, 8, true>
+           : width == 8 ? psops_keep_kernel<T, JOB, KIND, GATED, 8, false>
+           : width == 4 ? psops_keep_kernel<T, JOB, KIND, GATED, 4, false>
+           : width == 2 ? psops_keep_kernel<T, JOB, KIND, GATED, 2, false> : psops_keep_kernel<T, JOB, KIND, GATED, 1, false>;
 }
 template <class T, int JOB>
 Kernel by_kind(int kind, bool gated, int width)
@@ -46,7 +46,7 @@ Kernel kernel_of(int job, int kind, bool gated, int width)
            : job == kForward ? by_kind<T, kForward>(kind, gated, width) : by_kind<T, kBackward>(kind, gated, width);
 }
 
-int run(psops_keep8 *k, int job, int kind, int32_t type, int64_t rows, int64_t cols, bool gated, KeepParams P)
+int run(psops_keep *k, int job, int kind, int32_t type, int64_t rows, int64_t cols, bool gated, KeepParams P)
 {
     P.cols = (int)cols;
     const uint32_t of_row = (uint32_t)ceil_div(cols, kBlock);
@@ -66,12 +66,12 @@ int run(psops_keep8 *k, int job, int kind, int32_t type, int64_t rows, int64_t c
                       : width == 16 ? kTimes<kBackward, true> : kTimes<kBackward, false>;
     const int64_t of_cta = kThreads / (width >= 4 ? kLanes<4> : kLanes<1>) * times;
     const int64_t grid = std::min<int64_t>(ceil_div(rows * of_row, of_cta), (int64_t)k->sms * kCtasOfSm);
-    return launch(k, "psops_keep8_kernel",
+    return launch(k, "psops_keep_kernel",
                   type == PSOPS_F16 ? kernel_of<__half>(job, kind, gated, width) : kernel_of<__nv_bfloat16>(job, kind, gated, width),
                   dim3((unsigned)grid), kThreads, 0, 1, P);
 }
 
-int check(const psops_keep8 *k, int32_t type, int64_t rows, int64_t cols)
+int check(const psops_keep *k, int32_t type, int64_t rows, int64_t cols)
 {
     if (k == nullptr || (type != PSOPS_F16 && type != PSOPS_BF16) || rows < 0 || cols < 1 || cols > INT32_MAX - kBlock ||
         rows > kMostBlocksOfRows / ceil_div(cols, kBlock))
@@ -100,11 +100,11 @@ int check_kept(const void *codes, const void *scales, int64_t rows)
 
 extern "C" {
 
-int psops_keep8_create(psops_keep8 **out, void *cuda_stream)
+int psops_keep_create(psops_keep **out, void *cuda_stream)
 {
     if (out == nullptr) return PSOPS_EINVAL;
     *out = nullptr;
-    psops_keep8 *k = new (std::nothrow) psops_keep8();
+    psops_keep *k = new (std::nothrow) psops_keep();
     if (k == nullptr) return PSOPS_ENOMEM;
     k->stream = (cudaStream_t)cuda_stream;
     int rc = psops_host::not_capturing(k);
@@ -119,7 +119,7 @@ int psops_keep8_create(psops_keep8 **out, void *cuda_stream)
     return PSOPS_OK;
 }
 
-int psops_keep8_pack(psops_keep8 *k, int32_t type, int64_t rows, int64_t cols, const void *d_x, int64_t x_ld, void *d_codes, float *d_scales)
+int psops_keep_pack(psops_keep *k, int32_t type, int64_t rows, int64_t cols, const void *d_x, int64_t x_ld, void *d_codes, float *d_scales)
 {
     PSOPS_DO(check(k, type, rows, cols));
     PSOPS_DO(check_rows(d_x, x_ld, rows, cols));
@@ -132,7 +132,7 @@ int psops_keep8_pack(psops_keep8 *k, int32_t type, int64_t rows, int64_t cols, c
     return run(k, kPack, 0, type, rows, cols, false, P);
 }
 
-int psops_keep8_unpack(psops_keep8 *k, int32_t type, int64_t rows, int64_t cols, const void *d_codes, const float *d_scales, void *d_x, int64_t x_ld)
+int psops_keep_unpack(psops_keep *k, int32_t type, int64_t rows, int64_t cols, const void *d_codes, const float *d_scales, void *d_x, int64_t x_ld)
 {
     PSOPS_DO(check(k, type, rows, cols));
     PSOPS_DO(check_rows(d_x, x_ld, rows, cols));
@@ -145,7 +145,7 @@ int psops_keep8_unpack(psops_keep8 *k, int32_t type, int64_t rows, int64_t cols,
     return run(k, kUnpack, 0, type, rows, cols, false, P);
 }
 
-int psops_keep8_activate(psops_keep8 *k, int32_t kind, int32_t type, int64_t rows, int64_t cols, const void *d_a, int64_t a_ld, const void *d_b,
+int psops_keep_activate(psops_keep *k, int32_t kind, int32_t type, int64_t rows, int64_t cols, const void *d_a, int64_t a_ld, const void *d_b,
                          int64_t b_ld, void *d_y, int64_t y_ld, void *d_a_codes, float *d_a_scales, void *d_b_codes, float *d_b_scales)
 {
     PSOPS_DO(check(k, type, rows, cols));
@@ -168,7 +168,7 @@ int psops_keep8_activate(psops_keep8 *k, int32_t kind, int32_t type, int64_t row
     return run(k, kForward, kind, type, rows, cols, d_b != nullptr, P);
 }
 
-int psops_keep8_activate_backward(psops_keep8 *k, int32_t kind, int32_t type, int64_t rows, int64_t cols, const void *d_a_codes, const float *d_a_scales,
+int psops_keep_activate_backward(psops_keep *k, int32_t kind, int32_t type, int64_t rows, int64_t cols, const void *d_a_codes, const float *d_a_scales,
                                   const void *d_b_codes, const float *d_b_scales, const void *d_dy, int64_t dy_ld, void *d_da, int64_t da_ld,
                                   void *d_db, int64_t db_ld, void *d_y, int64_t y_ld)
 {
@@ -192,11 +192,11 @@ int psops_keep8_activate_backward(psops_keep8 *k, int32_t kind, int32_t type, in
     return run(k, kBackward, kind, type, rows, cols, d_b_codes != nullptr, P);
 }
 
-int psops_keep8_set_stream(psops_keep8 *k, void *cuda_stream) { return psops_host::set_stream(k, cuda_stream); }
-int64_t psops_keep8_launch_count(const psops_keep8 *k) { return k ? k->launches : 0; }
-const char *psops_keep8_last_error(const psops_keep8 *k) { return k ? k->err : ""; }
+int psops_keep_set_stream(psops_keep *k, void *cuda_stream) { return psops_host::set_stream(k, cuda_stream); }
+int64_t psops_keep_launch_count(const psops_keep *k) { return k ? k->launches : 0; }
+const char *psops_keep_last_error(const psops_keep *k) { return k ? k->err : ""; }
 
-int psops_keep8_destroy(psops_keep8 *k)
+int psops_keep_destroy(psops_keep *k)
 {
     if (k == nullptr) return PSOPS_EINVAL;
     OnDevice guard(k);

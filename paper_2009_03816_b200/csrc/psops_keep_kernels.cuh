@@ -1,4 +1,4 @@
-// psops_keep8_kernels.cuh -- activations kept in 8 bits for the backward pass.
+// psops_keep_kernels.cuh -- activations kept in 8 bits for the backward pass.
 //
 // A row's blocks of 128 elements share a scale: s = top / 127 with top the largest
 // magnitude, code = x / s rounded to the nearest, ties away from zero.
@@ -15,7 +15,7 @@
 
 #include "psops_umma.cuh"
 
-namespace psops_keep8_k {
+namespace psops_keep_k {
 
 constexpr int kBlock = 128;
 constexpr int kThreads = 256;
@@ -251,7 +251,7 @@ template <int JOB, bool WHOLE> constexpr int kTimes = JOB == kPack || JOB == kUn
 // `GATED` doubles the inputs.  A warp has a few blocks, U times over.  U: what kept
 // most bytes under way without costing warps their registers.
 template <class T, int JOB, int KIND, bool GATED, int W, bool WHOLE>
-__global__ void __launch_bounds__(kThreads) psops_keep8_kernel(const KeepParams P)
+__global__ void __launch_bounds__(kThreads) psops_keep_kernel(const KeepParams P)
 {
     constexpr int N = GATED ? 2 : 1;
     constexpr int U = kTimes<JOB, WHOLE>;
@@ -355,4 +355,4 @@ __global__ void __launch_bounds__(kThreads) psops_keep8_kernel(const KeepParams 
     }
 }
 
-} // namespace psops_keep8_k
+} // namespace psops_keep_k

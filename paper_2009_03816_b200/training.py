@@ -601,9 +601,9 @@ class Keep8(_Holder):
                       inputs kept in 8 bits: keep(a, b, "silu")
     """
 
-    _set_stream = staticmethod(binding.psops_keep8_set_stream)
-    _launch_count = staticmethod(binding.psops_keep8_launch_count)
-    _destroy = staticmethod(binding.psops_keep8_destroy)
+    _set_stream = staticmethod(binding.psops_keep_set_stream)
+    _launch_count = staticmethod(binding.psops_keep_launch_count)
+    _destroy = staticmethod(binding.psops_keep_destroy)
 
     def __init__(self, *, device="cuda", stream=None):
         device = torch.device(device)
@@ -613,7 +613,7 @@ class Keep8(_Holder):
         self._on(self.device, stream)
         with torch.cuda.device(self.device):
             self._follow()
-            self.ctx = binding.psops_keep8_create(self.stream)
+            self.ctx = binding.psops_keep_create(self.stream)
 
     def _rows(self, where, name, t, like=None):
         """(rows, elements of a row, stride) of a tensor with consecutive elements in each row, its leading dimensions
@@ -667,7 +667,7 @@ class Keep8(_Holder):
         rows, cols, ld = self._rows("Keep8.pack", "x", x)
         codes, scales = self._room(x)
         self._follow(x, codes, scales)
-        binding.psops_keep8_pack(self.ctx, _TYPES[x.dtype], rows, cols, x, ld, codes, scales)
+        binding.psops_keep_pack(self.ctx, _TYPES[x.dtype], rows, cols, x, ld, codes, scales)
         return codes, scales
 
     def unpack(self, codes, scales, shape, dtype, *, out=None):
@@ -687,7 +687,7 @@ class Keep8(_Holder):
             out, cols = scales.new_empty(shape, dtype=dtype), shape[-1]
             rows, ld = shape.numel() // cols, cols
         self._follow(codes, scales, out)
-        binding.psops_keep8_unpack(self.ctx, _TYPES[dtype], rows, cols, codes, scales, out, ld)
+        binding.psops_keep_unpack(self.ctx, _TYPES[dtype], rows, cols, codes, scales, out, ld)
         if given:
             _changed([out])
         return out
@@ -712,7 +712,7 @@ class Keep8(_Holder):
             out, y_ld = self._like(a), cols
         kept = self._room(a) + (self._room(a) if b is not None else ())
         self._follow(a, b, out, *kept)
-        binding.psops_keep8_activate(self.ctx, code, _TYPES[a.dtype], rows, cols, a, a_ld, b, b_ld, out, y_ld,
+        binding.psops_keep_activate(self.ctx, code, _TYPES[a.dtype], rows, cols, a, a_ld, b, b_ld, out, y_ld,
                                      *kept, *((None, None) if b is None else ()))
         if given:
             _changed([out])
@@ -743,7 +743,7 @@ class Keep8(_Holder):
             results.append(t)
             strides.append(ld_of)
         self._follow(grad, *kept, *results)
-        binding.psops_keep8_activate_backward(self.ctx, code, _TYPES[grad.dtype], rows, cols, *kept,
+        binding.psops_keep_activate_backward(self.ctx, code, _TYPES[grad.dtype], rows, cols, *kept,
                                               *(() if gated else (None, None)), grad, ld, results[0], strides[0],
                                               results[1], strides[1], results[2], strides[2])
         if given:

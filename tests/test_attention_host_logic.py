@@ -60,14 +60,14 @@ def test_attention_refuses_before_touching_cuda(lib):
 
 
 def test_keep8_refuses_before_touching_cuda(lib):
-    assert lib.psops_keep8_create(None, None) == binding.PSOPS_EINVAL
-    assert lib.psops_keep8_pack(None, BF16, 1, 1, None, 1, None, None) == binding.PSOPS_EINVAL
-    assert lib.psops_keep8_unpack(None, BF16, 1, 1, None, None, None, 1) == binding.PSOPS_EINVAL
-    assert lib.psops_keep8_activate(None, 0, BF16, 1, 1, None, 1, None, 0, None, 1, None, None, None, None) == binding.PSOPS_EINVAL
-    assert lib.psops_keep8_activate_backward(None, 0, BF16, 1, 1, None, None, None, None, None, 1, None, 0, None, 0, None,
+    assert lib.psops_keep_create(None, None) == binding.PSOPS_EINVAL
+    assert lib.psops_keep_pack(None, BF16, 1, 1, None, 1, None, None) == binding.PSOPS_EINVAL
+    assert lib.psops_keep_unpack(None, BF16, 1, 1, None, None, None, 1) == binding.PSOPS_EINVAL
+    assert lib.psops_keep_activate(None, 0, BF16, 1, 1, None, 1, None, 0, None, 1, None, None, None, None) == binding.PSOPS_EINVAL
+    assert lib.psops_keep_activate_backward(None, 0, BF16, 1, 1, None, None, None, None, None, 1, None, 0, None, 0, None,
                                              0) == binding.PSOPS_EINVAL
-    assert lib.psops_keep8_set_stream(None, None) == binding.PSOPS_EINVAL
-    assert lib.psops_keep8_destroy(None) == binding.PSOPS_EINVAL
+    assert lib.psops_keep_set_stream(None, None) == binding.PSOPS_EINVAL
+    assert lib.psops_keep_destroy(None) == binding.PSOPS_EINVAL
 
 
 @pytest.mark.parametrize("count,far", [(1, 1), (2, 2), (3, 9), (8, 32), (16, 64), (32, 128), (32, 512), (48, 1000), (64, 64), (64, 1024)])
@@ -167,7 +167,7 @@ def test_attention_holder_refuses(attention):
 def keep(monkeypatch):
     calls = []
     for name in ("pack", "unpack", "activate", "activate_backward"):
-        monkeypatch.setattr(binding, "psops_keep8_" + name, lambda *a, name=name: calls.append((name, a)))
+        monkeypatch.setattr(binding, "psops_keep_" + name, lambda *a, name=name: calls.append((name, a)))
     monkeypatch.setattr(training.Keep8, "_destroy", staticmethod(lambda ctx: None))
     monkeypatch.setattr(training.Keep8, "_follow", lambda op, *tensors: calls.append(("follow", tensors)))
     op = training.Keep8.__new__(training.Keep8)

@@ -165,20 +165,20 @@ def test_refusals_of_the_entries(keep):
     p, c, s, o = x.data_ptr(), codes.data_ptr(), scales.data_ptr(), y.data_ptr()
     kind = binding.PSOPS_BF16
     OK, EINVAL, EALIGN = binding.PSOPS_OK, binding.PSOPS_EINVAL, binding.PSOPS_EALIGN
-    assert lib.psops_keep8_pack(ctx, kind, 8, 64, p, 64, c, s) == OK
+    assert lib.psops_keep_pack(ctx, kind, 8, 64, p, 64, c, s) == OK
     for code, a in ((EINVAL, (binding.PSOPS_F32, 8, 64, p, 64, c, s)), (EINVAL, (kind, -1, 64, p, 64, c, s)), (EINVAL, (kind, 8, 0, p, 64, c, s)),
                     (EINVAL, (kind, 8, 64, None, 64, c, s)), (EINVAL, (kind, 8, 64, p, 63, c, s)), (EINVAL, (kind, 8, 64, p, 64, None, s)),
                     (EINVAL, (kind, 8, 64, p, 64, c, None)), (EINVAL, (kind, 1 << 31, 64, p, 64, c, s)), (EINVAL, (kind, 1, 1 << 31, p, 1 << 31, c, s)),
                     (EALIGN, (kind, 8, 64, p + 1, 64, c, s)), (EALIGN, (kind, 8, 64, p, 64, c + 8, s)), (EALIGN, (kind, 8, 64, p, 64, c, s + 2))):
-        assert lib.psops_keep8_pack(ctx, *a) == code, a
-    assert lib.psops_keep8_unpack(ctx, kind, 8, 64, c, s, o, 64) == OK
-    assert lib.psops_keep8_unpack(ctx, kind, 8, 64, c, s, None, 64) == EINVAL
-    assert lib.psops_keep8_unpack(ctx, kind, 8, 64, c, s, o + 1, 64) == EALIGN
-    act = lambda k=1, a=p, b=None, bc=None, bs=None, out=o: lib.psops_keep8_activate(ctx, k, kind, 8, 64, a, 64, b, 64, out, 64, c, s, bc, bs)
+        assert lib.psops_keep_pack(ctx, *a) == code, a
+    assert lib.psops_keep_unpack(ctx, kind, 8, 64, c, s, o, 64) == OK
+    assert lib.psops_keep_unpack(ctx, kind, 8, 64, c, s, None, 64) == EINVAL
+    assert lib.psops_keep_unpack(ctx, kind, 8, 64, c, s, o + 1, 64) == EALIGN
+    act = lambda k=1, a=p, b=None, bc=None, bs=None, out=o: lib.psops_keep_activate(ctx, k, kind, 8, 64, a, 64, b, 64, out, 64, c, s, bc, bs)
     assert act() == OK
     for kw in (dict(k=3), dict(k=-1), dict(a=None), dict(b=p), dict(out=None)):
         assert act(**kw) == EINVAL, kw
-    back = lambda k=1, bc=None, bs=None, dy=p, da=o, db=None, yy=None: lib.psops_keep8_activate_backward(ctx, k, kind, 8, 64, c, s, bc, bs, dy, 64, da, 64, db, 64, yy, 64)
+    back = lambda k=1, bc=None, bs=None, dy=p, da=o, db=None, yy=None: lib.psops_keep_activate_backward(ctx, k, kind, 8, 64, c, s, bc, bs, dy, 64, da, 64, db, 64, yy, 64)
     assert back() == OK and back(da=None) == OK
     for code, kw in ((EINVAL, dict(k=5)), (EINVAL, dict(dy=None)), (EINVAL, dict(db=o)), (EINVAL, dict(bc=c)), (EALIGN, dict(yy=o + 1)),
                      (EALIGN, dict(bc=c + 4, bs=s))):
