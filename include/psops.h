@@ -609,14 +609,16 @@ int psops_xent_destroy(psops_xent *x);
  * behind the last) are left as they were in all results, or become zeros if
  * zero_rest is not 0.
  *
- * Rounding: products are summed in fp32 by the tensor cores, softmax statistics
- * are fp32.  The tensor cores multiply 16-bit numbers: p and ds enter their
- * second products rounded to the type of q.  In fp16, p is kept scaled by a
- * power of two, and ds by one that the largest norms of the rows of do and v
+ * Rounding: products are summed in fp32 by the tensor cores, which cut sums off
+ * where fp32 would round; they add up at most 16,384 terms in one go, fp32
+ * additions do the rest (1.2e-4 of the largest partial sum at most, however long).
+ * Softmax statistics are fp32.  The tensor cores multiply 16-bit numbers: p and ds
+ * enter their second products rounded to the type of q.  In fp16, p is kept scaled
+ * by a power of two, and ds by one that the largest norms of the rows of do and v
  * allow, so that small ones keep their digits; results are rounded once, at the
- * end.  delta = do . out is taken from out as it was rounded.
+ * end.  do_i . out_i is corrected for the rounding of out.
  * Should a product ever wait in vain for its operands (four seconds), the
- * results of its tile are NaN.
+ * results of its tile, and of those that its CTA does after it, are NaN.
  */
 #define PSOPS_ATTENTION_GRADS  1u   /* reserve workspace for psops_attention_backward           */
 

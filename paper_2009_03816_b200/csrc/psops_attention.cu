@@ -394,8 +394,6 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         P.bias = bias_of(a, d_bias, bias_type);
         P.by_heads = divisor(H);
         P.by_kv_heads = divisor(G);
-        P.want_keys = dk != nullptr || dv != nullptr;
-        P.want_queries = dq != nullptr || d_dbias != nullptr;
         if (dq != nullptr) P.dq = heads_of(a, dq, tokens, H);
         if (dk != nullptr) P.dk = heads_of(a, dk, tokens, G);
         if (dv != nullptr) P.dv = heads_of(a, dv, tokens, G);
@@ -404,9 +402,12 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         if (join_within) P.join = J;
         size_t shared;
         BackwardKernel kernel = backward_kernel(a, &shared);
-        const int works = (P.want_keys ? G : 0) + (P.want_queries ? H : 0);
-        if (works > 0)
-            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, works, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
+        // dk needs the delta that the queries' use leaves
+        if (dq != nullptr || d_dbias != nullptr || dk != nullptr)
+            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, H, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
+        P.keys = 1;
+        if (dk != nullptr || dv != nullptr)
+            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, G, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
     }
     if (d_dbias == nullptr || join_within) return PSOPS_OK;
     return launch(a, "psops_attention_join_kernel",

@@ -501,9 +501,9 @@ struct Work {
     int head;
     bool some;
 };
-__device__ __forceinline__ Work work_at(const Item *items, int total, const Divisor &heads, uint32_t cta, int k)
+__device__ __forceinline__ Work work_at(const Item *items, int total, const Divisor &heads, int k)
 {
-    const uint32_t many = gridDim.x, i = k * many + (k & 1 ? many - 1 - cta : cta);
+    const uint32_t many = gridDim.x, i = k * many + (k & 1 ? many - 1 - blockIdx.x : blockIdx.x);
     Work w{};
     w.some = i < (uint32_t)total;
     if (w.some) {
@@ -700,7 +700,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         if (P.prep.fill > 0) fill_rest<kForwardThreads>(P.prep, blockIdx.x, gridDim.x);
     } else {
         total = *P.count * P.heads;
-        coming = work_at(P.items, total, P.by_heads, blockIdx.x, 0);
+        coming = work_at(P.items, total, P.by_heads, 0);
     }
 
     if (warp == 8) {
@@ -709,7 +709,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         int t = 0, n = 0;                        // tiles and works before this one
         for (int turn = 1; coming.some && ok; ++turn) {
             const Work w = coming;
-            coming = work_at(P.items, total, P.by_heads, blockIdx.x, turn);
+            coming = work_at(P.items, total, P.by_heads, turn);
             if (w.item.length <= 0) continue;
             const int first = w.item.first + w.item.level * kTile, kv = kv_of(w.head), q_stage = n % kStages;
             ok = wait_all(&bar_q_empty[q_stage], (n / kStages & 1) ^ 1, failed);
@@ -773,7 +773,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         auto next_work = [&]() {                 // the next one with tokens
             Work w = coming;
             while (w.some) {
-                coming = work_at(P.items, total, P.by_heads, blockIdx.x, turn++);
+                coming = work_at(P.items, total, P.by_heads, turn++);
                 if (w.item.length > 0) break;
                 w = coming;
             }
@@ -830,7 +830,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         int t = 0, n = 0, head_before = -1;
         for (int turn = 1; coming.some; ++turn) {
             const Work w = coming;
-            coming = work_at(P.items, total, P.by_heads, blockIdx.x, turn);
+            coming = work_at(P.items, total, P.by_heads, turn);
             if (w.item.length <= 0) continue;
             const int tile = w.item.level, first = w.item.first + tile * kTile;
             if constexpr (BIAS) {
@@ -1020,11 +1020,12 @@ struct BackwardParams {
     const int *count;
     int tokens, heads, group, dim;
     Divisor by_heads, by_kv_heads, by_group;
-    int want_keys, want_queries;
+    int keys;
     float scale, scale2;
     Heads q, k, grad;                        // read where numbers are not finite
     Heads dq, dk, dv;                        // an address is NULL where the result is not wanted
-    const float *lse, *delta;
+    const float *lse;
+    float *delta;                            // !KEYS makes it exact, for KEYS after it
     const float2 *norms;                     // NULL, or `blocks` of them
     int blocks;
     Bias bias;
@@ -1047,18 +1048,19 @@ struct Barriers {
 };
 template <bool BIAS>
 struct BackwardShared {
-    Barriers bars[2];                        // of the first use and of the second
+    Barriers bars;
     int dirty[2][2];                         // by parity of the work, and which of B
     alignas(16) float by_column[2][2][kTile];        // lse and delta of the queries
+    float of_half[2][kTile];
     typename Choose<BIAS>::Type tables;
 };
 
-// One kernel, two uses, one after the other.  A CTA keeps two tiles of 128 rows
+// One kernel, two uses, one launch each.  A CTA keeps two tiles of 128 rows
 // (A0, A1) and meets pairs of tiles of 128 rows (B0, B1) one after the other:
 //              A0  A1  B0  B1     S = A0 B0^T   T = A1 B1^T   sums
+//   !KEYS      q   do  k   v      scores        dp            dq += ds B0, mean key += p B0
 //   KEYS       k   v   q   do     scores^T      dp^T          dk += ds^T B0, dv += p^T B1
-//   !KEYS      q   do  k   v      scores        dp            dq += ds B0
-// The scores are computed in both: seven products instead of the five that a
+// The scores are computed in both: eight products instead of the five that a
 // single pass needs, and in exchange no sum passes between CTAs, so that all
 // gradients are the same in every run and dq needs no fp32 sums in memory.
 // KEYS goes through all query heads that share its keys.  p and ds go back into
@@ -1066,6 +1068,13 @@ struct BackwardShared {
 // threads have one row and 64 columns each.  While they form p, the products of
 // ds of the tile before and of dp run; while they form ds, those of p and of the
 // next scores.
+// delta = do . out comes with out's rounding and its probabilities', which would be
+// common to a row's ds (dq was off by 2.1 times what its own rounding leaves, dk by
+// 1.8).  But a row's ds have the sum zero: what they sum up to is what delta is off
+// by, and what their own rounding has in common.  !KEYS takes it out, in dq by the
+// mean key (one more product, p k; dq and dk are off by 1.3 to 1.5 times their
+// rounding then, for a tenth of the time), and leaves the corrected delta to KEYS.
+// Where a row has but one tile, delta is made from p and dp first.
 template <class T, int HALVES, bool KEYS, bool BIAS>
 __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const CUtensorMap &map_a1, const CUtensorMap &map_b0, const CUtensorMap &map_b1,
                                               const BackwardParams &P, BackwardShared<BIAS> &M, uint8_t *tiles, uint32_t tensor_base, float unit,
@@ -1075,11 +1084,11 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
     constexpr int kTileBytes = HALVES * kHalfBytes;
     constexpr int kOwn = 4;
     // scores in two places by turns, where tensor memory has room for them: the next ones need not wait for these
-    constexpr bool kTwice = !KEYS || HALVES == 1;
+    constexpr bool kTwice = KEYS && HALVES == 1;
     constexpr uint32_t kSecond = 3 * kTile;                                 // columns 384 to 511
     // fp16: probabilities are kept 2^14 times as large (dv is scaled back), ds by a power of two from the norms
     constexpr float kShift = kBf16 ? 0.0f : 14.0f;
-    Barriers &bars = M.bars[KEYS ? 0 : 1];
+    Barriers &bars = M.bars;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t a_at = umma::shared_address(tiles), b_at = a_at + 2 * kTileBytes;
     float *stripes = (float *)(tiles + 6 * kTileBytes), *bucket_sums = stripes + 8 * kStripeFloats<HALVES>;
@@ -1100,11 +1109,9 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
     umma::fence_after();
     const uint32_t s_at = tensor_base, t_at = s_at + kTile, sum0_at = t_at + kTile, sum1_at = sum0_at + HALVES * 64;
 
-    // those that got less of the first part come first in the second
     const Divisor &heads = KEYS ? P.by_kv_heads : P.by_heads;               // of A0
-    const uint32_t cta = KEYS ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
     const int total = *P.count * (int)heads.by;
-    auto work_of = [&](int turn) { return work_at(P.items, total, heads, cta, turn); };
+    auto work_of = [&](int turn) { return work_at(P.items, total, heads, turn); };
     Work coming = work_of(0);
     auto kv_of = [&](int head) { return (int)divide(head, P.by_group); };
     // A tile meets level + 1 tiles of B (of each head): !KEYS from the diagonal down, KEYS from the diagonal up.
@@ -1204,12 +1211,10 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                 };
                 // the place of the next scores has been read: bar_ds of the round before says so
                 if (kTwice && !(ok = next_scores())) break;
-                if (KEYS) {
-                    ok = wait_all(&bars.p, r & 1, failed);
-                    if (!ok) break;
-                    umma::fence_after();
-                    add(r, j, 1, s_at + (kTwice && (r & 1) ? kSecond : 0), sum1_at);
-                }
+                ok = wait_all(&bars.p, r & 1, failed);
+                if (!ok) break;
+                umma::fence_after();
+                add(r, j, KEYS ? 1 : 0, s_at + (kTwice && (r & 1) ? kSecond : 0), sum1_at);
                 if (!kTwice) {
                     // ... or follows in the order of the products
                     if (!(ok = next_scores())) break;
@@ -1240,6 +1245,13 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
         float far = 0.0f;
         const float *table = nullptr;
         if constexpr (BIAS) table = M.tables.distance + kBefore;
+        // what the two threads of a row have, together
+        auto both_halves = [&](float x) {
+            barrier_named(2 + (warp & 3), 64);                              // what they had before has been read
+            M.of_half[half][row] = x;
+            barrier_named(2 + (warp & 3), 64);
+            return M.of_half[0][row] + M.of_half[1][row];
+        };
         // where it is not, all works are gone through all the same, without waits, for the barriers in them
         bool ok = true;
         int r = 0, n = 0, chains = 0, head_before = -1;                     // rounds, works and chains of sums before
@@ -1251,7 +1263,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
             const int head = w.head, tile = tile_of(w), first = item.first + tile * kTile, meets = item.level + 1;
             const int rounds = KEYS ? meets * P.group : meets;
             const int left = item.length - tile * kTile;                        // rows of A that exist
-            float row_base = 0.0f, row_delta = 0.0f, far_sum = 0.0f, next_value = 0.0f;
+            float row_base = 0.0f, row_delta = 0.0f, row_sum = 0.0f, far_sum = 0.0f, next_value = 0.0f;
             if (!KEYS && row < left) {
                 const long long at = (long long)head * P.tokens + first + row;
                 row_base = kShift - base2(P.lse[at]);
@@ -1282,7 +1294,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                     // before p and ds of this round let the next chain begin
                     ok = ok && wait_all(&bars.sums, chains++ & 1, failed);
                     umma::fence_after();
-                    for (int which = 0; which < (KEYS ? 2 : 1); ++which)
+                    for (int which = 0; which < 2; ++which)
                         add_to_room(room_of(P.fold, blockIdx.x * 2 + which, row), (which ? sum1_at : sum0_at) + lanes - col0, half * 32 * HALVES,
                                     min((half + 1) * 32 * HALVES, P.dim), 1.0f, j > kChain);
                     umma::fence_before();
@@ -1384,21 +1396,33 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                         for (int i = c; i < c + 32; ++i)
                             if (!(keep[c / 32] >> (i - c) & 1)) p[i] = 0.0f;
                     }
-                    if (KEYS) {
-                        uint32_t w[16];
+                    uint32_t w[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[c + 2 * i], p[c + 2 * i + 1]);
-                        umma::tensor_memory_store16(here + c / 2, w);
-                    }
+                    for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[c + 2 * i], p[c + 2 * i + 1]);
+                    umma::tensor_memory_store16(here + c / 2, w);
                 }
-                if (KEYS) {
-                    umma::tensor_memory_stored();
-                    umma::fence_before();
-                    __syncwarp();
-                    if (lane == 0) umma::barrier_arrive(umma::shared_address(&bars.p));
-                }
+                umma::tensor_memory_stored();
+                umma::fence_before();
+                __syncwarp();
+                // (a warp arrives but once in a round: KEYS has a barrier in each, else the next scores wait for all to arrive)
+                if (lane == 0) umma::barrier_arrive(umma::shared_address(&bars.p));
                 ok = ok && wait_all(&bars.t, r & 1, failed);
                 umma::fence_after();
+                uint64_t rounded[4] = {0, 0, 0, 0};                             // sums of ds as it enters the products
+                if (!KEYS && rounds == 1) {
+                    // all of the row is here: delta from p and dp themselves
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int c = 0; c < 64; c += 32) {
+                        uint32_t u[32];
+                        umma::tensor_memory_load(t_at + lanes + c, u);
+                        umma::tensor_memory_loaded<32>(u);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (keep[c / 32] >> i & 1) sum = __fmaf_rn(p[c + i], __uint_as_float(u[i]), sum);
+                    }
+                    row_delta = -both_halves(sum) * (kBf16 ? 1.0f : unit_p * 0x1p-14f);
+                }
 #pragma unroll
                 for (int c = 0; c < 64; c += 32) {
                     uint32_t u[32];
@@ -1432,11 +1456,22 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
 #pragma unroll
                     for (int i = 0; i < 16; ++i) w[i] = pack2<T>(p[c + 2 * i], p[c + 2 * i + 1]);
                     umma::tensor_memory_store16(t_at + lanes + c / 2, w);
+                    if (!KEYS) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const float2 x = unpack2<T>(w[i]);
+                            rounded[i & 3] = add_both(rounded[i & 3], pair_of(__float_as_uint(x.x), __float_as_uint(x.y)));
+                        }
+                    }
                 }
                 umma::tensor_memory_stored();
                 umma::fence_before();
                 __syncwarp();
                 if (lane == 0) umma::barrier_arrive(umma::shared_address(&bars.ds));
+                if (!KEYS) {
+                    const uint64_t all = add_both(add_both(rounded[0], rounded[1]), add_both(rounded[2], rounded[3]));
+                    row_sum += low_of(all) + high_of(all);
+                }
                 if (BIAS && !KEYS && P.partials != nullptr) {
                     if (!near) {
                         uint64_t part[4] = {0, 0, 0, 0};
@@ -1520,6 +1555,13 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                     ++q_head;
                 }
             }
+            if (!KEYS) {
+                row_sum = both_halves(row_sum);
+                if (half == 0 && row < left) {
+                    const long long at = (long long)head * P.tokens + first + row;
+                    P.delta[at] = rounds > 1 ? P.delta[at] + row_sum / unit : -row_delta / unit_p;
+                }
+            }
             ok = ok && wait_all(&bars.sums, chains++ & 1, failed);
             umma::fence_after();
             if (threadIdx.x < 2) M.dirty[(n & 1) ^ 1][threadIdx.x] = 0;           // read by all in the work before
@@ -1541,6 +1583,19 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 if (c + i < end) x[i] = __fmaf_rn(folded[(c + i) * kTile], times, x[i]);
+                        }
+                        if (!KEYS) {
+                            // what the sum of the row's ds is off zero by, times the mean key
+                            const float off = -row_sum * times * (kBf16 ? 1.0f : 0x1p-14f);
+                            const float *folded = room_of(P.fold, blockIdx.x * 2 + 1, row);
+                            uint32_t u[32];
+                            umma::tensor_memory_load(sum1_at + lanes - col0 + c, u);
+                            umma::tensor_memory_loaded<32>(u);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                const float mean = __uint_as_float(u[i]) + (rounds > kChain && c + i < end ? folded[(c + i) * kTile] : 0.0f);
+                                x[i] = __fmaf_rn(mean, off, x[i]);
+                            }
                         }
                         if (!poisoned || row >= left) return;
                         // !KEYS: the keys of this tile up to the query; KEYS: queries (do) of this tile from the key on, all heads
@@ -1620,20 +1675,14 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_q, const
         }
     }
     const uint32_t tensor_base = tensor_base_slot;
-    if (P.want_keys) backward_part<T, HALVES, true, BIAS>(map_k, map_v, map_q, map_grad, P, shared, tiles, tensor_base, unit, &failed_slot);
-    if (P.want_queries) {
-        __syncwarp();
-        umma::fence_before();
-        __syncthreads();                                                    // tiles and sums of the first part are done with
-        umma::fence_after();
-        backward_part<T, HALVES, false, BIAS>(map_q, map_grad, map_k, map_v, P, shared, tiles, tensor_base, unit, &failed_slot);
-    }
+    if (P.keys) backward_part<T, HALVES, true, BIAS>(map_k, map_v, map_q, map_grad, P, shared, tiles, tensor_base, unit, &failed_slot);
+    else backward_part<T, HALVES, false, BIAS>(map_q, map_grad, map_k, map_v, P, shared, tiles, tensor_base, unit, &failed_slot);
     __syncwarp();
     umma::fence_before();
     __syncthreads();
     umma::fence_after();
     if (warp == 9) umma::tensor_columns_give<512>(tensor_base);
-    if (P.join.ticket == nullptr) return;
+    if (P.keys || P.join.ticket == nullptr) return;
     // few sums: the CTA that is done last joins them
     __shared__ int last;
     if (threadIdx.x == 0) {

@@ -451,4 +451,4 @@ def test_given_results_count_as_changes():
 def test_launches_are_counted():
     op, x, offsets = make([100], 1, 1, 16, BF16)
     both(op, x, offsets)
-    assert op.launches == 1 + 2                            # a short batch: no list forward; two kernels backward
+    assert op.launches == 1 + 3                            # a short batch: no list forward; list, queries and keys backward
