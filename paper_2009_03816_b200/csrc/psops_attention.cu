@@ -402,11 +402,11 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         if (join_within) P.join = J;
         size_t shared;
         BackwardKernel kernel = backward_kernel(a, &shared);
-        // dk needs the delta that the queries' use leaves
+        // dk and dbias need the delta that the queries' use leaves
         if (dq != nullptr || d_dbias != nullptr || dk != nullptr)
             PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, H, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
         P.keys = 1;
-        if (dk != nullptr || dv != nullptr)
+        if (dk != nullptr || dv != nullptr || d_dbias != nullptr)
             PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, G, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
     }
     if (d_dbias == nullptr || join_within) return PSOPS_OK;

@@ -1059,7 +1059,7 @@ struct BackwardShared {
 // (A0, A1) and meets pairs of tiles of 128 rows (B0, B1) one after the other:
 //              A0  A1  B0  B1     S = A0 B0^T   T = A1 B1^T   sums
 //   !KEYS      q   do  k   v      scores        dp            dq += ds B0, mean key += p B0
-//   KEYS       k   v   q   do     scores^T      dp^T          dk += ds^T B0, dv += p^T B1
+//   KEYS       k   v   q   do     scores^T      dp^T          dk += ds^T B0, dv += p^T B1, dbias
 // The scores are computed in both: eight products instead of the five that a
 // single pass needs, and in exchange no sum passes between CTAs, so that all
 // gradients are the same in every run and dq needs no fp32 sums in memory.
@@ -1102,7 +1102,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
         M.dirty[0][0] = M.dirty[0][1] = M.dirty[1][0] = M.dirty[1][1] = 0;
         umma::barrier_init_done();
     }
-    if (BIAS && !KEYS)
+    if (BIAS && KEYS)
         for (int i = threadIdx.x; i < 8 * kMostBuckets; i += kBackwardThreads) bucket_sums[i] = 0.0f;
     umma::fence_before();
     __syncthreads();
@@ -1472,7 +1472,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                     const uint64_t all = add_both(add_both(rounded[0], rounded[1]), add_both(rounded[2], rounded[3]));
                     row_sum += low_of(all) + high_of(all);
                 }
-                if (BIAS && !KEYS && P.partials != nullptr) {
+                if (BIAS && KEYS && P.partials != nullptr) {
                     if (!near) {
                         uint64_t part[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -1481,16 +1481,16 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                         far_sum += low_of(all) + high_of(all);
                     } else if constexpr (BIAS) {
                         // the warp's 32 rows x 64 columns have 95 diagonals, one distance each; diagonal 0's, and the buckets of all
-                        const int zero = apart * kTile + (warp & 3) * 32 - col0 - 63;
+                        const int zero = apart * kTile + col0 - (warp & 3) * 32 - 31;
                         const int low = M.tables.bucket[max(zero, 0)], high = zero + 94 < 0 ? low - 1 : M.tables.bucket[max(zero + 94, 0)];
                         float *mine = bucket_sums + warp * kMostBuckets;
                         if (high - low < kFewBuckets) {
                             // farther out a bucket is wide: its part of each row, as bits, one bucket after the other
                             for (int bucket = low; bucket <= high; ++bucket) {
-                                // distance of column c: row_zero - c
-                                const int row_zero = zero + 63 + lane;
-                                const int from = bucket == P.bias.buckets - 1 ? 0 : row_zero - M.tables.first[bucket + 1] + 1;
-                                const int to = row_zero - M.tables.first[bucket] + 1;
+                                // distance of column c: row_zero + c
+                                const int row_zero = zero + 31 - lane;
+                                const int from = M.tables.first[bucket] - row_zero;
+                                const int to = bucket == P.bias.buckets - 1 ? 64 : M.tables.first[bucket + 1] - row_zero;
                                 float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                                 for (int c = 0; c < 64; c += 32) {
@@ -1507,7 +1507,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                             }
                         } else {
                             // lane l sums the diagonals of numbers l, l + 32 and l + 64, read askew from shared memory some columns at a time (row r, column c: number
-                            // r - c + 63).  Then equal buckets are neighbours, summed across lanes in a fixed order.
+                            // c - r + 31).  Then equal buckets are neighbours, summed across lanes in a fixed order.
                             float *stripe = stripes + warp * kStripeFloats<HALVES>;
                             float sums[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
@@ -1515,15 +1515,15 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
 #pragma unroll
                                 for (int i = 0; i < kStripe<HALVES>; ++i) stripe[lane * (kStripe<HALVES> + 1) + i] = row < left ? p[c + i] : 0.0f;
                                 __syncwarp();
-                                // in columns 32 k .. 32 k + 31, row l + (c - 32 k) - 31 of lane l has number l + 32 (1 - k), and
-                                // 32 rows further down (where that is negative) number l + 32 (2 - k)
-                                const int high = c < 32 ? 2 : 1;
+                                // column 32 k + c of lane l: row c - l - 1 has number l + 32 (k + 1), or where that is negative the
+                                // row 32 further down number l + 32 k
+                                const int k = c / 32;
 #pragma unroll
                                 for (int i = 0; i < kStripe<HALVES>; ++i) {
-                                    const int r = lane + (c & 31) + i - 31;
+                                    const int r = (c & 31) + i - lane - 1;
                                     const float x = stripe[(r & 31) * (kStripe<HALVES> + 1) + i];
-                                    if (r >= 0) sums[high - 1] += x;
-                                    else sums[high] += x;
+                                    if (r >= 0) sums[k + 1] += x;
+                                    else sums[k] += x;
                                 }
                                 __syncwarp();
                             }
@@ -1549,6 +1549,24 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                             }
                         }
                     }
+                }
+                if (BIAS && KEYS && P.partials != nullptr && apart + 1 == meets) {
+                    // the sums of this query head
+                    far_sum = row < left ? far_sum : 0.0f;
+#pragma unroll
+                    for (int d = 16; d > 0; d /= 2) far_sum += __shfl_xor_sync(0xffffffffu, far_sum, d);
+                    if (lane == 0) bucket_sums[warp * kMostBuckets + P.bias.buckets - 1] += far_sum;
+                    far_sum = 0.0f;
+                    barrier_named(1, kSoftmaxThreads);
+                    if (threadIdx.x < P.bias.buckets) {
+                        float sum = 0.0f;
+                        for (int of = 0; of < 8; ++of) {
+                            sum += bucket_sums[of * kMostBuckets + threadIdx.x];
+                            bucket_sums[of * kMostBuckets + threadIdx.x] = 0.0f;
+                        }
+                        P.partials[((long long)item.slot * P.heads + q_head) * P.bias.buckets + threadIdx.x] = !ok || *failed ? NAN : sum / unit;
+                    }
+                    barrier_named(1, kSoftmaxThreads);                          // the next sums start from zero
                 }
                 if (++apart == meets) {
                     apart = 0;
@@ -1608,22 +1626,6 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                         }
                     });
             }
-            if (BIAS && !KEYS && P.partials != nullptr) {
-                if (row >= left) far_sum = 0.0f;
-#pragma unroll
-                for (int d = 16; d > 0; d /= 2) far_sum += __shfl_xor_sync(0xffffffffu, far_sum, d);
-                if (lane == 0) bucket_sums[warp * kMostBuckets + P.bias.buckets - 1] += far_sum;
-                barrier_named(1, kSoftmaxThreads);
-                if (threadIdx.x < P.bias.buckets) {
-                    float sum = 0.0f;
-                    for (int of = 0; of < 8; ++of) {
-                        sum += bucket_sums[of * kMostBuckets + threadIdx.x];
-                        bucket_sums[of * kMostBuckets + threadIdx.x] = 0.0f;
-                    }
-                    P.partials[((long long)item.slot * P.heads + head) * P.bias.buckets + threadIdx.x] = gone ? NAN : sum / unit;
-                }
-                barrier_named(1, kSoftmaxThreads);                              // the sums of the next work start from zero
-            }
             ++n;
         }
     }
@@ -1682,7 +1684,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_q, const
     __syncthreads();
     umma::fence_after();
     if (warp == 9) umma::tensor_columns_give<512>(tensor_base);
-    if (P.keys || P.join.ticket == nullptr) return;
+    if (!P.keys || P.join.ticket == nullptr) return;
     // few sums: the CTA that is done last joins them
     __shared__ int last;
     if (threadIdx.x == 0) {
