@@ -26,7 +26,7 @@ constexpr int64_t kJoinWithin = 8192;            // so few sums of dbias are joi
 
 struct Layout {
     int64_t capacity;                            // tiles of a call at most
-    size_t count, ticket, items, fold, used, norms, delta, partials, total;
+    size_t count, ticket, items, fold, arrived, used, norms, delta, partials, total;
 };
 
 using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -82,8 +82,12 @@ Layout make_layout(const psops_attention_config *c)
     l.ticket = take(sizeof(int));
     l.items = take((size_t)l.capacity * sizeof(Item));
     const bool grads = c->flags & PSOPS_ATTENTION_GRADS;
+    const bool grouped = grads && c->heads > c->kv_heads;
     if (c->max_tokens * (grads ? c->heads / c->kv_heads : 1) > (int64_t)kChain * kTile)
         l.fold = take((size_t)kMostCtas * kFoldFloats * sizeof(float));
+    else if (grouped)
+        l.fold = take((size_t)std::min<int64_t>(kMostCtas, 2 * l.capacity * c->heads) * kFoldFloats * sizeof(float));
+    if (grouped) l.arrived = take((size_t)kMostCtas * 2 * sizeof(int));
     if (grads) {
         l.used = take((size_t)l.capacity * sizeof(int));
         l.norms = take(kMostFillBlocks * sizeof(float2));
@@ -366,6 +370,12 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
     J.out = d_dbias;
     const bool join_within = d_dbias != nullptr && J.slots > 0 && (int64_t)J.slots * H * a->cfg.buckets <= kJoinWithin;
     if (join_within) J.ticket = L.ticket = a->at<int>(a->lay.ticket);
+    // few tiles: a CTA for each query head, and the last of those that share a key head adds them up
+    const bool split = H > G && (L.capacity - 1) * H <= std::min(a->sms, kMostCtas / 2) && L.capacity * G <= kMostCtas;
+    if (split) {
+        L.zero = a->at<int>(a->lay.arrived);
+        L.zeros = 2 * kMostCtas;
+    }
     PSOPS_DO(prepare(a, L, blocks));
     if (tokens > 0 && sequences > 0) {
         CUtensorMap mq, mk, mv, mg;
@@ -406,8 +416,12 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         if (dq != nullptr || d_dbias != nullptr || dk != nullptr)
             PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, H, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
         P.keys = 1;
+        P.split = split;
+        P.arrived = a->at<int>(a->lay.arrived);
+        P.unclean = P.arrived + kMostCtas;
+        if (split) P.by_kv_heads = divisor(H);
         if (dk != nullptr || dv != nullptr || d_dbias != nullptr)
-            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, G, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
+            PSOPS_DO(launch(a, "psops_attention_backward_kernel", kernel, works_grid(a, L, split ? H : G, 1), kBackwardThreads, shared, 1, mq, mk, mv, mg, P));
     }
     if (d_dbias == nullptr || join_within) return PSOPS_OK;
     return launch(a, "psops_attention_join_kernel",

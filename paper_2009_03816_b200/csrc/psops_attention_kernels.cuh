@@ -60,6 +60,8 @@ struct PrepParams {
     int *count;
     int *used;               // NULL, or by slot whether a tile has it
     int *ticket;             // NULL, or becomes zero
+    int *zero;               // so many numbers that become zero
+    int zeros;
     int heads, kv_heads, dim;
     int fill;                // how many of `rest` are to be zeroed where no sequence is
     Heads rest[3];
@@ -207,6 +209,7 @@ __device__ __forceinline__ void make_list(const PrepParams &P)
     const int bins = (most >> shift) + 1;
     for (int i = threadIdx.x; i <= bins; i += kPrepThreads) sequences_at[i] = rest_at[i] = 0;
     if (P.ticket != nullptr && threadIdx.x == 0) *P.ticket = 0;
+    for (int i = threadIdx.x; i < P.zeros; i += kPrepThreads) P.zero[i] = 0;
     if (P.used != nullptr)
         for (int i = threadIdx.x; i < P.capacity; i += kPrepThreads) P.used[i] = 0;
     __syncthreads();
@@ -1007,6 +1010,26 @@ struct JoinParams {
     void *out;                               // buckets x heads
     int *ticket;
 };
+// Slots from, from + step, ... of one of them, eight loads under way at a time.
+__device__ __forceinline__ double sum_of_slots(const JoinParams &P, int at, int from, int step)
+{
+    const int per_slot = P.heads * P.buckets;
+    double sum = 0.0;
+    for (int s = from; s < P.slots; s += 8 * step) {
+        float x[8];
+        int used[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int slot = min(s + i * step, P.slots - 1);
+            used[i] = s + i * step < P.slots ? P.used[slot] : 0;
+            x[i] = __ldcg(P.partials + (long long)slot * per_slot + at);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (used[i]) sum += (double)x[i];
+    }
+    return sum;
+}
 template <class T>
 __device__ __forceinline__ void put_dbias(const JoinParams &P, int at, double sum)
 {
@@ -1021,6 +1044,8 @@ struct BackwardParams {
     int tokens, heads, group, dim;
     Divisor by_heads, by_kv_heads, by_group;
     int keys;
+    int split;                               // KEYS: a work has one query head only, and the last of a key head's CTAs adds them up
+    int *arrived, *unclean;                  // for that, by slot and key head, from zero: CTAs that are done; which of dk, dv met no number
     float scale, scale2;
     Heads q, k, grad;                        // read where numbers are not finite
     Heads dq, dk, dv;                        // an address is NULL where the result is not wanted
@@ -1052,6 +1077,7 @@ struct BackwardShared {
     int dirty[2][2];                         // by parity of the work, and which of B
     alignas(16) float by_column[2][2][kTile];        // lse and delta of the queries
     float of_half[2][kTile];
+    int last, unclean;
     typename Choose<BIAS>::Type tables;
 };
 
@@ -1114,6 +1140,10 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
     auto work_of = [&](int turn) { return work_at(P.items, total, heads, turn); };
     Work coming = work_of(0);
     auto kv_of = [&](int head) { return (int)divide(head, P.by_group); };
+    // KEYS: the key head of a work, its first query head and how many
+    auto key_head_of = [&](const Work &w) { return P.split ? kv_of(w.head) : w.head; };
+    auto query_head_of = [&](const Work &w) { return P.split ? w.head : w.head * P.group; };
+    const int query_heads = P.split ? 1 : P.group;
     // A tile meets level + 1 tiles of B (of each head): !KEYS from the diagonal down, KEYS from the diagonal up.
     auto tile_of = [](const Work &w) { return KEYS ? (w.item.length + kTile - 1) / kTile - 1 - w.item.level : w.item.level; };
     auto token_of = [](int first, int meets, int j) { return KEYS ? first + (j % meets) * kTile : first - j * kTile; };
@@ -1126,20 +1156,21 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
             const Work w = coming;
             coming = work_of(turn);
             if (w.item.length <= 0) continue;
-            const int first = w.item.first + tile_of(w) * kTile, meets = w.item.level + 1, rounds = KEYS ? meets * P.group : meets;
+            const int first = w.item.first + tile_of(w) * kTile, meets = w.item.level + 1, rounds = KEYS ? meets * query_heads : meets;
+            const int a_head = KEYS ? key_head_of(w) : w.head;
             ok = wait_all(&bars.a_empty, (n & 1) ^ 1, failed);
             if (!ok) break;
             if (umma::elected()) {
                 umma::barrier_expect(umma::shared_address(&bars.a_full), 2 * kTileBytes);
                 for (int h = 0; h < HALVES; ++h) {
-                    umma::tensor_load3(a_at + h * kHalfBytes, &map_a0, h * 64, w.head, first, umma::shared_address(&bars.a_full));
-                    umma::tensor_load3(a_at + kTileBytes + h * kHalfBytes, &map_a1, h * 64, w.head, first, umma::shared_address(&bars.a_full));
+                    umma::tensor_load3(a_at + h * kHalfBytes, &map_a0, h * 64, a_head, first, umma::shared_address(&bars.a_full));
+                    umma::tensor_load3(a_at + kTileBytes + h * kHalfBytes, &map_a1, h * 64, a_head, first, umma::shared_address(&bars.a_full));
                 }
             }
             __syncwarp();
             ++n;
             for (int j = 0; j < rounds; ++j, ++r) {
-                const int stage = r & 1, token = token_of(first, meets, j), b_head = KEYS ? w.head * P.group + j / meets : kv_of(w.head);
+                const int stage = r & 1, token = token_of(first, meets, j), b_head = KEYS ? query_head_of(w) + j / meets : kv_of(w.head);
                 ok = wait_all(&bars.b_empty[stage], (r >> 1 & 1) ^ 1, failed);
                 if (!ok) break;
                 if (umma::elected()) {
@@ -1189,7 +1220,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
             const Work w = coming;
             coming = work_of(turn);
             if (w.item.length <= 0) continue;
-            const int meets = w.item.level + 1, rounds = KEYS ? meets * P.group : meets;
+            const int meets = w.item.level + 1, rounds = KEYS ? meets * query_heads : meets;
             auto loaded = [&](int r) { return wait_all(&bars.b_full[r & 1], r >> 1 & 1, failed); };
             auto last_scores = [&](int j) {                                  // A is read no more
                 if (j == rounds - 1 && umma::elected()) umma::products_arrive<false>(umma::shared_address(&bars.a_empty));
@@ -1260,8 +1291,8 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
             coming = work_of(turn);
             if (w.item.length <= 0) continue;
             const Item item = w.item;
-            const int head = w.head, tile = tile_of(w), first = item.first + tile * kTile, meets = item.level + 1;
-            const int rounds = KEYS ? meets * P.group : meets;
+            const int head = KEYS ? key_head_of(w) : w.head, tile = tile_of(w), first = item.first + tile * kTile, meets = item.level + 1;
+            const int rounds = KEYS ? meets * query_heads : meets;
             const int left = item.length - tile * kTile;                        // rows of A that exist
             float row_base = 0.0f, row_delta = 0.0f, row_sum = 0.0f, far_sum = 0.0f, next_value = 0.0f;
             if (!KEYS && row < left) {
@@ -1275,7 +1306,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                 if (token >= item.first + item.length) return 0.0f;
                 return (half == 0 ? P.lse : P.delta)[(long long)q_head * P.tokens + token];
             };
-            int apart = 0, q_head = KEYS ? head * P.group : head;               // tiles between queries and keys; KEYS: the query head
+            int apart = 0, q_head = KEYS ? query_head_of(w) : head;             // tiles between queries and keys; KEYS: the query head
             float column = KEYS ? fetch(0, q_head) : 0.0f;
             // the bias of the (first) query head
             auto value = [&](int q_head) { return threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, q_head) : 0.0f; };
@@ -1587,16 +1618,49 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
             const bool gone = !ok || *failed;
             // half of the columns of each sum
             const int begin = half * 32 * HALVES, end = min(begin + 32 * HALVES, P.dim);
+            int unclean = *(volatile int *)&M.dirty[n & 1][0] | *(volatile int *)&M.dirty[n & 1][1] << 1;
+            if (KEYS && P.split) {
+                // sums to this CTA's room; the last CTA of the key head reads them all, in the order of the heads
+                for (int which = 0; which < 2; ++which)
+                    add_to_room(room_of(P.fold, blockIdx.x * 2 + which, row), (which ? sum1_at : sum0_at) + lanes - col0, begin, end, 1.0f, rounds > kChain);
+                __threadfence();
+                barrier_named(1, kSoftmaxThreads);
+                const int at = item.slot * (int)divide(P.heads, P.by_group) + head;
+                if (threadIdx.x == 0) {
+                    if (gone) unclean |= 4;
+                    if (unclean != 0) atomicOr(P.unclean + at, unclean);
+                    __threadfence();
+                    M.last = atomicAdd(P.arrived + at, 1) == P.group - 1;
+                    __threadfence();
+                    M.unclean = *(volatile int *)(P.unclean + at);
+                }
+                barrier_named(1, kSoftmaxThreads);
+                unclean = M.unclean;
+                if (!M.last) continue;                                          // its only work
+            }
 #pragma unroll
             for (int which = 0; which < (KEYS ? 2 : 1); ++which) {
-                const bool poisoned = *(volatile int *)&M.dirty[n & 1][which] != 0;
+                const bool poisoned = unclean >> which & 1;
                 const Heads &O = !KEYS ? P.dq : which ? P.dv : P.dk;
                 if (O.p == nullptr) continue;
-                const float times = gone ? NAN : which ? (kBf16 ? 1.0f : 0x1p-14f) : P.scale / unit;
+                const float times = gone || unclean & 4 ? NAN : which ? (kBf16 ? 1.0f : 0x1p-14f) : P.scale / unit;
                 uint16_t *out = (uint16_t *)O.p + (long long)(first + (warp & 3) * 32) * O.token + head * O.head;
                 for (int c = begin; c < end; c += 32)
                     put_rows<T>((which ? sum1_at : sum0_at) + lanes - col0, times, out, O.token, c, P.dim, left - (warp & 3) * 32, [&](float *x) {
-                        if (rounds > kChain) {
+                        if (KEYS && P.split) {
+                            const int cta = (int)blockIdx.x - (w.head - head * P.group);                // of the first head; work i is CTA i's
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] = 0.0f;
+#pragma unroll 1
+                            for (int g = 0; g < P.group; ++g) {
+                                const float *from = room_of(P.fold, (cta + g) * 2 + which, row);
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (c + i < end) x[i] += __ldcg(from + (c + i) * kTile);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] *= times;
+                        } else if (rounds > kChain) {
                             const float *folded = room_of(P.fold, blockIdx.x * 2 + which, row);
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
@@ -1694,12 +1758,8 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_q, const
     }
     __syncthreads();
     if (last)
-        for (int at = threadIdx.x; at < P.join.heads * P.join.buckets; at += kBackwardThreads) {
-            double sum = 0.0;
-            for (int s = 0; s < P.join.slots; ++s)
-                if (P.join.used[s]) sum += (double)__ldcg(P.join.partials + (long long)s * P.join.heads * P.join.buckets + at);
-            put_dbias<T>(P.join, at, sum);
-        }
+        for (int at = threadIdx.x; at < P.join.heads * P.join.buckets; at += kBackwardThreads)
+            put_dbias<T>(P.join, at, sum_of_slots(P.join, at, 0, 1));
 }
 
 // dbias: the slots of all tiles joined in their order, in double.
@@ -1709,10 +1769,7 @@ __global__ void __launch_bounds__(32 * kJoinParts) psops_attention_join_kernel(c
     __shared__ double sums[kJoinParts][32];
     umma::after_the_kernel_before();
     const int per_slot = P.heads * P.buckets, at = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
-    double sum = 0.0;
-    if (at < per_slot)
-        for (int s = part; s < P.slots; s += kJoinParts)
-            if (P.used[s]) sum += (double)P.partials[(long long)s * per_slot + at];
+    double sum = at < per_slot ? sum_of_slots(P, at, part, kJoinParts) : 0.0;
     sums[part][threadIdx.x & 31] = sum;
     __syncthreads();
     if (part != 0 || at >= per_slot) return;
