@@ -646,9 +646,16 @@ constexpr int forward_shared() { return 1024 + (HALVES == 1 ? 6 : 3) * HALVES * 
 // A CTA has 128 queries of one head; two CTAs share an SM, so that one's softmax
 // runs under the other's products.  Per tile of 128 keys: S = Q K^T into tensor
 // memory; two threads have a row of it, 64 columns each, and tell one another
-// their maxima; P goes back into tensor memory as the left operand of O += P V.  For dim <= 64 the half of an SM's tensor memory that
-// a CTA has holds P beside S: the next scores are computed as soon as S has been
-// read, with two tiles of K and V under way.  For more, P takes the place of S.
+// their maxima; P goes back into tensor memory as the left operand of O += P V,
+// 32 columns of each half ahead of the others.  For dim <= 64 the half of an SM's
+// tensor memory that a CTA has holds P beside S: the next scores are computed as
+// soon as S has been read, with two tiles of K and V under way.  For more, P takes
+// the place of S.
+// 8,192 tokens, 16 heads (bf16, one sequence): dim 128 0.25 to 0.28 ms, 0.98 to 1.08
+// PFLOP/s, where exponentials and products take the same time and wait for one
+// another (54 % of each unit); dim 64 0.21 ms, 0.65 PFLOP/s, bound by the exponentials
+// and the issue slots about them (57 % of both).  37 sequences of some 440 tokens
+// have works of 3.5 tiles, whose beginnings and ends cost as much as the tiles.
 template <class T, int HALVES, bool BIAS>
 __global__ void __launch_bounds__(kForwardThreads, 2)
 psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -658,6 +665,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
     constexpr int kTileBytes = HALVES * kHalfBytes;
     constexpr bool kAhead = HALVES == 1;
     constexpr int kStages = kAhead ? 2 : 1;
+    // of 8,192 tokens: dim 64 every 4th pair 221 us, 8th 206, 12th 213, none 225; dim 128 271, 263, none 252
     constexpr int kOwn = kAhead ? 8 : 0;
     // fp16 has no numbers below 2^-24: probabilities, at most 2^kLazy, are kept higher up
     constexpr float kShift = kBf16 ? 0.0f : 7.0f;
@@ -1062,7 +1070,8 @@ struct BackwardParams {
 constexpr int kBackwardThreads = 320;        // as above
 // columns of ds that are summed along their diagonals at a time: as many as there is shared memory for
 template <int HALVES> constexpr int kStripe = HALVES == 1 ? 32 : 16;
-constexpr int kFewBuckets = 3;               // up to so many buckets in a warp's part of a tile are summed one by one
+constexpr int kFewBuckets = 3;               // fewer buckets in a warp's part of a tile are summed one by one: 185 to 181 us
+                                             // of a launch with 12,345 tokens, 12 heads and a bias to 512 (5: the same)
 template <int HALVES> constexpr int kStripeFloats = 32 * (kStripe<HALVES> + 1);
 
 template <int HALVES, bool BIAS>
@@ -1101,6 +1110,10 @@ struct BackwardShared {
 // mean key (one more product, p k; dq and dk are off by 1.3 to 1.5 times their
 // rounding then, for a tenth of the time), and leaves the corrected delta to KEYS.
 // Where a row has but one tile, delta is made from p and dp first.
+// 8,192 tokens, 16 heads of 128 on 4 (bf16, one sequence): queries 0.43 ms, keys 0.46,
+// 1.2 PFLOP/s: tensor unit 64 % of the time, fed from shared memory at its 128
+// bytes a clock in the scores' products; longer calls meet the power cap.  dim 64:
+// 0.35 and 0.39 ms, the softmax threads' latency (one CTA an SM).
 template <class T, int HALVES, bool KEYS, bool BIAS>
 __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const CUtensorMap &map_a1, const CUtensorMap &map_b0, const CUtensorMap &map_b1,
                                               const BackwardParams &P, BackwardShared<BIAS> &M, uint8_t *tiles, uint32_t tensor_base, float unit,
@@ -1108,7 +1121,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
 {
     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
     constexpr int kTileBytes = HALVES * kHalfBytes;
-    constexpr int kOwn = 4;
+    constexpr int kOwn = 4;                  // queries and keys of 8,192 tokens, 16 heads x 64: 784 us, 8th pair 789, none 813
     // scores in two places by turns, where tensor memory has room for them: the next ones need not wait for these
     constexpr bool kTwice = KEYS && HALVES == 1;
     constexpr uint32_t kSecond = 3 * kTile;                                 // columns 384 to 511
