@@ -1730,6 +1730,7 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_q, const
         umma::prefetch_map(&map_grad);
     }
     if (warp == 9) umma::tensor_columns_take<512>(umma::shared_address(&tensor_base_slot));
+    __syncthreads();                                                        // it has them before the next kernel may come
     umma::after_the_kernel_before();
     float unit = 1.0f;                                                      // of ds
     if (__is_same(T, __half)) {
