@@ -616,8 +616,9 @@ int psops_xent_destroy(psops_xent *x);
  * Softmax statistics are fp32.  The tensor cores multiply 16-bit numbers: p and ds
  * enter their second products rounded to the type of q.  In fp16, p is kept scaled
  * by a power of two, and ds by one that the largest norms of the rows of do and v
- * allow, so that small ones keep their digits; results are rounded once, at the
- * end.  do_i . out_i is corrected for the rounding of out.
+ * in the call's sequences allow, so that small ones keep their digits (the product
+ * of these two norms, D, is common to the call: a ds below 2^-26 D has fewer digits,
+ * one below 2^-37 D is lost); results are rounded once, at the end.  do_i . out_i is corrected for the rounding of out.
  * Should a product ever wait in vain for its operands (four seconds), the
  * results of its tile, and of those that its CTA does after it, are NaN.
  */

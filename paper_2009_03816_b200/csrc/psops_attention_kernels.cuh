@@ -304,8 +304,8 @@ __device__ __forceinline__ float dot8(uint4 a, uint4 b)
 }
 
 // delta[h, t] = do . o of each token and head: 16 lanes a row.  With norms, the
-// largest squared norm of a row of do and of v (rows that are not finite left
-// out): together they bound ds.
+// largest squared norm of a row of do and of v (rows that are not finite or of no
+// sequence left out): together they bound ds.
 template <class T>
 __device__ __forceinline__ void make_delta(const PrepParams &P, int block, int blocks)
 {
@@ -313,18 +313,26 @@ __device__ __forceinline__ void make_delta(const PrepParams &P, int block, int b
     const bool on = lane * 8 < P.dim;
     const long long rows = (long long)P.tokens * P.heads, step = (long long)blocks * teams;
     float most_grad = 0.0f, most_v = 0.0f;
+    int low = 0, high = 0;                                   // tokens of sequences
+    if (P.norms != nullptr && P.sequences > 0) {
+        low = clamped(P.offsets[0], 0, P.tokens);
+        high = max(clamped(P.offsets[P.sequences], 0, P.tokens), low);
+    }
     constexpr int U = 4;
     for (long long r0 = (long long)block * teams + threadIdx.x / 16; r0 - threadIdx.x / 16 < rows; r0 += U * step) {
         uint4 g[U], o[U];
         long long to[U];
+        bool counts[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const long long r = r0 + u * step;
             g[u] = o[u] = make_uint4(0, 0, 0, 0);
             to[u] = -1;
+            counts[u] = false;
             if (r < rows) {
                 const int token = (int)(r / P.heads), head = (int)(r % P.heads);
                 to[u] = (long long)head * P.tokens + token;
+                counts[u] = token >= low && token < high;
                 if (on) {
                     g[u] = *(const uint4 *)((const uint16_t *)P.grad.p + token * P.grad.token + head * P.grad.head + lane * 8);
                     o[u] = *(const uint4 *)((const uint16_t *)P.out.p + token * P.out.token + head * P.out.head + lane * 8);
@@ -340,12 +348,12 @@ __device__ __forceinline__ void make_delta(const PrepParams &P, int block, int b
                 square += __shfl_xor_sync(0xffffffffu, square, d);
             }
             if (lane == 0 && to[u] >= 0) P.delta[to[u]] = sum;
-            if (square < INFINITY) most_grad = fmaxf(most_grad, square);
+            if (counts[u] && square < INFINITY) most_grad = fmaxf(most_grad, square);
         }
     }
     if (P.norms == nullptr) return;
-    const long long v_rows = (long long)P.tokens * P.kv_heads;
-    for (long long r = (long long)block * teams + threadIdx.x / 16; r - threadIdx.x / 16 < v_rows; r += step) {
+    const long long v_rows = (long long)high * P.kv_heads, v_first = (long long)low * P.kv_heads;
+    for (long long r = v_first + (long long)block * teams + threadIdx.x / 16; r - threadIdx.x / 16 < v_rows; r += step) {
         uint4 v = make_uint4(0, 0, 0, 0);
         if (r < v_rows && on)
             v = *(const uint4 *)((const uint16_t *)P.v.p + r / P.kv_heads * P.v.token + r % P.kv_heads * P.v.head + lane * 8);

@@ -554,3 +554,20 @@ def test_a_whole_training_step_in_a_graph():
     for p, q, m in zip(eager.p, recorded.p, masters):
         assert float((p - q).norm()) < 0.05 * float((p - m).norm())
     assert recorded.opt.steps == eager.opt.steps == 4
+
+
+@pytest.mark.parametrize("kv_heads", [1, 4])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_large_numbers_in_rows_of_none_change_nothing(dtype, kv_heads):
+    """What lies in front and behind has no part in the scale of ds either."""
+    op, x, offsets = make([150, 40], 4, kv_heads, 64, dtype, 90, 110, buckets=[0, 1, 30])
+    x["grad"] *= 2.0 ** -10
+    clean = both(op, x, offsets)
+    compare({n: t[:, 90:280] if n == "lse" else t[90:280] for n, t in clean.items() if n in ("dq", "dk", "dv")},
+            reference(x["q"][90:280], x["k"][90:280], x["v"][90:280], [150, 40], 0, x["grad"][90:280], x["bias"], [0, 1, 30]))
+    y = {n: t.clone() for n, t in x.items()}
+    for n in ("q", "k", "v", "grad"):
+        y[n][:90] = y[n][280:] = 65504.0
+    got = both(op, y, offsets)
+    same(got, clean)
+    assert torch.equal(got["dbias"], clean["dbias"])
