@@ -199,7 +199,8 @@ __device__ __forceinline__ void bounds_of(const PrepParams &P, int b, int &first
 
 // One block.  Tiles go into bins by level (several levels to a bin only beyond
 // kBins of them); within a bin the order is left to chance, which changes when
-// a tile is done and nothing else.
+// a tile is done and nothing else.  There are capacity - 1 tiles at most, which grids
+// count on; offsets that decrease could make more, which are left out.
 __device__ __forceinline__ void make_list(const PrepParams &P)
 {
     __shared__ int sequences_at[kBins + 1], rest_at[kBins + 1], next[kBins];
@@ -245,16 +246,16 @@ __device__ __forceinline__ void make_list(const PrepParams &P)
             if (lane >= d) before += n;
         }
         for (int j = top - 1; j >= low; --j) next[j] += before - total;
-        if (lane == 31) *P.count = min(before, P.capacity);
+        if (lane == 31) *P.count = min(before, P.capacity - 1);
     }
     __syncthreads();
     auto place = [&](int first, int length, int slot, int level) {
         const int at = atomicAdd(&next[level >> shift], 1);
-        if (at < P.capacity && slot + level < P.capacity) {
+        if (at < P.capacity - 1 && slot + level < P.capacity) {
             P.items[at] = Item{first, length, level, slot + level};
             if (P.used != nullptr) P.used[slot + level] = 1;
-        } else if (at < P.capacity) {
-            P.items[at] = Item{0, 0, 0, 0};                  // offsets that decrease
+        } else if (at < P.capacity - 1) {
+            P.items[at] = Item{0, 0, 0, 0};                  // its slot belongs to another
         }
     };
     // a team of threads for each sequence: as many as there are for each, a warp at most

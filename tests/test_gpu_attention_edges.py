@@ -571,3 +571,16 @@ def test_large_numbers_in_rows_of_none_change_nothing(dtype, kv_heads):
     got = both(op, y, offsets)
     same(got, clean)
     assert torch.equal(got["dbias"], clean["dbias"])
+
+
+@pytest.mark.parametrize("order", [[0, 1024, 0, 1024], [1024, 0, 1024, 0], [0, 1024, 1000, 1024], [2000, -7, 1024, 3]], ids=str)
+def test_offsets_out_of_order_with_a_cta_for_each_head(order):
+    """More tiles than a batch in order could have: what is right is not said, but calls after it are."""
+    op = training.Attention(1024, 3, 12, 1, 64, dtype=BF16, buckets=[0, 5])
+    x = inputs(1024, 12, 1, 64, BF16, 0, True, [0, 5])
+    good = lengths_to_offsets([500, 24, 500])
+    want = both(op, x, good)
+    both(op, x, torch.tensor(order, dtype=torch.int32, device="cuda"))
+    got = both(op, x, good)
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
