@@ -603,12 +603,12 @@ int psops_xent_destroy(psops_xent *x);
  *
  * A row reads nothing of another sequence, of later tokens or of tokens of no
  * sequence, whatever these hold (NaN and infinities included).  A bias below
- * -1e30 (the lowest number of a type, -inf) takes its pairs out, whose numbers have
- * to be finite all the same: 0 is what their probabilities are multiplied with.  A
- * row that is left with no pair, or whose scores are all -inf, has out 0, lse -inf and no
- * gradient.  Sequences may be empty.  Rows of no sequence (in front of the first,
- * behind the last) are left as they were in all results, or become zeros if
- * zero_rest is not 0.
+ * -1e30 (-inf, the lowest number of bf16 and fp32, but not fp16's, which is a bias
+ * like any other) takes its pairs out, whose numbers have to be finite all the
+ * same: 0 is what their probabilities are multiplied with.  A row that is left with
+ * no pair, or whose scores are all -inf, has out 0, lse -inf and no gradient.
+ * Sequences may be empty.  Rows of no sequence (in front of the first, behind the
+ * last) are left as they were in all results, or become zeros if zero_rest is not 0.
  *
  * Rounding: products are summed in fp32 by the tensor cores, which cut sums off
  * where fp32 would round; they add up at most 16,384 terms in one go, fp32

@@ -404,15 +404,14 @@ struct Bias {
     int first[kMostBuckets];                 // the first distance of each bucket
 };
 
-// In base 2.  What lies below -1e30, such as the lowest number of a type, takes its
-// pairs out as -inf does: no row's lse could hold it beside a logarithm.
+// In base 2.  What lies below -1e30, such as the lowest number of bf16 and fp32, takes
+// its pairs out as -inf does.
 template <class T>
 __device__ __forceinline__ float bias_at(const Bias &B, int bucket, int heads, int head)
 {
     const long long i = (long long)bucket * heads + head;
     const float b = B.fp32 ? ((const float *)B.p)[i] : (float)((const T *)B.p)[i];
-    const float x = b * kLog2e;
-    return x < -1e30f ? -INFINITY : x;
+    return b < -1e30f ? -INFINITY : b * kLog2e;
 }
 __device__ __forceinline__ void barrier_named(int id, int threads)
 {
