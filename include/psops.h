@@ -610,6 +610,12 @@ int psops_xent_destroy(psops_xent *x);
  * Sequences may be empty.  Rows of no sequence (in front of the first, behind the
  * last) are left as they were in all results, or become zeros if zero_rest is not 0.
  *
+ * Biases may have any finite size: where the largest one that a row meets lies beyond
+ * 256, it is taken off all of them before scores are added, and the backward pass sums
+ * such a row up again (lse, which is rounded to fp32 as a whole, does not hold what it
+ * needs), a key at a time: masks over a sequence's first tokens cost nothing to speak
+ * of, a whole head at -1e9 does.
+ *
  * Rounding: products are summed in fp32 by the tensor cores, which cut sums off
  * where fp32 would round; they add up at most 16,384 terms in one go, fp32
  * additions do the rest (1.2e-4 of the largest partial sum at most, however long).

@@ -27,7 +27,7 @@ constexpr int64_t kJoinWithin = 8192;            // so few sums of dbias are joi
 
 struct Layout {
     int64_t capacity;                            // tiles of a call at most
-    size_t count, ticket, items, fold, arrived, used, norms, delta, partials, total;
+    size_t count, ticket, items, fold, arrived, used, norms, delta, levels, beside, partials, total;
 };
 
 using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -82,6 +82,7 @@ Layout make_layout(const psops_attention_config *c)
     l.count = take(sizeof(int));
     l.ticket = take(sizeof(int));
     l.items = take((size_t)l.capacity * sizeof(Item));
+    if (c->buckets > 0) l.levels = take(sizeof(int));
     const bool grads = c->flags & PSOPS_ATTENTION_GRADS;
     const bool grouped = grads && c->heads > c->kv_heads;
     if (c->max_tokens * (grads ? c->heads / c->kv_heads : 1) > (int64_t)kChain * kTile)
@@ -94,6 +95,7 @@ Layout make_layout(const psops_attention_config *c)
         l.norms = take(kMostFillBlocks * sizeof(float2));
         l.delta = take((size_t)c->max_tokens * c->heads * sizeof(float));
         l.partials = take((size_t)l.capacity * c->heads * c->buckets * sizeof(float));
+        if (c->buckets > 0) l.beside = take((size_t)c->max_tokens * c->heads * sizeof(float));
     }
     l.total = at;
     return l;
@@ -170,8 +172,11 @@ PrepParams prepare_params(const psops_attention *a, const Call &c)
     return P;
 }
 
-int prepare(psops_attention *a, const PrepParams &P, int64_t blocks)
+int prepare(psops_attention *a, PrepParams &P, int64_t blocks)
 {
+    P.blocks = (int)blocks;
+    if (P.beside != nullptr) blocks += std::min<int64_t>(2 * a->sms, ceil_div((int64_t)P.tokens * P.heads, kPrepThreads / 16));
+    else if (P.levels != nullptr) blocks += 1;
     return launch(a, "psops_attention_prepare_kernel",
                   a->cfg.type == PSOPS_F16 ? psops_attention_prepare_kernel<__half> : psops_attention_prepare_kernel<__nv_bfloat16>,
                   dim3((unsigned)(1 + blocks)), kPrepThreads, 0, 1, P);
@@ -295,6 +300,10 @@ int psops_attention_forward(psops_attention *a, const psops_heads *q, const psop
         L.rest_heads[0] = H;
         L.rest_lse = d_lse;
     }
+    if (a->cfg.buckets > 0) {
+        L.levels = a->at<int>(a->lay.levels);
+        L.bias = bias_of(a, d_bias, bias_type);
+    }
     // no more tiles than CTAs run at once: they need no list (short batches, where a launch counts)
     const bool own = sequences > 0 && (L.capacity - 1) * H <= std::min(2 * a->sms, kMostCtas);
     if (!own) PSOPS_DO(prepare(a, L, zero_rest ? std::min<int64_t>(a->sms, ceil_div(tokens * H * (a->cfg.dim / 8), kPrepThreads)) : 0));
@@ -317,6 +326,7 @@ int psops_attention_forward(psops_attention *a, const psops_heads *q, const psop
     P.v = V;
     P.lse = d_lse;
     P.bias = bias_of(a, d_bias, bias_type);
+    P.levels = L.levels;
     P.fold = a->at<float>(a->lay.fold);
     P.own = own;
     P.prep = L;
@@ -351,6 +361,15 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         L.v = heads_of(a, v, tokens, G);
         L.delta = a->at<float>(a->lay.delta);
         if (a->cfg.type == PSOPS_F16) L.norms = a->at<float2>(a->lay.norms);
+        if (a->cfg.buckets > 0) {
+            L.levels = a->at<int>(a->lay.levels);
+            L.bias = bias_of(a, d_bias, bias_type);
+            L.beside = a->at<float>(a->lay.beside);
+            L.lse = d_lse;
+            L.q = heads_of(a, q, tokens, H);
+            L.k = heads_of(a, k, tokens, G);
+            L.scale2 = a->cfg.scale * kLog2e;
+        }
         if (zero_rest) {
             const psops_heads *all[3] = {dq, dk, dv};
             for (int i = 0; i < 3; ++i)
@@ -400,6 +419,8 @@ int psops_attention_backward(psops_attention *a, const psops_heads *q, const pso
         P.k = K;
         P.grad = L.grad;
         P.lse = d_lse;
+        P.levels = L.levels;
+        P.beside = L.beside;
         P.delta = L.delta;
         P.norms = L.norms;
         P.blocks = (int)blocks;

@@ -53,6 +53,36 @@ struct Heads {               // tokens x heads x dim, elements of a head consecu
     long long token, head;   // strides in elements
 };
 
+struct Bias {
+    const void *p;                           // buckets x heads, NULL for none
+    int fp32;                                // else of the call's 16-bit type
+    int buckets, last;                       // last: the first distance of the last bucket
+    int first[kMostBuckets];                 // the first distance of each bucket
+};
+
+// What lies below -1e30, such as the lowest number of bf16 and fp32, takes its pairs
+// out as -inf does.
+template <class T>
+__device__ __forceinline__ float bias_at(const Bias &B, int bucket, int heads, int head)
+{
+    const long long i = (long long)bucket * heads + head;
+    const float b = B.fp32 ? ((const float *)B.p)[i] : (float)((const T *)B.p)[i];
+    return b < -1e30f ? -INFINITY : b;
+}
+
+// Beside a bias of -1e9 a score has no digits left in fp32, and a logarithm none in
+// lse.  So the level of a row is the largest bias of the buckets that it meets, those
+// up to the one of its position, where that lies beyond kPlain (an exponent of that
+// size is off by 2^-16); else 0.  It is taken off the row's biases before a score is
+// added, and off its lse, which the backward pass sums up once more for that (lse
+// itself is rounded as a whole); rows whose lse is not beyond kPlain need none of it
+// there.  Levels are rare (a mask of -1e9 over all that a sequence's first tokens
+// meet) and have code of their own, out of line: within the usual code they cost it 3
+// to 7 % of its time.
+constexpr float kPlain = 256.0f;
+__device__ __forceinline__ bool beyond_plain(float x) { return fabsf(x) > kPlain && fabsf(x) < INFINITY; }
+__device__ __forceinline__ float level_of(float most) { return beyond_plain(most) ? most : 0.0f; }
+
 struct PrepParams {
     const int *offsets;
     int sequences, tokens, capacity;
@@ -70,6 +100,13 @@ struct PrepParams {
     // backward
     Heads out, grad, v;
     float *delta;            // NULL in a forward pass
+    int blocks;              // for these two; those beyond are for
+    int *levels;             // ... whether any row can have a level, and
+    float *beside;           // (NULL in a forward pass) base 2: the log-sum-exps of rows with levels, beside those
+    const float *lse;
+    Heads q, k;
+    float scale2;
+    Bias bias;
     float2 *norms;           // NULL, or for each block but the first the largest squared norms of grad's and v's rows
 };
 
@@ -380,59 +417,173 @@ __device__ __forceinline__ void make_delta(const PrepParams &P, int block, int b
     }
 }
 
+// The log-sum-exp of one row beside its level, if it has one, key by key; by 16 lanes
+// (`team`).
 template <class T>
-__global__ void __launch_bounds__(kPrepThreads) psops_attention_prepare_kernel(const PrepParams P)
+__device__ __noinline__ void sum_beside_level(const PrepParams &P, int token, int head, uint32_t team)
+{
+    const int lane = threadIdx.x & 15;
+    // the last sequence that begins at the token or before
+    int low = 0, high = P.sequences;
+    while (low < high) {
+        const int mid = (low + high) / 2;
+        if (P.offsets[mid] <= token) low = mid + 1;
+        else high = mid;
+    }
+    if (low == 0 || token >= P.offsets[low]) return;
+    const int first = clamped(P.offsets[low - 1], 0, token);
+    float most = -INFINITY;
+    for (int b = lane; b < P.bias.buckets; b += 16)
+        if (P.bias.first[b] <= token - first) most = fmaxf(most, bias_at<T>(P.bias, b, P.heads, head));
+#pragma unroll
+    for (int d = 8; d > 0; d /= 2) most = fmaxf(most, __shfl_xor_sync(team, most, d));
+    const float level = level_of(most);
+    if (level == 0.0f) return;
+    const bool on = lane * 8 < P.dim;
+    const uint16_t *keys = (const uint16_t *)P.k.p + head / (P.heads / P.kv_heads) * P.k.head + lane * 8;
+    uint4 q = make_uint4(0, 0, 0, 0);
+    if (on) q = *(const uint4 *)((const uint16_t *)P.q.p + token * P.q.token + head * P.q.head + lane * 8);
+    int bucket = P.bias.buckets;
+    float beside = 0.0f, top = -INFINITY, sum = 0.0f;
+    constexpr int U = 4;                     // keys under way
+    for (int j0 = first; j0 <= token; j0 += U) {
+        uint4 k[U];
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            k[u] = make_uint4(0, 0, 0, 0);
+            if (on) k[u] = *(const uint4 *)(keys + min(j0 + u, token) * P.k.token);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            x[u] = dot8<T>(q, k[u]);
+#pragma unroll
+            for (int d = 8; d > 0; d /= 2) x[u] += __shfl_xor_sync(team, x[u], d);
+        }
+        float higher = top;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int distance = token - j0 - u;
+            if (distance >= 0 && (bucket == P.bias.buckets || distance < P.bias.first[bucket])) {
+                do --bucket;
+                while (distance < P.bias.first[bucket]);
+                beside = (bias_at<T>(P.bias, bucket, P.heads, head) - level) * kLog2e;
+            }
+            x[u] = distance >= 0 ? __fmaf_rn(x[u], P.scale2, beside) : -INFINITY;
+            higher = fmaxf(higher, x[u]);
+        }
+        if (higher > -INFINITY) {
+            sum *= exp2_fast(top - higher);
+#pragma unroll
+            for (int u = 0; u < U; ++u) sum += exp2_fast(x[u] - higher);
+        }
+        top = higher;
+    }
+    // a row without any score has no probabilities
+    if (lane == 0) P.beside[(long long)head * P.tokens + token] = top > -INFINITY ? top + log2_fast(sum) : INFINITY;
+}
+
+// By blocks of their own, which end where no row can have a level.
+template <class T>
+__device__ __forceinline__ void make_beside(const PrepParams &P, int block, int blocks)
+{
+    bool some = false;
+    const int entries = P.bias.buckets * P.heads;
+    for (int i = threadIdx.x; i < entries; i += kPrepThreads) some |= beyond_plain(bias_at<T>(P.bias, i / P.heads, P.heads, i % P.heads));
+    if (__syncthreads_or(some)) {
+        some = false;
+        for (int h = threadIdx.x; h < P.heads; h += kPrepThreads) {
+            float most = -INFINITY;
+            for (int b = 0; b < P.bias.buckets; ++b) {
+                most = fmaxf(most, bias_at<T>(P.bias, b, P.heads, h));
+                some |= level_of(most) != 0.0f;
+            }
+        }
+        some = __syncthreads_or(some);
+    }
+    if (block == 0 && threadIdx.x == 0) *P.levels = some;
+    if (!some || P.beside == nullptr) return;
+    const long long rows = (long long)P.tokens * P.heads;
+    for (long long r = (long long)block * (kPrepThreads / 16) + threadIdx.x / 16; r < rows; r += (long long)blocks * (kPrepThreads / 16)) {
+        // a block's rows are neighbours and read the same keys
+        const int token = (int)(r % P.tokens), head = (int)(r / P.tokens);
+        if (beyond_plain(P.lse[r])) sum_beside_level<T>(P, token, head, 0xffffu << (threadIdx.x & 16));
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kPrepThreads, 2) psops_attention_prepare_kernel(const __grid_constant__ PrepParams P)
 {
     umma::after_the_kernel_before();
     if (blockIdx.x == 0) {
         make_list(P);
         return;
     }
-    const int block = blockIdx.x - 1, blocks = gridDim.x - 1;
-    if (P.fill > 0) fill_rest<kPrepThreads>(P, block, blocks);
-    if (P.delta != nullptr) make_delta<T>(P, block, blocks);
+    const int block = blockIdx.x - 1, more = gridDim.x - 1 - P.blocks;
+    if (block >= P.blocks) {
+        make_beside<T>(P, block - P.blocks, more);
+        return;
+    }
+    if (P.fill > 0) fill_rest<kPrepThreads>(P, block, P.blocks);
+    if (P.delta != nullptr) make_delta<T>(P, block, P.blocks);
 }
 
 // ---------------------------------------------------------------------------
 // What the two tensor-core kernels share
 // ---------------------------------------------------------------------------
 
-struct Bias {
-    const void *p;                           // buckets x heads, NULL for none
-    int fp32;                                // else of the call's 16-bit type
-    int buckets, last;                       // last: the first distance of the last bucket
-    int first[kMostBuckets];                 // the first distance of each bucket
-};
-
-// In base 2.  What lies below -1e30, such as the lowest number of bf16 and fp32, takes
-// its pairs out as -inf does.
-template <class T>
-__device__ __forceinline__ float bias_at(const Bias &B, int bucket, int heads, int head)
-{
-    const long long i = (long long)bucket * heads + head;
-    const float b = B.fp32 ? ((const float *)B.p)[i] : (float)((const T *)B.p)[i];
-    return b < -1e30f ? -INFINITY : b * kLog2e;
-}
 __device__ __forceinline__ void barrier_named(int id, int threads)
 {
     asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+// The same; whether x is true in any of the threads.
+__device__ __forceinline__ bool barrier_any(int id, int threads, bool x)
+{
+    uint32_t any;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(any)
+                 : "r"((uint32_t)x), "r"(id), "r"(threads)
+                 : "memory");
+    return any != 0;
 }
 
 // What the softmax threads of a CTA keep of the bias; distances up to a tile's
 // reach beyond the last bucket's beginning.
 struct Tables {
-    float value[kMostBuckets];               // of the head at hand
+    float value[kMostBuckets];               // of the head at hand, base 2; LEVELS: as given
+    float level[kMostBuckets];               // LEVELS: of rows whose position is in a bucket
     int first[kMostBuckets];
     uint8_t bucket[kMostDistance + 2 * kTile];
-    float distance[kTableFloats];            // [kBefore + d]: the bias of distance d
+    float distance[kTableFloats];            // [kBefore + d]: the bias of distance d, base 2
+
+    __device__ __forceinline__ float level_at(const Bias &B, int position) const { return level[bucket[min(position, B.last)]]; }
+    // the bias of distance d beside a level, base 2; of distances below 0 any number
+    __device__ __forceinline__ float beside(int d, float level) const { return (value[bucket[max(d, 0)]] - level) * kLog2e; }
 };
-// By THREADS threads that share barrier 1, after each has put its part of `value` in place.
-template <int THREADS, bool BUCKETS>
-__device__ __forceinline__ void make_tables(const Bias &B, Tables &t)
+// By one warp, two buckets a lane: running maxima over the buckets.
+__device__ __noinline__ void make_levels(Tables &t, int buckets)
+{
+    const int lane = threadIdx.x & 31, b = 2 * lane;
+    const float one = b < buckets ? t.value[b] : -INFINITY, two = b + 1 < buckets ? t.value[b + 1] : -INFINITY;
+    float most = fmaxf(one, two);
+    for (int d = 1; d < 32; d *= 2) {
+        const float n = __shfl_up_sync(0xffffffffu, most, d);
+        if (lane >= d) most = fmaxf(most, n);
+    }
+    float before = __shfl_up_sync(0xffffffffu, most, 1);
+    if (lane == 0) before = -INFINITY;
+    t.level[b] = level_of(fmaxf(before, one));
+    t.level[b + 1] = level_of(most);
+}
+// By THREADS threads that share barrier 1; mine: of the first ones the bias of bucket threadIdx.x.
+template <int THREADS, bool BUCKETS, bool LEVELS>
+__device__ __forceinline__ void make_tables(const Bias &B, Tables &t, float mine)
 {
     const int many = B.last + 2 * kTile;
+    if (threadIdx.x < kMostBuckets) t.value[threadIdx.x] = LEVELS ? mine : mine * kLog2e;
     if (BUCKETS && threadIdx.x < kMostBuckets) t.first[threadIdx.x] = threadIdx.x < B.buckets ? B.first[threadIdx.x] : INT32_MAX;
     barrier_named(1, THREADS);
+    if (LEVELS && threadIdx.x < 32) make_levels(t, B.buckets);
     if (BUCKETS && threadIdx.x < kBefore) t.distance[threadIdx.x] = 0.0f;
     for (int d = threadIdx.x; d < many; d += THREADS) {
         int bucket;
@@ -445,7 +596,7 @@ __device__ __forceinline__ void make_tables(const Bias &B, Tables &t)
         } else {
             bucket = t.bucket[d];
         }
-        t.distance[kBefore + d] = t.value[bucket];
+        if (!LEVELS) t.distance[kBefore + d] = t.value[bucket];
     }
     barrier_named(1, THREADS);
 }
@@ -633,6 +784,7 @@ template <> struct Choose<false> { using Type = None; };
 struct ForwardParams {
     const Item *items;
     const int *count;
+    const int *levels;                       // with a list: whether any row can have a level
     int tokens, heads, dim;
     Divisor by_heads, by_group;
     float scale2;                            // scale, base 2
@@ -644,12 +796,233 @@ struct ForwardParams {
     PrepParams prep;
 };
 
+template <int HALVES, bool BIAS>
+struct ForwardShared {
+    static constexpr int kStages = HALVES == 1 ? 2 : 1;
+    alignas(8) uint64_t q_full[kStages], q_empty[kStages], k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages], s, read, p[2], o;
+    int failed, dirty[2];
+    float other[2][2][kTile], other_sum[2][kTile], fold_top[2][kTile];   // maxima (by parity of the tile) and sums of the rows' halves
+    typename Choose<BIAS>::Type tables;
+};
+
 constexpr int kForwardThreads = 320;         // eight warps of softmax, one of copies, one of products
 constexpr int kSoftmaxThreads = 256;
 constexpr float kLazy = 8.0f;                // a maximum moves only when it grows by more than this (base 2)
 
 template <int HALVES>
 constexpr int forward_shared() { return 1024 + (HALVES == 1 ? 6 : 3) * HALVES * kHalfBytes; }
+
+// Whether rows whose position is in bucket threadIdx.x have a level.
+template <class T>
+__device__ __forceinline__ bool head_has_levels(const Bias &B, int heads, int head)
+{
+    if (threadIdx.x >= B.buckets || !beyond_plain(bias_at<T>(B, threadIdx.x, heads, head))) return false;
+    float most = -INFINITY;
+    for (int b = 0; b <= (int)threadIdx.x; ++b) most = fmaxf(most, bias_at<T>(B, b, heads, head));
+    return level_of(most) != 0.0f;
+}
+
+// What the softmax threads of a CTA do, half a row each.
+template <class T, int HALVES, bool BIAS, bool LEVELS>
+__device__ __forceinline__ void forward_rows(const ForwardParams &P, ForwardShared<HALVES, BIAS> &M, uint8_t *tiles, uint32_t tensor_base, Work coming, int total)
+{
+    constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
+    constexpr int kTileBytes = HALVES * kHalfBytes;
+    constexpr bool kAhead = HALVES == 1;
+    constexpr int kStages = kAhead ? 2 : 1;
+    // of 8,192 tokens: dim 64 every 4th pair 221 us, 8th 206, 12th 213, none 225; dim 128 271, 263, none 252
+    constexpr int kOwn = kAhead ? 8 : 0;
+    // fp16 has no numbers below 2^-24: probabilities, at most 2^kLazy, are kept higher up
+    constexpr float kShift = kBf16 ? 0.0f : 7.0f;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int half = warp >> 2, row = threadIdx.x & (kTile - 1), col0 = half * 64;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t s_at = tensor_base, o_at = s_at + kTile, p_at = kAhead ? o_at + 64 : s_at;
+    const int o_begin = half * 32 * HALVES, o_end = min(o_begin + 32 * HALVES, P.dim);      // its columns of O
+    volatile int *failed = &M.failed;
+    auto kv_of = [&](int head) { return (int)divide(head, P.by_group); };
+    float far = 0.0f;
+    const float *table = nullptr;
+    if constexpr (BIAS) table = M.tables.distance + kBefore;
+    // where it is not, all works are gone through all the same, without waits, for the barriers in them
+    bool ok = true;
+    int t = 0, n = 0, head_before = -1;
+    for (int turn = 1; coming.some; ++turn) {
+        const Work w = coming;
+        coming = work_at(P.items, total, P.by_heads, turn);
+        if (w.item.length <= 0) continue;
+        const int tile = w.item.level, first = w.item.first + tile * kTile;
+        if constexpr (BIAS) {
+            if (w.head != head_before) {
+                const float mine = threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, w.head) : 0.0f;
+                if (n == 0) make_tables<kSoftmaxThreads, true, LEVELS>(P.bias, M.tables, mine);
+                else make_tables<kSoftmaxThreads, false, LEVELS>(P.bias, M.tables, mine);
+                far = M.tables.value[P.bias.buckets - 1];
+                head_before = w.head;
+            }
+            if constexpr (LEVELS) far = M.tables.beside(P.bias.last, M.tables.level_at(P.bias, tile * kTile + row));
+        }
+        float top = -INFINITY, sum = 0.0f;   // top: what is subtracted, base 2
+        for (int j = 0; j <= tile; ++j, ++t) {
+            ok = ok && wait_all(&M.s, t & 1, failed);
+            umma::fence_after();
+            if (j > 0 && j % kChain == 0) {
+                // a chain of sums ends: what lies in memory, of another maximum, and this one
+                if (kAhead) {
+                    ok = ok && wait_all(&M.o, (t & 1) ^ 1, failed);
+                    umma::fence_after();
+                }
+                float *folded = room_of(P.fold, blockIdx.x, row);
+                const float factor = top > -INFINITY ? exp2_fast(M.fold_top[half][row] - top) : 1.0f;
+                add_to_room(folded, o_at + lanes, o_begin, o_end, factor, j > kChain);
+                M.fold_top[half][row] = top;
+            }
+            const bool diagonal = j == 0, near = BIAS && j * kTile - (kTile - 1) < P.bias.last;
+            const float *distance = table + j * kTile + row - col0;           // - column
+            // half a row; with a bias it becomes the whole exponent here, else scale and bias come with the exponential
+            uint32_t s[64];
+            float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            umma::tensor_memory_load(s_at + lanes + col0, s);
+            umma::tensor_memory_load(s_at + lanes + col0 + 32, s + 32);
+            umma::tensor_memory_loaded<64>(s);
+            if constexpr (LEVELS) {
+                if (near) {
+                    const float level = M.tables.level_at(P.bias, tile * kTile + row);
+#pragma unroll
+                    for (int i = 0; i < 64; ++i)
+                        s[i] = __float_as_uint(__fmaf_rn(__uint_as_float(s[i]), P.scale2, M.tables.beside(j * kTile + row - col0 - i, level)));
+                }
+            }
+            if (near && !LEVELS) {
+#pragma unroll
+                for (int i = 0; i < 64; ++i) s[i] = __float_as_uint(__fmaf_rn(__uint_as_float(s[i]), P.scale2, distance[-i]));
+            }
+            if (diagonal) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t keep = below(row - col0 + 1 - 32 * c);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (!(keep >> i & 1)) s[32 * c + i] = 0xff800000u;   // -inf
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 64; i += 8)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) most[m] = max3(most[m], __uint_as_float(s[i + 2 * m]), __uint_as_float(s[i + 2 * m + 1]));
+            if (kAhead) {
+                umma::fence_before();
+                __syncwarp();
+                if (lane == 0) umma::barrier_arrive(umma::shared_address(&M.read));
+            }
+            float higher = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            M.other[t & 1][half][row] = higher;
+            barrier_named(2 + (warp & 3), 64);                           // the two warps that have these rows
+            higher = fmaxf(higher, M.other[t & 1][half ^ 1][row]);
+            if (!near) higher = __fmaf_rn(higher, P.scale2, far);
+            if (kAhead && t > 0) {           // else M.s has said so: the product of the tile before is complete
+                ok = ok && wait_all(&M.o, (t & 1) ^ 1, failed);
+                umma::fence_after();
+            }
+            if (__any_sync(0xffffffffu, higher > top + kLazy)) {
+                higher = fmaxf(higher, top);
+                const float factor = higher > -INFINITY ? exp2_fast(top - higher) : 1.0f;
+                top = higher;
+                sum *= factor;
+                if (j % kChain > 0) {
+                    for (int c = o_begin; c < o_end; c += 16) {
+                        uint32_t u[16];
+                        umma::tensor_memory_load16(o_at + lanes + c, u);
+                        umma::tensor_memory_loaded<16>(u);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * factor);
+                        umma::tensor_memory_store16(o_at + lanes + c, u);
+                    }
+                }
+            }
+            const float base = (near ? 0.0f : far) + kShift - (top > -INFINITY ? top : 0.0f);
+            const uint64_t times = both(near ? 1.0f : P.scale2), plus = both(base);
+            uint64_t parts[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                uint32_t p[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint64_t x = fma_both(pair_of(s[c + 2 * i], s[c + 2 * i + 1]), times, plus);
+                    const uint64_t e = exp2_pair<kOwn>(x, i);
+                    parts[i & 3] = add_both(parts[i & 3], e);
+                    p[i] = pack2<T>(low_of(e), high_of(e));
+                }
+                umma::tensor_memory_store16(p_at + lanes + (kAhead ? half * 32 : col0) + c / 2, p);
+                if (!diagonal) {
+                    umma::tensor_memory_stored();
+                    umma::fence_before();
+                    __syncwarp();
+                    if (lane == 0) umma::barrier_arrive(umma::shared_address(&M.p[c / 32]));
+                }
+            }
+            const uint64_t all = add_both(add_both(parts[0], parts[1]), add_both(parts[2], parts[3]));
+            sum += low_of(all) + high_of(all);
+            if (diagonal) {
+                // keys that are masked here may hold anything: rows of the next sequence, or of none
+                ok = ok && wait_all(&M.v_full[t % kStages], t / kStages & 1, failed);
+                uint8_t *v = tiles + (2 * kStages + t % kStages) * kTileBytes + half * kHalfBytes;
+                if (half < HALVES && not_clean<T>(v, row)) {
+                    clean_row<T>(v, row);
+                    M.dirty[n & 1] = 1;
+                }
+                umma::tensor_memory_stored();
+                umma::fence_before();
+                __syncwarp();
+                if (lane == 0)
+                    for (int i = 0; i < 2; ++i) umma::barrier_arrive(umma::shared_address(&M.p[i]));
+            }
+        }
+        // while the last product runs: the sum, and all that does not need O
+        const int left = w.item.length - tile * kTile;                        // queries of this tile
+        uint16_t *out = (uint16_t *)P.out.p + (long long)(first + (warp & 3) * 32) * P.out.token + w.head * P.out.head;
+        M.other_sum[half][row] = sum;
+        barrier_named(2 + (warp & 3), 64);
+        sum += M.other_sum[half ^ 1][row];
+        float unit = sum > 0.0f || sum != sum ? reciprocal(sum) : 0.0f;
+        if (half == 0 && row < left) {
+            float lse = sum == 0.0f ? -INFINITY : (top + (log2_fast(sum) - kShift)) * kLn2;
+            if constexpr (LEVELS) lse += M.tables.level_at(P.bias, tile * kTile + row);
+            P.lse[(long long)w.head * P.tokens + first + row] = lse;
+        }
+        ok = ok && wait_all(&M.o, (t & 1) ^ 1, failed);
+        umma::fence_after();
+        if (threadIdx.x == 0) M.dirty[(n & 1) ^ 1] = 0;                         // read by all in the work before
+        barrier_named(1, kSoftmaxThreads);
+        const bool poisoned = *(volatile int *)&M.dirty[n & 1] != 0;
+        if (!ok || *failed) {
+            unit = NAN;
+            if (half == 0 && row < left) P.lse[(long long)w.head * P.tokens + first + row] = NAN;
+        }
+        for (int c = o_begin; c < o_end; c += 32)
+            put_rows<T>(o_at + lanes, unit, out, P.out.token, c, P.dim, left - (warp & 3) * 32, [&](float *x) {
+                if (tile >= kChain) {
+                    const float *folded = room_of(P.fold, blockIdx.x, row);
+                    const float factor = top > -INFINITY ? exp2_fast(M.fold_top[half][row] - top) * unit : unit;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c + i < o_end) x[i] = __fmaf_rn(folded[(c + i) * kTile], factor, x[i]);
+                }
+                if (!poisoned) return;
+                const uint16_t *v = (const uint16_t *)P.v.p + (long long)first * P.v.token + kv_of(w.head) * P.v.head;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (c + i < o_end && row < left) x[i] += taken_away<T>(v + c + i, P.v.token, 0, row + 1);
+            });
+        ++n;
+    }
+}
+template <class T, int HALVES>
+__device__ __noinline__ void forward_rows_with_levels(const ForwardParams &P, ForwardShared<HALVES, true> &M, uint8_t *tiles, uint32_t tensor_base, Work coming,
+                                                      int total)
+{
+    forward_rows<T, HALVES, true, true>(P, M, tiles, tensor_base, coming, total);
+}
 
 // A CTA has 128 queries of one head; two CTAs share an SM, so that one's softmax
 // runs under the other's products.  Per tile of 128 keys: S = Q K^T into tensor
@@ -673,32 +1046,24 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
     constexpr int kTileBytes = HALVES * kHalfBytes;
     constexpr bool kAhead = HALVES == 1;
     constexpr int kStages = kAhead ? 2 : 1;
-    // of 8,192 tokens: dim 64 every 4th pair 221 us, 8th 206, 12th 213, none 225; dim 128 271, 263, none 252
-    constexpr int kOwn = kAhead ? 8 : 0;
-    // fp16 has no numbers below 2^-24: probabilities, at most 2^kLazy, are kept higher up
-    constexpr float kShift = kBf16 ? 0.0f : 7.0f;
     extern __shared__ uint8_t raw[];
-    __shared__ alignas(8) uint64_t bar_q_full[kStages], bar_q_empty[kStages], bar_k_full[kStages], bar_k_empty[kStages], bar_v_full[kStages],
-        bar_v_empty[kStages], bar_s, bar_read, bar_p[2], bar_o;
+    __shared__ ForwardShared<HALVES, BIAS> M;
     __shared__ uint32_t tensor_base_slot;
-    __shared__ int failed_slot, dirty[2];
-    __shared__ float other[2][2][kTile], other_sum[2][kTile], fold_top[2][kTile];      // maxima (by parity of the tile) and sums of the rows' halves
-    __shared__ typename Choose<BIAS>::Type tables;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    volatile int *failed = &failed_slot;
+    volatile int *failed = &M.failed;
     uint8_t *tiles = raw + (((umma::shared_address(raw) + 1023u) & ~1023u) - umma::shared_address(raw));
     const uint32_t q_at = umma::shared_address(tiles), k_at = q_at + kStages * kTileBytes, v_at = k_at + kStages * kTileBytes;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i)
-            for (uint64_t *b : {&bar_q_full[i], &bar_q_empty[i], &bar_k_full[i], &bar_k_empty[i], &bar_v_full[i], &bar_v_empty[i]})
+            for (uint64_t *b : {&M.q_full[i], &M.q_empty[i], &M.k_full[i], &M.k_empty[i], &M.v_full[i], &M.v_empty[i]})
                 umma::barrier_init(umma::shared_address(b), 1);
-        umma::barrier_init(umma::shared_address(&bar_s), 1);
-        umma::barrier_init(umma::shared_address(&bar_o), 1);
-        umma::barrier_init(umma::shared_address(&bar_read), 8);
-        for (int i = 0; i < 2; ++i) umma::barrier_init(umma::shared_address(&bar_p[i]), 8);
-        failed_slot = dirty[0] = dirty[1] = 0;
+        umma::barrier_init(umma::shared_address(&M.s), 1);
+        umma::barrier_init(umma::shared_address(&M.o), 1);
+        umma::barrier_init(umma::shared_address(&M.read), 8);
+        for (int i = 0; i < 2; ++i) umma::barrier_init(umma::shared_address(&M.p[i]), 8);
+        M.failed = M.dirty[0] = M.dirty[1] = 0;
         umma::barrier_init_done();
         umma::prefetch_map(&map_q);
         umma::prefetch_map(&map_k);
@@ -731,32 +1096,32 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
             coming = work_at(P.items, total, P.by_heads, turn);
             if (w.item.length <= 0) continue;
             const int first = w.item.first + w.item.level * kTile, kv = kv_of(w.head), q_stage = n % kStages;
-            ok = wait_all(&bar_q_empty[q_stage], (n / kStages & 1) ^ 1, failed);
+            ok = wait_all(&M.q_empty[q_stage], (n / kStages & 1) ^ 1, failed);
             if (!ok) break;
             if (umma::elected()) {
-                umma::barrier_expect(umma::shared_address(&bar_q_full[q_stage]), kTileBytes);
+                umma::barrier_expect(umma::shared_address(&M.q_full[q_stage]), kTileBytes);
                 for (int h = 0; h < HALVES; ++h)
-                    umma::tensor_load3(q_at + q_stage * kTileBytes + h * kHalfBytes, &map_q, h * 64, w.head, first, umma::shared_address(&bar_q_full[q_stage]));
+                    umma::tensor_load3(q_at + q_stage * kTileBytes + h * kHalfBytes, &map_q, h * 64, w.head, first, umma::shared_address(&M.q_full[q_stage]));
             }
             __syncwarp();
             ++n;
             for (int j = 0; j <= w.item.level; ++j, ++t) {
                 const int token = first - j * kTile, stage = t % kStages;
                 const uint32_t phase = (t / kStages & 1) ^ 1;
-                ok = wait_all(&bar_k_empty[stage], phase, failed);
+                ok = wait_all(&M.k_empty[stage], phase, failed);
                 if (!ok) break;
                 if (umma::elected()) {
-                    umma::barrier_expect(umma::shared_address(&bar_k_full[stage]), kTileBytes);
+                    umma::barrier_expect(umma::shared_address(&M.k_full[stage]), kTileBytes);
                     for (int h = 0; h < HALVES; ++h)
-                        umma::tensor_load3(k_at + stage * kTileBytes + h * kHalfBytes, &map_k, h * 64, kv, token, umma::shared_address(&bar_k_full[stage]));
+                        umma::tensor_load3(k_at + stage * kTileBytes + h * kHalfBytes, &map_k, h * 64, kv, token, umma::shared_address(&M.k_full[stage]));
                 }
                 __syncwarp();
-                ok = wait_all(&bar_v_empty[stage], phase, failed);
+                ok = wait_all(&M.v_empty[stage], phase, failed);
                 if (!ok) break;
                 if (umma::elected()) {
-                    umma::barrier_expect(umma::shared_address(&bar_v_full[stage]), kTileBytes);
+                    umma::barrier_expect(umma::shared_address(&M.v_full[stage]), kTileBytes);
                     for (int h = 0; h < HALVES; ++h)
-                        umma::tensor_load3(v_at + stage * kTileBytes + h * kHalfBytes, &map_v, h * 64, kv, token, umma::shared_address(&bar_v_full[stage]));
+                        umma::tensor_load3(v_at + stage * kTileBytes + h * kHalfBytes, &map_v, h * 64, kv, token, umma::shared_address(&M.v_full[stage]));
                 }
                 __syncwarp();
             }
@@ -772,18 +1137,18 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
         // scores of tile t, the `j`th of work n
         auto scores = [&](int t, int n, int j, int last) {
             const int stage = t % kStages, q_stage = n % kStages;
-            if (j == 0 && !wait_all(&bar_q_full[q_stage], n / kStages & 1, failed)) return false;
-            if (!wait_all(&bar_k_full[stage], t / kStages & 1, failed)) return false;
-            if (kAhead && t > 0 && !wait_all(&bar_read, (t & 1) ^ 1, failed)) return false;
+            if (j == 0 && !wait_all(&M.q_full[q_stage], n / kStages & 1, failed)) return false;
+            if (!wait_all(&M.k_full[stage], t / kStages & 1, failed)) return false;
+            if (kAhead && t > 0 && !wait_all(&M.read, (t & 1) ^ 1, failed)) return false;
             umma::fence_after();
             if (umma::elected()) {
                 for (int s = 0; s < steps; ++s) {
                     const uint32_t on = (s >> 2) * (kHalfBytes >> 4) + (s & 3) * 2;
                     umma::multiply<false>(s_at, dq + q_stage * kNext + on, dk + stage * kNext + on, instr_s, s > 0);
                 }
-                umma::products_arrive<false>(umma::shared_address(&bar_s));
-                umma::products_arrive<false>(umma::shared_address(&bar_k_empty[stage]));
-                if (j == last) umma::products_arrive<false>(umma::shared_address(&bar_q_empty[q_stage]));
+                umma::products_arrive<false>(umma::shared_address(&M.s));
+                umma::products_arrive<false>(umma::shared_address(&M.k_empty[stage]));
+                if (j == last) umma::products_arrive<false>(umma::shared_address(&M.q_empty[q_stage]));
             }
             __syncwarp();
             return true;
@@ -809,10 +1174,10 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
                     return j < w.item.level ? scores(t + 1, n, j + 1, w.item.level) : !then.some || scores(t + 1, n + 1, 0, then.item.level);
                 };
                 if (kAhead) ok = ahead();
-                ok = ok && wait_all(&bar_v_full[stage], t / kStages & 1, failed);
+                ok = ok && wait_all(&M.v_full[stage], t / kStages & 1, failed);
                 // the first 32 columns of both halves of a row, then the others
                 for (int part = 0; part < 2 && ok; ++part) {
-                    ok = wait_all(&bar_p[part], t & 1, failed);
+                    ok = wait_all(&M.p[part], t & 1, failed);
                     if (!ok) break;
                     umma::fence_after();
                     if (umma::elected()) {
@@ -824,8 +1189,8 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
                                                               dv + stage * kNext + s * 128, instr_o, j % kChain > 0 || part > 0 || i > 0);
                         }
                         if (part == 1) {
-                            umma::products_arrive<false>(umma::shared_address(&bar_v_empty[stage]));
-                            umma::products_arrive<false>(umma::shared_address(&bar_o));
+                            umma::products_arrive<false>(umma::shared_address(&M.v_empty[stage]));
+                            umma::products_arrive<false>(umma::shared_address(&M.o));
                         }
                     }
                     __syncwarp();
@@ -837,174 +1202,14 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
             w = then;
         }
     } else {
-        // ---- softmax: half a row a thread
-        const int half = warp >> 2, row = threadIdx.x & (kTile - 1), col0 = half * 64;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const int o_begin = half * 32 * HALVES, o_end = min(o_begin + 32 * HALVES, P.dim);      // its columns of O
-        float far = 0.0f;
-        const float *table = nullptr;
-        if constexpr (BIAS) table = tables.distance + kBefore;
-        // where it is not, all works are gone through all the same, without waits, for the barriers in them
-        bool ok = true;
-        int t = 0, n = 0, head_before = -1;
-        for (int turn = 1; coming.some; ++turn) {
-            const Work w = coming;
-            coming = work_at(P.items, total, P.by_heads, turn);
-            if (w.item.length <= 0) continue;
-            const int tile = w.item.level, first = w.item.first + tile * kTile;
-            if constexpr (BIAS) {
-                if (w.head != head_before) {
-                    if (threadIdx.x < kMostBuckets)
-                        tables.value[threadIdx.x] = threadIdx.x < P.bias.buckets ? bias_at<T>(P.bias, threadIdx.x, P.heads, w.head) : 0.0f;
-                    if (n == 0) make_tables<kSoftmaxThreads, true>(P.bias, tables);
-                    else make_tables<kSoftmaxThreads, false>(P.bias, tables);
-                    far = tables.value[P.bias.buckets - 1];
-                    head_before = w.head;
-                }
-            }
-            float top = -INFINITY, sum = 0.0f;   // top: what is subtracted, base 2
-            for (int j = 0; j <= tile; ++j, ++t) {
-                ok = ok && wait_all(&bar_s, t & 1, failed);
-                umma::fence_after();
-                if (j > 0 && j % kChain == 0) {
-                    // a chain of sums ends: what lies in memory, of another maximum, and this one
-                    if (kAhead) {
-                        ok = ok && wait_all(&bar_o, (t & 1) ^ 1, failed);
-                        umma::fence_after();
-                    }
-                    float *folded = room_of(P.fold, blockIdx.x, row);
-                    const float factor = top > -INFINITY ? exp2_fast(fold_top[half][row] - top) : 1.0f;
-                    add_to_room(folded, o_at + lanes, o_begin, o_end, factor, j > kChain);
-                    fold_top[half][row] = top;
-                }
-                const bool diagonal = j == 0, near = BIAS && j * kTile - (kTile - 1) < P.bias.last;
-                const float *distance = table + j * kTile + row - col0;           // - column
-                // half a row; with a bias it becomes the whole exponent here, else scale and bias come with the exponential
-                uint32_t s[64];
-                float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                umma::tensor_memory_load(s_at + lanes + col0, s);
-                umma::tensor_memory_load(s_at + lanes + col0 + 32, s + 32);
-                umma::tensor_memory_loaded<64>(s);
-                if (near) {
-#pragma unroll
-                    for (int i = 0; i < 64; ++i) s[i] = __float_as_uint(__fmaf_rn(__uint_as_float(s[i]), P.scale2, distance[-i]));
-                }
-                if (diagonal) {
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const uint32_t keep = below(row - col0 + 1 - 32 * c);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!(keep >> i & 1)) s[32 * c + i] = 0xff800000u;   // -inf
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 64; i += 8)
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) most[m] = max3(most[m], __uint_as_float(s[i + 2 * m]), __uint_as_float(s[i + 2 * m + 1]));
-                if (kAhead) {
-                    umma::fence_before();
-                    __syncwarp();
-                    if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_read));
-                }
-                float higher = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-                other[t & 1][half][row] = higher;
-                barrier_named(2 + (warp & 3), 64);                           // the two warps that have these rows
-                higher = fmaxf(higher, other[t & 1][half ^ 1][row]);
-                if (!near) higher = __fmaf_rn(higher, P.scale2, far);
-                if (kAhead && t > 0) {           // else bar_s has said so: the product of the tile before is complete
-                    ok = ok && wait_all(&bar_o, (t & 1) ^ 1, failed);
-                    umma::fence_after();
-                }
-                if (__any_sync(0xffffffffu, higher > top + kLazy)) {
-                    higher = fmaxf(higher, top);
-                    const float factor = higher > -INFINITY ? exp2_fast(top - higher) : 1.0f;
-                    top = higher;
-                    sum *= factor;
-                    if (j % kChain > 0) {
-                        for (int c = o_begin; c < o_end; c += 16) {
-                            uint32_t u[16];
-                            umma::tensor_memory_load16(o_at + lanes + c, u);
-                            umma::tensor_memory_loaded<16>(u);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(__uint_as_float(u[i]) * factor);
-                            umma::tensor_memory_store16(o_at + lanes + c, u);
-                        }
-                    }
-                }
-                const float base = (near ? 0.0f : far) + kShift - (top > -INFINITY ? top : 0.0f);
-                const uint64_t times = both(near ? 1.0f : P.scale2), plus = both(base);
-                uint64_t parts[4] = {0, 0, 0, 0};
-#pragma unroll
-                for (int c = 0; c < 64; c += 32) {
-                    uint32_t p[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const uint64_t x = fma_both(pair_of(s[c + 2 * i], s[c + 2 * i + 1]), times, plus);
-                        const uint64_t e = exp2_pair<kOwn>(x, i);
-                        parts[i & 3] = add_both(parts[i & 3], e);
-                        p[i] = pack2<T>(low_of(e), high_of(e));
-                    }
-                    umma::tensor_memory_store16(p_at + lanes + (kAhead ? half * 32 : col0) + c / 2, p);
-                    if (!diagonal) {
-                        umma::tensor_memory_stored();
-                        umma::fence_before();
-                        __syncwarp();
-                        if (lane == 0) umma::barrier_arrive(umma::shared_address(&bar_p[c / 32]));
-                    }
-                }
-                const uint64_t all = add_both(add_both(parts[0], parts[1]), add_both(parts[2], parts[3]));
-                sum += low_of(all) + high_of(all);
-                if (diagonal) {
-                    // keys that are masked here may hold anything: rows of the next sequence, or of none
-                    ok = ok && wait_all(&bar_v_full[t % kStages], t / kStages & 1, failed);
-                    uint8_t *v = tiles + (2 * kStages + t % kStages) * kTileBytes + half * kHalfBytes;
-                    if (half < HALVES && not_clean<T>(v, row)) {
-                        clean_row<T>(v, row);
-                        dirty[n & 1] = 1;
-                    }
-                    umma::tensor_memory_stored();
-                    umma::fence_before();
-                    __syncwarp();
-                    if (lane == 0)
-                        for (int i = 0; i < 2; ++i) umma::barrier_arrive(umma::shared_address(&bar_p[i]));
-                }
-            }
-            // while the last product runs: the sum, and all that does not need O
-            const int left = w.item.length - tile * kTile;                        // queries of this tile
-            uint16_t *out = (uint16_t *)P.out.p + (long long)(first + (warp & 3) * 32) * P.out.token + w.head * P.out.head;
-            other_sum[half][row] = sum;
-            barrier_named(2 + (warp & 3), 64);
-            sum += other_sum[half ^ 1][row];
-            float unit = sum > 0.0f || sum != sum ? reciprocal(sum) : 0.0f;
-            if (half == 0 && row < left)
-                P.lse[(long long)w.head * P.tokens + first + row] = sum == 0.0f ? -INFINITY : (top + (log2_fast(sum) - kShift)) * kLn2;
-            ok = ok && wait_all(&bar_o, (t & 1) ^ 1, failed);
-            umma::fence_after();
-            if (threadIdx.x == 0) dirty[(n & 1) ^ 1] = 0;                         // read by all in the work before
-            barrier_named(1, kSoftmaxThreads);
-            const bool poisoned = *(volatile int *)&dirty[n & 1] != 0;
-            if (!ok || *failed) {
-                unit = NAN;
-                if (half == 0 && row < left) P.lse[(long long)w.head * P.tokens + first + row] = NAN;
-            }
-            for (int c = o_begin; c < o_end; c += 32)
-                put_rows<T>(o_at + lanes, unit, out, P.out.token, c, P.dim, left - (warp & 3) * 32, [&](float *x) {
-                    if (tile >= kChain) {
-                        const float *folded = room_of(P.fold, blockIdx.x, row);
-                        const float factor = top > -INFINITY ? exp2_fast(fold_top[half][row] - top) * unit : unit;
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (c + i < o_end) x[i] = __fmaf_rn(folded[(c + i) * kTile], factor, x[i]);
-                    }
-                    if (!poisoned) return;
-                    const uint16_t *v = (const uint16_t *)P.v.p + (long long)first * P.v.token + kv_of(w.head) * P.v.head;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (c + i < o_end && row < left) x[i] += taken_away<T>(v + c + i, P.v.token, 0, row + 1);
-                });
-            ++n;
+        // ---- softmax
+        bool levels = false;
+        if constexpr (BIAS) {
+            if (P.own) levels = barrier_any(1, kSoftmaxThreads, coming.some && head_has_levels<T>(P.bias, P.heads, coming.head));
+            else levels = *P.levels != 0;
+            if (levels) forward_rows_with_levels<T, HALVES>(P, M, tiles, tensor_base_slot, coming, total);
         }
+        if (!levels) forward_rows<T, HALVES, BIAS, false>(P, M, tiles, tensor_base_slot, coming, total);
     }
     __syncwarp();
     umma::fence_before();
@@ -1065,7 +1270,8 @@ struct BackwardParams {
     float scale, scale2;
     Heads q, k, grad;                        // read where numbers are not finite
     Heads dq, dk, dv;                        // an address is NULL where the result is not wanted
-    const float *lse;
+    const float *lse, *beside;               // beside: of rows with levels
+    const int *levels;                       // whether there can be any
     float *delta;                            // !KEYS makes it exact, for KEYS after it
     const float2 *norms;                     // NULL, or `blocks` of them
     int blocks;
@@ -1093,6 +1299,7 @@ struct BackwardShared {
     Barriers bars;
     int dirty[2][2];                         // by parity of the work, and which of B
     alignas(16) float by_column[2][2][kTile];        // lse and delta of the queries
+    float level[BIAS ? 2 : 1][BIAS ? kTile : 1];     // and their levels
     float of_half[2][kTile];
     int last, unclean;
     typename Choose<BIAS>::Type tables;
@@ -1122,7 +1329,7 @@ struct BackwardShared {
 // 1.2 PFLOP/s: tensor unit 64 % of the time, fed from shared memory at its 128
 // bytes a clock in the scores' products; longer calls meet the power cap.  dim 64:
 // 0.35 and 0.39 ms, the softmax threads' latency (one CTA an SM).
-template <class T, int HALVES, bool KEYS, bool BIAS>
+template <class T, int HALVES, bool KEYS, bool BIAS, bool LEVELS>
 __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const CUtensorMap &map_a1, const CUtensorMap &map_b0, const CUtensorMap &map_b1,
                                               const BackwardParams &P, BackwardShared<BIAS> &M, uint8_t *tiles, uint32_t tensor_base, float unit,
                                               volatile int *failed)
@@ -1334,12 +1541,21 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
             if constexpr (BIAS) {
                 if (q_head != head_before) {
                     if (n > 0) barrier_named(1, kSoftmaxThreads);               // nobody reads the M.tables of the head before
-                    if (threadIdx.x < kMostBuckets) M.tables.value[threadIdx.x] = value(q_head);
-                    if (n == 0) make_tables<kSoftmaxThreads, true>(P.bias, M.tables);
-                    else make_tables<kSoftmaxThreads, false>(P.bias, M.tables);
-                    far = M.tables.value[P.bias.buckets - 1];
+                    const float mine = value(q_head);
+                    if (n == 0) make_tables<kSoftmaxThreads, true, LEVELS>(P.bias, M.tables, mine);
+                    else make_tables<kSoftmaxThreads, false, LEVELS>(P.bias, M.tables, mine);
+                    far = LEVELS ? M.tables.beside(P.bias.last, 0.0f) : M.tables.value[P.bias.buckets - 1];
                     head_before = q_head;
                 }
+            }
+            float row_level = 0.0f;
+            if constexpr (LEVELS && !KEYS) {
+                if (row < left) {
+                    const long long at = (long long)head * P.tokens + first + row;
+                    if (beyond_plain(P.lse[at])) row_level = M.tables.level_at(P.bias, tile * kTile + row);
+                    if (row_level != 0.0f) row_base = kShift - P.beside[at];
+                }
+                far = M.tables.beside(P.bias.last, row_level);
             }
             for (int j = 0; j < rounds; ++j, ++r) {
                 if (j > 0 && j % kChain == 0) {
@@ -1358,14 +1574,24 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
                     if constexpr (BIAS) {
                         if (j > 0 && diagonal) {
                             barrier_named(1, kSoftmaxThreads);                  // nobody reads the M.tables of the head before
-                            if (threadIdx.x < kMostBuckets) M.tables.value[threadIdx.x] = next_value;
-                            make_tables<kSoftmaxThreads, false>(P.bias, M.tables);
-                            far = M.tables.value[P.bias.buckets - 1];
+                            make_tables<kSoftmaxThreads, false, LEVELS>(P.bias, M.tables, next_value);
+                            far = LEVELS ? M.tables.beside(P.bias.last, 0.0f) : M.tables.value[P.bias.buckets - 1];
                             head_before = q_head;
                         }
                         if (diagonal && j + meets < rounds) next_value = value(q_head + 1);
                     }
-                    M.by_column[r & 1][half][row] = half == 0 ? kShift - base2(column) + (near ? 0.0f : far) : -column * unit_p;
+                    float of = half == 0 ? kShift - base2(column) + (near ? 0.0f : far) : -column * unit_p;
+                    if constexpr (LEVELS) {
+                        if (half == 0) {
+                            // (where there is no query, column is 0)
+                            const float level = beyond_plain(column) ? M.tables.level_at(P.bias, (tile + apart) * kTile + row) : 0.0f;
+                            M.level[r & 1][row] = level;
+                            if (level != 0.0f)
+                                of = kShift - P.beside[(long long)q_head * P.tokens + first + apart * kTile + row] +
+                                     (near ? 0.0f : M.tables.beside(P.bias.last, level));
+                        }
+                    }
+                    M.by_column[r & 1][half][row] = of;
                     barrier_named(1, kSoftmaxThreads);
                     const bool last = apart + 1 == meets;
                     if (j + 1 < rounds) column = fetch(last ? 0 : apart + 1, last ? q_head + 1 : q_head);
@@ -1411,7 +1637,16 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
 #pragma unroll
                 for (int c = 0; c < 64; c += 32) {
                     // what a score's product is added to: shift, bias, -lse
-                    if (KEYS && near) {
+                    if (LEVELS && near) {
+                        if constexpr (LEVELS) {
+#pragma unroll
+                            for (int i = c; i < c + 32; ++i) {
+                                const int d = KEYS ? apart * kTile + col0 + i - row : apart * kTile + row - col0 - i;
+                                p[i] = (KEYS ? M.by_column[r & 1][0][col0 + i] : row_base) +
+                                       M.tables.beside(d, KEYS ? M.level[r & 1][col0 + i] : row_level);
+                            }
+                        }
+                    } else if (KEYS && near) {
 #pragma unroll
                         for (int i = c; i < c + 32; i += 4) {
                             const float4 of = *(const float4 *)&M.by_column[r & 1][0][col0 + i];
@@ -1716,6 +1951,14 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
     }
 }
 
+template <class T, int HALVES, bool KEYS>
+__device__ __noinline__ void backward_part_with_levels(const CUtensorMap &map_a0, const CUtensorMap &map_a1, const CUtensorMap &map_b0, const CUtensorMap &map_b1,
+                                                       const BackwardParams &P, BackwardShared<true> &M, uint8_t *tiles, uint32_t tensor_base, float unit,
+                                                       volatile int *failed)
+{
+    backward_part<T, HALVES, KEYS, true, true>(map_a0, map_a1, map_b0, map_b1, P, M, tiles, tensor_base, unit, failed);
+}
+
 template <class T, int HALVES, bool BIAS>
 __global__ void __launch_bounds__(kBackwardThreads, 1)
 psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -1763,8 +2006,18 @@ psops_attention_backward_kernel(const __grid_constant__ CUtensorMap map_q, const
         }
     }
     const uint32_t tensor_base = tensor_base_slot;
-    if (P.keys) backward_part<T, HALVES, true, BIAS>(map_k, map_v, map_q, map_grad, P, shared, tiles, tensor_base, unit, &failed_slot);
-    else backward_part<T, HALVES, false, BIAS>(map_q, map_grad, map_k, map_v, P, shared, tiles, tensor_base, unit, &failed_slot);
+    bool levels = false;
+    if constexpr (BIAS) {
+        levels = *P.levels != 0;
+        if (levels) {
+            if (P.keys) backward_part_with_levels<T, HALVES, true>(map_k, map_v, map_q, map_grad, P, shared, tiles, tensor_base, unit, &failed_slot);
+            else backward_part_with_levels<T, HALVES, false>(map_q, map_grad, map_k, map_v, P, shared, tiles, tensor_base, unit, &failed_slot);
+        }
+    }
+    if (!levels) {
+        if (P.keys) backward_part<T, HALVES, true, BIAS, false>(map_k, map_v, map_q, map_grad, P, shared, tiles, tensor_base, unit, &failed_slot);
+        else backward_part<T, HALVES, false, BIAS, false>(map_q, map_grad, map_k, map_v, P, shared, tiles, tensor_base, unit, &failed_slot);
+    }
     __syncwarp();
     umma::fence_before();
     __syncthreads();
