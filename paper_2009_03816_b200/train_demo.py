@@ -19,7 +19,8 @@ With --model block the worker's model is one transformer layer instead, fed with
 packed sequences of uneven lengths from the same source: embedding, causal
 attention with grouped heads and a learned bias by distance (training.Attention),
 a gated activation that keeps its inputs in 8 bits (training.Keep8, which also holds
-what autograd saves of the layer), residual connections, and the same head.
+what autograd saves of the layer's other operations but the attention), residual
+connections, and the same head.
 
 And every `step` iterations each worker's loss on a common held-out batch --
 LinearXent's forward alone, written straight into the swarm's loss vector -- is

@@ -28,6 +28,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import threading
 
 import torch
 
@@ -79,6 +80,22 @@ def _device_of(where, tensors):
 def _is_capturing(stream):
     with torch.cuda.stream(stream):
         return torch.cuda.is_current_stream_capturing()
+
+
+class _Exactly(threading.local):
+    """Around an operation that saves statistics of its inputs beside them: Keep8.hooks leaves these inputs alone, since
+    with others the statistics would be wrong (probabilities that do not sum to 1, beyond a 16-bit type's range even)."""
+
+    depth = 0
+
+    def __enter__(self):
+        self.depth += 1
+
+    def __exit__(self, *error):
+        self.depth -= 1
+
+
+_exactly = _Exactly()
 
 
 class _Holder:
@@ -317,7 +334,8 @@ class LinearXent(_Holder):
             w = w.contiguous()
         if isinstance(targets, torch.Tensor):
             targets = targets.contiguous()
-        return _LinearXentFunction.apply(h, w, targets, self, reduction)
+        with _exactly:
+            return _LinearXentFunction.apply(h, w, targets, self, reduction)
 
     @property
     def launches(self) -> int:
@@ -559,7 +577,8 @@ class Attention(_Holder):
         q, k, v = map(self._fitting, (q, k, v))
         if isinstance(bias, torch.Tensor):
             bias = bias.contiguous()
-        return _AttentionFunction.apply(q, k, v, bias, offsets, self)
+        with _exactly:
+            return _AttentionFunction.apply(q, k, v, bias, offsets, self)
 
 
 class _AttentionFunction(torch.autograd.Function):
@@ -768,10 +787,11 @@ class Keep8(_Holder):
 
     def hooks(self, least=4096):
         """A context in which autograd keeps the 16-bit tensors that it saves in 8 bits: those of `least` elements or
-        more on this GPU, but for leaves that have gradients (weights) and views of them, which are there anyway."""
+        more on this GPU, but for leaves that have gradients (weights) and views of them, which are there anyway, and
+        for what Attention and LinearXent save, whose statistics belong to the numbers as they are."""
         def pack(t):
             base = t._base if t._is_view() else t
-            if t.get_device() != self.device.index or t.dtype not in (torch.float16, torch.bfloat16) or \
+            if _exactly.depth or t.get_device() != self.device.index or t.dtype not in (torch.float16, torch.bfloat16) or \
                     t.numel() < max(1, least) or t.dim() < 1 or base.is_leaf and base.requires_grad:
                 return t
             with torch.no_grad():
