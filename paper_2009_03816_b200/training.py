@@ -793,21 +793,35 @@ class Keep8(_Holder):
             base = t._base if t._is_view() else t
             if _exactly.depth or t.get_device() != self.device.index or t.dtype not in (torch.float16, torch.bfloat16) or \
                     t.numel() < max(1, least) or t.dim() < 1 or base.is_leaf and base.requires_grad:
-                return t
+                return _AsItIs(t)
             with torch.no_grad():
                 codes, scales = self.pack(self._fitting(t.detach()))
                 self._join()
             return codes, scales, t.shape, t.dtype
 
         def unpack(kept):
-            if isinstance(kept, torch.Tensor):
-                return kept
+            if isinstance(kept, _AsItIs):
+                return kept.get()
             with torch.no_grad():
                 x = self.unpack(*kept)
                 self._join()
             return x
 
         return torch.autograd.graph.saved_tensors_hooks(pack, unpack)
+
+
+class _AsItIs:
+    """A tensor that Keep8.hooks leaves alone.  Autograd does not look at versions where there are hooks."""
+
+    def __init__(self, t):
+        self.tensor, self.version = t, t._version
+
+    def get(self):
+        if self.tensor._version != self.version:
+            raise RuntimeError(f"one of the variables needed for gradient computation has been modified by an inplace operation: "
+                               f"{tuple(self.tensor.shape)} {self.tensor.dtype}, at version {self.tensor._version}, saved at version "
+                               f"{self.version} (kept as it is by Keep8.hooks)")
+        return self.tensor
 
 
 class _Keep8Function(torch.autograd.Function):

@@ -57,3 +57,14 @@ def test_linear_cross_entropy_keeps_what_its_statistics_belong_to(keep, dtype):
         assert torch.equal(a.grad, b.grad)
 
 
+def test_a_weight_stepped_too_early_is_noticed(keep):
+    master = torch.randn(128, 128, device="cuda")
+    w = master.to(BF16).requires_grad_()
+    grad = torch.zeros_like(w)
+    opt = training.AdamW([master], [grad], copies=[w])
+    x = torch.randn(64, 128, device="cuda").to(BF16).requires_grad_()
+    with keep.hooks():
+        y = ((x * 1.0) @ w).sum()
+    opt.step(1e-3)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.backward()

@@ -1,0 +1,77 @@
+"""What Keep8.hooks() keeps and what it leaves alone, on the CPU: a stand-in takes the place of the kernels, which copies."""
+import gc
+import weakref
+
+import pytest
+import torch
+
+from paper_2009_03816_b200 import training
+
+
+class Stand(training.Keep8):
+    """Keeps CPU tensors: codes are a copy, in 16 bits for want of a kernel."""
+
+    def __init__(self):
+        self.device = type("Device", (), {"index": -1})()            # what get_device() says of CPU tensors
+        self.packed = []
+
+    def _join(self):
+        pass
+
+    def pack(self, x):
+        self.packed.append(tuple(x.shape))
+        return x.clone(), torch.zeros(1)
+
+    def unpack(self, codes, scales, shape, dtype, *, out=None):
+        return codes.clone()
+
+
+@pytest.fixture
+def keep():
+    return Stand()
+
+
+def some(*shape, seed=0, dtype=torch.bfloat16):
+    return torch.empty(*shape).normal_(generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+@pytest.mark.parametrize("change", ["weight", "small", "fp32"])
+def test_what_is_changed_after_it_was_saved_is_noticed(keep, change):
+    """As without the hooks: a weight stepped before its backward pass raises an error."""
+    dtype = torch.float32 if change == "fp32" else torch.bfloat16
+    w = some(64, 128, dtype=dtype).requires_grad_()
+    x = some(8 if change == "small" else 100, 64, seed=1, dtype=dtype)
+    with keep.hooks():
+        h = x.clone().requires_grad_() * 1.0
+        y = (h @ w).sum()
+    with torch.no_grad():
+        (w if change == "weight" else h).mul_(2.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.backward()
+
+
+def test_what_is_kept_in_8_bits_may_change(keep):
+    """Its codes are a copy."""
+    w, x = some(64, 128).requires_grad_(), some(100, 64, seed=1)
+    with keep.hooks():
+        h = x.clone().requires_grad_() * 1.0
+        y = (h @ w).sum()
+    with torch.no_grad():
+        h.zero_()
+    y.backward()
+    assert keep.packed == [(100, 64)]
+    torch.testing.assert_close(w.grad, x.T @ torch.ones(100, 128, dtype=torch.bfloat16))
+
+
+def test_second_derivatives_of_what_is_left_alone(keep):
+    x, w = some(5, 6, dtype=torch.float64).requires_grad_(), some(6, 7, seed=1, dtype=torch.float64).requires_grad_()
+    f = lambda: torch.tanh(x @ w).pow(3).sum()
+    with keep.hooks():
+        y = f()
+        (dx,) = torch.autograd.grad(y, x, create_graph=True)
+        got = torch.autograd.grad(dx.square().sum(), (x, w))
+    (dx,) = torch.autograd.grad(f(), x, create_graph=True)
+    for a, b in zip(got, torch.autograd.grad(dx.square().sum(), (x, w))):
+        assert torch.equal(a, b)
+
+
