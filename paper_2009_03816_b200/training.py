@@ -811,10 +811,11 @@ class Keep8(_Holder):
 
 
 class _AsItIs:
-    """A tensor that Keep8.hooks leaves alone.  Autograd does not look at versions where there are hooks."""
+    """A tensor that Keep8.hooks leaves alone.  Autograd does not look at versions where there are hooks, and an operation's
+    own result would hold the graph that holds it, so that neither were ever freed."""
 
     def __init__(self, t):
-        self.tensor, self.version = t, t._version
+        self.tensor, self.version = t.detach(), t._version
 
     def get(self):
         if self.tensor._version != self.version:

@@ -75,3 +75,16 @@ def test_second_derivatives_of_what_is_left_alone(keep):
         assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_results_that_are_left_alone_are_freed(keep, dtype):
+    """What an operation saves of its own result must not keep the graph alive that holds it."""
+    held = []
+    for _ in range(3):
+        x = some(20, 30, dtype=dtype).requires_grad_()
+        with keep.hooks():
+            y = torch.softmax(torch.exp(x), -1)
+        held.append(weakref.ref(y))
+        held.append(weakref.ref(x))
+        del x, y
+    gc.collect()
+    assert all(ref() is None for ref in held)
