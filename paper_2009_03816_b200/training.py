@@ -29,8 +29,10 @@ from __future__ import annotations
 import ctypes
 import math
 import threading
+import weakref
 
 import torch
+from torch.multiprocessing.reductions import StorageWeakRef
 
 from . import binding
 from .binding import (PSOPS_ATTENTION_GRADS, PSOPS_BF16, PSOPS_GELU, PSOPS_RELU, PSOPS_SILU, PSOPS_EINVAL, PSOPS_ESTATE, PSOPS_F16, PSOPS_F32, PSOPS_MEAN, PSOPS_NONE,
@@ -788,26 +790,44 @@ class Keep8(_Holder):
     def hooks(self, least=4096):
         """A context in which autograd keeps the 16-bit tensors that it saves in 8 bits: those of `least` elements or
         more on this GPU, but for leaves that have gradients (weights) and views of them, which are there anyway, and
-        for what Attention and LinearXent save, whose statistics belong to the numbers as they are."""
+        for what Attention and LinearXent save, whose statistics belong to the numbers as they are.  A tensor that
+        several operations save is kept once, as long as nothing writes to it in between that autograd does not see
+        (through .data, say)."""
+        kept_now = weakref.WeakValueDictionary()       # what graphs hold, by where it came from
+
         def pack(t):
             base = t._base if t._is_view() else t
             if _exactly.depth or t.get_device() != self.device.index or t.dtype not in (torch.float16, torch.bfloat16) or \
                     t.numel() < max(1, least) or t.dim() < 1 or base.is_leaf and base.requires_grad:
                 return _AsItIs(t)
-            with torch.no_grad():
-                codes, scales = self.pack(self._fitting(t.detach()))
-                self._join()
-            return codes, scales, t.shape, t.dtype
+            # a weak reference: no other storage is known by its number as long as there is one
+            source = StorageWeakRef(t.untyped_storage())
+            now = None if t.get_device() < 0 else (torch._C._cuda_getCurrentRawStream(t.get_device()), torch.cuda.is_current_stream_capturing())
+            key = source.cdata, t.storage_offset(), t.shape, t.stride(), t.dtype, t._version, now
+            kept = kept_now.get(key)
+            if kept is None:
+                with torch.no_grad():
+                    codes, scales = self.pack(self._fitting(t.detach()))
+                    self._join()
+                kept = kept_now[key] = _InCodes(codes, scales, t.shape, t.dtype, source)
+            return kept
 
         def unpack(kept):
             if isinstance(kept, _AsItIs):
                 return kept.get()
             with torch.no_grad():
-                x = self.unpack(*kept)
+                x = self.unpack(kept.codes, kept.scales, kept.shape, kept.dtype)
                 self._join()
             return x
 
         return torch.autograd.graph.saved_tensors_hooks(pack, unpack)
+
+
+class _InCodes:
+    """A tensor that Keep8.hooks keeps in 8 bits."""
+
+    def __init__(self, codes, scales, shape, dtype, source):
+        self.codes, self.scales, self.shape, self.dtype, self.source = codes, scales, shape, dtype, source
 
 
 class _AsItIs:

@@ -68,3 +68,20 @@ def test_a_weight_stepped_too_early_is_noticed(keep):
     opt.step(1e-3)
     with pytest.raises(RuntimeError, match="modified by an inplace"):
         y.backward()
+
+
+def test_what_one_input_of_three_products_takes(keep):
+    """1.03 bytes an element, not three times that."""
+    rows, width = 4096, 1024
+    x = torch.empty(rows, width, dtype=BF16, device="cuda").normal_().requires_grad_()
+    ws = [(torch.randn(width, 16, device="cuda") / 32).to(BF16).requires_grad_() for _ in range(3)]
+    sum((x * 1.0 @ w).float().sum() for w in ws).backward()          # the products' own workspaces
+    with keep.hooks():
+        h = x * 1.0
+        before = torch.cuda.memory_allocated()
+        y = sum((h @ w).float().sum() for w in ws)
+        held = torch.cuda.memory_allocated() - before
+    exact = rows * width + 4 * rows * width // 128
+    assert exact <= held < 1.1 * exact + 3 * rows * 16 * 4 * 3, (held, exact)
+    del h
+    y.backward()

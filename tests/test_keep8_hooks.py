@@ -88,3 +88,50 @@ def test_results_that_are_left_alone_are_freed(keep, dtype):
         del x, y
     gc.collect()
     assert all(ref() is None for ref in held)
+
+
+def test_one_tensor_is_kept_once(keep):
+    """However many operations save it; what has changed in between is another tensor, and so are other views."""
+    x = some(100, 64).requires_grad_() * 1.0
+    ws = [some(64, 64, seed=i).requires_grad_() for i in range(3)]
+    with keep.hooks():
+        y = sum((x @ w).float().sum() for w in ws)
+        assert keep.packed == [(100, 64)]
+        y.backward()
+    want = x.detach().T @ torch.ones(100, 64, dtype=torch.bfloat16)
+    for w in ws:
+        torch.testing.assert_close(w.grad, want)
+    keep.packed.clear()
+    leaf = some(2, 50, 64).requires_grad_()
+    with keep.hooks():
+        t = leaf * 1.0
+        y = sum((t @ w).float().sum() for w in ws)                   # a view of t each time
+        assert len(keep.packed) == 1
+        u = t * t                                                    # another shape
+        assert len(keep.packed) == 2
+        old = t @ ws[0]
+        with torch.no_grad():
+            t.mul_(2.0)
+        new = t @ ws[0]
+        assert len(keep.packed) == 3
+    del u, y
+    ws[0].grad = None
+    (old + new).float().sum().backward()
+    ones = torch.ones(100, 64, dtype=torch.bfloat16)
+    kept = leaf.detach().reshape(100, 64)
+    torch.testing.assert_close(ws[0].grad, (kept.T @ ones) + (2 * kept).T @ ones, rtol=2e-2, atol=1e-1)
+
+
+def test_nothing_outlives_its_graph(keep):
+    """Once the graphs that hold them are gone, the codes are; another tensor at the same place is another tensor."""
+    w = some(64, 64).requires_grad_()
+    context = keep.hooks()
+    for i in range(20):
+        x = some(100, 64, seed=i).requires_grad_() * 1.0
+        with context:
+            y = (x @ w).sum()
+        w.grad = None
+        y.backward()
+        torch.testing.assert_close(w.grad, x.detach().T @ torch.ones(100, 64, dtype=torch.bfloat16))
+        del x, y
+    assert len(keep.packed) == 20
