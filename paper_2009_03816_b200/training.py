@@ -789,16 +789,15 @@ class Keep8(_Holder):
 
     def hooks(self, least=4096):
         """A context in which autograd keeps the 16-bit tensors that it saves in 8 bits: those of `least` elements or
-        more on this GPU, but for leaves that have gradients (weights) and views of them, which are there anyway, and
-        for what Attention and LinearXent save, whose statistics belong to the numbers as they are.  A tensor that
+        more on this GPU, but for leaves that have gradients (weights), views of them, which are there anyway, and casts
+        of them, which are weights all the same, and for what Attention and LinearXent save, whose statistics belong to the numbers as they are.  A tensor that
         several operations save is kept once, as long as nothing writes to it in between that autograd does not see
         (through .data, say)."""
         kept_now = weakref.WeakValueDictionary()       # what graphs hold, by where it came from
 
         def pack(t):
-            base = t._base if t._is_view() else t
             if _exactly.depth or t.get_device() != self.device.index or t.dtype not in (torch.float16, torch.bfloat16) or \
-                    t.numel() < max(1, least) or t.dim() < 1 or base.is_leaf and base.requires_grad:
+                    t.numel() < max(1, least) or t.dim() < 1 or _is_of_a_leaf(t):
                 return _AsItIs(t)
             # a weak reference: no other storage is known by its number as long as there is one
             source = StorageWeakRef(t.untyped_storage())
@@ -821,6 +820,23 @@ class Keep8(_Holder):
             return x
 
         return torch.autograd.graph.saved_tensors_hooks(pack, unpack)
+
+
+# Operations whose result is their input in another type or seen in another way.
+_SAME_NUMBERS = frozenset(f"{name}Backward0" for name in (
+    "ToCopy", "View", "UnsafeView", "ReshapeAlias", "AsStrided", "T", "Transpose", "Permute", "Select", "Slice", "Split", "SplitWithSizes", "Unbind",
+    "Squeeze", "Unsqueeze", "Alias"))
+
+
+def _is_of_a_leaf(t):
+    """Whether this is a leaf that has gradients, a view or a cast of one."""
+    base = t._base if t._is_view() else t
+    if base.is_leaf:
+        return base.requires_grad
+    node = t.grad_fn
+    while node is not None and node.name() in _SAME_NUMBERS:
+        node = node.next_functions[0][0]
+    return node is not None and node.name() == "torch::autograd::AccumulateGrad"
 
 
 class _InCodes:

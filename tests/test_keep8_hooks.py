@@ -135,3 +135,21 @@ def test_nothing_outlives_its_graph(keep):
         torch.testing.assert_close(w.grad, x.detach().T @ torch.ones(100, 64, dtype=torch.bfloat16))
         del x, y
     assert len(keep.packed) == 20
+
+
+def test_casts_of_weights_are_left_alone(keep):
+    """A master weight in fp32 that is cast for each product, as autocast does too."""
+    w = some(64, 128, dtype=torch.float32).requires_grad_()
+    x = some(100, 64, seed=1).requires_grad_()
+    with keep.hooks():
+        h = x * 1.0
+        y = h @ w.bfloat16()
+        z = y @ w.to(torch.bfloat16).t()
+        assert keep.packed == [(100, 64), (100, 128)]
+    z.sum().backward()
+    keep.packed.clear()
+    with keep.hooks(), torch.autocast("cpu", dtype=torch.bfloat16):
+        h = torch.tanh(torch.nn.functional.linear(x * 1.0, w.t()))
+        h = torch.nn.functional.linear(h, w)
+    assert (128, 64) not in keep.packed and (64, 128) not in keep.packed and (100, 128) in keep.packed
+    h.sum().backward()
