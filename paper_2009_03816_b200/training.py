@@ -788,16 +788,18 @@ class Keep8(_Holder):
         return _Keep8Function.apply(self._fitting(a), self._fitting(b), kind, self)
 
     def hooks(self, least=4096):
-        """A context in which autograd keeps the 16-bit tensors that it saves in 8 bits: those of `least` elements or
-        more on this GPU, but for leaves that have gradients (weights), views of them, which are there anyway, and casts
-        of them, which are weights all the same, and for what Attention and LinearXent save, whose statistics belong to the numbers as they are.  A tensor that
-        several operations save is kept once, as long as nothing writes to it in between that autograd does not see
-        (through .data, say)."""
+        """A context in which autograd keeps the 16-bit tensors that it saves in 8 bits, those of `least` elements or
+        more on this GPU.  Left alone are leaves that have gradients (weights), views of them, which are there anyway,
+        and casts of them, which are weights all the same; broadcast tensors, which take less room as they are; and
+        what Attention and LinearXent save, whose statistics belong to the numbers as they are.  A tensor that several
+        operations save is kept once, as long as nothing writes to it in between that autograd does not see (through
+        .data, say)."""
         kept_now = weakref.WeakValueDictionary()       # what graphs hold, by where it came from
 
         def pack(t):
             if _exactly.depth or t.get_device() != self.device.index or t.dtype not in (torch.float16, torch.bfloat16) or \
-                    t.numel() < max(1, least) or t.dim() < 1 or _is_of_a_leaf(t):
+                    t.numel() < max(1, least) or t.dim() < 1 or _is_of_a_leaf(t) or \
+                    any(n > 1 and ld == 0 for n, ld in zip(t.shape, t.stride())):
                 return _AsItIs(t)
             # a weak reference: no other storage is known by its number as long as there is one
             source = StorageWeakRef(t.untyped_storage())

@@ -153,3 +153,13 @@ def test_casts_of_weights_are_left_alone(keep):
         h = torch.nn.functional.linear(h, w)
     assert (128, 64) not in keep.packed and (64, 128) not in keep.packed and (100, 128) in keep.packed
     h.sum().backward()
+
+
+def test_broadcast_tensors_are_left_alone(keep):
+    """Their codes would take more room than they do."""
+    row = some(1, 128, seed=2).requires_grad_() * 1.0
+    x = some(100, 128).requires_grad_() * 1.0
+    with keep.hooks():
+        y = x * row.expand(100, 128)
+        assert keep.packed == [(100, 128)]
+    y.sum().backward()
