@@ -191,8 +191,8 @@ __device__ __forceinline__ uint64_t mul_both(uint64_t a, uint64_t b)
 // 2^x of two numbers without the special-function unit, which has 16 results a clock
 // where a tile of products of dim 128 takes 16 scores a clock: 2^n times a
 // polynomial for 2^f, f in [-1/2, 1/2] (least largest relative error at degree 5, by
-// Remez's exchange: 1.5e-7 with these coefficients).  Below 2^-126 it is zero; NaN
-// stays NaN.
+// Remez's exchange: 1.6e-7 with these coefficients, 2.2e-7 evaluated in fp32).
+// Below 2^-126 it is zero; NaN stays NaN.
 __device__ __forceinline__ uint64_t exp2_both(uint64_t x)
 {
     float a = low_of(x), b = high_of(x);
@@ -209,12 +209,11 @@ __device__ __forceinline__ uint64_t exp2_both(uint64_t x)
     p = fma_both(p, f, both(1.0f));
     return mul_both(p, pair_of(((uint32_t)t << 23) + 0x3f800000u, ((uint32_t)(t >> 32) << 23) + 0x3f800000u));
 }
-// Two probabilities; every OWN-th pair of a row by the polynomial (0: none).
+// Two probabilities; every OWN-th of 16 pairs by the polynomial.
 template <int OWN>
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t x, int i)
 {
-    if constexpr (OWN > 0)
-        if (i % OWN == OWN - 1) return exp2_both(x);
+    if (i % OWN == OWN - 1) return exp2_both(x);
     return pair_of(__float_as_uint(exp2_fast(low_of(x))), __float_as_uint(exp2_fast(high_of(x))));
 }
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -830,8 +829,8 @@ __device__ __forceinline__ void forward_rows(const ForwardParams &P, ForwardShar
     constexpr int kTileBytes = HALVES * kHalfBytes;
     constexpr bool kAhead = HALVES == 1;
     constexpr int kStages = kAhead ? 2 : 1;
-    // of 8,192 tokens: dim 64 every 4th pair 221 us, 8th 206, 12th 213, none 225; dim 128 271, 263, none 252
-    constexpr int kOwn = kAhead ? 8 : 0;
+    // of 16 pairs, 8,192 tokens, 16 heads: dim 64 four 208 us, two 199, one 215, none 220; dim 128 two 258, the 12th 254, the last 259, none 265
+    constexpr int kOwn = kAhead ? 8 : 12;
     // fp16 has no numbers below 2^-24: probabilities, at most 2^kLazy, are kept higher up
     constexpr float kShift = kBf16 ? 0.0f : 7.0f;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -1336,7 +1335,7 @@ __device__ __forceinline__ void backward_part(const CUtensorMap &map_a0, const C
 {
     constexpr bool kBf16 = __is_same(T, __nv_bfloat16);
     constexpr int kTileBytes = HALVES * kHalfBytes;
-    constexpr int kOwn = 4;                  // queries and keys of 8,192 tokens, 16 heads x 64: 784 us, 8th pair 789, none 813
+    constexpr int kOwn = 4;                  // queries and keys of 8,192 tokens, 16 heads x 64: 780 us, every 8th pair 800, none 808
     // scores in two places by turns, where tensor memory has room for them: the next ones need not wait for these
     constexpr bool kTwice = KEYS && HALVES == 1;
     constexpr uint32_t kSecond = 3 * kTile;                                 // columns 384 to 511

@@ -140,3 +140,35 @@ def test_beside_infinities():
     shift[0, 30:] = -1e9 + FAR
     small[4, 0] = held[4, 0] = -torch.inf
     check([300, 9, 1], F16, 64, held, small, shift)
+
+
+@pytest.mark.parametrize("lengths", [[100, 60], [700, 300, 2] * 20], ids=["few tiles", "many"])
+def test_levels_that_come_and_go_in_a_graph(lengths):
+    """What a table asks for is found on the device: a recorded pass is right for the tables of all its replays."""
+    T = sum(lengths)
+    x = inputs(T, 4, 2, 64, BF16, 1)
+    bias, offsets = table(F32), lengths_to_offsets(lengths)
+    op = training.Attention(T, len(lengths), 4, 2, 64, buckets=BUCKETS)
+
+    def both(op):
+        out, lse = op.forward(x["q"], x["k"], x["v"], offsets, bias)
+        return (out, lse, *op.backward(x["q"], x["k"], x["v"], offsets, out, lse, x["grad"], bias))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both(op)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        held = both(op)
+    for seed, level in ((1, None), (2, -1e9), (3, None), (4, 1e6)):
+        bias.copy_(table(F32, seed=seed))
+        if level is not None:
+            bias[:2, 1:] = level
+        graph.replay()
+        torch.cuda.synchronize()
+        fresh = training.Attention(T, len(lengths), 4, 2, 64, buckets=BUCKETS)
+        for a, b in zip(held, both(fresh)):
+            assert torch.equal(a, b), (seed, level)
+        fresh.close()
