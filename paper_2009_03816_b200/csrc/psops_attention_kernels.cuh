@@ -553,11 +553,11 @@ struct Tables {
     float level[kMostBuckets];               // LEVELS: of rows whose position is in a bucket
     int first[kMostBuckets];
     uint8_t bucket[kMostDistance + 2 * kTile];
-    float distance[kTableFloats];            // [kBefore + d]: the bias of distance d, base 2
+    float distance[kTableFloats];            // [kBefore + d]: the bias of distance d, as in `value`
 
     __device__ __forceinline__ float level_at(const Bias &B, int position) const { return level[bucket[min(position, B.last)]]; }
-    // the bias of distance d beside a level, base 2; of distances below 0 any number
-    __device__ __forceinline__ float beside(int d, float level) const { return (value[bucket[max(d, 0)]] - level) * kLog2e; }
+    // LEVELS: the bias of distance d beside a level, base 2; of distances below 0 any number
+    __device__ __forceinline__ float beside(int d, float level) const { return (distance[kBefore + d] - level) * kLog2e; }
 };
 // By one warp, two buckets a lane: running maxima over the buckets.
 __device__ __noinline__ void make_levels(Tables &t, int buckets)
@@ -595,7 +595,7 @@ __device__ __forceinline__ void make_tables(const Bias &B, Tables &t, float mine
         } else {
             bucket = t.bucket[d];
         }
-        if (!LEVELS) t.distance[kBefore + d] = t.value[bucket];
+        t.distance[kBefore + d] = t.value[bucket];
     }
     barrier_named(1, THREADS);
 }
