@@ -429,7 +429,7 @@ class Attention(_Holder):
     q is tokens x heads x dim, k and v are tokens x kv_heads x dim, with consecutive elements in each head and rows on
     multiples of 16 bytes (views of one projection's output, for instance); `offsets` (int32, on the GPU, one more than
     there are sequences) has each sequence's first token, and behind the last one its end; `bias` is buckets x heads, fp32
-    or of q's type.  Rows of no sequence are zeros in results that a call makes, and left as they were in given ones.
+    or of q's type, of any finite size, and -inf takes its pairs out.  Rows of no sequence are zeros in results that a call makes, and left as they were in given ones.
     Calling the object gives the output as a torch value with gradients (of the first order)::
 
         out = attention(q, k, v, offsets, bias)
@@ -784,7 +784,8 @@ class Keep8(_Holder):
         return t.contiguous()
 
     def __call__(self, a, b=None, kind="silu"):
-        """f(a), or f(a) * b, with gradients.  Here a and b may have any strides."""
+        """f(a), or f(a) * b, with gradients.  Here a and b may have any strides.  The result is kept by what uses it, as
+        any tensor is (in 8 bits under hooks()); activate and activate_backward with `again` do without that."""
         return _Keep8Function.apply(self._fitting(a), self._fitting(b), kind, self)
 
     def hooks(self, least=4096):
