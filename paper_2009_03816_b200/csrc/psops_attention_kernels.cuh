@@ -1049,7 +1049,7 @@ psops_attention_forward_kernel(const __grid_constant__ CUtensorMap map_q, const 
     __shared__ ForwardShared<HALVES, BIAS> M;
     __shared__ uint32_t tensor_base_slot;
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5;
     volatile int *failed = &M.failed;
     uint8_t *tiles = raw + (((umma::shared_address(raw) + 1023u) & ~1023u) - umma::shared_address(raw));
     const uint32_t q_at = umma::shared_address(tiles), k_at = q_at + kStages * kTileBytes, v_at = k_at + kStages * kTileBytes;
